@@ -322,6 +322,82 @@ int mx_gemm_hw(const bdr_config_t* cfg_a /*host*/, const bdr_planes_t* a /*host 
                const bdr_config_t* cfg_b /*host*/, const bdr_planes_t* b /*host struct*/, int64_t M, int64_t N,
                int64_t K, int r, int f, float* c, int64_t ldc, void* stream);
 
+/* ---- Serving ------------------------------------------------------------------------------------------------
+ * Token-by-token inference on MX storage (Section V, inferencing): products of a few activations with packed
+ * weights, a key-value cache kept in the MX format, and the attention of one new token over it.  These calls take
+ * the Table II formats with ties to even (k1 = 16, k2 = 2, d2 = 1, m in {2, 4, 7}); anything else is
+ * BDR_ERR_UNSUPPORTED.  Blocks with the exponent byte 0xFF (Inf/NaN) decode to NaN; blocks with the exponent byte 0
+ * (zeros and values below 2^-126) decode to zero. */
+
+/* y[T,N] (row pitch ldy) = x[T,K] (row pitch ldx) deq(W)[N,K]^T for a few rows of x and weights packed along K (axis-1
+ * planes of W).  The activations are used as they are: bf16 values enter the tensor core unchanged, fp32 values as the
+ * exact sum of three bf16 parts; accumulation is fp32 and the result is rounded once to y's type.  Only the summation
+ * order is unspecified (it depends on the shape, not on the run).  Any N, K and T (K = 0 gives zeros); W is read once
+ * for every 64 rows of bf16 x, or 21 rows of fp32 x, so larger T belongs to mx_gemm_ws.  Rows of x that are 16-byte
+ * aligned are read faster. */
+int mx_gemv(const bdr_config_t* cfg_w /*host*/, const bdr_planes_t* w /*host struct*/, int64_t N, int64_t K, const void* x,
+            bdr_dtype_t x_dt, int64_t ldx, int64_t T, void* y, bdr_dtype_t y_dt, int64_t ldy, void* stream);
+
+/* A paged key-value cache in MX format.  A slot is one token's line of n_kv * head_dim elements; the planes of keys and of
+ * values are axis-1 planes of [n_pages * page_size, n_kv * head_dim] tensors (sizes and pitches: bdr_packed_sizes), so
+ * bdr_unpack and bdr_gather_rows read a cache as they read any packed tensor.  Slot = page * page_size + offset.  Blocks
+ * run along the head dimension (the reduction dimension of the scores; values are stored the same way so that a token
+ * can be appended without touching its neighbours).  head_dim: a multiple of 16 up to 256; any page_size;
+ * n_pages * page_size < 2^31 - 64.  The two formats may differ. */
+typedef struct {
+    bdr_config_t cfg_k, cfg_v;
+    bdr_planes_t k, v;
+    int64_t n_pages;
+    int32_t page_size, n_kv, head_dim;
+} mx_kv_cache_t;
+
+/* Rotary positions: cos and sin are [n_pos, ld] fp32 tables (device) with one angle per pair in the first rot_dim / 2
+ * columns, positions[t] (int64, device) the row of token t.  Pairs are (i, i + rot_dim / 2) of a head's first rot_dim elements, or
+ * (2i, 2i + 1) when interleaved != 0; the elements beyond rot_dim stay as they are. */
+typedef struct {
+    const float *cos, *sin;
+    const int64_t* positions;
+    int64_t ld, n_pos;
+    int32_t rot_dim, interleaved;
+} mx_rotation_t;
+
+/* Appends n_tokens tokens to the cache.  k and v are [n_tokens, n_kv, head_dim] of `dt` with token pitches ldk and ldv
+ * (elements; a token's heads are contiguous, so slices of a fused projection's output work).  Every key head is rotated (rot ==
+ * NULL: not at all), (a, b) -> (a cos - b sin, b cos + a sin), each product and each sum rounded to fp32; the fp32 result
+ * is quantized without an intermediate rounding to `dt`, and the lines of slot slots[t] (int64, device) are written in
+ * both caches, every byte up to the pitch, exactly as bdr_pack would.  slots[t] < 0 marks a padding token: nothing is
+ * stored for it.  Slots of one call must differ.
+ *   q, q_out    NULL, or queries [n_tokens, n_q, head_dim] (pitch ldq) and where to put them rotated and rounded to `dt`
+ *               (pitch ldq_out; not the same memory as q)
+ *   k_dq, v_dq  NULL, or contiguous 16-byte aligned [n_tokens, n_kv, head_dim] tensors of `dt` for the values that the cache
+ *               now stands for (for attention within a prompt, say); written for padding tokens too
+ * A slot >= n_pages * page_size, or a position outside [0, n_pos), is seen on the device only: nothing is stored for that
+ * token, BDR_ERR_SIZE is left in the sticky word of bdr_device_status, and a bad position also makes the token's rotated
+ * outputs NaN. */
+int mx_kv_append(const mx_kv_cache_t* cache /*host*/, const void* k, int64_t ldk, const void* v, int64_t ldv, bdr_dtype_t dt,
+                 int64_t n_tokens, const int64_t* slots, const mx_rotation_t* rot /*host*/, const void* q, int64_t ldq, int32_t n_q,
+                 void* q_out, int64_t ldq_out, void* k_dq, void* v_dq, void* stream);
+
+/* Attention of one new token per sequence over its cached keys and values:
+ *     out[s, h] = sum_t p_t V[t, h / (n_q / n_kv)],  p = softmax_t(scale * <q[s, h], K[t, h / (n_q / n_kv)]>)
+ * over the positions t < lengths[s] (int32, device; the new token's own key counts once it has been appended), or only the last
+ * `window` of them when window > 0.  Position t of sequence s lives in page page_table[s, t / page_size] (int32, device, row pitch
+ * ld_table >= max_pages).  Positions outside the range are never read, whatever the pages hold there.
+ *   q, out   [n_seqs, n_q, head_dim] of `dt` with sequence pitches ldq and ldo; n_q a multiple of n_kv
+ *   lse      NULL, or [n_seqs, n_q] fp32 (contiguous): log of the sum of exp(scale <q, k>), for joining with attention over other
+ *            positions.  A sequence without positions gives out = 0 and lse = -infinity.
+ * Scores, softmax statistics and sums are fp32.  bf16 queries: the softmax weights enter the second product rounded to bf16
+ * (their sum is taken before that rounding); fp32 queries: both enter as sums of bf16 parts, which keeps 16 bits of the
+ * weights and all of the queries.  The cache is split over its length across the GPU and the parts are joined in a fixed
+ * order: the result does not change from run to run.  workspace: 16-byte aligned device scratch of at least
+ * mx_attn_decode_workspace_bytes(cache, n_seqs, n_q) bytes, contents overwritten.
+ * A page id outside [0, n_pages) or a length beyond max_pages * page_size is seen on the device only: the sequence's outputs
+ * are NaN and BDR_ERR_SIZE is left in the sticky word of bdr_device_status.  A negative length counts as zero. */
+int64_t mx_attn_decode_workspace_bytes(const mx_kv_cache_t* cache /*host*/, int64_t n_seqs, int32_t n_q);
+int mx_attn_decode(const mx_kv_cache_t* cache /*host*/, const void* q, int64_t ldq, bdr_dtype_t dt, int64_t n_seqs, int32_t n_q,
+                   const int32_t* page_table, int64_t ld_table, int64_t max_pages, const int32_t* lengths, float scale, int32_t window,
+                   void* out, int64_t ldo, float* lse, void* workspace, int64_t workspace_bytes, void* stream);
+
 /* BDR_OK, or BDR_ERR_TIMEOUT if any mx_gemm launch on the current device gave up a bounded wait
  * (sticky).  Host call; synchronises with the device (it copies one word back). */
 int mx_gemm_status(void);

@@ -22,7 +22,8 @@ F32, BF16 = 0, 1
 EXPORTS = ("bdr_strerror", "bdr_device_status", "bdr_packed_sizes", "bdr_quant_dequant", "bdr_pack", "bdr_unpack",
            "bdr_qsnr_workspace_bytes", "bdr_qsnr", "bdr_qsnr_static_max_cfgs", "bdr_qsnr_static", "mx_gemm",
            "mx_gemm_workspace_bytes", "mx_gemm_ws", "mx_gemm_f8_workspace_bytes", "mx_gemm_f8", "bdr_reencode_e4m3", "mx_gemm_e4m3", "bdr_set_workspace",
-           "mx_gemm_status", "bdr_selftest_bounded_wait", "bdr_selftest_host", "bdr_qsnr_from_sums", "bdr_pack2", "bdr_qsnr_delayed", "bdr_amax", "bdr_tile_packing_efficiency", "mx_gemm_hw", "bdr_gather_rows", "bdr_device_status_reset", "bdr_quant_dequant_parent")
+           "mx_gemm_status", "bdr_selftest_bounded_wait", "bdr_selftest_host", "bdr_qsnr_from_sums", "bdr_pack2", "bdr_qsnr_delayed", "bdr_amax", "bdr_tile_packing_efficiency", "mx_gemm_hw", "bdr_gather_rows", "bdr_device_status_reset", "bdr_quant_dequant_parent",
+           "mx_gemv", "mx_kv_append", "mx_attn_decode", "mx_attn_decode_workspace_bytes")
 
 
 class BdrError(RuntimeError):
@@ -38,6 +39,16 @@ class _Config(C.Structure):
 class _Planes(C.Structure):
     _fields_ = [("exps", C.c_void_p), ("micro", C.c_void_p), ("elems", C.c_void_p),
                 ("ld_exps", C.c_int64), ("ld_micro", C.c_int64), ("ld_elems", C.c_int64)]
+
+
+class _KVCache(C.Structure):
+    _fields_ = [("cfg_k", _Config), ("cfg_v", _Config), ("k", _Planes), ("v", _Planes), ("n_pages", C.c_int64),
+                ("page_size", C.c_int32), ("n_kv", C.c_int32), ("head_dim", C.c_int32)]
+
+
+class _Rotation(C.Structure):
+    _fields_ = [("cos", C.c_void_p), ("sin", C.c_void_p), ("positions", C.c_void_p), ("ld", C.c_int64), ("n_pos", C.c_int64),
+                ("rot_dim", C.c_int32), ("interleaved", C.c_int32)]
 
 
 @dataclass(frozen=True)
@@ -71,6 +82,33 @@ class Planes:
         return _Planes(self.exps.data_ptr(), self.micro.data_ptr() if self.micro.numel() else None,
                        self.elems.data_ptr(), self.exps.stride(0), self.micro.stride(0) if self.micro.numel() else 0,
                        self.elems.stride(0))
+
+
+@dataclass
+class KVCache:
+    """mx_kv_cache_t: a paged key-value cache in MX format.  `k` and `v` are axis-1 planes of [n_pages * page_size,
+    n_kv * head_dim] tensors; the object keeps them alive and is described to the library once, when it is made."""
+    cfg_k: Config
+    cfg_v: Config
+    k: Planes
+    v: Planes
+    n_pages: int
+    page_size: int
+    n_kv: int
+    head_dim: int
+
+    def __post_init__(self):
+        for p in (self.k, self.v):
+            for t in (p.exps, p.micro, p.elems):
+                if t.dtype != torch.uint8 or t.dim() != 2 or t.stride(1) != 1 or t.shape[0] < self.n_pages * self.page_size:
+                    raise ValueError("cache planes are uint8 [n_pages * page_size, pitch] tensors")
+        self._c = _KVCache(self.cfg_k.c(), self.cfg_v.c(), self.k.c(), self.v.c(), self.n_pages, self.page_size, self.n_kv, self.head_dim)
+        self._ref = C.addressof(self._c)
+
+
+def alloc_kv_cache(cfg_k: Config, cfg_v: Config, n_pages: int, page_size: int, n_kv: int, head_dim: int, device="cuda") -> KVCache:
+    planes = [alloc_planes(cfg, n_pages * page_size, n_kv * head_dim, 1, device) for cfg in (cfg_k, cfg_v)]
+    return KVCache(cfg_k, cfg_v, planes[0], planes[1], n_pages, page_size, n_kv, head_dim)
 
 
 _lib = None
@@ -151,6 +189,15 @@ def lib():
         L.bdr_selftest_host.argtypes = []
         L.bdr_qsnr_from_sums.restype = C.c_int
         L.bdr_qsnr_from_sums.argtypes = [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p]
+        i32, i64, ptr = C.c_int32, C.c_int64, C.c_void_p
+        L.mx_gemv.restype = C.c_int
+        L.mx_gemv.argtypes = [ptr, ptr, i64, i64, ptr, C.c_int, i64, i64, ptr, C.c_int, i64, ptr]
+        L.mx_kv_append.restype = C.c_int
+        L.mx_kv_append.argtypes = [ptr, ptr, i64, ptr, i64, C.c_int, i64, ptr, ptr, ptr, i64, i32, ptr, i64, ptr, ptr, ptr]
+        L.mx_attn_decode_workspace_bytes.restype = C.c_int64
+        L.mx_attn_decode_workspace_bytes.argtypes = [ptr, i64, i32]
+        L.mx_attn_decode.restype = C.c_int
+        L.mx_attn_decode.argtypes = [ptr, ptr, i64, C.c_int, i64, i32, ptr, i64, i64, ptr, C.c_float, i32, ptr, i64, ptr, ptr, i64, ptr]
         for fn in (L.bdr_packed_sizes, L.bdr_quant_dequant, L.bdr_pack, L.bdr_unpack, L.bdr_qsnr, L.mx_gemm):
             fn.restype = C.c_int
         _lib = L
@@ -400,6 +447,101 @@ def mx_gemm_e4m3(a: torch.Tensor, scales_a: torch.Tensor, b: torch.Tensor, scale
     _check(lib().mx_gemm_e4m3(_ptr(a), _ptr(scales_a), _ptr(b), _ptr(scales_b), M, N, K, _ptr(c), c.stride(0), _stream(stream)),
            "mx_gemm_e4m3")
     return c
+
+
+def _on_gpu(*tensors):
+    for t in tensors:
+        if t is not None and not t.is_cuda:
+            raise ValueError("expected CUDA tensors")
+
+
+def mx_gemv(cfg_w: Config, w: Planes, N: int, K: int, x: torch.Tensor, y: torch.Tensor, stream=None) -> torch.Tensor:
+    """y[T,N] = x[T,K] @ deq(w)[N,K]^T for a few rows of x (float32 or bfloat16; y likewise) and weights packed along K."""
+    x2, y2 = _as2d(x), _as2d(y)
+    _on_gpu(x, y, w.exps, w.micro, w.elems)
+    if x2.shape[1] != K or y2.shape != (x2.shape[0], N) or min(w.exps.shape[0], w.micro.shape[0], w.elems.shape[0]) < N:
+        raise ValueError("x is [T, K], y is [T, N] and the planes hold N lines")
+    c, p = cfg_w.c(), w.c()
+    _check(lib().mx_gemv(C.addressof(c), C.addressof(p), N, K, x2.data_ptr(), _dt(x2), max(x2.stride(0), K), x2.shape[0], y2.data_ptr(),
+                         _dt(y2), max(y2.stride(0), N), _stream(stream)), "mx_gemv")
+    return y
+
+
+def _heads(t: torch.Tensor, what: str):
+    """Pitch of a [tokens, heads, head_dim] tensor whose tokens are contiguous."""
+    if t.dim() != 3 or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+        raise ValueError("%s: expected [tokens, heads, head_dim] with contiguous heads" % what)
+    return max(t.stride(0), t.shape[1] * t.shape[2])
+
+
+def mx_kv_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, positions: torch.Tensor | None = None,
+                 cos: torch.Tensor | None = None, sin: torch.Tensor | None = None, interleaved: bool = False,
+                 q: torch.Tensor | None = None, q_out: torch.Tensor | None = None, k_dq: torch.Tensor | None = None,
+                 v_dq: torch.Tensor | None = None, stream=None) -> KVCache:
+    """Rotates the keys k [T, n_kv, head_dim] (cos, sin: float32 [n_pos, rot_dim / 2] tables, positions: int64 [T]; None: no
+    rotation), quantizes them and v, and writes the lines of `slots` (int64 [T], negative = padding).  Optionally rotates the
+    queries q into q_out and returns the quantized values in k_dq / v_dq."""
+    T = k.shape[0]
+    _on_gpu(k, v, slots, positions, cos, sin, q, q_out, k_dq, v_dq, cache.k.elems)
+    shape = (T, cache.n_kv, cache.head_dim)
+    if k.shape != shape or v.shape != shape or v.dtype != k.dtype:
+        raise ValueError("k and v are [tokens, n_kv, head_dim] of one dtype")
+    if slots.dtype != torch.int64 or slots.shape != (T,) or not slots.is_contiguous():
+        raise ValueError("slots: contiguous int64 [tokens]")
+    rot = None
+    if cos is not None:
+        if sin is None or positions is None:
+            raise ValueError("cos, sin and positions go together")
+        if cos.dtype != torch.float32 or sin.dtype != torch.float32 or cos.dim() != 2 or cos.shape != sin.shape or cos.stride(1) != 1 or \
+                sin.stride() != cos.stride():
+            raise ValueError("cos, sin: float32 [n_pos, rot_dim / 2] with one pitch")
+        if positions.dtype != torch.int64 or positions.shape != (T,) or not positions.is_contiguous():
+            raise ValueError("positions: contiguous int64 [tokens]")
+        rot = _Rotation(cos.data_ptr(), sin.data_ptr(), positions.data_ptr(), max(cos.stride(0), cos.shape[1]), cos.shape[0],
+                        2 * cos.shape[1], int(interleaved))
+    n_q = ldq = ldo = 0
+    if q is not None:
+        if q_out is None or q_out.shape != q.shape or q_out.dtype != k.dtype or q.dtype != k.dtype or q.dim() != 3 or q.shape[0] != T or \
+                q.shape[2] != cache.head_dim:
+            raise ValueError("q and q_out are [tokens, n_q, head_dim] of k's dtype")
+        n_q, ldq, ldo = q.shape[1], _heads(q, "q"), _heads(q_out, "q_out")
+    for t in (k_dq, v_dq):
+        if t is not None and (t.shape != shape or t.dtype != k.dtype or not t.is_contiguous()):
+            raise ValueError("k_dq, v_dq: contiguous, like k")
+    _check(lib().mx_kv_append(cache._ref, k.data_ptr(), _heads(k, "k"), v.data_ptr(), _heads(v, "v"), _dt(k), T, slots.data_ptr(),
+                              C.addressof(rot) if rot is not None else None, q.data_ptr() if n_q else None, ldq, n_q,
+                              q_out.data_ptr() if n_q else None, ldo, k_dq.data_ptr() if k_dq is not None else None,
+                              v_dq.data_ptr() if v_dq is not None else None, _stream(stream)), "mx_kv_append")
+    return cache
+
+
+def mx_attn_decode_workspace_bytes(cache: KVCache, n_seqs: int, n_q: int) -> int:
+    return int(lib().mx_attn_decode_workspace_bytes(cache._ref, n_seqs, n_q))
+
+
+def mx_attn_decode(cache: KVCache, q: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, out: torch.Tensor,
+                   workspace: torch.Tensor, scale: float | None = None, window: int = 0, lse: torch.Tensor | None = None,
+                   stream=None) -> torch.Tensor:
+    """out [B, n_q, head_dim] = attention of one query token per sequence, q [B, n_q, head_dim], over the cached positions
+    t < lengths[b] (int32 [B]; the last `window` of them when window > 0) whose pages are page_table[b] (int32 [B, max_pages]).
+    lse: float32 [B, n_q].  scale: head_dim ** -0.5 when None."""
+    _on_gpu(q, page_table, lengths, out, workspace, lse, cache.k.elems)
+    B, n_q = q.shape[0], q.shape[1]
+    ldq, ldo = _heads(q, "q"), _heads(out, "out")
+    if q.shape[2] != cache.head_dim or out.shape != q.shape or out.dtype != q.dtype:
+        raise ValueError("q and out are [sequences, n_q, head_dim] of one dtype")
+    if page_table.dtype != torch.int32 or page_table.dim() != 2 or page_table.shape[0] != B or page_table.stride(1) != 1 and page_table.shape[1] > 1:
+        raise ValueError("page_table: int32 [sequences, max_pages]")
+    if lengths.dtype != torch.int32 or lengths.shape != (B,) or not lengths.is_contiguous():
+        raise ValueError("lengths: contiguous int32 [sequences]")
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (B, n_q) or not lse.is_contiguous()):
+        raise ValueError("lse: contiguous float32 [sequences, n_q]")
+    _check(lib().mx_attn_decode(cache._ref, q.data_ptr(), ldq, _dt(q), B, n_q, page_table.data_ptr(),
+                                max(page_table.stride(0), page_table.shape[1]), page_table.shape[1], lengths.data_ptr(),
+                                cache.head_dim ** -0.5 if scale is None else scale, window, out.data_ptr(), ldo,
+                                lse.data_ptr() if lse is not None else None, workspace.data_ptr(),
+                                workspace.numel() * workspace.element_size(), _stream(stream)), "mx_attn_decode")
+    return out
 
 
 def bdr_device_status() -> int:

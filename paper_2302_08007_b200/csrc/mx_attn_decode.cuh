@@ -1,0 +1,488 @@
+// Attention of one new token per sequence over a paged key-value cache in MX format (see mx_attn_decode in bdr.h).
+//
+// The cache is read once and every element of it is used for the few query heads that share it, so the bounds are the bytes
+// of the cache and the instructions that decode them.  A warp owns one "unit", a key-value head with its query heads (small
+// heads are merged until a unit fills 128 elements), and walks over tiles of 16 tokens:
+//   scores    S^T[16 tokens, 8 columns] = K[16, d] Q^T: the key blocks are decoded straight into the A fragment (lane (g, c)
+//             decodes whole blocks of tokens g and g + 8); Q waits in shared memory in the order of the B fragment;
+//   softmax   with a running reference per column instead of the running maximum: it is raised only when a score passes it
+//             by kSlack (in powers of two), so most tiles need a vote and no reduction over lanes;
+//   output    O^T[d, 8 columns] += V^T P^T: V is decoded like K (lane (g, c): block g of four tokens), a byte permutation pairs
+//             neighbouring tokens for the A fragment, and P^T is the 8x8 transpose of the score fragment.
+// The packed bytes of the next tile are fetched while the present one is computed: keys as soon as the scores are done,
+// values as soon as the output is.
+//
+// Work is split over the length of the cache: the tiles of all sequences form one long line that is cut into equal parts,
+// one per worker CTA, whatever the individual lengths are (each worker finds its part from `lengths`).  A part that covers a
+// sequence's whole range writes the result; other parts leave their sums and references in the workspace, where a second
+// kernel joins them in order.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "bdr_device.cuh"
+#include "bdr_host.h"
+#include "mx_frag.cuh"
+
+namespace bdr {
+
+constexpr int kAtThreads = 256, kAtWarps = kAtThreads / 32;
+constexpr float kAtSlack = 8.f;   // a softmax weight relative to the running reference stays below 2^8
+
+struct AttnArgs {
+    bdr_planes_t k, v;
+    const void* q;
+    void* out;
+    float* lse;
+    const int32_t *table, *lengths;
+    float* part_o;          // [worker][2][n_q][d]
+    float2* part_ml;        // [worker][2][n_q]: reference (base 2) and sum of weights
+    int64_t ldq, ldo, ld_table;
+    int n_seqs, n_q, n_kv, group, d, nb;   // group: query heads per key-value head; nb: blocks per head
+    int merge, per_pass, passes, n_units;  // key-value heads of a unit, query heads per pass of each, passes, units
+    int hw, tw, workers;                   // warps over units, warps over tokens, worker CTAs per group of units
+    int n_pages, max_pages, cap, window;   // cap = max_pages * page_size
+    FastDiv page;
+    float scale2;                          // 2 scale log2(e): the keys are decoded halved
+    int* status;
+};
+
+// Tiles of 16 tw tokens that sequence b's positions touch.
+struct SeqRange {
+    int start, end, first, count;
+};
+__device__ __forceinline__ SeqRange seq_range(const AttnArgs& a, int b) {
+    SeqRange r;
+    const int len = min(__ldg(a.lengths + b), a.cap + 1);  // a position beyond the table's pages poisons the result
+    r.end = max(len, 0);
+    r.start = a.window > 0 ? max(0, r.end - a.window) : 0;
+    const int mt = 16 * a.tw;
+    r.first = r.start / mt;
+    r.count = r.end > r.start ? (r.end + mt - 1) / mt - r.first : 0;
+    return r;
+}
+
+// Tiles of all sequences together (called by whole warps).
+__device__ __forceinline__ int64_t total_tiles(const AttnArgs& a, int lane) {
+    int64_t n = 0;
+    for (int b = lane; b < a.n_seqs; b += 32) n += seq_range(a, b).count;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(0xFFFFFFFFu, n, o);
+    return n;
+}
+
+// Tiles of the sequences before `limit`, stopping early before the sequence that holds tile `u` (u < 0: no such stop).
+// Returns the prefix and leaves the sequence in b.
+__device__ __forceinline__ int64_t walk_tiles(const AttnArgs& a, int lane, int limit, int64_t u, int& b) {
+    int64_t p = 0;
+    for (int base = 0;; base += 32) {
+        const int mine = base + lane;
+        int64_t n = mine < limit ? seq_range(a, mine).count : 0;
+        int64_t incl = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+            if (lane >= o) incl += v;
+        }
+        const int64_t all = __shfl_sync(0xFFFFFFFFu, incl, 31);
+        if (base + 32 >= limit || (u >= 0 && p + all > u)) {
+            if (u < 0) { b = limit; return p + all; }
+            const unsigned hit = __ballot_sync(0xFFFFFFFFu, p + incl > u);
+            const int at = hit ? __ffs(hit) - 1 : 31;
+            b = base + at;
+            return p + __shfl_sync(0xFFFFFFFFu, incl - n, at);
+        }
+        p += all;
+    }
+}
+
+__device__ __forceinline__ int64_t worker_begin(int64_t total, int w, int workers) { return total * w / workers; }
+
+__device__ __forceinline__ float exp2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
+    uint32_t d;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    return d;
+}
+
+// MAXB: blocks of a unit (8 or 16); NT: groups of eight columns (query heads); F32: 32-bit queries and results.
+template <int WK, int WV, int MAXB, int NT, bool F32>
+struct AttnShape {
+    static constexpr int kKeyBlocks = MAXB / 4, kValBlocks = MAXB / 8;  // per lane and token
+    static constexpr int kParts = F32 ? 3 : 1;
+    static constexpr int kD = 16 * MAXB;
+    static constexpr size_t kQBytes = (size_t)kParts * MAXB * NT * 32 * 8;          // per warp
+    static constexpr int kOPitch = kD + 4;
+    static constexpr size_t kOBytes = (size_t)8 * NT * kOPitch * 4 + 8 * NT * 8;    // per warp: sums, references and weights
+    static constexpr size_t kSmem = kAtWarps * (kQBytes + kOBytes);
+};
+
+template <int WK, int WV, int MAXB, int NT, bool F32>
+__global__ void __launch_bounds__(kAtThreads) mx_attn_decode_kernel(const AttnArgs a) {
+    using S = AttnShape<WK, WV, MAXB, NT, F32>;
+    using T = typename std::conditional<F32, float, __nv_bfloat16>::type;
+    constexpr int KB = S::kKeyBlocks, VB = S::kValBlocks, PARTS = S::kParts;
+    extern __shared__ __align__(16) uint8_t smem[];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
+    uint2* qs = reinterpret_cast<uint2*>(smem + warp * S::kQBytes);
+    float* os_all = reinterpret_cast<float*>(smem + kAtWarps * S::kQBytes);
+    constexpr int kOFloats = (int)(S::kOBytes / 4);
+    float* os = os_all + warp * kOFloats;
+    const int hw = warp % a.hw, tw = warp / a.hw;
+    const int unit = blockIdx.y * a.hw + hw;
+    const bool live = unit < a.n_units && tw < a.tw;
+    const int mk = unit / a.passes, pass = unit - mk * a.passes, kv0 = mk * a.merge;
+    const int kv_n = live ? min(a.merge, a.n_kv - kv0) : 0, blocks = kv_n * a.nb, block0 = kv0 * a.nb;
+
+    const int64_t total = total_tiles(a, lane);
+    int64_t u = worker_begin(total, blockIdx.x, a.workers);
+    const int64_t u_end = worker_begin(total, blockIdx.x + 1, a.workers);
+    if (u >= u_end) return;  // uniform for the CTA
+    int b = 0;
+    int64_t prefix = walk_tiles(a, lane, a.n_seqs, u, b);
+    bool first_segment = true;
+
+    // query head of a column, or -1
+    auto head_of = [&](int col) {
+        const int f = col / a.per_pass, i = pass * a.per_pass + (col - f * a.per_pass);
+        return f < kv_n && i < a.group ? (kv0 + f) * a.group + i : -1;
+    };
+
+    while (u < u_end) {
+        const SeqRange r = seq_range(a, b);
+        if (r.count == 0) { ++b; continue; }
+        const int t0 = (int)(u - prefix), t1 = (int)min((int64_t)r.count, u_end - prefix);
+
+        // ---- queries into shared memory: [part][step j][column group][lane], pairs (4j, 4j+1), (4j+2, 4j+3) of the lane's elements
+        if (live) {
+            for (int n = 0; n < NT; ++n) {
+                const int col = 8 * n + g, head = head_of(col), f = col / a.per_pass;
+                const T* q = static_cast<const T*>(a.q) + (int64_t)b * a.ldq + (int64_t)max(head, 0) * a.d;
+                for (int j = 0; j < MAXB; ++j) {
+                    uint16_t p[4][3];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int at = c * KB * 16 + 4 * j + e - f * a.d;  // element of the head
+                        const bool in = head >= 0 && at >= 0 && at < a.d;
+                        p[e][0] = p[e][1] = p[e][2] = 0;
+                        if (in) {
+                            if constexpr (F32) frag::split3(q[at], p[e]);
+                            else p[e][0] = __bfloat16_as_ushort(q[at]);
+                        }
+                    }
+#pragma unroll
+                    for (int part = 0; part < PARTS; ++part)
+                        qs[((part * MAXB + j) * NT + n) * 32 + lane] =
+                            make_uint2(frag::pack2(p[0][part], p[1][part]), frag::pack2(p[2][part], p[3][part]));
+                }
+            }
+        }
+        __syncwarp();
+
+        float o[VB * 8][NT][4], ref[NT][2], sum[NT][2];
+#pragma unroll
+        for (int i = 0; i < VB * 8; ++i)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[i][n][e] = 0.f;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) { ref[n][0] = ref[n][1] = -INFINITY; sum[n][0] = sum[n][1] = 0.f; }
+
+        int tile = (r.first + t0) * a.tw + tw;
+        int tile_end = live ? min((r.first + t1) * a.tw, (r.end + 15) / 16) : 0;
+        while (tile < tile_end && tile * 16 + 16 <= r.start) tile += a.tw;
+
+        // slot of token 16 tile + lane (lanes 0 .. 15): -1 outside the range, -2 for a page that does not exist
+        auto slot_of = [&](int t) {
+            const int tok = 16 * t + (lane & 15);
+            int slot = -1;
+            if (t < tile_end && tok >= r.start && tok < r.end) {
+                const int pg = (int)fastdiv((uint32_t)tok, a.page);
+                const int id = pg < a.max_pages ? __ldg(a.table + (int64_t)b * a.ld_table + pg) : -1;
+                const bool ok = id >= 0 && id < a.n_pages;
+                slot = ok ? id * (int)a.page.d + (tok - pg * (int)a.page.d) : -2;
+                if (!ok) atomicCAS(a.status, 0, (int)BDR_ERR_SIZE);
+            }
+            return slot;
+        };
+        frag::Block<WK> kb[2][KB];
+        frag::Block<WV> vb[4][VB];
+        uint32_t kf[2][KB], km[2][KB], vf[4][VB], vm[4][VB];
+        int key_slot[2];
+        auto load_keys = [&](int slots) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int slot = __shfl_sync(0xFFFFFFFFu, slots, g + 8 * i);
+                key_slot[i] = slot;
+#pragma unroll
+                for (int x = 0; x < KB; ++x) {
+                    const int blk = c * KB + x;
+                    kf[i][x] = km[i][x] = 0;
+#pragma unroll
+                    for (int w = 0; w < frag::Block<WK>::kWords; ++w) kb[i][x].w[w] = 0;
+                    if (slot >= 0 && blk < blocks) {
+                        kb[i][x] = frag::load_block<WK>(a.k.elems + (int64_t)slot * a.k.ld_elems + (block0 + blk) * (2 * WK));
+                        kf[i][x] = __ldg(a.k.exps + (int64_t)slot * a.k.ld_exps + block0 + blk);
+                        km[i][x] = __ldg(a.k.micro + (int64_t)slot * a.k.ld_micro + block0 + blk);
+                    }
+                }
+            }
+        };
+        auto load_values = [&](int slots) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int slot = __shfl_sync(0xFFFFFFFFu, slots, 2 * c + (i & 1) + 8 * (i >> 1));
+#pragma unroll
+                for (int x = 0; x < VB; ++x) {
+                    const int blk = g * VB + x;
+                    vf[i][x] = vm[i][x] = 0;  // a zero block: tokens outside the range count as zeros whatever their slot holds
+#pragma unroll
+                    for (int w = 0; w < frag::Block<WV>::kWords; ++w) vb[i][x].w[w] = 0;
+                    if (slot >= 0 && blk < blocks) {
+                        vb[i][x] = frag::load_block<WV>(a.v.elems + (int64_t)slot * a.v.ld_elems + (block0 + blk) * (2 * WV));
+                        vf[i][x] = __ldg(a.v.exps + (int64_t)slot * a.v.ld_exps + block0 + blk);
+                        vm[i][x] = __ldg(a.v.micro + (int64_t)slot * a.v.ld_micro + block0 + blk);
+                    }
+                }
+            }
+        };
+
+        int next = slot_of(tile);
+        if (tile < tile_end) {
+            load_keys(next);
+            load_values(next);
+            next = slot_of(tile + a.tw);
+        }
+        for (; tile < tile_end; tile += a.tw) {
+            // ---- scores
+            float s[NT][4];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
+            // Merged heads share the reduction: a NaN block of one head must not reach the others' columns through their zero
+            // queries, so it is decoded as zeros and its head's scores are made NaN below.
+            uint32_t spoilt[2] = {0, 0};  // per row: the unit's heads with such a block
+            if (a.merge > 1) {
+                bool any = false;
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int x = 0; x < KB; ++x) any |= kf[i][x] == 255u;
+                if (__any_sync(0xFFFFFFFFu, any)) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+#pragma unroll
+                        for (int x = 0; x < KB; ++x)
+                            if (kf[i][x] == 255u) {
+                                spoilt[i] |= 1u << ((c * KB + x) / a.nb);
+                                kf[i][x] = 0;
+                            }
+                        spoilt[i] |= __shfl_xor_sync(0xFFFFFFFFu, spoilt[i], 1);
+                        spoilt[i] |= __shfl_xor_sync(0xFFFFFFFFu, spoilt[i], 2);
+                    }
+                }
+            }
+#pragma unroll
+            for (int x = 0; x < KB; ++x) {
+                uint32_t y0[8], y1[8];
+                frag::align_block(kb[0][x], (uint32_t)((block0 + c * KB + x) * (2 * WK)));
+                frag::align_block(kb[1][x], (uint32_t)((block0 + c * KB + x) * (2 * WK)));
+                frag::decode_block<WK>(kb[0][x].w, 0, kf[0][x], km[0][x], y0);
+                frag::decode_block<WK>(kb[1][x].w, 0, kf[1][x], km[1][x], y1);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int part = PARTS - 1; part >= 0; --part)
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            const uint2 qv = qs[((part * MAXB + 4 * x + j) * NT + n) * 32 + lane];
+                            frag::mma_bf16(s[n], y0[2 * j], y1[2 * j], y0[2 * j + 1], y1[2 * j + 1], qv.x, qv.y);
+                        }
+            }
+            if (spoilt[0] | spoilt[1]) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (spoilt[e >> 1] >> ((8 * n + 2 * c + (e & 1)) / a.per_pass) & 1u) s[n][e] = __uint_as_float(0x7FC00000u);
+            }
+            bool raise = false;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int slot = key_slot[e >> 1];
+                    s[n][e] = slot >= 0 ? s[n][e] * a.scale2 : (slot == -1 ? -INFINITY : __uint_as_float(0x7FC00000u));
+                    raise |= s[n][e] > ref[n][e & 1] + kAtSlack;
+                }
+            const bool more = tile + a.tw < tile_end;
+            if (more) load_keys(next);
+            // ---- softmax weights relative to the running references
+            if (__any_sync(0xFFFFFFFFu, raise)) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float top = fmaxf(s[n][e], s[n][e + 2]);
+#pragma unroll
+                        for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
+                        top = fmaxf(top, ref[n][e]);
+                        const float f = ref[n][e] == -INFINITY ? 0.f : exp2_approx(ref[n][e] - top);
+                        ref[n][e] = top;
+                        sum[n][e] *= f;
+#pragma unroll
+                        for (int i = 0; i < VB * 8; ++i) { o[i][n][e] *= f; o[i][n][e + 2] *= f; }
+                    }
+            }
+            uint32_t pb[NT][F32 ? 2 : 1][2];  // P^T fragments (32-bit: the weight's leading and remaining bits)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                float p[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float m = ref[n][e & 1];
+                    p[e] = exp2_approx(s[n][e] - (m == -INFINITY ? 0.f : m));
+                    sum[n][e & 1] += p[e];
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t hi = pack_bf16x2(p[2 * h], p[2 * h + 1]);
+                    pb[n][0][h] = frag::transpose8x8(hi);
+                    if constexpr (F32)
+                        pb[n][1][h] = frag::transpose8x8(pack_bf16x2(p[2 * h] - __uint_as_float(hi << 16),
+                                                                     p[2 * h + 1] - __uint_as_float(hi & 0xFFFF0000u)));
+                }
+            }
+            // ---- output
+#pragma unroll
+            for (int x = 0; x < VB; ++x) {
+                uint32_t y[4][8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    frag::align_block(vb[i][x], (uint32_t)((block0 + g * VB + x) * (2 * WV)));
+                    frag::decode_block<WV>(vb[i][x].w, 0, vf[i][x], vm[i][x], y[i]);
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const uint32_t a0 = __byte_perm(y[0][j], y[1][j], 0x5410), a1 = __byte_perm(y[0][j], y[1][j], 0x7632);
+                    const uint32_t a2 = __byte_perm(y[2][j], y[3][j], 0x5410), a3 = __byte_perm(y[2][j], y[3][j], 0x7632);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        frag::mma_bf16(o[8 * x + j][n], a0, a1, a2, a3, pb[n][0][0], pb[n][0][1]);
+                        if constexpr (F32) frag::mma_bf16(o[8 * x + j][n], a0, a1, a2, a3, pb[n][1][0], pb[n][1][1]);
+                    }
+                }
+            }
+            if (more) {
+                load_values(next);
+                next = slot_of(tile + 2 * a.tw);
+            }
+        }
+
+        // ---- the segment's result: every warp's sums into shared memory, then joined over the token warps
+        float2* ml = reinterpret_cast<float2*>(os + 8 * NT * S::kOPitch);
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float l = sum[n][e];
+#pragma unroll
+                for (int x = 4; x < 32; x <<= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, x);
+                const int col = 8 * n + 2 * c + e;
+                if (g == 0) ml[col] = make_float2(ref[n][e], l);
+#pragma unroll
+                for (int x = 0; x < VB; ++x)
+#pragma unroll
+                    for (int j = 0; j < 8; j += 2)
+                        *reinterpret_cast<float4*>(os + col * S::kOPitch + (g * VB + x) * 16 + 2 * j) =
+                            make_float4(o[8 * x + j][n][e], o[8 * x + j][n][e + 2], o[8 * x + j + 1][n][e], o[8 * x + j + 1][n][e + 2]);
+            }
+        if (a.tw > 1) __syncthreads();
+        else __syncwarp();
+        const bool whole = t0 == 0 && t1 == r.count;
+        if (live) {
+            for (int col = tw; col < 8 * NT; col += a.tw) {
+                const int head = head_of(col);
+                if (head < 0) continue;
+                const int f = col / a.per_pass;
+                float m = -INFINITY, l = 0.f;
+                for (int w = 0; w < a.tw; ++w)
+                    m = fmaxf(m, reinterpret_cast<float2*>(os_all + (hw + w * a.hw) * kOFloats + 8 * NT * S::kOPitch)[col].x);
+                for (int w = 0; w < a.tw; ++w) {
+                    const float2 x = reinterpret_cast<float2*>(os_all + (hw + w * a.hw) * kOFloats + 8 * NT * S::kOPitch)[col];
+                    l += x.x == -INFINITY ? x.y : x.y * exp2_approx(x.x - m);
+                }
+                const float norm = whole ? (l == 0.f ? 0.f : 2.f / l) : 2.f;  // the values were decoded halved
+                const int64_t part = ((int64_t)blockIdx.x * 2 + (first_segment ? 0 : 1)) * a.n_q + head;
+                for (int e = lane; e < a.d; e += 32) {
+                    float v = 0.f;
+                    for (int w = 0; w < a.tw; ++w) {
+                        const float* ow = os_all + (hw + w * a.hw) * kOFloats;
+                        const float mw = reinterpret_cast<const float2*>(ow + 8 * NT * S::kOPitch)[col].x;
+                        const float x = ow[col * S::kOPitch + f * a.d + e];
+                        v += mw == -INFINITY ? x : x * exp2_approx(mw - m);
+                    }
+                    v *= norm;
+                    if (whole) {
+                        T* out = static_cast<T*>(a.out) + (int64_t)b * a.ldo + (int64_t)head * a.d + e;
+                        if constexpr (F32) *out = v;
+                        else *out = __float2bfloat16_rn(v);
+                    } else {
+                        a.part_o[part * a.d + e] = v;
+                    }
+                }
+                if (lane == 0) {
+                    if (!whole) a.part_ml[part] = make_float2(m, l);
+                    else if (a.lse) a.lse[(int64_t)b * a.n_q + head] = (m + log2f(l)) * 0.69314718055994531f;
+                }
+            }
+        }
+        if (a.tw > 1) __syncthreads();
+        else __syncwarp();
+        first_segment = false;
+        u = prefix + t1;
+        if (t1 == r.count) { prefix += r.count; ++b; }
+    }
+}
+
+// host side of one key format; the files that include this instantiate it
+template <int WK>
+int launch_attn(const AttnArgs& a, int wv, int maxb, int nt, bool f32, int groups, cudaStream_t st);
+
+template <int WK, int WV, int MAXB, int NT, bool F32>
+int launch_attn_one(const AttnArgs& a, int groups, cudaStream_t st) {
+    using S = AttnShape<WK, WV, MAXB, NT, F32>;
+    static PerDevice once;
+    if (kernel_setup(once, mx_attn_decode_kernel<WK, WV, MAXB, NT, F32>, kAtThreads, S::kSmem) < 1) return BDR_ERR_CUDA;
+    mx_attn_decode_kernel<WK, WV, MAXB, NT, F32><<<dim3(a.workers, groups), kAtThreads, S::kSmem, st>>>(a);
+    return cudaGetLastError() == cudaSuccess ? BDR_OK : BDR_ERR_CUDA;
+}
+
+template <int WK, int WV>
+int launch_attn_shape(const AttnArgs& a, int maxb, int nt, bool f32, int groups, cudaStream_t st) {
+    if (maxb == 8) {
+        if (f32) return launch_attn_one<WK, WV, 8, 1, true>(a, groups, st);
+        return nt == 1 ? launch_attn_one<WK, WV, 8, 1, false>(a, groups, st) : launch_attn_one<WK, WV, 8, 2, false>(a, groups, st);
+    }
+    return f32 ? launch_attn_one<WK, WV, 16, 1, true>(a, groups, st) : launch_attn_one<WK, WV, 16, 1, false>(a, groups, st);
+}
+
+#define BDR_ATTN_KEY_FORMAT(WK)                                                                                              \
+    template <>                                                                                                              \
+    int launch_attn<WK>(const AttnArgs& a, int wv, int maxb, int nt, bool f32, int groups, cudaStream_t st) {               \
+        switch (wv) {                                                                                                        \
+            case 3: return launch_attn_shape<WK, 3>(a, maxb, nt, f32, groups, st);                                           \
+            case 5: return launch_attn_shape<WK, 5>(a, maxb, nt, f32, groups, st);                                           \
+            default: return launch_attn_shape<WK, 8>(a, maxb, nt, f32, groups, st);                                          \
+        }                                                                                                                    \
+    }
+
+}  // namespace bdr
