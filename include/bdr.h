@@ -333,8 +333,8 @@ int mx_gemm_hw(const bdr_config_t* cfg_a /*host*/, const bdr_planes_t* a /*host 
  * planes of W).  The activations are used as they are: bf16 values enter the tensor core unchanged, fp32 values as the
  * exact sum of three bf16 parts; accumulation is fp32 and the result is rounded once to y's type.  Only the summation
  * order is unspecified (it depends on the shape, not on the run).  Any N, K and T (K = 0 gives zeros); W is read once
- * for every 64 rows of bf16 x, or 21 rows of fp32 x, so larger T belongs to mx_gemm_ws.  Rows of x that are 16-byte
- * aligned are read faster. */
+ * for every 64 rows of bf16 x, or 21 rows of fp32 x, so larger T belongs to mx_gemm_ws.  Rows of x that start at a
+ * multiple of four elements' bytes are read faster. */
 int mx_gemv(const bdr_config_t* cfg_w /*host*/, const bdr_planes_t* w /*host struct*/, int64_t N, int64_t K, const void* x,
             bdr_dtype_t x_dt, int64_t ldx, int64_t T, void* y, bdr_dtype_t y_dt, int64_t ldy, void* stream);
 

@@ -63,7 +63,11 @@ class Config:
     rounding: int = ROUND_NEAREST_EVEN
 
     def c(self) -> _Config:
-        return _Config(self.k1, self.d1, self.k2, self.d2, self.m, self.scale_kind, self.rounding)
+        try:
+            return self._c
+        except AttributeError:
+            object.__setattr__(self, "_c", _Config(self.k1, self.d1, self.k2, self.d2, self.m, self.scale_kind, self.rounding))
+            return self._c
 
 
 MX9 = Config(16, 8, 2, 1, 7)
@@ -78,10 +82,21 @@ class Planes:
     micro: torch.Tensor
     elems: torch.Tensor
 
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        if name != "_c":
+            object.__setattr__(self, "_c", None)
+
+    def __reduce__(self):
+        return Planes, (self.exps, self.micro, self.elems)
+
     def c(self) -> _Planes:
-        return _Planes(self.exps.data_ptr(), self.micro.data_ptr() if self.micro.numel() else None,
-                       self.elems.data_ptr(), self.exps.stride(0), self.micro.stride(0) if self.micro.numel() else 0,
-                       self.elems.stride(0))
+        """The C view of the planes, made once (and again when a plane is replaced)."""
+        if self._c is None:
+            self._c = _Planes(self.exps.data_ptr(), self.micro.data_ptr() if self.micro.numel() else None,
+                              self.elems.data_ptr(), self.exps.stride(0), self.micro.stride(0) if self.micro.numel() else 0,
+                              self.elems.stride(0))
+        return self._c
 
 
 @dataclass

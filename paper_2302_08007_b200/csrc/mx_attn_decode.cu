@@ -9,19 +9,42 @@ namespace bdr {
 
 int* device_status_word();
 int check_kv_cache(const mx_kv_cache_t* c);
-template <> int launch_attn<3>(const AttnArgs&, int, int, int, bool, int, cudaStream_t);
-template <> int launch_attn<5>(const AttnArgs&, int, int, int, bool, int, cudaStream_t);
-template <> int launch_attn<8>(const AttnArgs&, int, int, int, bool, int, cudaStream_t);
+template <> int launch_attn<3>(const AttnArgs&, int, int, int, bool, bool, int, cudaStream_t);
+template <> int launch_attn<5>(const AttnArgs&, int, int, int, bool, bool, int, cudaStream_t);
+template <> int launch_attn<8>(const AttnArgs&, int, int, int, bool, bool, int, cudaStream_t);
 
 // One CTA per sequence and query head: sums the parts that the workers left, in the order of their positions.  A sequence
-// that one worker covered is finished already; one without positions gets zeros.
-constexpr int kJoinThreads = 128;
+// that one worker covered is finished already; one without positions gets zeros.  The parts are dealt to the CTA's warps
+// (32 lanes read a row of a part, 16 bytes each), whose sums are added in order at the end.
+// Launched while the workers still run (programmatic dependent launch): what it needs of `lengths` it has read by the time
+// their results are complete.
+constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
 template <bool F32>
 __global__ void __launch_bounds__(kJoinThreads) mx_attn_join_kernel(const AttnArgs a) {
-    const int b = blockIdx.x / a.n_q, head = blockIdx.x - b * a.n_q, lane = threadIdx.x & 31;
+    __shared__ float2 wml[kJoinWarps];
+    __shared__ __align__(16) float wo[kJoinWarps][256];
+    const int b = blockIdx.x / a.n_q, head = blockIdx.x - b * a.n_q, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     using T = typename std::conditional<F32, float, __nv_bfloat16>::type;
     T* out = static_cast<T*>(a.out) + (int64_t)b * a.ldo + (int64_t)head * a.d;
     const SeqRange r = seq_range(a, b);
+    int w0 = 0, w1 = -1;
+    int64_t total = 0, p = 0;
+    if (r.count > 0) {
+        total = total_tiles(a, lane);
+        int unused = 0;
+        p = walk_tiles(a, lane, b, -1, unused);
+        // the last worker whose part starts at or before a tile holds it: begin(w) = floor(total w / workers) <= tile
+        auto holder = [&](int64_t tile) {
+            int w = min((int)((tile * a.workers + a.workers - 1) / total), a.workers - 1);
+            while (w + 1 < a.workers && worker_begin(total, w + 1, a.workers) <= tile) ++w;
+            while (w > 0 && worker_begin(total, w, a.workers) > tile) --w;
+            return w;
+        };
+        w0 = holder(p);
+        w1 = holder(p + r.count - 1);
+    }
+    cudaGridDependencySynchronize();
+    if (w0 == w1) return;
     if (r.count == 0) {
         for (int e = threadIdx.x; e < a.d; e += kJoinThreads) {
             if constexpr (F32) out[e] = 0.f;
@@ -30,53 +53,96 @@ __global__ void __launch_bounds__(kJoinThreads) mx_attn_join_kernel(const AttnAr
         if (threadIdx.x == 0 && a.lse) a.lse[(int64_t)b * a.n_q + head] = -INFINITY;
         return;
     }
-    const int64_t total = total_tiles(a, lane);
-    int unused = 0;
-    const int64_t p = walk_tiles(a, lane, b, -1, unused);
-    // the last worker whose part starts at or before a tile holds it
-    auto holder = [&](int64_t tile) {
-        int w = (int)((tile * a.workers + a.workers - 1) / total);  // begin(w) = floor(total w / workers) <= tile
-        while (w + 1 <= a.workers - 1 && worker_begin(total, w + 1, a.workers) <= tile) ++w;
-        while (w > 0 && (w > a.workers - 1 || worker_begin(total, w, a.workers) > tile)) --w;
-        return w;
-    };
-    const int w0 = holder(p), w1 = holder(p + r.count - 1);
-    if (w0 == w1) return;
-    float m = -INFINITY;
-    for (int w = w0; w <= w1; ++w) {
-        const int64_t begin = worker_begin(total, w, a.workers);
-        if (begin == worker_begin(total, w + 1, a.workers)) continue;  // a worker without work
-        m = fmaxf(m, a.part_ml[((int64_t)w * 2 + (begin < p ? 1 : 0)) * a.n_q + head].x);
-    }
-    float acc[2] = {0.f, 0.f}, l = 0.f;
-    for (int w = w0; w <= w1; ++w) {
-        const int64_t begin = worker_begin(total, w, a.workers);
-        if (begin == worker_begin(total, w + 1, a.workers)) continue;
-        const int64_t part = ((int64_t)w * 2 + (begin < p ? 1 : 0)) * a.n_q + head;
-        const float2 x = a.part_ml[part];
-        const float f = x.x == -INFINITY ? 1.f : exp2_approx(x.x - m);
-        l += x.y * f;
+    float m = -INFINITY, l = 0.f, acc[8];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int e = threadIdx.x + i * kJoinThreads;
-            if (e < a.d) acc[i] += a.part_o[part * a.d + e] * f;
+    for (int i = 0; i < 8; ++i) acc[i] = 0.f;
+    const int rows4 = a.d / 4;  // 16-byte words of a row: at most 64
+    // a lane looks up one part, then the warp adds the parts it found one by one
+    for (int base = w0; base <= w1; base += kJoinThreads) {
+        const int mine = base + warp + kJoinWarps * lane;
+        float2 x = make_float2(-INFINITY, 0.f);
+        int64_t part = -1;
+        if (mine <= w1) {
+            const int64_t begin = worker_begin(total, mine, a.workers);
+            if (begin != worker_begin(total, mine + 1, a.workers)) {  // else a worker without work
+                part = ((int64_t)mine * 2 + (begin < p ? 1 : 0)) * a.n_q + head;
+                x = __ldcg(a.part_ml + part);
+            }
+        }
+        float top = x.x;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+        top = fmaxf(top, m);
+        const float old = m == -INFINITY ? 1.f : exp2_approx(m - top);
+        m = top;
+        l *= old;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[i] *= old;
+        const float f = x.x == -INFINITY ? 1.f : exp2_approx(x.x - m);  // a part without a reference holds zeros or NaN
+        float sum = x.y * f;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+        l += sum;
+        const int count = min(32, (w1 - base - warp) / kJoinWarps + 1);
+#pragma unroll 4
+        for (int i = 0; i < count; ++i) {
+            const int64_t row = __shfl_sync(0xFFFFFFFFu, part, i);
+            const float fi = __shfl_sync(0xFFFFFFFFu, f, i);
+            if (row < 0) continue;
+            const float4* src = reinterpret_cast<const float4*>(a.part_o + row * a.d);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (lane + 32 * h < rows4) {
+                    const float4 v = __ldcg(src + lane + 32 * h);
+                    acc[4 * h] += v.x * fi;
+                    acc[4 * h + 1] += v.y * fi;
+                    acc[4 * h + 2] += v.z * fi;
+                    acc[4 * h + 3] += v.w * fi;
+                }
         }
     }
-    const float norm = l == 0.f ? 0.f : 1.f / l;
+    if (lane == 0) wml[warp] = make_float2(m, l);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int e = threadIdx.x + i * kJoinThreads;
-        if (e < a.d) {
-            if constexpr (F32) out[e] = acc[i] * norm;
-            else out[e] = __float2bfloat16_rn(acc[i] * norm);
-        }
+    for (int h = 0; h < 2; ++h)
+        if (lane + 32 * h < rows4)
+            *reinterpret_cast<float4*>(&wo[warp][4 * (lane + 32 * h)]) = make_float4(acc[4 * h], acc[4 * h + 1], acc[4 * h + 2], acc[4 * h + 3]);
+    __syncthreads();
+    float mm = -INFINITY, ll = 0.f;
+#pragma unroll
+    for (int w = 0; w < kJoinWarps; ++w) mm = fmaxf(mm, wml[w].x);
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < kJoinWarps; ++w) {
+        const float f = wml[w].x == -INFINITY ? 1.f : exp2_approx(wml[w].x - mm);
+        ll += wml[w].y * f;
+        if (threadIdx.x < a.d) v += wo[w][threadIdx.x] * f;
     }
-    if (threadIdx.x == 0 && a.lse) a.lse[(int64_t)b * a.n_q + head] = (m + log2f(l)) * 0.69314718055994531f;
+    if (threadIdx.x < a.d) {
+        v *= ll == 0.f ? 0.f : 1.f / ll;
+        if constexpr (F32) out[threadIdx.x] = v;
+        else out[threadIdx.x] = __float2bfloat16_rn(v);
+    }
+    if (threadIdx.x == 0 && a.lse) a.lse[(int64_t)b * a.n_q + head] = (mm + log2f(ll)) * 0.69314718055994531f;
+}
+
+template <bool F32>
+static int launch_join(const AttnArgs& a, cudaStream_t st) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((int64_t)a.n_seqs * a.n_q));
+    cfg.blockDim = dim3(kJoinThreads);
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, mx_attn_join_kernel<F32>, a) == cudaSuccess ? BDR_OK : BDR_ERR_CUDA;
 }
 
 // How units, columns and warps are laid out for a cache and a number of query heads.
 struct AttnPlan {
     int maxb, nt, merge, per_pass, passes, n_units, hw, groups, workers;
+    bool full;
 };
 static AttnPlan plan_attn(const mx_kv_cache_t& c, int n_q, bool f32) {
     AttnPlan p;
@@ -90,6 +156,7 @@ static AttnPlan plan_attn(const mx_kv_cache_t& c, int n_q, bool f32) {
     p.passes = p.merge > 1 ? 1 : (group + 8 * p.nt - 1) / (8 * p.nt);
     p.per_pass = (group + p.passes - 1) / p.passes;
     p.n_units = (c.n_kv + p.merge - 1) / p.merge * p.passes;
+    p.full = p.merge * nb == p.maxb && c.n_kv % p.merge == 0;
     p.hw = kAtWarps;
     while (p.n_units % p.hw) p.hw /= 2;
     p.groups = p.n_units / p.hw;
@@ -143,18 +210,17 @@ int mx_attn_decode(const mx_kv_cache_t* cache, const void* q, int64_t ldq, bdr_d
     a.hw = p.hw; a.tw = kAtWarps / p.hw; a.workers = p.workers;
     a.n_pages = (int)cache->n_pages; a.max_pages = (int)max_pages; a.cap = (int)max_pages * cache->page_size; a.window = window;
     a.page = make_fastdiv((uint32_t)cache->page_size);
+    a.q_vec = (uintptr_t)q % (2 * eb) == 0 && (n_seqs == 1 || ldq % 2 == 0);
     a.scale2 = 2.f * scale * 1.44269504088896341f;
     cudaStream_t st = (cudaStream_t)stream;
     const int wv = cache->cfg_v.m + 1;
     switch (cache->cfg_k.m) {
-        case 2: rc = launch_attn<3>(a, wv, p.maxb, p.nt, f32, p.groups, st); break;
-        case 4: rc = launch_attn<5>(a, wv, p.maxb, p.nt, f32, p.groups, st); break;
-        default: rc = launch_attn<8>(a, wv, p.maxb, p.nt, f32, p.groups, st); break;
+        case 2: rc = launch_attn<3>(a, wv, p.maxb, p.nt, f32, p.full, p.groups, st); break;
+        case 4: rc = launch_attn<5>(a, wv, p.maxb, p.nt, f32, p.full, p.groups, st); break;
+        default: rc = launch_attn<8>(a, wv, p.maxb, p.nt, f32, p.full, p.groups, st); break;
     }
     if (rc) return rc;
-    if (f32) mx_attn_join_kernel<true><<<(unsigned)(n_seqs * n_q), kJoinThreads, 0, st>>>(a);
-    else mx_attn_join_kernel<false><<<(unsigned)(n_seqs * n_q), kJoinThreads, 0, st>>>(a);
-    return cudaGetLastError() == cudaSuccess ? BDR_OK : BDR_ERR_CUDA;
+    return f32 ? launch_join<true>(a, st) : launch_join<false>(a, st);
 }
 
 }  // extern "C"

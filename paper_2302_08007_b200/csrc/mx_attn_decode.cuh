@@ -7,8 +7,8 @@
 //             decodes whole blocks of tokens g and g + 8); Q waits in shared memory in the order of the B fragment;
 //   softmax   with a running reference per column instead of the running maximum: it is raised only when a score passes it
 //             by kSlack (in powers of two), so most tiles need a vote and no reduction over lanes;
-//   output    O^T[d, 8 columns] += V^T P^T: V is decoded like K (lane (g, c): block g of four tokens), a byte permutation pairs
-//             neighbouring tokens for the A fragment, and P^T is the 8x8 transpose of the score fragment.
+//   output    O^T[d, 8 columns] += V^T P^T: V is decoded like K (lane (g, c): block g of four tokens, two tokens to a word as the A
+//             fragment wants them), and P^T is the 8x8 transpose of the score fragment.
 // The packed bytes of the next tile are fetched while the present one is computed: keys as soon as the scores are done,
 // values as soon as the output is.
 //
@@ -44,6 +44,7 @@ struct AttnArgs {
     int merge, per_pass, passes, n_units;  // key-value heads of a unit, query heads per pass of each, passes, units
     int hw, tw, workers;                   // warps over units, warps over tokens, worker CTAs per group of units
     int n_pages, max_pages, cap, window;   // cap = max_pages * page_size
+    int q_vec;                             // two query elements may be read at once
     FastDiv page;
     float scale2;                          // 2 scale log2(e): the keys are decoded halved
     int* status;
@@ -111,7 +112,8 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
     return d;
 }
 
-// MAXB: blocks of a unit (8 or 16); NT: groups of eight columns (query heads); F32: 32-bit queries and results.
+// MAXB: blocks of a unit (8 or 16); NT: groups of eight columns (query heads); F32: 32-bit queries and results; FULL: every
+// unit has all MAXB blocks, so a lane's key blocks are whole aligned words.
 template <int WK, int WV, int MAXB, int NT, bool F32>
 struct AttnShape {
     static constexpr int kKeyBlocks = MAXB / 4, kValBlocks = MAXB / 8;  // per lane and token
@@ -123,8 +125,9 @@ struct AttnShape {
     static constexpr size_t kSmem = kAtWarps * (kQBytes + kOBytes);
 };
 
-template <int WK, int WV, int MAXB, int NT, bool F32>
-__global__ void __launch_bounds__(kAtThreads) mx_attn_decode_kernel(const AttnArgs a) {
+template <int WK, int WV, int MAXB, int NT, bool F32, bool FULL>
+__global__ void __launch_bounds__(kAtThreads, MAXB == 8 && NT == 1 ? 2 : 1) mx_attn_decode_kernel(const AttnArgs a) {
+    cudaTriggerProgrammaticLaunchCompletion();  // the joining kernel may take its place as soon as there is room
     using S = AttnShape<WK, WV, MAXB, NT, F32>;
     using T = typename std::conditional<F32, float, __nv_bfloat16>::type;
     constexpr int KB = S::kKeyBlocks, VB = S::kValBlocks, PARTS = S::kParts;
@@ -159,27 +162,40 @@ __global__ void __launch_bounds__(kAtThreads) mx_attn_decode_kernel(const AttnAr
         if (r.count == 0) { ++b; continue; }
         const int t0 = (int)(u - prefix), t1 = (int)min((int64_t)r.count, u_end - prefix);
 
-        // ---- queries into shared memory: [part][step j][column group][lane], pairs (4j, 4j+1), (4j+2, 4j+3) of the lane's elements
+        // ---- queries into shared memory: [part][step][column group][lane].  Step 8 x + j of a lane holds elements 2j and 2j + 1 of
+        // blocks 2x and 2x + 1 of its own: {2x: 2j, 2x+1: 2j}, {2x: 2j+1, 2x+1: 2j+1}.
         if (live) {
+#pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const int col = 8 * n + g, head = head_of(col), f = col / a.per_pass;
                 const T* q = static_cast<const T*>(a.q) + (int64_t)b * a.ldq + (int64_t)max(head, 0) * a.d;
-                for (int j = 0; j < MAXB; ++j) {
-                    uint16_t p[4][3];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int at = c * KB * 16 + 4 * j + e - f * a.d;  // element of the head
-                        const bool in = head >= 0 && at >= 0 && at < a.d;
-                        p[e][0] = p[e][1] = p[e][2] = 0;
-                        if (in) {
-                            if constexpr (F32) frag::split3(q[at], p[e]);
-                            else p[e][0] = __bfloat16_as_ushort(q[at]);
+                for (int x = 0; x < KB / 2; ++x) {
+                    const int at0 = (c * KB + 2 * x) * 16 - f * a.d, at1 = at0 + 16;  // elements of the head
+                    const bool in0 = head >= 0 && at0 >= 0 && at0 < a.d, in1 = head >= 0 && at1 >= 0 && at1 < a.d;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        uint16_t p[4][3];
+                        if constexpr (F32) {
+                            float2 u = make_float2(0.f, 0.f), v = u;
+                            if (in0) u = a.q_vec ? __ldg(reinterpret_cast<const float2*>(q + at0 + 2 * j)) : make_float2(q[at0 + 2 * j], q[at0 + 2 * j + 1]);
+                            if (in1) v = a.q_vec ? __ldg(reinterpret_cast<const float2*>(q + at1 + 2 * j)) : make_float2(q[at1 + 2 * j], q[at1 + 2 * j + 1]);
+                            frag::split3(u.x, p[0]);
+                            frag::split3(v.x, p[1]);
+                            frag::split3(u.y, p[2]);
+                            frag::split3(v.y, p[3]);
+                        } else {
+                            const uint16_t* h = reinterpret_cast<const uint16_t*>(q);
+                            uint32_t u = 0, v = 0;
+                            if (in0) u = a.q_vec ? __ldg(reinterpret_cast<const uint32_t*>(h + at0 + 2 * j)) : frag::pack2(h[at0 + 2 * j], h[at0 + 2 * j + 1]);
+                            if (in1) v = a.q_vec ? __ldg(reinterpret_cast<const uint32_t*>(h + at1 + 2 * j)) : frag::pack2(h[at1 + 2 * j], h[at1 + 2 * j + 1]);
+                            p[0][0] = (uint16_t)u; p[1][0] = (uint16_t)v; p[2][0] = (uint16_t)(u >> 16); p[3][0] = (uint16_t)(v >> 16);
                         }
-                    }
 #pragma unroll
-                    for (int part = 0; part < PARTS; ++part)
-                        qs[((part * MAXB + j) * NT + n) * 32 + lane] =
-                            make_uint2(frag::pack2(p[0][part], p[1][part]), frag::pack2(p[2][part], p[3][part]));
+                        for (int part = 0; part < PARTS; ++part)
+                            qs[((part * MAXB + 8 * x + j) * NT + n) * 32 + lane] =
+                                make_uint2(frag::pack2(p[0][part], p[1][part]), frag::pack2(p[2][part], p[3][part]));
+                    }
                 }
             }
         }
@@ -212,25 +228,56 @@ __global__ void __launch_bounds__(kAtThreads) mx_attn_decode_kernel(const AttnAr
             }
             return slot;
         };
-        frag::Block<WK> kb[2][KB];
+        // the fetched bytes: keys of tokens g and g + 8, values of tokens 2c, 2c + 1, 2c + 8 and 2c + 9; exponents and
+        // microexponents of a lane's blocks in the bytes of one word
+        uint32_t kr[2][FULL ? KB * WK / 2 : KB * frag::Block<WK>::kWords];
+        uint32_t kf[2], km[2], vf[4], vm[4];
         frag::Block<WV> vb[4][VB];
-        uint32_t kf[2][KB], km[2][KB], vf[4][VB], vm[4][VB];
         int key_slot[2];
+        const uint8_t* const ke = a.k.elems + (block0 + c * KB) * (2 * WK);
+        const uint8_t* const kx = a.k.exps + block0 + c * KB;
+        const uint8_t* const ki = a.k.micro + block0 + c * KB;
+        const uint8_t* const ve = a.v.elems + (block0 + g * VB) * (2 * WV);
+        const uint8_t* const vx = a.v.exps + block0 + g * VB;
+        const uint8_t* const vi = a.v.micro + block0 + g * VB;
         auto load_keys = [&](int slots) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const int slot = __shfl_sync(0xFFFFFFFFu, slots, g + 8 * i);
                 key_slot[i] = slot;
+                const uint32_t at = (uint32_t)max(slot, 0);
+                const uint8_t* e = ke + (uint64_t)at * (uint32_t)a.k.ld_elems;
+                const uint8_t* x = kx + (uint64_t)at * (uint32_t)a.k.ld_exps;
+                const uint8_t* m = ki + (uint64_t)at * (uint32_t)a.k.ld_micro;
+                if constexpr (FULL) {  // blocks of neighbouring positions: whole words, all present; a token outside the range reads slot 0
+                    if (a.n_pages > 0) {
+                        if constexpr (KB == 2) { kf[i] = __ldg(reinterpret_cast<const uint16_t*>(x)); km[i] = __ldg(reinterpret_cast<const uint16_t*>(m)); }
+                        else { kf[i] = __ldg(reinterpret_cast<const uint32_t*>(x)); km[i] = __ldg(reinterpret_cast<const uint32_t*>(m)); }
+                        if constexpr (WK == 8) {
 #pragma unroll
-                for (int x = 0; x < KB; ++x) {
-                    const int blk = c * KB + x;
-                    kf[i][x] = km[i][x] = 0;
+                            for (int w = 0; w < KB; ++w) {
+                                const uint4 v = __ldg(reinterpret_cast<const uint4*>(e) + w);
+                                kr[i][4 * w] = v.x; kr[i][4 * w + 1] = v.y; kr[i][4 * w + 2] = v.z; kr[i][4 * w + 3] = v.w;
+                            }
+                        } else {
 #pragma unroll
-                    for (int w = 0; w < frag::Block<WK>::kWords; ++w) kb[i][x].w[w] = 0;
-                    if (slot >= 0 && blk < blocks) {
-                        kb[i][x] = frag::load_block<WK>(a.k.elems + (int64_t)slot * a.k.ld_elems + (block0 + blk) * (2 * WK));
-                        kf[i][x] = __ldg(a.k.exps + (int64_t)slot * a.k.ld_exps + block0 + blk);
-                        km[i][x] = __ldg(a.k.micro + (int64_t)slot * a.k.ld_micro + block0 + blk);
+                            for (int w = 0; w < KB * WK / 2; ++w) kr[i][w] = __ldg(reinterpret_cast<const uint32_t*>(e) + w);
+                        }
+                    }
+                } else {
+                    kf[i] = km[i] = 0;
+#pragma unroll
+                    for (int y = 0; y < KB; ++y) {
+                        constexpr int BW = frag::Block<WK>::kWords;
+#pragma unroll
+                        for (int w = 0; w < BW; ++w) kr[i][y * BW + w] = 0;
+                        if (slot >= 0 && c * KB + y < blocks) {
+                            const frag::Block<WK> blk = frag::load_block<WK>(e + y * (2 * WK));
+#pragma unroll
+                            for (int w = 0; w < BW; ++w) kr[i][y * BW + w] = blk.w[w];
+                            kf[i] |= (uint32_t)__ldg(x + y) << (8 * y);
+                            km[i] |= (uint32_t)__ldg(m + y) << (8 * y);
+                        }
                     }
                 }
             }
@@ -239,16 +286,18 @@ __global__ void __launch_bounds__(kAtThreads) mx_attn_decode_kernel(const AttnAr
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int slot = __shfl_sync(0xFFFFFFFFu, slots, 2 * c + (i & 1) + 8 * (i >> 1));
+                vf[i] = vm[i] = 0;  // zero blocks: tokens outside the range count as zeros whatever their slot holds
+                if (slot >= 0 && (FULL || g * VB < blocks)) {
+                    const uint8_t* e = ve + (uint64_t)(uint32_t)slot * (uint32_t)a.v.ld_elems;
+                    const uint8_t* x = vx + (uint64_t)(uint32_t)slot * (uint32_t)a.v.ld_exps;
+                    const uint8_t* m = vi + (uint64_t)(uint32_t)slot * (uint32_t)a.v.ld_micro;
 #pragma unroll
-                for (int x = 0; x < VB; ++x) {
-                    const int blk = g * VB + x;
-                    vf[i][x] = vm[i][x] = 0;  // a zero block: tokens outside the range count as zeros whatever their slot holds
-#pragma unroll
-                    for (int w = 0; w < frag::Block<WV>::kWords; ++w) vb[i][x].w[w] = 0;
-                    if (slot >= 0 && blk < blocks) {
-                        vb[i][x] = frag::load_block<WV>(a.v.elems + (int64_t)slot * a.v.ld_elems + (block0 + blk) * (2 * WV));
-                        vf[i][x] = __ldg(a.v.exps + (int64_t)slot * a.v.ld_exps + block0 + blk);
-                        vm[i][x] = __ldg(a.v.micro + (int64_t)slot * a.v.ld_micro + block0 + blk);
+                    for (int y = 0; y < VB; ++y) {
+                        if (FULL || g * VB + y < blocks) {
+                            vb[i][y] = frag::load_block<WV>(e + y * (2 * WV));
+                            vf[i] |= (uint32_t)__ldg(x + y) << (8 * y);
+                            vm[i] |= (uint32_t)__ldg(m + y) << (8 * y);
+                        }
                     }
                 }
             }
@@ -275,15 +324,15 @@ __global__ void __launch_bounds__(kAtThreads) mx_attn_decode_kernel(const AttnAr
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
-                    for (int x = 0; x < KB; ++x) any |= kf[i][x] == 255u;
+                    for (int x = 0; x < KB; ++x) any |= ((kf[i] >> (8 * x)) & 0xFFu) == 255u;
                 if (__any_sync(0xFFFFFFFFu, any)) {
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
 #pragma unroll
                         for (int x = 0; x < KB; ++x)
-                            if (kf[i][x] == 255u) {
+                            if (((kf[i] >> (8 * x)) & 0xFFu) == 255u) {
                                 spoilt[i] |= 1u << ((c * KB + x) / a.nb);
-                                kf[i][x] = 0;
+                                kf[i] &= ~(0xFFu << (8 * x));
                             }
                         spoilt[i] |= __shfl_xor_sync(0xFFFFFFFFu, spoilt[i], 1);
                         spoilt[i] |= __shfl_xor_sync(0xFFFFFFFFu, spoilt[i], 2);
@@ -291,21 +340,40 @@ __global__ void __launch_bounds__(kAtThreads) mx_attn_decode_kernel(const AttnAr
                 }
             }
 #pragma unroll
-            for (int x = 0; x < KB; ++x) {
-                uint32_t y0[8], y1[8];
-                frag::align_block(kb[0][x], (uint32_t)((block0 + c * KB + x) * (2 * WK)));
-                frag::align_block(kb[1][x], (uint32_t)((block0 + c * KB + x) * (2 * WK)));
-                frag::decode_block<WK>(kb[0][x].w, 0, kf[0][x], km[0][x], y0);
-                frag::decode_block<WK>(kb[1][x].w, 0, kf[1][x], km[1][x], y1);
+            for (int x = 0; x < KB / 2; ++x) {
+                frag::Scales sc[2];
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
+                for (int i = 0; i < 2; ++i)
+                    sc[i] = frag::make_scales(frag::spread_bytes(kf[i] >> (16 * x)), frag::spread_bytes(km[i] >> (16 * x)));
+                if constexpr (!FULL) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int y = 2 * x; y < 2 * x + 2; ++y) {
+                            constexpr int BW = frag::Block<WK>::kWords;
+                            frag::Block<WK> blk;
+#pragma unroll
+                            for (int w = 0; w < BW; ++w) blk.w[w] = kr[i][y * BW + w];
+                            frag::align_block(blk, (uint32_t)((block0 + c * KB + y) * (2 * WK)));
+#pragma unroll
+                            for (int w = 0; w < BW; ++w) kr[i][y * BW + w] = blk.w[w];
+                        }
+                }
+                constexpr int kBits = FULL ? 16 * WK : 32 * frag::Block<WK>::kWords;  // from one block's stream to the next's
+                const int b0 = 2 * x * kBits, b1 = b0 + kBits;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const uint32_t s0 = frag::scale_word(sc[0], j), s1 = frag::scale_word(sc[1], j);
+                    const uint32_t a0 = frag::decode_word<WK>(kr[0], b0, kr[0], b1, 2 * j, s0), a1 = frag::decode_word<WK>(kr[1], b0, kr[1], b1, 2 * j, s1);
+                    const uint32_t a2 = frag::decode_word<WK>(kr[0], b0, kr[0], b1, 2 * j + 1, s0), a3 = frag::decode_word<WK>(kr[1], b0, kr[1], b1, 2 * j + 1, s1);
 #pragma unroll
                     for (int part = PARTS - 1; part >= 0; --part)
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
-                            const uint2 qv = qs[((part * MAXB + 4 * x + j) * NT + n) * 32 + lane];
-                            frag::mma_bf16(s[n], y0[2 * j], y1[2 * j], y0[2 * j + 1], y1[2 * j + 1], qv.x, qv.y);
+                            const uint2 qv = qs[((part * MAXB + 8 * x + j) * NT + n) * 32 + lane];
+                            frag::mma_bf16(s[n], a0, a1, a2, a3, qv.x, qv.y);
                         }
+                }
             }
             if (spoilt[0] | spoilt[1]) {
 #pragma unroll
@@ -342,7 +410,7 @@ __global__ void __launch_bounds__(kAtThreads) mx_attn_decode_kernel(const AttnAr
                         for (int i = 0; i < VB * 8; ++i) { o[i][n][e] *= f; o[i][n][e + 2] *= f; }
                     }
             }
-            uint32_t pb[NT][F32 ? 2 : 1][2];  // P^T fragments (32-bit: the weight's leading and remaining bits)
+            uint32_t pb[NT][PARTS][2];  // P^T fragments (32-bit: three parts of eight bits)
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 float p[4];
@@ -354,31 +422,32 @@ __global__ void __launch_bounds__(kAtThreads) mx_attn_decode_kernel(const AttnAr
                 }
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const uint32_t hi = pack_bf16x2(p[2 * h], p[2 * h + 1]);
-                    pb[n][0][h] = frag::transpose8x8(hi);
-                    if constexpr (F32)
-                        pb[n][1][h] = frag::transpose8x8(pack_bf16x2(p[2 * h] - __uint_as_float(hi << 16),
-                                                                     p[2 * h + 1] - __uint_as_float(hi & 0xFFFF0000u)));
+                    float lo = p[2 * h], hi = p[2 * h + 1];
+#pragma unroll
+                    for (int part = 0; part < PARTS; ++part) {
+                        const uint32_t w = pack_bf16x2(lo, hi);
+                        pb[n][part][h] = frag::transpose8x8(w);
+                        lo -= __uint_as_float(w << 16);
+                        hi -= __uint_as_float(w & 0xFFFF0000u);
+                    }
                 }
             }
             // ---- output
 #pragma unroll
             for (int x = 0; x < VB; ++x) {
-                uint32_t y[4][8];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    frag::align_block(vb[i][x], (uint32_t)((block0 + g * VB + x) * (2 * WV)));
-                    frag::decode_block<WV>(vb[i][x].w, 0, vf[i][x], vm[i][x], y[i]);
-                }
+                for (int i = 0; i < 4; ++i) frag::align_block(vb[i][x], (uint32_t)((block0 + g * VB + x) * (2 * WV)));
+                const frag::Scales s0 = frag::make_scales((vf[0] >> (8 * x)) & 0xFFu, (vf[1] >> (8 * x)) & 0xFFu, (vm[0] >> (8 * x)) & 0xFFu, (vm[1] >> (8 * x)) & 0xFFu);
+                const frag::Scales s1 = frag::make_scales((vf[2] >> (8 * x)) & 0xFFu, (vf[3] >> (8 * x)) & 0xFFu, (vm[2] >> (8 * x)) & 0xFFu, (vm[3] >> (8 * x)) & 0xFFu);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const uint32_t a0 = __byte_perm(y[0][j], y[1][j], 0x5410), a1 = __byte_perm(y[0][j], y[1][j], 0x7632);
-                    const uint32_t a2 = __byte_perm(y[2][j], y[3][j], 0x5410), a3 = __byte_perm(y[2][j], y[3][j], 0x7632);
+                    const uint32_t w0 = frag::scale_word(s0, j), w1 = frag::scale_word(s1, j);
+                    const uint32_t a0 = frag::decode_word<WV>(vb[0][x].w, 0, vb[1][x].w, 0, 2 * j, w0), a1 = frag::decode_word<WV>(vb[0][x].w, 0, vb[1][x].w, 0, 2 * j + 1, w0);
+                    const uint32_t a2 = frag::decode_word<WV>(vb[2][x].w, 0, vb[3][x].w, 0, 2 * j, w1), a3 = frag::decode_word<WV>(vb[2][x].w, 0, vb[3][x].w, 0, 2 * j + 1, w1);
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        frag::mma_bf16(o[8 * x + j][n], a0, a1, a2, a3, pb[n][0][0], pb[n][0][1]);
-                        if constexpr (F32) frag::mma_bf16(o[8 * x + j][n], a0, a1, a2, a3, pb[n][1][0], pb[n][1][1]);
-                    }
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int part = PARTS - 1; part >= 0; --part) frag::mma_bf16(o[8 * x + j][n], a0, a1, a2, a3, pb[n][part][0], pb[n][part][1]);
                 }
             }
             if (more) {
@@ -455,34 +524,34 @@ __global__ void __launch_bounds__(kAtThreads) mx_attn_decode_kernel(const AttnAr
 
 // host side of one key format; the files that include this instantiate it
 template <int WK>
-int launch_attn(const AttnArgs& a, int wv, int maxb, int nt, bool f32, int groups, cudaStream_t st);
+int launch_attn(const AttnArgs& a, int wv, int maxb, int nt, bool f32, bool full, int groups, cudaStream_t st);
 
-template <int WK, int WV, int MAXB, int NT, bool F32>
+template <int WK, int WV, int MAXB, int NT, bool F32, bool FULL>
 int launch_attn_one(const AttnArgs& a, int groups, cudaStream_t st) {
     using S = AttnShape<WK, WV, MAXB, NT, F32>;
     static PerDevice once;
-    if (kernel_setup(once, mx_attn_decode_kernel<WK, WV, MAXB, NT, F32>, kAtThreads, S::kSmem) < 1) return BDR_ERR_CUDA;
-    mx_attn_decode_kernel<WK, WV, MAXB, NT, F32><<<dim3(a.workers, groups), kAtThreads, S::kSmem, st>>>(a);
+    if (kernel_setup(once, mx_attn_decode_kernel<WK, WV, MAXB, NT, F32, FULL>, kAtThreads, S::kSmem) < 1) return BDR_ERR_CUDA;
+    mx_attn_decode_kernel<WK, WV, MAXB, NT, F32, FULL><<<dim3(a.workers, groups), kAtThreads, S::kSmem, st>>>(a);
     return cudaGetLastError() == cudaSuccess ? BDR_OK : BDR_ERR_CUDA;
 }
 
-template <int WK, int WV>
+template <int WK, int WV, bool FULL>
 int launch_attn_shape(const AttnArgs& a, int maxb, int nt, bool f32, int groups, cudaStream_t st) {
     if (maxb == 8) {
-        if (f32) return launch_attn_one<WK, WV, 8, 1, true>(a, groups, st);
-        return nt == 1 ? launch_attn_one<WK, WV, 8, 1, false>(a, groups, st) : launch_attn_one<WK, WV, 8, 2, false>(a, groups, st);
+        if (f32) return launch_attn_one<WK, WV, 8, 1, true, FULL>(a, groups, st);
+        return nt == 1 ? launch_attn_one<WK, WV, 8, 1, false, FULL>(a, groups, st) : launch_attn_one<WK, WV, 8, 2, false, FULL>(a, groups, st);
     }
-    return f32 ? launch_attn_one<WK, WV, 16, 1, true>(a, groups, st) : launch_attn_one<WK, WV, 16, 1, false>(a, groups, st);
+    return f32 ? launch_attn_one<WK, WV, 16, 1, true, FULL>(a, groups, st) : launch_attn_one<WK, WV, 16, 1, false, FULL>(a, groups, st);
 }
 
-#define BDR_ATTN_KEY_FORMAT(WK)                                                                                              \
-    template <>                                                                                                              \
-    int launch_attn<WK>(const AttnArgs& a, int wv, int maxb, int nt, bool f32, int groups, cudaStream_t st) {               \
-        switch (wv) {                                                                                                        \
-            case 3: return launch_attn_shape<WK, 3>(a, maxb, nt, f32, groups, st);                                           \
-            case 5: return launch_attn_shape<WK, 5>(a, maxb, nt, f32, groups, st);                                           \
-            default: return launch_attn_shape<WK, 8>(a, maxb, nt, f32, groups, st);                                          \
-        }                                                                                                                    \
+#define BDR_ATTN_KEY_FORMAT(WK)                                                                                                        \
+    template <>                                                                                                                        \
+    int launch_attn<WK>(const AttnArgs& a, int wv, int maxb, int nt, bool f32, bool full, int groups, cudaStream_t st) {              \
+        switch (wv) {                                                                                                                  \
+            case 3: return full ? launch_attn_shape<WK, 3, true>(a, maxb, nt, f32, groups, st) : launch_attn_shape<WK, 3, false>(a, maxb, nt, f32, groups, st); \
+            case 5: return full ? launch_attn_shape<WK, 5, true>(a, maxb, nt, f32, groups, st) : launch_attn_shape<WK, 5, false>(a, maxb, nt, f32, groups, st); \
+            default: return full ? launch_attn_shape<WK, 8, true>(a, maxb, nt, f32, groups, st) : launch_attn_shape<WK, 8, false>(a, maxb, nt, f32, groups, st); \
+        }                                                                                                                              \
     }
 
 }  // namespace bdr

@@ -15,6 +15,11 @@
 // for every finite block without a special case at either end of the exponent range: nothing overflows because the value is
 // halved, F = 255 makes S infinite and the result NaN, and F = 0 (zeros, and values below 2^-126, which count as zero here)
 // makes S zero.  The kernels double their results once, in fp32.
+//
+// The two halves of a decoded word are the same element of TWO blocks (two blocks of a line, or one block of two lines),
+// not two neighbours: a sub-block's two elements then use the same scale word, which halves the work on microexponents
+// (the integer/logic pipe, at half the rate of the FMA pipe, is what decoding keeps busy: 3.5 of its instructions per word
+// of MX9 or MX4, 4.2 for MX6), and a product over lines gets its pairs of lines without a transposition.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -74,40 +79,63 @@ __device__ __forceinline__ void align_block(Block<W>& b, uint32_t off) {
     }
 }
 
-// Pair j (elements 2j, 2j+1) of a stream of W-bit codes: the magnitudes at the top of the seven mantissa bits of each half,
-// the sign bits where sign_of() expects them; other bits hold leftovers.
-template <int W, int NW>
-__device__ __forceinline__ uint32_t code_pair(const uint32_t (&s)[NW], int j) {
-    if constexpr (W == 8) {
-        return __byte_perm(s[j >> 1], 0u, (j & 1) ? 0x3322 : 0x1100);  // each code in both bytes of its half
-    } else {
-        const int bit = 2 * W * j, wi = bit >> 5, sh = bit & 31;
-        uint32_t f = sh == 0 ? s[wi] : (sh + 2 * W > 32 ? __funnelshift_r(s[wi], s[wi + 1], sh) : s[wi] >> sh);
-        f &= (1u << (2 * W)) - 1u;
-        return f * ((1u << (8 - W)) + (1u << (24 - 2 * W)));  // the two copies do not overlap: 2 W <= 16 - W + W
-    }
-}
-
-template <int W> struct PairMask {  // magnitude bits of a half: W - 1 bits ending at bit 6
-    static constexpr uint32_t kMag = (0x7Fu & ~((1u << (8 - W)) - 1u)) * 0x00010001u;
+// The exponents and microexponents of the two blocks of a word: S0 holds F << 7 per half, micro the eight shifts of each
+// block in the low byte of its half.
+struct Scales {
+    uint32_t S0, micro;
 };
-
-// The eight pairs of a block as bf16x2 words, halved (see above).  `s` holds the stream from word/bit 0 of pair `first`.
-template <int W, int NW>
-__device__ __forceinline__ void decode_block(const uint32_t (&s)[NW], int first, uint32_t F, uint32_t micro, uint32_t (&y)[8]) {
-    const uint32_t S0 = F * 0x00800080u;
-    // zero and Inf/NaN blocks keep their scale whatever their microexponents say
-    const uint32_t mb = (F - 1u) < 254u ? micro : 0u;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const uint32_t c = code_pair<W, NW>(s, first + j);
-        const uint32_t S = S0 - (mb & (1u << j)) * (0x00800080u >> j);  // minus tau in both exponent fields
-        uint32_t d;
-        asm("{.reg .b32 n; neg.bf16x2 n, %2; fma.rn.bf16x2 %0, %1, %2, n;}" : "=r"(d) : "r"((c & PairMask<W>::kMag) | 0x3F803F80u), "r"(S));
-        const uint32_t sign = W == 8 ? c : c << 8;
-        y[j] = d ^ (sign & 0x80008000u);
-    }
+// F2, micro2: one byte per half.  Zero blocks and Inf/NaN blocks (F = 0, 255) keep their scale whatever their
+// microexponents say.
+__device__ __forceinline__ Scales make_scales(uint32_t F2, uint32_t micro2) {
+    uint32_t one;
+    asm("min.u16x2 %0, %1, %2;" : "=r"(one) : "r"((F2 + 0x00010001u) & 0x00FE00FEu), "r"(0x00010001u));
+    return {F2 * 0x80u, micro2 & (one * 0xFFu)};
 }
+__device__ __forceinline__ Scales make_scales(uint32_t Fa, uint32_t Fb, uint32_t ma, uint32_t mb) {
+    return make_scales(Fa + (Fb << 16), ma + (mb << 16));
+}
+// bytes 0 and 1 of a word, one per half
+__device__ __forceinline__ uint32_t spread_bytes(uint32_t w) { return __byte_perm(w, 0u, 0x4140); }
+
+// sixteen bits of a stream at a bit offset (a constant once loops are unrolled), in the low half or, when `high` says so, in
+// the high half of the result; the other half holds leftovers
+template <int NW>
+__device__ __forceinline__ uint32_t window(const uint32_t (&s)[NW], int bit, bool& high) {
+    const int wi = bit >> 5, sh = bit & 31;
+    high = sh == 16;
+    if (sh == 0 || sh == 16) return s[wi];
+    return sh > 16 && wi + 1 < NW ? __funnelshift_r(s[wi], s[wi + 1 < NW ? wi + 1 : wi], sh) : s[wi] >> sh;
+}
+
+// Elements e of two blocks whose streams of W-bit codes start at bits a0 of `a` and b0 of `b`, halved (see above), with the
+// scale word S of the element's sub-block.  Streams of 3- and 5-bit codes are taken in groups of five and three codes (15 bits):
+// one group of each block side by side serves the group's elements.
+template <int W, int NA, int NB>
+__device__ __forceinline__ uint32_t decode_word(const uint32_t (&a)[NA], int a0, const uint32_t (&b)[NB], int b0, int e, uint32_t S) {
+    uint32_t mag, sign;
+    if constexpr (W == 8) {
+        const int x = e & 3;  // the code in both bytes of its half: the sign bit is where it belongs
+        const uint32_t c = __byte_perm(a[(a0 >> 5) + (e >> 2)], b[(b0 >> 5) + (e >> 2)], ((4 + x) << 12) | ((4 + x) << 8) | (x << 4) | x);
+        mag = c & 0x007F007Fu;
+        sign = c;
+    } else {
+        constexpr int kGroup = 15 / W;
+        const int i = e / kGroup, r = e - i * kGroup;
+        bool ha, hb;
+        const uint32_t wa = window(a, a0 + 15 * i, ha), wb = window(b, b0 + 15 * i, hb);
+        const uint32_t G = __byte_perm(wa, wb, (hb ? 0x7600 : 0x5400) | (ha ? 0x32 : 0x10));
+        const int up = 8 - W - W * r;  // brings the magnitude to the top of the mantissa
+        constexpr uint32_t kMag = (0x7Fu & ~((1u << (8 - W)) - 1u)) * 0x00010001u;
+        mag = (up >= 0 ? G << (up >= 0 ? up : 0) : G >> (up < 0 ? -up : 0)) & kMag;
+        sign = G << (16 - W - W * r);
+    }
+    uint32_t d;
+    asm("{.reg .b32 n; neg.bf16x2 n, %2; fma.rn.bf16x2 %0, %1, %2, n;}" : "=r"(d) : "r"(mag | 0x3F803F80u), "r"(S));
+    return d ^ (sign & 0x80008000u);
+}
+
+// the scale word of sub-block j: tau off the exponent field of each half
+__device__ __forceinline__ uint32_t scale_word(const Scales& s, int j) { return s.S0 - (s.micro & (0x00010001u << j)) * (0x80u >> j); }
 
 // A 24-bit fp32 value as the sum of three bf16 values (truncated eight bits at a time, so the sum is exact; parts below the
 // bf16 range are dropped).  An infinity stays in the first part, a NaN becomes the quiet NaN.

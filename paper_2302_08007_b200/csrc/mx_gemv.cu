@@ -32,7 +32,7 @@ struct GemvArgs {
     int64_t n, k;
     int tokens, tokens_per_pass;
     int x32, y32;        // 32-bit activations / results (else bf16)
-    int xvec;            // activation rows may be read 16 bytes at a time
+    int xvec;            // activations may be read four at a time
     int rw;              // row tiles of a CTA (a power of two up to 8)
     int phase_steps;     // steps whose activations fit in shared memory at once
 };
@@ -83,71 +83,98 @@ __device__ __forceinline__ void load_run(Run<W>& r, const bdr_planes_t& p, int64
     }
 }
 
-// Activations k0 .. k0 + 256 steps of the pass's columns into shared memory.  Element r = 64 c + 8 jj + e of a step goes to
-// 32 jj + 8 c + e: a lane's eight elements for two matrix instructions are one 16-byte word, and the eight lanes that a
-// shared-memory request serves at a time (two columns, four c) hit different banks (column pitch 64 bytes off a multiple of 128).
+// Activations of K steps k0 / 256 .. into shared memory, in the order of the B fragments: a lane's word for two matrix
+// instructions holds elements 4h .. 4h+3 of blocks 2p and 2p+1 of its four, alternating.  Word (p, h) of lane column c lies
+// at 16 (4 p + h) + 4 c 32-bit words of the step: the eight lanes that a shared-memory request serves at a time (two columns,
+// four c) hit different banks (column pitch 64 bytes off a multiple of 128).
 template <bool X32>
 __device__ __forceinline__ void stage_x(const GemvArgs& a, uint16_t* xs, int64_t pitch, int t0, int nt, int64_t k0, int span) {
     const int per = span / 8;
     for (int i = threadIdx.x; i < nt * per; i += kGvThreads) {
         const int t = i / per, v = i - t * per;
-        const int64_t k = k0 + 8 * v;
-        const int s = v >> 5, c = (v >> 3) & 3, jj = v & 7;
-        const int64_t at = (int64_t)s * kGvStep + jj * 32 + c * 8;
+        const int s = v >> 5, c = (v >> 3) & 3, p = (v >> 2) & 1, h = v & 3;
+        const int64_t k = k0 + (int64_t)s * kGvStep + 64 * c + 32 * p + 4 * h;
+        const int64_t at = (int64_t)s * kGvStep + (4 * p + h) * 32 + c * 8;
         if constexpr (X32) {
             const float* x = static_cast<const float*>(a.x) + (int64_t)(t0 + t) * a.ldx + k;
             float f[8];
-            if (a.xvec && k + 8 <= a.k) {
-                const float4 u = __ldg(reinterpret_cast<const float4*>(x)), w = __ldg(reinterpret_cast<const float4*>(x) + 1);
-                f[0] = u.x; f[1] = u.y; f[2] = u.z; f[3] = u.w; f[4] = w.x; f[5] = w.y; f[6] = w.z; f[7] = w.w;
+            if (a.xvec && k + 20 <= a.k) {
+                const float4 u = __ldg(reinterpret_cast<const float4*>(x)), w = __ldg(reinterpret_cast<const float4*>(x) + 4);
+                f[0] = u.x; f[1] = w.x; f[2] = u.y; f[3] = w.y; f[4] = u.z; f[5] = w.z; f[6] = u.w; f[7] = w.w;
             } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) f[e] = k + e < a.k ? __ldg(x + e) : 0.f;
+                for (int e = 0; e < 8; ++e) {
+                    const int o = (e >> 1) + 16 * (e & 1);
+                    f[e] = k + o < a.k ? __ldg(x + o) : 0.f;
+                }
             }
-            uint16_t p[8][3];
+            uint16_t q[8][3];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) frag::split3(f[e], p[e]);
+            for (int e = 0; e < 8; ++e) frag::split3(f[e], q[e]);
 #pragma unroll
             for (int part = 0; part < 3; ++part)
                 *reinterpret_cast<uint4*>(xs + (3 * t + part) * pitch + at) =
-                    make_uint4(frag::pack2(p[0][part], p[1][part]), frag::pack2(p[2][part], p[3][part]),
-                               frag::pack2(p[4][part], p[5][part]), frag::pack2(p[6][part], p[7][part]));
+                    make_uint4(frag::pack2(q[0][part], q[1][part]), frag::pack2(q[2][part], q[3][part]),
+                               frag::pack2(q[4][part], q[5][part]), frag::pack2(q[6][part], q[7][part]));
         } else {
             const uint16_t* x = static_cast<const uint16_t*>(a.x) + (int64_t)(t0 + t) * a.ldx + k;
-            uint4 w;
-            if (a.xvec && k + 8 <= a.k) {
-                w = __ldg(reinterpret_cast<const uint4*>(x));
+            uint2 u, w;
+            if (a.xvec && k + 20 <= a.k) {
+                u = __ldg(reinterpret_cast<const uint2*>(x));
+                w = __ldg(reinterpret_cast<const uint2*>(x) + 4);
             } else {
-                uint16_t h[8];
+                uint16_t q[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) h[e] = k + e < a.k ? __ldg(x + e) : (uint16_t)0;
-                w = make_uint4(frag::pack2(h[0], h[1]), frag::pack2(h[2], h[3]), frag::pack2(h[4], h[5]), frag::pack2(h[6], h[7]));
+                for (int e = 0; e < 8; ++e) {
+                    const int o = (e & 3) + 16 * (e >> 2);
+                    q[e] = k + o < a.k ? __ldg(x + o) : (uint16_t)0;
+                }
+                u = make_uint2(frag::pack2(q[0], q[1]), frag::pack2(q[2], q[3]));
+                w = make_uint2(frag::pack2(q[4], q[5]), frag::pack2(q[6], q[7]));
             }
-            *reinterpret_cast<uint4*>(xs + t * pitch + at) = w;
+            *reinterpret_cast<uint4*>(xs + t * pitch + at) =
+                make_uint4(__byte_perm(u.x, w.x, 0x5410), __byte_perm(u.x, w.x, 0x7632), __byte_perm(u.y, w.y, 0x5410), __byte_perm(u.y, w.y, 0x7632));
         }
     }
 }
 
+// One step of a warp.  The tensor core's fp32 additions are cut off rather than rounded, so a step's products are summed from
+// zero and then added to the totals with a rounded addition: 16 instructions in a chain instead of K / 16.
 template <int W, int NT>
 __device__ __forceinline__ void run_step(const Run<W>& r0, const Run<W>& r1, const uint16_t* xs, int64_t pitch, int cols, int lane,
                                          float (&acc)[NT][4]) {
     const int g = lane >> 2, c = lane & 3;
+    float part[NT][4];
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
-        uint32_t y0[8], y1[8];
-        frag::decode_block<W>(r0.w, 8 * b, (r0.exps >> (8 * b)) & 0xFFu, (r0.micro >> (8 * b)) & 0xFFu, y0);
-        frag::decode_block<W>(r1.w, 8 * b, (r1.exps >> (8 * b)) & 0xFFu, (r1.micro >> (8 * b)) & 0xFFu, y1);
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int i = 0; i < 4; ++i) part[n][i] = 0.f;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+        const frag::Scales s0 = frag::make_scales(frag::spread_bytes(r0.exps >> (16 * p)), frag::spread_bytes(r0.micro >> (16 * p)));
+        const frag::Scales s1 = frag::make_scales(frag::spread_bytes(r1.exps >> (16 * p)), frag::spread_bytes(r1.micro >> (16 * p)));
+        const int a0 = 32 * W * p, b0 = a0 + 16 * W;
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            uint32_t y0[4], y1[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                y0[e] = frag::decode_word<W>(r0.w, a0, r0.w, b0, 4 * h + e, frag::scale_word(s0, 2 * h + (e >> 1)));
+                y1[e] = frag::decode_word<W>(r1.w, a0, r1.w, b0, 4 * h + e, frag::scale_word(s1, 2 * h + (e >> 1)));
+            }
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 uint4 x = make_uint4(0, 0, 0, 0);
-                if (8 * n + g < cols) x = *reinterpret_cast<const uint4*>(xs + (8 * n + g) * pitch + (2 * b + h) * 32 + c * 8);
-                frag::mma_bf16(acc[n], y0[4 * h], y1[4 * h], y0[4 * h + 1], y1[4 * h + 1], x.x, x.y);
-                frag::mma_bf16(acc[n], y0[4 * h + 2], y1[4 * h + 2], y0[4 * h + 3], y1[4 * h + 3], x.z, x.w);
+                if (8 * n + g < cols) x = *reinterpret_cast<const uint4*>(xs + (8 * n + g) * pitch + (4 * p + h) * 32 + c * 8);
+                frag::mma_bf16(part[n], y0[0], y1[0], y0[1], y1[1], x.x, x.y);
+                frag::mma_bf16(part[n], y0[2], y1[2], y0[3], y1[3], x.z, x.w);
             }
         }
     }
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[n][i] += part[n][i];
 }
 
 template <int W, int NT, bool X32>
@@ -262,7 +289,7 @@ extern "C" int mx_gemv(const bdr_config_t* cfg_w, const bdr_planes_t* w, int64_t
     a.x = x; a.y = y; a.ldx = ldx; a.ldy = ldy; a.n = N; a.k = K; a.tokens = (int)T;
     a.x32 = x_dt == BDR_F32; a.y32 = y_dt == BDR_F32;
     const int64_t xb = a.x32 ? 4 : 2;
-    a.xvec = (uintptr_t)x % 16 == 0 && (T == 1 || ldx * xb % 16 == 0);
+    a.xvec = (uintptr_t)x % (4 * xb) == 0 && (T == 1 || ldx % 4 == 0);
     cudaStream_t st = (cudaStream_t)stream;
     switch (cfg_w->m) {
         case 2: return a.x32 ? pick_columns<3, true>(a, st) : pick_columns<3, false>(a, st);

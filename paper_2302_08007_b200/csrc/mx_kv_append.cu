@@ -254,6 +254,8 @@ int check_kv_cache(const mx_kv_cache_t* c) {
     if (c->n_pages < 0 || c->page_size < 1 || c->n_kv < 1 || c->head_dim < 1) return BDR_ERR_SIZE;
     if (c->n_pages > ((1ll << 31) - 64) / c->page_size || c->n_kv > 65535) return BDR_ERR_SIZE;
     if (c->head_dim % 16 || c->head_dim > 256) return BDR_ERR_UNSUPPORTED;
+    for (const bdr_planes_t* p : {&c->k, &c->v})
+        if (p->ld_exps > INT32_MAX || p->ld_micro > INT32_MAX || p->ld_elems > INT32_MAX) return BDR_ERR_SIZE;
     if (c->n_pages == 0) return BDR_OK;
     const int64_t line = (int64_t)c->n_kv * c->head_dim;
     const int rc = check_table2_planes(&c->cfg_k, &c->k, line);
