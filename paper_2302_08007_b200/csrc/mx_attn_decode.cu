@@ -53,14 +53,14 @@ __global__ void __launch_bounds__(kJoinThreads) mx_attn_join_kernel(const AttnAr
         if (threadIdx.x == 0 && a.lse) a.lse[(int64_t)b * a.n_q + head] = -INFINITY;
         return;
     }
-    float m = -INFINITY, l = 0.f, acc[8];
+    float m = kAtNone, l = 0.f, acc[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) acc[i] = 0.f;
     const int rows4 = a.d / 4;  // 16-byte words of a row: at most 64
     // a lane looks up one part, then the warp adds the parts it found one by one
     for (int base = w0; base <= w1; base += kJoinThreads) {
         const int mine = base + warp + kJoinWarps * lane;
-        float2 x = make_float2(-INFINITY, 0.f);
+        float2 x = make_float2(kAtNone, 0.f);
         int64_t part = -1;
         if (mine <= w1) {
             const int64_t begin = worker_begin(total, mine, a.workers);
@@ -73,12 +73,12 @@ __global__ void __launch_bounds__(kJoinThreads) mx_attn_join_kernel(const AttnAr
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
         top = fmaxf(top, m);
-        const float old = m == -INFINITY ? 1.f : exp2_approx(m - top);
+        const float old = exp2_approx(m - top);
         m = top;
         l *= old;
 #pragma unroll
         for (int i = 0; i < 8; ++i) acc[i] *= old;
-        const float f = x.x == -INFINITY ? 1.f : exp2_approx(x.x - m);  // a part without a reference holds zeros or NaN
+        const float f = exp2_approx(x.x - m);
         float sum = x.y * f;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
@@ -107,13 +107,13 @@ __global__ void __launch_bounds__(kJoinThreads) mx_attn_join_kernel(const AttnAr
         if (lane + 32 * h < rows4)
             *reinterpret_cast<float4*>(&wo[warp][4 * (lane + 32 * h)]) = make_float4(acc[4 * h], acc[4 * h + 1], acc[4 * h + 2], acc[4 * h + 3]);
     __syncthreads();
-    float mm = -INFINITY, ll = 0.f;
+    float mm = kAtNone, ll = 0.f;
 #pragma unroll
     for (int w = 0; w < kJoinWarps; ++w) mm = fmaxf(mm, wml[w].x);
     float v = 0.f;
 #pragma unroll
     for (int w = 0; w < kJoinWarps; ++w) {
-        const float f = wml[w].x == -INFINITY ? 1.f : exp2_approx(wml[w].x - mm);
+        const float f = exp2_approx(wml[w].x - mm);
         ll += wml[w].y * f;
         if (threadIdx.x < a.d) v += wo[w][threadIdx.x] * f;
     }
@@ -200,6 +200,10 @@ int mx_attn_decode(const mx_kv_cache_t* cache, const void* q, int64_t ldq, bdr_d
     a.status = device_status_word();
     if (!a.status) return BDR_ERR_CUDA;
     a.k = cache->k; a.v = cache->v;
+    if (cache->n_pages == 0) {  // there is no slot to read: every position is a bad page, whatever is read in its place
+        const uint8_t* any = static_cast<const uint8_t*>(workspace);
+        a.k = a.v = {const_cast<uint8_t*>(any), const_cast<uint8_t*>(any), const_cast<uint8_t*>(any), 0, 0, 0};
+    }
     a.q = q; a.out = out; a.lse = lse; a.table = page_table; a.lengths = lengths;
     a.part_o = static_cast<float*>(workspace);
     a.part_ml = reinterpret_cast<float2*>(a.part_o + (int64_t)p.workers * 2 * n_q * cache->head_dim);

@@ -29,7 +29,8 @@
 namespace bdr {
 
 constexpr int kAtThreads = 256, kAtWarps = kAtThreads / 32;
-constexpr float kAtSlack = 8.f;   // a softmax weight relative to the running reference stays below 2^8
+constexpr float kAtSlack = 8.f;     // a softmax weight relative to the running reference stays below 2^8
+constexpr float kAtNone = -3.0e38f;  // the reference before the first score: below every finite score, and finite itself
 
 struct AttnArgs {
     bdr_planes_t k, v;
@@ -133,7 +134,7 @@ __global__ void __launch_bounds__(kAtThreads, MAXB == 8 && NT == 1 ? 2 : 1) mx_a
     constexpr int KB = S::kKeyBlocks, VB = S::kValBlocks, PARTS = S::kParts;
     extern __shared__ __align__(16) uint8_t smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
-    uint2* qs = reinterpret_cast<uint2*>(smem + warp * S::kQBytes);
+    uint4* qs = reinterpret_cast<uint4*>(smem + warp * S::kQBytes);
     float* os_all = reinterpret_cast<float*>(smem + kAtWarps * S::kQBytes);
     constexpr int kOFloats = (int)(S::kOBytes / 4);
     float* os = os_all + warp * kOFloats;
@@ -162,7 +163,7 @@ __global__ void __launch_bounds__(kAtThreads, MAXB == 8 && NT == 1 ? 2 : 1) mx_a
         if (r.count == 0) { ++b; continue; }
         const int t0 = (int)(u - prefix), t1 = (int)min((int64_t)r.count, u_end - prefix);
 
-        // ---- queries into shared memory: [part][step][column group][lane].  Step 8 x + j of a lane holds elements 2j and 2j + 1 of
+        // ---- queries into shared memory: [part][pair of steps][column group][lane].  Step 8 x + j of a lane holds elements 2j and 2j + 1 of
         // blocks 2x and 2x + 1 of its own: {2x: 2j, 2x+1: 2j}, {2x: 2j+1, 2x+1: 2j+1}.
         if (live) {
 #pragma unroll
@@ -193,7 +194,7 @@ __global__ void __launch_bounds__(kAtThreads, MAXB == 8 && NT == 1 ? 2 : 1) mx_a
                         }
 #pragma unroll
                         for (int part = 0; part < PARTS; ++part)
-                            qs[((part * MAXB + 8 * x + j) * NT + n) * 32 + lane] =
+                            reinterpret_cast<uint2*>(qs + ((part * MAXB / 2 + 4 * x + j / 2) * NT + n) * 32 + lane)[j & 1] =
                                 make_uint2(frag::pack2(p[0][part], p[1][part]), frag::pack2(p[2][part], p[3][part]));
                     }
                 }
@@ -209,7 +210,7 @@ __global__ void __launch_bounds__(kAtThreads, MAXB == 8 && NT == 1 ? 2 : 1) mx_a
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[i][n][e] = 0.f;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) { ref[n][0] = ref[n][1] = -INFINITY; sum[n][0] = sum[n][1] = 0.f; }
+        for (int n = 0; n < NT; ++n) { ref[n][0] = ref[n][1] = kAtNone; sum[n][0] = sum[n][1] = 0.f; }
 
         int tile = (r.first + t0) * a.tw + tw;
         int tile_end = live ? min((r.first + t1) * a.tw, (r.end + 15) / 16) : 0;
@@ -233,45 +234,39 @@ __global__ void __launch_bounds__(kAtThreads, MAXB == 8 && NT == 1 ? 2 : 1) mx_a
         uint32_t kr[2][FULL ? KB * WK / 2 : KB * frag::Block<WK>::kWords];
         uint32_t kf[2], km[2], vf[4], vm[4];
         frag::Block<WV> vb[4][VB];
-        int key_slot[2];
         const uint8_t* const ke = a.k.elems + (block0 + c * KB) * (2 * WK);
         const uint8_t* const kx = a.k.exps + block0 + c * KB;
         const uint8_t* const ki = a.k.micro + block0 + c * KB;
         const uint8_t* const ve = a.v.elems + (block0 + g * VB) * (2 * WV);
         const uint8_t* const vx = a.v.exps + block0 + g * VB;
         const uint8_t* const vi = a.v.micro + block0 + g * VB;
+        // A token outside the range reads slot 0; what it gives is replaced below.
         auto load_keys = [&](int slots) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const int slot = __shfl_sync(0xFFFFFFFFu, slots, g + 8 * i);
-                key_slot[i] = slot;
-                const uint32_t at = (uint32_t)max(slot, 0);
+                const uint32_t at = (uint32_t)max(__shfl_sync(0xFFFFFFFFu, slots, g + 8 * i), 0);
                 const uint8_t* e = ke + (uint64_t)at * (uint32_t)a.k.ld_elems;
                 const uint8_t* x = kx + (uint64_t)at * (uint32_t)a.k.ld_exps;
                 const uint8_t* m = ki + (uint64_t)at * (uint32_t)a.k.ld_micro;
-                if constexpr (FULL) {  // blocks of neighbouring positions: whole words, all present; a token outside the range reads slot 0
-                    if (a.n_pages > 0) {
-                        if constexpr (KB == 2) { kf[i] = __ldg(reinterpret_cast<const uint16_t*>(x)); km[i] = __ldg(reinterpret_cast<const uint16_t*>(m)); }
-                        else { kf[i] = __ldg(reinterpret_cast<const uint32_t*>(x)); km[i] = __ldg(reinterpret_cast<const uint32_t*>(m)); }
-                        if constexpr (WK == 8) {
+                if constexpr (FULL) {  // neighbouring blocks, all present: whole aligned words
+                    if constexpr (KB == 2) { kf[i] = __ldg(reinterpret_cast<const uint16_t*>(x)); km[i] = __ldg(reinterpret_cast<const uint16_t*>(m)); }
+                    else { kf[i] = __ldg(reinterpret_cast<const uint32_t*>(x)); km[i] = __ldg(reinterpret_cast<const uint32_t*>(m)); }
+                    if constexpr (WK == 8) {
 #pragma unroll
-                            for (int w = 0; w < KB; ++w) {
-                                const uint4 v = __ldg(reinterpret_cast<const uint4*>(e) + w);
-                                kr[i][4 * w] = v.x; kr[i][4 * w + 1] = v.y; kr[i][4 * w + 2] = v.z; kr[i][4 * w + 3] = v.w;
-                            }
-                        } else {
-#pragma unroll
-                            for (int w = 0; w < KB * WK / 2; ++w) kr[i][w] = __ldg(reinterpret_cast<const uint32_t*>(e) + w);
+                        for (int w = 0; w < KB; ++w) {
+                            const uint4 v = __ldg(reinterpret_cast<const uint4*>(e) + w);
+                            kr[i][4 * w] = v.x; kr[i][4 * w + 1] = v.y; kr[i][4 * w + 2] = v.z; kr[i][4 * w + 3] = v.w;
                         }
+                    } else {
+#pragma unroll
+                        for (int w = 0; w < KB * WK / 2; ++w) kr[i][w] = __ldg(reinterpret_cast<const uint32_t*>(e) + w);
                     }
                 } else {
                     kf[i] = km[i] = 0;
 #pragma unroll
                     for (int y = 0; y < KB; ++y) {
-                        constexpr int BW = frag::Block<WK>::kWords;
-#pragma unroll
-                        for (int w = 0; w < BW; ++w) kr[i][y * BW + w] = 0;
-                        if (slot >= 0 && c * KB + y < blocks) {
+                        if (c * KB + y < blocks) {
+                            constexpr int BW = frag::Block<WK>::kWords;
                             const frag::Block<WK> blk = frag::load_block<WK>(e + y * (2 * WK));
 #pragma unroll
                             for (int w = 0; w < BW; ++w) kr[i][y * BW + w] = blk.w[w];
@@ -285,25 +280,24 @@ __global__ void __launch_bounds__(kAtThreads, MAXB == 8 && NT == 1 ? 2 : 1) mx_a
         auto load_values = [&](int slots) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int slot = __shfl_sync(0xFFFFFFFFu, slots, 2 * c + (i & 1) + 8 * (i >> 1));
-                vf[i] = vm[i] = 0;  // zero blocks: tokens outside the range count as zeros whatever their slot holds
-                if (slot >= 0 && (FULL || g * VB < blocks)) {
-                    const uint8_t* e = ve + (uint64_t)(uint32_t)slot * (uint32_t)a.v.ld_elems;
-                    const uint8_t* x = vx + (uint64_t)(uint32_t)slot * (uint32_t)a.v.ld_exps;
-                    const uint8_t* m = vi + (uint64_t)(uint32_t)slot * (uint32_t)a.v.ld_micro;
+                const uint32_t at = (uint32_t)max(__shfl_sync(0xFFFFFFFFu, slots, 2 * c + (i & 1) + 8 * (i >> 1)), 0);
+                const uint8_t* e = ve + (uint64_t)at * (uint32_t)a.v.ld_elems;
+                const uint8_t* x = vx + (uint64_t)at * (uint32_t)a.v.ld_exps;
+                const uint8_t* m = vi + (uint64_t)at * (uint32_t)a.v.ld_micro;
+                if constexpr (!FULL) vf[i] = vm[i] = 0;
 #pragma unroll
-                    for (int y = 0; y < VB; ++y) {
-                        if (FULL || g * VB + y < blocks) {
-                            vb[i][y] = frag::load_block<WV>(e + y * (2 * WV));
-                            vf[i] |= (uint32_t)__ldg(x + y) << (8 * y);
-                            vm[i] |= (uint32_t)__ldg(m + y) << (8 * y);
-                        }
+                for (int y = 0; y < VB; ++y) {
+                    if (FULL || g * VB + y < blocks) {
+                        vb[i][y] = frag::load_block<WV>(e + y * (2 * WV));
+                        const uint32_t f = __ldg(x + y), u = __ldg(m + y);
+                        if (FULL && y == 0) { vf[i] = f; vm[i] = u; }
+                        else { vf[i] |= f << (8 * y); vm[i] |= u << (8 * y); }
                     }
                 }
             }
         };
 
-        int next = slot_of(tile);
+        int next = slot_of(tile), now = next;
         if (tile < tile_end) {
             load_keys(next);
             load_values(next);
@@ -362,16 +356,20 @@ __global__ void __launch_bounds__(kAtThreads, MAXB == 8 && NT == 1 ? 2 : 1) mx_a
                 constexpr int kBits = FULL ? 16 * WK : 32 * frag::Block<WK>::kWords;  // from one block's stream to the next's
                 const int b0 = 2 * x * kBits, b1 = b0 + kBits;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const uint32_t s0 = frag::scale_word(sc[0], j), s1 = frag::scale_word(sc[1], j);
-                    const uint32_t a0 = frag::decode_word<WK>(kr[0], b0, kr[0], b1, 2 * j, s0), a1 = frag::decode_word<WK>(kr[1], b0, kr[1], b1, 2 * j, s1);
-                    const uint32_t a2 = frag::decode_word<WK>(kr[0], b0, kr[0], b1, 2 * j + 1, s0), a3 = frag::decode_word<WK>(kr[1], b0, kr[1], b1, 2 * j + 1, s1);
+                for (int j = 0; j < 8; j += 2) {
+                    uint32_t y[2][4];  // rows g and g + 8, elements 2j .. 2j + 3
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            y[i][e] = frag::decode_word<WK>(kr[i], b0, kr[i], b1, 2 * j + e, frag::scale_word(sc[i], j + (e >> 1)));
 #pragma unroll
                     for (int part = PARTS - 1; part >= 0; --part)
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
-                            const uint2 qv = qs[((part * MAXB + 8 * x + j) * NT + n) * 32 + lane];
-                            frag::mma_bf16(s[n], a0, a1, a2, a3, qv.x, qv.y);
+                            const uint4 qv = qs[((part * MAXB / 2 + 4 * x + j / 2) * NT + n) * 32 + lane];
+                            frag::mma_bf16(s[n], y[0][0], y[1][0], y[0][1], y[1][1], qv.x, qv.y);
+                            frag::mma_bf16(s[n], y[0][2], y[1][2], y[0][3], y[1][3], qv.z, qv.w);
                         }
                 }
             }
@@ -382,19 +380,36 @@ __global__ void __launch_bounds__(kAtThreads, MAXB == 8 && NT == 1 ? 2 : 1) mx_a
                     for (int e = 0; e < 4; ++e)
                         if (spoilt[e >> 1] >> ((8 * n + 2 * c + (e & 1)) / a.per_pass) & 1u) s[n][e] = __uint_as_float(0x7FC00000u);
             }
-            bool raise = false;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[n][e] *= a.scale2;
+            if (!__all_sync(0xFFFFFFFFu, now >= 0)) {  // a tile at an end of the range, or with a page that does not exist
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int slot = __shfl_sync(0xFFFFFFFFu, now, g + 8 * i);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int e = 2 * i; e < 2 * i + 2; ++e)
+                            if (slot < 0) s[n][e] = slot == -1 ? -INFINITY : __uint_as_float(0x7FC00000u);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)  // zero blocks: a weight of zero times anything that a slot may hold would not do
+                    if (__shfl_sync(0xFFFFFFFFu, now, 2 * c + (i & 1) + 8 * (i >> 1)) < 0) vf[i] = 0;
+            }
+            const bool more = tile + a.tw < tile_end;
+            if (more) load_keys(next);
+            // ---- softmax weights relative to the running references, t = log2 of a weight
+            float t[NT][4], high = 0.f;
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int slot = key_slot[e >> 1];
-                    s[n][e] = slot >= 0 ? s[n][e] * a.scale2 : (slot == -1 ? -INFINITY : __uint_as_float(0x7FC00000u));
-                    raise |= s[n][e] > ref[n][e & 1] + kAtSlack;
+                    t[n][e] = s[n][e] - ref[n][e & 1];
+                    high = fmaxf(high, t[n][e]);
                 }
-            const bool more = tile + a.tw < tile_end;
-            if (more) load_keys(next);
-            // ---- softmax weights relative to the running references
-            if (__any_sync(0xFFFFFFFFu, raise)) {
+            if (__any_sync(0xFFFFFFFFu, high > kAtSlack)) {
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -403,9 +418,11 @@ __global__ void __launch_bounds__(kAtThreads, MAXB == 8 && NT == 1 ? 2 : 1) mx_a
 #pragma unroll
                         for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
                         top = fmaxf(top, ref[n][e]);
-                        const float f = ref[n][e] == -INFINITY ? 0.f : exp2_approx(ref[n][e] - top);
+                        const float f = exp2_approx(ref[n][e] - top);
                         ref[n][e] = top;
                         sum[n][e] *= f;
+                        t[n][e] = s[n][e] - top;
+                        t[n][e + 2] = s[n][e + 2] - top;
 #pragma unroll
                         for (int i = 0; i < VB * 8; ++i) { o[i][n][e] *= f; o[i][n][e + 2] *= f; }
                     }
@@ -416,8 +433,7 @@ __global__ void __launch_bounds__(kAtThreads, MAXB == 8 && NT == 1 ? 2 : 1) mx_a
                 float p[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float m = ref[n][e & 1];
-                    p[e] = exp2_approx(s[n][e] - (m == -INFINITY ? 0.f : m));
+                    p[e] = exp2_approx(t[n][e]);
                     sum[n][e & 1] += p[e];
                 }
 #pragma unroll
@@ -452,6 +468,7 @@ __global__ void __launch_bounds__(kAtThreads, MAXB == 8 && NT == 1 ? 2 : 1) mx_a
             }
             if (more) {
                 load_values(next);
+                now = next;
                 next = slot_of(tile + 2 * a.tw);
             }
         }
@@ -482,12 +499,12 @@ __global__ void __launch_bounds__(kAtThreads, MAXB == 8 && NT == 1 ? 2 : 1) mx_a
                 const int head = head_of(col);
                 if (head < 0) continue;
                 const int f = col / a.per_pass;
-                float m = -INFINITY, l = 0.f;
+                float m = kAtNone, l = 0.f;
                 for (int w = 0; w < a.tw; ++w)
                     m = fmaxf(m, reinterpret_cast<float2*>(os_all + (hw + w * a.hw) * kOFloats + 8 * NT * S::kOPitch)[col].x);
                 for (int w = 0; w < a.tw; ++w) {
                     const float2 x = reinterpret_cast<float2*>(os_all + (hw + w * a.hw) * kOFloats + 8 * NT * S::kOPitch)[col];
-                    l += x.x == -INFINITY ? x.y : x.y * exp2_approx(x.x - m);
+                    l += x.y * exp2_approx(x.x - m);
                 }
                 const float norm = whole ? (l == 0.f ? 0.f : 2.f / l) : 2.f;  // the values were decoded halved
                 const int64_t part = ((int64_t)blockIdx.x * 2 + (first_segment ? 0 : 1)) * a.n_q + head;
@@ -497,7 +514,7 @@ __global__ void __launch_bounds__(kAtThreads, MAXB == 8 && NT == 1 ? 2 : 1) mx_a
                         const float* ow = os_all + (hw + w * a.hw) * kOFloats;
                         const float mw = reinterpret_cast<const float2*>(ow + 8 * NT * S::kOPitch)[col].x;
                         const float x = ow[col * S::kOPitch + f * a.d + e];
-                        v += mw == -INFINITY ? x : x * exp2_approx(mw - m);
+                        v += x * exp2_approx(mw - m);
                     }
                     v *= norm;
                     if (whole) {

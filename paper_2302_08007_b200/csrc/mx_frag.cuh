@@ -134,8 +134,13 @@ __device__ __forceinline__ uint32_t decode_word(const uint32_t (&a)[NA], int a0,
     return d ^ (sign & 0x80008000u);
 }
 
-// the scale word of sub-block j: tau off the exponent field of each half
-__device__ __forceinline__ uint32_t scale_word(const Scales& s, int j) { return s.S0 - (s.micro & (0x00010001u << j)) * (0x80u >> j); }
+// The scale word of sub-block j: tau off the exponent field of each half.  Written as the multiply-add it is meant to be: a
+// compiler would shift and subtract, on the pipe that is busy.
+__device__ __forceinline__ uint32_t scale_word(const Scales& s, int j) {
+    uint32_t S;
+    asm("mad.lo.u32 %0, %1, %2, %3;" : "=r"(S) : "r"(s.micro & (0x00010001u << j)), "r"(0u - (0x80u >> j)), "r"(s.S0));
+    return S;
+}
 
 // A 24-bit fp32 value as the sum of three bf16 values (truncated eight bits at a time, so the sum is exact; parts below the
 // bf16 range are dropped).  An infinity stays in the first part, a NaN becomes the quiet NaN.

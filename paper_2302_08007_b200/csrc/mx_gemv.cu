@@ -164,8 +164,8 @@ __device__ __forceinline__ void run_step(const Run<W>& r0, const Run<W>& r1, con
             }
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                uint4 x = make_uint4(0, 0, 0, 0);
-                if (8 * n + g < cols) x = *reinterpret_cast<const uint4*>(xs + (8 * n + g) * pitch + (4 * p + h) * 32 + c * 8);
+                // a column beyond the last repeats it: what it gives is not looked at
+                const uint4 x = *reinterpret_cast<const uint4*>(xs + min(8 * n + g, cols - 1) * pitch + (4 * p + h) * 32 + c * 8);
                 frag::mma_bf16(part[n], y0[0], y1[0], y0[1], y1[1], x.x, x.y);
                 frag::mma_bf16(part[n], y0[2], y1[2], y0[3], y1[3], x.z, x.w);
             }
@@ -178,7 +178,7 @@ __device__ __forceinline__ void run_step(const Run<W>& r0, const Run<W>& r1, con
 }
 
 template <int W, int NT, bool X32>
-__global__ void __launch_bounds__(kGvThreads) mx_gemv_kernel(const GemvArgs a) {
+__global__ void __launch_bounds__(kGvThreads, NT <= 2 ? 3 : 2) mx_gemv_kernel(const GemvArgs a) {
     extern __shared__ __align__(16) uint8_t smem[];
     uint16_t* xs = reinterpret_cast<uint16_t*>(smem);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
@@ -194,23 +194,22 @@ __global__ void __launch_bounds__(kGvThreads) mx_gemv_kernel(const GemvArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[n][i] = 0.f;
 
-    Run<W> cur[2], nxt[2];
-    auto fetch = [&](Run<W>(&r)[2], int s) {
-        load_run<W>(r[0], a.w, row0, 16 * s + 4 * c, nb);
-        load_run<W>(r[1], a.w, row1, 16 * s + 4 * c, nb);
+    // The next step's words are fetched once the present one is decoded; the SM's other warps cover the wait.
+    Run<W> run[2];
+    auto fetch = [&](int s) {
+        load_run<W>(run[0], a.w, row0, 16 * s + 4 * c, nb);
+        load_run<W>(run[1], a.w, row1, 16 * s + 4 * c, nb);
     };
     int s = my_k;
-    if (s < steps) fetch(cur, s);
+    if (s < steps) fetch(s);
     for (int p0 = 0; p0 < steps; p0 += a.phase_steps) {
         const int p1 = min(p0 + a.phase_steps, steps);
         if (p0) __syncthreads();  // everyone is done with the phase before
         stage_x<X32>(a, xs, pitch, t0, nt, (int64_t)p0 * kGvStep, (p1 - p0) * kGvStep);
         __syncthreads();
         for (; s < p1; s += kw) {
-            if (s + kw < steps) fetch(nxt, s + kw);
-            run_step<W, NT>(cur[0], cur[1], xs + (int64_t)(s - p0) * kGvStep, pitch, cols, lane, acc);
-            cur[0] = nxt[0];
-            cur[1] = nxt[1];
+            run_step<W, NT>(run[0], run[1], xs + (int64_t)(s - p0) * kGvStep, pitch, cols, lane, acc);
+            if (s + kw < steps) fetch(s + kw);
         }
     }
     // the shares of K, added in order; each row tile's results are [column][16 rows]
