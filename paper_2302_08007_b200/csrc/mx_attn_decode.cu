@@ -3,11 +3,11 @@
 #include <algorithm>
 #include <cmath>
 
+#include "bdr_async.cuh"
 #include "mx_attn_decode.cuh"
 
 namespace bdr {
 
-int* device_status_word();
 int check_kv_cache(const mx_kv_cache_t* c);
 template <> int launch_attn<3>(const AttnArgs&, int, int, int, bool, bool, int, cudaStream_t);
 template <> int launch_attn<5>(const AttnArgs&, int, int, int, bool, bool, int, cudaStream_t);
@@ -141,7 +141,7 @@ static int launch_join(const AttnArgs& a, cudaStream_t st) {
 
 // How units, columns and warps are laid out for a cache and a number of query heads.
 struct AttnPlan {
-    int maxb, nt, merge, per_pass, passes, n_units, hw, groups, workers;
+    int maxb, nt, merge, per_pass, passes, n_units, hw, tw, groups, workers;
     bool full;
 };
 static AttnPlan plan_attn(const mx_kv_cache_t& c, int n_q, bool f32) {
@@ -157,10 +157,12 @@ static AttnPlan plan_attn(const mx_kv_cache_t& c, int n_q, bool f32) {
     p.per_pass = (group + p.passes - 1) / p.passes;
     p.n_units = (c.n_kv + p.merge - 1) / p.merge * p.passes;
     p.full = p.merge * nb == p.maxb && c.n_kv % p.merge == 0;
-    p.hw = kAtWarps;
+    const int warps = p.maxb == 8 && p.nt == 1 ? AttnShape<8, 1, false>::kWarps : AttnShape<16, 1, false>::kWarps;
+    p.hw = f32 ? AttnShape<8, 1, true>::kMaxUnits : AttnShape<8, 1, false>::kMaxUnits;  // neighbouring units side by side: they share the sectors of the scale planes
     while (p.n_units % p.hw) p.hw /= 2;
+    p.tw = warps / p.hw;
     p.groups = p.n_units / p.hw;
-    p.workers = std::max(1, 2 * sm_count() / p.groups);
+    p.workers = std::max(1, sm_count() / p.groups);
     return p;
 }
 
@@ -200,10 +202,6 @@ int mx_attn_decode(const mx_kv_cache_t* cache, const void* q, int64_t ldq, bdr_d
     a.status = device_status_word();
     if (!a.status) return BDR_ERR_CUDA;
     a.k = cache->k; a.v = cache->v;
-    if (cache->n_pages == 0) {  // there is no slot to read: every position is a bad page, whatever is read in its place
-        const uint8_t* any = static_cast<const uint8_t*>(workspace);
-        a.k = a.v = {const_cast<uint8_t*>(any), const_cast<uint8_t*>(any), const_cast<uint8_t*>(any), 0, 0, 0};
-    }
     a.q = q; a.out = out; a.lse = lse; a.table = page_table; a.lengths = lengths;
     a.part_o = static_cast<float*>(workspace);
     a.part_ml = reinterpret_cast<float2*>(a.part_o + (int64_t)p.workers * 2 * n_q * cache->head_dim);
@@ -211,10 +209,11 @@ int mx_attn_decode(const mx_kv_cache_t* cache, const void* q, int64_t ldq, bdr_d
     a.n_seqs = (int)n_seqs; a.n_q = n_q; a.n_kv = cache->n_kv; a.group = n_q / cache->n_kv;
     a.d = cache->head_dim; a.nb = cache->head_dim / 16;
     a.merge = p.merge; a.per_pass = p.per_pass; a.passes = p.passes; a.n_units = p.n_units;
-    a.hw = p.hw; a.tw = kAtWarps / p.hw; a.workers = p.workers;
+    a.hw = p.hw; a.tw = p.tw; a.workers = p.workers;
     a.n_pages = (int)cache->n_pages; a.max_pages = (int)max_pages; a.cap = (int)max_pages * cache->page_size; a.window = window;
     a.page = make_fastdiv((uint32_t)cache->page_size);
     a.q_vec = (uintptr_t)q % (2 * eb) == 0 && (n_seqs == 1 || ldq % 2 == 0);
+    a.o_vec = (uintptr_t)out % 16 == 0 && (n_seqs == 1 || ldo * eb % 16 == 0);
     a.scale2 = 2.f * scale * 1.44269504088896341f;
     cudaStream_t st = (cudaStream_t)stream;
     const int wv = cache->cfg_v.m + 1;

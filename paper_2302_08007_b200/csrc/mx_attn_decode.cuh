@@ -1,26 +1,31 @@
 // Attention of one new token per sequence over a paged key-value cache in MX format (see mx_attn_decode in bdr.h).
 //
 // The cache is read once and every element of it is used for the few query heads that share it, so the bounds are the bytes
-// of the cache and the instructions that decode them.  A warp owns one "unit", a key-value head with its query heads (small
-// heads are merged until a unit fills 128 elements), and walks over tiles of 16 tokens:
+// of the cache and the instructions that decode them.  A warp owns one "unit", a key-value head with its query heads (small heads
+// are merged until a unit fills 128 elements), and walks over tiles of 16 tokens.  It copies its tiles' packed bytes into a ring of
+// its own in shared memory with asynchronous 16- and 8-byte copies, a lane per piece, a tile or two ahead: no registers are
+// tied up by bytes in flight, fetching costs about 50 instructions a tile where loads into registers cost 230, and nothing
+// but the warp itself has to be waited for.  (One bulk copy per token and plane by a producer warp, tried instead, was twice
+// as slow as loads into registers: the pieces, 64 to 640 bytes, are too small for the bulk-copy unit.)
 //   scores    S^T[16 tokens, 8 columns] = K[16, d] Q^T: the key blocks are decoded straight into the A fragment (lane (g, c)
 //             decodes whole blocks of tokens g and g + 8); Q waits in shared memory in the order of the B fragment;
 //   softmax   with a running reference per column instead of the running maximum: it is raised only when a score passes it
-//             by kSlack (in powers of two), so most tiles need a vote and no reduction over lanes;
+//             by kAtSlack (in powers of two), so most tiles need a vote and no reduction over lanes;
 //   output    O^T[d, 8 columns] += V^T P^T: V is decoded like K (lane (g, c): block g of four tokens, two tokens to a word as the A
 //             fragment wants them), and P^T is the 8x8 transpose of the score fragment.
-// The packed bytes of the next tile are fetched while the present one is computed: keys as soon as the scores are done,
-// values as soon as the output is.
 //
 // Work is split over the length of the cache: the tiles of all sequences form one long line that is cut into equal parts,
-// one per worker CTA, whatever the individual lengths are (each worker finds its part from `lengths`).  A part that covers a
-// sequence's whole range writes the result; other parts leave their sums and references in the workspace, where a second
-// kernel joins them in order.
+// one per worker CTA, whatever the individual lengths are (each worker finds its part from `lengths`).  Where a group has
+// fewer units than the CTA has warps, several sets of warps take turns with the tiles and are joined in shared memory.  A part
+// that covers a sequence's whole range writes the result; other parts leave their sums and references in the workspace, where
+// a second kernel joins them in order.
 #pragma once
 
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
+
+#include <type_traits>
 
 #include "bdr_device.cuh"
 #include "bdr_host.h"
@@ -28,7 +33,7 @@
 
 namespace bdr {
 
-constexpr int kAtThreads = 256, kAtWarps = kAtThreads / 32;
+constexpr int kAtSmemBytes = 227 * 1024;
 constexpr float kAtSlack = 8.f;     // a softmax weight relative to the running reference stays below 2^8
 constexpr float kAtNone = -3.0e38f;  // the reference before the first score: below every finite score, and finite itself
 
@@ -43,15 +48,15 @@ struct AttnArgs {
     int64_t ldq, ldo, ld_table;
     int n_seqs, n_q, n_kv, group, d, nb;   // group: query heads per key-value head; nb: blocks per head
     int merge, per_pass, passes, n_units;  // key-value heads of a unit, query heads per pass of each, passes, units
-    int hw, tw, workers;                   // warps over units, warps over tokens, worker CTAs per group of units
+    int hw, tw, workers;                   // units of a group (one per warp), sets of warps, worker CTAs per group
     int n_pages, max_pages, cap, window;   // cap = max_pages * page_size
-    int q_vec;                             // two query elements may be read at once
+    int q_vec, o_vec;                      // two query elements may be read at once; results may be written 16 bytes at a time
     FastDiv page;
     float scale2;                          // 2 scale log2(e): the keys are decoded halved
     int* status;
 };
 
-// Tiles of 16 tw tokens that sequence b's positions touch.
+// Tiles of 16 tokens that sequence b's positions touch.
 struct SeqRange {
     int start, end, first, count;
 };
@@ -60,9 +65,8 @@ __device__ __forceinline__ SeqRange seq_range(const AttnArgs& a, int b) {
     const int len = min(__ldg(a.lengths + b), a.cap + 1);  // a position beyond the table's pages poisons the result
     r.end = max(len, 0);
     r.start = a.window > 0 ? max(0, r.end - a.window) : 0;
-    const int mt = 16 * a.tw;
-    r.first = r.start / mt;
-    r.count = r.end > r.start ? (r.end + mt - 1) / mt - r.first : 0;
+    r.first = r.start / 16;
+    r.count = r.end > r.start ? (r.end + 15) / 16 - r.first : 0;
     return r;
 }
 
@@ -115,57 +119,183 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
 
 // MAXB: blocks of a unit (8 or 16); NT: groups of eight columns (query heads); F32: 32-bit queries and results; FULL: every
 // unit has all MAXB blocks, so a lane's key blocks are whole aligned words.
-template <int WK, int WV, int MAXB, int NT, bool F32>
+template <int MAXB, int NT, bool F32>
 struct AttnShape {
+    static constexpr int kWarps = MAXB == 8 && NT == 1 ? 16 : 8;  // as many as the registers allow
+    static constexpr int kThreads = 32 * kWarps;
     static constexpr int kKeyBlocks = MAXB / 4, kValBlocks = MAXB / 8;  // per lane and token
     static constexpr int kParts = F32 ? 3 : 1;
-    static constexpr int kD = 16 * MAXB;
-    static constexpr size_t kQBytes = (size_t)kParts * MAXB * NT * 32 * 8;          // per warp
-    static constexpr int kOPitch = kD + 4;
-    static constexpr size_t kOBytes = (size_t)8 * NT * kOPitch * 4 + 8 * NT * 8;    // per warp: sums, references and weights
-    static constexpr size_t kSmem = kAtWarps * (kQBytes + kOBytes);
+    static constexpr int kMaxUnits = F32 ? 4 : 8;  // units of a group: their queries share the memory with the rings
+    static constexpr int kQBytes = kParts * MAXB * NT * 32 * 8;          // per unit
+    static constexpr int kSums = kValBlocks * 8 * NT * 4 + NT * 4;       // a lane's sums, references and weights
+    static constexpr int kJoinBytes = kSums * 32 * 4;                    // what a warp hands over (in its own ring)
+};
+
+// A tile in shared memory: 16 rows of key codes, 16 of value codes, 16 of scales (key exponents, key microexponents, value
+// exponents, value microexponents).  Pitches are odd multiples of 16 bytes, so that eight rows at one offset start in eight
+// different groups of banks.  Where units do not start at multiples of the copies' sizes, rows hold the words around them.
+template <int WK, int WV, int MAXB, bool FULL>
+struct AttnTile {
+    static constexpr int code_pitch(int w) {
+        const int len = FULL || w == 8 ? MAXB * 2 * w : ((MAXB - 1) * 2 * w + 14 + 15) / 16 * 16;
+        return len % 32 == 16 ? len : len + 16;
+    }
+    static constexpr int kPitchK = code_pitch(WK), kPitchV = code_pitch(WV);
+    static constexpr int kScale = FULL ? MAXB : MAXB == 8 ? 16 : 24;  // bytes of a plane's scales in a row
+    static constexpr int kPitchX = 4 * kScale % 32 == 16 ? 4 * kScale : 4 * kScale + 16;
+    static constexpr int kAtV = 16 * kPitchK, kAtX = kAtV + 16 * kPitchV, kBytes = kAtX + 16 * kPitchX;
+    // tiles in a warp's ring: what 227 KB hold, two at least, three at most
+    static constexpr int kStages = MAXB == 8 && 16 * 3 * kBytes + 4 * AttnShape<8, 1, true>::kQBytes <= kAtSmemBytes ? 3 : 2;
+};
+
+// a warp's part of shared memory: its ring, or the sums it hands over
+template <int WK, int WV, int MAXB, int NT, bool F32, bool FULL>
+__host__ __device__ constexpr int attn_ring_bytes() {
+    using L = AttnTile<WK, WV, MAXB, FULL>;
+    return L::kStages * L::kBytes > AttnShape<MAXB, NT, F32>::kJoinBytes ? L::kStages * L::kBytes : AttnShape<MAXB, NT, F32>::kJoinBytes;
+}
+
+// The bytes of a token's line that a unit needs, rounded out to aligned pieces.
+struct RowSpan {
+    int from, len, skew;  // first byte, bytes, where the unit's first block lies in them
+};
+template <int ALIGN>
+__device__ __forceinline__ RowSpan row_span(int block0, int blocks, int block_bytes) {
+    const int at = block0 * block_bytes;
+    RowSpan s;
+    s.from = at & ~(ALIGN - 1);
+    s.skew = at - s.from;
+    s.len = (s.skew + blocks * block_bytes + ALIGN - 1) & ~(ALIGN - 1);
+    return s;
+}
+
+// one block of W-bit codes from shared memory, at any two-byte boundary
+template <int W>
+__device__ __forceinline__ frag::Block<W> shared_block(const uint8_t* base, int off) {
+    frag::Block<W> b;
+    if constexpr (W == 8) {
+        const uint4 v = *reinterpret_cast<const uint4*>(base + off);
+        b.w[0] = v.x; b.w[1] = v.y; b.w[2] = v.z; b.w[3] = v.w;
+    } else {
+        const uint32_t* q = reinterpret_cast<const uint32_t*>(base + (off & ~3));
+#pragma unroll
+        for (int i = 0; i < frag::Block<W>::kWords; ++i) b.w[i] = q[i];
+    }
+    return b;
+}
+
+// A worker's part of the line of tiles, sequence by sequence.
+struct Segments {
+    int64_t u, u_end, prefix;
+    int b;
+    SeqRange r;
+    int t0, t1;
+    // false when the part is done; else tiles t0 .. t1 of sequence b (counted from the first that its range touches)
+    __device__ __forceinline__ bool next(const AttnArgs& a) {
+        if (u >= u_end) return false;
+        r = seq_range(a, b);
+        while (r.count == 0) r = seq_range(a, ++b);
+        t0 = (int)(u - prefix);
+        t1 = (int)min((int64_t)r.count, u_end - prefix);
+        return true;
+    }
+    __device__ __forceinline__ void advance() {
+        u = prefix + t1;
+        if (t1 == r.count) { prefix += r.count; ++b; }
+    }
 };
 
 template <int WK, int WV, int MAXB, int NT, bool F32, bool FULL>
-__global__ void __launch_bounds__(kAtThreads, MAXB == 8 && NT == 1 ? 2 : 1) mx_attn_decode_kernel(const AttnArgs a) {
+__global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_attn_decode_kernel(const AttnArgs a) {
     cudaTriggerProgrammaticLaunchCompletion();  // the joining kernel may take its place as soon as there is room
-    using S = AttnShape<WK, WV, MAXB, NT, F32>;
+    using S = AttnShape<MAXB, NT, F32>;
+    using L = AttnTile<WK, WV, MAXB, FULL>;
     using T = typename std::conditional<F32, float, __nv_bfloat16>::type;
-    constexpr int KB = S::kKeyBlocks, VB = S::kValBlocks, PARTS = S::kParts;
-    extern __shared__ __align__(16) uint8_t smem[];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
-    uint4* qs = reinterpret_cast<uint4*>(smem + warp * S::kQBytes);
-    float* os_all = reinterpret_cast<float*>(smem + kAtWarps * S::kQBytes);
-    constexpr int kOFloats = (int)(S::kOBytes / 4);
-    float* os = os_all + warp * kOFloats;
-    const int hw = warp % a.hw, tw = warp / a.hw;
-    const int unit = blockIdx.y * a.hw + hw;
-    const bool live = unit < a.n_units && tw < a.tw;
-    const int mk = unit / a.passes, pass = unit - mk * a.passes, kv0 = mk * a.merge;
-    const int kv_n = live ? min(a.merge, a.n_kv - kv0) : 0, blocks = kv_n * a.nb, block0 = kv0 * a.nb;
-
+    constexpr int KB = S::kKeyBlocks, VB = S::kValBlocks, PARTS = S::kParts, D = L::kStages;
+    constexpr int kRing = attn_ring_bytes<WK, WV, MAXB, NT, F32, FULL>();
+    extern __shared__ __align__(128) uint8_t smem[];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t total = total_tiles(a, lane);
-    int64_t u = worker_begin(total, blockIdx.x, a.workers);
-    const int64_t u_end = worker_begin(total, blockIdx.x + 1, a.workers);
-    if (u >= u_end) return;  // uniform for the CTA
-    int b = 0;
-    int64_t prefix = walk_tiles(a, lane, a.n_seqs, u, b);
-    bool first_segment = true;
+    Segments seg;
+    seg.u = worker_begin(total, blockIdx.x, a.workers);
+    seg.u_end = worker_begin(total, blockIdx.x + 1, a.workers);
+    if (seg.u >= seg.u_end) return;  // uniform for the CTA
+    seg.b = 0;
+    seg.prefix = walk_tiles(a, lane, a.n_seqs, seg.u, seg.b);
+
+    const int g = lane >> 2, c = lane & 3, hw = warp % a.hw, tw = warp / a.hw;
+    const int unit = blockIdx.y * a.hw + hw, mk = unit / a.passes, pass = unit - mk * a.passes, kv0 = mk * a.merge;
+    const int kv_n = min(a.merge, a.n_kv - kv0), blocks = kv_n * a.nb, block0 = kv0 * a.nb;
+    uint4* const qs = reinterpret_cast<uint4*>(smem + hw * S::kQBytes);
+    uint8_t* const rings = smem + a.hw * S::kQBytes;
+    uint8_t* const ring = rings + warp * kRing;
+    // the bytes of a token's line that the unit needs, rounded out to the pieces that are copied
+    const RowSpan span_k = row_span<16>(block0, blocks, 2 * WK), span_v = row_span<16>(block0, blocks, 2 * WV), span_x = row_span<8>(block0, blocks, 1);
+    // byte offsets of this lane's rows within a tile; a block that the unit does not have is read as its first and ignored
+    const int off_k = g * L::kPitchK + (FULL ? c * KB * (2 * WK) : span_k.skew);
+    const int off_kx = L::kAtX + g * L::kPitchX + (FULL ? c * KB : span_x.skew);
+    const int val_block = FULL || g * VB < blocks ? g * VB : 0;
+    const int off_v = L::kAtV + 2 * c * L::kPitchV + span_v.skew + val_block * (2 * WV);
+    const int off_vx = L::kAtX + 2 * c * L::kPitchX + 2 * L::kScale + span_x.skew + val_block;
+
+    // Queues the copies of a tile whose token i has the slot that lane i (and i + 16) holds; negative slots are left out.
+    auto fetch = [&](uint8_t* to, int slot) {
+        auto rows = [&](auto width, const bdr_planes_t& pl, const RowSpan& sp, int at, auto pitch) {
+            constexpr int kPieces = decltype(width)::value * MAXB / 8;  // of a full unit's row: 16 bytes each
+            if constexpr (FULL) {
+                constexpr int kRows = 32 / kPieces;  // rows to an instruction
+                const int r0 = lane / kPieces, piece = lane - r0 * kPieces;
+#pragma unroll
+                for (int r = 0; r < 16; r += kRows) {
+                    const int from = __shfl_sync(0xFFFFFFFFu, slot, (r + r0) & 15);
+                    if (r0 < kRows && r + r0 < 16 && from >= 0)
+                        cp_async16(to + at + (r + r0) * decltype(pitch)::value + 16 * piece,
+                                   pl.elems + (uint64_t)(uint32_t)from * (uint32_t)pl.ld_elems + sp.from + 16 * piece);
+                }
+            } else {
+                const int pieces = sp.len / 16, inv = 65536 / pieces + 1;
+                for (int i = lane; i < (16 * pieces + 31) / 32 * 32; i += 32) {
+                    const int r = (i * inv) >> 16, piece = i - r * pieces;
+                    const int from = __shfl_sync(0xFFFFFFFFu, slot, r & 15);
+                    if (r < 16 && from >= 0)
+                        cp_async16(to + at + r * decltype(pitch)::value + 16 * piece,
+                                   pl.elems + (uint64_t)(uint32_t)from * (uint32_t)pl.ld_elems + sp.from + 16 * piece);
+                }
+            }
+        };
+        rows(std::integral_constant<int, WK>{}, a.k, span_k, 0, std::integral_constant<int, L::kPitchK>{});
+        rows(std::integral_constant<int, WV>{}, a.v, span_v, L::kAtV, std::integral_constant<int, L::kPitchV>{});
+        // scales: lanes 0 .. 15 the exponents, lanes 16 .. 31 the microexponents of their token
+        if (slot >= 0) {
+            const bool micro = lane >= 16;
+            const uint8_t* k = (micro ? a.k.micro : a.k.exps) + (uint64_t)(uint32_t)slot * (uint32_t)(micro ? a.k.ld_micro : a.k.ld_exps) + span_x.from;
+            const uint8_t* v = (micro ? a.v.micro : a.v.exps) + (uint64_t)(uint32_t)slot * (uint32_t)(micro ? a.v.ld_micro : a.v.ld_exps) + span_x.from;
+            uint8_t* x = to + L::kAtX + (lane & 15) * L::kPitchX + (micro ? L::kScale : 0);
+#pragma unroll
+            for (int i = 0; i < L::kScale; i += 8)
+                if (FULL || i < span_x.len) {
+                    cp_async8(x + i, k + i);
+                    cp_async8(x + 2 * L::kScale + i, v + i);
+                }
+        }
+    };
 
     // query head of a column, or -1
     auto head_of = [&](int col) {
         const int f = col / a.per_pass, i = pass * a.per_pass + (col - f * a.per_pass);
         return f < kv_n && i < a.group ? (kv0 + f) * a.group + i : -1;
     };
+    auto sync_all = [&] {  // where one set of warps works alone there is nobody to wait for but the queries' loader, the warp itself
+        if (a.tw > 1) __syncthreads();
+        else __syncwarp();
+    };
 
-    while (u < u_end) {
-        const SeqRange r = seq_range(a, b);
-        if (r.count == 0) { ++b; continue; }
-        const int t0 = (int)(u - prefix), t1 = (int)min((int64_t)r.count, u_end - prefix);
-
+    bool first_segment = true;
+    for (; seg.next(a); seg.advance(), first_segment = false) {
+        const int b = seg.b;
         // ---- queries into shared memory: [part][pair of steps][column group][lane].  Step 8 x + j of a lane holds elements 2j and 2j + 1 of
         // blocks 2x and 2x + 1 of its own: {2x: 2j, 2x+1: 2j}, {2x: 2j+1, 2x+1: 2j+1}.
-        if (live) {
+        if (tw == 0) {
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const int col = 8 * n + g, head = head_of(col), f = col / a.per_pass;
@@ -200,7 +330,7 @@ __global__ void __launch_bounds__(kAtThreads, MAXB == 8 && NT == 1 ? 2 : 1) mx_a
                 }
             }
         }
-        __syncwarp();
+        sync_all();
 
         float o[VB * 8][NT][4], ref[NT][2], sum[NT][2];
 #pragma unroll
@@ -212,104 +342,91 @@ __global__ void __launch_bounds__(kAtThreads, MAXB == 8 && NT == 1 ? 2 : 1) mx_a
 #pragma unroll
         for (int n = 0; n < NT; ++n) { ref[n][0] = ref[n][1] = kAtNone; sum[n][0] = sum[n][1] = 0.f; }
 
-        int tile = (r.first + t0) * a.tw + tw;
-        int tile_end = live ? min((r.first + t1) * a.tw, (r.end + 15) / 16) : 0;
-        while (tile < tile_end && tile * 16 + 16 <= r.start) tile += a.tw;
-
-        // slot of token 16 tile + lane (lanes 0 .. 15): -1 outside the range, -2 for a page that does not exist
+        // slot of token 16 tile + lane % 16: -1 outside the range, -2 for a page that does not exist
+        const int tile_end = seg.r.first + seg.t1;
         auto slot_of = [&](int t) {
             const int tok = 16 * t + (lane & 15);
             int slot = -1;
-            if (t < tile_end && tok >= r.start && tok < r.end) {
+            if (t < tile_end && tok >= seg.r.start && tok < seg.r.end) {
                 const int pg = (int)fastdiv((uint32_t)tok, a.page);
                 const int id = pg < a.max_pages ? __ldg(a.table + (int64_t)b * a.ld_table + pg) : -1;
                 const bool ok = id >= 0 && id < a.n_pages;
                 slot = ok ? id * (int)a.page.d + (tok - pg * (int)a.page.d) : -2;
-                if (!ok) atomicCAS(a.status, 0, (int)BDR_ERR_SIZE);
             }
             return slot;
         };
-        // the fetched bytes: keys of tokens g and g + 8, values of tokens 2c, 2c + 1, 2c + 8 and 2c + 9; exponents and
-        // microexponents of a lane's blocks in the bytes of one word
-        uint32_t kr[2][FULL ? KB * WK / 2 : KB * frag::Block<WK>::kWords];
-        uint32_t kf[2], km[2], vf[4], vm[4];
-        frag::Block<WV> vb[4][VB];
-        const uint8_t* const ke = a.k.elems + (block0 + c * KB) * (2 * WK);
-        const uint8_t* const kx = a.k.exps + block0 + c * KB;
-        const uint8_t* const ki = a.k.micro + block0 + c * KB;
-        const uint8_t* const ve = a.v.elems + (block0 + g * VB) * (2 * WV);
-        const uint8_t* const vx = a.v.exps + block0 + g * VB;
-        const uint8_t* const vi = a.v.micro + block0 + g * VB;
-        // A token outside the range reads slot 0; what it gives is replaced below.
-        auto load_keys = [&](int slots) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const uint32_t at = (uint32_t)max(__shfl_sync(0xFFFFFFFFu, slots, g + 8 * i), 0);
-                const uint8_t* e = ke + (uint64_t)at * (uint32_t)a.k.ld_elems;
-                const uint8_t* x = kx + (uint64_t)at * (uint32_t)a.k.ld_exps;
-                const uint8_t* m = ki + (uint64_t)at * (uint32_t)a.k.ld_micro;
-                if constexpr (FULL) {  // neighbouring blocks, all present: whole aligned words
-                    if constexpr (KB == 2) { kf[i] = __ldg(reinterpret_cast<const uint16_t*>(x)); km[i] = __ldg(reinterpret_cast<const uint16_t*>(m)); }
-                    else { kf[i] = __ldg(reinterpret_cast<const uint32_t*>(x)); km[i] = __ldg(reinterpret_cast<const uint32_t*>(m)); }
-                    if constexpr (WK == 8) {
-#pragma unroll
-                        for (int w = 0; w < KB; ++w) {
-                            const uint4 v = __ldg(reinterpret_cast<const uint4*>(e) + w);
-                            kr[i][4 * w] = v.x; kr[i][4 * w + 1] = v.y; kr[i][4 * w + 2] = v.z; kr[i][4 * w + 3] = v.w;
-                        }
-                    } else {
-#pragma unroll
-                        for (int w = 0; w < KB * WK / 2; ++w) kr[i][w] = __ldg(reinterpret_cast<const uint32_t*>(e) + w);
-                    }
-                } else {
-                    kf[i] = km[i] = 0;
-#pragma unroll
-                    for (int y = 0; y < KB; ++y) {
-                        if (c * KB + y < blocks) {
-                            constexpr int BW = frag::Block<WK>::kWords;
-                            const frag::Block<WK> blk = frag::load_block<WK>(e + y * (2 * WK));
-#pragma unroll
-                            for (int w = 0; w < BW; ++w) kr[i][y * BW + w] = blk.w[w];
-                            kf[i] |= (uint32_t)__ldg(x + y) << (8 * y);
-                            km[i] |= (uint32_t)__ldg(m + y) << (8 * y);
-                        }
-                    }
-                }
-            }
+        // tokens present (bits 0 .. 15) and tokens of bad pages (16 .. 31)
+        auto marks = [&](int slot) {
+            const uint32_t present = __ballot_sync(0xFFFFFFFFu, slot >= 0) & 0xFFFFu;
+            return present | (present == 0xFFFFu ? 0u : __ballot_sync(0xFFFFFFFFu, slot == -2) << 16);
         };
-        auto load_values = [&](int slots) {
+        int tile = seg.r.first + seg.t0 + tw, slot = slot_of(tile), to = 0;
+        uint32_t held[D];  // marks of the tiles in the ring, the present one first
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t at = (uint32_t)max(__shfl_sync(0xFFFFFFFFu, slots, 2 * c + (i & 1) + 8 * (i >> 1)), 0);
-                const uint8_t* e = ve + (uint64_t)at * (uint32_t)a.v.ld_elems;
-                const uint8_t* x = vx + (uint64_t)at * (uint32_t)a.v.ld_exps;
-                const uint8_t* m = vi + (uint64_t)at * (uint32_t)a.v.ld_micro;
-                if constexpr (!FULL) vf[i] = vm[i] = 0;
-#pragma unroll
-                for (int y = 0; y < VB; ++y) {
-                    if (FULL || g * VB + y < blocks) {
-                        vb[i][y] = frag::load_block<WV>(e + y * (2 * WV));
-                        const uint32_t f = __ldg(x + y), u = __ldg(m + y);
-                        if (FULL && y == 0) { vf[i] = f; vm[i] = u; }
-                        else { vf[i] |= f << (8 * y); vm[i] |= u << (8 * y); }
-                    }
-                }
-            }
-        };
-
-        int next = slot_of(tile), now = next;
-        if (tile < tile_end) {
-            load_keys(next);
-            load_values(next);
-            next = slot_of(tile + a.tw);
+        for (int i = 0; i + 1 < D; ++i) {
+            fetch(ring + to, slot);
+            cp_async_commit();
+            held[i] = marks(slot);
+            slot = slot_of(tile + (i + 1) * a.tw);
+            to += L::kBytes;
         }
+        int at = 0;
         for (; tile < tile_end; tile += a.tw) {
+            if (tile + (D - 1) * a.tw < tile_end) fetch(ring + to, slot);
+            cp_async_commit();
+            held[D - 1] = marks(slot);
+            slot = slot_of(tile + D * a.tw);
+            to = to + L::kBytes == D * L::kBytes ? 0 : to + L::kBytes;
+            cp_async_wait<D - 1>();
+            __syncwarp();  // every lane's pieces of the tile are in place
+            const uint8_t* const st = ring + at;
+            const uint32_t here = held[0];
+            at = at + L::kBytes == D * L::kBytes ? 0 : at + L::kBytes;
+#pragma unroll
+            for (int i = 0; i + 1 < D; ++i) held[i] = held[i + 1];
+            if (here >> 16 && lane == 0) atomicCAS(a.status, 0, (int)BDR_ERR_SIZE);
             // ---- scores
             float s[NT][4];
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
+            constexpr int BW = frag::Block<WK>::kWords;
+            uint32_t kr[2][FULL ? KB * WK / 2 : KB * BW], kf[2], km[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint8_t* e = st + off_k + 8 * i * L::kPitchK;
+                const uint8_t* x = st + off_kx + 8 * i * L::kPitchX;
+                if constexpr (FULL) {
+                    if constexpr (KB == 2) { kf[i] = *reinterpret_cast<const uint16_t*>(x); km[i] = *reinterpret_cast<const uint16_t*>(x + L::kScale); }
+                    else { kf[i] = *reinterpret_cast<const uint32_t*>(x); km[i] = *reinterpret_cast<const uint32_t*>(x + L::kScale); }
+                    if constexpr (WK == 8) {
+#pragma unroll
+                        for (int w = 0; w < KB; ++w) {
+                            const uint4 v = reinterpret_cast<const uint4*>(e)[w];
+                            kr[i][4 * w] = v.x; kr[i][4 * w + 1] = v.y; kr[i][4 * w + 2] = v.z; kr[i][4 * w + 3] = v.w;
+                        }
+                    } else {
+#pragma unroll
+                        for (int w = 0; w < KB * WK / 2; ++w) kr[i][w] = reinterpret_cast<const uint32_t*>(e)[w];
+                    }
+                } else {
+                    kf[i] = km[i] = 0;
+#pragma unroll
+                    for (int y = 0; y < KB; ++y) {
+                        const int blk = c * KB + y < blocks ? c * KB + y : 0;
+                        const int off = off_k + 8 * i * L::kPitchK + blk * (2 * WK);
+                        frag::Block<WK> v = shared_block<WK>(st, off);
+                        frag::align_block(v, (uint32_t)off);
+#pragma unroll
+                        for (int w = 0; w < BW; ++w) kr[i][y * BW + w] = v.w[w];
+                        if (c * KB + y < blocks) {
+                            kf[i] |= (uint32_t)x[blk] << (8 * y);
+                            km[i] |= (uint32_t)x[blk + L::kScale] << (8 * y);
+                        }
+                    }
+                }
+            }
             // Merged heads share the reduction: a NaN block of one head must not reach the others' columns through their zero
             // queries, so it is decoded as zeros and its head's scores are made NaN below.
             uint32_t spoilt[2] = {0, 0};  // per row: the unit's heads with such a block
@@ -339,21 +456,7 @@ __global__ void __launch_bounds__(kAtThreads, MAXB == 8 && NT == 1 ? 2 : 1) mx_a
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
                     sc[i] = frag::make_scales(frag::spread_bytes(kf[i] >> (16 * x)), frag::spread_bytes(km[i] >> (16 * x)));
-                if constexpr (!FULL) {
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-#pragma unroll
-                        for (int y = 2 * x; y < 2 * x + 2; ++y) {
-                            constexpr int BW = frag::Block<WK>::kWords;
-                            frag::Block<WK> blk;
-#pragma unroll
-                            for (int w = 0; w < BW; ++w) blk.w[w] = kr[i][y * BW + w];
-                            frag::align_block(blk, (uint32_t)((block0 + c * KB + y) * (2 * WK)));
-#pragma unroll
-                            for (int w = 0; w < BW; ++w) kr[i][y * BW + w] = blk.w[w];
-                        }
-                }
-                constexpr int kBits = FULL ? 16 * WK : 32 * frag::Block<WK>::kWords;  // from one block's stream to the next's
+                constexpr int kBits = FULL ? 16 * WK : 32 * BW;  // from one block's stream to the next's
                 const int b0 = 2 * x * kBits, b1 = b0 + kBits;
 #pragma unroll
                 for (int j = 0; j < 8; j += 2) {
@@ -373,6 +476,10 @@ __global__ void __launch_bounds__(kAtThreads, MAXB == 8 && NT == 1 ? 2 : 1) mx_a
                         }
                 }
             }
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[n][e] *= a.scale2;
             if (spoilt[0] | spoilt[1]) {
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
@@ -380,26 +487,47 @@ __global__ void __launch_bounds__(kAtThreads, MAXB == 8 && NT == 1 ? 2 : 1) mx_a
                     for (int e = 0; e < 4; ++e)
                         if (spoilt[e >> 1] >> ((8 * n + 2 * c + (e & 1)) / a.per_pass) & 1u) s[n][e] = __uint_as_float(0x7FC00000u);
             }
+            // ---- the tile's values
+            frag::Block<WV> vb[4][VB];
+            uint32_t vf[4], vm[4];
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+            for (int i = 0; i < 4; ++i) {
+                const int r = (i & 1) + 8 * (i >> 1);  // token 2c + r
+                const int off = off_v + r * L::kPitchV;
+                const uint8_t* x = st + off_vx + r * L::kPitchX;
+                if constexpr (VB == 1) {
+                    vb[i][0] = shared_block<WV>(st, off);
+                    vf[i] = x[0];
+                    vm[i] = x[L::kScale];
+                    if (!FULL && g >= blocks) vf[i] = 0;
+                } else {
+                    vf[i] = vm[i] = 0;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[n][e] *= a.scale2;
-            if (!__all_sync(0xFFFFFFFFu, now >= 0)) {  // a tile at an end of the range, or with a page that does not exist
+                    for (int y = 0; y < VB; ++y) {
+                        const int blk = FULL || g * VB + y < blocks ? y : 0;
+                        vb[i][y] = shared_block<WV>(st, off + blk * (2 * WV));
+                        if (FULL || g * VB + y < blocks) {
+                            vf[i] |= (uint32_t)x[blk] << (8 * y);
+                            vm[i] |= (uint32_t)x[blk + L::kScale] << (8 * y);
+                        }
+                    }
+                }
+            }
+            if (here != 0xFFFFu) {  // a tile at an end of the range, or with a page that does not exist
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const int slot = __shfl_sync(0xFFFFFFFFu, now, g + 8 * i);
+                    const int tok = g + 8 * i;
+                    const bool bad = here >> (16 + tok) & 1u;
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
                         for (int e = 2 * i; e < 2 * i + 2; ++e)
-                            if (slot < 0) s[n][e] = slot == -1 ? -INFINITY : __uint_as_float(0x7FC00000u);
+                            if (!(here >> tok & 1u)) s[n][e] = bad ? __uint_as_float(0x7FC00000u) : -INFINITY;
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i)  // zero blocks: a weight of zero times anything that a slot may hold would not do
-                    if (__shfl_sync(0xFFFFFFFFu, now, 2 * c + (i & 1) + 8 * (i >> 1)) < 0) vf[i] = 0;
+                for (int i = 0; i < 4; ++i)  // zero blocks: a weight of zero times whatever lies there would not do
+                    if (!(here >> (2 * c + (i & 1) + 8 * (i >> 1)) & 1u)) vf[i] = 0;
             }
-            const bool more = tile + a.tw < tile_end;
-            if (more) load_keys(next);
             // ---- softmax weights relative to the running references, t = log2 of a weight
             float t[NT][4], high = 0.f;
 #pragma unroll
@@ -452,7 +580,7 @@ __global__ void __launch_bounds__(kAtThreads, MAXB == 8 && NT == 1 ? 2 : 1) mx_a
 #pragma unroll
             for (int x = 0; x < VB; ++x) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) frag::align_block(vb[i][x], (uint32_t)((block0 + g * VB + x) * (2 * WV)));
+                for (int i = 0; i < 4; ++i) frag::align_block(vb[i][x], (uint32_t)(off_v + (FULL || g * VB + x < blocks ? x : 0) * (2 * WV)));  // row pitches are multiples of 16
                 const frag::Scales s0 = frag::make_scales((vf[0] >> (8 * x)) & 0xFFu, (vf[1] >> (8 * x)) & 0xFFu, (vm[0] >> (8 * x)) & 0xFFu, (vm[1] >> (8 * x)) & 0xFFu);
                 const frag::Scales s1 = frag::make_scales((vf[2] >> (8 * x)) & 0xFFu, (vf[3] >> (8 * x)) & 0xFFu, (vm[2] >> (8 * x)) & 0xFFu, (vm[3] >> (8 * x)) & 0xFFu);
 #pragma unroll
@@ -466,76 +594,88 @@ __global__ void __launch_bounds__(kAtThreads, MAXB == 8 && NT == 1 ? 2 : 1) mx_a
                         for (int part = PARTS - 1; part >= 0; --part) frag::mma_bf16(o[8 * x + j][n], a0, a1, a2, a3, pb[n][part][0], pb[n][part][1]);
                 }
             }
-            if (more) {
-                load_values(next);
-                now = next;
-                next = slot_of(tile + 2 * a.tw);
+            __syncwarp();  // the next copies may overwrite the tile
+        }
+        cp_async_wait<0>();
+
+        // ---- join the sets of warps: in each round the upper half hands its sums to the lower half
+        for (int half = a.tw / 2; half >= 1; half >>= 1) {
+            if (tw >= half && tw < 2 * half) {
+                float* to = reinterpret_cast<float*>(ring) + lane;
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) { to[64 * (2 * n + e)] = ref[n][e]; to[64 * (2 * n + e) + 32] = sum[n][e]; }
+#pragma unroll
+                for (int i = 0; i < VB * 8; ++i)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) to[128 * NT + 32 * ((i * NT + n) * 4 + e)] = o[i][n][e];
+            }
+            sync_all();
+            if (tw < half) {
+                const float* from = reinterpret_cast<const float*>(rings + (warp + half * a.hw) * kRing) + lane;
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float other = from[64 * (2 * n + e)], top = fmaxf(ref[n][e], other);
+                        const float f0 = exp2_approx(ref[n][e] - top), f1 = exp2_approx(other - top);
+                        ref[n][e] = top;
+                        sum[n][e] = sum[n][e] * f0 + from[64 * (2 * n + e) + 32] * f1;
+#pragma unroll
+                        for (int i = 0; i < VB * 8; ++i)
+#pragma unroll
+                            for (int h = e; h < 4; h += 2) o[i][n][h] = o[i][n][h] * f0 + from[128 * NT + 32 * ((i * NT + n) * 4 + h)] * f1;
+                    }
             }
         }
 
-        // ---- the segment's result: every warp's sums into shared memory, then joined over the token warps
-        float2* ml = reinterpret_cast<float2*>(os + 8 * NT * S::kOPitch);
+        // ---- the segment's result: lane (g, c) holds elements 16 (g VB + x) .. + 15 of columns 2c and 2c + 1
+        const bool whole = seg.t0 == 0 && seg.t1 == seg.r.count;
+        if (tw == 0) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                float l = sum[n][e];
+                for (int e = 0; e < 2; ++e) {
+                    float l = sum[n][e];
 #pragma unroll
-                for (int x = 4; x < 32; x <<= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, x);
-                const int col = 8 * n + 2 * c + e;
-                if (g == 0) ml[col] = make_float2(ref[n][e], l);
+                    for (int x = 4; x < 32; x <<= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, x);
+                    const int col = 8 * n + 2 * c + e, head = head_of(col), f = col / a.per_pass;
+                    if (head < 0) continue;
+                    const float norm = whole ? (l == 0.f ? 0.f : 2.f / l) : 2.f;  // the values were decoded halved
+                    const int64_t part = ((int64_t)blockIdx.x * 2 + (first_segment ? 0 : 1)) * a.n_q + head;
 #pragma unroll
-                for (int x = 0; x < VB; ++x)
+                    for (int x = 0; x < VB; ++x) {
+                        const int blk = g * VB + x - f * a.nb;
+                        if (blk < 0 || blk >= a.nb) continue;
+                        uint32_t v[16];
 #pragma unroll
-                    for (int j = 0; j < 8; j += 2)
-                        *reinterpret_cast<float4*>(os + col * S::kOPitch + (g * VB + x) * 16 + 2 * j) =
-                            make_float4(o[8 * x + j][n][e], o[8 * x + j][n][e + 2], o[8 * x + j + 1][n][e], o[8 * x + j + 1][n][e + 2]);
-            }
-        if (a.tw > 1) __syncthreads();
-        else __syncwarp();
-        const bool whole = t0 == 0 && t1 == r.count;
-        if (live) {
-            for (int col = tw; col < 8 * NT; col += a.tw) {
-                const int head = head_of(col);
-                if (head < 0) continue;
-                const int f = col / a.per_pass;
-                float m = kAtNone, l = 0.f;
-                for (int w = 0; w < a.tw; ++w)
-                    m = fmaxf(m, reinterpret_cast<float2*>(os_all + (hw + w * a.hw) * kOFloats + 8 * NT * S::kOPitch)[col].x);
-                for (int w = 0; w < a.tw; ++w) {
-                    const float2 x = reinterpret_cast<float2*>(os_all + (hw + w * a.hw) * kOFloats + 8 * NT * S::kOPitch)[col];
-                    l += x.y * exp2_approx(x.x - m);
-                }
-                const float norm = whole ? (l == 0.f ? 0.f : 2.f / l) : 2.f;  // the values were decoded halved
-                const int64_t part = ((int64_t)blockIdx.x * 2 + (first_segment ? 0 : 1)) * a.n_q + head;
-                for (int e = lane; e < a.d; e += 32) {
-                    float v = 0.f;
-                    for (int w = 0; w < a.tw; ++w) {
-                        const float* ow = os_all + (hw + w * a.hw) * kOFloats;
-                        const float mw = reinterpret_cast<const float2*>(ow + 8 * NT * S::kOPitch)[col].x;
-                        const float x = ow[col * S::kOPitch + f * a.d + e];
-                        v += x * exp2_approx(mw - m);
+                        for (int j = 0; j < 8; ++j) {
+                            v[2 * j] = __float_as_uint(o[8 * x + j][n][e] * norm);
+                            v[2 * j + 1] = __float_as_uint(o[8 * x + j][n][e + 2] * norm);
+                        }
+                        if (!whole) {
+                            store_slice_vec(a.part_o + part * a.d + 16 * blk, v);
+                        } else {
+                            T* out = static_cast<T*>(a.out) + (int64_t)b * a.ldo + (int64_t)head * a.d + 16 * blk;
+                            if constexpr (!F32) {
+#pragma unroll
+                                for (int j = 0; j < 16; ++j)
+                                    v[j] = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(__uint_as_float(v[j]))) << 16;
+                            }
+                            if (a.o_vec) store_slice_vec(out, v);
+                            else store_slice_guarded(out, 1, kSlice, v);
+                        }
                     }
-                    v *= norm;
-                    if (whole) {
-                        T* out = static_cast<T*>(a.out) + (int64_t)b * a.ldo + (int64_t)head * a.d + e;
-                        if constexpr (F32) *out = v;
-                        else *out = __float2bfloat16_rn(v);
-                    } else {
-                        a.part_o[part * a.d + e] = v;
+                    if (g == 0) {
+                        if (!whole) a.part_ml[part] = make_float2(ref[n][e], l);
+                        else if (a.lse) a.lse[(int64_t)b * a.n_q + head] = (ref[n][e] + log2f(l)) * 0.69314718055994531f;
                     }
                 }
-                if (lane == 0) {
-                    if (!whole) a.part_ml[part] = make_float2(m, l);
-                    else if (a.lse) a.lse[(int64_t)b * a.n_q + head] = (m + log2f(l)) * 0.69314718055994531f;
-                }
-            }
         }
-        if (a.tw > 1) __syncthreads();
-        else __syncwarp();
-        first_segment = false;
-        u = prefix + t1;
-        if (t1 == r.count) { prefix += r.count; ++b; }
+        sync_all();  // nobody overwrites the queries or the handed-over sums while others still read them
     }
 }
 
@@ -545,10 +685,13 @@ int launch_attn(const AttnArgs& a, int wv, int maxb, int nt, bool f32, bool full
 
 template <int WK, int WV, int MAXB, int NT, bool F32, bool FULL>
 int launch_attn_one(const AttnArgs& a, int groups, cudaStream_t st) {
-    using S = AttnShape<WK, WV, MAXB, NT, F32>;
+    using S = AttnShape<MAXB, NT, F32>;
+    constexpr int kRing = attn_ring_bytes<WK, WV, MAXB, NT, F32, FULL>();
+    static_assert(S::kMaxUnits * S::kQBytes + S::kWarps * kRing <= kAtSmemBytes, "queries and rings have to fit");
     static PerDevice once;
-    if (kernel_setup(once, mx_attn_decode_kernel<WK, WV, MAXB, NT, F32, FULL>, kAtThreads, S::kSmem) < 1) return BDR_ERR_CUDA;
-    mx_attn_decode_kernel<WK, WV, MAXB, NT, F32, FULL><<<dim3(a.workers, groups), kAtThreads, S::kSmem, st>>>(a);
+    if (kernel_setup(once, mx_attn_decode_kernel<WK, WV, MAXB, NT, F32, FULL>, S::kThreads, kAtSmemBytes) < 1) return BDR_ERR_CUDA;
+    const size_t smem = a.hw * S::kQBytes + S::kWarps * kRing;
+    mx_attn_decode_kernel<WK, WV, MAXB, NT, F32, FULL><<<dim3(a.workers, groups), S::kThreads, smem, st>>>(a);
     return cudaGetLastError() == cudaSuccess ? BDR_OK : BDR_ERR_CUDA;
 }
 

@@ -45,27 +45,13 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
     return d;
 }
 
-// 32-bit words that hold one block of W-bit codes, and the words a reader of a block at a two-byte boundary fetches: the
-// aligned words around it (16 or 10 or 6 bytes; never beyond the next four-byte boundary after the block)
+// 32-bit words that hold one block of W-bit codes.  A reader of a block at a two-byte boundary fetches the aligned words around
+// it (16 or 10 or 6 bytes; never beyond the next four-byte boundary after the block).
 template <int W> struct Block {
     static constexpr int kBytes = 2 * W;
     static constexpr int kWords = (kBytes + 3) / 4;
     uint32_t w[kWords];
 };
-
-template <int W>
-__device__ __forceinline__ Block<W> load_block(const uint8_t* p) {
-    Block<W> b;
-    if constexpr (W == 8) {
-        const uint4 v = __ldg(reinterpret_cast<const uint4*>(p));
-        b.w[0] = v.x; b.w[1] = v.y; b.w[2] = v.z; b.w[3] = v.w;
-    } else {
-        const uint32_t* q = reinterpret_cast<const uint32_t*>(reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)3);
-#pragma unroll
-        for (int i = 0; i < Block<W>::kWords; ++i) b.w[i] = __ldg(q + i);
-    }
-    return b;
-}
 
 // moves the stream of a block that was fetched from a two-byte boundary (off = its byte offset, or only the offset's low
 // bits) down to bit 0
