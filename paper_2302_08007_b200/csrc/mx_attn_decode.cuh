@@ -238,38 +238,46 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
     const int off_v = L::kAtV + 2 * c * L::kPitchV + span_v.skew + val_block * (2 * WV);
     const int off_vx = L::kAtX + 2 * c * L::kPitchX + 2 * L::kScale + span_x.skew + val_block;
 
-    // Queues the copies of a tile whose token i has the slot that lane i (and i + 16) holds; negative slots are left out.
-    auto fetch = [&](uint8_t* to, int slot) {
-        auto rows = [&](auto width, const bdr_planes_t& pl, const RowSpan& sp, int at, auto pitch) {
-            constexpr int kPieces = decltype(width)::value * MAXB / 8;  // of a full unit's row: 16 bytes each
+    // Where this lane's pieces come from: piece `lane % pieces` of every row's codes, and the exponents (lanes 0 .. 15) or
+    // microexponents (lanes 16 .. 31) of token lane % 16.  Kept in registers: the compiler would rather rebuild them per tile.
+    constexpr int kPiecesK = WK * MAXB / 8, kPiecesV = WV * MAXB / 8;  // 16-byte pieces of a full unit's row
+    const bool micro = lane >= 16;
+    const uint8_t* src_k = a.k.elems + span_k.from + (FULL ? lane % kPiecesK * 16 : 0);
+    const uint8_t* src_v = a.v.elems + span_v.from + (FULL ? lane % kPiecesV * 16 : 0);
+    const uint8_t* src_kx = (micro ? a.k.micro : a.k.exps) + span_x.from;
+    const uint8_t* src_vx = (micro ? a.v.micro : a.v.exps) + span_x.from;
+    uint32_t ld_kx = (uint32_t)(micro ? a.k.ld_micro : a.k.ld_exps), ld_vx = (uint32_t)(micro ? a.v.ld_micro : a.v.ld_exps);
+    asm volatile("" : "+l"(src_k), "+l"(src_v), "+l"(src_kx), "+l"(src_vx), "+r"(ld_kx), "+r"(ld_vx));
+    // Queues the copies of a tile whose token i has the slot that lane i (and i + 16) holds; ALL: every token is there, else
+    // tokens with negative slots are left out.
+    auto fetch = [&](uint8_t* to, int slot, auto all) {
+        constexpr bool ALL = decltype(all)::value;
+        auto rows = [&](auto pieces_, const uint8_t* src, uint32_t ld, int len, uint8_t* dst, auto pitch_) {
+            constexpr int kPitch = decltype(pitch_)::value;
             if constexpr (FULL) {
-                constexpr int kRows = 32 / kPieces;  // rows to an instruction
-                const int r0 = lane / kPieces, piece = lane - r0 * kPieces;
+                constexpr int kPieces = decltype(pieces_)::value, kRows = 32 / kPieces;  // rows to an instruction
+                const int r0 = lane / kPieces;
+                uint8_t* const d = dst + r0 * kPitch + 16 * (lane - r0 * kPieces);
 #pragma unroll
                 for (int r = 0; r < 16; r += kRows) {
                     const int from = __shfl_sync(0xFFFFFFFFu, slot, (r + r0) & 15);
-                    if (r0 < kRows && r + r0 < 16 && from >= 0)
-                        cp_async16(to + at + (r + r0) * decltype(pitch)::value + 16 * piece,
-                                   pl.elems + (uint64_t)(uint32_t)from * (uint32_t)pl.ld_elems + sp.from + 16 * piece);
+                    if ((32 % kPieces == 0 || r0 < kRows) && (r + kRows <= 16 || r + r0 < 16) && (ALL || from >= 0))
+                        cp_async16(d + r * kPitch, src + (uint64_t)(uint32_t)from * ld);
                 }
             } else {
-                const int pieces = sp.len / 16, inv = 65536 / pieces + 1;
+                const int pieces = len / 16, inv = 65536 / pieces + 1;
                 for (int i = lane; i < (16 * pieces + 31) / 32 * 32; i += 32) {
                     const int r = (i * inv) >> 16, piece = i - r * pieces;
                     const int from = __shfl_sync(0xFFFFFFFFu, slot, r & 15);
-                    if (r < 16 && from >= 0)
-                        cp_async16(to + at + r * decltype(pitch)::value + 16 * piece,
-                                   pl.elems + (uint64_t)(uint32_t)from * (uint32_t)pl.ld_elems + sp.from + 16 * piece);
+                    if (r < 16 && (ALL || from >= 0)) cp_async16(dst + r * kPitch + 16 * piece, src + (uint64_t)(uint32_t)from * ld + 16 * piece);
                 }
             }
         };
-        rows(std::integral_constant<int, WK>{}, a.k, span_k, 0, std::integral_constant<int, L::kPitchK>{});
-        rows(std::integral_constant<int, WV>{}, a.v, span_v, L::kAtV, std::integral_constant<int, L::kPitchV>{});
-        // scales: lanes 0 .. 15 the exponents, lanes 16 .. 31 the microexponents of their token
-        if (slot >= 0) {
-            const bool micro = lane >= 16;
-            const uint8_t* k = (micro ? a.k.micro : a.k.exps) + (uint64_t)(uint32_t)slot * (uint32_t)(micro ? a.k.ld_micro : a.k.ld_exps) + span_x.from;
-            const uint8_t* v = (micro ? a.v.micro : a.v.exps) + (uint64_t)(uint32_t)slot * (uint32_t)(micro ? a.v.ld_micro : a.v.ld_exps) + span_x.from;
+        rows(std::integral_constant<int, kPiecesK>{}, src_k, (uint32_t)a.k.ld_elems, span_k.len, to, std::integral_constant<int, L::kPitchK>{});
+        rows(std::integral_constant<int, kPiecesV>{}, src_v, (uint32_t)a.v.ld_elems, span_v.len, to + L::kAtV, std::integral_constant<int, L::kPitchV>{});
+        if (ALL || slot >= 0) {
+            const uint8_t* k = src_kx + (uint64_t)(uint32_t)slot * ld_kx;
+            const uint8_t* v = src_vx + (uint64_t)(uint32_t)slot * ld_vx;
             uint8_t* x = to + L::kAtX + (lane & 15) * L::kPitchX + (micro ? L::kScale : 0);
 #pragma unroll
             for (int i = 0; i < L::kScale; i += 8)
@@ -364,7 +372,7 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
         uint32_t held[D];  // marks of the tiles in the ring, the present one first
 #pragma unroll
         for (int i = 0; i + 1 < D; ++i) {
-            fetch(ring + to, slot);
+            fetch(ring + to, slot, std::false_type{});
             cp_async_commit();
             held[i] = marks(slot);
             slot = slot_of(tile + (i + 1) * a.tw);
@@ -372,9 +380,10 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
         }
         int at = 0;
         for (; tile < tile_end; tile += a.tw) {
-            if (tile + (D - 1) * a.tw < tile_end) fetch(ring + to, slot);
-            cp_async_commit();
             held[D - 1] = marks(slot);
+            if (held[D - 1] == 0xFFFFu) fetch(ring + to, slot, std::true_type{});
+            else if (tile + (D - 1) * a.tw < tile_end) fetch(ring + to, slot, std::false_type{});
+            cp_async_commit();
             slot = slot_of(tile + D * a.tw);
             to = to + L::kBytes == D * L::kBytes ? 0 : to + L::kBytes;
             cp_async_wait<D - 1>();
