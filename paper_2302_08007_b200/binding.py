@@ -84,8 +84,14 @@ class Planes:
 
     def __setattr__(self, name, value):
         object.__setattr__(self, name, value)
-        if name != "_c":
+        if name in ("exps", "micro", "elems"):
             object.__setattr__(self, "_c", None)
+
+    def lines(self) -> int:
+        """Lines that every plane holds."""
+        if self._c is None:
+            self.c()
+        return self._lines
 
     def __reduce__(self):
         return Planes, (self.exps, self.micro, self.elems)
@@ -96,6 +102,7 @@ class Planes:
             self._c = _Planes(self.exps.data_ptr(), self.micro.data_ptr() if self.micro.numel() else None,
                               self.elems.data_ptr(), self.exps.stride(0), self.micro.stride(0) if self.micro.numel() else 0,
                               self.elems.stride(0))
+            self._lines = min(t.shape[0] for t in (self.exps, self.micro, self.elems) if t.numel()) if self.exps.numel() else 0
         return self._c
 
 
@@ -236,9 +243,18 @@ def _dt(t: torch.Tensor) -> int:
     raise TypeError("tensor dtype must be float32 or bfloat16")
 
 
-def _stream(stream) -> C.c_void_p:
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return C.c_void_p(s.cuda_stream)
+# The current stream's handle without building a Stream object (3 us of a call that takes 5 in all); torch versions without this
+# entry take the ordinary way.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_raw_device = getattr(torch._C, "_cuda_getDevice", None)
+
+
+def _stream(stream):
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is not None and _raw_device is not None and torch.cuda.is_initialized():
+        return _raw_stream(_raw_device())
+    return torch.cuda.current_stream().cuda_stream
 
 
 def _as2d(t: torch.Tensor):
@@ -472,21 +488,25 @@ def _on_gpu(*tensors):
 
 def mx_gemv(cfg_w: Config, w: Planes, N: int, K: int, x: torch.Tensor, y: torch.Tensor, stream=None) -> torch.Tensor:
     """y[T,N] = x[T,K] @ deq(w)[N,K]^T for a few rows of x (float32 or bfloat16; y likewise) and weights packed along K."""
-    x2, y2 = _as2d(x), _as2d(y)
-    _on_gpu(x, y, w.exps, w.micro, w.elems)
-    if x2.shape[1] != K or y2.shape != (x2.shape[0], N) or min(w.exps.shape[0], w.micro.shape[0], w.elems.shape[0]) < N:
-        raise ValueError("x is [T, K], y is [T, N] and the planes hold N lines")
+    x2, y2 = x if x.dim() == 2 else x.unsqueeze(0), y if y.dim() == 2 else y.unsqueeze(0)
+    (T, k), (ldx, sx), (ldy, sy) = x2.shape, x2.stride(), y2.stride()
+    if k != K or y2.shape != (T, N) or (sx != 1 and K > 1) or (sy != 1 and N > 1) or w.lines() < N:
+        raise ValueError("x is [T, K], y is [T, N], rows contiguous, and the planes hold N lines")
+    _on_gpu(x, y, w.elems)
     c, p = cfg_w.c(), w.c()
-    _check(lib().mx_gemv(C.addressof(c), C.addressof(p), N, K, x2.data_ptr(), _dt(x2), max(x2.stride(0), K), x2.shape[0], y2.data_ptr(),
-                         _dt(y2), max(y2.stride(0), N), _stream(stream)), "mx_gemv")
+    _check(lib().mx_gemv(C.addressof(c), C.addressof(p), N, K, x2.data_ptr(), _dt(x2), ldx if ldx > K else K, T, y2.data_ptr(), _dt(y2),
+                         ldy if ldy > N else N, _stream(stream)), "mx_gemv")
     return y
 
 
 def _heads(t: torch.Tensor, what: str):
-    """Pitch of a [tokens, heads, head_dim] tensor whose tokens are contiguous."""
-    if t.dim() != 3 or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
-        raise ValueError("%s: expected [tokens, heads, head_dim] with contiguous heads" % what)
-    return max(t.stride(0), t.shape[1] * t.shape[2])
+    """Shape and token pitch of a [tokens, heads, head_dim] tensor whose tokens are contiguous."""
+    if t.dim() != 3:
+        raise ValueError("%s: expected [tokens, heads, head_dim]" % what)
+    (n, h, d), (s0, s1, s2) = shape, _ = t.shape, t.stride()
+    if s2 != 1 or (s1 != d and h > 1):
+        raise ValueError("%s: expected contiguous heads" % what)
+    return shape, s0 if s0 > h * d else h * d
 
 
 def mx_kv_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, positions: torch.Tensor | None = None,
@@ -496,10 +516,11 @@ def mx_kv_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.
     """Rotates the keys k [T, n_kv, head_dim] (cos, sin: float32 [n_pos, rot_dim / 2] tables, positions: int64 [T]; None: no
     rotation), quantizes them and v, and writes the lines of `slots` (int64 [T], negative = padding).  Optionally rotates the
     queries q into q_out and returns the quantized values in k_dq / v_dq."""
-    T = k.shape[0]
-    _on_gpu(k, v, slots, positions, cos, sin, q, q_out, k_dq, v_dq, cache.k.elems)
-    shape = (T, cache.n_kv, cache.head_dim)
-    if k.shape != shape or v.shape != shape or v.dtype != k.dtype:
+    shape, ldk = _heads(k, "k")
+    vshape, ldv = _heads(v, "v")
+    T, dtype = shape[0], k.dtype
+    _on_gpu(k, v, slots, cache.k.elems)
+    if vshape != shape or shape[1] != cache.n_kv or shape[2] != cache.head_dim or v.dtype != dtype:
         raise ValueError("k and v are [tokens, n_kv, head_dim] of one dtype")
     if slots.dtype != torch.int64 or slots.shape != (T,) or not slots.is_contiguous():
         raise ValueError("slots: contiguous int64 [tokens]")
@@ -507,26 +528,30 @@ def mx_kv_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.
     if cos is not None:
         if sin is None or positions is None:
             raise ValueError("cos, sin and positions go together")
-        if cos.dtype != torch.float32 or sin.dtype != torch.float32 or cos.dim() != 2 or cos.shape != sin.shape or cos.stride(1) != 1 or \
-                sin.stride() != cos.stride():
+        _on_gpu(cos, sin, positions)
+        (n_pos, half), pitch = cos.shape, cos.stride()
+        if cos.dtype != torch.float32 or sin.dtype != torch.float32 or sin.shape != cos.shape or sin.stride() != pitch or (pitch[1] != 1 and half > 1):
             raise ValueError("cos, sin: float32 [n_pos, rot_dim / 2] with one pitch")
         if positions.dtype != torch.int64 or positions.shape != (T,) or not positions.is_contiguous():
             raise ValueError("positions: contiguous int64 [tokens]")
-        rot = _Rotation(cos.data_ptr(), sin.data_ptr(), positions.data_ptr(), max(cos.stride(0), cos.shape[1]), cos.shape[0],
-                        2 * cos.shape[1], int(interleaved))
+        rotation = _Rotation(cos.data_ptr(), sin.data_ptr(), positions.data_ptr(), max(pitch[0], half), n_pos, 2 * half, int(interleaved))
+        rot = C.addressof(rotation)
     n_q = ldq = ldo = 0
     if q is not None:
-        if q_out is None or q_out.shape != q.shape or q_out.dtype != k.dtype or q.dtype != k.dtype or q.dim() != 3 or q.shape[0] != T or \
-                q.shape[2] != cache.head_dim:
+        if q_out is None:
+            raise ValueError("q needs q_out")
+        _on_gpu(q, q_out)
+        (tq, n_q, dq), ldq = _heads(q, "q")
+        oshape, ldo = _heads(q_out, "q_out")
+        if tq != T or dq != cache.head_dim or oshape != q.shape or q.dtype != dtype or q_out.dtype != dtype:
             raise ValueError("q and q_out are [tokens, n_q, head_dim] of k's dtype")
-        n_q, ldq, ldo = q.shape[1], _heads(q, "q"), _heads(q_out, "q_out")
     for t in (k_dq, v_dq):
-        if t is not None and (t.shape != shape or t.dtype != k.dtype or not t.is_contiguous()):
+        if t is not None and (t.shape != shape or t.dtype != dtype or not t.is_contiguous() or not t.is_cuda):
             raise ValueError("k_dq, v_dq: contiguous, like k")
-    _check(lib().mx_kv_append(cache._ref, k.data_ptr(), _heads(k, "k"), v.data_ptr(), _heads(v, "v"), _dt(k), T, slots.data_ptr(),
-                              C.addressof(rot) if rot is not None else None, q.data_ptr() if n_q else None, ldq, n_q,
-                              q_out.data_ptr() if n_q else None, ldo, k_dq.data_ptr() if k_dq is not None else None,
-                              v_dq.data_ptr() if v_dq is not None else None, _stream(stream)), "mx_kv_append")
+    _check(lib().mx_kv_append(cache._ref, k.data_ptr(), ldk, v.data_ptr(), ldv, _dt(k), T, slots.data_ptr(), rot,
+                              q.data_ptr() if n_q else None, ldq, n_q, q_out.data_ptr() if n_q else None, ldo,
+                              k_dq.data_ptr() if k_dq is not None else None, v_dq.data_ptr() if v_dq is not None else None,
+                              _stream(stream)), "mx_kv_append")
     return cache
 
 
@@ -540,22 +565,22 @@ def mx_attn_decode(cache: KVCache, q: torch.Tensor, page_table: torch.Tensor, le
     """out [B, n_q, head_dim] = attention of one query token per sequence, q [B, n_q, head_dim], over the cached positions
     t < lengths[b] (int32 [B]; the last `window` of them when window > 0) whose pages are page_table[b] (int32 [B, max_pages]).
     lse: float32 [B, n_q].  scale: head_dim ** -0.5 when None."""
-    _on_gpu(q, page_table, lengths, out, workspace, lse, cache.k.elems)
-    B, n_q = q.shape[0], q.shape[1]
-    ldq, ldo = _heads(q, "q"), _heads(out, "out")
-    if q.shape[2] != cache.head_dim or out.shape != q.shape or out.dtype != q.dtype:
+    _on_gpu(q, page_table, lengths, out, workspace, cache.k.elems)
+    (B, n_q, d), ldq = _heads(q, "q")
+    oshape, ldo = _heads(out, "out")
+    if d != cache.head_dim or oshape != q.shape or out.dtype != q.dtype:
         raise ValueError("q and out are [sequences, n_q, head_dim] of one dtype")
-    if page_table.dtype != torch.int32 or page_table.dim() != 2 or page_table.shape[0] != B or page_table.stride(1) != 1 and page_table.shape[1] > 1:
+    (rows, max_pages), (ld_table, step) = page_table.shape, page_table.stride()
+    if page_table.dtype != torch.int32 or rows != B or (step != 1 and max_pages > 1):
         raise ValueError("page_table: int32 [sequences, max_pages]")
     if lengths.dtype != torch.int32 or lengths.shape != (B,) or not lengths.is_contiguous():
         raise ValueError("lengths: contiguous int32 [sequences]")
-    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (B, n_q) or not lse.is_contiguous()):
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (B, n_q) or not lse.is_contiguous() or not lse.is_cuda):
         raise ValueError("lse: contiguous float32 [sequences, n_q]")
     _check(lib().mx_attn_decode(cache._ref, q.data_ptr(), ldq, _dt(q), B, n_q, page_table.data_ptr(),
-                                max(page_table.stride(0), page_table.shape[1]), page_table.shape[1], lengths.data_ptr(),
-                                cache.head_dim ** -0.5 if scale is None else scale, window, out.data_ptr(), ldo,
-                                lse.data_ptr() if lse is not None else None, workspace.data_ptr(),
-                                workspace.numel() * workspace.element_size(), _stream(stream)), "mx_attn_decode")
+                                ld_table if ld_table > max_pages else max_pages, max_pages, lengths.data_ptr(),
+                                d ** -0.5 if scale is None else scale, window, out.data_ptr(), ldo, lse.data_ptr() if lse is not None else None,
+                                workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream)), "mx_attn_decode")
     return out
 
 
