@@ -65,6 +65,15 @@ __device__ __forceinline__ void align_block(Block<W>& b, uint32_t off) {
     }
 }
 
+// One three-input logic instruction.  Written out where it matters: the compiler splits (a & b) | c with two constants in two.
+template <int TABLE>
+__device__ __forceinline__ uint32_t lop3(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t d;
+    asm("lop3.b32 %0, %1, %2, %3, %4;" : "=r"(d) : "r"(a), "r"(b), "r"(c), "n"(TABLE));
+    return d;
+}
+constexpr int kAndOr = 0xEA, kXorAnd = 0x78;  // (a & b) | c,  a ^ (b & c)
+
 // The exponents and microexponents of the two blocks of a word: S0 holds F << 7 per half, micro the eight shifts of each
 // block in the low byte of its half.
 struct Scales {
@@ -102,7 +111,7 @@ __device__ __forceinline__ uint32_t decode_word(const uint32_t (&a)[NA], int a0,
     if constexpr (W == 8) {
         const int x = e & 3;  // the code in both bytes of its half: the sign bit is where it belongs
         const uint32_t c = __byte_perm(a[(a0 >> 5) + (e >> 2)], b[(b0 >> 5) + (e >> 2)], ((4 + x) << 12) | ((4 + x) << 8) | (x << 4) | x);
-        mag = c & 0x007F007Fu;
+        mag = lop3<kAndOr>(c, 0x007F007Fu, 0x3F803F80u);
         sign = c;
     } else {
         constexpr int kGroup = 15 / W;
@@ -112,12 +121,12 @@ __device__ __forceinline__ uint32_t decode_word(const uint32_t (&a)[NA], int a0,
         const uint32_t G = __byte_perm(wa, wb, (hb ? 0x7600 : 0x5400) | (ha ? 0x32 : 0x10));
         const int up = 8 - W - W * r;  // brings the magnitude to the top of the mantissa
         constexpr uint32_t kMag = (0x7Fu & ~((1u << (8 - W)) - 1u)) * 0x00010001u;
-        mag = (up >= 0 ? G << (up >= 0 ? up : 0) : G >> (up < 0 ? -up : 0)) & kMag;
+        mag = lop3<kAndOr>(up >= 0 ? G << (up >= 0 ? up : 0) : G >> (up < 0 ? -up : 0), kMag, 0x3F803F80u);
         sign = G << (16 - W - W * r);
     }
     uint32_t d;
-    asm("{.reg .b32 n; neg.bf16x2 n, %2; fma.rn.bf16x2 %0, %1, %2, n;}" : "=r"(d) : "r"(mag | 0x3F803F80u), "r"(S));
-    return d ^ (sign & 0x80008000u);
+    asm("{.reg .b32 n; neg.bf16x2 n, %2; fma.rn.bf16x2 %0, %1, %2, n;}" : "=r"(d) : "r"(mag), "r"(S));
+    return lop3<kXorAnd>(d, sign, 0x80008000u);
 }
 
 // The scale word of sub-block j: tau off the exponent field of each half.  Written as the multiply-add it is meant to be: a
