@@ -34,7 +34,8 @@
 namespace bdr {
 
 constexpr int kAtSmemBytes = 227 * 1024;
-constexpr float kAtSlack = 8.f;     // a softmax weight relative to the running reference stays below 2^8
+constexpr float kAtLift = 32.f;      // weights carry the factor 2^32 that the first way of decoding the values leaves out
+constexpr float kAtSlack = 8.f;      // a weight stays below 2^8 times that
 constexpr float kAtNone = -3.0e38f;  // the reference before the first score: below every finite score, and finite itself
 
 struct AttnArgs {
@@ -420,7 +421,8 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
                         for (int w = 0; w < KB * WK / 2; ++w) kr[i][w] = reinterpret_cast<const uint32_t*>(e)[w];
                     }
                 } else {
-                    kf[i] = km[i] = 0;
+                    kf[i] = 0x7F7F7F7Fu;  // absent blocks: an ordinary exponent, zero queries
+                    km[i] = 0;
 #pragma unroll
                     for (int y = 0; y < KB; ++y) {
                         const int blk = c * KB + y < blocks ? c * KB + y : 0;
@@ -430,16 +432,39 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
 #pragma unroll
                         for (int w = 0; w < BW; ++w) kr[i][y * BW + w] = v.w[w];
                         if (c * KB + y < blocks) {
-                            kf[i] |= (uint32_t)x[blk] << (8 * y);
+                            kf[i] ^= (uint32_t)(0x7F ^ x[blk]) << (8 * y);
                             km[i] |= (uint32_t)x[blk + L::kScale] << (8 * y);
                         }
                     }
                 }
             }
+            uint32_t vf[4], vm[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = (i & 1) + 8 * (i >> 1);  // token 2c + r
+                const uint8_t* x = st + off_vx + r * L::kPitchX;
+                if constexpr (FULL && VB == 1) {
+                    vf[i] = x[0];
+                    vm[i] = x[L::kScale];
+                } else {
+                    vf[i] = VB == 1 ? 0x7Fu : 0x7F7Fu;
+                    vm[i] = 0;
+#pragma unroll
+                    for (int y = 0; y < VB; ++y)
+                        if (FULL || g * VB + y < blocks) {
+                            vf[i] ^= (uint32_t)(0x7F ^ x[y]) << (8 * y);
+                            vm[i] |= (uint32_t)x[y + L::kScale] << (8 * y);
+                        }
+                }
+            }
+            bool ordinary;
+            if constexpr (VB == 1) ordinary = frag::all_fast((kf[0] & 0xFFFFu) + (kf[1] << 16)) && frag::all_fast(vf[0] + (vf[1] << 8) + (vf[2] << 16) + (vf[3] << 24));
+            else ordinary = frag::all_fast(kf[0]) && frag::all_fast(kf[1]) && frag::all_fast(vf[0] + (vf[1] << 16)) && frag::all_fast(vf[2] + (vf[3] << 16));
+            const bool fast = __all_sync(0xFFFFFFFFu, ordinary);
             // Merged heads share the reduction: a NaN block of one head must not reach the others' columns through their zero
             // queries, so it is decoded as zeros and its head's scores are made NaN below.
             uint32_t spoilt[2] = {0, 0};  // per row: the unit's heads with such a block
-            if (a.merge > 1) {
+            if (!fast && a.merge > 1) {
                 bool any = false;
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
@@ -459,36 +484,42 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
                     }
                 }
             }
+            auto scores = [&](auto way) {
+                constexpr bool FAST = decltype(way)::value;
 #pragma unroll
-            for (int x = 0; x < KB / 2; ++x) {
-                frag::Scales sc[2];
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    sc[i] = frag::make_scales(frag::spread_bytes(kf[i] >> (16 * x)), frag::spread_bytes(km[i] >> (16 * x)));
-                constexpr int kBits = FULL ? 16 * WK : 32 * BW;  // from one block's stream to the next's
-                const int b0 = 2 * x * kBits, b1 = b0 + kBits;
-#pragma unroll
-                for (int j = 0; j < 8; j += 2) {
-                    uint32_t y[2][4];  // rows g and g + 8, elements 2j .. 2j + 3
+                for (int x = 0; x < KB / 2; ++x) {
+                    frag::Scales sc[2];
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
+                        sc[i] = frag::make_scales<FAST>(frag::spread_bytes(kf[i] >> (16 * x)), frag::spread_bytes(km[i] >> (16 * x)));
+                    constexpr int kBits = FULL ? 16 * WK : 32 * BW;  // from one block's stream to the next's
+                    const int b0 = 2 * x * kBits, b1 = b0 + kBits;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            y[i][e] = frag::decode_word<WK>(kr[i], b0, kr[i], b1, 2 * j + e, frag::scale_word(sc[i], j + (e >> 1)));
+                    for (int j = 0; j < 8; j += 2) {
+                        uint32_t y[2][4];  // rows g and g + 8, elements 2j .. 2j + 3
 #pragma unroll
-                    for (int part = PARTS - 1; part >= 0; --part)
+                        for (int i = 0; i < 2; ++i)
 #pragma unroll
-                        for (int n = 0; n < NT; ++n) {
-                            const uint4 qv = qs[((part * MAXB / 2 + 4 * x + j / 2) * NT + n) * 32 + lane];
-                            frag::mma_bf16(s[n], y[0][0], y[1][0], y[0][1], y[1][1], qv.x, qv.y);
-                            frag::mma_bf16(s[n], y[0][2], y[1][2], y[0][3], y[1][3], qv.z, qv.w);
-                        }
+                            for (int e = 0; e < 4; ++e)
+                                y[i][e] = frag::decode_word<WK, FAST>(kr[i], b0, kr[i], b1, 2 * j + e, frag::scale_word(sc[i], j + (e >> 1)));
+#pragma unroll
+                        for (int part = PARTS - 1; part >= 0; --part)
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) {
+                                const uint4 qv = qs[((part * MAXB / 2 + 4 * x + j / 2) * NT + n) * 32 + lane];
+                                frag::mma_bf16(s[n], y[0][0], y[1][0], y[0][1], y[1][1], qv.x, qv.y);
+                                frag::mma_bf16(s[n], y[0][2], y[1][2], y[0][3], y[1][3], qv.z, qv.w);
+                            }
+                    }
                 }
-            }
+            };
+            if (fast) scores(std::true_type{});
+            else scores(std::false_type{});
+            const float scale = fast ? a.scale2 * frag::kFastFactor : a.scale2;
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[n][e] *= a.scale2;
+                for (int e = 0; e < 4; ++e) s[n][e] *= scale;
             if (spoilt[0] | spoilt[1]) {
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
@@ -498,30 +529,14 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
             }
             // ---- the tile's values
             frag::Block<WV> vb[4][VB];
-            uint32_t vf[4], vm[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int r = (i & 1) + 8 * (i >> 1);  // token 2c + r
-                const int off = off_v + r * L::kPitchV;
-                const uint8_t* x = st + off_vx + r * L::kPitchX;
-                if constexpr (VB == 1) {
-                    vb[i][0] = shared_block<WV>(st, off);
-                    vf[i] = x[0];
-                    vm[i] = x[L::kScale];
-                    if (!FULL && g >= blocks) vf[i] = 0;
-                } else {
-                    vf[i] = vm[i] = 0;
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-                    for (int y = 0; y < VB; ++y) {
-                        const int blk = FULL || g * VB + y < blocks ? y : 0;
-                        vb[i][y] = shared_block<WV>(st, off + blk * (2 * WV));
-                        if (FULL || g * VB + y < blocks) {
-                            vf[i] |= (uint32_t)x[blk] << (8 * y);
-                            vm[i] |= (uint32_t)x[blk + L::kScale] << (8 * y);
-                        }
-                    }
+                for (int y = 0; y < VB; ++y) {
+                    const int off = off_v + ((i & 1) + 8 * (i >> 1)) * L::kPitchV + (FULL || g * VB + y < blocks ? y : 0) * (2 * WV);
+                    vb[i][y] = shared_block<WV>(st, off);
+                    frag::align_block(vb[i][y], (uint32_t)off);
                 }
-            }
             if (here != 0xFFFFu) {  // a tile at an end of the range, or with a page that does not exist
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
@@ -534,10 +549,10 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
                             if (!(here >> tok & 1u)) s[n][e] = bad ? __uint_as_float(0x7FC00000u) : -INFINITY;
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i)  // zero blocks: a weight of zero times whatever lies there would not do
-                    if (!(here >> (2 * c + (i & 1) + 8 * (i >> 1)) & 1u)) vf[i] = 0;
+                for (int i = 0; i < 4; ++i)  // finite values: a weight of zero times an infinity that may lie there would not do
+                    if (!(here >> (2 * c + (i & 1) + 8 * (i >> 1)) & 1u)) vf[i] = 0x7F7Fu;
             }
-            // ---- softmax weights relative to the running references, t = log2 of a weight
+            // ---- softmax weights relative to the running references, t = log2 of a weight (lifted by kAtLift)
             float t[NT][4], high = 0.f;
 #pragma unroll
             for (int n = 0; n < NT; ++n)
@@ -546,7 +561,7 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
                     t[n][e] = s[n][e] - ref[n][e & 1];
                     high = fmaxf(high, t[n][e]);
                 }
-            if (__any_sync(0xFFFFFFFFu, high > kAtSlack)) {
+            if (__any_sync(0xFFFFFFFFu, high > kAtLift + kAtSlack)) {
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -554,7 +569,7 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
                         float top = fmaxf(s[n][e], s[n][e + 2]);
 #pragma unroll
                         for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
-                        top = fmaxf(top, ref[n][e]);
+                        top = fmaxf(top - kAtLift, ref[n][e]);
                         const float f = exp2_approx(ref[n][e] - top);
                         ref[n][e] = top;
                         sum[n][e] *= f;
@@ -576,6 +591,7 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     float lo = p[2 * h], hi = p[2 * h + 1];
+                    if (!fast) { lo *= 1.f / frag::kFastFactor; hi *= 1.f / frag::kFastFactor; }
 #pragma unroll
                     for (int part = 0; part < PARTS; ++part) {
                         const uint32_t w = pack_bf16x2(lo, hi);
@@ -586,23 +602,26 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
                 }
             }
             // ---- output
+            auto output = [&](auto way) {
+                constexpr bool FAST = decltype(way)::value;
 #pragma unroll
-            for (int x = 0; x < VB; ++x) {
+                for (int x = 0; x < VB; ++x) {
+                    const frag::Scales s0 = frag::make_scales<FAST>((vf[0] >> (8 * x)) & 0xFFu, (vf[1] >> (8 * x)) & 0xFFu, (vm[0] >> (8 * x)) & 0xFFu, (vm[1] >> (8 * x)) & 0xFFu);
+                    const frag::Scales s1 = frag::make_scales<FAST>((vf[2] >> (8 * x)) & 0xFFu, (vf[3] >> (8 * x)) & 0xFFu, (vm[2] >> (8 * x)) & 0xFFu, (vm[3] >> (8 * x)) & 0xFFu);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) frag::align_block(vb[i][x], (uint32_t)(off_v + (FULL || g * VB + x < blocks ? x : 0) * (2 * WV)));  // row pitches are multiples of 16
-                const frag::Scales s0 = frag::make_scales((vf[0] >> (8 * x)) & 0xFFu, (vf[1] >> (8 * x)) & 0xFFu, (vm[0] >> (8 * x)) & 0xFFu, (vm[1] >> (8 * x)) & 0xFFu);
-                const frag::Scales s1 = frag::make_scales((vf[2] >> (8 * x)) & 0xFFu, (vf[3] >> (8 * x)) & 0xFFu, (vm[2] >> (8 * x)) & 0xFFu, (vm[3] >> (8 * x)) & 0xFFu);
+                    for (int j = 0; j < 8; ++j) {
+                        const uint32_t w0 = frag::scale_word(s0, j), w1 = frag::scale_word(s1, j);
+                        const uint32_t a0 = frag::decode_word<WV, FAST>(vb[0][x].w, 0, vb[1][x].w, 0, 2 * j, w0), a1 = frag::decode_word<WV, FAST>(vb[0][x].w, 0, vb[1][x].w, 0, 2 * j + 1, w0);
+                        const uint32_t a2 = frag::decode_word<WV, FAST>(vb[2][x].w, 0, vb[3][x].w, 0, 2 * j, w1), a3 = frag::decode_word<WV, FAST>(vb[2][x].w, 0, vb[3][x].w, 0, 2 * j + 1, w1);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const uint32_t w0 = frag::scale_word(s0, j), w1 = frag::scale_word(s1, j);
-                    const uint32_t a0 = frag::decode_word<WV>(vb[0][x].w, 0, vb[1][x].w, 0, 2 * j, w0), a1 = frag::decode_word<WV>(vb[0][x].w, 0, vb[1][x].w, 0, 2 * j + 1, w0);
-                    const uint32_t a2 = frag::decode_word<WV>(vb[2][x].w, 0, vb[3][x].w, 0, 2 * j, w1), a3 = frag::decode_word<WV>(vb[2][x].w, 0, vb[3][x].w, 0, 2 * j + 1, w1);
+                        for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int part = PARTS - 1; part >= 0; --part) frag::mma_bf16(o[8 * x + j][n], a0, a1, a2, a3, pb[n][part][0], pb[n][part][1]);
+                            for (int part = PARTS - 1; part >= 0; --part) frag::mma_bf16(o[8 * x + j][n], a0, a1, a2, a3, pb[n][part][0], pb[n][part][1]);
+                    }
                 }
-            }
+            };
+            if (fast) output(std::true_type{});
+            else output(std::false_type{});
             __syncwarp();  // the next copies may overwrite the tile
         }
         cp_async_wait<0>();
@@ -653,6 +672,7 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
                     for (int x = 4; x < 32; x <<= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, x);
                     const int col = 8 * n + 2 * c + e, head = head_of(col), f = col / a.per_pass;
                     if (head < 0) continue;
+                    l *= 1.f / frag::kFastFactor;  // the weights' factor; the values' own is in the sums
                     const float norm = whole ? (l == 0.f ? 0.f : 2.f / l) : 2.f;  // the values were decoded halved
                     const int64_t part = ((int64_t)blockIdx.x * 2 + (first_segment ? 0 : 1)) * a.n_q + head;
 #pragma unroll
@@ -679,8 +699,8 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
                         }
                     }
                     if (g == 0) {
-                        if (!whole) a.part_ml[part] = make_float2(ref[n][e], l);
-                        else if (a.lse) a.lse[(int64_t)b * a.n_q + head] = (ref[n][e] + log2f(l)) * 0.69314718055994531f;
+                        if (!whole) a.part_ml[part] = make_float2(ref[n][e] + kAtLift, l);
+                        else if (a.lse) a.lse[(int64_t)b * a.n_q + head] = (ref[n][e] + kAtLift + log2f(l)) * 0.69314718055994531f;
                     }
                 }
         }

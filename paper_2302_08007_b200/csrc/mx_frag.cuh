@@ -8,18 +8,24 @@
 // is given whole 16-element blocks (contiguous bytes of the packed line) instead of the scattered pairs of the
 // instruction's own order.
 //
-// Decoding: an element is (-1)^s q 2^(F-127-tau-(m-1)), two neighbouring elements share tau.  With f = q / 2^m (q moved to
-// the top of the seven bf16 mantissa bits, so 1 + f is 0x3F80 | bits) and S = 2^(F-127-tau), whose bf16 pattern is simply
-// (F - tau) << 7,
-//     fma(1 + f, S, -S) = f S = value / 2       exactly (f S is a multiple of 2^-133, a bf16 number for every F - tau >= 1),
-// for every finite block without a special case at either end of the exponent range: nothing overflows because the value is
-// halved, F = 255 makes S infinite and the result NaN, and F = 0 (zeros, and values below 2^-126, which count as zero here)
-// makes S zero.  The kernels double their results once, in fp32.
+// Decoding.  An element is (-1)^s q 2^(F-127-tau-(m-1)); two neighbouring elements share tau.  With f = q / 2^m, q at the top
+// of the seven mantissa bits of a bf16 number, and S = 2^(F-127-tau), whose bf16 pattern is simply (F - tau) << 7, value / 2 is
+// f S.  Two ways to it, both exact:
+//   blocks with 96 <= F <= 159 (largest element between 2^-31 and 2^33): the mantissa bits alone, under the code's sign and a zero
+//     exponent, are the subnormal +-f 2^-126; one multiplication by 2^(F-tau-33), a normal number, gives value / 2 * 2^-32
+//     (the kernels put the factor 2^33 back in fp32);
+//   any block: fma(1 + f, S, -S) = f S (1 + f is 0x3F80 | bits), then the sign.  Nothing overflows because the value is halved,
+//     F = 255 makes S infinite and the result NaN, and F = 0 (zeros, and values below 2^-126, which count as zero here) makes
+//     S zero.
+// A warp takes the first way when all of its blocks allow it.
 //
 // The two halves of a decoded word are the same element of TWO blocks (two blocks of a line, or one block of two lines),
-// not two neighbours: a sub-block's two elements then use the same scale word, which halves the work on microexponents
-// (the integer/logic pipe, at half the rate of the FMA pipe, is what decoding keeps busy: 3.5 of its instructions per word
-// of MX9 or MX4, 4.2 for MX6), and a product over lines gets its pairs of lines without a transposition.
+// not two neighbours: a sub-block's two elements then use the same scale word, which halves the work on microexponents, and
+// a product over lines gets its pairs of lines without a transposition.  Codes of 3 and 5 bits are first spread to bytes with
+// the sign in bit 7 (four codes at a time: 2 or 3 shifts and as many selections); a byte permutation then puts one code into
+// both bytes of each half, where the sign is the half's sign bit and the magnitude is in the mantissa.  The integer/logic
+// pipe, which issues at half the rate of the FMA pipe, is what decoding keeps busy: per word 2.5 of its instructions for
+// MX9, 3.9 for MX6, 3.4 for MX4, of 4.0, 6.5 and 6.0 in all on the first way.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -72,62 +78,31 @@ __device__ __forceinline__ uint32_t lop3(uint32_t a, uint32_t b, uint32_t c) {
     asm("lop3.b32 %0, %1, %2, %3, %4;" : "=r"(d) : "r"(a), "r"(b), "r"(c), "n"(TABLE));
     return d;
 }
-constexpr int kAndOr = 0xEA, kXorAnd = 0x78;  // (a & b) | c,  a ^ (b & c)
+constexpr int kAndOr = 0xEA, kXorAnd = 0x78, kSelect = 0xD8;  // (a & b) | c,  a ^ (b & c),  c ? b : a
 
-// The exponents and microexponents of the two blocks of a word: S0 holds F << 7 per half, micro the eight shifts of each
-// block in the low byte of its half.
+// The exponents and microexponents of the two blocks of a word: S0 holds the scale of an unshifted sub-block per half, micro
+// the eight shifts of each block in the low byte of its half.
 struct Scales {
     uint32_t S0, micro;
 };
-// F2, micro2: one byte per half.  Zero blocks and Inf/NaN blocks (F = 0, 255) keep their scale whatever their
-// microexponents say.
+constexpr float kFastFactor = 4294967296.f;  // 2^32: what the first way leaves out
+// F2, micro2: one byte per half.
+template <bool FAST>
 __device__ __forceinline__ Scales make_scales(uint32_t F2, uint32_t micro2) {
+    if constexpr (FAST) return {F2 * 0x80u + (94u << 7) * 0x00010001u, micro2};
+    // zero blocks and Inf/NaN blocks (F = 0, 255) keep their scale whatever their microexponents say
     uint32_t one;
     asm("min.u16x2 %0, %1, %2;" : "=r"(one) : "r"((F2 + 0x00010001u) & 0x00FE00FEu), "r"(0x00010001u));
     return {F2 * 0x80u, micro2 & (one * 0xFFu)};
 }
+template <bool FAST>
 __device__ __forceinline__ Scales make_scales(uint32_t Fa, uint32_t Fb, uint32_t ma, uint32_t mb) {
-    return make_scales(Fa + (Fb << 16), ma + (mb << 16));
+    return make_scales<FAST>(Fa + (Fb << 16), ma + (mb << 16));
 }
 // bytes 0 and 1 of a word, one per half
 __device__ __forceinline__ uint32_t spread_bytes(uint32_t w) { return __byte_perm(w, 0u, 0x4140); }
-
-// sixteen bits of a stream at a bit offset (a constant once loops are unrolled), in the low half or, when `high` says so, in
-// the high half of the result; the other half holds leftovers
-template <int NW>
-__device__ __forceinline__ uint32_t window(const uint32_t (&s)[NW], int bit, bool& high) {
-    const int wi = bit >> 5, sh = bit & 31;
-    high = sh == 16;
-    if (sh == 0 || sh == 16) return s[wi];
-    return sh > 16 && wi + 1 < NW ? __funnelshift_r(s[wi], s[wi + 1 < NW ? wi + 1 : wi], sh) : s[wi] >> sh;
-}
-
-// Elements e of two blocks whose streams of W-bit codes start at bits a0 of `a` and b0 of `b`, halved (see above), with the
-// scale word S of the element's sub-block.  Streams of 3- and 5-bit codes are taken in groups of five and three codes (15 bits):
-// one group of each block side by side serves the group's elements.
-template <int W, int NA, int NB>
-__device__ __forceinline__ uint32_t decode_word(const uint32_t (&a)[NA], int a0, const uint32_t (&b)[NB], int b0, int e, uint32_t S) {
-    uint32_t mag, sign;
-    if constexpr (W == 8) {
-        const int x = e & 3;  // the code in both bytes of its half: the sign bit is where it belongs
-        const uint32_t c = __byte_perm(a[(a0 >> 5) + (e >> 2)], b[(b0 >> 5) + (e >> 2)], ((4 + x) << 12) | ((4 + x) << 8) | (x << 4) | x);
-        mag = lop3<kAndOr>(c, 0x007F007Fu, 0x3F803F80u);
-        sign = c;
-    } else {
-        constexpr int kGroup = 15 / W;
-        const int i = e / kGroup, r = e - i * kGroup;
-        bool ha, hb;
-        const uint32_t wa = window(a, a0 + 15 * i, ha), wb = window(b, b0 + 15 * i, hb);
-        const uint32_t G = __byte_perm(wa, wb, (hb ? 0x7600 : 0x5400) | (ha ? 0x32 : 0x10));
-        const int up = 8 - W - W * r;  // brings the magnitude to the top of the mantissa
-        constexpr uint32_t kMag = (0x7Fu & ~((1u << (8 - W)) - 1u)) * 0x00010001u;
-        mag = lop3<kAndOr>(up >= 0 ? G << (up >= 0 ? up : 0) : G >> (up < 0 ? -up : 0), kMag, 0x3F803F80u);
-        sign = G << (16 - W - W * r);
-    }
-    uint32_t d;
-    asm("{.reg .b32 n; neg.bf16x2 n, %2; fma.rn.bf16x2 %0, %1, %2, n;}" : "=r"(d) : "r"(mag), "r"(S));
-    return lop3<kXorAnd>(d, sign, 0x80008000u);
-}
+// whether all four bytes of F4 are exponents of the first way: their top three bits are 011 or 100
+__device__ __forceinline__ bool all_fast(uint32_t F4) { return (lop3<0x18>(F4, F4 << 1, F4 << 2) & 0x80808080u) == 0x80808080u; }
 
 // The scale word of sub-block j: tau off the exponent field of each half.  Written as the multiply-add it is meant to be: a
 // compiler would shift and subtract, on the pipe that is busy.
@@ -135,6 +110,54 @@ __device__ __forceinline__ uint32_t scale_word(const Scales& s, int j) {
     uint32_t S;
     asm("mad.lo.u32 %0, %1, %2, %3;" : "=r"(S) : "r"(s.micro & (0x00010001u << j)), "r"(0u - (0x80u >> j)), "r"(s.S0));
     return S;
+}
+
+// bits [bit, bit + 32) of a stream (a constant offset once loops are unrolled); bits beyond its words are zero or leftovers
+template <int NW>
+__device__ __forceinline__ uint32_t stream_bits(const uint32_t (&s)[NW], int bit) {
+    const int wi = bit >> 5, sh = bit & 31;
+    if (sh == 0) return s[wi];
+    return wi + 1 < NW ? __funnelshift_r(s[wi], s[wi + 1 < NW ? wi + 1 : wi], sh) : s[wi] >> sh;
+}
+
+// Four codes of the block whose stream of W-bit codes starts at bit `at`, one per byte, the sign in bit 7 and the magnitude below it
+// (other bits hold leftovers).  Word u of the four of a block: codes 4u .. 4u + 3; for 3-bit codes the even (u even) or odd (u odd)
+// ones of codes 8 (u / 2) .. + 7.
+template <int W, int NW>
+__device__ __forceinline__ uint32_t code_bytes(const uint32_t (&s)[NW], int at, int u) {
+    if constexpr (W == 8) {
+        return s[(at >> 5) + u];
+    } else if constexpr (W == 5) {
+        const int bit = at + 20 * u;  // the first code goes to bits 3 .. 7
+        const uint32_t v = bit % 32 < 3 ? stream_bits(s, bit) << 3 : stream_bits(s, bit - 3);
+        const uint32_t w = lop3<kSelect>(v, v << 6, 0xFFFF0000u);
+        return lop3<kSelect>(w, w << 3, 0xFF00FF00u);
+    } else {
+        static_assert(W == 3, "code widths of Table II");
+        const int bit = at + 24 * (u >> 1);  // the first code goes to bits 1 .. 3
+        const uint32_t v = bit % 32 < 1 ? stream_bits(s, bit) << 1 : stream_bits(s, bit - 1);
+        const uint32_t w = lop3<kSelect>(v, v << 4, 0xFFFF0000u);
+        const uint32_t x = lop3<kSelect>(w, w << 2, 0xFF00FF00u);
+        const uint32_t y = lop3<kSelect>(x, x << 1, 0xF0F0F0F0u);
+        return u & 1 ? y : y << 4;
+    }
+}
+
+// Elements e of two blocks whose streams of W-bit codes start at bits a0 of `a` and b0 of `b`, halved (see above), with the
+// scale word S of the element's sub-block.
+template <int W, bool FAST, int NA, int NB>
+__device__ __forceinline__ uint32_t decode_word(const uint32_t (&a)[NA], int a0, const uint32_t (&b)[NB], int b0, int e, uint32_t S) {
+    constexpr uint32_t kMag = (0x7Fu & ~((1u << (8 - W)) - 1u)) * 0x00010001u;
+    const int u = W == 3 ? 2 * (e >> 3) + (e & 1) : e >> 2, x = W == 3 ? (e >> 1) & 3 : e & 3;
+    // the code in both bytes of its half
+    const uint32_t c = __byte_perm(code_bytes<W>(a, a0, u), code_bytes<W>(b, b0, u), ((4 + x) << 12) | ((4 + x) << 8) | (x << 4) | x);
+    uint32_t d;
+    if constexpr (FAST) {
+        asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(c & (kMag | 0x80008000u)), "r"(S));
+        return d;
+    }
+    asm("{.reg .b32 n; neg.bf16x2 n, %2; fma.rn.bf16x2 %0, %1, %2, n;}" : "=r"(d) : "r"(lop3<kAndOr>(c, kMag, 0x3F803F80u)), "r"(S));
+    return lop3<kXorAnd>(d, c, 0x80008000u);
 }
 
 // A 24-bit fp32 value as the sum of three bf16 values (truncated eight bits at a time, so the sum is exact; parts below the

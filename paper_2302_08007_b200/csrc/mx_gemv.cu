@@ -4,10 +4,13 @@
 // Every packed weight is read once and used for T columns, so the kernel is bound by the bytes of W as long as decoding keeps
 // up.  A warp owns 16 rows of W and walks along K in steps of 256 elements: lane (g, c) of the matrix instruction's layout
 // takes blocks 4c .. 4c+3 of rows g and g + 8 (64 contiguous elements each: 24, 40 or 64 bytes of codes and one word each of
-// exponents and microexponents), decodes them in registers and feeds 16 matrix instructions.  The activations sit in shared
-// memory in the order those instructions want them, as bf16; a 32-bit activation is split exactly into three bf16 columns,
-// which costs nothing while the eight columns of an instruction are not full.  The warps of a CTA split into rw row tiles
-// times kw shares of K; the shares are added in shared memory in a fixed order.
+// exponents and microexponents), decodes them in registers and feeds 16 matrix instructions, while the next step's bytes are on
+// their way into a second set of registers.  The activations sit in shared memory in the order those instructions want them,
+// as bf16; a 32-bit activation is split exactly into three bf16 columns, which costs nothing while the eight columns of an
+// instruction are not full.
+// One CTA per SM stays for the whole call (the activations are staged once) and its warps form groups of kw that share a
+// tile's K; a group's sums are added in shared memory in a fixed order.  The host picks kw so that the longest group's
+// walk is shortest: few large groups balance few rows, many small ones need fewer joins.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -19,10 +22,15 @@
 
 namespace bdr {
 
-constexpr int kGvThreads = 256, kGvWarps = kGvThreads / 32;
 constexpr int kGvStep = 256;                 // elements of K per warp step
-constexpr int kGvSmem = 72 * 1024;           // most shared memory for activations: three CTAs fit on an SM
+constexpr int kGvSmem = 227 * 1024;
 constexpr int kGvMaxCols = 64;               // columns (tokens, or thirds of a 32-bit token) of one pass
+
+// warps of a CTA: what the registers allow
+template <int NT> struct GemvShape {
+    static constexpr int kWarps = NT <= 2 ? 16 : 8, kThreads = 32 * kWarps;
+    static constexpr int kRed = kWarps * 8 * NT * 16 * 4;  // bytes of all warps' sums of a tile
+};
 
 struct GemvArgs {
     bdr_planes_t w;
@@ -33,8 +41,8 @@ struct GemvArgs {
     int tokens, tokens_per_pass;
     int x32, y32;        // 32-bit activations / results (else bf16)
     int xvec;            // activations may be read four at a time
-    int rw;              // row tiles of a CTA (a power of two up to 8)
-    int phase_steps;     // steps whose activations fit in shared memory at once
+    int kw;              // warps that share a tile's K (a power of two, at most the steps there are)
+    int phase_steps;     // steps whose activations fit in shared memory at once (a multiple of kw)
 };
 
 // four consecutive blocks of one row
@@ -64,14 +72,15 @@ __device__ __forceinline__ void load_run(Run<W>& r, const bdr_planes_t& p, int64
                 r.w[2 * i] = v.x; r.w[2 * i + 1] = v.y;
             }
         }
-    } else {  // the end of a line: block by block, absent blocks are zero blocks
-        r.exps = r.micro = 0;
+    } else {  // the end of a line: block by block, absent blocks are zeros with an ordinary exponent
+        r.exps = 0x7F7F7F7Fu;
+        r.micro = 0;
 #pragma unroll
         for (int i = 0; i < 2 * W; ++i) r.w[i] = 0;
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
             if (block + b < nb) {
-                r.exps |= (uint32_t)__ldg(ex + b) << (8 * b);
+                r.exps ^= (uint32_t)(0x7F ^ __ldg(ex + b)) << (8 * b);
                 r.micro |= (uint32_t)__ldg(mi + b) << (8 * b);
 #pragma unroll
                 for (int h = 0; h < W; ++h) {
@@ -90,7 +99,7 @@ __device__ __forceinline__ void load_run(Run<W>& r, const bdr_planes_t& p, int64
 template <bool X32>
 __device__ __forceinline__ void stage_x(const GemvArgs& a, uint16_t* xs, int64_t pitch, int t0, int nt, int64_t k0, int span) {
     const int per = span / 8;
-    for (int i = threadIdx.x; i < nt * per; i += kGvThreads) {
+    for (int i = threadIdx.x; i < nt * per; i += blockDim.x) {
         const int t = i / per, v = i - t * per;
         const int s = v >> 5, c = (v >> 3) & 3, p = (v >> 2) & 1, h = v & 3;
         const int64_t k = k0 + (int64_t)s * kGvStep + 64 * c + 32 * p + 4 * h;
@@ -140,9 +149,9 @@ __device__ __forceinline__ void stage_x(const GemvArgs& a, uint16_t* xs, int64_t
 
 // One step of a warp.  The tensor core's fp32 additions are cut off rather than rounded, so a step's products are summed from
 // zero and then added to the totals with a rounded addition: 16 instructions in a chain instead of K / 16.
-template <int W, int NT>
-__device__ __forceinline__ void run_step(const Run<W>& r0, const Run<W>& r1, const uint16_t* xs, int64_t pitch, int cols, int lane,
-                                         float (&acc)[NT][4]) {
+template <int W, int NT, bool FAST>
+__device__ __forceinline__ void run_step_as(const Run<W>& r0, const Run<W>& r1, const uint16_t* xs, int64_t pitch, int cols, int lane,
+                                            float (&acc)[NT][4]) {
     const int g = lane >> 2, c = lane & 3;
     float part[NT][4];
 #pragma unroll
@@ -151,16 +160,16 @@ __device__ __forceinline__ void run_step(const Run<W>& r0, const Run<W>& r1, con
         for (int i = 0; i < 4; ++i) part[n][i] = 0.f;
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
-        const frag::Scales s0 = frag::make_scales(frag::spread_bytes(r0.exps >> (16 * p)), frag::spread_bytes(r0.micro >> (16 * p)));
-        const frag::Scales s1 = frag::make_scales(frag::spread_bytes(r1.exps >> (16 * p)), frag::spread_bytes(r1.micro >> (16 * p)));
+        const frag::Scales s0 = frag::make_scales<FAST>(frag::spread_bytes(r0.exps >> (16 * p)), frag::spread_bytes(r0.micro >> (16 * p)));
+        const frag::Scales s1 = frag::make_scales<FAST>(frag::spread_bytes(r1.exps >> (16 * p)), frag::spread_bytes(r1.micro >> (16 * p)));
         const int a0 = 32 * W * p, b0 = a0 + 16 * W;
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
             uint32_t y0[4], y1[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                y0[e] = frag::decode_word<W>(r0.w, a0, r0.w, b0, 4 * h + e, frag::scale_word(s0, 2 * h + (e >> 1)));
-                y1[e] = frag::decode_word<W>(r1.w, a0, r1.w, b0, 4 * h + e, frag::scale_word(s1, 2 * h + (e >> 1)));
+                y0[e] = frag::decode_word<W, FAST>(r0.w, a0, r0.w, b0, 4 * h + e, frag::scale_word(s0, 2 * h + (e >> 1)));
+                y1[e] = frag::decode_word<W, FAST>(r1.w, a0, r1.w, b0, 4 * h + e, frag::scale_word(s1, 2 * h + (e >> 1)));
             }
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
@@ -174,19 +183,27 @@ __device__ __forceinline__ void run_step(const Run<W>& r0, const Run<W>& r1, con
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[n][i] += part[n][i];
+        for (int i = 0; i < 4; ++i) acc[n][i] = FAST ? fmaf(part[n][i], frag::kFastFactor, acc[n][i]) : acc[n][i] + part[n][i];
+}
+template <int W, int NT>
+__device__ __forceinline__ void run_step(const Run<W>& r0, const Run<W>& r1, const uint16_t* xs, int64_t pitch, int cols, int lane,
+                                         float (&acc)[NT][4]) {
+    if (__all_sync(0xFFFFFFFFu, frag::all_fast(r0.exps) && frag::all_fast(r1.exps))) run_step_as<W, NT, true>(r0, r1, xs, pitch, cols, lane, acc);
+    else run_step_as<W, NT, false>(r0, r1, xs, pitch, cols, lane, acc);
 }
 
 template <int W, int NT, bool X32>
-__global__ void __launch_bounds__(kGvThreads, NT <= 2 ? 3 : 2) mx_gemv_kernel(const GemvArgs a) {
+__global__ void __launch_bounds__(GemvShape<NT>::kThreads, 1) mx_gemv_kernel(const GemvArgs a) {
+    constexpr int kWarps = GemvShape<NT>::kWarps;
     extern __shared__ __align__(16) uint8_t smem[];
-    uint16_t* xs = reinterpret_cast<uint16_t*>(smem);
+    float* const red = reinterpret_cast<float*>(smem);
+    uint16_t* const xs = reinterpret_cast<uint16_t*>(smem + 2 * GemvShape<NT>::kRed);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
-    const int rw = a.rw, kw = kGvWarps / rw, my_r = warp & (rw - 1), my_k = warp / rw;
-    const int64_t n0 = (int64_t)blockIdx.x * (16 * rw);
+    const int kw = a.kw, my_k = warp & (kw - 1), group = warp / kw, groups = kWarps / kw;
     const int t0 = blockIdx.y * a.tokens_per_pass, nt = min(a.tokens_per_pass, a.tokens - t0), cols = X32 ? 3 * nt : nt;
     const int nb = (int)((a.k + 15) / 16), steps = (nb + 15) / 16;
-    const int64_t row0 = min(n0 + 16 * my_r + g, a.n - 1), row1 = min(n0 + 16 * my_r + g + 8, a.n - 1);
+    const int64_t tiles = (a.n + 15) / 16, stride = (int64_t)gridDim.x * groups, first = (int64_t)blockIdx.x * groups;
+    const int rounds = (int)((tiles - first + stride - 1) / stride);  // of the CTA's first group; the others may have one fewer
     const int64_t pitch = (int64_t)min(a.phase_steps, steps) * kGvStep + 32;
     float acc[NT][4];
 #pragma unroll
@@ -194,63 +211,95 @@ __global__ void __launch_bounds__(kGvThreads, NT <= 2 ? 3 : 2) mx_gemv_kernel(co
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[n][i] = 0.f;
 
-    // The next step's words are fetched once the present one is decoded; the SM's other warps cover the wait.
-    Run<W> run[2];
-    auto fetch = [&](int s) {
-        load_run<W>(run[0], a.w, row0, 16 * s + 4 * c, nb);
-        load_run<W>(run[1], a.w, row1, 16 * s + 4 * c, nb);
+    auto fetch = [&](Run<W>(&r)[2], int64_t tile, int s) {
+        load_run<W>(r[0], a.w, min(16 * tile + g, a.n - 1), 16 * s + 4 * c, nb);
+        load_run<W>(r[1], a.w, min(16 * tile + g + 8, a.n - 1), 16 * s + 4 * c, nb);
     };
-    int s = my_k;
-    if (s < steps) fetch(s);
-    for (int p0 = 0; p0 < steps; p0 += a.phase_steps) {
-        const int p1 = min(p0 + a.phase_steps, steps);
-        if (p0) __syncthreads();  // everyone is done with the phase before
-        stage_x<X32>(a, xs, pitch, t0, nt, (int64_t)p0 * kGvStep, (p1 - p0) * kGvStep);
-        __syncthreads();
-        for (; s < p1; s += kw) {
-            run_step<W, NT>(run[0], run[1], xs + (int64_t)(s - p0) * kGvStep, pitch, cols, lane, acc);
-            if (s + kw < steps) fetch(s + kw);
+    Run<W> even[2], odd[2];
+    int64_t tile = first + group;
+    int s = my_k, round = 0;
+    bool use_odd = false;
+    if (tile < tiles) fetch(even, tile, s);
+    // one step, with the next one (of this tile or of the group's next) fetched ahead
+    auto advance = [&](Run<W>(&now)[2], Run<W>(&next)[2], const uint16_t* xp) {
+        const bool last = s + kw >= steps;
+        if (!last || tile + stride < tiles) fetch(next, last ? tile + stride : tile, last ? my_k : s + kw);
+        run_step<W, NT>(now[0], now[1], xp + (int64_t)s * kGvStep, pitch, cols, lane, acc);
+        s += kw;
+    };
+    for (; round < rounds; ++round, tile += stride) {
+        const bool active = tile < tiles;
+        for (int p0 = 0; p0 < steps; p0 += a.phase_steps) {
+            const int p1 = min(p0 + a.phase_steps, steps);
+            if (a.phase_steps < steps || round == 0) {
+                if (p0 || round) __syncthreads();  // everyone is done with the activations before
+                stage_x<X32>(a, xs, pitch, t0, nt, (int64_t)p0 * kGvStep, (p1 - p0) * kGvStep);
+                __syncthreads();
+            }
+            if (!active) continue;
+            const uint16_t* const xp = xs - (int64_t)p0 * kGvStep;
+            while (s < p1) {
+                if (!use_odd) advance(even, odd, xp);
+                else advance(odd, even, xp);
+                use_odd = !use_odd;
+            }
         }
-    }
-    // the shares of K, added in order; each row tile's results are [column][16 rows]
-    __syncthreads();
-    float* red = reinterpret_cast<float*>(smem);
-    const int tile = 8 * NT * 16;
+        if (!active) continue;
+        s = my_k;
+        // the shares of K, added in order; a warp's sums are [column][16 rows].  Two buffers: the sums of a tile are read before
+        // anyone passes the barrier of the next, and only then overwritten.
+        float* const mine = red + (round & 1) * (GemvShape<NT>::kRed / 4) + warp * (8 * NT * 16);
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) red[(my_k * rw + my_r) * tile + (8 * n + 2 * c + (i & 1)) * 16 + g + 8 * (i >> 1)] = acc[n][i];
-    __syncthreads();
-    for (int i = threadIdx.x; i < nt * 16 * rw; i += kGvThreads) {
-        const int t = i / (16 * rw), r = i - t * (16 * rw);
-        if (n0 + r >= a.n) continue;
-        float v = 0.f;
-        for (int part = 0; part < (X32 ? 3 : 1); ++part) {
-            const int col = X32 ? 3 * t + (2 - part) : t;  // smallest part first
-            for (int q = 0; q < kw; ++q) v += red[(q * rw + (r >> 4)) * tile + col * 16 + (r & 15)];
+            for (int i = 0; i < 4; ++i) {
+                mine[(8 * n + 2 * c + (i & 1)) * 16 + g + 8 * (i >> 1)] = acc[n][i];
+                acc[n][i] = 0.f;
+            }
+        if (kw == 1) __syncwarp();
+        else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(32 * kw) : "memory");
+        const float* const from = mine - my_k * (8 * NT * 16);
+        for (int i = my_k * 32 + lane; i < nt * 16; i += kw * 32) {
+            const int t = i >> 4, r = i & 15;
+            if (16 * tile + r >= a.n) continue;
+            float v = 0.f;
+#pragma unroll
+            for (int part = 0; part < (X32 ? 3 : 1); ++part) {
+                const int col = X32 ? 3 * t + (2 - part) : t;  // smallest part first
+                for (int q = 0; q < kw; ++q) v += from[q * (8 * NT * 16) + col * 16 + r];
+            }
+            v *= 2.f;  // the operand was decoded halved
+            const int64_t at = (int64_t)(t0 + t) * a.ldy + 16 * tile + r;
+            if (a.y32) static_cast<float*>(a.y)[at] = v;
+            else static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(v);
         }
-        v *= 2.f;  // the operand was decoded halved
-        const int64_t at = (int64_t)(t0 + t) * a.ldy + n0 + r;
-        if (a.y32) static_cast<float*>(a.y)[at] = v;
-        else static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(v);
+        if (kw == 1) __syncwarp();
     }
 }
 
 template <int W, int NT, bool X32>
 static int launch_gemv(GemvArgs a, cudaStream_t st) {
+    using S = GemvShape<NT>;
     static PerDevice once;
-    if (kernel_setup(once, mx_gemv_kernel<W, NT, X32>, kGvThreads, kGvSmem) < 1) return BDR_ERR_CUDA;
+    if (kernel_setup(once, mx_gemv_kernel<W, NT, X32>, S::kThreads, kGvSmem) < 1) return BDR_ERR_CUDA;
     const int cols = (X32 ? 3 : 1) * std::min(a.tokens, a.tokens_per_pass);
-    const int steps = (int)((a.k + kGvStep - 1) / kGvStep);
-    // as many row tiles per CTA as there are groups of eight columns: the activations are fetched once per CTA, and a CTA's
-    // weights should outweigh them
-    a.rw = NT >= 4 ? 4 : NT;
-    const int kw = kGvWarps / a.rw;
-    a.phase_steps = (int)((kGvSmem / cols - 64) / (2 * kGvStep)) / kw * kw;
-    const size_t smem = std::max<size_t>((size_t)cols * (std::min(a.phase_steps, steps) * kGvStep * 2 + 64),
-                                         (size_t)kGvWarps * 8 * NT * 16 * 4);
-    const dim3 grid((unsigned)((a.n + 16 * a.rw - 1) / (16 * a.rw)), (unsigned)((a.tokens + a.tokens_per_pass - 1) / a.tokens_per_pass));
-    mx_gemv_kernel<W, NT, X32><<<grid, kGvThreads, smem, st>>>(a);
+    const int steps = (int)((a.k + kGvStep - 1) / kGvStep), sms = sm_count();
+    const int64_t tiles = (a.n + 15) / 16;
+    // the longest walk in steps, a tile's join counted as a third of one
+    double best = 0;
+    const int fit = (int)(((kGvSmem - 2 * S::kRed) / cols - 64) / (2 * kGvStep));  // steps whose activations fit: four at least
+    for (int kw = 1; kw <= S::kWarps && kw <= std::max(1, steps) && kw <= fit; kw *= 2) {
+        const int64_t rounds = (tiles + (int64_t)sms * (S::kWarps / kw) - 1) / ((int64_t)sms * (S::kWarps / kw));
+        // activations that do not fit at once are staged again for every round: about 1/240 of a step per column and step
+        const double stage = cols * steps / 240.0 * (steps > fit ? (double)rounds : 1.0);
+        const double walk = (double)rounds * ((steps + kw - 1) / kw + 0.33) + stage;
+        if (kw == 1 || walk < best) { best = walk; a.kw = kw; }
+    }
+    a.phase_steps = fit / a.kw * a.kw;
+    const size_t smem = 2 * S::kRed + (size_t)cols * (std::min(a.phase_steps, steps) * kGvStep * 2 + 64);
+    const int64_t ctas = std::min<int64_t>(sms, (tiles + S::kWarps / a.kw - 1) / (S::kWarps / a.kw));
+    const dim3 grid((unsigned)ctas, (unsigned)((a.tokens + a.tokens_per_pass - 1) / a.tokens_per_pass));
+    mx_gemv_kernel<W, NT, X32><<<grid, S::kThreads, smem, st>>>(a);
     return cudaGetLastError() == cudaSuccess ? BDR_OK : BDR_ERR_CUDA;
 }
 
