@@ -3,9 +3,10 @@
 //
 // Every packed weight is read once and used for T columns, so the kernel is bound by the bytes of W as long as decoding keeps
 // up.  A warp owns 16 rows of W and walks along K in steps of 256 elements: lane (g, c) of the matrix instruction's layout
-// takes blocks 4c .. 4c+3 of rows g and g + 8 (64 contiguous elements each: 24, 40 or 64 bytes of codes and one word each of
-// exponents and microexponents), decodes them in registers and feeds 16 matrix instructions, while the next step's bytes are on
-// their way into a second set of registers.  The activations sit in shared memory in the order those instructions want them,
+// takes four blocks of rows g and g + 8 (24, 40 or 64 bytes of codes each), decodes them in registers and feeds 16 matrix instructions.  The bytes come through a ring of
+// the warp's own in shared memory, filled by 16-byte asynchronous copies one or two steps ahead: a lane's own bytes are
+// strided in memory, and loads of them straight into registers kept the L1 busy with four times as many lines per request and
+// the compiler moving them down to where they were needed.  The activations sit in shared memory in the order those instructions want them,
 // as bf16; a 32-bit activation is split exactly into three bf16 columns, which costs nothing while the eight columns of an
 // instruction are not full.
 // One CTA per SM stays for the whole call (the activations are staged once) and its warps form groups of kw that share a
@@ -17,6 +18,7 @@
 
 #include <algorithm>
 
+#include "bdr_device.cuh"
 #include "bdr_host.h"
 #include "mx_frag.cuh"
 
@@ -26,10 +28,15 @@ constexpr int kGvStep = 256;                 // elements of K per warp step
 constexpr int kGvSmem = 227 * 1024;
 constexpr int kGvMaxCols = 64;               // columns (tokens, or thirds of a 32-bit token) of one pass
 
-// warps of a CTA: what the registers allow
-template <int NT> struct GemvShape {
-    static constexpr int kWarps = NT <= 2 ? 16 : 8, kThreads = 32 * kWarps;
+// Warps of a CTA and steps in a warp's ring: 16 warps of up to 128 registers when there are few columns, 8 (and shared memory left
+// for the activations) when there are more.
+template <int W, int NT> struct GemvShape {
+    static constexpr int kWarps = NT == 1 ? 16 : 8, kThreads = 32 * kWarps;
     static constexpr int kRed = kWarps * 8 * NT * 16 * 4;  // bytes of all warps' sums of a tile
+    static constexpr int kPitch = 32 * W;                  // bytes of codes of a row and step
+    static constexpr int kAtX = 16 * kPitch, kStage = kAtX + 2 * 256;  // 16 rows of codes, of exponents, of microexponents
+    static constexpr int kStages = NT <= 2 && !(W == 8 && NT == 1) ? 3 : 2;
+    static constexpr int kXs = 2 * kRed + kWarps * kStages * kStage;   // where the activations start
 };
 
 struct GemvArgs {
@@ -45,75 +52,107 @@ struct GemvArgs {
     int phase_steps;     // steps whose activations fit in shared memory at once (a multiple of kw)
 };
 
-// four consecutive blocks of one row
+// Four blocks of one row.  3- and 5-bit codes: blocks 4c .. 4c + 3 of a step, 24 or 40 contiguous bytes of the ring, which eight
+// lanes (two rows, four c) read from different banks as they lie.  8-bit codes: blocks c, c + 4, c + 8, c + 12, so that the four
+// lanes of a row read 64 contiguous bytes at a time (the upper and lower half of a row's 128 bytes change places in odd rows);
+// of the scales they read the row's whole word of sixteen and pick theirs.
 template <int W> struct Run {
     uint32_t w[2 * W];
-    uint32_t exps, micro;
+    uint32_t exps[2], micro[2];  // of blocks 2p and 2p + 1 of the run, one per half (8-bit codes: bits 8 .. 15 of micro are leftovers)
 };
+template <int W>
+__device__ __forceinline__ constexpr int run_block(int c, int i) { return W == 8 ? c + 4 * i : 4 * c + i; }
 
 template <int W>
-__device__ __forceinline__ void load_run(Run<W>& r, const bdr_planes_t& p, int64_t row, int block, int nb) {
-    const uint8_t* codes = p.elems + row * p.ld_elems + (int64_t)block * (2 * W);
-    const uint8_t* ex = p.exps + row * p.ld_exps + block;
-    const uint8_t* mi = p.micro + row * p.ld_micro + block;
-    if (block + 4 <= nb) {
-        r.exps = __ldg(reinterpret_cast<const uint32_t*>(ex));
-        r.micro = __ldg(reinterpret_cast<const uint32_t*>(mi));
-        if constexpr (W == 8) {
+__device__ __forceinline__ void read_run(Run<W>& r, const uint8_t* stage, int row, int c) {
+    constexpr int kPitch = 32 * W, kAtX = 16 * kPitch;
+    const uint8_t* codes = stage + row * kPitch;
+    const uint8_t* scales = stage + kAtX + row * 16;
+    if constexpr (W == 8) {
+        const uint4 e = *reinterpret_cast<const uint4*>(scales), m = *reinterpret_cast<const uint4*>(scales + 256);
+        const uint32_t pick = 0x4400u + 0x1111u * c;  // byte c of one word in the low half, of the other in the high half
+        r.exps[0] = __byte_perm(e.x, e.y, pick) & 0x00FF00FFu;
+        r.exps[1] = __byte_perm(e.z, e.w, pick) & 0x00FF00FFu;
+        r.micro[0] = __byte_perm(m.x, m.y, pick);
+        r.micro[1] = __byte_perm(m.z, m.w, pick);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint4 v = __ldg(reinterpret_cast<const uint4*>(codes) + i);
-                r.w[4 * i] = v.x; r.w[4 * i + 1] = v.y; r.w[4 * i + 2] = v.z; r.w[4 * i + 3] = v.w;
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < W; ++i) {
-                const uint2 v = __ldg(reinterpret_cast<const uint2*>(codes) + i);
-                r.w[2 * i] = v.x; r.w[2 * i + 1] = v.y;
-            }
+        for (int i = 0; i < 4; ++i) {
+            const uint4 v = *reinterpret_cast<const uint4*>(codes + 16 * ((c + 4 * i) ^ (4 * (row & 1))));
+            r.w[4 * i] = v.x; r.w[4 * i + 1] = v.y; r.w[4 * i + 2] = v.z; r.w[4 * i + 3] = v.w;
         }
-    } else {  // the end of a line: block by block, absent blocks are zeros with an ordinary exponent
-        r.exps = 0x7F7F7F7Fu;
-        r.micro = 0;
+    } else {
+        const uint32_t e = *reinterpret_cast<const uint32_t*>(scales + 4 * c), m = *reinterpret_cast<const uint32_t*>(scales + 256 + 4 * c);
 #pragma unroll
-        for (int i = 0; i < 2 * W; ++i) r.w[i] = 0;
+        for (int p = 0; p < 2; ++p) {
+            r.exps[p] = frag::spread_bytes(e >> (16 * p));
+            r.micro[p] = frag::spread_bytes(m >> (16 * p));
+        }
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            if (block + b < nb) {
-                r.exps ^= (uint32_t)(0x7F ^ __ldg(ex + b)) << (8 * b);
-                r.micro |= (uint32_t)__ldg(mi + b) << (8 * b);
-#pragma unroll
-                for (int h = 0; h < W; ++h) {
-                    const int o = 2 * W * b + 2 * h;
-                    r.w[o >> 2] |= (uint32_t)__ldg(reinterpret_cast<const uint16_t*>(codes + o)) << (8 * (o & 2));
-                }
-            }
+        for (int i = 0; i < W; ++i) {
+            const uint2 v = reinterpret_cast<const uint2*>(codes + 8 * W * c)[i];
+            r.w[2 * i] = v.x; r.w[2 * i + 1] = v.y;
         }
     }
 }
+
+// s * bytes + p in one instruction of the multiply-add pipe
+__device__ __forceinline__ const uint8_t* step_from(const uint8_t* p, int s, uint32_t bytes) {
+    const uint8_t* q;
+    asm("mad.wide.u32 %0, %1, %2, %3;" : "=l"(q) : "r"((uint32_t)s), "r"(bytes), "l"(p));
+    return q;
+}
+
+// A warp's copies of a step of a row tile, with their sources kept as pointers into the tile's rows.
+template <int W>
+struct StepCopies {
+    static constexpr int kPieces = 2 * W, kCount = 16 * kPieces / 32;  // 16-byte pieces of a row; copies per lane
+    static constexpr int kPitch = 32 * W, kAtX = 16 * kPitch;
+    const uint8_t *code[kCount], *scale;
+    __device__ __forceinline__ void point(const bdr_planes_t& p, int64_t tile, int64_t n, int lane) {
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) {
+            const int at = lane + 32 * i, row = at / kPieces;
+            code[i] = p.elems + min(16 * tile + row, n - 1) * p.ld_elems + 16 * (at - row * kPieces);
+        }
+        const int64_t row = min(16 * tile + (lane & 15), n - 1);
+        scale = lane < 16 ? p.exps + row * p.ld_exps : p.micro + row * p.ld_micro;
+    }
+    // TAIL: the step may pass the end of the rows; what lies beyond a row's pitch is left out
+    template <bool TAIL>
+    __device__ __forceinline__ void queue(uint8_t* stage, const bdr_planes_t& p, int s, int lane) const {
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) {
+            const int at = lane + 32 * i, row = at / kPieces, piece = at - row * kPieces;
+            const int unit = W == 8 ? piece ^ (4 * (row & 1)) : piece;
+            if (!TAIL || (int64_t)s * kPitch + 16 * piece < p.ld_elems) cp_async16(stage + row * kPitch + 16 * unit, step_from(code[i], s, kPitch));
+        }
+        if (!TAIL || (int64_t)s * 16 < (lane < 16 ? p.ld_exps : p.ld_micro)) cp_async16(stage + kAtX + lane * 16, step_from(scale, s, 16));
+    }
+};
 
 // Activations of K steps k0 / 256 .. into shared memory, in the order of the B fragments: a lane's word for two matrix
 // instructions holds elements 4h .. 4h+3 of blocks 2p and 2p+1 of its four, alternating.  Word (p, h) of lane column c lies
 // at 16 (4 p + h) + 4 c 32-bit words of the step: the eight lanes that a shared-memory request serves at a time (two columns,
 // four c) hit different banks (column pitch 64 bytes off a multiple of 128).
-template <bool X32>
+template <int W, bool X32>
 __device__ __forceinline__ void stage_x(const GemvArgs& a, uint16_t* xs, int64_t pitch, int t0, int nt, int64_t k0, int span) {
     const int per = span / 8;
     for (int i = threadIdx.x; i < nt * per; i += blockDim.x) {
         const int t = i / per, v = i - t * per;
         const int s = v >> 5, c = (v >> 3) & 3, p = (v >> 2) & 1, h = v & 3;
-        const int64_t k = k0 + (int64_t)s * kGvStep + 64 * c + 32 * p + 4 * h;
+        const int64_t k = k0 + (int64_t)s * kGvStep + 16 * run_block<W>(c, 2 * p) + 4 * h;
         const int64_t at = (int64_t)s * kGvStep + (4 * p + h) * 32 + c * 8;
+        constexpr int kNext = 16 * (run_block<W>(0, 1) - run_block<W>(0, 0));  // elements from block 2p to block 2p + 1
         if constexpr (X32) {
             const float* x = static_cast<const float*>(a.x) + (int64_t)(t0 + t) * a.ldx + k;
             float f[8];
-            if (a.xvec && k + 20 <= a.k) {
-                const float4 u = __ldg(reinterpret_cast<const float4*>(x)), w = __ldg(reinterpret_cast<const float4*>(x) + 4);
+            if (a.xvec && k + kNext + 4 <= a.k) {
+                const float4 u = __ldg(reinterpret_cast<const float4*>(x)), w = __ldg(reinterpret_cast<const float4*>(x + kNext));
                 f[0] = u.x; f[1] = w.x; f[2] = u.y; f[3] = w.y; f[4] = u.z; f[5] = w.z; f[6] = u.w; f[7] = w.w;
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const int o = (e >> 1) + 16 * (e & 1);
+                    const int o = (e >> 1) + kNext * (e & 1);
                     f[e] = k + o < a.k ? __ldg(x + o) : 0.f;
                 }
             }
@@ -128,14 +167,14 @@ __device__ __forceinline__ void stage_x(const GemvArgs& a, uint16_t* xs, int64_t
         } else {
             const uint16_t* x = static_cast<const uint16_t*>(a.x) + (int64_t)(t0 + t) * a.ldx + k;
             uint2 u, w;
-            if (a.xvec && k + 20 <= a.k) {
+            if (a.xvec && k + kNext + 4 <= a.k) {
                 u = __ldg(reinterpret_cast<const uint2*>(x));
-                w = __ldg(reinterpret_cast<const uint2*>(x) + 4);
+                w = __ldg(reinterpret_cast<const uint2*>(x + kNext));
             } else {
                 uint16_t q[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const int o = (e & 3) + 16 * (e >> 2);
+                    const int o = (e & 3) + kNext * (e >> 2);
                     q[e] = k + o < a.k ? __ldg(x + o) : (uint16_t)0;
                 }
                 u = make_uint2(frag::pack2(q[0], q[1]), frag::pack2(q[2], q[3]));
@@ -160,8 +199,8 @@ __device__ __forceinline__ void run_step_as(const Run<W>& r0, const Run<W>& r1, 
         for (int i = 0; i < 4; ++i) part[n][i] = 0.f;
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
-        const frag::Scales s0 = frag::make_scales<FAST>(frag::spread_bytes(r0.exps >> (16 * p)), frag::spread_bytes(r0.micro >> (16 * p)));
-        const frag::Scales s1 = frag::make_scales<FAST>(frag::spread_bytes(r1.exps >> (16 * p)), frag::spread_bytes(r1.micro >> (16 * p)));
+        const frag::Scales s0 = frag::make_scales<FAST>(r0.exps[p], r0.micro[p]);
+        const frag::Scales s1 = frag::make_scales<FAST>(r1.exps[p], r1.micro[p]);
         const int a0 = 32 * W * p, b0 = a0 + 16 * W;
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
@@ -188,22 +227,25 @@ __device__ __forceinline__ void run_step_as(const Run<W>& r0, const Run<W>& r1, 
 template <int W, int NT>
 __device__ __forceinline__ void run_step(const Run<W>& r0, const Run<W>& r1, const uint16_t* xs, int64_t pitch, int cols, int lane,
                                          float (&acc)[NT][4]) {
-    if (__all_sync(0xFFFFFFFFu, frag::all_fast(r0.exps) && frag::all_fast(r1.exps))) run_step_as<W, NT, true>(r0, r1, xs, pitch, cols, lane, acc);
+    if (__all_sync(0xFFFFFFFFu, frag::all_fast(r0.exps[0] + (r0.exps[1] << 8)) && frag::all_fast(r1.exps[0] + (r1.exps[1] << 8)))) run_step_as<W, NT, true>(r0, r1, xs, pitch, cols, lane, acc);
     else run_step_as<W, NT, false>(r0, r1, xs, pitch, cols, lane, acc);
 }
 
 template <int W, int NT, bool X32>
-__global__ void __launch_bounds__(GemvShape<NT>::kThreads, 1) mx_gemv_kernel(const GemvArgs a) {
-    constexpr int kWarps = GemvShape<NT>::kWarps;
+__global__ void __launch_bounds__((GemvShape<W, NT>::kThreads), 1) mx_gemv_kernel(const GemvArgs a) {
+    using S = GemvShape<W, NT>;
+    constexpr int kWarps = S::kWarps, D = S::kStages;
     extern __shared__ __align__(16) uint8_t smem[];
     float* const red = reinterpret_cast<float*>(smem);
-    uint16_t* const xs = reinterpret_cast<uint16_t*>(smem + 2 * GemvShape<NT>::kRed);
+    uint16_t* const xs = reinterpret_cast<uint16_t*>(smem + S::kXs);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
+    uint8_t* const ring = smem + 2 * S::kRed + warp * (D * S::kStage);
     const int kw = a.kw, my_k = warp & (kw - 1), group = warp / kw, groups = kWarps / kw;
     const int t0 = blockIdx.y * a.tokens_per_pass, nt = min(a.tokens_per_pass, a.tokens - t0), cols = X32 ? 3 * nt : nt;
     const int nb = (int)((a.k + 15) / 16), steps = (nb + 15) / 16;
-    const int64_t tiles = (a.n + 15) / 16, stride = (int64_t)gridDim.x * groups, first = (int64_t)blockIdx.x * groups;
-    const int rounds = (int)((tiles - first + stride - 1) / stride);  // of the CTA's first group; the others may have one fewer
+    // tiles go to the CTAs in turn, then to a CTA's groups: every SM has the same number to within one
+    const int64_t tiles = (a.n + 15) / 16, stride = (int64_t)gridDim.x * groups;
+    const int rounds = (int)((tiles - blockIdx.x + stride - 1) / stride);  // of the CTA's first group; the others may have one fewer
     const int64_t pitch = (int64_t)min(a.phase_steps, steps) * kGvStep + 32;
     float acc[NT][4];
 #pragma unroll
@@ -211,44 +253,66 @@ __global__ void __launch_bounds__(GemvShape<NT>::kThreads, 1) mx_gemv_kernel(con
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[n][i] = 0.f;
 
-    auto fetch = [&](Run<W>(&r)[2], int64_t tile, int s) {
-        load_run<W>(r[0], a.w, min(16 * tile + g, a.n - 1), 16 * s + 4 * c, nb);
-        load_run<W>(r[1], a.w, min(16 * tile + g + 8, a.n - 1), 16 * s + 4 * c, nb);
+    int64_t tile = blockIdx.x + (int64_t)group * gridDim.x;
+    // the copies run ahead of the computation, across the ends of tiles
+    StepCopies<W> copies;
+    int64_t ahead_tile = tile;
+    int ahead = my_k, to = 0, at = 0;
+    if (ahead_tile < tiles) copies.point(a.w, ahead_tile, a.n, lane);
+    auto queue_next = [&] {
+        if (ahead_tile < tiles && ahead < steps) {
+            if (16 * ahead + 16 <= nb) copies.template queue<false>(ring + to, a.w, ahead, lane);
+            else copies.template queue<true>(ring + to, a.w, ahead, lane);
+            ahead += kw;
+            if (ahead >= steps) {
+                ahead = my_k;
+                ahead_tile += stride;
+                if (ahead_tile < tiles) copies.point(a.w, ahead_tile, a.n, lane);
+            }
+        }
+        cp_async_commit();
+        to = to + S::kStage == D * S::kStage ? 0 : to + S::kStage;
     };
-    Run<W> even[2], odd[2];
-    int64_t tile = first + group;
+#pragma unroll
+    for (int i = 0; i + 1 < D; ++i) queue_next();
     int s = my_k, round = 0;
-    bool use_odd = false;
-    if (tile < tiles) fetch(even, tile, s);
-    // one step, with the next one (of this tile or of the group's next) fetched ahead
-    auto advance = [&](Run<W>(&now)[2], Run<W>(&next)[2], const uint16_t* xp) {
-        const bool last = s + kw >= steps;
-        if (!last || tile + stride < tiles) fetch(next, last ? tile + stride : tile, last ? my_k : s + kw);
-        run_step<W, NT>(now[0], now[1], xp + (int64_t)s * kGvStep, pitch, cols, lane, acc);
-        s += kw;
-    };
     for (; round < rounds; ++round, tile += stride) {
         const bool active = tile < tiles;
         for (int p0 = 0; p0 < steps; p0 += a.phase_steps) {
             const int p1 = min(p0 + a.phase_steps, steps);
             if (a.phase_steps < steps || round == 0) {
                 if (p0 || round) __syncthreads();  // everyone is done with the activations before
-                stage_x<X32>(a, xs, pitch, t0, nt, (int64_t)p0 * kGvStep, (p1 - p0) * kGvStep);
+                stage_x<W, X32>(a, xs, pitch, t0, nt, (int64_t)p0 * kGvStep, (p1 - p0) * kGvStep);
                 __syncthreads();
             }
             if (!active) continue;
             const uint16_t* const xp = xs - (int64_t)p0 * kGvStep;
-            while (s < p1) {
-                if (!use_odd) advance(even, odd, xp);
-                else advance(odd, even, xp);
-                use_odd = !use_odd;
+            for (; s < p1; s += kw) {
+                queue_next();
+                cp_async_wait<D - 1>();
+                __syncwarp();  // every lane's pieces of the step are in place
+                Run<W> run[2];
+                read_run<W>(run[0], ring + at, g, c);
+                read_run<W>(run[1], ring + at, g + 8, c);
+                if (16 * s + 16 > nb) {  // the end of a line: an ordinary exponent for the blocks that are not there (their activations are zero)
+#pragma unroll
+                    for (int b = 0; b < 4; ++b)
+                        if (16 * s + run_block<W>(c, b) >= nb) {
+                            const uint32_t mask = 0xFFu << (16 * (b & 1));
+                            run[0].exps[b >> 1] = (run[0].exps[b >> 1] & ~mask) | (0x007F007Fu & mask);
+                            run[1].exps[b >> 1] = (run[1].exps[b >> 1] & ~mask) | (0x007F007Fu & mask);
+                        }
+                }
+                at = at + S::kStage == D * S::kStage ? 0 : at + S::kStage;
+                run_step<W, NT>(run[0], run[1], xp + (int64_t)s * kGvStep, pitch, cols, lane, acc);
+                __syncwarp();  // the next copies may overwrite the step
             }
         }
         if (!active) continue;
         s = my_k;
         // the shares of K, added in order; a warp's sums are [column][16 rows].  Two buffers: the sums of a tile are read before
         // anyone passes the barrier of the next, and only then overwritten.
-        float* const mine = red + (round & 1) * (GemvShape<NT>::kRed / 4) + warp * (8 * NT * 16);
+        float* const mine = red + (round & 1) * (S::kRed / 4) + warp * (8 * NT * 16);
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -275,11 +339,12 @@ __global__ void __launch_bounds__(GemvShape<NT>::kThreads, 1) mx_gemv_kernel(con
         }
         if (kw == 1) __syncwarp();
     }
+    cp_async_wait<0>();
 }
 
 template <int W, int NT, bool X32>
 static int launch_gemv(GemvArgs a, cudaStream_t st) {
-    using S = GemvShape<NT>;
+    using S = GemvShape<W, NT>;
     static PerDevice once;
     if (kernel_setup(once, mx_gemv_kernel<W, NT, X32>, S::kThreads, kGvSmem) < 1) return BDR_ERR_CUDA;
     const int cols = (X32 ? 3 : 1) * std::min(a.tokens, a.tokens_per_pass);
@@ -287,17 +352,17 @@ static int launch_gemv(GemvArgs a, cudaStream_t st) {
     const int64_t tiles = (a.n + 15) / 16;
     // the longest walk in steps, a tile's join counted as a third of one
     double best = 0;
-    const int fit = (int)(((kGvSmem - 2 * S::kRed) / cols - 64) / (2 * kGvStep));  // steps whose activations fit: four at least
+    const int fit = (int)(((kGvSmem - S::kXs) / cols - 64) / (2 * kGvStep));  // steps whose activations fit: two at least
     for (int kw = 1; kw <= S::kWarps && kw <= std::max(1, steps) && kw <= fit; kw *= 2) {
-        const int64_t rounds = (tiles + (int64_t)sms * (S::kWarps / kw) - 1) / ((int64_t)sms * (S::kWarps / kw));
+        const int64_t rounds = ((tiles + sms - 1) / sms + S::kWarps / kw - 1) / (S::kWarps / kw);
         // activations that do not fit at once are staged again for every round: about 1/240 of a step per column and step
         const double stage = cols * steps / 240.0 * (steps > fit ? (double)rounds : 1.0);
         const double walk = (double)rounds * ((steps + kw - 1) / kw + 0.33) + stage;
         if (kw == 1 || walk < best) { best = walk; a.kw = kw; }
     }
     a.phase_steps = fit / a.kw * a.kw;
-    const size_t smem = 2 * S::kRed + (size_t)cols * (std::min(a.phase_steps, steps) * kGvStep * 2 + 64);
-    const int64_t ctas = std::min<int64_t>(sms, (tiles + S::kWarps / a.kw - 1) / (S::kWarps / a.kw));
+    const size_t smem = S::kXs + (size_t)cols * (std::min(a.phase_steps, steps) * kGvStep * 2 + 64);
+    const int64_t ctas = std::min<int64_t>(sms, tiles);
     const dim3 grid((unsigned)ctas, (unsigned)((a.tokens + a.tokens_per_pass - 1) / a.tokens_per_pass));
     mx_gemv_kernel<W, NT, X32><<<grid, S::kThreads, smem, st>>>(a);
     return cudaGetLastError() == cudaSuccess ? BDR_OK : BDR_ERR_CUDA;
