@@ -13,6 +13,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "bdr_device.cuh"
 #include "bdr_host.h"
@@ -23,6 +24,7 @@ namespace bdr {
 int* device_status_word();
 
 constexpr int kApThreads = 256, kApWarps = kApThreads / 32;
+constexpr int kApStages = 4;  // iterations in a warp's ring
 
 struct AppendArgs {
     bdr_planes_t plane[2];       // keys, values
@@ -61,6 +63,19 @@ __device__ __forceinline__ void load_units(const T* p, uint32_t* u) {
     }
 }
 
+// eight elements in shared memory as fp32 bit patterns
+__device__ __forceinline__ void shared_units(const __nv_bfloat16* p, uint32_t* u) {
+    const uint4 w = *reinterpret_cast<const uint4*>(p);
+    const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) { u[2 * k] = ws[k] << 16; u[2 * k + 1] = ws[k] & 0xFFFF0000u; }
+}
+__device__ __forceinline__ void shared_units(const float* p, uint32_t* u) {
+    const uint4 w = reinterpret_cast<const uint4*>(p)[0], v = reinterpret_cast<const uint4*>(p)[1];
+    u[0] = w.x; u[1] = w.y; u[2] = w.z; u[3] = w.w;
+    u[4] = v.x; u[5] = v.y; u[6] = v.z; u[7] = v.w;
+}
+
 template <int W>
 __device__ __forceinline__ void store_codes(uint8_t* p, const uint32_t (&u)[kSlice], const uint32_t (&rq)[kSlice],
                                             const uint32_t (&cb)[kSlice / 2]) {
@@ -74,31 +89,63 @@ __device__ __forceinline__ void store_codes(uint8_t* p, const uint32_t (&u)[kSli
     }
 }
 
-// One block of 16 values (fp32 bits u) of the key (which = 0) or value line of a slot.
-__device__ __forceinline__ void pack_block_to(const AppendArgs& a, int which, int64_t slot, int block, const uint32_t (&u)[kSlice],
-                                              uint32_t (&yb)[kSlice], bool store) {
-    QParams qp;
-    qp.k1 = 16; qp.k2 = 2; qp.d2 = 1; qp.m = a.m[which]; qp.rounding = BDR_ROUND_NEAREST_EVEN;
-    qp.beta = 1;
-    qp.qmax = (1u << qp.m) - 1u;
-    uint32_t ej[kSlice / 2], eb[1] = {0}, rq[kSlice], cb[kSlice / 2], tau[kSlice / 2];
-    subblock_exponents<2>(u, ej);
-#pragma unroll
-    for (int j = 0; j < kSlice / 2; ++j) eb[0] = max(eb[0], ej[j]);
-    double e2 = 0.0, s2 = 0.0;
-    quantize_slice<2, kSlice, false, true, true>(u, ej, eb, qp, yb, rq, cb, tau, e2, s2);
-    if (!store) return;
-    const bdr_planes_t& p = a.plane[which];
+// Q(.) of a finite block of a Table II format, the fast formulation of quantize_slice for exactly this shape: u holds the fp32
+// bits; yb the quantized values' bits; rq, cb the raw magnitudes and their offsets for pack_words; returns the microexponents.
+template <int W>
+__device__ __forceinline__ uint32_t quantize_table2(const uint32_t (&u)[kSlice], const uint32_t (&pm)[kSlice / 2], uint32_t F23,
+                                                    uint32_t (&yb)[kSlice], uint32_t (&rq)[kSlice], uint32_t (&cb)[kSlice / 2]) {
+    constexpr uint32_t kBase = ((uint32_t)(127 + 23 - (W - 2)) << 23) | 0x400000u, kMax = (1u << (W - 1)) - 1u;
+    const float K = __uint_as_float(max(0x7F000000u - F23, 0x00400000u)), Kinv = __uint_as_float(max(F23, 0x00400000u));  // 2^(127-F), 2^(F-127)
     uint32_t micro = 0;
 #pragma unroll
-    for (int j = 0; j < kSlice / 2; ++j) micro |= tau[j] << j;
-    p.exps[slot * p.ld_exps + block] = (uint8_t)(eb[0] >> 23);
+    for (int j = 0; j < kSlice / 2; ++j) {
+        const uint32_t dm = min(F23 - (pm[j] & kExpMask), 0x00800000u);  // tau << 23
+        cb[j] = kBase - dm;
+        micro |= dm >> (23 - j);
+        const float C = __uint_as_float(cb[j]), Cmax = __uint_as_float(cb[j] + kMax);
+#pragma unroll
+        for (int k = 2 * j; k < 2 * j + 2; ++k) {
+            // the scaling is exact, so the one rounding of the multiply-add is the one to the format's grid
+            const float r = fminf(fmaf(fabsf(__uint_as_float(u[k])), K, C), Cmax);
+            rq[k] = __float_as_uint(r);
+            yb[k] = __float_as_uint(__fmul_rn(__fsub_rn(r, C), Kinv)) | (u[k] & 0x80000000u);
+        }
+    }
+    return micro;
+}
+
+// One block of 16 values (fp32 bits u) of the key (which = 0) or value line of a slot.
+template <int W>
+__device__ __forceinline__ void pack_block_as(const bdr_planes_t& p, int64_t slot, int block, uint32_t (&u)[kSlice], uint32_t (&yb)[kSlice], bool store) {
+    uint32_t pm[kSlice / 2], top = 0;
+#pragma unroll
+    for (int j = 0; j < kSlice / 2; ++j) {
+        pm[j] = max(u[2 * j] & 0x7FFFFFFFu, u[2 * j + 1] & 0x7FFFFFFFu);
+        top = max(top, pm[j]);
+    }
+    const uint32_t F23 = top & kExpMask;
+    uint32_t rq[kSlice], cb[kSlice / 2], micro;
+    if (F23 != kExpMask) {
+        micro = quantize_table2<W>(u, pm, F23, yb, rq, cb);
+    } else {  // an infinity or a NaN: codes and microexponents zero, values NaN
+        micro = 0;
+#pragma unroll
+        for (int k = 0; k < kSlice; ++k) {
+            yb[k] = 0x7FC00000u;
+            u[k] = rq[k] = cb[k / 2] = 0;
+        }
+    }
+    if (!store) return;
+    p.exps[slot * p.ld_exps + block] = (uint8_t)(F23 >> 23);
     p.micro[slot * p.ld_micro + block] = (uint8_t)micro;
-    uint8_t* codes = p.elems + slot * p.ld_elems;
-    switch (qp.m) {
-        case 2: store_codes<3>(codes + block * 6, u, rq, cb); break;
-        case 4: store_codes<5>(codes + block * 10, u, rq, cb); break;
-        default: store_codes<8>(codes + block * 16, u, rq, cb); break;
+    store_codes<W>(p.elems + slot * p.ld_elems + block * (2 * W), u, rq, cb);
+}
+__device__ __forceinline__ void pack_block_to(const AppendArgs& a, int which, int64_t slot, int block, uint32_t (&u)[kSlice],
+                                              uint32_t (&yb)[kSlice], bool store) {
+    switch (a.m[which]) {
+        case 2: pack_block_as<3>(a.plane[which], slot, block, u, yb, store); break;
+        case 4: pack_block_as<5>(a.plane[which], slot, block, u, yb, store); break;
+        default: pack_block_as<8>(a.plane[which], slot, block, u, yb, store); break;
     }
 }
 
@@ -113,7 +160,7 @@ __device__ __forceinline__ void pad_lines(const AppendArgs& a, int which, int64_
 
 // U: how many elements may be loaded at once at multiples of U elements of a head, at rot_dim / 2 and in the tables
 template <typename T, int U, bool INTERLEAVED>
-__global__ void __launch_bounds__(kApThreads) mx_kv_append_kernel(const AppendArgs a) {
+__global__ void __launch_bounds__(kApThreads, 2) mx_kv_append_kernel(const AppendArgs a) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int wpt = a.warps_per_token;
     const int64_t t = (int64_t)blockIdx.x * (kApWarps / wpt) + warp / wpt;
@@ -153,92 +200,147 @@ __global__ void __launch_bounds__(kApThreads) mx_kv_append_kernel(const AppendAr
 #pragma unroll
             for (int k = 0; k < UA; ++k) {
                 cs[i + k] = in ? __uint_as_float(c4[k]) : 1.f;
-                sn[i + k] = in ? __uint_as_float(s4[k]) : 0.f;
+                // half layout, first half: a cos - b sin = a cos + b (-sin), bit for bit
+                sn[i + k] = in ? __uint_as_float(s4[k] ^ (!INTERLEAVED && e < half ? 0x80000000u : 0u)) : 0.f;
             }
         }
     }
+    const int e0 = 16 * b;
+    // U == 8: the heads of an iteration (a contiguous run of the token's row) come through a ring of the warp's own in shared
+    // memory, three iterations ahead, whatever their kind; else every lane loads for itself.
+    constexpr bool kRing = U == 8;
+    constexpr int kChunk = 32 * kSlice, D = kApStages;  // elements of an iteration at most
+    extern __shared__ __align__(16) uint8_t smem[];
+    T* const ring = reinterpret_cast<T*>(smem) + warp * (D * kChunk);
+    const int sub = warp % wpt;  // of the token's warps; iterations are dealt to them in turn
     const int total = a.iters[0] + a.iters[1] + a.iters[2];
-    for (int it = warp % wpt; it < total; it += wpt) {
-        const int kind = it < a.iters[0] ? 0 : (it < a.iters[0] + a.iters[1] ? 1 : 2);
-        const int first = kind == 0 ? it : (kind == 1 ? it - a.iters[0] : it - a.iters[0] - a.iters[1]);
-        const int h = first * hpi + hl;
-        if (hl < hpi && h < a.heads[kind]) {
-            const T* x = static_cast<const T*>(a.src[kind]) + t * a.ld_src[kind] + (int64_t)h * d;
-            uint32_t u[kSlice];
+    int ahead = sub, to = 0, at = 0;
+    auto fetch_next = [&] {
+        if (ahead < total) {
+            const int kind = ahead < a.iters[0] ? 0 : (ahead < a.iters[0] + a.iters[1] ? 1 : 2);
+            const int first = (ahead - (kind == 0 ? 0 : (kind == 1 ? a.iters[0] : a.iters[0] + a.iters[1]))) * hpi;
+            const T* from = static_cast<const T*>(a.src[kind]) + t * a.ld_src[kind] + (int64_t)first * d;
+            const int n = min(hpi, a.heads[kind] - first) * d;
+            constexpr int kPer = 16 / (int)sizeof(T);
 #pragma unroll
-            for (int i = 0; i < kSlice; i += U) load_units<T, U>(x + 16 * b + i, u + i);
-            if (rot && kind < 2) {
-                if constexpr (INTERLEAVED) {
+            for (int i = 0; i < kChunk; i += 32 * kPer)
+                if (i + lane * kPer < n) cp_async16(ring + to + i + lane * kPer, from + i + lane * kPer);
+            ahead += wpt;
+        }
+        cp_async_commit();
+        to = to + kChunk == D * kChunk ? 0 : to + kChunk;
+    };
+    if constexpr (kRing) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        if (8 * b + i < half) {
-                            const float p = __uint_as_float(u[2 * i]), q = __uint_as_float(u[2 * i + 1]);
-                            u[2 * i] = __float_as_uint(__fsub_rn(__fmul_rn(p, cs[i]), __fmul_rn(q, sn[i])));
-                            u[2 * i + 1] = __float_as_uint(__fadd_rn(__fmul_rn(q, cs[i]), __fmul_rn(p, sn[i])));
+        for (int i = 0; i + 1 < D; ++i) fetch_next();
+    }
+    // All heads of one kind (0: queries, 1: keys, 2: values), `before` iterations into the token's work.
+    auto heads_of = [&](auto kind, int before) {
+        constexpr int KIND = decltype(kind)::value;
+        const int n = a.heads[KIND], step = wpt * hpi;
+        int h = ((sub + wpt * 8 - before % wpt) % wpt) * hpi + hl;
+        const bool mine = hl < hpi, turns = KIND < 2 && rot && e0 < rot;
+        const T* x = static_cast<const T*>(a.src[KIND]) + t * a.ld_src[KIND] + (int64_t)h * d;
+        T* y = static_cast<T*>(a.dst[KIND]) + (KIND == 0 ? t * a.ld_q : t * ((int64_t)n * d)) + (int64_t)h * d + e0;
+#pragma unroll 1
+        for (; h - hl < n; h += step, x += (int64_t)step * d, y += (int64_t)step * d) {
+            const T* head = ring + at + hl * d;
+            if constexpr (kRing) {
+                fetch_next();
+                cp_async_wait<D - 1>();
+                __syncwarp();  // every lane's pieces are in place
+                at = at + kChunk == D * kChunk ? 0 : at + kChunk;
+            }
+            if (mine && h < n) {
+                uint32_t u[kSlice];
+#pragma unroll
+                for (int i = 0; i < kSlice; i += U) {
+                    if constexpr (kRing) shared_units(head + e0 + i, u + i);
+                    else load_units<T, U>(x + e0 + i, u + i);
+                }
+                if (turns) {
+                    if constexpr (INTERLEAVED) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            if (8 * b + i < half) {
+                                const float p = __uint_as_float(u[2 * i]), q = __uint_as_float(u[2 * i + 1]);
+                                u[2 * i] = __float_as_uint(__fsub_rn(__fmul_rn(p, cs[i]), __fmul_rn(q, sn[i])));
+                                u[2 * i + 1] = __float_as_uint(__fadd_rn(__fmul_rn(q, cs[i]), __fmul_rn(p, sn[i])));
+                            }
                         }
-                    }
-                } else {
+                    } else {
 #pragma unroll
-                    for (int i = 0; i < kSlice; i += U) {
-                        const int e = 16 * b + i;
-                        if (e < rot) {
-                            uint32_t v[U];
-                            load_units<T, U>(x + (e < half ? e + half : e - half), v);
+                        for (int i = 0; i < kSlice; i += U) {
+                            const int e = e0 + i;
+                            if (e < rot) {
+                                uint32_t v[U];
+                                const int from = e < half ? e + half : e - half;
+                                if constexpr (kRing) shared_units(head + from, v);
+                                else load_units<T, U>(x + from, v);
 #pragma unroll
-                            for (int k = 0; k < U; ++k) {
-                                const float own = __fmul_rn(__uint_as_float(u[i + k]), cs[i + k]);
-                                const float other = __fmul_rn(__uint_as_float(v[k]), sn[i + k]);
-                                u[i + k] = __float_as_uint(e < half ? __fsub_rn(own, other) : __fadd_rn(own, other));
+                                for (int k = 0; k < U; ++k)
+                                    u[i + k] = __float_as_uint(__fadd_rn(__fmul_rn(__uint_as_float(u[i + k]), cs[i + k]), __fmul_rn(__uint_as_float(v[k]), sn[i + k])));
                             }
                         }
                     }
                 }
-            }
-            if (kind < 2 && bad) {
+                if (KIND < 2 && bad) {
 #pragma unroll
-                for (int i = 0; i < kSlice; ++i) u[i] = 0x7FC00000u;
-            }
-            if (kind == 0) {
-                T* y = static_cast<T*>(a.dst[0]) + t * a.ld_q + (int64_t)h * d + 16 * b;
-                if constexpr (sizeof(T) == 2) {  // round to the tensor's type
-#pragma unroll
-                    for (int i = 0; i < kSlice; ++i)
-                        u[i] = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(__uint_as_float(u[i]))) << 16;
+                    for (int i = 0; i < kSlice; ++i) u[i] = 0x7FC00000u;
                 }
-                if constexpr (U >= 4) {
-                    if constexpr (U == 8 || sizeof(T) == 4) {
+                if constexpr (KIND == 0) {
+                    if constexpr (sizeof(T) == 2) {  // round to the tensor's type
+                        uint32_t w[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const __nv_bfloat162 p = __floats2bfloat162_rn(__uint_as_float(u[2 * i]), __uint_as_float(u[2 * i + 1]));
+                            w[i] = *reinterpret_cast<const uint32_t*>(&p);
+                        }
+                        if constexpr (U == 8) {
+                            reinterpret_cast<uint4*>(y)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+                            reinterpret_cast<uint4*>(y)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+                        } else if constexpr (U == 4) {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) reinterpret_cast<uint2*>(y)[i] = make_uint2(w[2 * i], w[2 * i + 1]);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < kSlice; ++i) reinterpret_cast<uint16_t*>(y)[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+                        }
+                    } else if constexpr (U >= 4) {
                         store_slice_vec(y, u);
                     } else {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            reinterpret_cast<uint2*>(y)[i] = make_uint2((u[4 * i] >> 16) | u[4 * i + 1], (u[4 * i + 2] >> 16) | u[4 * i + 3]);
+                        store_slice_guarded(y, 1, kSlice, u);
                     }
                 } else {
-                    store_slice_guarded(y, 1, kSlice, u);
-                }
-            } else {
-                uint32_t yb[kSlice];
-                pack_block_to(a, kind - 1, slot, h * nb + b, u, yb, store);
-                if (a.dst[kind]) {
-                    T* y = static_cast<T*>(a.dst[kind]) + (t * a.heads[1] + h) * d + 16 * b;  // 16-byte aligned
-                    store_slice_vec(y, yb);
+                    uint32_t yb[kSlice];
+                    pack_block_to(a, KIND - 1, slot, h * nb + b, u, yb, store);
+                    if (a.dst[KIND]) store_slice_vec(y, yb);  // 16-byte aligned
                 }
             }
+            if (KIND > 0 && store && h == hl) pad_lines(a, KIND - 1, slot, lane);
+            if constexpr (kRing) __syncwarp();  // the next copies may overwrite the heads
         }
-        if (store && kind > 0 && first == 0) pad_lines(a, kind - 1, slot, lane);
-    }
+    };
+    heads_of(std::integral_constant<int, 0>{}, 0);
+    heads_of(std::integral_constant<int, 1>{}, a.iters[0]);
+    heads_of(std::integral_constant<int, 2>{}, a.iters[0] + a.iters[1]);
+    if constexpr (kRing) cp_async_wait<0>();
 }
 
 template <typename T>
 static int launch_append(const AppendArgs& a, int unit, bool interleaved, cudaStream_t st) {
     const int64_t tokens_per_cta = kApWarps / a.warps_per_token;
     const unsigned grid = (unsigned)((a.n_tokens + tokens_per_cta - 1) / tokens_per_cta);
-#define BDR_APPEND(U)                                                                          \
-    (interleaved ? mx_kv_append_kernel<T, U, true><<<grid, kApThreads, 0, st>>>(a)             \
-                 : mx_kv_append_kernel<T, U, false><<<grid, kApThreads, 0, st>>>(a))
-    if (unit == 8) BDR_APPEND(8);
-    else if (unit == 4) BDR_APPEND(4);
-    else BDR_APPEND(1);
+    constexpr int kRingBytes = kApWarps * kApStages * 32 * kSlice * (int)sizeof(T);
+    static PerDevice once, once_inter;
+    if (kernel_setup(once, mx_kv_append_kernel<T, 8, false>, kApThreads, kRingBytes) < 1) return BDR_ERR_CUDA;
+    if (kernel_setup(once_inter, mx_kv_append_kernel<T, 8, true>, kApThreads, kRingBytes) < 1) return BDR_ERR_CUDA;
+#define BDR_APPEND(U, BYTES)                                                                   \
+    (interleaved ? mx_kv_append_kernel<T, U, true><<<grid, kApThreads, BYTES, st>>>(a)         \
+                 : mx_kv_append_kernel<T, U, false><<<grid, kApThreads, BYTES, st>>>(a))
+    if (unit == 8) BDR_APPEND(8, kRingBytes);
+    else if (unit == 4) BDR_APPEND(4, 0);
+    else BDR_APPEND(1, 0);
 #undef BDR_APPEND
     return cudaGetLastError() == cudaSuccess ? BDR_OK : BDR_ERR_CUDA;
 }
