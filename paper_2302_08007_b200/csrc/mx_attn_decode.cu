@@ -215,6 +215,8 @@ int mx_attn_decode(const mx_kv_cache_t* cache, const void* q, int64_t ldq, bdr_d
     a.q_vec = (uintptr_t)q % (2 * eb) == 0 && (n_seqs == 1 || ldq % 2 == 0);
     a.o_vec = (uintptr_t)out % 16 == 0 && (n_seqs == 1 || ldo * eb % 16 == 0);
     a.scale2 = 2.f * scale * 1.44269504088896341f;
+    a.scale2_fast = a.scale2 * frag::kFastFactor;
+    if (max_pages == 0) { a.table = lengths; a.ld_table = 0; }  // never used, but read
     cudaStream_t st = (cudaStream_t)stream;
     const int wv = cache->cfg_v.m + 1;
     switch (cache->cfg_k.m) {

@@ -53,7 +53,7 @@ struct AttnArgs {
     int n_pages, max_pages, cap, window;   // cap = max_pages * page_size
     int q_vec, o_vec;                      // two query elements may be read at once; results may be written 16 bytes at a time
     FastDiv page;
-    float scale2;                          // 2 scale log2(e): the keys are decoded halved
+    float scale2, scale2_fast;             // 2 scale log2(e): the keys are decoded halved (and on the first way scaled)
     int* status;
 };
 
@@ -304,7 +304,7 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
         const int b = seg.b;
         // ---- queries into shared memory: [part][pair of steps][column group][lane].  Step 8 x + j of a lane holds elements 2j and 2j + 1 of
         // blocks 2x and 2x + 1 of its own: {2x: 2j, 2x+1: 2j}, {2x: 2j+1, 2x+1: 2j+1}.
-        if (tw == 0) {
+        {
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const int col = 8 * n + g, head = head_of(col), f = col / a.per_pass;
@@ -315,6 +315,7 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
                     const bool in0 = head >= 0 && at0 >= 0 && at0 < a.d, in1 = head >= 0 && at1 >= 0 && at1 < a.d;
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
+                        if ((j & (a.tw - 1)) != tw) continue;  // the unit's sets of warps share the work
                         uint16_t p[4][3];
                         if constexpr (F32) {
                             float2 u = make_float2(0.f, 0.f), v = u;
@@ -353,15 +354,14 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
 
         // slot of token 16 tile + lane % 16: -1 outside the range, -2 for a page that does not exist
         const int tile_end = seg.r.first + seg.t1;
+        const int32_t* const table = a.table + (int64_t)b * a.ld_table;
         auto slot_of = [&](int t) {
             const int tok = 16 * t + (lane & 15);
-            int slot = -1;
-            if (t < tile_end && tok >= seg.r.start && tok < seg.r.end) {
-                const int pg = (int)fastdiv((uint32_t)tok, a.page);
-                const int id = pg < a.max_pages ? __ldg(a.table + (int64_t)b * a.ld_table + pg) : -1;
-                const bool ok = id >= 0 && id < a.n_pages;
-                slot = ok ? id * (int)a.page.d + (tok - pg * (int)a.page.d) : -2;
-            }
+            const int pg = (int)fastdiv((uint32_t)tok, a.page), known = min(pg, max(a.max_pages - 1, 0));
+            const int id = __ldg(table + known);
+            int slot = id * (int)a.page.d + (tok - pg * (int)a.page.d);
+            slot = pg < a.max_pages && (uint32_t)id < (uint32_t)a.n_pages ? slot : -2;
+            slot = t < tile_end && tok >= seg.r.start && tok < seg.r.end ? slot : -1;
             return slot;
         };
         // tokens present (bits 0 .. 15) and tokens of bad pages (16 .. 31)
@@ -394,7 +394,6 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
             at = at + L::kBytes == D * L::kBytes ? 0 : at + L::kBytes;
 #pragma unroll
             for (int i = 0; i + 1 < D; ++i) held[i] = held[i + 1];
-            if (here >> 16 && lane == 0) atomicCAS(a.status, 0, (int)BDR_ERR_SIZE);
             // ---- scores
             float s[NT][4];
 #pragma unroll
@@ -461,29 +460,6 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
             if constexpr (VB == 1) ordinary = frag::all_fast((kf[0] & 0xFFFFu) + (kf[1] << 16)) && frag::all_fast(vf[0] + (vf[1] << 8) + (vf[2] << 16) + (vf[3] << 24));
             else ordinary = frag::all_fast(kf[0]) && frag::all_fast(kf[1]) && frag::all_fast(vf[0] + (vf[1] << 16)) && frag::all_fast(vf[2] + (vf[3] << 16));
             const bool fast = __all_sync(0xFFFFFFFFu, ordinary);
-            // Merged heads share the reduction: a NaN block of one head must not reach the others' columns through their zero
-            // queries, so it is decoded as zeros and its head's scores are made NaN below.
-            uint32_t spoilt[2] = {0, 0};  // per row: the unit's heads with such a block
-            if (!fast && a.merge > 1) {
-                bool any = false;
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int x = 0; x < KB; ++x) any |= ((kf[i] >> (8 * x)) & 0xFFu) == 255u;
-                if (__any_sync(0xFFFFFFFFu, any)) {
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-#pragma unroll
-                        for (int x = 0; x < KB; ++x)
-                            if (((kf[i] >> (8 * x)) & 0xFFu) == 255u) {
-                                spoilt[i] |= 1u << ((c * KB + x) / a.nb);
-                                kf[i] &= ~(0xFFu << (8 * x));
-                            }
-                        spoilt[i] |= __shfl_xor_sync(0xFFFFFFFFu, spoilt[i], 1);
-                        spoilt[i] |= __shfl_xor_sync(0xFFFFFFFFu, spoilt[i], 2);
-                    }
-                }
-            }
             auto scores = [&](auto way) {
                 constexpr bool FAST = decltype(way)::value;
 #pragma unroll
@@ -513,19 +489,48 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
                     }
                 }
             };
-            if (fast) scores(std::true_type{});
-            else scores(std::false_type{});
-            const float scale = fast ? a.scale2 * frag::kFastFactor : a.scale2;
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s[n][e] *= scale;
-            if (spoilt[0] | spoilt[1]) {
+            if (fast) {
+                scores(std::true_type{});
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (spoilt[e >> 1] >> ((8 * n + 2 * c + (e & 1)) / a.per_pass) & 1u) s[n][e] = __uint_as_float(0x7FC00000u);
+                    for (int e = 0; e < 4; ++e) s[n][e] *= a.scale2_fast;
+            } else {
+                // Merged heads share the reduction: a NaN block of one head must not reach the others' columns through their zero
+                // queries, so it is decoded as zeros and its head's scores are made NaN below.
+                uint32_t spoilt[2] = {0, 0};  // per row: the unit's heads with such a block
+                if (a.merge > 1) {
+                    bool any = false;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int x = 0; x < KB; ++x) any |= ((kf[i] >> (8 * x)) & 0xFFu) == 255u;
+                    if (__any_sync(0xFFFFFFFFu, any)) {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+#pragma unroll
+                            for (int x = 0; x < KB; ++x)
+                                if (((kf[i] >> (8 * x)) & 0xFFu) == 255u) {
+                                    spoilt[i] |= 1u << ((c * KB + x) / a.nb);
+                                    kf[i] &= ~(0xFFu << (8 * x));
+                                }
+                            spoilt[i] |= __shfl_xor_sync(0xFFFFFFFFu, spoilt[i], 1);
+                            spoilt[i] |= __shfl_xor_sync(0xFFFFFFFFu, spoilt[i], 2);
+                        }
+                    }
+                }
+                scores(std::false_type{});
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[n][e] *= a.scale2;
+                if (spoilt[0] | spoilt[1]) {
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (spoilt[e >> 1] >> ((8 * n + 2 * c + (e & 1)) / a.per_pass) & 1u) s[n][e] = __uint_as_float(0x7FC00000u);
+                }
             }
             // ---- the tile's values
             frag::Block<WV> vb[4][VB];
@@ -538,6 +543,7 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
                     frag::align_block(vb[i][y], (uint32_t)off);
                 }
             if (here != 0xFFFFu) {  // a tile at an end of the range, or with a page that does not exist
+                if (here >> 16 && lane == 0) atomicCAS(a.status, 0, (int)BDR_ERR_SIZE);
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const int tok = g + 8 * i;
@@ -579,31 +585,32 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
                         for (int i = 0; i < VB * 8; ++i) { o[i][n][e] *= f; o[i][n][e + 2] *= f; }
                     }
             }
-            uint32_t pb[NT][PARTS][2];  // P^T fragments (32-bit: three parts of eight bits)
+            float p[NT][4];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                float p[4];
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    p[e] = exp2_approx(t[n][e]);
-                    sum[n][e & 1] += p[e];
+                    p[n][e] = exp2_approx(t[n][e]);
+                    sum[n][e & 1] += p[n][e];
                 }
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    float lo = p[2 * h], hi = p[2 * h + 1];
-                    if (!fast) { lo *= 1.f / frag::kFastFactor; hi *= 1.f / frag::kFastFactor; }
-#pragma unroll
-                    for (int part = 0; part < PARTS; ++part) {
-                        const uint32_t w = pack_bf16x2(lo, hi);
-                        pb[n][part][h] = frag::transpose8x8(w);
-                        lo -= __uint_as_float(w << 16);
-                        hi -= __uint_as_float(w & 0xFFFF0000u);
-                    }
-                }
-            }
             // ---- output
             auto output = [&](auto way) {
                 constexpr bool FAST = decltype(way)::value;
+                uint32_t pb[NT][PARTS][2];  // P^T fragments (32-bit: three parts of eight bits)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        constexpr float kLower = FAST ? 1.f : 1.f / frag::kFastFactor;
+                        float lo = p[n][2 * h] * kLower, hi = p[n][2 * h + 1] * kLower;
+#pragma unroll
+                        for (int part = 0; part < PARTS; ++part) {
+                            const uint32_t w = pack_bf16x2(lo, hi);
+                            pb[n][part][h] = frag::transpose8x8(w);
+                            lo -= __uint_as_float(w << 16);
+                            hi -= __uint_as_float(w & 0xFFFF0000u);
+                        }
+                    }
 #pragma unroll
                 for (int x = 0; x < VB; ++x) {
                     const frag::Scales s0 = frag::make_scales<FAST>((vf[0] >> (8 * x)) & 0xFFu, (vf[1] >> (8 * x)) & 0xFFu, (vm[0] >> (8 * x)) & 0xFFu, (vm[1] >> (8 * x)) & 0xFFu);
