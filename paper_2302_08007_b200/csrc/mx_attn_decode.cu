@@ -30,9 +30,9 @@ __global__ void __launch_bounds__(kJoinThreads) mx_attn_join_kernel(const AttnAr
     int w0 = 0, w1 = -1;
     int64_t total = 0, p = 0;
     if (r.count > 0) {
-        total = total_tiles(a, lane);
-        int unused = 0;
-        p = walk_tiles(a, lane, b, -1, unused);
+        const TileCounts c = count_tiles(a, lane, b);
+        total = c.total;
+        p = c.prefix;
         // the last worker whose part starts at or before a tile holds it: begin(w) = floor(total w / workers) <= tile
         auto holder = [&](int64_t tile) {
             int w = min((int)((tile * a.workers + a.workers - 1) / total), a.workers - 1);

@@ -71,38 +71,32 @@ __device__ __forceinline__ SeqRange seq_range(const AttnArgs& a, int b) {
     return r;
 }
 
-// Tiles of all sequences together (called by whole warps).
-__device__ __forceinline__ int64_t total_tiles(const AttnArgs& a, int lane) {
-    int64_t n = 0;
-    for (int b = lane; b < a.n_seqs; b += 32) n += seq_range(a, b).count;
+// Tiles of all sequences together, and of those before sequence `b` (called by whole warps).  Up to 32 sequences, a lane each,
+// take one round of loads.
+struct TileCounts {
+    int64_t total, prefix;
+};
+__device__ __forceinline__ int64_t inclusive_scan(int64_t n, int lane) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(0xFFFFFFFFu, n, o);
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t v = __shfl_up_sync(0xFFFFFFFFu, n, o);
+        if (lane >= o) n += v;
+    }
     return n;
 }
-
-// Tiles of the sequences before `limit`, stopping early before the sequence that holds tile `u` (u < 0: no such stop).
-// Returns the prefix and leaves the sequence in b.
-__device__ __forceinline__ int64_t walk_tiles(const AttnArgs& a, int lane, int limit, int64_t u, int& b) {
-    int64_t p = 0;
-    for (int base = 0;; base += 32) {
-        const int mine = base + lane;
-        int64_t n = mine < limit ? seq_range(a, mine).count : 0;
-        int64_t incl = n;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int64_t v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-            if (lane >= o) incl += v;
-        }
-        const int64_t all = __shfl_sync(0xFFFFFFFFu, incl, 31);
-        if (base + 32 >= limit || (u >= 0 && p + all > u)) {
-            if (u < 0) { b = limit; return p + all; }
-            const unsigned hit = __ballot_sync(0xFFFFFFFFu, p + incl > u);
-            const int at = hit ? __ffs(hit) - 1 : 31;
-            b = base + at;
-            return p + __shfl_sync(0xFFFFFFFFu, incl - n, at);
-        }
-        p += all;
+__device__ __forceinline__ TileCounts count_tiles(const AttnArgs& a, int lane, int b) {
+    TileCounts c = {0, 0};
+    for (int i = lane; i < a.n_seqs; i += 32) {
+        const int n = seq_range(a, i).count;
+        c.total += n;
+        if (i < b) c.prefix += n;
     }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        c.total += __shfl_xor_sync(0xFFFFFFFFu, c.total, o);
+        c.prefix += __shfl_xor_sync(0xFFFFFFFFu, c.prefix, o);
+    }
+    return c;
 }
 
 __device__ __forceinline__ int64_t worker_begin(int64_t total, int w, int workers) { return total * w / workers; }
@@ -191,18 +185,56 @@ struct Segments {
     int b;
     SeqRange r;
     int t0, t1;
+    bool known;  // r is sequence b's
+    // finds the part of worker w (called by whole warps)
+    __device__ __forceinline__ void begin(const AttnArgs& a, int w, int lane) {
+        if (a.n_seqs <= 32) {
+            r = {0, 0, 0, 0};
+            if (lane < a.n_seqs) r = seq_range(a, lane);
+            const int64_t incl = inclusive_scan(r.count, lane), total = __shfl_sync(0xFFFFFFFFu, incl, 31);
+            u = worker_begin(total, w, a.workers);
+            u_end = worker_begin(total, w + 1, a.workers);
+            const unsigned hit = __ballot_sync(0xFFFFFFFFu, incl > u);
+            b = hit ? __ffs(hit) - 1 : 0;
+            prefix = __shfl_sync(0xFFFFFFFFu, incl - r.count, b);
+            r.start = __shfl_sync(0xFFFFFFFFu, r.start, b);
+            r.end = __shfl_sync(0xFFFFFFFFu, r.end, b);
+            r.first = __shfl_sync(0xFFFFFFFFu, r.first, b);
+            r.count = __shfl_sync(0xFFFFFFFFu, r.count, b);
+            known = true;
+            return;
+        }
+        const int64_t total = count_tiles(a, lane, 0).total;
+        u = worker_begin(total, w, a.workers);
+        u_end = worker_begin(total, w + 1, a.workers);
+        known = false;
+        prefix = 0;
+        if (u >= u_end) return;
+        for (b = 0;; b += 32) {  // 32 sequences at a time up to the one that holds tile u
+            const int64_t n = b + lane < a.n_seqs ? seq_range(a, b + lane).count : 0, incl = inclusive_scan(n, lane);
+            const unsigned hit = __ballot_sync(0xFFFFFFFFu, prefix + incl > u);
+            if (hit) {
+                const int at = __ffs(hit) - 1;
+                prefix += __shfl_sync(0xFFFFFFFFu, incl - n, at);
+                b += at;
+                return;
+            }
+            prefix += __shfl_sync(0xFFFFFFFFu, incl, 31);
+        }
+    }
     // false when the part is done; else tiles t0 .. t1 of sequence b (counted from the first that its range touches)
     __device__ __forceinline__ bool next(const AttnArgs& a) {
         if (u >= u_end) return false;
-        r = seq_range(a, b);
+        if (!known) r = seq_range(a, b);
         while (r.count == 0) r = seq_range(a, ++b);
+        known = true;
         t0 = (int)(u - prefix);
         t1 = (int)min((int64_t)r.count, u_end - prefix);
         return true;
     }
     __device__ __forceinline__ void advance() {
         u = prefix + t1;
-        if (t1 == r.count) { prefix += r.count; ++b; }
+        if (t1 == r.count) { prefix += r.count; ++b; known = false; }
     }
 };
 
@@ -216,13 +248,9 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
     constexpr int kRing = attn_ring_bytes<WK, WV, MAXB, NT, F32, FULL>();
     extern __shared__ __align__(128) uint8_t smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t total = total_tiles(a, lane);
     Segments seg;
-    seg.u = worker_begin(total, blockIdx.x, a.workers);
-    seg.u_end = worker_begin(total, blockIdx.x + 1, a.workers);
+    seg.begin(a, blockIdx.x, lane);
     if (seg.u >= seg.u_end) return;  // uniform for the CTA
-    seg.b = 0;
-    seg.prefix = walk_tiles(a, lane, a.n_seqs, seg.u, seg.b);
 
     const int g = lane >> 2, c = lane & 3, hw = warp % a.hw, tw = warp / a.hw;
     const int unit = blockIdx.y * a.hw + hw, mk = unit / a.passes, pass = unit - mk * a.passes, kv0 = mk * a.merge;
@@ -621,9 +649,17 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
                         const uint32_t a0 = frag::decode_word<WV, FAST>(vb[0][x].w, 0, vb[1][x].w, 0, 2 * j, w0), a1 = frag::decode_word<WV, FAST>(vb[0][x].w, 0, vb[1][x].w, 0, 2 * j + 1, w0);
                         const uint32_t a2 = frag::decode_word<WV, FAST>(vb[2][x].w, 0, vb[3][x].w, 0, 2 * j, w1), a3 = frag::decode_word<WV, FAST>(vb[2][x].w, 0, vb[3][x].w, 0, 2 * j + 1, w1);
 #pragma unroll
-                        for (int n = 0; n < NT; ++n)
+                        for (int n = 0; n < NT; ++n) {
+                            if constexpr (F32) {  // a long sum in the tensor core need not round to nearest: a tile's products are added with fp32 additions
+                                float d[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                            for (int part = PARTS - 1; part >= 0; --part) frag::mma_bf16(o[8 * x + j][n], a0, a1, a2, a3, pb[n][part][0], pb[n][part][1]);
+                                for (int part = PARTS - 1; part >= 0; --part) frag::mma_bf16(d, a0, a1, a2, a3, pb[n][part][0], pb[n][part][1]);
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) o[8 * x + j][n][e] += d[e];
+                            } else {
+                                frag::mma_bf16(o[8 * x + j][n], a0, a1, a2, a3, pb[n][0][0], pb[n][0][1]);
+                            }
+                        }
                     }
                 }
             };
