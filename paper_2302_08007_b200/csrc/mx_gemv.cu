@@ -17,6 +17,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "bdr_device.cuh"
 #include "bdr_host.h"
@@ -35,8 +36,9 @@ template <int W, int NT> struct GemvShape {
     static constexpr int kRed = kWarps * 8 * NT * 16 * 4;  // bytes of all warps' sums of a tile
     static constexpr int kPitch = 32 * W;                  // bytes of codes of a row and step
     static constexpr int kAtX = 16 * kPitch, kStage = kAtX + 2 * 256;  // 16 rows of codes, of exponents, of microexponents
-    static constexpr int kStages = NT <= 2 && !(W == 8 && NT == 1) ? 3 : 2;
-    static constexpr int kXs = 2 * kRed + kWarps * kStages * kStage;   // where the activations start
+    static constexpr int kStages = NT <= 2 && W != 8 ? 3 : 2;
+    static constexpr int kReds = NT < 4 ? 2 : 1;                       // buffers of sums
+    static constexpr int kXs = kReds * kRed + kWarps * kStages * kStage;  // where the activations start
 };
 
 struct GemvArgs {
@@ -47,9 +49,9 @@ struct GemvArgs {
     int64_t n, k;
     int tokens, tokens_per_pass;
     int x32, y32;        // 32-bit activations / results (else bf16)
-    int xvec;            // activations may be read four at a time
+    int xvec;            // rows of activations start on 16-byte boundaries
     int kw;              // warps that share a tile's K (a power of two, at most the steps there are)
-    int phase_steps;     // steps whose activations fit in shared memory at once (a multiple of kw)
+    int phase_steps;     // steps whose activations are in shared memory at once: all, or a multiple of kw in each of two buffers
 };
 
 // Four blocks of one row.  3- and 5-bit codes: blocks 4c .. 4c + 3 of a step, 24 or 40 contiguous bytes of the ring, which eight
@@ -130,61 +132,112 @@ struct StepCopies {
     }
 };
 
-// Activations of K steps k0 / 256 .. into shared memory, in the order of the B fragments: a lane's word for two matrix
-// instructions holds elements 4h .. 4h+3 of blocks 2p and 2p+1 of its four, alternating.  Word (p, h) of lane column c lies
-// at 16 (4 p + h) + 4 c 32-bit words of the step: the eight lanes that a shared-memory request serves at a time (two columns,
-// four c) hit different banks (column pitch 64 bytes off a multiple of 128).
-template <int W, bool X32>
-__device__ __forceinline__ void stage_x(const GemvArgs& a, uint16_t* xs, int64_t pitch, int t0, int nt, int64_t k0, int span) {
-    const int per = span / 8;
-    for (int i = threadIdx.x; i < nt * per; i += blockDim.x) {
-        const int t = i / per, v = i - t * per;
-        const int s = v >> 5, c = (v >> 3) & 3, p = (v >> 2) & 1, h = v & 3;
-        const int64_t k = k0 + (int64_t)s * kGvStep + 16 * run_block<W>(c, 2 * p) + 4 * h;
-        const int64_t at = (int64_t)s * kGvStep + (4 * p + h) * 32 + c * 8;
-        constexpr int kNext = 16 * (run_block<W>(0, 1) - run_block<W>(0, 0));  // elements from block 2p to block 2p + 1
-        if constexpr (X32) {
-            const float* x = static_cast<const float*>(a.x) + (int64_t)(t0 + t) * a.ldx + k;
-            float f[8];
-            if (a.xvec && k + kNext + 4 <= a.k) {
-                const float4 u = __ldg(reinterpret_cast<const float4*>(x)), w = __ldg(reinterpret_cast<const float4*>(x + kNext));
-                f[0] = u.x; f[1] = w.x; f[2] = u.y; f[3] = w.y; f[4] = u.z; f[5] = w.z; f[6] = u.w; f[7] = w.w;
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int o = (e >> 1) + kNext * (e & 1);
-                    f[e] = k + o < a.k ? __ldg(x + o) : 0.f;
-                }
-            }
-            uint16_t q[8][3];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) frag::split3(f[e], q[e]);
-#pragma unroll
-            for (int part = 0; part < 3; ++part)
-                *reinterpret_cast<uint4*>(xs + (3 * t + part) * pitch + at) =
-                    make_uint4(frag::pack2(q[0][part], q[1][part]), frag::pack2(q[2][part], q[3][part]),
-                               frag::pack2(q[4][part], q[5][part]), frag::pack2(q[6][part], q[7][part]));
-        } else {
-            const uint16_t* x = static_cast<const uint16_t*>(a.x) + (int64_t)(t0 + t) * a.ldx + k;
-            uint2 u, w;
-            if (a.xvec && k + kNext + 4 <= a.k) {
-                u = __ldg(reinterpret_cast<const uint2*>(x));
-                w = __ldg(reinterpret_cast<const uint2*>(x + kNext));
-            } else {
-                uint16_t q[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int o = (e & 3) + kNext * (e >> 2);
-                    q[e] = k + o < a.k ? __ldg(x + o) : (uint16_t)0;
-                }
-                u = make_uint2(frag::pack2(q[0], q[1]), frag::pack2(q[2], q[3]));
-                w = make_uint2(frag::pack2(q[4], q[5]), frag::pack2(q[6], q[7]));
-            }
-            *reinterpret_cast<uint4*>(xs + t * pitch + at) =
-                make_uint4(__byte_perm(u.x, w.x, 0x5410), __byte_perm(u.x, w.x, 0x7632), __byte_perm(u.y, w.y, 0x5410), __byte_perm(u.y, w.y, 0x7632));
+// Activations of some K steps in shared memory, in the order of the B fragments: a lane's 16 bytes for two matrix instructions hold
+// elements 4h .. 4h+3 of blocks 2p and 2p+1 of its four, alternating.  Where they lie in a column's step of 512 bytes, in units of 16:
+// the eight lanes that a shared-memory request serves at a time (two columns, 64 bytes off a multiple of 128 apart, and four c) hit
+// different banks, and so do those that put the activations in order (below).
+// That order costs the reader more address arithmetic, so up to eight columns, which are put in order quickly, do without.
+template <int W, int NT>
+__device__ __forceinline__ int x_slot(int c, int p, int h) { return W == 8 || NT == 1 ? 4 * (4 * p + h) + c : 8 * c + ((4 * p + h) ^ c); }
+
+// They come as they are, by asynchronous copies that run while the phase before is computed, and are put in order in place by the warp
+// that copied them.  A warp's share is a step of two tokens (32-bit ones: of one token, in the first two of its three columns).
+template <int W, int NT, bool X32>
+struct StageX {
+    int t, s, dt, ds, steps;
+    __device__ __forceinline__ StageX(int n_steps) {  // not zero
+        const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5;
+        steps = n_steps;
+        t = dt = 0; s = warp; ds = warps;
+        if (warps > n_steps) {
+            t = warp / n_steps; s = warp - t * n_steps;
+            dt = warps / n_steps; ds = warps - dt * n_steps;
+            if constexpr (!X32) { t *= 2; dt *= 2; }
         }
     }
-}
+    __device__ __forceinline__ void next() {
+        t += dt; s += ds;
+        if (s >= steps) { s -= steps; t += X32 ? 1 : 2; }
+    }
+    // the 16 bytes of a row at x, of which `left` elements exist, zeros behind them
+    template <typename T>
+    __device__ static __forceinline__ void piece(uint16_t* to, const T* x, const T* row, int64_t left, bool vec) {
+        constexpr int kN = X32 ? 4 : 8;
+        if (vec && left >= kN) {
+            cp_async16(to, x);
+        } else if (vec) {
+            const int n = (int)max((int64_t)0, left);
+            cp_async16_part(to, n ? x : row, n * (int)sizeof(T));
+        } else {
+            T q[kN];
+#pragma unroll
+            for (int e = 0; e < kN; ++e) q[e] = e < left ? __ldg(x + e) : (T)0;
+            *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(q);
+        }
+    }
+    // starts the copies of steps s0 .. s0 + n_steps - 1 of nt tokens
+    __device__ static __forceinline__ void copy(const GemvArgs& a, uint16_t* xs, int64_t pitch, int t0, int nt, int s0, int n_steps) {
+        using T = typename std::conditional<X32, float, uint16_t>::type;
+        const int lane = threadIdx.x & 31;
+        const bool vec = a.xvec;
+        for (StageX m(n_steps); m.t < nt; m.next()) {
+            const T* const row = static_cast<const T*>(a.x) + (t0 + m.t) * a.ldx;
+            uint16_t* const to = xs + (X32 ? 3 : 1) * m.t * pitch + m.s * kGvStep + 8 * lane;
+            const int64_t k = (int64_t)(s0 + m.s) * kGvStep + (X32 ? 4 : 8) * lane, left = a.k - k;
+            piece<T>(to, row + k, row, left, vec);
+            if constexpr (X32) piece<T>(to + pitch, row + k + kGvStep / 2, row, left - kGvStep / 2, vec);
+            else if (m.t + 1 < nt) piece<T>(to + pitch, row + a.ldx + k, row, left, vec);
+        }
+    }
+    // puts them in order, once the warp's copies are there
+    __device__ static __forceinline__ void arrange(uint16_t* xs, int64_t pitch, int nt, int n_steps) {
+        const int lane = threadIdx.x & 31;
+        __syncwarp();
+        for (StageX m(n_steps); m.t < nt; m.next()) {
+            uint16_t* const at = xs + (X32 ? 3 : 1) * m.t * pitch + m.s * kGvStep;
+            if constexpr (X32) {
+                const int h = lane & 3, c = W == 8 ? (lane >> 2) & 3 : lane >> 3, p = W == 8 ? lane >> 4 : (lane >> 2) & 1;
+                auto from = [&](int i) {  // elements 4h .. of block 2p + i
+                    const int piece = 4 * run_block<W>(c, 2 * p + i) + h;
+                    return reinterpret_cast<const float4*>(at + (piece >> 5) * pitch + 8 * (piece & 31));
+                };
+                const float4 u = *from(0), w = *from(1);
+                __syncwarp();
+                const float f[8] = {u.x, w.x, u.y, w.y, u.z, w.z, u.w, w.w};
+                uint16_t q[8][3];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) frag::split3(f[e], q[e]);
+#pragma unroll
+                for (int part = 0; part < 3; ++part)
+                    *reinterpret_cast<uint4*>(at + part * pitch + 8 * x_slot<W, NT>(c, p, h)) =
+                        make_uint4(frag::pack2(q[0][part], q[1][part]), frag::pack2(q[2][part], q[3][part]),
+                                   frag::pack2(q[4][part], q[5][part]), frag::pack2(q[6][part], q[7][part]));
+            } else {
+                // elements 8 half .. of blocks 2p and 2p + 1.  To hit all banks, lanes of odd c (3 and 5 bits) read the second block first,
+                // and lanes of the upper half (8 bits) write the second 16 bytes first.
+                const int half = lane & 1, c = W == 8 ? (lane >> 1) & 3 : (lane >> 2) & 3, p = W == 8 ? (lane >> 3) & 1 : (lane >> 1) & 1;
+                const bool there = m.t + (lane >> 4) < nt;
+                uint16_t* const mine = at + (lane >> 4) * pitch;
+                const int swap = W == 8 ? 0 : c & 1;
+                uint4 u = make_uint4(0, 0, 0, 0), w = u;
+                if (there) {
+                    u = *reinterpret_cast<const uint4*>(mine + 8 * (2 * run_block<W>(c, 2 * p + swap) + half));
+                    w = *reinterpret_cast<const uint4*>(mine + 8 * (2 * run_block<W>(c, 2 * p + 1 - swap) + half));
+                }
+                __syncwarp();
+                const uint32_t low = swap ? 0x1054u : 0x5410u, high = swap ? 0x3276u : 0x7632u;
+                uint4 a0 = make_uint4(__byte_perm(u.x, w.x, low), __byte_perm(u.x, w.x, high), __byte_perm(u.y, w.y, low), __byte_perm(u.y, w.y, high));
+                uint4 a1 = make_uint4(__byte_perm(u.z, w.z, low), __byte_perm(u.z, w.z, high), __byte_perm(u.w, w.w, low), __byte_perm(u.w, w.w, high));
+                const int first = W == 8 ? half : 0;
+                if (W == 8 && first) { const uint4 x = a0; a0 = a1; a1 = x; }
+                if (there) {
+                    *reinterpret_cast<uint4*>(mine + 8 * x_slot<W, NT>(c, p, 2 * half + first)) = a0;
+                    *reinterpret_cast<uint4*>(mine + 8 * x_slot<W, NT>(c, p, 2 * half + 1 - first)) = a1;
+                }
+            }
+        }
+    }
+};
 
 // One step of a warp.  The tensor core's fp32 additions are cut off rather than rounded, so a step's products are summed from
 // zero and then added to the totals with a rounded addition: 16 instructions in a chain instead of K / 16.
@@ -213,7 +266,7 @@ __device__ __forceinline__ void run_step_as(const Run<W>& r0, const Run<W>& r1, 
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 // a column beyond the last repeats it: what it gives is not looked at
-                const uint4 x = *reinterpret_cast<const uint4*>(xs + min(8 * n + g, cols - 1) * pitch + (4 * p + h) * 32 + c * 8);
+                const uint4 x = *reinterpret_cast<const uint4*>(xs + min(8 * n + g, cols - 1) * pitch + 8 * x_slot<W, NT>(c, p, h));
                 frag::mma_bf16(part[n], y0[0], y1[0], y0[1], y1[1], x.x, x.y);
                 frag::mma_bf16(part[n], y0[2], y1[2], y0[3], y1[3], x.z, x.w);
             }
@@ -239,7 +292,7 @@ __global__ void __launch_bounds__((GemvShape<W, NT>::kThreads), 1) mx_gemv_kerne
     float* const red = reinterpret_cast<float*>(smem);
     uint16_t* const xs = reinterpret_cast<uint16_t*>(smem + S::kXs);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
-    uint8_t* const ring = smem + 2 * S::kRed + warp * (D * S::kStage);
+    uint8_t* const ring = smem + S::kReds * S::kRed + warp * (D * S::kStage);
     const int kw = a.kw, my_k = warp & (kw - 1), group = warp / kw, groups = kWarps / kw;
     const int t0 = blockIdx.y * a.tokens_per_pass, nt = min(a.tokens_per_pass, a.tokens - t0), cols = X32 ? 3 * nt : nt;
     const int nb = (int)((a.k + 15) / 16), steps = (nb + 15) / 16;
@@ -273,22 +326,50 @@ __global__ void __launch_bounds__((GemvShape<W, NT>::kThreads), 1) mx_gemv_kerne
         cp_async_commit();
         to = to + S::kStage == D * S::kStage ? 0 : to + S::kStage;
     };
+    // Activations: the first phase now, each other one while the phase before it is computed.  With few columns and a ring of three
+    // steps, the first step of weights goes ahead of them (16384 x 4096 MX6: 18.7 us, else 19.0; with two steps MX9 16.5, else 16.2).
+    constexpr bool kWeightsFirst = NT == 1 && D == 3;
+    constexpr int kBehind = kWeightsFirst ? D - 2 : D - 1;  // steps of weights behind the activations
+    const int phases = (steps + a.phase_steps - 1) / a.phase_steps;
+    using X = StageX<W, NT, X32>;
+    if (kWeightsFirst) queue_next();
+    if (steps > 0) X::copy(a, xs, pitch, t0, nt, 0, min(a.phase_steps, steps));
+    cp_async_commit();
 #pragma unroll
-    for (int i = 0; i + 1 < D; ++i) queue_next();
+    for (int i = 0; i < kBehind; ++i) queue_next();
+    cp_async_wait<kBehind>();
+    if (steps > 0) X::arrange(xs, pitch, nt, min(a.phase_steps, steps));
+    __syncthreads();
+    int64_t buffer = 0, other = cols * pitch;  // where the phase's activations are, and the next one's
+    int queued = 0;                            // groups of copies since those of the next phase's activations began
+    bool first = true;
     int s = my_k, round = 0;
     for (; round < rounds; ++round, tile += stride) {
         const bool active = tile < tiles;
         for (int p0 = 0; p0 < steps; p0 += a.phase_steps) {
             const int p1 = min(p0 + a.phase_steps, steps);
-            if (a.phase_steps < steps || round == 0) {
-                if (p0 || round) __syncthreads();  // everyone is done with the activations before
-                stage_x<W, X32>(a, xs, pitch, t0, nt, (int64_t)p0 * kGvStep, (p1 - p0) * kGvStep);
-                __syncthreads();
+            if (phases > 1) {
+                if (!first) {
+                    // the group with this phase's activations is the first of `queued`; with D or more it has been waited for
+                    if (queued == 0) cp_async_commit();
+                    if (queued < 2) cp_async_wait<0>();
+                    else if (D == 3 && queued == 2) cp_async_wait<1>();
+                    X::arrange(xs + other, pitch, nt, p1 - p0);
+                    __syncthreads();  // in order for everyone, and everyone is done with the phase before
+                    const int64_t was = buffer;
+                    buffer = other;
+                    other = was;
+                }
+                first = false;
+                queued = 0;
+                if (p1 < steps) X::copy(a, xs + other, pitch, t0, nt, p1, min(a.phase_steps, steps - p1));
+                else if (round + 1 < rounds) X::copy(a, xs + other, pitch, t0, nt, 0, a.phase_steps);
             }
             if (!active) continue;
-            const uint16_t* const xp = xs - (int64_t)p0 * kGvStep;
+            const uint16_t* const xp = xs + buffer - (int64_t)p0 * kGvStep;
             for (; s < p1; s += kw) {
                 queue_next();
+                ++queued;
                 cp_async_wait<D - 1>();
                 __syncwarp();  // every lane's pieces of the step are in place
                 Run<W> run[2];
@@ -312,7 +393,7 @@ __global__ void __launch_bounds__((GemvShape<W, NT>::kThreads), 1) mx_gemv_kerne
         s = my_k;
         // the shares of K, added in order; a warp's sums are [column][16 rows].  Two buffers: the sums of a tile are read before
         // anyone passes the barrier of the next, and only then overwritten.
-        float* const mine = red + (round & 1) * (S::kRed / 4) + warp * (8 * NT * 16);
+        float* const mine = red + (S::kReds == 2 ? round & 1 : 0) * (S::kRed / 4) + warp * (8 * NT * 16);
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -338,6 +419,7 @@ __global__ void __launch_bounds__((GemvShape<W, NT>::kThreads), 1) mx_gemv_kerne
             else static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(v);
         }
         if (kw == 1) __syncwarp();
+        else if (S::kReds == 1) asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(32 * kw) : "memory");
     }
     cp_async_wait<0>();
 }
@@ -350,18 +432,22 @@ static int launch_gemv(GemvArgs a, cudaStream_t st) {
     const int cols = (X32 ? 3 : 1) * std::min(a.tokens, a.tokens_per_pass);
     const int steps = (int)((a.k + kGvStep - 1) / kGvStep), sms = sm_count();
     const int64_t tiles = (a.n + 15) / 16;
-    // the longest walk in steps, a tile's join counted as a third of one
+    // the longest walk in steps, where a tile's join counts as a third of one and, if the activations come in phases, so does each phase's
+    // barrier; putting a column's step in order, again for every round, takes about 1/500
     double best = 0;
-    const int fit = (int)(((kGvSmem - S::kXs) / cols - 64) / (2 * kGvStep));  // steps whose activations fit: two at least
-    for (int kw = 1; kw <= S::kWarps && kw <= std::max(1, steps) && kw <= fit; kw *= 2) {
+    // steps whose activations fit, and of which two sets fit: one at least
+    const int room = (kGvSmem - S::kXs) / cols, fit = (room - 64) / (2 * kGvStep), half = (room / 2 - 64) / (2 * kGvStep);
+    for (int kw = 1; kw <= S::kWarps && kw <= std::max(1, steps) && (steps <= fit || kw <= half); kw *= 2) {
         const int64_t rounds = ((tiles + sms - 1) / sms + S::kWarps / kw - 1) / (S::kWarps / kw);
-        // activations that do not fit at once are staged again for every round: about 1/240 of a step per column and step
-        const double stage = cols * steps / 240.0 * (steps > fit ? (double)rounds : 1.0);
-        const double walk = (double)rounds * ((steps + kw - 1) / kw + 0.33) + stage;
+        const double walk = (double)rounds * ((steps + kw - 1) / kw + 0.33 + (steps > fit ? 0.3 * steps / (half / kw * kw) + cols * steps / 500.0 : 0));
         if (kw == 1 || walk < best) { best = walk; a.kw = kw; }
     }
-    a.phase_steps = fit / a.kw * a.kw;
-    const size_t smem = S::kXs + (size_t)cols * (std::min(a.phase_steps, steps) * kGvStep * 2 + 64);
+    a.phase_steps = std::max(1, steps);
+    if (steps > fit) {  // phases of about the same length
+        const int most = half / a.kw * a.kw, phases = (steps + most - 1) / most;
+        a.phase_steps = ((steps + phases - 1) / phases + a.kw - 1) / a.kw * a.kw;
+    }
+    const size_t smem = S::kXs + (size_t)(steps > fit ? 2 : 1) * cols * (a.phase_steps * kGvStep * 2 + 64);
     const int64_t ctas = std::min<int64_t>(sms, tiles);
     const dim3 grid((unsigned)ctas, (unsigned)((a.tokens + a.tokens_per_pass - 1) / a.tokens_per_pass));
     mx_gemv_kernel<W, NT, X32><<<grid, S::kThreads, smem, st>>>(a);
@@ -402,7 +488,7 @@ extern "C" int mx_gemv(const bdr_config_t* cfg_w, const bdr_planes_t* w, int64_t
     a.x = x; a.y = y; a.ldx = ldx; a.ldy = ldy; a.n = N; a.k = K; a.tokens = (int)T;
     a.x32 = x_dt == BDR_F32; a.y32 = y_dt == BDR_F32;
     const int64_t xb = a.x32 ? 4 : 2;
-    a.xvec = (uintptr_t)x % (4 * xb) == 0 && (T == 1 || ldx % 4 == 0);
+    a.xvec = (uintptr_t)x % 16 == 0 && (T == 1 || ldx * xb % 16 == 0);
     cudaStream_t st = (cudaStream_t)stream;
     switch (cfg_w->m) {
         case 2: return a.x32 ? pick_columns<3, true>(a, st) : pick_columns<3, false>(a, st);

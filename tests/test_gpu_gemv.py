@@ -70,6 +70,24 @@ def test_every_width_of_a_pass_and_several_passes(t, dtype):
     check(y, x, w_dq, k, "f32")
 
 
+@pytest.mark.parametrize("fmt,n,k,t", [("MX9", 19040, 1100, 60), ("MX6", 7110, 2999, 30), ("MX4", 7110, 2999, 20)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rounds_of_tiles_that_go_through_the_phases_again(fmt, n, k, t, dtype):
+    w, x = make(n, k, t, 8, dtype)
+    planes, w_dq = packed(FMT[fmt], w)
+    xd = H.host_to_device(x, dtype)
+    shifted = torch.zeros((t, k + 8), dtype=xd.dtype, device="cuda")[:, 1:1 + k]
+    shifted.copy_(xd)                                    # not on 16-byte boundaries
+    y = torch.empty((t, n), dtype=torch.float32, device="cuda")
+    bdr.mx_gemv(FMT[fmt], planes, n, k, shifted, y)
+    check(y, x, w_dq, k, "f32")
+    again = torch.zeros_like(y)
+    aligned = torch.zeros((t, (k + 7) // 8 * 8), dtype=xd.dtype, device="cuda")[:, :k]
+    aligned.copy_(xd)
+    bdr.mx_gemv(FMT[fmt], planes, n, k, aligned, again)
+    assert torch.equal(y, again)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_strided_and_misaligned_operands(dtype):
     n, k, t = 50, 333, 4
