@@ -32,6 +32,7 @@ struct AppendArgs {
     const void* src[3];          // q, k, v
     void* dst[3];                // rotated q, quantized k, quantized v (the last two contiguous; NULL = not wanted)
     int64_t ld_src[3], ld_q;
+    bool wide[3];                // of dst: blocks start on 32-byte boundaries
     int heads[3], iters[3];      // heads of each, and warp iterations over them
     const int64_t *slots, *positions;
     const float *cosv, *sinv;
@@ -75,6 +76,38 @@ __device__ __forceinline__ void shared_units(const float* p, uint32_t* u) {
     u[0] = w.x; u[1] = w.y; u[2] = w.z; u[3] = w.w;
     u[4] = v.x; u[5] = v.y; u[6] = v.z; u[7] = v.w;
 }
+
+// A lane's 16 results at p; WIDE: p is on a 32-byte boundary, so that every store fills whole sectors.
+__device__ __forceinline__ void store_eight(void* p, const uint32_t (&w)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
+                 "r"(w[5]), "r"(w[6]), "r"(w[7])
+                 : "memory");
+}
+__device__ __forceinline__ void store_block(__nv_bfloat16* p, const uint32_t (&w)[8], bool wide) {  // already two to a word
+    if (wide) {
+        store_eight(p, w);
+    } else {
+        reinterpret_cast<uint4*>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        reinterpret_cast<uint4*>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+}
+__device__ __forceinline__ void store_block(float* p, const uint32_t (&u)[kSlice], bool wide) {
+    if (wide) {
+        const uint32_t a[8] = {u[0], u[1], u[2], u[3], u[4], u[5], u[6], u[7]}, b[8] = {u[8], u[9], u[10], u[11], u[12], u[13], u[14], u[15]};
+        store_eight(p, a);
+        store_eight(p + 8, b);
+    } else {
+        store_slice_vec(p, u);
+    }
+}
+// quantized values of 7 mantissa bits at most: the upper half of each word
+__device__ __forceinline__ void store_values(__nv_bfloat16* p, const uint32_t (&u)[kSlice], bool wide) {
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = __byte_perm(u[2 * i], u[2 * i + 1], 0x7632);
+    store_block(p, w, wide);
+}
+__device__ __forceinline__ void store_values(float* p, const uint32_t (&u)[kSlice], bool wide) { store_block(p, u, wide); }
 
 template <int W>
 __device__ __forceinline__ void store_codes(uint8_t* p, const uint32_t (&u)[kSlice], const uint32_t (&rq)[kSlice],
@@ -297,8 +330,7 @@ __global__ void __launch_bounds__(kApThreads, 2) mx_kv_append_kernel(const Appen
                             w[i] = *reinterpret_cast<const uint32_t*>(&p);
                         }
                         if constexpr (U == 8) {
-                            reinterpret_cast<uint4*>(y)[0] = make_uint4(w[0], w[1], w[2], w[3]);
-                            reinterpret_cast<uint4*>(y)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+                            store_block(y, w, a.wide[0]);
                         } else if constexpr (U == 4) {
 #pragma unroll
                             for (int i = 0; i < 4; ++i) reinterpret_cast<uint2*>(y)[i] = make_uint2(w[2 * i], w[2 * i + 1]);
@@ -307,14 +339,14 @@ __global__ void __launch_bounds__(kApThreads, 2) mx_kv_append_kernel(const Appen
                             for (int i = 0; i < kSlice; ++i) reinterpret_cast<uint16_t*>(y)[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
                         }
                     } else if constexpr (U >= 4) {
-                        store_slice_vec(y, u);
+                        store_block(y, u, a.wide[0]);
                     } else {
                         store_slice_guarded(y, 1, kSlice, u);
                     }
                 } else {
                     uint32_t yb[kSlice];
                     pack_block_to(a, KIND - 1, slot, h * nb + b, u, yb, store);
-                    if (a.dst[KIND]) store_slice_vec(y, yb);  // 16-byte aligned
+                    if (a.dst[KIND]) store_values(y, yb, a.wide[KIND]);  // 16-byte aligned
                 }
             }
             if (KIND > 0 && store && h == hl) pad_lines(a, KIND - 1, slot, lane);
@@ -397,6 +429,7 @@ extern "C" int mx_kv_append(const mx_kv_cache_t* cache, const void* k, int64_t l
     a.src[0] = q; a.src[1] = k; a.src[2] = v;
     a.dst[0] = q_out; a.dst[1] = k_dq; a.dst[2] = v_dq;
     a.ld_src[0] = ldq; a.ld_src[1] = ldk; a.ld_src[2] = ldv; a.ld_q = ldq_out;
+    for (int i = 0; i < 3; ++i) a.wide[i] = (uintptr_t)a.dst[i] % 32 == 0 && (i > 0 || n_tokens == 1 || ldq_out * eb % 32 == 0);
     a.nb = (int)(d / 16);
     a.heads[0] = q ? n_q : 0; a.heads[1] = a.heads[2] = cache->n_kv;
     const int hpi = 32 / a.nb;
