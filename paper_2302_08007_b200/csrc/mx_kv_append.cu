@@ -113,28 +113,49 @@ template <int W>
 __device__ __forceinline__ void store_codes(uint8_t* p, const uint32_t (&u)[kSlice], const uint32_t (&rq)[kSlice],
                                             const uint32_t (&cb)[kSlice / 2]) {
     uint32_t words[(kSlice * W + 31) / 32];
-    pack_words<W, kSlice, 2>(u, rq, cb, words);
     if constexpr (W == 8) {
+        // a word's four magnitudes by multiply-adds, its four signs from the top bytes of the values
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t q = rq[4 * i] + rq[4 * i + 1] * 0x100u + (rq[4 * i + 2] + rq[4 * i + 3] * 0x100u) * 0x10000u -
+                               (cb[2 * i] + cb[2 * i + 1] * 0x10000u) * 0x101u;
+            const uint32_t s = __byte_perm(__byte_perm(u[4 * i], u[4 * i + 1], 0x0073), __byte_perm(u[4 * i + 2], u[4 * i + 3], 0x0073), 0x5410);
+            words[i] = frag::lop3<frag::kAndOr>(s, 0x80808080u, q);
+        }
         *reinterpret_cast<uint4*>(p) = make_uint4(words[0], words[1], words[2], words[3]);
     } else {  // 10 or 6 bytes at a two-byte boundary
+        pack_words<W, kSlice, 2>(u, rq, cb, words);
 #pragma unroll
         for (int h = 0; h < W; ++h) *reinterpret_cast<uint16_t*>(p + 2 * h) = (uint16_t)(words[h >> 1] >> (16 * (h & 1)));
     }
 }
 
+// maxima that keep a NaN
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
+__device__ __forceinline__ float max_nan(float a, float b, float c) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+
 // Q(.) of a finite block of a Table II format, the fast formulation of quantize_slice for exactly this shape: u holds the fp32
-// bits; yb the quantized values' bits; rq, cb the raw magnitudes and their offsets for pack_words; returns the microexponents.
+// bits, pm the larger magnitude of each pair; yb the quantized values' bits; rq, cb the raw magnitudes and their offsets for
+// pack_words; returns the microexponents.
 template <int W>
-__device__ __forceinline__ uint32_t quantize_table2(const uint32_t (&u)[kSlice], const uint32_t (&pm)[kSlice / 2], uint32_t F23,
+__device__ __forceinline__ uint32_t quantize_table2(const uint32_t (&u)[kSlice], const float (&pm)[kSlice / 2], uint32_t F23,
                                                     uint32_t (&yb)[kSlice], uint32_t (&rq)[kSlice], uint32_t (&cb)[kSlice / 2]) {
     constexpr uint32_t kBase = ((uint32_t)(127 + 23 - (W - 2)) << 23) | 0x400000u, kMax = (1u << (W - 1)) - 1u;
     const float K = __uint_as_float(max(0x7F000000u - F23, 0x00400000u)), Kinv = __uint_as_float(max(F23, 0x00400000u));  // 2^(127-F), 2^(F-127)
     uint32_t micro = 0;
 #pragma unroll
     for (int j = 0; j < kSlice / 2; ++j) {
-        const uint32_t dm = min(F23 - (pm[j] & kExpMask), 0x00800000u);  // tau << 23
-        cb[j] = kBase - dm;
-        micro |= dm >> (23 - j);
+        const bool low = pm[j] < __uint_as_float(F23);  // tau: both below 2^(F-127)
+        cb[j] = low ? kBase - 0x00800000u : kBase;
+        if (low) micro |= 1u << j;
         const float C = __uint_as_float(cb[j]), Cmax = __uint_as_float(cb[j] + kMax);
 #pragma unroll
         for (int k = 2 * j; k < 2 * j + 2; ++k) {
@@ -150,13 +171,11 @@ __device__ __forceinline__ uint32_t quantize_table2(const uint32_t (&u)[kSlice],
 // One block of 16 values (fp32 bits u) of the key (which = 0) or value line of a slot.
 template <int W>
 __device__ __forceinline__ void pack_block_as(const bdr_planes_t& p, int64_t slot, int block, uint32_t (&u)[kSlice], uint32_t (&yb)[kSlice], bool store) {
-    uint32_t pm[kSlice / 2], top = 0;
+    float pm[kSlice / 2];  // a NaN stays one
 #pragma unroll
-    for (int j = 0; j < kSlice / 2; ++j) {
-        pm[j] = max(u[2 * j] & 0x7FFFFFFFu, u[2 * j + 1] & 0x7FFFFFFFu);
-        top = max(top, pm[j]);
-    }
-    const uint32_t F23 = top & kExpMask;
+    for (int j = 0; j < kSlice / 2; ++j) pm[j] = max_nan(fabsf(__uint_as_float(u[2 * j])), fabsf(__uint_as_float(u[2 * j + 1])));
+    const float top = max_nan(max_nan(max_nan(pm[0], pm[1], pm[2]), pm[3], pm[4]), max_nan(pm[5], pm[6], pm[7]));
+    const uint32_t F23 = __float_as_uint(top) & kExpMask;
     uint32_t rq[kSlice], cb[kSlice / 2], micro;
     if (F23 != kExpMask) {
         micro = quantize_table2<W>(u, pm, F23, yb, rq, cb);
@@ -247,23 +266,34 @@ __global__ void __launch_bounds__(kApThreads, 2) mx_kv_append_kernel(const Appen
     T* const ring = reinterpret_cast<T*>(smem) + warp * (D * kChunk);
     const int sub = warp % wpt;  // of the token's warps; iterations are dealt to them in turn
     const int total = a.iters[0] + a.iters[1] + a.iters[2];
-    int ahead = sub, to = 0, at = 0;
+    constexpr int kPer = 16 / (int)sizeof(T);
+    const int run = hpi * d;  // elements of an iteration
+    int ahead = sub, kind = -1, kind_end = 0, to = 0, at = 0, left = 0;
+    const T* from = nullptr;
+    auto find_kind = [&] {  // where iteration `ahead` finds its heads, and how many elements of the kind are left from there (of this lane's pieces on)
+        if (ahead >= total) return;
+        while (ahead >= kind_end) kind_end += a.iters[++kind];
+        const int first = (ahead - (kind_end - a.iters[kind])) * hpi;
+        from = static_cast<const T*>(a.src[kind]) + t * a.ld_src[kind] + (int64_t)first * d + lane * kPer;
+        left = (a.heads[kind] - first) * d - lane * kPer;
+    };
     auto fetch_next = [&] {
         if (ahead < total) {
-            const int kind = ahead < a.iters[0] ? 0 : (ahead < a.iters[0] + a.iters[1] ? 1 : 2);
-            const int first = (ahead - (kind == 0 ? 0 : (kind == 1 ? a.iters[0] : a.iters[0] + a.iters[1]))) * hpi;
-            const T* from = static_cast<const T*>(a.src[kind]) + t * a.ld_src[kind] + (int64_t)first * d;
-            const int n = min(hpi, a.heads[kind] - first) * d;
-            constexpr int kPer = 16 / (int)sizeof(T);
+            const int n = min(left, run - lane * kPer);
+            T* const dst = ring + to + lane * kPer;
 #pragma unroll
             for (int i = 0; i < kChunk; i += 32 * kPer)
-                if (i + lane * kPer < n) cp_async16(ring + to + i + lane * kPer, from + i + lane * kPer);
+                if (i < n) cp_async16(dst + i, from + i);
             ahead += wpt;
+            from += wpt * run;
+            left -= wpt * run;
+            if (ahead >= kind_end) find_kind();
         }
         cp_async_commit();
         to = to + kChunk == D * kChunk ? 0 : to + kChunk;
     };
     if constexpr (kRing) {
+        find_kind();
 #pragma unroll
         for (int i = 0; i + 1 < D; ++i) fetch_next();
     }
