@@ -37,7 +37,8 @@ struct AppendArgs {
     const int64_t *slots, *positions;
     const float *cosv, *sinv;
     int64_t ld_rot, n_pos, n_slots, n_tokens;
-    int rot_dim, nb, warps_per_token;
+    int rot_dim, nb, warps_per_token, wpt_log;  // (a power of two)
+    bool pad[2];                 // lines with bytes between their natural length and the pitch
     int* status;
 };
 
@@ -215,7 +216,7 @@ template <typename T, int U, bool INTERLEAVED>
 __global__ void __launch_bounds__(kApThreads, 2) mx_kv_append_kernel(const AppendArgs a) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int wpt = a.warps_per_token;
-    const int64_t t = (int64_t)blockIdx.x * (kApWarps / wpt) + warp / wpt;
+    const int64_t t = ((int64_t)blockIdx.x * kApWarps + warp) >> a.wpt_log;
     if (t >= a.n_tokens) return;
     const int nb = a.nb, hpi = 32 / nb, hl = lane / nb, b = lane - hl * nb;  // heads per iteration, this lane's head and block
     const int d = 16 * nb, rot = a.rot_dim, half = rot / 2;
@@ -264,7 +265,7 @@ __global__ void __launch_bounds__(kApThreads, 2) mx_kv_append_kernel(const Appen
     constexpr int kChunk = 32 * kSlice, D = kApStages;  // elements of an iteration at most
     extern __shared__ __align__(16) uint8_t smem[];
     T* const ring = reinterpret_cast<T*>(smem) + warp * (D * kChunk);
-    const int sub = warp % wpt;  // of the token's warps; iterations are dealt to them in turn
+    const int sub = warp & (wpt - 1);  // of the token's warps; iterations are dealt to them in turn
     const int total = a.iters[0] + a.iters[1] + a.iters[2];
     constexpr int kPer = 16 / (int)sizeof(T);
     const int run = hpi * d;  // elements of an iteration
@@ -301,7 +302,7 @@ __global__ void __launch_bounds__(kApThreads, 2) mx_kv_append_kernel(const Appen
     auto heads_of = [&](auto kind, int before) {
         constexpr int KIND = decltype(kind)::value;
         const int n = a.heads[KIND], step = wpt * hpi;
-        int h = ((sub + wpt * 8 - before % wpt) % wpt) * hpi + hl;
+        int h = ((sub - before) & (wpt - 1)) * hpi + hl;
         const bool mine = hl < hpi, turns = KIND < 2 && rot && e0 < rot;
         const T* x = static_cast<const T*>(a.src[KIND]) + t * a.ld_src[KIND] + (int64_t)h * d;
         T* y = static_cast<T*>(a.dst[KIND]) + (KIND == 0 ? t * a.ld_q : t * ((int64_t)n * d)) + (int64_t)h * d + e0;
@@ -379,7 +380,7 @@ __global__ void __launch_bounds__(kApThreads, 2) mx_kv_append_kernel(const Appen
                     if (a.dst[KIND]) store_values(y, yb, a.wide[KIND]);  // 16-byte aligned
                 }
             }
-            if (KIND > 0 && store && h == hl) pad_lines(a, KIND - 1, slot, lane);
+            if (KIND > 0 && store && a.pad[KIND == 2] && h == hl) pad_lines(a, KIND - 1, slot, lane);
             if constexpr (kRing) __syncwarp();  // the next copies may overwrite the heads
         }
     };
@@ -462,6 +463,10 @@ extern "C" int mx_kv_append(const mx_kv_cache_t* cache, const void* k, int64_t l
     for (int i = 0; i < 3; ++i) a.wide[i] = (uintptr_t)a.dst[i] % 32 == 0 && (i > 0 || n_tokens == 1 || ldq_out * eb % 32 == 0);
     a.nb = (int)(d / 16);
     a.heads[0] = q ? n_q : 0; a.heads[1] = a.heads[2] = cache->n_kv;
+    for (int i = 0; i < 2; ++i) {
+        const int64_t n = line / 16;
+        a.pad[i] = a.plane[i].ld_exps > n || a.plane[i].ld_micro > n || a.plane[i].ld_elems > n * 2 * (a.m[i] + 1);
+    }
     const int hpi = 32 / a.nb;
     for (int i = 0; i < 3; ++i) a.iters[i] = (a.heads[i] + hpi - 1) / hpi;
     a.slots = slots;
@@ -485,6 +490,7 @@ extern "C" int mx_kv_append(const mx_kv_cache_t* cache, const void* k, int64_t l
     int wpt = 1;
     while (wpt < kApWarps && n_tokens * wpt < (int64_t)sm_count() * kApWarps) wpt *= 2;
     a.warps_per_token = wpt;
+    while (1 << a.wpt_log < wpt) ++a.wpt_log;
     const bool inter = rotate && rot->interleaved;
     cudaStream_t st = (cudaStream_t)stream;
     return dt == BDR_F32 ? launch_append<float>(a, unit, inter, st) : launch_append<__nv_bfloat16>(a, unit, inter, st);
