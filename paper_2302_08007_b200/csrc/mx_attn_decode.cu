@@ -23,25 +23,16 @@ template <bool F32>
 __global__ void __launch_bounds__(kJoinThreads) mx_attn_join_kernel(const AttnArgs a) {
     __shared__ float2 wml[kJoinWarps];
     __shared__ __align__(16) float wo[kJoinWarps][256];
-    const int b = blockIdx.x / a.n_q, head = blockIdx.x - b * a.n_q, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int b = blockIdx.x, head = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     using T = typename std::conditional<F32, float, __nv_bfloat16>::type;
     T* out = static_cast<T*>(a.out) + (int64_t)b * a.ldo + (int64_t)head * a.d;
     const SeqRange r = seq_range(a, b);
     int w0 = 0, w1 = -1;
-    int64_t total = 0, p = 0;
+    const TileCounts c = count_tiles(a, lane, b);
+    const Split split(a, c.total);
     if (r.count > 0) {
-        const TileCounts c = count_tiles(a, lane, b);
-        total = c.total;
-        p = c.prefix;
-        // the last worker whose part starts at or before a tile holds it: begin(w) = floor(total w / workers) <= tile
-        auto holder = [&](int64_t tile) {
-            int w = min((int)((tile * a.workers + a.workers - 1) / total), a.workers - 1);
-            while (w + 1 < a.workers && worker_begin(total, w + 1, a.workers) <= tile) ++w;
-            while (w > 0 && worker_begin(total, w, a.workers) > tile) --w;
-            return w;
-        };
-        w0 = holder(p);
-        w1 = holder(p + r.count - 1);
+        w0 = split.holder(c.prefix);
+        w1 = split.holder(c.prefix + r.count - 1);
     }
     cudaGridDependencySynchronize();
     if (w0 == w1) return;
@@ -63,11 +54,8 @@ __global__ void __launch_bounds__(kJoinThreads) mx_attn_join_kernel(const AttnAr
         float2 x = make_float2(kAtNone, 0.f);
         int64_t part = -1;
         if (mine <= w1) {
-            const int64_t begin = worker_begin(total, mine, a.workers);
-            if (begin != worker_begin(total, mine + 1, a.workers)) {  // else a worker without work
-                part = ((int64_t)mine * 2 + (begin < p ? 1 : 0)) * a.n_q + head;
-                x = __ldcg(a.part_ml + part);
-            }
+            part = ((int64_t)mine * 2 + (split.begin(mine) < c.prefix ? 1 : 0)) * a.n_q + head;
+            x = __ldcg(a.part_ml + part);
         }
         float top = x.x;
 #pragma unroll
@@ -128,7 +116,7 @@ __global__ void __launch_bounds__(kJoinThreads) mx_attn_join_kernel(const AttnAr
 template <bool F32>
 static int launch_join(const AttnArgs& a, cudaStream_t st) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((int64_t)a.n_seqs * a.n_q));
+    cfg.gridDim = dim3((unsigned)a.n_seqs, (unsigned)a.n_q);
     cfg.blockDim = dim3(kJoinThreads);
     cfg.stream = st;
     cudaLaunchAttribute at[1];
@@ -212,6 +200,9 @@ int mx_attn_decode(const mx_kv_cache_t* cache, const void* q, int64_t ldq, bdr_d
     a.hw = p.hw; a.tw = p.tw; a.workers = p.workers;
     a.n_pages = (int)cache->n_pages; a.max_pages = (int)max_pages; a.cap = (int)max_pages * cache->page_size; a.window = window;
     a.page = make_fastdiv((uint32_t)cache->page_size);
+    a.by_workers = make_fastdiv((uint32_t)p.workers);
+    a.inv_pass = 65536 / p.per_pass + 1;
+    while (1 << a.hw_log < p.hw) ++a.hw_log;
     a.q_vec = (uintptr_t)q % (2 * eb) == 0 && (n_seqs == 1 || ldq % 2 == 0);
     a.o_vec = (uintptr_t)out % 16 == 0 && (n_seqs == 1 || ldo * eb % 16 == 0);
     a.scale2 = 2.f * scale * 1.44269504088896341f;

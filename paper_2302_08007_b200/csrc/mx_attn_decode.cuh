@@ -52,7 +52,8 @@ struct AttnArgs {
     int hw, tw, workers;                   // units of a group (one per warp), sets of warps, worker CTAs per group
     int n_pages, max_pages, cap, window;   // cap = max_pages * page_size
     int q_vec, o_vec;                      // two query elements may be read at once; results may be written 16 bytes at a time
-    FastDiv page;
+    FastDiv page, by_workers;
+    int hw_log, inv_pass;                  // log2 of hw; 65536 / per_pass rounded up
     float scale2, scale2_fast;             // 2 scale log2(e): the keys are decoded halved (and on the first way scaled)
     int* status;
 };
@@ -99,7 +100,21 @@ __device__ __forceinline__ TileCounts count_tiles(const AttnArgs& a, int lane, i
     return c;
 }
 
-__device__ __forceinline__ int64_t worker_begin(int64_t total, int w, int workers) { return total * w / workers; }
+// The line of all tiles in equal parts, one per worker: the first `more` have one tile more than the others' `each`.
+struct Split {
+    int64_t each, more;
+    __device__ __forceinline__ Split(const AttnArgs& a, int64_t total) {
+        each = total < (1ll << 31) ? (int64_t)fastdiv((uint32_t)total, a.by_workers) : total / a.workers;
+        more = total - each * a.workers;
+    }
+    __device__ __forceinline__ int64_t begin(int w) const { return each * w + min((int64_t)w, more); }
+    // the worker that has a tile of the line
+    __device__ __forceinline__ int holder(int64_t tile) const {
+        const int64_t bound = more * (each + 1), at = tile < bound ? tile : tile - bound, n = tile < bound ? each + 1 : each;
+        const int64_t w = at < (1ll << 31) && n < (1ll << 31) ? (int64_t)((uint32_t)at / (uint32_t)n) : at / n;
+        return (int)(tile < bound ? w : more + w);
+    }
+};
 
 __device__ __forceinline__ float exp2_approx(float x) {
     float y;
@@ -192,8 +207,9 @@ struct Segments {
             r = {0, 0, 0, 0};
             if (lane < a.n_seqs) r = seq_range(a, lane);
             const int64_t incl = inclusive_scan(r.count, lane), total = __shfl_sync(0xFFFFFFFFu, incl, 31);
-            u = worker_begin(total, w, a.workers);
-            u_end = worker_begin(total, w + 1, a.workers);
+            const Split split(a, total);
+            u = split.begin(w);
+            u_end = split.begin(w + 1);
             const unsigned hit = __ballot_sync(0xFFFFFFFFu, incl > u);
             b = hit ? __ffs(hit) - 1 : 0;
             prefix = __shfl_sync(0xFFFFFFFFu, incl - r.count, b);
@@ -204,9 +220,9 @@ struct Segments {
             known = true;
             return;
         }
-        const int64_t total = count_tiles(a, lane, 0).total;
-        u = worker_begin(total, w, a.workers);
-        u_end = worker_begin(total, w + 1, a.workers);
+        const Split split(a, count_tiles(a, lane, 0).total);
+        u = split.begin(w);
+        u_end = split.begin(w + 1);
         known = false;
         prefix = 0;
         if (u >= u_end) return;
@@ -252,7 +268,7 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
     seg.begin(a, blockIdx.x, lane);
     if (seg.u >= seg.u_end) return;  // uniform for the CTA
 
-    const int g = lane >> 2, c = lane & 3, hw = warp % a.hw, tw = warp / a.hw;
+    const int g = lane >> 2, c = lane & 3, hw = warp & (a.hw - 1), tw = warp >> a.hw_log;
     const int unit = blockIdx.y * a.hw + hw, mk = unit / a.passes, pass = unit - mk * a.passes, kv0 = mk * a.merge;
     const int kv_n = min(a.merge, a.n_kv - kv0), blocks = kv_n * a.nb, block0 = kv0 * a.nb;
     uint4* const qs = reinterpret_cast<uint4*>(smem + hw * S::kQBytes);
@@ -317,9 +333,10 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
         }
     };
 
-    // query head of a column, or -1
+    // query head of a column, or -1; the key-value head of the unit that it belongs to (below 16 columns the product is exact)
+    auto kv_of = [&](int col) { return (col * a.inv_pass) >> 16; };
     auto head_of = [&](int col) {
-        const int f = col / a.per_pass, i = pass * a.per_pass + (col - f * a.per_pass);
+        const int f = kv_of(col), i = pass * a.per_pass + (col - f * a.per_pass);
         return f < kv_n && i < a.group ? (kv0 + f) * a.group + i : -1;
     };
     auto sync_all = [&] {  // where one set of warps works alone there is nobody to wait for but the queries' loader, the warp itself
@@ -335,7 +352,7 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
         {
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const int col = 8 * n + g, head = head_of(col), f = col / a.per_pass;
+                const int col = 8 * n + g, head = head_of(col), f = kv_of(col);
                 const T* q = static_cast<const T*>(a.q) + (int64_t)b * a.ldq + (int64_t)max(head, 0) * a.d;
 #pragma unroll
                 for (int x = 0; x < KB / 2; ++x) {
@@ -557,7 +574,7 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            if (spoilt[e >> 1] >> ((8 * n + 2 * c + (e & 1)) / a.per_pass) & 1u) s[n][e] = __uint_as_float(0x7FC00000u);
+                            if (spoilt[e >> 1] >> kv_of(8 * n + 2 * c + (e & 1)) & 1u) s[n][e] = __uint_as_float(0x7FC00000u);
                 }
             }
             // ---- the tile's values
@@ -713,7 +730,7 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
                     float l = sum[n][e];
 #pragma unroll
                     for (int x = 4; x < 32; x <<= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, x);
-                    const int col = 8 * n + 2 * c + e, head = head_of(col), f = col / a.per_pass;
+                    const int col = 8 * n + 2 * c + e, head = head_of(col), f = kv_of(col);
                     if (head < 0) continue;
                     l *= 1.f / frag::kFastFactor;  // the weights' factor; the values' own is in the sums
                     const float norm = whole ? (l == 0.f ? 0.f : 2.f / l) : 2.f;  // the values were decoded halved

@@ -50,7 +50,9 @@ struct GemvArgs {
     int tokens, tokens_per_pass;
     int x32, y32;        // 32-bit activations / results (else bf16)
     int xvec;            // rows of activations start on 16-byte boundaries
-    int kw;              // warps that share a tile's K (a power of two, at most the steps there are)
+    int kw, kw_log;      // warps that share a tile's K (a power of two, at most the steps there are)
+    int rounds;          // of the groups over all tiles, rounded down; the first `rest` CTAs have one more
+    unsigned rest;
     int phase_steps;     // steps whose activations are in shared memory at once: all, or a multiple of kw in each of two buffers
 };
 
@@ -293,12 +295,12 @@ __global__ void __launch_bounds__((GemvShape<W, NT>::kThreads), 1) mx_gemv_kerne
     uint16_t* const xs = reinterpret_cast<uint16_t*>(smem + S::kXs);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
     uint8_t* const ring = smem + S::kReds * S::kRed + warp * (D * S::kStage);
-    const int kw = a.kw, my_k = warp & (kw - 1), group = warp / kw, groups = kWarps / kw;
+    const int kw = a.kw, my_k = warp & (kw - 1), group = warp >> a.kw_log, groups = kWarps >> a.kw_log;
     const int t0 = blockIdx.y * a.tokens_per_pass, nt = min(a.tokens_per_pass, a.tokens - t0), cols = X32 ? 3 * nt : nt;
     const int nb = (int)((a.k + 15) / 16), steps = (nb + 15) / 16;
     // tiles go to the CTAs in turn, then to a CTA's groups: every SM has the same number to within one
     const int64_t tiles = (a.n + 15) / 16, stride = (int64_t)gridDim.x * groups;
-    const int rounds = (int)((tiles - blockIdx.x + stride - 1) / stride);  // of the CTA's first group; the others may have one fewer
+    const int rounds = a.rounds + (blockIdx.x < a.rest ? 1 : 0);  // of the CTA's first group; the others may have one fewer
     const int64_t pitch = (int64_t)min(a.phase_steps, steps) * kGvStep + 32;
     float acc[NT][4];
 #pragma unroll
@@ -330,7 +332,6 @@ __global__ void __launch_bounds__((GemvShape<W, NT>::kThreads), 1) mx_gemv_kerne
     // steps, the first step of weights goes ahead of them (16384 x 4096 MX6: 18.7 us, else 19.0; with two steps MX9 16.5, else 16.2).
     constexpr bool kWeightsFirst = NT == 1 && D == 3;
     constexpr int kBehind = kWeightsFirst ? D - 2 : D - 1;  // steps of weights behind the activations
-    const int phases = (steps + a.phase_steps - 1) / a.phase_steps;
     using X = StageX<W, NT, X32>;
     if (kWeightsFirst) queue_next();
     if (steps > 0) X::copy(a, xs, pitch, t0, nt, 0, min(a.phase_steps, steps));
@@ -348,7 +349,7 @@ __global__ void __launch_bounds__((GemvShape<W, NT>::kThreads), 1) mx_gemv_kerne
         const bool active = tile < tiles;
         for (int p0 = 0; p0 < steps; p0 += a.phase_steps) {
             const int p1 = min(p0 + a.phase_steps, steps);
-            if (phases > 1) {
+            if (a.phase_steps < steps) {
                 if (!first) {
                     // the group with this phase's activations is the first of `queued`; with D or more it has been waited for
                     if (queued == 0) cp_async_commit();
@@ -448,7 +449,10 @@ static int launch_gemv(GemvArgs a, cudaStream_t st) {
         a.phase_steps = ((steps + phases - 1) / phases + a.kw - 1) / a.kw * a.kw;
     }
     const size_t smem = S::kXs + (size_t)(steps > fit ? 2 : 1) * cols * (a.phase_steps * kGvStep * 2 + 64);
-    const int64_t ctas = std::min<int64_t>(sms, tiles);
+    const int64_t ctas = std::min<int64_t>(sms, tiles), stride = ctas * (S::kWarps / a.kw);
+    while (1 << a.kw_log < a.kw) ++a.kw_log;
+    a.rounds = (int)(tiles / stride);
+    a.rest = (unsigned)std::min<int64_t>(tiles % stride, ctas);
     const dim3 grid((unsigned)ctas, (unsigned)((a.tokens + a.tokens_per_pass - 1) / a.tokens_per_pass));
     mx_gemv_kernel<W, NT, X32><<<grid, S::kThreads, smem, st>>>(a);
     return cudaGetLastError() == cudaSuccess ? BDR_OK : BDR_ERR_CUDA;
