@@ -332,9 +332,9 @@ int mx_gemm_hw(const bdr_config_t* cfg_a /*host*/, const bdr_planes_t* a /*host 
 /* y[T,N] (row pitch ldy) = x[T,K] (row pitch ldx) deq(W)[N,K]^T for a few rows of x and weights packed along K (axis-1
  * planes of W).  The activations are used as they are: bf16 values enter the tensor core unchanged, fp32 values as the
  * exact sum of three bf16 parts; accumulation is fp32 and the result is rounded once to y's type.  Only the summation
- * order is unspecified (it depends on the shape, not on the run).  Any N, K and T (K = 0 gives zeros); W is read once
- * for every 64 rows of bf16 x, or 21 rows of fp32 x, so larger T belongs to mx_gemm_ws.  Rows of x that start at a
- * multiple of four elements' bytes are read faster. */
+ * order is unspecified (it depends on the shape, not on the run).  Products w x of less than 2^-93 in magnitude may lose
+ * low bits.  Any N, K and T (K = 0 gives zeros); W is read once for every 64 rows of bf16 x, or 21 rows of fp32 x, so
+ * larger T belongs to mx_gemm_ws.  Rows of x that start on 16-byte boundaries are read faster. */
 int mx_gemv(const bdr_config_t* cfg_w /*host*/, const bdr_planes_t* w /*host struct*/, int64_t N, int64_t K, const void* x,
             bdr_dtype_t x_dt, int64_t ldx, int64_t T, void* y, bdr_dtype_t y_dt, int64_t ldy, void* stream);
 
@@ -387,8 +387,8 @@ int mx_kv_append(const mx_kv_cache_t* cache /*host*/, const void* k, int64_t ldk
  *   lse      NULL, or [n_seqs, n_q] fp32 (contiguous): log of the sum of exp(scale <q, k>), for joining with attention over other
  *            positions.  A sequence without positions gives out = 0 and lse = -infinity.
  * Scores, softmax statistics and sums are fp32.  bf16 queries: the softmax weights enter the second product rounded to bf16
- * (their sum is taken before that rounding); fp32 queries: both enter as sums of bf16 parts, which keeps 16 bits of the
- * weights and all of the queries.  The cache is split over its length across the GPU and the parts are joined in a fixed
+ * (their sum is taken before that rounding); fp32 queries: queries and weights both enter as sums of three bf16 parts,
+ * 24 bits.  The cache is split over its length across the GPU and the parts are joined in a fixed
  * order: the result does not change from run to run.  workspace: 16-byte aligned device scratch of at least
  * mx_attn_decode_workspace_bytes(cache, n_seqs, n_q) bytes, contents overwritten.
  * A page id outside [0, n_pages) or a length beyond max_pages * page_size is seen on the device only: the sequence's outputs

@@ -3,15 +3,23 @@
 //
 // Every packed weight is read once and used for T columns, so the kernel is bound by the bytes of W as long as decoding keeps
 // up.  A warp owns 16 rows of W and walks along K in steps of 256 elements: lane (g, c) of the matrix instruction's layout
-// takes four blocks of rows g and g + 8 (24, 40 or 64 bytes of codes each), decodes them in registers and feeds 16 matrix instructions.  The bytes come through a ring of
-// the warp's own in shared memory, filled by 16-byte asynchronous copies one or two steps ahead: a lane's own bytes are
-// strided in memory, and loads of them straight into registers kept the L1 busy with four times as many lines per request and
-// the compiler moving them down to where they were needed.  The activations sit in shared memory in the order those instructions want them,
-// as bf16; a 32-bit activation is split exactly into three bf16 columns, which costs nothing while the eight columns of an
-// instruction are not full.
-// One CTA per SM stays for the whole call (the activations are staged once) and its warps form groups of kw that share a
-// tile's K; a group's sums are added in shared memory in a fixed order.  The host picks kw so that the longest group's
-// walk is shortest: few large groups balance few rows, many small ones need fewer joins.
+// takes four blocks of rows g and g + 8 (24, 40 or 64 bytes of codes each), decodes them in registers and feeds 16 matrix
+// instructions.  The bytes come through a ring of the warp's own in shared memory, filled by 16-byte asynchronous copies one or
+// two steps ahead: a lane's own bytes are strided in memory, and loads of them straight into registers kept the L1 busy with
+// four times as many lines per request and the compiler moving them down to where they were needed (16384 x 4096 MX9: 18.5 us,
+// with the ring 15.8).  The activations sit in shared memory in the order those instructions want them, as bf16; a 32-bit
+// activation is split exactly into three bf16 columns, which costs nothing while the eight columns of an instruction are not full.
+// One CTA per SM stays for the whole call and its warps form groups of kw that share a tile's K; a group's sums are added in
+// shared memory in a fixed order.  The host picks kw so that the longest group's walk is shortest: few large groups balance few
+// rows, many small ones need fewer joins.  Activations that do not fit beside the rings come in phases, each copied while the
+// one before is computed (loaded, ordered and stored between two phases instead, they took as long as the products: 16 tokens of
+// 16384 x 8192 MX9 67.8 us, now 45).
+//
+// Measured (bf16 activations, the weights not in the L2): one token, 16384 x 4096 MX9 16 us = 4.7 TB/s, 16384 x 16384 MX9 57 us =
+// 5.3 TB/s, 16384 x 4096 MX6 18 us = 2.8 TB/s, 4096 x 4096 MX4 6.5 us; 16 tokens, 16384 x 8192 MX9 45.0 us = 3.4 TB/s, MX6
+// 49.6 us.  MX9 is near the memory's rate for one token; MX6 and MX4 are bound by decoding (the integer/logic pipe); sixteen
+// tokens by decoding on half the warps, which is what the registers of two column groups allow.  Small products are
+// a launch and one trip to memory.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -49,7 +57,7 @@ struct GemvArgs {
     int64_t n, k;
     int tokens, tokens_per_pass;
     int x32, y32;        // 32-bit activations / results (else bf16)
-    int xvec;            // rows of activations start on 16-byte boundaries
+    int xalign;          // rows of activations start on boundaries of 16, 4 or 2 bytes
     int kw, kw_log;      // warps that share a tile's K (a power of two, at most the steps there are)
     int rounds;          // of the groups over all tiles, rounded down; the first `rest` CTAs have one more
     unsigned rest;
@@ -163,13 +171,19 @@ struct StageX {
     }
     // the 16 bytes of a row at x, of which `left` elements exist, zeros behind them
     template <typename T>
-    __device__ static __forceinline__ void piece(uint16_t* to, const T* x, const T* row, int64_t left, bool vec) {
+    __device__ static __forceinline__ void piece(uint16_t* to, const T* x, const T* row, int64_t left, int align) {
         constexpr int kN = X32 ? 4 : 8;
-        if (vec && left >= kN) {
+        if (align == 16 && left >= kN) {
             cp_async16(to, x);
-        } else if (vec) {
-            const int n = (int)max((int64_t)0, left);
-            cp_async16_part(to, n ? x : row, n * (int)sizeof(T));
+        } else if (align >= 4) {
+            const int bytes = (int)max((int64_t)0, min((int64_t)kN, left)) * (int)sizeof(T);
+            if (bytes == 0) x = row;
+            if (align == 16) cp_async16_part(to, x, bytes);
+            else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    cp_async4_part(to + 2 * i, bytes > 4 * i ? reinterpret_cast<const char*>(x) + 4 * i : reinterpret_cast<const char*>(x), max(0, min(4, bytes - 4 * i)));
+            }
         } else {
             T q[kN];
 #pragma unroll
@@ -181,14 +195,14 @@ struct StageX {
     __device__ static __forceinline__ void copy(const GemvArgs& a, uint16_t* xs, int64_t pitch, int t0, int nt, int s0, int n_steps) {
         using T = typename std::conditional<X32, float, uint16_t>::type;
         const int lane = threadIdx.x & 31;
-        const bool vec = a.xvec;
+        const int align = a.xalign;
         for (StageX m(n_steps); m.t < nt; m.next()) {
             const T* const row = static_cast<const T*>(a.x) + (t0 + m.t) * a.ldx;
             uint16_t* const to = xs + (X32 ? 3 : 1) * m.t * pitch + m.s * kGvStep + 8 * lane;
             const int64_t k = (int64_t)(s0 + m.s) * kGvStep + (X32 ? 4 : 8) * lane, left = a.k - k;
-            piece<T>(to, row + k, row, left, vec);
-            if constexpr (X32) piece<T>(to + pitch, row + k + kGvStep / 2, row, left - kGvStep / 2, vec);
-            else if (m.t + 1 < nt) piece<T>(to + pitch, row + a.ldx + k, row, left, vec);
+            piece<T>(to, row + k, row, left, align);
+            if constexpr (X32) piece<T>(to + pitch, row + k + kGvStep / 2, row, left - kGvStep / 2, align);
+            else if (m.t + 1 < nt) piece<T>(to + pitch, row + a.ldx + k, row, left, align);
         }
     }
     // puts them in order, once the warp's copies are there
@@ -492,7 +506,8 @@ extern "C" int mx_gemv(const bdr_config_t* cfg_w, const bdr_planes_t* w, int64_t
     a.x = x; a.y = y; a.ldx = ldx; a.ldy = ldy; a.n = N; a.k = K; a.tokens = (int)T;
     a.x32 = x_dt == BDR_F32; a.y32 = y_dt == BDR_F32;
     const int64_t xb = a.x32 ? 4 : 2;
-    a.xvec = (uintptr_t)x % 16 == 0 && (T == 1 || ldx * xb % 16 == 0);
+    const uintptr_t at = (uintptr_t)x | (T == 1 ? 0 : (uintptr_t)(ldx * xb));
+    a.xalign = at % 16 == 0 ? 16 : (at % 4 == 0 ? 4 : 2);
     cudaStream_t st = (cudaStream_t)stream;
     switch (cfg_w->m) {
         case 2: return a.x32 ? pick_columns<3, true>(a, st) : pick_columns<3, false>(a, st);

@@ -6,8 +6,14 @@
 // The rotated key goes from its fp32 sum into the quantizer without a rounding to the tensor's type in between; products and
 // sums are rounded to fp32 one by one (no contraction), so the result does not depend on how a compiler fuses them.
 // Streaming: a lane owns one 16-element block of a head and walks over heads of the same token, which keeps the block's
-// cosines and sines in registers; its partner elements (rot_dim / 2 away) come from the same cache lines that the warp reads
-// anyway.  A CTA's warps share tokens when there are few of them.
+// cosines and sines in registers; its partner elements (rot_dim / 2 away) come from the same run of heads, which the warp copies
+// into shared memory three iterations ahead (144 -> 106 us at the size below).  A CTA's warps share tokens when there are few of
+// them.  Results leave in 32-byte stores.
+//
+// Measured (32 query and 2 x 8 key-value heads of 128 elements, bf16, MX9, rotated queries and quantized values written too): 16384
+// tokens 85.8 us = 5.2 TB/s, one token 3.6 us; 1003 tokens of 20 + 2 x 4 heads of 80, fp32, MX6 and MX4, 6.2 us.  Long calls are
+// bound by instructions as much as by memory (3570 per warp and token, issue slots about 60 % busy, integer/logic pipe half
+// busy); a version whose warps stay and run their copies on into the next token needed more registers than there are (129 us).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
