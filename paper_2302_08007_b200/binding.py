@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass
 
 import torch
@@ -49,6 +50,9 @@ class _KVCache(C.Structure):
 class _Rotation(C.Structure):
     _fields_ = [("cos", C.c_void_p), ("sin", C.c_void_p), ("positions", C.c_void_p), ("ld", C.c_int64), ("n_pos", C.c_int64),
                 ("rot_dim", C.c_int32), ("interleaved", C.c_int32)]
+
+
+_ROTATION = struct.Struct("@PPPqqii")  # the same bytes, made once per call
 
 
 @dataclass(frozen=True)
@@ -501,9 +505,13 @@ def mx_gemv(cfg_w: Config, w: Planes, N: int, K: int, x: torch.Tensor, y: torch.
 
 def _heads(t: torch.Tensor, what: str):
     """Shape and token pitch of a [tokens, heads, head_dim] tensor whose tokens are contiguous."""
-    if t.dim() != 3:
+    shape = t.shape
+    if len(shape) != 3:
         raise ValueError("%s: expected [tokens, heads, head_dim]" % what)
-    (n, h, d), (s0, s1, s2) = shape, _ = t.shape, t.stride()
+    n, h, d = shape
+    if t.is_contiguous():
+        return shape, h * d
+    s0, s1, s2 = t.stride()
     if s2 != 1 or (s1 != d and h > 1):
         raise ValueError("%s: expected contiguous heads" % what)
     return shape, s0 if s0 > h * d else h * d
@@ -519,7 +527,8 @@ def mx_kv_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.
     shape, ldk = _heads(k, "k")
     vshape, ldv = _heads(v, "v")
     T, dtype = shape[0], k.dtype
-    _on_gpu(k, v, slots, cache.k.elems)
+    if not (k.is_cuda and v.is_cuda and slots.is_cuda and cache.k.elems.is_cuda):
+        raise ValueError("expected CUDA tensors")
     if vshape != shape or shape[1] != cache.n_kv or shape[2] != cache.head_dim or v.dtype != dtype:
         raise ValueError("k and v are [tokens, n_kv, head_dim] of one dtype")
     if slots.dtype != torch.int64 or slots.shape != (T,) or not slots.is_contiguous():
@@ -528,19 +537,20 @@ def mx_kv_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.
     if cos is not None:
         if sin is None or positions is None:
             raise ValueError("cos, sin and positions go together")
-        _on_gpu(cos, sin, positions)
+        if not (cos.is_cuda and sin.is_cuda and positions.is_cuda):
+            raise ValueError("expected CUDA tensors")
         (n_pos, half), pitch = cos.shape, cos.stride()
         if cos.dtype != torch.float32 or sin.dtype != torch.float32 or sin.shape != cos.shape or sin.stride() != pitch or (pitch[1] != 1 and half > 1):
             raise ValueError("cos, sin: float32 [n_pos, rot_dim / 2] with one pitch")
         if positions.dtype != torch.int64 or positions.shape != (T,) or not positions.is_contiguous():
             raise ValueError("positions: contiguous int64 [tokens]")
-        rotation = _Rotation(cos.data_ptr(), sin.data_ptr(), positions.data_ptr(), max(pitch[0], half), n_pos, 2 * half, int(interleaved))
-        rot = C.addressof(rotation)
+        rot = _ROTATION.pack(cos.data_ptr(), sin.data_ptr(), positions.data_ptr(), max(pitch[0], half), n_pos, 2 * half, interleaved)
     n_q = ldq = ldo = 0
     if q is not None:
         if q_out is None:
             raise ValueError("q needs q_out")
-        _on_gpu(q, q_out)
+        if not (q.is_cuda and q_out.is_cuda):
+            raise ValueError("expected CUDA tensors")
         (tq, n_q, dq), ldq = _heads(q, "q")
         oshape, ldo = _heads(q_out, "q_out")
         if tq != T or dq != cache.head_dim or oshape != q.shape or q.dtype != dtype or q_out.dtype != dtype:
@@ -565,7 +575,8 @@ def mx_attn_decode(cache: KVCache, q: torch.Tensor, page_table: torch.Tensor, le
     """out [B, n_q, head_dim] = attention of one query token per sequence, q [B, n_q, head_dim], over the cached positions
     t < lengths[b] (int32 [B]; the last `window` of them when window > 0) whose pages are page_table[b] (int32 [B, max_pages]).
     lse: float32 [B, n_q].  scale: head_dim ** -0.5 when None."""
-    _on_gpu(q, page_table, lengths, out, workspace, cache.k.elems)
+    if not (q.is_cuda and page_table.is_cuda and lengths.is_cuda and out.is_cuda and workspace.is_cuda and cache.k.elems.is_cuda):
+        raise ValueError("expected CUDA tensors")
     (B, n_q, d), ldq = _heads(q, "q")
     oshape, ldo = _heads(out, "out")
     if d != cache.head_dim or oshape != q.shape or out.dtype != q.dtype:
