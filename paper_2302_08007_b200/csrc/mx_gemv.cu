@@ -38,13 +38,15 @@ constexpr int kGvSmem = 227 * 1024;
 constexpr int kGvMaxCols = 64;               // columns (tokens, or thirds of a 32-bit token) of one pass
 
 // Warps of a CTA and steps in a warp's ring: 16 warps of up to 128 registers when there are few columns, 8 (and shared memory left
-// for the activations) when there are more.
+// for the activations) when there are more.  Two groups of columns run with 16 warps for 3-bit codes, whose rings are small (16 tokens of
+// 4096 x 4096: 9.7 us, with eight warps 10.9; 10 of 16384 x 4096: 20.2, 23.1); with 5-bit codes the activations of K = 4096 would no
+// longer fit beside the rings (16 of 4096 x 4096: 13.5 us, with eight 11.5).
 template <int W, int NT> struct GemvShape {
-    static constexpr int kWarps = NT == 1 ? 16 : 8, kThreads = 32 * kWarps;
+    static constexpr int kWarps = NT == 1 || (NT == 2 && W == 3) ? 16 : 8, kThreads = 32 * kWarps;
     static constexpr int kRed = kWarps * 8 * NT * 16 * 4;  // bytes of all warps' sums of a tile
     static constexpr int kPitch = 32 * W;                  // bytes of codes of a row and step
     static constexpr int kAtX = 16 * kPitch, kStage = kAtX + 2 * 256;  // 16 rows of codes, of exponents, of microexponents
-    static constexpr int kStages = NT <= 2 && W != 8 ? 3 : 2;
+    static constexpr int kStages = W != 8 && (NT == 1 || (NT == 2 && W == 5)) ? 3 : 2;
     static constexpr int kReds = NT < 4 ? 2 : 1;                       // buffers of sums
     static constexpr int kXs = kReds * kRed + kWarps * kStages * kStage;  // where the activations start
 };
