@@ -267,6 +267,9 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
     using L = AttnTile<WK, WV, MAXB, FULL>;
     using T = typename std::conditional<F32, float, __nv_bfloat16>::type;
     constexpr int KB = S::kKeyBlocks, VB = S::kValBlocks, PARTS = S::kParts, D = L::kStages;
+    // The weights' factor 2^32 is part of the exponent's argument, which costs its last bits; 32-bit queries have it multiplied to the
+    // weights instead (with the partial sums of scores, below, that took their error from 9e-7 to 2.4e-7 of the result).
+    constexpr float kLift = F32 ? 0.f : kAtLift;
     constexpr int kRing = attn_ring_bytes<WK, WV, MAXB, NT, F32, FULL>();
     extern __shared__ __align__(128) uint8_t smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -530,13 +533,19 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
                             for (int e = 0; e < 4; ++e)
                                 y[i][e] = frag::decode_word<WK, FAST>(kr[i], b0, kr[i], b1, 2 * j + e, frag::scale_word(sc[i], j + (e >> 1)));
 #pragma unroll
-                        for (int part = PARTS - 1; part >= 0; --part)
+                        for (int n = 0; n < NT; ++n) {
+                            float d[4] = {0.f, 0.f, 0.f, 0.f};  // 32-bit queries: short sums in the tensor core, as for the output below
 #pragma unroll
-                            for (int n = 0; n < NT; ++n) {
+                            for (int part = PARTS - 1; part >= 0; --part) {
                                 const uint4 qv = qs[((part * MAXB / 2 + 4 * x + j / 2) * NT + n) * 32 + lane];
-                                frag::mma_bf16(s[n], y[0][0], y[1][0], y[0][1], y[1][1], qv.x, qv.y);
-                                frag::mma_bf16(s[n], y[0][2], y[1][2], y[0][3], y[1][3], qv.z, qv.w);
+                                frag::mma_bf16(F32 ? d : s[n], y[0][0], y[1][0], y[0][1], y[1][1], qv.x, qv.y);
+                                frag::mma_bf16(F32 ? d : s[n], y[0][2], y[1][2], y[0][3], y[1][3], qv.z, qv.w);
                             }
+                            if constexpr (F32) {
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) s[n][e] += d[e];
+                            }
+                        }
                     }
                 }
             };
@@ -609,7 +618,7 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
                 for (int i = 0; i < 4; ++i)  // finite values: a weight of zero times an infinity that may lie there would not do
                     if (!(here >> (2 * c + (i & 1) + 8 * (i >> 1)) & 1u)) vf[i] = 0x7F7Fu;
             }
-            // ---- softmax weights relative to the running references, t = log2 of a weight (lifted by kAtLift)
+            // ---- softmax weights relative to the running references, t = log2 of a weight (lifted by kLift)
             float t[NT][4], high = 0.f;
 #pragma unroll
             for (int n = 0; n < NT; ++n)
@@ -618,7 +627,7 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
                     t[n][e] = s[n][e] - ref[n][e & 1];
                     high = fmaxf(high, t[n][e]);
                 }
-            if (__any_sync(0xFFFFFFFFu, high > kAtLift + kAtSlack)) {
+            if (__any_sync(0xFFFFFFFFu, high > kLift + kAtSlack)) {
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -626,7 +635,7 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
                         float top = fmaxf(s[n][e], s[n][e + 2]);
 #pragma unroll
                         for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
-                        top = fmaxf(top - kAtLift, ref[n][e]);
+                        top = fmaxf(top - kLift, ref[n][e]);
                         const float f = exp2_approx(ref[n][e] - top);
                         ref[n][e] = top;
                         sum[n][e] *= f;
@@ -642,6 +651,7 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     p[n][e] = exp2_approx(t[n][e]);
+                    if constexpr (F32) p[n][e] *= frag::kFastFactor;
                     sum[n][e & 1] += p[n][e];
                 }
             // ---- output
@@ -765,8 +775,8 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
                         }
                     }
                     if (g == 0) {
-                        if (!whole) a.part_ml[part] = make_float2(ref[n][e] + kAtLift, l);
-                        else if (a.lse) a.lse[(int64_t)b * a.n_q + head] = (ref[n][e] + kAtLift + log2f(l)) * 0.69314718055994531f;
+                        if (!whole) a.part_ml[part] = make_float2(ref[n][e] + kLift, l);
+                        else if (a.lse) a.lse[(int64_t)b * a.n_q + head] = (ref[n][e] + kLift + log2f(l)) * 0.69314718055994531f;
                     }
                 }
         }
