@@ -386,10 +386,10 @@ int mx_kv_append(const mx_kv_cache_t* cache /*host*/, const void* k, int64_t ldk
  *   q, out   [n_seqs, n_q, head_dim] of `dt` with sequence pitches ldq and ldo; n_q a multiple of n_kv
  *   lse      NULL, or [n_seqs, n_q] fp32 (contiguous): log of the sum of exp(scale <q, k>), for joining with attention over other
  *            positions.  A sequence without positions gives out = 0 and lse = -infinity.
- * Scores, softmax statistics and sums are fp32.  bf16 queries: the softmax weights enter the second product rounded to bf16
- * (their sum is taken before that rounding); fp32 queries: queries and weights both enter as sums of three bf16 parts,
- * 24 bits.  The cache is split over its length across the GPU and the parts are joined in a fixed
- * order: the result does not change from run to run.  workspace: 16-byte aligned device scratch of at least
+ * Scores, softmax statistics and sums are fp32.  The softmax weights enter the second product as sums of two bf16 parts (bf16
+ * queries: 16 bits; the weights' sum is taken before that rounding) or three (fp32 queries: 24 bits, as the queries themselves).
+ * The cache is split over its length across the GPU and the parts are joined in a fixed order: the result does not change from
+ * run to run.  workspace: 16-byte aligned device scratch of at least
  * mx_attn_decode_workspace_bytes(cache, n_seqs, n_q) bytes, contents overwritten.
  * A page id outside [0, n_pages) or a length beyond max_pages * page_size is seen on the device only: the sequence's outputs
  * are NaN and BDR_ERR_SIZE is left in the sticky word of bdr_device_status.  A negative length counts as zero. */

@@ -141,6 +141,9 @@ struct AttnShape {
     static constexpr int kThreads = 32 * kWarps;
     static constexpr int kKeyBlocks = MAXB / 4, kValBlocks = MAXB / 8;  // per lane and token
     static constexpr int kParts = F32 ? 3 : 1;
+    // bf16 parts of a softmax weight.  One, rounded to eight bits, took the error of a bf16 result from 1.7e-3 (the result's own rounding)
+    // to 2.3e-3 over long sequences; the second costs 1 to 4 % (64 sequences of 2048 to 8096, MX6: 187 us, with one 184).
+    static constexpr int kWeightParts = F32 ? 3 : 2;
     static constexpr int kMaxUnits = F32 ? 4 : 8;  // units of a group: their queries share the memory with the rings
     static constexpr int kQBytes = kParts * MAXB * NT * 32 * 8;          // per unit
     static constexpr int kSums = kValBlocks * 8 * NT * 4 + NT * 4;       // a lane's sums, references and weights
@@ -266,7 +269,7 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
     using S = AttnShape<MAXB, NT, F32>;
     using L = AttnTile<WK, WV, MAXB, FULL>;
     using T = typename std::conditional<F32, float, __nv_bfloat16>::type;
-    constexpr int KB = S::kKeyBlocks, VB = S::kValBlocks, PARTS = S::kParts, D = L::kStages;
+    constexpr int KB = S::kKeyBlocks, VB = S::kValBlocks, PARTS = S::kParts, WPARTS = S::kWeightParts, D = L::kStages;
     // The weights' factor 2^32 is part of the exponent's argument, which costs its last bits; 32-bit queries have it multiplied to the
     // weights instead (with the partial sums of scores, below, that took their error from 9e-7 to 2.4e-7 of the result).
     constexpr float kLift = F32 ? 0.f : kAtLift;
@@ -657,7 +660,7 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
             // ---- output
             auto output = [&](auto way) {
                 constexpr bool FAST = decltype(way)::value;
-                uint32_t pb[NT][PARTS][2];  // P^T fragments (32-bit: three parts of eight bits)
+                uint32_t pb[NT][WPARTS][2];  // P^T fragments
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -665,7 +668,7 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
                         constexpr float kLower = FAST ? 1.f : 1.f / frag::kFastFactor;
                         float lo = p[n][2 * h] * kLower, hi = p[n][2 * h + 1] * kLower;
 #pragma unroll
-                        for (int part = 0; part < PARTS; ++part) {
+                        for (int part = 0; part < WPARTS; ++part) {
                             const uint32_t w = pack_bf16x2(lo, hi);
                             pb[n][part][h] = frag::transpose8x8(w);
                             lo -= __uint_as_float(w << 16);
@@ -683,14 +686,17 @@ __global__ void __launch_bounds__((AttnShape<MAXB, NT, F32>::kThreads), 1) mx_at
                         const uint32_t a2 = frag::decode_word<WV, FAST>(vb[2][x].w, 0, vb[3][x].w, 0, 2 * j, w1), a3 = frag::decode_word<WV, FAST>(vb[2][x].w, 0, vb[3][x].w, 0, 2 * j + 1, w1);
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
-                            if constexpr (F32) {  // a long sum in the tensor core need not round to nearest: a tile's products are added with fp32 additions
+                            // A long sum in the tensor core is cut off rather than rounded, up to 2^-23 of it per tile.  32-bit queries have a tile's
+                            // products added with fp32 additions; a bf16 result, rounded by 2^-9 itself, would gain nothing from the 1 to 4 % that costs.
+                            if constexpr (F32) {
                                 float d[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                                for (int part = PARTS - 1; part >= 0; --part) frag::mma_bf16(d, a0, a1, a2, a3, pb[n][part][0], pb[n][part][1]);
+                                for (int part = WPARTS - 1; part >= 0; --part) frag::mma_bf16(d, a0, a1, a2, a3, pb[n][part][0], pb[n][part][1]);
 #pragma unroll
                                 for (int e = 0; e < 4; ++e) o[8 * x + j][n][e] += d[e];
                             } else {
-                                frag::mma_bf16(o[8 * x + j][n], a0, a1, a2, a3, pb[n][0][0], pb[n][0][1]);
+#pragma unroll
+                                for (int part = WPARTS - 1; part >= 0; --part) frag::mma_bf16(o[8 * x + j][n], a0, a1, a2, a3, pb[n][part][0], pb[n][part][1]);
                             }
                         }
                     }
