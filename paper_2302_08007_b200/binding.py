@@ -490,6 +490,16 @@ def _on_gpu(*tensors):
             raise ValueError("expected CUDA tensors")
 
 
+def _pitch(stride: int, rows: int, width: int, what: str) -> int:
+    """The pitch of `rows` rows of `width` elements.  With one row at most a stride means nothing; else rows that share memory (an
+    expanded view, say) are refused, since a kernel takes a pitch of at least a row."""
+    if stride >= width:
+        return stride
+    if rows > 1:
+        raise ValueError("%s: rows share memory (an expanded or overlapping view): make it contiguous" % what)
+    return width
+
+
 def mx_gemv(cfg_w: Config, w: Planes, N: int, K: int, x: torch.Tensor, y: torch.Tensor, stream=None) -> torch.Tensor:
     """y[T,N] = x[T,K] @ deq(w)[N,K]^T for a few rows of x (float32 or bfloat16; y likewise) and weights packed along K."""
     x2, y2 = x if x.dim() == 2 else x.unsqueeze(0), y if y.dim() == 2 else y.unsqueeze(0)
@@ -498,8 +508,8 @@ def mx_gemv(cfg_w: Config, w: Planes, N: int, K: int, x: torch.Tensor, y: torch.
         raise ValueError("x is [T, K], y is [T, N], rows contiguous, and the planes hold N lines")
     _on_gpu(x, y, w.elems)
     c, p = cfg_w.c(), w.c()
-    _check(lib().mx_gemv(C.addressof(c), C.addressof(p), N, K, x2.data_ptr(), _dt(x2), ldx if ldx > K else K, T, y2.data_ptr(), _dt(y2),
-                         ldy if ldy > N else N, _stream(stream)), "mx_gemv")
+    _check(lib().mx_gemv(C.addressof(c), C.addressof(p), N, K, x2.data_ptr(), _dt(x2), _pitch(ldx, T, K, "x"), T, y2.data_ptr(), _dt(y2),
+                         _pitch(ldy, T, N, "y"), _stream(stream)), "mx_gemv")
     return y
 
 
@@ -514,7 +524,7 @@ def _heads(t: torch.Tensor, what: str):
     s0, s1, s2 = t.stride()
     if s2 != 1 or (s1 != d and h > 1):
         raise ValueError("%s: expected contiguous heads" % what)
-    return shape, s0 if s0 > h * d else h * d
+    return shape, _pitch(s0, n, h * d, what)
 
 
 def mx_kv_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, positions: torch.Tensor | None = None,
@@ -544,7 +554,7 @@ def mx_kv_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.
             raise ValueError("cos, sin: float32 [n_pos, rot_dim / 2] with one pitch")
         if positions.dtype != torch.int64 or positions.shape != (T,) or not positions.is_contiguous():
             raise ValueError("positions: contiguous int64 [tokens]")
-        rot = _ROTATION.pack(cos.data_ptr(), sin.data_ptr(), positions.data_ptr(), max(pitch[0], half), n_pos, 2 * half, interleaved)
+        rot = _ROTATION.pack(cos.data_ptr(), sin.data_ptr(), positions.data_ptr(), _pitch(pitch[0], n_pos, half, "cos, sin"), n_pos, 2 * half, interleaved)
     n_q = ldq = ldo = 0
     if q is not None:
         if q_out is None:
@@ -589,7 +599,7 @@ def mx_attn_decode(cache: KVCache, q: torch.Tensor, page_table: torch.Tensor, le
     if lse is not None and (lse.dtype != torch.float32 or lse.shape != (B, n_q) or not lse.is_contiguous() or not lse.is_cuda):
         raise ValueError("lse: contiguous float32 [sequences, n_q]")
     _check(lib().mx_attn_decode(cache._ref, q.data_ptr(), ldq, _dt(q), B, n_q, page_table.data_ptr(),
-                                ld_table if ld_table > max_pages else max_pages, max_pages, lengths.data_ptr(),
+                                _pitch(ld_table, B, max_pages, "page_table"), max_pages, lengths.data_ptr(),
                                 d ** -0.5 if scale is None else scale, window, out.data_ptr(), ldo, lse.data_ptr() if lse is not None else None,
                                 workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream)), "mx_attn_decode")
     return out
