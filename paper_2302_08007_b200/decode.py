@@ -57,10 +57,16 @@ def alloc(cfg_w: bdr.Config, w_qkv: torch.Tensor, w_out: torch.Tensor, cache: bd
 
 
 def slots_of(page_table: torch.Tensor, positions: torch.Tensor, page_size: int) -> torch.Tensor:
-    """Cache slot of position `positions[s]` of every sequence s (int64)."""
-    pos = positions.long()
-    pages = page_table.gather(1, torch.div(pos, page_size, rounding_mode="floor")[:, None])[:, 0].long()
-    return pages * page_size + pos % page_size
+    """Cache slot of position `positions[s]` of every sequence s (int64).  A negative position gives a negative slot (padding), one beyond
+    the page table a slot that no cache has, which mx_kv_append reports; neither is looked up."""
+    pos, n = positions.long(), page_table.shape[1]
+    absent = pos * 2 ** 31                                       # caches have fewer slots than 2^31
+    if n == 0:
+        return torch.where(pos < 0, absent, 2 ** 31)
+    page = torch.div(pos, page_size, rounding_mode="floor")
+    known = page.clamp(0, n - 1)
+    slots = page_table.gather(1, known[:, None])[:, 0].long() * page_size + pos % page_size
+    return torch.where(page == known, slots, absent)
 
 
 def step(block: AttentionBlock, h: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, out: torch.Tensor | None = None,
