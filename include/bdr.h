@@ -353,7 +353,7 @@ typedef struct {
 
 /* Rotary positions: cos and sin are [n_pos, ld] fp32 tables (device) with one angle per pair in the first rot_dim / 2
  * columns, positions[t] (int64, device) the row of token t.  Pairs are (i, i + rot_dim / 2) of a head's first rot_dim elements, or
- * (2i, 2i + 1) when interleaved != 0; the elements beyond rot_dim stay as they are. */
+ * (2i, 2i + 1) when interleaved != 0; the elements beyond rot_dim stay as they are.  Tables without a row (n_pos = 0) may be NULL. */
 typedef struct {
     const float *cos, *sin;
     const int64_t* positions;

@@ -251,7 +251,7 @@ __global__ void __launch_bounds__(kApThreads, 2) mx_kv_append_kernel(const Appen
             const int e = INTERLEAVED ? 8 * b + i : 16 * b + i;  // (half layout: element index, its angle is e or e - half)
             const int at = INTERLEAVED ? e : (e < half ? e : e - half);
             uint32_t c4[UA], s4[UA];
-            const bool in = INTERLEAVED ? e < half : e < rot;
+            const bool in = !bad && (INTERLEAVED ? e < half : e < rot);  // a table may have no row at all
             if (in) {
                 load_units<float, UA>(cr + at, c4);
                 load_units<float, UA>(sr + at, s4);
@@ -453,7 +453,7 @@ extern "C" int mx_kv_append(const mx_kv_cache_t* cache, const void* k, int64_t l
     if (q && q == q_out) return BDR_ERR_UNSUPPORTED;
     if (n_tokens == 0) return BDR_OK;
     if (!k || !v || !slots || (q && !q_out)) return BDR_ERR_NULL;
-    if (rotate && (!rot->cos || !rot->sin || !rot->positions)) return BDR_ERR_NULL;
+    if (rotate && (!rot->positions || (rot->n_pos > 0 && (!rot->cos || !rot->sin)))) return BDR_ERR_NULL;
     if ((uintptr_t)slots % 8 || (rotate && (uintptr_t)rot->positions % 8)) return BDR_ERR_MISALIGNED;
     if (((uintptr_t)k | (uintptr_t)v | (uintptr_t)q | (uintptr_t)q_out) % eb) return BDR_ERR_MISALIGNED;
     if (rotate && ((uintptr_t)rot->cos | (uintptr_t)rot->sin) % 4) return BDR_ERR_MISALIGNED;
