@@ -373,7 +373,7 @@ typedef struct {
  *               now stands for (for attention within a prompt, say); written for padding tokens too
  * A slot >= n_pages * page_size, or a position outside [0, n_pos), is seen on the device only: nothing is stored for that
  * token, BDR_ERR_SIZE is left in the sticky word of bdr_device_status, and a bad position also makes the token's rotated
- * outputs NaN. */
+ * outputs NaN.  A padding token's position is not reported (its rotated outputs are NaN all the same). */
 int mx_kv_append(const mx_kv_cache_t* cache /*host*/, const void* k, int64_t ldk, const void* v, int64_t ldv, bdr_dtype_t dt,
                  int64_t n_tokens, const int64_t* slots, const mx_rotation_t* rot /*host*/, const void* q, int64_t ldq, int32_t n_q,
                  void* q_out, int64_t ldq_out, void* k_dq, void* v_dq, void* stream);

@@ -236,7 +236,7 @@ __global__ void __launch_bounds__(kApThreads, 2) mx_kv_append_kernel(const Appen
             bad = true;
             store = false;
             pos = 0;
-            if (lane == 0) atomicCAS(a.status, 0, (int)BDR_ERR_SIZE);
+            if (lane == 0 && slot >= 0) atomicCAS(a.status, 0, (int)BDR_ERR_SIZE);  // nothing was asked for a padding token
         }
     }
     // this block's angles: pair i of the head has angle i; an element beyond rot_dim is not rotated

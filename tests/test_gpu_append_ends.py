@@ -36,3 +36,17 @@ def test_tables_without_a_row_are_not_read(dtype, rot, interleaved):
     assert bdr.bdr_device_status_reset() == -5
     assert untouched(cache) and bool(torch.isnan(q_out).all()) and bool(torch.isnan(k_dq).all())
     assert np.isfinite(H.device_to_host_f32(v_dq)).all()
+
+
+def test_padding_tokens_with_positions_out_of_range_are_not_errors():
+    cache, (q, k, v) = prepared(3, 2, 32, "bf16")
+    ang = torch.rand((4, 16), device="cuda")
+    q_out = torch.empty_like(q)
+    bdr.mx_kv_append(cache, k, v, torch.tensor([-1, 6, -7], device="cuda"), torch.tensor([-1, 3, 4], device="cuda"), ang.cos(), ang.sin(), q=q, q_out=q_out)
+    torch.cuda.synchronize()
+    assert bdr.bdr_device_status_reset() == 0
+    assert torch.isnan(q_out).flatten(1).all(1).tolist() == [True, False, True]
+    assert (cache.k.elems != 0xA5).any(1).nonzero().flatten().tolist() == [6]
+    bdr.mx_kv_append(cache, k, v, torch.tensor([-1, 6, 2], device="cuda"), torch.tensor([-1, 3, 4], device="cuda"), ang.cos(), ang.sin())
+    torch.cuda.synchronize()
+    assert bdr.bdr_device_status_reset() == -5 and bool((cache.k.elems[2] == 0xA5).all())

@@ -59,3 +59,10 @@ def test_a_negative_length_counts_as_an_empty_sequence():
     assert set(sum(changed, [])) == {6 * PAGE + 2, 2 * PAGE}
     bdr.bdr_device_status_reset()
     assert np.isfinite(H.device_to_host_f32(got)).all()
+
+
+def test_a_negative_length_is_not_an_error():
+    table = torch.tensor([[6, 1], [3, 0], [2, 7]], dtype=torch.int32, device="cuda")
+    decode.step(block(), h(), table, torch.tensor([2, -3, 0], dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    assert bdr.bdr_device_status_reset() == 0
