@@ -86,34 +86,34 @@ class Planes:
     micro: torch.Tensor
     elems: torch.Tensor
 
-    def __setattr__(self, name, value):
-        object.__setattr__(self, name, value)
-        if name in ("exps", "micro", "elems"):
-            object.__setattr__(self, "_c", None)
+    _known = _c = None
 
     def lines(self) -> int:
         """Lines that every plane holds."""
-        if self._c is None:
-            self.c()
+        self.c()
         return self._lines
 
     def __reduce__(self):
         return Planes, (self.exps, self.micro, self.elems)
 
     def c(self) -> _Planes:
-        """The C view of the planes, made once (and again when a plane is replaced)."""
-        if self._c is None:
-            self._c = _Planes(self.exps.data_ptr(), self.micro.data_ptr() if self.micro.numel() else None,
-                              self.elems.data_ptr(), self.exps.stride(0), self.micro.stride(0) if self.micro.numel() else 0,
-                              self.elems.stride(0))
-            self._lines = min(t.shape[0] for t in (self.exps, self.micro, self.elems) if t.numel()) if self.exps.numel() else 0
+        """The C view of the planes.  It is kept from call to call and made again when a plane, or the memory or layout of one, is not
+        what it was."""
+        e, m, x = self.exps, self.micro, self.elems
+        known = (e.data_ptr(), m.data_ptr(), x.data_ptr(), e.stride(), m.stride(), x.stride(), e.numel(), m.numel(), x.numel())
+        if known != self._known:
+            self._c = _Planes(e.data_ptr(), m.data_ptr() if m.numel() else None, x.data_ptr(), e.stride(0), m.stride(0) if m.numel() else 0,
+                              x.stride(0))
+            self._lines = min(t.shape[0] for t in (e, m, x) if t.numel()) if e.numel() else 0
+            self._known = known
         return self._c
 
 
 @dataclass
 class KVCache:
     """mx_kv_cache_t: a paged key-value cache in MX format.  `k` and `v` are axis-1 planes of [n_pages * page_size,
-    n_kv * head_dim] tensors; the object keeps them alive and is described to the library once, when it is made."""
+    n_kv * head_dim] tensors; the object keeps them alive.  Planes and sizes may be replaced, by larger ones for example: the next call
+    checks and describes them anew."""
     cfg_k: Config
     cfg_v: Config
     k: Planes
@@ -124,12 +124,27 @@ class KVCache:
     head_dim: int
 
     def __post_init__(self):
-        for p in (self.k, self.v):
-            for t in (p.exps, p.micro, p.elems):
-                if t.dtype != torch.uint8 or t.dim() != 2 or t.stride(1) != 1 or t.shape[0] < self.n_pages * self.page_size:
-                    raise ValueError("cache planes are uint8 [n_pages * page_size, pitch] tensors")
-        self._c = _KVCache(self.cfg_k.c(), self.cfg_v.c(), self.k.c(), self.v.c(), self.n_pages, self.page_size, self.n_kv, self.head_dim)
-        self._ref = C.addressof(self._c)
+        self.ref()
+
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        object.__setattr__(self, "_parts", None)
+
+    def __reduce__(self):
+        return KVCache, (self.cfg_k, self.cfg_v, self.k, self.v, self.n_pages, self.page_size, self.n_kv, self.head_dim)
+
+    def ref(self) -> int:
+        """Address of the cache's C description, which lives as long as the object and is made again when it does not hold any more."""
+        k, v, parts = self.k.c(), self.v.c(), self._parts
+        if parts is None or parts[0] is not k or parts[1] is not v:
+            for p in (self.k, self.v):
+                for t in (p.exps, p.micro, p.elems):
+                    if t.dtype != torch.uint8 or t.dim() != 2 or t.stride(1) != 1 or t.shape[0] < self.n_pages * self.page_size:
+                        raise ValueError("cache planes are uint8 [n_pages * page_size, pitch] tensors")
+            c = _KVCache(self.cfg_k.c(), self.cfg_v.c(), k, v, self.n_pages, self.page_size, self.n_kv, self.head_dim)
+            parts = (k, v, c, C.addressof(c))
+            object.__setattr__(self, "_parts", parts)
+        return parts[3]
 
 
 def alloc_kv_cache(cfg_k: Config, cfg_v: Config, n_pages: int, page_size: int, n_kv: int, head_dim: int, device="cuda") -> KVCache:
@@ -504,10 +519,10 @@ def mx_gemv(cfg_w: Config, w: Planes, N: int, K: int, x: torch.Tensor, y: torch.
     """y[T,N] = x[T,K] @ deq(w)[N,K]^T for a few rows of x (float32 or bfloat16; y likewise) and weights packed along K."""
     x2, y2 = x if x.dim() == 2 else x.unsqueeze(0), y if y.dim() == 2 else y.unsqueeze(0)
     (T, k), (ldx, sx), (ldy, sy) = x2.shape, x2.stride(), y2.stride()
-    if k != K or y2.shape != (T, N) or (sx != 1 and K > 1) or (sy != 1 and N > 1) or w.lines() < N:
+    c, p = cfg_w.c(), w.c()
+    if k != K or y2.shape != (T, N) or (sx != 1 and K > 1) or (sy != 1 and N > 1) or w._lines < N:
         raise ValueError("x is [T, K], y is [T, N], rows contiguous, and the planes hold N lines")
     _on_gpu(x, y, w.elems)
-    c, p = cfg_w.c(), w.c()
     _check(lib().mx_gemv(C.addressof(c), C.addressof(p), N, K, x2.data_ptr(), _dt(x2), _pitch(ldx, T, K, "x"), T, y2.data_ptr(), _dt(y2),
                          _pitch(ldy, T, N, "y"), _stream(stream)), "mx_gemv")
     return y
@@ -568,7 +583,7 @@ def mx_kv_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.
     for t in (k_dq, v_dq):
         if t is not None and (t.shape != shape or t.dtype != dtype or not t.is_contiguous() or not t.is_cuda):
             raise ValueError("k_dq, v_dq: contiguous, like k")
-    _check(lib().mx_kv_append(cache._ref, k.data_ptr(), ldk, v.data_ptr(), ldv, _dt(k), T, slots.data_ptr(), rot,
+    _check(lib().mx_kv_append(cache.ref(), k.data_ptr(), ldk, v.data_ptr(), ldv, _dt(k), T, slots.data_ptr(), rot,
                               q.data_ptr() if n_q else None, ldq, n_q, q_out.data_ptr() if n_q else None, ldo,
                               k_dq.data_ptr() if k_dq is not None else None, v_dq.data_ptr() if v_dq is not None else None,
                               _stream(stream)), "mx_kv_append")
@@ -576,7 +591,7 @@ def mx_kv_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.
 
 
 def mx_attn_decode_workspace_bytes(cache: KVCache, n_seqs: int, n_q: int) -> int:
-    return int(lib().mx_attn_decode_workspace_bytes(cache._ref, n_seqs, n_q))
+    return int(lib().mx_attn_decode_workspace_bytes(cache.ref(), n_seqs, n_q))
 
 
 def mx_attn_decode(cache: KVCache, q: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, out: torch.Tensor,
@@ -598,7 +613,7 @@ def mx_attn_decode(cache: KVCache, q: torch.Tensor, page_table: torch.Tensor, le
         raise ValueError("lengths: contiguous int32 [sequences]")
     if lse is not None and (lse.dtype != torch.float32 or lse.shape != (B, n_q) or not lse.is_contiguous() or not lse.is_cuda):
         raise ValueError("lse: contiguous float32 [sequences, n_q]")
-    _check(lib().mx_attn_decode(cache._ref, q.data_ptr(), ldq, _dt(q), B, n_q, page_table.data_ptr(),
+    _check(lib().mx_attn_decode(cache.ref(), q.data_ptr(), ldq, _dt(q), B, n_q, page_table.data_ptr(),
                                 _pitch(ld_table, B, max_pages, "page_table"), max_pages, lengths.data_ptr(),
                                 d ** -0.5 if scale is None else scale, window, out.data_ptr(), ldo, lse.data_ptr() if lse is not None else None,
                                 workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream)), "mx_attn_decode")
