@@ -72,13 +72,14 @@ def slots_of(page_table: torch.Tensor, positions: torch.Tensor, page_size: int) 
 def step(block: AttentionBlock, h: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, out: torch.Tensor | None = None,
          window: int = 0, stream=None) -> torch.Tensor:
     """One token per sequence: h [n_seqs, d_model] of the tokens at positions lengths[s] (int32: how many tokens the cache holds before
-    this one).  Appends their keys and values and returns the block's output [n_seqs, d_model]; `lengths` is raised by one."""
+    this one).  Appends their keys and values and returns the block's output [n_seqs, d_model]; `lengths` is raised by one.  Everything runs on
+    `stream` (the current one when None): the inputs have to be ready there, and an output that the step allocates belongs to it."""
     c, n_q = block.cache, block.n_q
     n_seqs, d_model = h.shape
     heads = n_q + 2 * c.n_kv
-    if out is None:
-        out = torch.empty_like(h)
     with torch.cuda.stream(stream) if stream is not None else torch.cuda.stream(torch.cuda.current_stream()):
+        if out is None:
+            out = torch.empty_like(h)
         bdr.mx_gemv(block.cfg_w, block.w_qkv, heads * c.head_dim, d_model, h, block.qkv.view(n_seqs, -1))
         q, k, v = block.qkv.split((n_q, c.n_kv, c.n_kv), 1)
         positions = lengths.long()
