@@ -70,9 +70,10 @@ def slots_of(page_table: torch.Tensor, positions: torch.Tensor, page_size: int) 
 
 
 def step(block: AttentionBlock, h: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, out: torch.Tensor | None = None,
-         window: int = 0, stream=None) -> torch.Tensor:
+         window: int = 0, stream=None, advance: bool = True) -> torch.Tensor:
     """One token per sequence: h [n_seqs, d_model] of the tokens at positions lengths[s] (int32: how many tokens the cache holds before
-    this one).  Appends their keys and values and returns the block's output [n_seqs, d_model]; `lengths` is raised by one.  Everything runs on
+    this one).  Appends their keys and values and returns the block's output [n_seqs, d_model]; `lengths` is raised by one if
+    `advance` (the blocks of a model share one tensor of lengths, which only the last of them advances).  Everything runs on
     `stream` (the current one when None): the inputs have to be ready there, and an output that the step allocates belongs to it."""
     c, n_q = block.cache, block.n_q
     n_seqs, d_model = h.shape
@@ -84,7 +85,7 @@ def step(block: AttentionBlock, h: torch.Tensor, page_table: torch.Tensor, lengt
         q, k, v = block.qkv.split((n_q, c.n_kv, c.n_kv), 1)
         positions = lengths.long()
         bdr.mx_kv_append(c, k, v, slots_of(page_table, positions, c.page_size), positions, block.cos, block.sin, q=q, q_out=block.q)
-        lengths += 1
-        bdr.mx_attn_decode(c, block.q, page_table, lengths, block.attended, block.workspace, window=window)
+        held = lengths.add_(1) if advance else lengths + 1
+        bdr.mx_attn_decode(c, block.q, page_table, held, block.attended, block.workspace, window=window)
         bdr.mx_gemv(block.cfg_w, block.w_out, d_model, n_q * c.head_dim, block.attended.view(n_seqs, -1), out)
     return out

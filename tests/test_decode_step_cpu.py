@@ -48,3 +48,17 @@ def test_the_result_is_allocated_on_the_stream_that_writes_it(world, stream):
     assert {s for _, s, _ in seen} == {stream or "current"} and [n for n, _, _ in seen].count("empty_like") == 1
     assert [n for n, _, _ in seen if n != "empty_like"] == ["mx_gemv", "mx_kv_append", "mx_attn_decode", "mx_gemv"]
     assert seen[-1][2][-1] is out
+
+
+def appended_and_attended(seen):
+    by = {n: a for n, _, a in seen}
+    return by["mx_kv_append"][3].tolist(), by["mx_kv_append"][4].tolist(), by["mx_attn_decode"][3].tolist()
+
+
+def test_blocks_of_one_model_share_the_lengths(world):
+    block, table, lengths, h, seen = world
+    for advance, after in ((False, [3, 5]), (False, [3, 5]), (True, [4, 6])):
+        seen.clear()
+        decode.step(block, h, table, lengths, advance=advance)
+        assert appended_and_attended(seen) == ([3, 5 * PAGE + 1], [3, 5], [4, 6])
+        assert lengths.tolist() == after and lengths.dtype == torch.int32

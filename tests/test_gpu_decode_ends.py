@@ -66,3 +66,15 @@ def test_a_negative_length_is_not_an_error():
     decode.step(block(), h(), table, torch.tensor([2, -3, 0], dtype=torch.int32, device="cuda"))
     torch.cuda.synchronize()
     assert bdr.bdr_device_status_reset() == 0
+
+
+def test_two_blocks_with_one_tensor_of_lengths():
+    table = torch.tensor([[6, 1], [3, 0], [2, 7]], dtype=torch.int32, device="cuda")
+    start = torch.tensor([2, 5, 0], dtype=torch.int32, device="cuda")
+    pair = lambda: (block(), block())  # noqa: E731
+    x, (a, b), la, lb = h(), pair(), start.clone(), start.clone()
+    want = [decode.step(b, decode.step(a, x, table, la), table, lb).clone() for _ in range(2)]
+    (a, b), lengths = pair(), start.clone()
+    got = [decode.step(b, decode.step(a, x, table, lengths, advance=False), table, lengths).clone() for _ in range(2)]
+    assert all(torch.equal(g, w) for g, w in zip(got, want)) and lengths.tolist() == [4, 7, 2]
+    assert bdr.bdr_device_status() == 0
