@@ -75,6 +75,8 @@ def step(block: AttentionBlock, h: torch.Tensor, page_table: torch.Tensor, lengt
     this one).  Appends their keys and values and returns the block's output [n_seqs, d_model]; `lengths` is raised by one if
     `advance` (the blocks of a model share one tensor of lengths, which only the last of them advances).  Everything runs on
     `stream` (the current one when None): the inputs have to be ready there, and an output that the step allocates belongs to it."""
+    if lengths.dtype != torch.int32:
+        raise ValueError("lengths: int32 [sequences]")
     c, n_q = block.cache, block.n_q
     n_seqs, d_model = h.shape
     heads = n_q + 2 * c.n_kv

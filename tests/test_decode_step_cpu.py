@@ -62,3 +62,11 @@ def test_blocks_of_one_model_share_the_lengths(world):
         decode.step(block, h, table, lengths, advance=advance)
         assert appended_and_attended(seen) == ([3, 5 * PAGE + 1], [3, 5], [4, 6])
         assert lengths.tolist() == after and lengths.dtype == torch.int32
+
+
+def test_lengths_of_another_type_are_refused_before_anything_is_done(world):
+    block, table, lengths, h, seen = world
+    wide = lengths.long()
+    with pytest.raises(ValueError):
+        decode.step(block, h, table, wide)
+    assert not seen and wide.tolist() == [3, 5]
