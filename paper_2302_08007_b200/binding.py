@@ -613,6 +613,10 @@ def mx_attn_decode(cache: KVCache, q: torch.Tensor, page_table: torch.Tensor, le
         raise ValueError("lengths: contiguous int32 [sequences]")
     if lse is not None and (lse.dtype != torch.float32 or lse.shape != (B, n_q) or not lse.is_contiguous() or not lse.is_cuda):
         raise ValueError("lse: contiguous float32 [sequences, n_q]")
+    if not -2 ** 31 <= window < 2 ** 31:                         # as a 32-bit number it would be another one
+        if window < 0:
+            raise ValueError("window: not negative")
+        window = 2 ** 31 - 1                                     # more positions than a cache can have
     _check(lib().mx_attn_decode(cache.ref(), q.data_ptr(), ldq, _dt(q), B, n_q, page_table.data_ptr(),
                                 _pitch(ld_table, B, max_pages, "page_table"), max_pages, lengths.data_ptr(),
                                 d ** -0.5 if scale is None else scale, window, out.data_ptr(), ldo, lse.data_ptr() if lse is not None else None,

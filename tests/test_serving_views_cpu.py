@@ -99,3 +99,13 @@ def test_sequences_of_an_attention(calls):
     go(q=overlapping((1, 4, 32), 0), out=overlapping((1, 4, 32), 0), table=overlapping((1, 5), 0, torch.int32))
     a = [x for _, x in calls]
     assert [(x[2], x[7], x[8], x[13]) for x in a] == [(128, 5, 5, 128), (128, 9, 5, 128), (128, 5, 5, 128)]
+
+
+def test_a_window_wider_than_any_cache_is_no_narrower_one(calls):
+    q, table, lengths, ws = t(3, 4, 32), t(3, 5, dtype=torch.int32), t(3, dtype=torch.int32), t(1 << 16, dtype=torch.uint8)
+    for window, want in ((0, 0), (7, 7), (2 ** 31 - 1, 2 ** 31 - 1), (2 ** 31, 2 ** 31 - 1), (2 ** 32 + 5, 2 ** 31 - 1), (2 ** 63 - 1, 2 ** 31 - 1), (-1, -1)):
+        calls.clear()
+        bdr.mx_attn_decode(cache(), q, table, lengths, torch.empty_like(q), ws, window=window)
+        assert calls[0][1][11] == want
+    with pytest.raises(ValueError):
+        bdr.mx_attn_decode(cache(), q, table, lengths, torch.empty_like(q), ws, window=-2 ** 32 + 3)
