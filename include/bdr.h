@@ -380,7 +380,7 @@ int mx_kv_append(const mx_kv_cache_t* cache /*host*/, const void* k, int64_t ldk
 
 /* Attention of one new token per sequence over its cached keys and values:
  *     out[s, h] = sum_t p_t V[t, h / (n_q / n_kv)],  p = softmax_t(scale * <q[s, h], K[t, h / (n_q / n_kv)]>)
- * over the positions t < lengths[s] (int32, device; the new token's own key counts once it has been appended), or only the last
+ * (|scale| < 2^94) over the positions t < lengths[s] (int32, device; the new token's own key counts once it has been appended), or only the last
  * `window` of them when window > 0.  Position t of sequence s lives in page page_table[s, t / page_size] (int32, device, row pitch
  * ld_table >= max_pages).  Positions outside the range are never read, whatever the pages hold there.
  *   q, out   [n_seqs, n_q, head_dim] of `dt` with sequence pitches ldq and ldo; n_q a multiple of n_kv

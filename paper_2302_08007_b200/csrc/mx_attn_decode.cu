@@ -182,7 +182,8 @@ int mx_attn_decode(const mx_kv_cache_t* cache, const void* q, int64_t ldq, bdr_d
     if (((uintptr_t)q | (uintptr_t)out) % eb || ((uintptr_t)page_table | (uintptr_t)lengths | (uintptr_t)lse) % 4) return BDR_ERR_MISALIGNED;
     if (!workspace || workspace_bytes < mx_attn_decode_workspace_bytes(cache, n_seqs, n_q)) return BDR_ERR_WORKSPACE;
     if ((uintptr_t)workspace % 16) return BDR_ERR_MISALIGNED;
-    if (!(std::fabs(scale) < INFINITY)) return BDR_ERR_BAD_CONFIG;
+    // in base 2, and with the factor that the first way of decoding leaves out, it has to be finite as well
+    if (!(std::fabs(scale) < 0x1p94f)) return BDR_ERR_BAD_CONFIG;
     const bool f32 = dt == BDR_F32;
     const AttnPlan p = plan_attn(*cache, n_q, f32);
     if (p.groups > 65535) return BDR_ERR_SIZE;
