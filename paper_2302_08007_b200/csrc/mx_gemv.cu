@@ -37,18 +37,26 @@ constexpr int kGvStep = 256;                 // elements of K per warp step
 constexpr int kGvSmem = 227 * 1024;
 constexpr int kGvMaxCols = 64;               // columns (tokens, or thirds of a 32-bit token) of one pass
 
-// Warps of a CTA and steps in a warp's ring: 16 warps of up to 128 registers when there are few columns, 8 (and shared memory left
-// for the activations) when there are more.  Two groups of columns run with 16 warps for 3-bit codes, whose rings are small (16 tokens of
-// 4096 x 4096: 9.7 us, with eight warps 10.9; 10 of 16384 x 4096: 20.2, 23.1); with 5-bit codes the activations of K = 4096 would no
-// longer fit beside the rings (16 of 4096 x 4096: 13.5 us, with eight 11.5).
-template <int W, int NT> struct GemvShape {
-    static constexpr int kWarps = NT == 1 || (NT == 2 && W == 3) ? 16 : 8, kThreads = 32 * kWarps;
+// Warps of a CTA: 16 of up to 128 registers when there are few columns, 8 (and shared memory left for the activations) when there are
+// more.  Two groups of columns run with 16 warps for 3-bit codes, whose rings are small; with 5-bit codes the activations of K = 4096 would
+// no longer fit beside the rings (16 of 4096 x 4096: 13.5 us, with eight 11.5).  For 3-bit codes the choice is made per call.  Where the
+// activations fit beside either's rings, or beside neither's, 16 warps are 3 to 17 % faster (16 tokens of 4096 x 4096: 9.7 us, with eight
+// 10.9).  Where they fit beside those of eight only, eight win as long as an SM has at most two row tiles, whose phases nothing hides (16
+// tokens of 2048 x 4352: 9.5 us, with sixteen 10.4; of 4096 x 5120 13.3, 13.8; 9 of 1024 x 8960 12.7, 15.1); from three tiles on sixteen are
+// ahead (16 tokens of 5120 x 5120: 16.3 us, with eight 17.0; of 16384 x 5120 28.3, 30.0; 9 of 16384 x 8960 42.5, 45.7; of 8192 x 4352 they
+// lose by 4 %).
+__host__ __device__ constexpr int gemv_warps(int w, int nt) { return nt == 1 || (nt == 2 && w == 3) ? 16 : 8; }
+
+template <int W, int NT, int WARPS> struct GemvShape {
+    static constexpr int kWarps = WARPS, kThreads = 32 * kWarps;
     static constexpr int kRed = kWarps * 8 * NT * 16 * 4;  // bytes of all warps' sums of a tile
     static constexpr int kPitch = 32 * W;                  // bytes of codes of a row and step
     static constexpr int kAtX = 16 * kPitch, kStage = kAtX + 2 * 256;  // 16 rows of codes, of exponents, of microexponents
-    static constexpr int kStages = W != 8 && (NT == 1 || (NT == 2 && W == 5)) ? 3 : 2;
+    static constexpr int kStages = W != 8 && (NT == 1 || (NT == 2 && W == 5)) ? 3 : 2;  // steps in a warp's ring
     static constexpr int kReds = NT < 4 ? 2 : 1;                       // buffers of sums
     static constexpr int kXs = kReds * kRed + kWarps * kStages * kStage;  // where the activations start
+    // steps whose activations fit beside the rings, for a number of columns
+    static int fit(int cols) { return ((kGvSmem - kXs) / cols - 64) / (2 * kGvStep); }
 };
 
 struct GemvArgs {
@@ -302,9 +310,9 @@ __device__ __forceinline__ void run_step(const Run<W>& r0, const Run<W>& r1, con
     else run_step_as<W, NT, false>(r0, r1, xs, pitch, cols, lane, acc);
 }
 
-template <int W, int NT, bool X32>
-__global__ void __launch_bounds__((GemvShape<W, NT>::kThreads), 1) mx_gemv_kernel(const GemvArgs a) {
-    using S = GemvShape<W, NT>;
+template <int W, int NT, bool X32, int WARPS>
+__global__ void __launch_bounds__((GemvShape<W, NT, WARPS>::kThreads), 1) mx_gemv_kernel(const GemvArgs a) {
+    using S = GemvShape<W, NT, WARPS>;
     constexpr int kWarps = S::kWarps, D = S::kStages;
     extern __shared__ __align__(16) uint8_t smem[];
     float* const red = reinterpret_cast<float*>(smem);
@@ -441,11 +449,11 @@ __global__ void __launch_bounds__((GemvShape<W, NT>::kThreads), 1) mx_gemv_kerne
     cp_async_wait<0>();
 }
 
-template <int W, int NT, bool X32>
+template <int W, int NT, bool X32, int WARPS = gemv_warps(W, NT)>
 static int launch_gemv(GemvArgs a, cudaStream_t st) {
-    using S = GemvShape<W, NT>;
+    using S = GemvShape<W, NT, WARPS>;
     static PerDevice once;
-    if (kernel_setup(once, mx_gemv_kernel<W, NT, X32>, S::kThreads, kGvSmem) < 1) return BDR_ERR_CUDA;
+    if (kernel_setup(once, mx_gemv_kernel<W, NT, X32, WARPS>, S::kThreads, kGvSmem) < 1) return BDR_ERR_CUDA;
     const int cols = (X32 ? 3 : 1) * std::min(a.tokens, a.tokens_per_pass);
     const int steps = (int)((a.k + kGvStep - 1) / kGvStep), sms = sm_count();
     const int64_t tiles = (a.n + 15) / 16;
@@ -453,7 +461,7 @@ static int launch_gemv(GemvArgs a, cudaStream_t st) {
     // barrier; putting a column's step in order, again for every round, takes about 1/500
     double best = 0;
     // steps whose activations fit, and of which two sets fit: one at least
-    const int room = (kGvSmem - S::kXs) / cols, fit = (room - 64) / (2 * kGvStep), half = (room / 2 - 64) / (2 * kGvStep);
+    const int room = (kGvSmem - S::kXs) / cols, fit = S::fit(cols), half = (room / 2 - 64) / (2 * kGvStep);
     for (int kw = 1; kw <= S::kWarps && kw <= std::max(1, steps) && (steps <= fit || kw <= half); kw *= 2) {
         const int64_t rounds = ((tiles + sms - 1) / sms + S::kWarps / kw - 1) / (S::kWarps / kw);
         const double walk = (double)rounds * ((steps + kw - 1) / kw + 0.33 + (steps > fit ? 0.3 * steps / (half / kw * kw) + cols * steps / 500.0 : 0));
@@ -470,7 +478,7 @@ static int launch_gemv(GemvArgs a, cudaStream_t st) {
     a.rounds = (int)(tiles / stride);
     a.rest = (unsigned)std::min<int64_t>(tiles % stride, ctas);
     const dim3 grid((unsigned)ctas, (unsigned)((a.tokens + a.tokens_per_pass - 1) / a.tokens_per_pass));
-    mx_gemv_kernel<W, NT, X32><<<grid, S::kThreads, smem, st>>>(a);
+    mx_gemv_kernel<W, NT, X32, WARPS><<<grid, S::kThreads, smem, st>>>(a);
     return cudaGetLastError() == cudaSuccess ? BDR_OK : BDR_ERR_CUDA;
 }
 
@@ -479,7 +487,14 @@ static int pick_columns(GemvArgs a, cudaStream_t st) {
     a.tokens_per_pass = X32 ? kGvMaxCols / 3 : kGvMaxCols;
     const int cols = (X32 ? 3 : 1) * std::min(a.tokens, a.tokens_per_pass);
     if (cols <= 8) return launch_gemv<W, 1, X32>(a, st);
-    if (cols <= 16) return launch_gemv<W, 2, X32>(a, st);
+    if (cols <= 16) {
+        if constexpr (W == 3) {  // see gemv_warps
+            const int64_t steps = (a.k + kGvStep - 1) / kGvStep;
+            if (steps > GemvShape<3, 2, 16>::fit(cols) && steps <= GemvShape<3, 2, 8>::fit(cols) && (a.n + 15) / 16 <= 2 * sm_count())
+                return launch_gemv<W, 2, X32, 8>(a, st);
+        }
+        return launch_gemv<W, 2, X32>(a, st);
+    }
     if (cols <= 32) return launch_gemv<W, 4, X32>(a, st);
     return launch_gemv<W, 8, X32>(a, st);
 }
