@@ -323,11 +323,12 @@ int mx_gemm_hw(const bdr_config_t* cfg_a /*host*/, const bdr_planes_t* a /*host 
                int64_t K, int r, int f, float* c, int64_t ldc, void* stream);
 
 /* ---- Serving ------------------------------------------------------------------------------------------------
- * Token-by-token inference on MX storage (Section V, inferencing): products of a few activations with packed
- * weights, a key-value cache kept in the MX format, and the attention of one new token over it.  These calls take
- * the Table II formats with ties to even (k1 = 16, k2 = 2, d2 = 1, m in {2, 4, 7}); anything else is
- * BDR_ERR_UNSUPPORTED.  Blocks with the exponent byte 0xFF (Inf/NaN) decode to NaN; blocks with the exponent byte 0
- * (zeros and values below 2^-126) decode to zero. */
+ * Token-by-token inference on MX storage: products of a few activations with packed weights (Section V, inferencing; the
+ * activations are not quantized here, which the section does), a key-value cache kept in the MX format, and the attention
+ * of one new token over it.  These calls take the Table II formats with ties to even (k1 = 16, k2 = 2, d2 = 1, m in
+ * {2, 4, 7}; mx_gemv, which only decodes, takes either tie rule); anything else is BDR_ERR_UNSUPPORTED.  Blocks with the
+ * exponent byte 0xFF (Inf/NaN) decode to NaN; blocks with the exponent byte 0 (zeros and values below 2^-126) decode to
+ * zero. */
 
 /* y[T,N] (row pitch ldy) = x[T,K] (row pitch ldx) deq(W)[N,K]^T for a few rows of x and weights packed along K (axis-1
  * planes of W).  The activations are used as they are: bf16 values enter the tensor core unchanged, fp32 values as the

@@ -1,5 +1,6 @@
-// Few-token product with packed weights: y[T, N] = x[T, K] deq(W)[N, K]^T, the linear layers of token-by-token inference
-// (Section V, inferencing: weights are stored in the MX format; the activations stay as they are).
+// Few-token product with packed weights: y[T, N] = x[T, K] deq(W)[N, K]^T, the linear layers of token-by-token inference.  The weights
+// are kept in the MX format (Section V, inferencing).  That the activations stay as they are is this library's choice: the section
+// quantizes them on the way to the product, which pays where the product itself is computed on the format.
 //
 // Every packed weight is read once and used for T columns, so the kernel is bound by the bytes of W as long as decoding keeps
 // up.  A warp owns 16 rows of W and walks along K in steps of 256 elements: lane (g, c) of the matrix instruction's layout

@@ -1,6 +1,6 @@
-"""The attention half of a decoder block, one new token per sequence, on MX storage (Section V, inferencing: weights and the
-key-value cache are kept in the MX format, activations stay in bf16 or fp32).  Like ``linear``, this module only sequences calls
-of the C ABI; all arithmetic is in the kernels.
+"""The attention half of a decoder block, one new token per sequence, on MX storage: the weights (Section V, inferencing) and the
+key-value cache are kept in the MX format; the activations stay in bf16 or fp32, which is this library's choice (the section
+quantizes them too).  Like ``linear``, this module only sequences calls of the C ABI; all arithmetic is in the kernels.
 
     qkv  = h Wqkv^T                      mx_gemv
     k, q rotated by position; k, v       mx_kv_append: quantized and written to the sequences' next slots
