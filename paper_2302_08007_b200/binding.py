@@ -86,11 +86,27 @@ class Planes:
     micro: torch.Tensor
     elems: torch.Tensor
 
-    _known = _c = None
+    _probe = None
+
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        object.__setattr__(self, "_probe", None)
+
+    def _describe(self) -> None:
+        """Makes the C view, and the calls that tell whether it still holds (a tensor's memory and layout can be exchanged in place)."""
+        e, m, x = self.exps, self.micro, self.elems
+        probe = (e.data_ptr, m.data_ptr, x.data_ptr, e.stride, m.stride, x.stride)
+        view = _Planes(e.data_ptr(), m.data_ptr() if m.numel() else None, x.data_ptr(), e.stride(0), m.stride(0) if m.numel() else 0, x.stride(0))
+        sizes = (e.numel, m.numel, x.numel)
+        lines = min(t.shape[0] for t in (e, m, x) if t.numel()) if e.numel() else 0
+        self.__dict__.update(_view=view, _known=tuple(f() for f in probe), _probe=probe, _sizes=sizes, _counts=tuple(f() for f in sizes), _lines=lines)
 
     def lines(self) -> int:
         """Lines that every plane holds."""
         self.c()
+        n = self._sizes
+        if (n[0](), n[1](), n[2]()) != self._counts:            # cut or extended within its memory
+            self._describe()
         return self._lines
 
     def __reduce__(self):
@@ -99,14 +115,10 @@ class Planes:
     def c(self) -> _Planes:
         """The C view of the planes.  It is kept from call to call and made again when a plane, or the memory or layout of one, is not
         what it was."""
-        e, m, x = self.exps, self.micro, self.elems
-        known = (e.data_ptr(), m.data_ptr(), x.data_ptr(), e.stride(), m.stride(), x.stride(), e.numel(), m.numel(), x.numel())
-        if known != self._known:
-            self._c = _Planes(e.data_ptr(), m.data_ptr() if m.numel() else None, x.data_ptr(), e.stride(0), m.stride(0) if m.numel() else 0,
-                              x.stride(0))
-            self._lines = min(t.shape[0] for t in (e, m, x) if t.numel()) if e.numel() else 0
-            self._known = known
-        return self._c
+        p = self._probe
+        if p is None or (p[0](), p[1](), p[2](), p[3](), p[4](), p[5]()) != self._known:
+            self._describe()
+        return self._view
 
 
 @dataclass
@@ -133,18 +145,24 @@ class KVCache:
     def __reduce__(self):
         return KVCache, (self.cfg_k, self.cfg_v, self.k, self.v, self.n_pages, self.page_size, self.n_kv, self.head_dim)
 
+    def _describe(self) -> int:
+        for p in (self.k, self.v):
+            for t in (p.exps, p.micro, p.elems):
+                if t.dtype != torch.uint8 or t.dim() != 2 or t.stride(1) != 1 or t.shape[0] < self.n_pages * self.page_size:
+                    raise ValueError("cache planes are uint8 [n_pages * page_size, pitch] tensors")
+        k, v = self.k, self.v
+        c = _KVCache(self.cfg_k.c(), self.cfg_v.c(), k.c(), v.c(), self.n_pages, self.page_size, self.n_kv, self.head_dim)
+        object.__setattr__(self, "_parts", (k, v, k._probe, v._probe, k._known + v._known, C.addressof(c), c))
+        return C.addressof(c)
+
     def ref(self) -> int:
         """Address of the cache's C description, which lives as long as the object and is made again when it does not hold any more."""
-        k, v, parts = self.k.c(), self.v.c(), self._parts
-        if parts is None or parts[0] is not k or parts[1] is not v:
-            for p in (self.k, self.v):
-                for t in (p.exps, p.micro, p.elems):
-                    if t.dtype != torch.uint8 or t.dim() != 2 or t.stride(1) != 1 or t.shape[0] < self.n_pages * self.page_size:
-                        raise ValueError("cache planes are uint8 [n_pages * page_size, pitch] tensors")
-            c = _KVCache(self.cfg_k.c(), self.cfg_v.c(), k, v, self.n_pages, self.page_size, self.n_kv, self.head_dim)
-            parts = (k, v, c, C.addressof(c))
-            object.__setattr__(self, "_parts", parts)
-        return parts[3]
+        parts = self._parts
+        if parts is not None:
+            k, v, p, q, known, address, _ = parts
+            if k._probe is p and v._probe is q and (p[0](), p[1](), p[2](), p[3](), p[4](), p[5](), q[0](), q[1](), q[2](), q[3](), q[4](), q[5]()) == known:
+                return address
+        return self._describe()
 
 
 def alloc_kv_cache(cfg_k: Config, cfg_v: Config, n_pages: int, page_size: int, n_kv: int, head_dim: int, device="cuda") -> KVCache:
@@ -519,8 +537,8 @@ def mx_gemv(cfg_w: Config, w: Planes, N: int, K: int, x: torch.Tensor, y: torch.
     """y[T,N] = x[T,K] @ deq(w)[N,K]^T for a few rows of x (float32 or bfloat16; y likewise) and weights packed along K."""
     x2, y2 = x if x.dim() == 2 else x.unsqueeze(0), y if y.dim() == 2 else y.unsqueeze(0)
     (T, k), (ldx, sx), (ldy, sy) = x2.shape, x2.stride(), y2.stride()
-    c, p = cfg_w.c(), w.c()
-    if k != K or y2.shape != (T, N) or (sx != 1 and K > 1) or (sy != 1 and N > 1) or w._lines < N:
+    lines, c, p = w.lines(), cfg_w.c(), w._view
+    if k != K or y2.shape != (T, N) or (sx != 1 and K > 1) or (sy != 1 and N > 1) or lines < N:
         raise ValueError("x is [T, K], y is [T, N], rows contiguous, and the planes hold N lines")
     _on_gpu(x, y, w.elems)
     _check(lib().mx_gemv(C.addressof(c), C.addressof(p), N, K, x2.data_ptr(), _dt(x2), _pitch(ldx, T, K, "x"), T, y2.data_ptr(), _dt(y2),
@@ -539,7 +557,7 @@ def _heads(t: torch.Tensor, what: str):
     s0, s1, s2 = t.stride()
     if s2 != 1 or (s1 != d and h > 1):
         raise ValueError("%s: expected contiguous heads" % what)
-    return shape, _pitch(s0, n, h * d, what)
+    return shape, s0 if s0 >= h * d else _pitch(s0, n, h * d, what)
 
 
 def mx_kv_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, positions: torch.Tensor | None = None,
