@@ -20,11 +20,12 @@
 // that covers a sequence's whole range writes the result; other parts leave their sums and references in the workspace, where
 // a second kernel joins them in order.
 //
-// Measured (32 query heads on 8 key-value heads of 128 elements, bf16, both kernels): 64 sequences of 2048 to 8192 tokens, MX6,
-// 184 us = 2.75 TB/s of cache; 16 sequences of 500 to 4096, MX9, 31.6 us = 2.69 TB/s; one of 777, MX9, 11.4 us; 64 query heads, one
-// sequence of 131072, MX4, 76 us = 1.77 TB/s.  A tile of 16 x 128 keys and values takes 770 instructions in MX6, 710 in MX4 and
-// 650 in MX9, 60 % of them the decoding; the integer/logic pipe is busy 64 to 71 % of the time and the issue slots 66 to 70 %
-// (MX9: 48 %, waiting for copies as well).  Short calls are two launches and a chain of dependent reads: lengths, page, bytes.
+// Measured (32 query heads on 8 key-value heads of 128 elements, bf16, both kernels, the cache not in the L2): 64 sequences of 2048 to
+// 8192 tokens, MX6, 190 us = 2.65 TB/s of cache; 16 sequences of 500 to 4096, MX9, 34.3 us = 2.5 TB/s; one of 777, MX9, 12 us; 64 query
+// heads, one sequence of 131072, MX4, 78 us = 1.7 TB/s.  With 32-bit queries 64 sequences of 2048 to 8096, MX6, take 247 us.  A tile of
+// 16 x 128 keys and values takes 790 instructions in MX6, 730 in MX4 and 670 in MX9, 60 % of them the decoding; the integer/logic pipe
+// is busy 62 to 65 % of the time and the issue slots 68 to 70 % (MX9: 49 %, waiting for copies as well).  Short calls are two
+// launches and a chain of dependent reads: lengths, page, bytes.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -137,7 +138,9 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
 // unit has all MAXB blocks, so a lane's key blocks are whole aligned words.
 template <int MAXB, int NT, bool F32>
 struct AttnShape {
-    static constexpr int kWarps = MAXB == 8 && NT == 1 ? 16 : 8;  // as many as the registers allow
+    // As many as the registers allow: at 128 a thread (16 warps) most kernels spill a little, 8 to 52 bytes with bf16 queries and 20 to 92
+    // with 32-bit ones.
+    static constexpr int kWarps = MAXB == 8 && NT == 1 ? 16 : 8;
     static constexpr int kThreads = 32 * kWarps;
     static constexpr int kKeyBlocks = MAXB / 4, kValBlocks = MAXB / 8;  // per lane and token
     static constexpr int kParts = F32 ? 3 : 1;

@@ -7,8 +7,8 @@
 // takes four blocks of rows g and g + 8 (24, 40 or 64 bytes of codes each), decodes them in registers and feeds 16 matrix
 // instructions.  The bytes come through a ring of the warp's own in shared memory, filled by 16-byte asynchronous copies one or
 // two steps ahead: a lane's own bytes are strided in memory, and loads of them straight into registers kept the L1 busy with
-// four times as many lines per request and the compiler moving them down to where they were needed (16384 x 4096 MX9: 18.5 us,
-// with the ring 15.8).  The activations sit in shared memory in the order those instructions want them, as bf16; a 32-bit
+// four times as many lines per request and the compiler moving them down to where they were needed (16384 x 4096 MX9, the same
+// weights again and again: 18.5 us, with the ring 15.8).  The activations sit in shared memory in the order those instructions want them, as bf16; a 32-bit
 // activation is split exactly into three bf16 columns, which costs nothing while the eight columns of an instruction are not full.
 // One CTA per SM stays for the whole call and its warps form groups of kw that share a tile's K; a group's sums are added in
 // shared memory in a fixed order.  The host picks kw so that the longest group's walk is shortest: few large groups balance few
@@ -16,10 +16,11 @@
 // one before is computed (loaded, ordered and stored between two phases instead, they took as long as the products: 16 tokens of
 // 16384 x 8192 MX9 67.8 us, now 45).
 //
-// Measured (bf16 activations, the weights not in the L2): one token, 16384 x 4096 MX9 16 us = 4.7 TB/s, 16384 x 16384 MX9 57 us =
-// 5.3 TB/s, 16384 x 4096 MX6 18 us = 2.8 TB/s, 4096 x 4096 MX4 6.5 us; 16 tokens, 16384 x 8192 MX9 45.0 us = 3.4 TB/s, MX6
-// 49.6 us.  MX9 is near the memory's rate for one token; MX6 and MX4 are bound by decoding (the integer/logic pipe); sixteen
-// tokens by decoding on half the warps, which is what the registers of two column groups allow.  Small products are
+// Measured (bf16 activations, the weights not in the L2): one token, 16384 x 4096 MX9 17.9 us = 4.2 TB/s, 16384 x 16384 MX9 57 us =
+// 5.3 TB/s, MX6 68 us = 3.0 TB/s, MX4 58 us = 2.3 TB/s, 16384 x 4096 MX6 20 us = 2.5 TB/s, 4096 x 4096 MX4 7.4 us; 16 tokens,
+// 16384 x 8192 MX9 45.6 us = 3.3 TB/s, MX6 50.5 us; 32 and 64 tokens, 16384 x 4096 MX9 34.5 and 63.6 us (16: 26.0).  MX9 is near the
+// memory's rate for one token; MX6 and MX4 are bound by decoding (the integer/logic pipe, and latency: no pipe is more than two thirds
+// busy); sixteen tokens by decoding on half the warps, which is what the registers of two column groups allow.  Small products are
 // a launch and one trip to memory.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -41,8 +42,8 @@ constexpr int kGvMaxCols = 64;               // columns (tokens, or thirds of a 
 // Warps of a CTA: 16 of up to 128 registers when there are few columns, 8 (and shared memory left for the activations) when there are
 // more.  Two groups of columns run with 16 warps for 3-bit codes, whose rings are small; with 5-bit codes the activations of K = 4096 would
 // no longer fit beside the rings (16 of 4096 x 4096: 13.5 us, with eight 11.5).  For 3-bit codes the choice is made per call.  Where the
-// activations fit beside either's rings, or beside neither's, 16 warps are 3 to 17 % faster (16 tokens of 4096 x 4096: 9.7 us, with eight
-// 10.9).  Where they fit beside those of eight only, eight win as long as an SM has at most two row tiles, whose phases nothing hides (16
+// activations fit beside either's rings, or beside neither's, 16 warps are 3 to 17 % faster (16 tokens of 4096 x 4096: 10.0 us, with eight
+// 11.3).  Where they fit beside those of eight only, eight win as long as an SM has at most two row tiles, whose phases nothing hides (16
 // tokens of 2048 x 4352: 9.5 us, with sixteen 10.4; of 4096 x 5120 13.3, 13.8; 9 of 1024 x 8960 12.7, 15.1); from three tiles on sixteen are
 // ahead (16 tokens of 5120 x 5120: 16.3 us, with eight 17.0; of 16384 x 5120 28.3, 30.0; 9 of 16384 x 8960 42.5, 45.7; of 8192 x 4352 they
 // lose by 4 %).

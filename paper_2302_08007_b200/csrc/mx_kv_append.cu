@@ -11,7 +11,7 @@
 // them.  Results leave in 32-byte stores.
 //
 // Measured (32 query and 2 x 8 key-value heads of 128 elements, bf16, MX9, rotated queries and quantized values written too): 16384
-// tokens 85.8 us = 5.2 TB/s, one token 3.6 us; 1003 tokens of 20 + 2 x 4 heads of 80, fp32, MX6 and MX4, 6.2 us.  Long calls are
+// tokens 86.6 us = 5.2 TB/s, one token 3.9 us; 1003 tokens of 20 + 2 x 4 heads of 80, fp32, MX6 and MX4, 7.9 us (6.2 from the L2).  Long calls are
 // bound by instructions as much as by memory (3570 per warp and token, issue slots about 60 % busy, integer/logic pipe half
 // busy); a version whose warps stay and run their copies on into the next token needed more registers than there are (129 us).
 #include <cuda_bf16.h>
