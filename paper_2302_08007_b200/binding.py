@@ -99,7 +99,8 @@ class Planes:
         view = _Planes(e.data_ptr(), m.data_ptr() if m.numel() else None, x.data_ptr(), e.stride(0), m.stride(0) if m.numel() else 0, x.stride(0))
         sizes = (e.numel, m.numel, x.numel)
         lines = min(t.shape[0] for t in (e, m, x) if t.numel()) if e.numel() else 0
-        self.__dict__.update(_view=view, _known=tuple(f() for f in probe), _probe=probe, _sizes=sizes, _counts=tuple(f() for f in sizes), _lines=lines)
+        on_gpu = e.is_cuda and x.is_cuda and (m.is_cuda or not m.numel())
+        self.__dict__.update(_on_gpu=on_gpu, _view=view, _known=tuple(f() for f in probe), _probe=probe, _sizes=sizes, _counts=tuple(f() for f in sizes), _lines=lines)
 
     def lines(self) -> int:
         """Lines that every plane holds."""
@@ -151,7 +152,9 @@ class KVCache:
                 if t.dtype != torch.uint8 or t.dim() != 2 or t.stride(1) != 1 or t.shape[0] < self.n_pages * self.page_size:
                     raise ValueError("cache planes are uint8 [n_pages * page_size, pitch] tensors")
         k, v = self.k, self.v
-        c = _KVCache(self.cfg_k.c(), self.cfg_v.c(), k.c(), v.c(), self.n_pages, self.page_size, self.n_kv, self.head_dim)
+        views = k.c(), v.c()
+        object.__setattr__(self, "_on_gpu", k._on_gpu and v._on_gpu)
+        c = _KVCache(self.cfg_k.c(), self.cfg_v.c(), *views, self.n_pages, self.page_size, self.n_kv, self.head_dim)
         object.__setattr__(self, "_parts", (k, v, k._probe, v._probe, k._known + v._known, C.addressof(c), c))
         return C.addressof(c)
 
@@ -517,12 +520,6 @@ def mx_gemm_e4m3(a: torch.Tensor, scales_a: torch.Tensor, b: torch.Tensor, scale
     return c
 
 
-def _on_gpu(*tensors):
-    for t in tensors:
-        if t is not None and not t.is_cuda:
-            raise ValueError("expected CUDA tensors")
-
-
 def _pitch(stride: int, rows: int, width: int, what: str) -> int:
     """The pitch of `rows` rows of `width` elements.  With one row at most a stride means nothing; else rows that share memory (an
     expanded view, say) are refused, since a kernel takes a pitch of at least a row."""
@@ -540,7 +537,8 @@ def mx_gemv(cfg_w: Config, w: Planes, N: int, K: int, x: torch.Tensor, y: torch.
     lines, c, p = w.lines(), cfg_w.c(), w._view
     if k != K or y2.shape != (T, N) or (sx != 1 and K > 1) or (sy != 1 and N > 1) or lines < N:
         raise ValueError("x is [T, K], y is [T, N], rows contiguous, and the planes hold N lines")
-    _on_gpu(x, y, w.elems)
+    if not (x.is_cuda and y.is_cuda and w._on_gpu):
+        raise ValueError("expected CUDA tensors")
     _check(lib().mx_gemv(C.addressof(c), C.addressof(p), N, K, x2.data_ptr(), _dt(x2), _pitch(ldx, T, K, "x"), T, y2.data_ptr(), _dt(y2),
                          _pitch(ldy, T, N, "y"), _stream(stream)), "mx_gemv")
     return y
@@ -570,7 +568,8 @@ def mx_kv_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.
     shape, ldk = _heads(k, "k")
     vshape, ldv = _heads(v, "v")
     T, dtype = shape[0], k.dtype
-    if not (k.is_cuda and v.is_cuda and slots.is_cuda and cache.k.elems.is_cuda):
+    ref = cache.ref()
+    if not (k.is_cuda and v.is_cuda and slots.is_cuda and cache._on_gpu):
         raise ValueError("expected CUDA tensors")
     if vshape != shape or shape[1] != cache.n_kv or shape[2] != cache.head_dim or v.dtype != dtype:
         raise ValueError("k and v are [tokens, n_kv, head_dim] of one dtype")
@@ -601,7 +600,7 @@ def mx_kv_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.
     for t in (k_dq, v_dq):
         if t is not None and (t.shape != shape or t.dtype != dtype or not t.is_contiguous() or not t.is_cuda):
             raise ValueError("k_dq, v_dq: contiguous, like k")
-    _check(lib().mx_kv_append(cache.ref(), k.data_ptr(), ldk, v.data_ptr(), ldv, _dt(k), T, slots.data_ptr(), rot,
+    _check(lib().mx_kv_append(ref, k.data_ptr(), ldk, v.data_ptr(), ldv, _dt(k), T, slots.data_ptr(), rot,
                               q.data_ptr() if n_q else None, ldq, n_q, q_out.data_ptr() if n_q else None, ldo,
                               k_dq.data_ptr() if k_dq is not None else None, v_dq.data_ptr() if v_dq is not None else None,
                               _stream(stream)), "mx_kv_append")
@@ -618,7 +617,8 @@ def mx_attn_decode(cache: KVCache, q: torch.Tensor, page_table: torch.Tensor, le
     """out [B, n_q, head_dim] = attention of one query token per sequence, q [B, n_q, head_dim], over the cached positions
     t < lengths[b] (int32 [B]; the last `window` of them when window > 0) whose pages are page_table[b] (int32 [B, max_pages]).
     lse: float32 [B, n_q].  scale: head_dim ** -0.5 when None."""
-    if not (q.is_cuda and page_table.is_cuda and lengths.is_cuda and out.is_cuda and workspace.is_cuda and cache.k.elems.is_cuda):
+    ref = cache.ref()
+    if not (q.is_cuda and page_table.is_cuda and lengths.is_cuda and out.is_cuda and workspace.is_cuda and cache._on_gpu):
         raise ValueError("expected CUDA tensors")
     (B, n_q, d), ldq = _heads(q, "q")
     oshape, ldo = _heads(out, "out")
@@ -635,7 +635,7 @@ def mx_attn_decode(cache: KVCache, q: torch.Tensor, page_table: torch.Tensor, le
         if window < 0:
             raise ValueError("window: not negative")
         window = 2 ** 31 - 1                                     # more positions than a cache can have
-    _check(lib().mx_attn_decode(cache.ref(), q.data_ptr(), ldq, _dt(q), B, n_q, page_table.data_ptr(),
+    _check(lib().mx_attn_decode(ref, q.data_ptr(), ldq, _dt(q), B, n_q, page_table.data_ptr(),
                                 _pitch(ld_table, B, max_pages, "page_table"), max_pages, lengths.data_ptr(),
                                 d ** -0.5 if scale is None else scale, window, out.data_ptr(), ldo, lse.data_ptr() if lse is not None else None,
                                 workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream)), "mx_attn_decode")

@@ -109,3 +109,21 @@ def test_a_window_wider_than_any_cache_is_no_narrower_one(calls):
         assert calls[0][1][11] == want
     with pytest.raises(ValueError):
         bdr.mx_attn_decode(cache(), q, table, lengths, torch.empty_like(q), ws, window=-2 ** 32 + 3)
+
+
+def test_planes_that_are_not_all_on_a_gpu(calls):
+    host = lambda *s: torch.zeros(s, dtype=torch.uint8)  # noqa: E731
+    q, k, slots, table, lengths, ws = t(3, 4, 32), t(3, 2, 32), t(3, dtype=torch.int64), t(3, 5, dtype=torch.int32), t(3, dtype=torch.int32), t(1 << 16, dtype=torch.uint8)
+    for name in ("exps", "micro", "elems"):
+        w = planes(8, 32)
+        setattr(w, name, host(*getattr(w, name).shape))
+        with pytest.raises(ValueError):
+            bdr.mx_gemv(bdr.MX6, w, 8, 32, t(4, 32), t(4, 8))
+        for which in ("k", "v"):
+            c = cache()
+            setattr(getattr(c, which), name, host(*getattr(getattr(c, which), name).shape))
+            with pytest.raises(ValueError):
+                bdr.mx_kv_append(c, k, k, slots)
+            with pytest.raises(ValueError):
+                bdr.mx_attn_decode(c, q, table, lengths, torch.empty_like(q), ws)
+    assert not calls
