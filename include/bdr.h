@@ -399,6 +399,63 @@ int mx_attn_decode(const mx_kv_cache_t* cache /*host*/, const void* q, int64_t l
                    const int32_t* page_table, int64_t ld_table, int64_t max_pages, const int32_t* lengths, float scale, int32_t window,
                    void* out, int64_t ldo, float* lse, void* workspace, int64_t workspace_bytes, void* stream);
 
+/* ---- Feed-forward layer and vocabulary head of a language model ------------------------------------------------
+ * Products of packed operands with what follows them fused to them.  Operands are axis-1 planes in the Table II formats (k1 = 16,
+ * k2 = 2, d2 = 1, m in {2, 4, 7}; either tie rule; the two formats of a call may differ), any sizes with K >= 1; pitches and plane
+ * addresses are multiples of 16 bytes.  Products are those of the decoded values (in bf16, so blocks whose unit is below 2^-133 lose
+ * low bits, as in mx_gemm_ws) with fp32 accumulation; blocks with the exponent byte 0xFF decode to NaN.  Results do not change from run to run.
+ * A workspace is device scratch, 256-byte aligned, contents overwritten, of the size that the call's _workspace_bytes gives (0 for
+ * sizes that the call refuses).  Bounded waits that run out leave BDR_ERR_TIMEOUT in the sticky word of bdr_device_status. */
+
+/* Activations.  SILU x / (1 + exp(-x)); GELU x Phi(x); GELU_TANH x (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))) / 2; RELU max(x, 0),
+ * with derivative 0 at 0. */
+typedef enum { MX_ACT_SILU = 0, MX_ACT_GELU = 1, MX_ACT_GELU_TANH = 2, MX_ACT_RELU = 3 } mx_act_t;
+
+/* Gated feed-forward layer, both projections, the activation and the product in one kernel:
+ *     h[M,N] (row pitch ldh) = act(A Wg^T) * (A Wu^T)
+ * A is packed [M,K], w packed [2 N, K]: first the N lines of Wg, then those of Wu.  `dt` is the type of h and of gate_up: NULL, or
+ * [M, 2 N] (row pitch ld_gate_up) for the two products A Wg^T and A Wu^T, rounded, which the backward pass reads. */
+int64_t mx_gated_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K);
+int mx_gated_gemm(const bdr_config_t* cfg_a /*host*/, const bdr_planes_t* a /*host struct*/, const bdr_config_t* cfg_w /*host*/,
+                  const bdr_planes_t* w /*host struct*/, int64_t M, int64_t N, int64_t K, int32_t act, void* h, bdr_dtype_t dt,
+                  int64_t ldh, void* gate_up, int64_t ld_gate_up, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Its gradients, with regard to the decoded values of A and W:
+ *     dG = dh * u * act'(g), dU = dh * act(g);   dA[M,K] = dG Wg + dU Wu;   dW[2 N, K] = [dG dU]^T A
+ * for g, u from gate_up, or computed again from A and W when it is NULL.  dh [M,N], gate_up, dA and dW are of type `dt`; dA or dW may
+ * be NULL (not wanted).  dG and dU enter the products as bf16 for dt = BF16 and as the sums of three bf16 parts
+ * (24 bits) for F32. */
+int64_t mx_gated_gemm_bwd_workspace_bytes(int64_t M, int64_t N, int64_t K, bdr_dtype_t dt);
+int mx_gated_gemm_bwd(const bdr_config_t* cfg_a /*host*/, const bdr_planes_t* a /*host struct*/, const bdr_config_t* cfg_w /*host*/,
+                      const bdr_planes_t* w /*host struct*/, int64_t M, int64_t N, int64_t K, int32_t act, const void* dh, bdr_dtype_t dt,
+                      int64_t ld_dh, const void* gate_up, int64_t ld_gate_up, void* da, int64_t ld_da, void* dw, int64_t ld_dw,
+                      void* workspace, int64_t workspace_bytes, void* stream);
+
+/* The gated layer for a few tokens whose activations are not packed: h[T,N] = act(x Wg^T) * (x Wu^T), with the types, limits and
+ * rounding of mx_gemv; w as in mx_gated_gemm. */
+int mx_gated_gemv(const bdr_config_t* cfg_w /*host*/, const bdr_planes_t* w /*host struct*/, int64_t N, int64_t K, const void* x,
+                  bdr_dtype_t x_dt, int64_t ldx, int64_t T, int32_t act, void* h, bdr_dtype_t h_dt, int64_t ldh, void* stream);
+
+/* Softmax cross entropy of logits l = A W^T (A packed [M,K], w packed [V,K], V >= 1) that are never stored:
+ *     lse[i] = log sum_j exp(l_ij),   loss[i] = lse[i] - l[i, targets[i]]
+ * (fp32 [M]; targets int64 [M], device).  A row with a negative target does not count: its loss is 0.  A target >= V is seen on the
+ * device only: the row's loss is NaN and BDR_ERR_SIZE is left in the sticky word of bdr_device_status. */
+int64_t mx_cross_entropy_workspace_bytes(int64_t M, int64_t V, int64_t K);
+int mx_cross_entropy(const bdr_config_t* cfg_a /*host*/, const bdr_planes_t* a /*host struct*/, const bdr_config_t* cfg_w /*host*/,
+                     const bdr_planes_t* w /*host struct*/, int64_t M, int64_t V, int64_t K, const int64_t* targets, float* loss, float* lse,
+                     void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Its gradients with regard to the decoded values of A and W, from the lse of the forward call and dloss (fp32 [M]):
+ *     d_ij = dloss[i] (exp(l_ij - lse[i]) - [j = targets[i]]),   dA[M,K] = d W,   dW[V,K] = d^T A
+ * Rows whose target is negative, or >= V, have none (whatever dloss, lse and their logits are).  The logits are computed again, piece by piece
+ * of the vocabulary.  dA and dW are of type `dt`, either may be NULL; d enters the products as bf16 for dt = BF16 and as the sum of three
+ * bf16 parts (24 bits) for F32. */
+int64_t mx_cross_entropy_bwd_workspace_bytes(int64_t M, int64_t V, int64_t K, bdr_dtype_t dt);
+int mx_cross_entropy_bwd(const bdr_config_t* cfg_a /*host*/, const bdr_planes_t* a /*host struct*/, const bdr_config_t* cfg_w /*host*/,
+                         const bdr_planes_t* w /*host struct*/, int64_t M, int64_t V, int64_t K, const int64_t* targets, const float* lse,
+                         const float* dloss, void* da, int64_t ld_da, void* dw, int64_t ld_dw, bdr_dtype_t dt, void* workspace,
+                         int64_t workspace_bytes, void* stream);
+
 /* BDR_OK, or BDR_ERR_TIMEOUT if any mx_gemm launch on the current device gave up a bounded wait
  * (sticky).  Host call; synchronises with the device (it copies one word back). */
 int mx_gemm_status(void);

@@ -19,12 +19,15 @@ LIB_PATH = os.path.join(_PKG, "libbdr_b200.so")
 SCALE_POW2, SCALE_FP32_INT, SCALE_FP32_FP, SCALE_FP32_VSQ = 0, 1, 2, 3
 ROUND_NEAREST_EVEN, ROUND_NEAREST_AWAY = 0, 1
 F32, BF16 = 0, 1
+ACT_SILU, ACT_GELU, ACT_GELU_TANH, ACT_RELU = 0, 1, 2, 3
 
 EXPORTS = ("bdr_strerror", "bdr_device_status", "bdr_packed_sizes", "bdr_quant_dequant", "bdr_pack", "bdr_unpack",
            "bdr_qsnr_workspace_bytes", "bdr_qsnr", "bdr_qsnr_static_max_cfgs", "bdr_qsnr_static", "mx_gemm",
            "mx_gemm_workspace_bytes", "mx_gemm_ws", "mx_gemm_f8_workspace_bytes", "mx_gemm_f8", "bdr_reencode_e4m3", "mx_gemm_e4m3", "bdr_set_workspace",
            "mx_gemm_status", "bdr_selftest_bounded_wait", "bdr_selftest_host", "bdr_qsnr_from_sums", "bdr_pack2", "bdr_qsnr_delayed", "bdr_amax", "bdr_tile_packing_efficiency", "mx_gemm_hw", "bdr_gather_rows", "bdr_device_status_reset", "bdr_quant_dequant_parent",
-           "mx_gemv", "mx_kv_append", "mx_attn_decode", "mx_attn_decode_workspace_bytes")
+           "mx_gemv", "mx_kv_append", "mx_attn_decode", "mx_attn_decode_workspace_bytes",
+           "mx_gated_gemm", "mx_gated_gemm_workspace_bytes", "mx_gated_gemm_bwd", "mx_gated_gemm_bwd_workspace_bytes", "mx_gated_gemv",
+           "mx_cross_entropy", "mx_cross_entropy_workspace_bytes", "mx_cross_entropy_bwd", "mx_cross_entropy_bwd_workspace_bytes")
 
 
 class BdrError(RuntimeError):
@@ -260,6 +263,24 @@ def lib():
         L.mx_attn_decode_workspace_bytes.argtypes = [ptr, i64, i32]
         L.mx_attn_decode.restype = C.c_int
         L.mx_attn_decode.argtypes = [ptr, ptr, i64, C.c_int, i64, i32, ptr, i64, i64, ptr, C.c_float, i32, ptr, i64, ptr, ptr, i64, ptr]
+        L.mx_gated_gemv.restype = C.c_int
+        L.mx_gated_gemv.argtypes = [ptr, ptr, i64, i64, ptr, C.c_int, i64, i64, i32, ptr, C.c_int, i64, ptr]
+        L.mx_gated_gemm_workspace_bytes.restype = i64
+        L.mx_gated_gemm_workspace_bytes.argtypes = [i64, i64, i64]
+        L.mx_gated_gemm.restype = C.c_int
+        L.mx_gated_gemm.argtypes = [ptr, ptr, ptr, ptr, i64, i64, i64, i32, ptr, C.c_int, i64, ptr, i64, ptr, i64, ptr]
+        L.mx_gated_gemm_bwd_workspace_bytes.restype = i64
+        L.mx_gated_gemm_bwd_workspace_bytes.argtypes = [i64, i64, i64, C.c_int]
+        L.mx_gated_gemm_bwd.restype = C.c_int
+        L.mx_gated_gemm_bwd.argtypes = [ptr, ptr, ptr, ptr, i64, i64, i64, i32, ptr, C.c_int, i64, ptr, i64, ptr, i64, ptr, i64, ptr, i64, ptr]
+        L.mx_cross_entropy_workspace_bytes.restype = i64
+        L.mx_cross_entropy_workspace_bytes.argtypes = [i64, i64, i64]
+        L.mx_cross_entropy.restype = C.c_int
+        L.mx_cross_entropy.argtypes = [ptr, ptr, ptr, ptr, i64, i64, i64, ptr, ptr, ptr, ptr, i64, ptr]
+        L.mx_cross_entropy_bwd_workspace_bytes.restype = i64
+        L.mx_cross_entropy_bwd_workspace_bytes.argtypes = [i64, i64, i64, C.c_int]
+        L.mx_cross_entropy_bwd.restype = C.c_int
+        L.mx_cross_entropy_bwd.argtypes = [ptr, ptr, ptr, ptr, i64, i64, i64, ptr, ptr, ptr, ptr, i64, ptr, i64, C.c_int, ptr, i64, ptr]
         for fn in (L.bdr_packed_sizes, L.bdr_quant_dequant, L.bdr_pack, L.bdr_unpack, L.bdr_qsnr, L.mx_gemm):
             fn.restype = C.c_int
         _lib = L
@@ -542,6 +563,145 @@ def mx_gemv(cfg_w: Config, w: Planes, N: int, K: int, x: torch.Tensor, y: torch.
     _check(lib().mx_gemv(C.addressof(c), C.addressof(p), N, K, x2.data_ptr(), _dt(x2), _pitch(ldx, T, K, "x"), T, y2.data_ptr(), _dt(y2),
                          _pitch(ldy, T, N, "y"), _stream(stream)), "mx_gemv")
     return y
+
+
+def mx_gated_gemv(cfg_w: Config, w: Planes, N: int, K: int, x: torch.Tensor, h: torch.Tensor, act: int = ACT_SILU,
+                  stream=None) -> torch.Tensor:
+    """h[T,N] = act(x Wg^T) * (x Wu^T) for a few rows of x [T,K] (float32 or bfloat16; h likewise); w is packed [2 N, K], the N
+    lines of Wg before those of Wu."""
+    x2, h2 = x if x.dim() == 2 else x.unsqueeze(0), h if h.dim() == 2 else h.unsqueeze(0)
+    (T, k), (ldx, sx), (ldh, sh) = x2.shape, x2.stride(), h2.stride()
+    lines, c, p = w.lines(), cfg_w.c(), w._view
+    if k != K or h2.shape != (T, N) or (sx != 1 and K > 1) or (sh != 1 and N > 1) or lines < 2 * N:
+        raise ValueError("x is [T, K], h is [T, N], rows contiguous, and the planes hold 2 N lines")
+    if not (x.is_cuda and h.is_cuda and w._on_gpu):
+        raise ValueError("expected CUDA tensors")
+    _check(lib().mx_gated_gemv(C.addressof(c), C.addressof(p), N, K, x2.data_ptr(), _dt(x2), _pitch(ldx, T, K, "x"), T, act, h2.data_ptr(),
+                               _dt(h2), _pitch(ldh, T, N, "h"), _stream(stream)), "mx_gated_gemv")
+    return h
+
+
+def _rows(t: torch.Tensor, rows: int, cols: int, dtype, what: str) -> int:
+    """Row pitch of a [rows, cols] CUDA tensor of `dtype` whose rows are contiguous."""
+    if t.dtype != dtype or t.shape != (rows, cols) or (t.stride(1) != 1 and cols > 1):
+        raise ValueError("%s: expected %s [%d, %d] with contiguous rows" % (what, dtype, rows, cols))
+    return _pitch(t.stride(0), rows, cols, what)
+
+
+def _vector(t: torch.Tensor, n: int, dtype, what: str) -> None:
+    if t.dtype != dtype or t.shape != (n,) or not t.is_contiguous():
+        raise ValueError("%s: contiguous %s [%d]" % (what, dtype, n))
+
+
+def _operand(p: Planes, lines: int, what: str):
+    if p.lines() < lines:
+        raise ValueError("%s: the planes hold fewer than %d lines" % (what, lines))
+    return p._view
+
+
+def _on_current(*tensors) -> None:
+    """All (None: left out) on the GPU that launches go to."""
+    here = torch.cuda.current_device() if torch.cuda.is_available() else None
+    for t in tensors:
+        if t is None:
+            continue
+        if isinstance(t, Planes):
+            t.c()
+            if not t._on_gpu:
+                raise ValueError("expected CUDA tensors")
+            t = t.exps
+        if not t.is_cuda:
+            raise ValueError("expected CUDA tensors")
+        if t.device.index != here:
+            raise ValueError("expected tensors of the current device")
+
+
+def _bytes(t: torch.Tensor) -> int:
+    if not t.is_contiguous():
+        raise ValueError("workspace: expected a contiguous tensor")
+    return t.numel() * t.element_size()
+
+
+def mx_gated_gemm_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(lib().mx_gated_gemm_workspace_bytes(M, N, K))
+
+
+def mx_gated_gemm(cfg_a: Config, a: Planes, cfg_w: Config, w: Planes, M: int, N: int, K: int, h: torch.Tensor, workspace: torch.Tensor,
+                  act: int = ACT_SILU, gate_up: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """h[M,N] (float32 or bfloat16) = act(A Wg^T) * (A Wu^T) for A packed [M, K] and w packed [2 N, K], the N lines of Wg before those
+    of Wu.  gate_up: [M, 2 N] of h's type for both products, which mx_gated_gemm_bwd reads."""
+    ca, cw, pa, pw = cfg_a.c(), cfg_w.c(), _operand(a, M, "a"), _operand(w, 2 * N, "w")
+    dt, ldh = _dt(h), _rows(h, M, N, h.dtype, "h")
+    ldg = _rows(gate_up, M, 2 * N, h.dtype, "gate_up") if gate_up is not None else 0
+    _on_current(a, w, h, gate_up, workspace)
+    _check(lib().mx_gated_gemm(C.addressof(ca), C.addressof(pa), C.addressof(cw), C.addressof(pw), M, N, K, act, _ptr(h), dt, ldh,
+                               _ptr(gate_up), ldg, _ptr(workspace), _bytes(workspace), _stream(stream)), "mx_gated_gemm")
+    return h
+
+
+def mx_gated_gemm_bwd_workspace_bytes(M: int, N: int, K: int, dtype: torch.dtype = torch.bfloat16) -> int:
+    """dtype: of the gradients."""
+    return int(lib().mx_gated_gemm_bwd_workspace_bytes(M, N, K, F32 if dtype == torch.float32 else BF16))
+
+
+def mx_gated_gemm_bwd(cfg_a: Config, a: Planes, cfg_w: Config, w: Planes, M: int, N: int, K: int, dh: torch.Tensor, da: torch.Tensor | None,
+                      dw: torch.Tensor | None, workspace: torch.Tensor, act: int = ACT_SILU, gate_up: torch.Tensor | None = None, stream=None):
+    """Gradients of mx_gated_gemm from dh [M, N]: da [M, K] and dw [2 N, K] of dh's type (None: not wanted).  gate_up: what the forward
+    call stored; None: both products are computed again."""
+    ca, cw, pa, pw = cfg_a.c(), cfg_w.c(), _operand(a, M, "a"), _operand(w, 2 * N, "w")
+    dt, ldh = _dt(dh), _rows(dh, M, N, dh.dtype, "dh")
+    ldg = _rows(gate_up, M, 2 * N, dh.dtype, "gate_up") if gate_up is not None else 0
+    lda = _rows(da, M, K, dh.dtype, "da") if da is not None else 0
+    ldw = _rows(dw, 2 * N, K, dh.dtype, "dw") if dw is not None else 0
+    _on_current(a, w, dh, gate_up, da, dw, workspace)
+    _check(lib().mx_gated_gemm_bwd(C.addressof(ca), C.addressof(pa), C.addressof(cw), C.addressof(pw), M, N, K, act, _ptr(dh), dt, ldh,
+                                   _ptr(gate_up), ldg, _ptr(da), lda, _ptr(dw), ldw, _ptr(workspace), _bytes(workspace), _stream(stream)),
+           "mx_gated_gemm_bwd")
+    return da, dw
+
+
+def mx_cross_entropy_workspace_bytes(M: int, V: int, K: int) -> int:
+    return int(lib().mx_cross_entropy_workspace_bytes(M, V, K))
+
+
+def mx_cross_entropy(cfg_a: Config, a: Planes, cfg_w: Config, w: Planes, M: int, V: int, K: int, targets: torch.Tensor, loss: torch.Tensor,
+                     lse: torch.Tensor, workspace: torch.Tensor, stream=None):
+    """loss and lse (float32 [M]) of the logits A W^T, which are not stored, for A packed [M, K] and w packed [V, K]; targets: int64
+    [M], negative = the row does not count (loss 0)."""
+    ca, cw, pa, pw = cfg_a.c(), cfg_w.c(), _operand(a, M, "a"), _operand(w, V, "w")
+    _vector(targets, M, torch.int64, "targets")
+    _vector(loss, M, torch.float32, "loss")
+    _vector(lse, M, torch.float32, "lse")
+    _on_current(a, w, targets, loss, lse, workspace)
+    _check(lib().mx_cross_entropy(C.addressof(ca), C.addressof(pa), C.addressof(cw), C.addressof(pw), M, V, K, _ptr(targets), _ptr(loss),
+                                  _ptr(lse), _ptr(workspace), _bytes(workspace), _stream(stream)), "mx_cross_entropy")
+    return loss, lse
+
+
+def mx_cross_entropy_bwd_workspace_bytes(M: int, V: int, K: int, dtype: torch.dtype = torch.bfloat16) -> int:
+    """dtype: of the gradients."""
+    return int(lib().mx_cross_entropy_bwd_workspace_bytes(M, V, K, F32 if dtype == torch.float32 else BF16))
+
+
+def mx_cross_entropy_bwd(cfg_a: Config, a: Planes, cfg_w: Config, w: Planes, M: int, V: int, K: int, targets: torch.Tensor, lse: torch.Tensor,
+                         dloss: torch.Tensor, da: torch.Tensor | None, dw: torch.Tensor | None, workspace: torch.Tensor, stream=None):
+    """Gradients of mx_cross_entropy from dloss (float32 [M]) and the forward call's lse: da [M, K] and dw [V, K], both float32 or both
+    bfloat16 (None: not wanted)."""
+    ca, cw, pa, pw = cfg_a.c(), cfg_w.c(), _operand(a, M, "a"), _operand(w, V, "w")
+    _vector(targets, M, torch.int64, "targets")
+    _vector(lse, M, torch.float32, "lse")
+    _vector(dloss, M, torch.float32, "dloss")
+    dtype = (da if da is not None else dw).dtype if da is not None or dw is not None else torch.float32
+    lda = _rows(da, M, K, dtype, "da") if da is not None else 0
+    ldw = _rows(dw, V, K, dtype, "dw") if dw is not None else 0
+    dt = F32 if dtype == torch.float32 else BF16
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("tensor dtype must be float32 or bfloat16")
+    _on_current(a, w, targets, lse, dloss, da, dw, workspace)
+    _check(lib().mx_cross_entropy_bwd(C.addressof(ca), C.addressof(pa), C.addressof(cw), C.addressof(pw), M, V, K, _ptr(targets), _ptr(lse),
+                                      _ptr(dloss), _ptr(da), lda, _ptr(dw), ldw, dt, _ptr(workspace), _bytes(workspace), _stream(stream)),
+           "mx_cross_entropy_bwd")
+    return da, dw
 
 
 def _heads(t: torch.Tensor, what: str):

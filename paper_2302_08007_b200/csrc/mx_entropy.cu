@@ -1,0 +1,315 @@
+// Softmax cross entropy over a vocabulary, from packed hidden states A [M, K] and packed vocabulary weights W [V, K]: with l = A W^T,
+//     lse_i = log sum_j exp(l_ij),   loss_i = lse_i - l_i,t_i      (rows whose target is negative do not count: loss 0, no gradient)
+//     d_ij = dloss_i (exp(l_ij - lse_i) - [j = t_i]),   dA = d W,   dW = d^T A
+// The logits are never stored.  Forward: the epilogue of the product reduces a row's 128 columns to their maximum and their sum of
+// exponentials (fp32), which a second kernel joins; the thread that meets a row's target column writes that logit.  Backward: pieces of
+// the vocabulary, each computed again, turned into d (bf16, or three bf16 parts) by the epilogue, and multiplied with W and A by the two
+// products of mx_grad_gemm.cu; dA is summed over the pieces in fp32, in order.
+#include <algorithm>
+
+#include "mx_frag.cuh"
+#include "mx_fused_gemm.cuh"
+
+namespace bdr {
+namespace {
+
+using fused::kRows;
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ float exp2_of(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// GRAD: the epilogue writes d instead of a row's maxima and sums
+template <bool GRAD>
+struct EntropyJob {
+    struct Params {
+        CUtensorMap a, w;         // bf16 [M][K]; [columns of this piece][K]
+        int n_items, tiles_m, tiles_n, band_rows, steps;
+        int M, cols;
+        int64_t col0;             // the piece's first column
+        const int64_t* targets;
+        float2* parts;            // [columns / 128][M]: maximum, sum of exp(l - maximum)
+        float* hit;               // [M]: the target's logit
+        const float *lse, *dloss;
+        __nv_bfloat16* d;         // [n_parts][M][pitch_d]
+        int64_t pitch_d;
+        int64_t vocab;
+        int n_parts;
+        int* status;
+    };
+    struct Item { int steps, tm, tn; };
+    static constexpr bool b_mn = false;
+    static __device__ __forceinline__ bool a_mn(const Item&) { return false; }
+    static __device__ __forceinline__ Item item(const Params& p, int i) {
+        Item it;
+        it.steps = p.steps;
+        gemm_tile_coords(i, p.tiles_m, p.tiles_n, p.band_rows, it.tm, it.tn);
+        return it;
+    }
+    static __device__ __forceinline__ void load(const Params& p, const Item& it, int kk, int rank, uint8_t* dst, uint64_t* bar) {
+        tma_load_3d(dst, &p.a, kk * kBK, (it.tm * 2 + rank) * kRows, 0, bar);
+        tma_load_3d(dst + fused::kOperandBytes, &p.w, kk * kBK, (it.tn * 2 + rank) * kRows, 0, bar);
+    }
+    static __device__ __forceinline__ void epilogue(const Params& p, const Item& it, int r, int half, uint32_t tmem) {
+        const int64_t row = (int64_t)it.tm * 256 + r;
+        const int first = it.tn * 256 + half * 128;  // column in the piece
+        const bool live = row < p.M;
+        const int64_t target = live ? p.targets[row] : -1;
+        const int64_t at = target - p.col0 - first;  // column of the target among these 128
+        if constexpr (!GRAD) {
+            float top = -INFINITY, sum = 0.f;
+#pragma unroll 1
+            for (int c = 0; c < 128; c += 32) {
+                __syncwarp();
+                uint32_t u[32];
+                tmem_ld32(tmem + (uint32_t)(half * 128 + c), u);
+                float v[32];
+                const int n = p.cols - first - c;
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[j] = j < n ? __uint_as_float(u[j]) : -INFINITY;
+                if (at >= c && at < c + 32 && at < c + n) {
+                    float x = 0.f;
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) x = at - c == j ? v[j] : x;
+                    p.hit[row] = x;
+                }
+                float m = v[0];
+#pragma unroll
+                for (int j = 1; j < 32; ++j) m = fmaxf(m, v[j]);
+                m = fmaxf(m, top);
+                const float ref = m == -INFINITY ? 0.f : m;  // nothing yet: every term is zero (a NaN among the terms stays one)
+                float s = sum * exp2_of((top - ref) * kLog2e);
+#pragma unroll
+                for (int j = 0; j < 32; ++j) s += exp2_of((v[j] - ref) * kLog2e);
+                top = m;
+                sum = s;
+            }
+            if (live && first < p.cols) p.parts[((p.col0 + first) >> 7) * p.M + row] = make_float2(top, sum);
+        } else {
+            const float lse = live ? p.lse[row] : 0.f, scale = live ? p.dloss[row] : 0.f;
+            const bool counts = target >= 0 && target < p.vocab;
+#pragma unroll 1
+            for (int c = 0; c < 128; c += 32) {
+                __syncwarp();
+                uint32_t u[32];
+                tmem_ld32(tmem + (uint32_t)(half * 128 + c), u);
+                const int n = min(32, p.cols - first - c);
+                if (!live || n <= 0) continue;
+                float v[32];
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    const float e = exp2_of((__uint_as_float(u[j]) - lse) * kLog2e) - (at - c == j ? 1.f : 0.f);
+                    v[j] = counts ? scale * e : 0.f;
+                }
+                fused::store_parts(p.d + row * p.pitch_d + first + c, p.M * p.pitch_d, p.n_parts, v, n);
+            }
+        }
+    }
+};
+
+// Joins a row's maxima and sums: 32 rows per block, their pieces shared out to 32 warps.
+__global__ void __launch_bounds__(1024) entropy_join_kernel(const float2* parts, int n_parts, int64_t M, const float* hit, const int64_t* targets,
+                                                            int64_t V, float* loss, float* lse, int* status) {
+    __shared__ float2 shared[32][33];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t row = (int64_t)blockIdx.x * 32 + lane;
+    auto join = [](float2 a, float2 b) {
+        const float m = fmaxf(a.x, b.x), ref = m == -INFINITY ? 0.f : m;
+        return make_float2(m, a.y * exp2_of((a.x - ref) * kLog2e) + b.y * exp2_of((b.x - ref) * kLog2e));
+    };
+    float2 mine = make_float2(-INFINITY, 0.f);
+    if (row < M)
+        for (int i = warp; i < n_parts; i += 32) mine = join(mine, parts[(int64_t)i * M + row]);
+    shared[warp][lane] = mine;
+    __syncthreads();
+    if (warp == 0 && row < M) {
+        for (int i = 1; i < 32; ++i) mine = join(mine, shared[i][lane]);
+        const float l = mine.x + logf(mine.y);
+        lse[row] = l;
+        const int64_t t = targets[row];
+        if (t >= V) atomicCAS(status, 0, (int)BDR_ERR_SIZE);
+        loss[row] = t < 0 ? 0.f : (t < V ? l - hit[row] : __int_as_float(0x7FC00000));
+    }
+}
+
+// Pieces of the vocabulary: as few as keep the decoded weights, and d, within a bound, all of about the same size.
+int64_t piece_columns(int64_t V, int64_t most) {
+    most = std::max<int64_t>(256, most / 256 * 256);
+    const int64_t n = (V + most - 1) / most;
+    return round_up((V + n - 1) / n, 256);
+}
+constexpr int64_t kMostWeights = 512ll << 20;   // bytes of decoded weights at a time
+constexpr int64_t kMostD = 256ll << 20;         // bytes of d at a time
+
+struct EntropySpace {
+    int64_t pitch_k, piece, a, w, parts, hit, bytes;
+    EntropySpace(int64_t M, int64_t V, int64_t K) {
+        pitch_k = line_pitch(K);
+        piece = piece_columns(V, kMostWeights / (pitch_k * 2));
+        a = 0;
+        w = a + round_up(M * pitch_k * 2, 256);
+        parts = w + round_up(std::min(piece, V) * pitch_k * 2, 256);
+        hit = parts + round_up((V + 127) / 128 * M * 8, 256);
+        bytes = hit + round_up(M * 4, 256);
+    }
+};
+struct EntropyGradSpace {
+    int64_t pitch_k, piece, a, w, d, acc, bytes;
+    EntropyGradSpace(int64_t M, int64_t V, int64_t K, int n_parts) {
+        pitch_k = line_pitch(K);
+        piece = piece_columns(V, std::min(kMostWeights / (pitch_k * 2), kMostD / (std::max<int64_t>(M, 1) * 2 * n_parts)));
+        a = 0;
+        w = a + round_up(M * pitch_k * 2, 256);
+        d = w + round_up(std::min(piece, V) * pitch_k * 2, 256);
+        acc = d + round_up(n_parts * M * piece * 2, 256);
+        bytes = acc + (piece < V ? round_up(M * pitch_k * 4, 256) : 0);
+    }
+};
+
+constexpr int64_t kMost = 1ll << 30;
+
+template <class Params>
+int set_piece(Params& p, int64_t M, int64_t K, int64_t col0, int64_t cols, int64_t pitch_k, const uint8_t* a, const uint8_t* w) {
+    if (!fused::make_map(&p.a, a, K, M, 1, pitch_k, M * pitch_k, kRows) || !fused::make_map(&p.w, w, K, cols, 1, pitch_k, cols * pitch_k, kRows))
+        return BDR_ERR_CUDA;
+    p.tiles_m = (int)((M + 255) / 256);
+    p.tiles_n = (int)((cols + 255) / 256);
+    p.n_items = p.tiles_m * p.tiles_n;
+    p.band_rows = gemm_band_rows((M + cols) * K * 2);
+    p.steps = (int)((K + kBK - 1) / kBK);
+    p.M = (int)M;
+    p.cols = (int)cols;
+    p.col0 = col0;
+    return BDR_OK;
+}
+
+bdr_planes_t lines_from(const bdr_planes_t& w, int64_t line) {
+    bdr_planes_t p = w;
+    p.exps += line * p.ld_exps;
+    p.micro += line * p.ld_micro;
+    p.elems += line * p.ld_elems;
+    return p;
+}
+
+int check_entropy(const bdr_config_t* cfg_a, const bdr_config_t* cfg_w, int64_t M, int64_t V, int64_t K) {
+    if (M < 0 || V < 1 || K < 0 || M > kMost || V > kMost || K > kMost) return BDR_ERR_SIZE;
+    const int64_t tm = (M + 255) / 256, tv = (V + 255) / 256, tk = (K + 255) / 256;
+    if (K == 0 || tm * std::max(tv, tk) >= (1ll << 29) || tv * tk >= (1ll << 29)) return BDR_ERR_UNSUPPORTED;
+    const int rc = check_table2_config(cfg_a);
+    return rc ? rc : check_table2_config(cfg_w);
+}
+
+}  // namespace
+}  // namespace bdr
+
+using namespace bdr;
+
+extern "C" {
+
+int64_t mx_cross_entropy_workspace_bytes(int64_t M, int64_t V, int64_t K) {
+    if (M < 0 || V < 1 || K < 1 || M > kMost || V > kMost || K > kMost) return 0;
+    return EntropySpace(M, V, K).bytes;
+}
+
+int mx_cross_entropy(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bdr_config_t* cfg_w, const bdr_planes_t* w, int64_t M, int64_t V,
+                     int64_t K, const int64_t* targets, float* loss, float* lse, void* workspace, int64_t workspace_bytes, void* stream) {
+    int rc = check_entropy(cfg_a, cfg_w, M, V, K);
+    if (rc || M == 0) return rc;
+    if ((rc = check_fused_operands(cfg_a, a, cfg_w, w, K))) return rc;
+    if (!targets || !loss || !lse) return BDR_ERR_NULL;
+    if ((uintptr_t)targets % 8 || ((uintptr_t)loss | (uintptr_t)lse) % 4) return BDR_ERR_MISALIGNED;
+    const EntropySpace s(M, V, K);
+    if (!workspace || workspace_bytes < s.bytes) return BDR_ERR_WORKSPACE;
+    if ((uintptr_t)workspace % 256) return BDR_ERR_MISALIGNED;
+    cudaStream_t st = (cudaStream_t)stream;
+    uint8_t* const ws = static_cast<uint8_t*>(workspace);
+    EntropyJob<false>::Params p = {};
+    p.targets = targets;
+    p.vocab = V;
+    p.parts = reinterpret_cast<float2*>(ws + s.parts);
+    p.hit = reinterpret_cast<float*>(ws + s.hit);
+    p.status = device_status_word();
+    if (!p.status) return BDR_ERR_CUDA;
+    if ((rc = decode_lines(*a, cfg_a->m, M, K, reinterpret_cast<__nv_bfloat16*>(ws + s.a), s.pitch_k, st))) return rc;
+    for (int64_t v = 0; v < V; v += s.piece) {
+        const int64_t cols = std::min(s.piece, V - v);
+        if ((rc = decode_lines(lines_from(*w, v), cfg_w->m, cols, K, reinterpret_cast<__nv_bfloat16*>(ws + s.w), s.pitch_k, st))) return rc;
+        if ((rc = set_piece(p, M, K, v, cols, s.pitch_k, ws + s.a, ws + s.w))) return rc;
+        if ((rc = fused::launch<EntropyJob<false>>(p, st))) return rc;
+    }
+    entropy_join_kernel<<<(unsigned)((M + 31) / 32), 1024, 0, st>>>(p.parts, (int)((V + 127) / 128), M, p.hit, targets, V, loss, lse, p.status);
+    return cudaGetLastError() == cudaSuccess ? BDR_OK : BDR_ERR_CUDA;
+}
+
+int64_t mx_cross_entropy_bwd_workspace_bytes(int64_t M, int64_t V, int64_t K, bdr_dtype_t dt) {
+    if (M < 0 || V < 1 || K < 1 || M > kMost || V > kMost || K > kMost) return 0;
+    return EntropyGradSpace(M, V, K, dt == BDR_F32 ? fused::kPartsF32 : 1).bytes;
+}
+
+int mx_cross_entropy_bwd(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bdr_config_t* cfg_w, const bdr_planes_t* w, int64_t M, int64_t V,
+                         int64_t K, const int64_t* targets, const float* lse, const float* dloss, void* da, int64_t ld_da, void* dw, int64_t ld_dw,
+                         bdr_dtype_t dt, void* workspace, int64_t workspace_bytes, void* stream) {
+    if (dt != BDR_F32 && dt != BDR_BF16) return BDR_ERR_UNSUPPORTED;
+    int rc = check_entropy(cfg_a, cfg_w, M, V, K);
+    if (rc) return rc;
+    const int width = dt == BDR_F32 ? 4 : 2;
+    for (int i = 0; i < 2; ++i) {
+        const void* g = i ? dw : da;
+        if (!g || (i == 0 && M == 0)) continue;
+        if ((i ? ld_dw : ld_da) < K) return BDR_ERR_SIZE;
+        if ((uintptr_t)g % width) return BDR_ERR_MISALIGNED;
+    }
+    cudaStream_t st = (cudaStream_t)stream;
+    if (M == 0) {  // a sum over nothing
+        if (dw && cudaMemset2DAsync(dw, ld_dw * width, 0, K * width, V, st) != cudaSuccess) return BDR_ERR_CUDA;
+        return BDR_OK;
+    }
+    if (!da && !dw) return BDR_OK;
+    if ((rc = check_fused_operands(cfg_a, a, cfg_w, w, K))) return rc;
+    if (!targets || !lse || !dloss) return BDR_ERR_NULL;
+    if ((uintptr_t)targets % 8 || ((uintptr_t)dloss | (uintptr_t)lse) % 4) return BDR_ERR_MISALIGNED;
+    const int n_parts = dt == BDR_F32 ? fused::kPartsF32 : 1;
+    const EntropyGradSpace s(M, V, K, n_parts);
+    if (!workspace || workspace_bytes < s.bytes) return BDR_ERR_WORKSPACE;
+    if ((uintptr_t)workspace % 256) return BDR_ERR_MISALIGNED;
+    uint8_t* const ws = static_cast<uint8_t*>(workspace);
+    EntropyJob<true>::Params p = {};
+    p.targets = targets;
+    p.vocab = V;
+    p.lse = lse;
+    p.dloss = dloss;
+    p.d = reinterpret_cast<__nv_bfloat16*>(ws + s.d);
+    p.pitch_d = s.piece;
+    p.n_parts = n_parts;
+    p.status = device_status_word();
+    if (!p.status) return BDR_ERR_CUDA;
+    GradProducts g = {};
+    g.d = p.d;
+    g.a = reinterpret_cast<__nv_bfloat16*>(ws + s.a);
+    g.w = reinterpret_cast<__nv_bfloat16*>(ws + s.w);
+    g.M = M; g.K = K; g.pitch_d = s.piece; g.pitch_k = s.pitch_k;
+    g.segs = 1; g.parts = n_parts;
+    g.da = da; g.ld_da = ld_da; g.ld_dw = ld_dw;
+    g.f32 = dt == BDR_F32;
+    g.acc = s.piece < V ? reinterpret_cast<float*>(ws + s.acc) : nullptr;
+    g.ld_acc = s.pitch_k;
+    if ((rc = decode_lines(*a, cfg_a->m, M, K, reinterpret_cast<__nv_bfloat16*>(ws + s.a), s.pitch_k, st))) return rc;
+    for (int64_t v = 0; v < V; v += s.piece) {
+        const int64_t cols = std::min(s.piece, V - v);
+        if ((rc = decode_lines(lines_from(*w, v), cfg_w->m, cols, K, reinterpret_cast<__nv_bfloat16*>(ws + s.w), s.pitch_k, st))) return rc;
+        if ((rc = set_piece(p, M, K, v, cols, s.pitch_k, ws + s.a, ws + s.w))) return rc;
+        if ((rc = fused::launch<EntropyJob<true>>(p, st))) return rc;
+        g.N = cols;
+        g.dw = dw ? static_cast<char*>(dw) + v * ld_dw * width : nullptr;
+        g.first = v == 0;
+        g.last = v + s.piece >= V;
+        if ((rc = launch_grad_products(g, st))) return rc;
+    }
+    return BDR_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,42 @@
+// Host-side declarations shared by the operators that fuse work to a product of packed operands (gated feed-forward layer,
+// cross entropy): decoding into a workspace, and the two gradient products.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "bdr.h"
+
+namespace bdr {
+
+int* device_status_word();
+
+constexpr int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+// Pitch (elements) of lines of K decoded elements: whole items of the decode kernel.
+constexpr int64_t line_pitch(int64_t K) { return round_up(K, 32); }
+
+// Packed lines (Table II formats, m magnitude bits) -> bf16 [rows, pitch]; what lies behind K in a row is unspecified.
+int decode_lines(const bdr_planes_t& in, int m, int64_t rows, int64_t K, __nv_bfloat16* out, int64_t pitch, cudaStream_t st);
+
+// The gradient products.  D is bf16 [parts * segs][M][pitch_d] of which N columns count: D = sum over parts, segment s belongs to
+// the weight lines w + s * N * pitch_k.  dA[M, K] (+)= sum_s D_s W_s, dW[s * N + n, K] = D_s^T A.  W is bf16 [segs * N, pitch_k],
+// A bf16 [M, pitch_k].
+struct GradProducts {
+    const __nv_bfloat16 *d, *a, *w;
+    int64_t M, N, K, pitch_d, pitch_k;
+    int segs, parts;
+    void *da, *dw;          // either may be NULL: not computed
+    int64_t ld_da, ld_dw;   // elements
+    bool f32;               // type of da and dw (else bf16)
+    float* acc;             // fp32 [M, ld_acc] running sum of dA over several calls; NULL: this call is the only one
+    int64_t ld_acc;
+    bool first, last;       // of those calls: the first does not read acc, the last writes da
+};
+int launch_grad_products(const GradProducts& g, cudaStream_t st);
+
+// What the operators accept of two packed operands A [M, K] and W [lines, K] (host).
+int check_fused_operands(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bdr_config_t* cfg_w, const bdr_planes_t* w, int64_t K);
+
+}  // namespace bdr

@@ -1,0 +1,309 @@
+// Gated feed-forward layer on packed operands: h[M, N] = act(A Wg^T) * (A Wu^T), and its gradients.
+//
+// Forward.  The two weights are one packed tensor of 2 N lines (gate first).  Both are decoded to bf16 once (exact: at most seven
+// magnitude bits), and one persistent kernel computes both products: a cluster's 256-column accumulator holds 128 columns of the gate
+// (which the leader CTA loads) and the same 128 columns of the other projection (its peer's), so that a thread of the epilogue has both values
+// of an output in its own tensor-memory lane and writes h without either product passing through memory.  For training they are
+// stored on the side, rounded to h's type.
+// Backward.  dG = dh * u * act'(g), dU = dh * act(g); dA = dG Wg + dU Wu, dWg = dG^T A, dWu = dU^T A.  With the products stored by the
+// forward pass the first step is an elementwise kernel; without them they are computed again, in the same kernel as the forward's, whose
+// epilogue then reads dh and writes dG and dU.  The gradient products are those of mx_grad_gemm.cu.
+#include <algorithm>
+
+#include "mx_act.cuh"
+#include "mx_frag.cuh"
+#include "mx_fused_gemm.cuh"
+
+namespace bdr {
+namespace {
+
+using fused::kRows;
+
+struct Rows {           // a row-major tensor of the call's type
+    void* p;
+    int64_t ld;
+    int vec;            // 16-byte accesses at multiples of 32 columns
+    __device__ __forceinline__ void* row(int64_t r, int f32) const { return static_cast<char*>(p) + r * ld * (f32 ? 4 : 2); }
+};
+
+// GRAD: the epilogue writes dG and dU instead of h
+template <bool GRAD>
+struct GatedJob {
+    struct Params {
+        CUtensorMap a, w;          // bf16 [M][K]; [2][N][K]
+        int n_items, tiles_m, tiles_n, band_rows, steps;
+        int M, N, act, f32;
+        Rows h;                    // h, or dh
+        Rows gate, up;             // where the two products go (NULL: nowhere)
+        __nv_bfloat16* d;          // [parts][2][M][pitch_d]
+        int64_t pitch_d;
+        int parts;
+        int* status;
+    };
+    struct Item { int steps, tm, tn; };
+    static constexpr bool b_mn = false;
+    static __device__ __forceinline__ bool a_mn(const Item&) { return false; }
+    static __device__ __forceinline__ Item item(const Params& p, int i) {
+        Item it;
+        it.steps = p.steps;
+        gemm_tile_coords(i, p.tiles_m, p.tiles_n, p.band_rows, it.tm, it.tn);
+        return it;
+    }
+    static __device__ __forceinline__ void load(const Params& p, const Item& it, int kk, int rank, uint8_t* dst, uint64_t* bar) {
+        tma_load_3d(dst, &p.a, kk * kBK, (it.tm * 2 + rank) * kRows, 0, bar);
+        tma_load_3d(dst + fused::kOperandBytes, &p.w, kk * kBK, it.tn * kRows, rank, bar);
+    }
+    static __device__ __forceinline__ void epilogue(const Params& p, const Item& it, int r, int half, uint32_t tmem) {
+        const int64_t row = (int64_t)it.tm * 256 + r;
+#pragma unroll 1
+        for (int c = half * 64; c < half * 64 + 64; c += 32) {
+            __syncwarp();
+            uint32_t gu[2][32];
+            tmem_ld32_nowait(tmem + (uint32_t)c, gu[0]);
+            tmem_ld32_nowait(tmem + (uint32_t)(128 + c), gu[1]);
+            tmem_ld_wait();
+            const int col = it.tn * kRows + c, n = min(32, p.N - col);
+            if (row >= p.M || n <= 0) continue;
+            float g[32], u[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) { g[j] = __uint_as_float(gu[0][j]); u[j] = __uint_as_float(gu[1][j]); }
+            if constexpr (!GRAD) {
+                if (p.gate.p) {
+                    fused::store_run(p.gate.row(row, p.f32), col, g, n, p.f32, p.gate.vec);
+                    fused::store_run(p.up.row(row, p.f32), col, u, n, p.f32, p.up.vec);
+                }
+                act::with(p.act, [&](auto f) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) g[j] = act::of<decltype(f)::value>(g[j]) * u[j];
+                });
+                fused::store_run(p.h.row(row, p.f32), col, g, n, p.f32, p.h.vec);
+            } else {
+                float dh[32];
+                fused::load_run(p.h.row(row, p.f32), col, dh, n, p.f32, p.h.vec);
+                act::with(p.act, [&](auto f) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) {
+                        float y, slope;
+                        act::both<decltype(f)::value>(g[j], y, slope);
+                        g[j] = dh[j] * u[j] * slope;
+                        u[j] = dh[j] * y;
+                    }
+                });
+                __nv_bfloat16* const to = p.d + row * p.pitch_d + col;
+                const int64_t z = (int64_t)p.M * p.pitch_d;
+                fused::store_parts(to, 2 * z, p.parts, g, n);
+                fused::store_parts(to + z, 2 * z, p.parts, u, n);
+            }
+        }
+    }
+};
+
+// dG and dU from the stored products: eight columns of a row per thread.  Bound by memory (bf16: 6 bytes in, 4 out per output).
+template <bool F32>
+__global__ void __launch_bounds__(256) gated_grad_kernel(Rows gate, Rows up, Rows dh, int act, int64_t M, int N, __nv_bfloat16* d, int64_t pitch_d) {
+    const int groups = (N + 7) / 8;
+    const int64_t total = M * groups, stride = (int64_t)gridDim.x * 256, z = M * pitch_d;
+    auto get = [&](const Rows& t, int64_t row, int col, int n, float (&v)[8]) {
+        if constexpr (F32) {
+            const float* from = static_cast<const float*>(t.row(row, 1)) + col;
+            if (t.vec && n == 8) {
+                const float4 a = *reinterpret_cast<const float4*>(from), b = *reinterpret_cast<const float4*>(from + 4);
+                v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = j < n ? from[j] : 0.f;
+            }
+        } else {
+            const __nv_bfloat16* from = static_cast<const __nv_bfloat16*>(t.row(row, 0)) + col;
+            if (t.vec && n == 8) {
+                const uint4 x = *reinterpret_cast<const uint4*>(from);
+                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) { v[2 * e] = __uint_as_float(w[e] << 16); v[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u); }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = j < n ? __bfloat162float(from[j]) : 0.f;
+            }
+        }
+    };
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += stride) {
+        const int64_t row = i / groups;
+        const int col = (int)(i - row * groups) * 8, n = min(8, N - col);
+        float g[8], u[8], e[8];
+        get(gate, row, col, n, g);
+        get(up, row, col, n, u);
+        get(dh, row, col, n, e);
+        act::with(act, [&](auto f) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                float y, slope;
+                act::both<decltype(f)::value>(g[j], y, slope);
+                g[j] = e[j] * u[j] * slope;
+                u[j] = e[j] * y;
+            }
+        });
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            float(&v)[8] = s ? u : g;
+            __nv_bfloat16* const to = d + s * z + row * pitch_d + col;  // (the pitch has room for whole groups)
+#pragma unroll
+            for (int part = 0; part < (F32 ? fused::kPartsF32 : 1); ++part) {
+                *reinterpret_cast<uint4*>(to + 2 * part * z) = make_uint4(fused::bf16x2(v[0], v[1]), fused::bf16x2(v[2], v[3]), fused::bf16x2(v[4], v[5]), fused::bf16x2(v[6], v[7]));
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] -= __bfloat162float(__float2bfloat16_rn(v[j]));
+            }
+        }
+    }
+}
+
+// Workspace: A, W and, for gradients, D.
+struct GatedSpace {
+    int64_t pitch_k, pitch_d, a, w, d, bytes;  // offsets in bytes
+    GatedSpace(int64_t M, int64_t N, int64_t K, int parts) {
+        pitch_k = line_pitch(K);
+        pitch_d = round_up(N, 64);
+        a = 0;
+        w = a + round_up(M * pitch_k * 2, 256);
+        d = w + round_up(2 * N * pitch_k * 2, 256);
+        bytes = d + (parts ? round_up((int64_t)parts * 2 * M * pitch_d * 2, 256) : 0);
+    }
+};
+
+constexpr int64_t kMostRows = 1ll << 30;
+
+int check_rows(const void* p, int64_t ld, int64_t cols, int width) {
+    if (!p) return BDR_ERR_NULL;
+    if (ld < cols) return BDR_ERR_SIZE;
+    return (uintptr_t)p % width ? BDR_ERR_MISALIGNED : BDR_OK;
+}
+
+Rows make_rows(const void* p, int64_t ld, int width) { return {const_cast<void*>(p), ld, p ? fused::rows_aligned(p, ld, width) : 0}; }
+
+template <class Params>
+int set_products(Params& p, int64_t M, int64_t N, int64_t K, const GatedSpace& s, uint8_t* ws) {
+    if (!fused::make_map(&p.a, ws + s.a, K, M, 1, s.pitch_k, M * s.pitch_k, kRows) ||
+        !fused::make_map(&p.w, ws + s.w, K, N, 2, s.pitch_k, N * s.pitch_k, kRows))
+        return BDR_ERR_CUDA;
+    p.tiles_m = (int)((M + 255) / 256);
+    p.tiles_n = (int)((N + kRows - 1) / kRows);
+    p.n_items = p.tiles_m * p.tiles_n;
+    p.band_rows = gemm_band_rows((M + 2 * N) * K * 2);
+    p.steps = (int)((K + kBK - 1) / kBK);
+    p.M = (int)M;
+    p.N = (int)N;
+    p.status = device_status_word();
+    return p.status ? BDR_OK : BDR_ERR_CUDA;
+}
+
+}  // namespace
+}  // namespace bdr
+
+using namespace bdr;
+
+extern "C" {
+
+int64_t mx_gated_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K) {
+    if (M < 0 || N < 0 || K < 0 || M > kMostRows || N > kMostRows || K > kMostRows) return 0;
+    return GatedSpace(M, N, K, 0).bytes;
+}
+
+int mx_gated_gemm(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bdr_config_t* cfg_w, const bdr_planes_t* w, int64_t M, int64_t N,
+                  int64_t K, int32_t act, void* h, bdr_dtype_t dt, int64_t ldh, void* gate_up, int64_t ld_gate_up, void* workspace,
+                  int64_t workspace_bytes, void* stream) {
+    if (dt != BDR_F32 && dt != BDR_BF16) return BDR_ERR_UNSUPPORTED;
+    if (!act::known(act)) return BDR_ERR_UNSUPPORTED;
+    if (M < 0 || N < 0 || K < 0 || M > kMostRows || N > kMostRows / 2 || K > kMostRows) return BDR_ERR_SIZE;
+    if (K == 0 || ((M + 255) / 256) * ((N + kRows - 1) / kRows) >= (1ll << 30)) return BDR_ERR_UNSUPPORTED;
+    int rc = check_table2_config(cfg_a);
+    if (!rc) rc = check_table2_config(cfg_w);
+    if (rc || M == 0 || N == 0) return rc;
+    if ((rc = check_fused_operands(cfg_a, a, cfg_w, w, K))) return rc;
+    const int width = dt == BDR_F32 ? 4 : 2;
+    if ((rc = check_rows(h, ldh, N, width))) return rc;
+    if (gate_up && (rc = check_rows(gate_up, ld_gate_up, 2 * N, width))) return rc;
+    const GatedSpace s(M, N, K, 0);
+    if (!workspace || workspace_bytes < s.bytes) return BDR_ERR_WORKSPACE;
+    if ((uintptr_t)workspace % 256) return BDR_ERR_MISALIGNED;
+    cudaStream_t st = (cudaStream_t)stream;
+    uint8_t* const ws = static_cast<uint8_t*>(workspace);
+    if ((rc = decode_lines(*a, cfg_a->m, M, K, reinterpret_cast<__nv_bfloat16*>(ws + s.a), s.pitch_k, st))) return rc;
+    if ((rc = decode_lines(*w, cfg_w->m, 2 * N, K, reinterpret_cast<__nv_bfloat16*>(ws + s.w), s.pitch_k, st))) return rc;
+    GatedJob<false>::Params p = {};
+    if ((rc = set_products(p, M, N, K, s, ws))) return rc;
+    p.act = act;
+    p.f32 = dt == BDR_F32;
+    p.h = make_rows(h, ldh, width);
+    p.gate = make_rows(gate_up, ld_gate_up, width);
+    p.up = make_rows(gate_up ? static_cast<char*>(gate_up) + N * width : nullptr, ld_gate_up, width);
+    return fused::launch<GatedJob<false>>(p, st);
+}
+
+int64_t mx_gated_gemm_bwd_workspace_bytes(int64_t M, int64_t N, int64_t K, bdr_dtype_t dt) {
+    if (M < 0 || N < 0 || K < 0 || M > kMostRows || N > kMostRows || K > kMostRows) return 0;
+    return GatedSpace(M, N, K, dt == BDR_F32 ? fused::kPartsF32 : 1).bytes;
+}
+
+int mx_gated_gemm_bwd(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bdr_config_t* cfg_w, const bdr_planes_t* w, int64_t M, int64_t N,
+                      int64_t K, int32_t act, const void* dh, bdr_dtype_t dt, int64_t ld_dh, const void* gate_up, int64_t ld_gate_up, void* da,
+                      int64_t ld_da, void* dw, int64_t ld_dw, void* workspace, int64_t workspace_bytes, void* stream) {
+    if (dt != BDR_F32 && dt != BDR_BF16) return BDR_ERR_UNSUPPORTED;
+    if (!act::known(act)) return BDR_ERR_UNSUPPORTED;
+    if (M < 0 || N < 0 || K < 0 || M > kMostRows || N > kMostRows / 2 || K > kMostRows) return BDR_ERR_SIZE;
+    const int64_t tiles_k = (K + 255) / 256;
+    if (K == 0 || ((M + 255) / 256) * std::max(tiles_k, (N + kRows - 1) / kRows) >= (1ll << 29) || ((N + 255) / 256) * tiles_k >= (1ll << 29) ||
+        (N + kBK - 1) / kBK * 4 >= (1ll << 30))
+        return BDR_ERR_UNSUPPORTED;
+    int rc = check_table2_config(cfg_a);
+    if (!rc) rc = check_table2_config(cfg_w);
+    if (rc) return rc;
+    const int width = dt == BDR_F32 ? 4 : 2;
+    if (da && M > 0 && (rc = check_rows(da, ld_da, K, width))) return rc;
+    if (dw && N > 0 && (rc = check_rows(dw, ld_dw, K, width))) return rc;
+    cudaStream_t st = (cudaStream_t)stream;
+    if (M == 0 || N == 0) {  // sums over nothing
+        if (da && M > 0 && cudaMemset2DAsync(da, ld_da * width, 0, K * width, M, st) != cudaSuccess) return BDR_ERR_CUDA;
+        if (dw && N > 0 && cudaMemset2DAsync(dw, ld_dw * width, 0, K * width, 2 * N, st) != cudaSuccess) return BDR_ERR_CUDA;
+        return BDR_OK;
+    }
+    if (!da && !dw) return BDR_OK;
+    if ((rc = check_fused_operands(cfg_a, a, cfg_w, w, K))) return rc;
+    if ((rc = check_rows(dh, ld_dh, N, width))) return rc;
+    if (gate_up && (rc = check_rows(gate_up, ld_gate_up, 2 * N, width))) return rc;
+    const int parts = dt == BDR_F32 ? fused::kPartsF32 : 1;
+    const GatedSpace s(M, N, K, parts);
+    if (!workspace || workspace_bytes < s.bytes) return BDR_ERR_WORKSPACE;
+    if ((uintptr_t)workspace % 256) return BDR_ERR_MISALIGNED;
+    uint8_t* const ws = static_cast<uint8_t*>(workspace);
+    __nv_bfloat16 *const wa = reinterpret_cast<__nv_bfloat16*>(ws + s.a), *const ww = reinterpret_cast<__nv_bfloat16*>(ws + s.w),
+                         *const d = reinterpret_cast<__nv_bfloat16*>(ws + s.d);
+    if ((rc = decode_lines(*a, cfg_a->m, M, K, wa, s.pitch_k, st))) return rc;
+    if ((rc = decode_lines(*w, cfg_w->m, 2 * N, K, ww, s.pitch_k, st))) return rc;
+    const Rows dh_rows = make_rows(dh, ld_dh, width);
+    if (gate_up) {
+        const Rows g = make_rows(gate_up, ld_gate_up, width), u = make_rows(static_cast<const char*>(gate_up) + N * width, ld_gate_up, width);
+        const unsigned grid = (unsigned)std::min<int64_t>((M * ((N + 7) / 8) + 255) / 256, (int64_t)sm_count() * 16);
+        if (dt == BDR_F32) gated_grad_kernel<true><<<grid, 256, 0, st>>>(g, u, dh_rows, act, M, (int)N, d, s.pitch_d);
+        else gated_grad_kernel<false><<<grid, 256, 0, st>>>(g, u, dh_rows, act, M, (int)N, d, s.pitch_d);
+        if (cudaGetLastError() != cudaSuccess) return BDR_ERR_CUDA;
+    } else {
+        GatedJob<true>::Params p = {};
+        if ((rc = set_products(p, M, N, K, s, ws))) return rc;
+        p.act = act;
+        p.f32 = dt == BDR_F32;
+        p.h = dh_rows;
+        p.d = d;
+        p.pitch_d = s.pitch_d;
+        p.parts = parts;
+        if ((rc = fused::launch<GatedJob<true>>(p, st))) return rc;
+    }
+    GradProducts g = {};
+    g.d = d; g.a = wa; g.w = ww;
+    g.M = M; g.N = N; g.K = K; g.pitch_d = s.pitch_d; g.pitch_k = s.pitch_k;
+    g.segs = 2; g.parts = parts;
+    g.da = da; g.dw = dw; g.ld_da = ld_da; g.ld_dw = ld_dw;
+    g.f32 = dt == BDR_F32;
+    g.first = g.last = true;
+    return launch_grad_products(g, st);
+}
+
+}  // extern "C"

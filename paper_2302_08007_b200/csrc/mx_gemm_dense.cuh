@@ -37,11 +37,6 @@ struct DenseMaps {
     CUtensorMap a, b;  // bf16 [rows, K], box 64 x 128, 128-byte swizzle
 };
 
-__device__ __forceinline__ void tmem_alloc2_cols(uint32_t* dst_smem, uint32_t ncols) {
-    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(dst_smem)), "r"(ncols) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-}
-
 __device__ __forceinline__ void red_add_v4(float* p, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p), "f"(__uint_as_float(a)), "f"(__uint_as_float(b)),
                  "f"(__uint_as_float(c)), "f"(__uint_as_float(d))

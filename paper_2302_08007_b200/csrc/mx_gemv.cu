@@ -31,6 +31,7 @@
 
 #include "bdr_device.cuh"
 #include "bdr_host.h"
+#include "mx_act.cuh"
 #include "mx_frag.cuh"
 
 namespace bdr {
@@ -66,13 +67,14 @@ struct GemvArgs {
     const void* x;
     void* y;
     int64_t ldx, ldy;
-    int64_t n, k;
+    int64_t n, k;        // columns of y, elements of a row of x
     int tokens, tokens_per_pass;
     int x32, y32;        // 32-bit activations / results (else bf16)
     int xalign;          // rows of activations start on boundaries of 16, 4 or 2 bytes
     int kw, kw_log;      // warps that share a tile's K (a power of two, at most the steps there are)
     int rounds;          // of the groups over all tiles, rounded down; the first `rest` CTAs have one more
     unsigned rest;
+    int act;             // GATED: the activation
     int phase_steps;     // steps whose activations are in shared memory at once: all, or a multiple of kw in each of two buffers
 };
 
@@ -126,8 +128,16 @@ __device__ __forceinline__ const uint8_t* step_from(const uint8_t* p, int s, uin
     return q;
 }
 
+// The weight line of a row of a tile.  GATED: rows 0 .. 7 are lines of the gate, rows 8 .. 15 the same lines of the other projection,
+// n lines further on; rows beyond the end repeat the last.
+template <bool GATED>
+__device__ __forceinline__ int64_t line_of(int64_t tile, int row, int64_t n) {
+    if constexpr (GATED) return min(8 * tile + (row & 7), n - 1) + (row & 8 ? n : 0);
+    return min(16 * tile + row, n - 1);
+}
+
 // A warp's copies of a step of a row tile, with their sources kept as pointers into the tile's rows.
-template <int W>
+template <int W, bool GATED>
 struct StepCopies {
     static constexpr int kPieces = 2 * W, kCount = 16 * kPieces / 32;  // 16-byte pieces of a row; copies per lane
     static constexpr int kPitch = 32 * W, kAtX = 16 * kPitch;
@@ -136,9 +146,9 @@ struct StepCopies {
 #pragma unroll
         for (int i = 0; i < kCount; ++i) {
             const int at = lane + 32 * i, row = at / kPieces;
-            code[i] = p.elems + min(16 * tile + row, n - 1) * p.ld_elems + 16 * (at - row * kPieces);
+            code[i] = p.elems + line_of<GATED>(tile, row, n) * p.ld_elems + 16 * (at - row * kPieces);
         }
-        const int64_t row = min(16 * tile + (lane & 15), n - 1);
+        const int64_t row = line_of<GATED>(tile, lane & 15, n);
         scale = lane < 16 ? p.exps + row * p.ld_exps : p.micro + row * p.ld_micro;
     }
     // TAIL: the step may pass the end of the rows; what lies beyond a row's pitch is left out
@@ -312,7 +322,8 @@ __device__ __forceinline__ void run_step(const Run<W>& r0, const Run<W>& r1, con
     else run_step_as<W, NT, false>(r0, r1, xs, pitch, cols, lane, acc);
 }
 
-template <int W, int NT, bool X32, int WARPS>
+// GATED: y = act(x Wg^T) * (x Wu^T) for the 2 n lines of W; a tile is eight outputs
+template <int W, int NT, bool X32, int WARPS, bool GATED>
 __global__ void __launch_bounds__((GemvShape<W, NT, WARPS>::kThreads), 1) mx_gemv_kernel(const GemvArgs a) {
     using S = GemvShape<W, NT, WARPS>;
     constexpr int kWarps = S::kWarps, D = S::kStages;
@@ -325,7 +336,8 @@ __global__ void __launch_bounds__((GemvShape<W, NT, WARPS>::kThreads), 1) mx_gem
     const int t0 = blockIdx.y * a.tokens_per_pass, nt = min(a.tokens_per_pass, a.tokens - t0), cols = X32 ? 3 * nt : nt;
     const int nb = (int)((a.k + 15) / 16), steps = (nb + 15) / 16;
     // tiles go to the CTAs in turn, then to a CTA's groups: every SM has the same number to within one
-    const int64_t tiles = (a.n + 15) / 16, stride = (int64_t)gridDim.x * groups;
+    constexpr int kOut = GATED ? 8 : 16;  // outputs of a tile
+    const int64_t tiles = (a.n + kOut - 1) / kOut, stride = (int64_t)gridDim.x * groups;
     const int rounds = a.rounds + (blockIdx.x < a.rest ? 1 : 0);  // of the CTA's first group; the others may have one fewer
     const int64_t pitch = (int64_t)min(a.phase_steps, steps) * kGvStep + 32;
     float acc[NT][4];
@@ -336,7 +348,7 @@ __global__ void __launch_bounds__((GemvShape<W, NT, WARPS>::kThreads), 1) mx_gem
 
     int64_t tile = blockIdx.x + (int64_t)group * gridDim.x;
     // the copies run ahead of the computation, across the ends of tiles
-    StepCopies<W> copies;
+    StepCopies<W, GATED> copies;
     int64_t ahead_tile = tile;
     int ahead = my_k, to = 0, at = 0;
     if (ahead_tile < tiles) copies.point(a.w, ahead_tile, a.n, lane);
@@ -431,17 +443,21 @@ __global__ void __launch_bounds__((GemvShape<W, NT, WARPS>::kThreads), 1) mx_gem
         if (kw == 1) __syncwarp();
         else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(32 * kw) : "memory");
         const float* const from = mine - my_k * (8 * NT * 16);
-        for (int i = my_k * 32 + lane; i < nt * 16; i += kw * 32) {
-            const int t = i >> 4, r = i & 15;
-            if (16 * tile + r >= a.n) continue;
-            float v = 0.f;
+        for (int i = my_k * 32 + lane; i < nt * kOut; i += kw * 32) {
+            const int t = i / kOut, r = i % kOut;
+            if (kOut * tile + r >= a.n) continue;
+            auto total = [&](int row) {
+                float v = 0.f;
 #pragma unroll
-            for (int part = 0; part < (X32 ? 3 : 1); ++part) {
-                const int col = X32 ? 3 * t + (2 - part) : t;  // smallest part first
-                for (int q = 0; q < kw; ++q) v += from[q * (8 * NT * 16) + col * 16 + r];
-            }
-            v *= 2.f;  // the operand was decoded halved
-            const int64_t at = (int64_t)(t0 + t) * a.ldy + 16 * tile + r;
+                for (int part = 0; part < (X32 ? 3 : 1); ++part) {
+                    const int col = X32 ? 3 * t + (2 - part) : t;  // smallest part first
+                    for (int q = 0; q < kw; ++q) v += from[q * (8 * NT * 16) + col * 16 + row];
+                }
+                return v * 2.f;  // the operand was decoded halved
+            };
+            float v = total(r);
+            if constexpr (GATED) act::with(a.act, [&](auto f) { v = act::of<decltype(f)::value>(v) * total(r + 8); });
+            const int64_t at = (int64_t)(t0 + t) * a.ldy + kOut * tile + r;
             if (a.y32) static_cast<float*>(a.y)[at] = v;
             else static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(v);
         }
@@ -451,14 +467,14 @@ __global__ void __launch_bounds__((GemvShape<W, NT, WARPS>::kThreads), 1) mx_gem
     cp_async_wait<0>();
 }
 
-template <int W, int NT, bool X32, int WARPS = gemv_warps(W, NT)>
+template <int W, int NT, bool X32, bool GATED, int WARPS = gemv_warps(W, NT)>
 static int launch_gemv(GemvArgs a, cudaStream_t st) {
     using S = GemvShape<W, NT, WARPS>;
     static PerDevice once;
-    if (kernel_setup(once, mx_gemv_kernel<W, NT, X32, WARPS>, S::kThreads, kGvSmem) < 1) return BDR_ERR_CUDA;
+    if (kernel_setup(once, mx_gemv_kernel<W, NT, X32, WARPS, GATED>, S::kThreads, kGvSmem) < 1) return BDR_ERR_CUDA;
     const int cols = (X32 ? 3 : 1) * std::min(a.tokens, a.tokens_per_pass);
     const int steps = (int)((a.k + kGvStep - 1) / kGvStep), sms = sm_count();
-    const int64_t tiles = (a.n + 15) / 16;
+    const int64_t tiles = GATED ? (a.n + 7) / 8 : (a.n + 15) / 16;
     // the longest walk in steps, where a tile's join counts as a third of one and, if the activations come in phases, so does each phase's
     // barrier; putting a column's step in order, again for every round, takes about 1/500
     double best = 0;
@@ -480,35 +496,38 @@ static int launch_gemv(GemvArgs a, cudaStream_t st) {
     a.rounds = (int)(tiles / stride);
     a.rest = (unsigned)std::min<int64_t>(tiles % stride, ctas);
     const dim3 grid((unsigned)ctas, (unsigned)((a.tokens + a.tokens_per_pass - 1) / a.tokens_per_pass));
-    mx_gemv_kernel<W, NT, X32, WARPS><<<grid, S::kThreads, smem, st>>>(a);
+    mx_gemv_kernel<W, NT, X32, WARPS, GATED><<<grid, S::kThreads, smem, st>>>(a);
     return cudaGetLastError() == cudaSuccess ? BDR_OK : BDR_ERR_CUDA;
 }
 
-template <int W, bool X32>
+template <int W, bool X32, bool GATED>
 static int pick_columns(GemvArgs a, cudaStream_t st) {
     a.tokens_per_pass = X32 ? kGvMaxCols / 3 : kGvMaxCols;
     const int cols = (X32 ? 3 : 1) * std::min(a.tokens, a.tokens_per_pass);
-    if (cols <= 8) return launch_gemv<W, 1, X32>(a, st);
+    if (cols <= 8) return launch_gemv<W, 1, X32, GATED>(a, st);
     if (cols <= 16) {
         if constexpr (W == 3) {  // see gemv_warps
             const int64_t steps = (a.k + kGvStep - 1) / kGvStep;
-            if (steps > GemvShape<3, 2, 16>::fit(cols) && steps <= GemvShape<3, 2, 8>::fit(cols) && (a.n + 15) / 16 <= 2 * sm_count())
-                return launch_gemv<W, 2, X32, 8>(a, st);
+            if (steps > GemvShape<3, 2, 16>::fit(cols) && steps <= GemvShape<3, 2, 8>::fit(cols) && (GATED ? (a.n + 7) / 8 : (a.n + 15) / 16) <= 2 * sm_count())
+                return launch_gemv<W, 2, X32, GATED, 8>(a, st);
         }
-        return launch_gemv<W, 2, X32>(a, st);
+        return launch_gemv<W, 2, X32, GATED>(a, st);
     }
-    if (cols <= 32) return launch_gemv<W, 4, X32>(a, st);
-    return launch_gemv<W, 8, X32>(a, st);
+    if (cols <= 32) return launch_gemv<W, 4, X32, GATED>(a, st);
+    return launch_gemv<W, 8, X32, GATED>(a, st);
 }
 
 }  // namespace bdr
 
 using namespace bdr;
 
-extern "C" int mx_gemv(const bdr_config_t* cfg_w, const bdr_planes_t* w, int64_t N, int64_t K, const void* x, bdr_dtype_t x_dt,
-                       int64_t ldx, int64_t T, void* y, bdr_dtype_t y_dt, int64_t ldy, void* stream) {
+// mx_gemv, and the gated layer, whose W has 2 N lines
+template <bool GATED>
+static int run_gemv(const bdr_config_t* cfg_w, const bdr_planes_t* w, int64_t N, int64_t K, const void* x, bdr_dtype_t x_dt,
+                    int64_t ldx, int64_t T, int act, void* y, bdr_dtype_t y_dt, int64_t ldy, void* stream) {
     int rc = check_table2_config(cfg_w);
     if (rc) return rc;
+    if (GATED && !act::known(act)) return BDR_ERR_UNSUPPORTED;
     for (int dt : {(int)x_dt, (int)y_dt})
         if (dt != BDR_F32 && dt != BDR_BF16) return BDR_ERR_UNSUPPORTED;
     if (N < 0 || K < 0 || T < 0 || ldx < K || ldy < N || K > (1ll << 30) || N > (1ll << 34) || T > (1ll << 20)) return BDR_ERR_SIZE;
@@ -523,15 +542,26 @@ extern "C" int mx_gemv(const bdr_config_t* cfg_w, const bdr_planes_t* w, int64_t
         a.w = *w;
     }
     a.x = x; a.y = y; a.ldx = ldx; a.ldy = ldy; a.n = N; a.k = K; a.tokens = (int)T;
+    a.act = act;
     a.x32 = x_dt == BDR_F32; a.y32 = y_dt == BDR_F32;
     const int64_t xb = a.x32 ? 4 : 2;
     const uintptr_t at = (uintptr_t)x | (T == 1 ? 0 : (uintptr_t)(ldx * xb));
     a.xalign = at % 16 == 0 ? 16 : (at % 4 == 0 ? 4 : 2);
     cudaStream_t st = (cudaStream_t)stream;
     switch (cfg_w->m) {
-        case 2: return a.x32 ? pick_columns<3, true>(a, st) : pick_columns<3, false>(a, st);
-        case 4: return a.x32 ? pick_columns<5, true>(a, st) : pick_columns<5, false>(a, st);
-        case 7: return a.x32 ? pick_columns<8, true>(a, st) : pick_columns<8, false>(a, st);
+        case 2: return a.x32 ? pick_columns<3, true, GATED>(a, st) : pick_columns<3, false, GATED>(a, st);
+        case 4: return a.x32 ? pick_columns<5, true, GATED>(a, st) : pick_columns<5, false, GATED>(a, st);
+        case 7: return a.x32 ? pick_columns<8, true, GATED>(a, st) : pick_columns<8, false, GATED>(a, st);
     }
     return BDR_ERR_UNSUPPORTED;
+}
+
+extern "C" int mx_gemv(const bdr_config_t* cfg_w, const bdr_planes_t* w, int64_t N, int64_t K, const void* x, bdr_dtype_t x_dt,
+                       int64_t ldx, int64_t T, void* y, bdr_dtype_t y_dt, int64_t ldy, void* stream) {
+    return run_gemv<false>(cfg_w, w, N, K, x, x_dt, ldx, T, 0, y, y_dt, ldy, stream);
+}
+
+extern "C" int mx_gated_gemv(const bdr_config_t* cfg_w, const bdr_planes_t* w, int64_t N, int64_t K, const void* x, bdr_dtype_t x_dt,
+                             int64_t ldx, int64_t T, int32_t act, void* h, bdr_dtype_t h_dt, int64_t ldh, void* stream) {
+    return run_gemv<true>(cfg_w, w, N, K, x, x_dt, ldx, T, act, h, h_dt, ldh, stream);
 }

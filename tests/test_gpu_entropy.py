@@ -1,0 +1,228 @@
+"""Cross entropy over a packed vocabulary without the logits: loss, lse and gradients against the formulas in 64 bits."""
+import pytest
+import torch
+
+import fused_helpers as f
+from paper_2302_08007_b200 import binding as bdr
+
+pytestmark = pytest.mark.gpu
+
+
+def operands(m, v, k, fa="mx6", fw="mx6", seed=0, scale=2.0):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    a = torch.randn(m, k, device="cuda", generator=gen) * scale
+    w = torch.randn(v, k, device="cuda", generator=gen) * k ** -0.5
+    targets = torch.randint(0, v, (m,), device="cuda", generator=gen)
+    return f.packed(f.CFG[fa], a), f.packed(f.CFG[fw], w), targets, gen
+
+
+def run(pa, pw, fa, fw, m, v, k, targets):
+    loss, lse = (torch.full((m,), float("nan"), device="cuda") for _ in range(2))
+    ws = f.workspace(bdr.mx_cross_entropy_workspace_bytes(m, v, k))
+    bdr.mx_cross_entropy(f.CFG[fa], pa, f.CFG[fw], pw, m, v, k, targets, loss, lse, ws)
+    return loss, lse
+
+
+def run_grads(pa, pw, fa, fw, m, v, k, targets, lse, dloss, dtype):
+    da, dw = torch.full((m, k), float("nan"), device="cuda", dtype=dtype), torch.full((v, k), float("nan"), device="cuda", dtype=dtype)
+    ws = f.workspace(bdr.mx_cross_entropy_bwd_workspace_bytes(m, v, k, dtype))
+    bdr.mx_cross_entropy_bwd(f.CFG[fa], pa, f.CFG[fw], pw, m, v, k, targets, lse, dloss, da, dw, ws)
+    return da, dw
+
+
+SIZES = [(1, 1, 1), (1, 2, 17), (1, 300, 64), (3, 127, 100), (16, 129, 256), (17, 513, 300), (128, 256, 64), (129, 255, 65), (300, 1000, 1111), (515, 4100, 256)]
+
+
+@pytest.mark.parametrize("m,v,k", SIZES)
+def test_loss(m, v, k):
+    (pa, a), (pw, w), targets, gen = operands(m, v, k)
+    targets[::7] = -100
+    targets[-1] = v - 1
+    targets[0] = 0
+    loss, lse = run(pa, pw, "mx6", "mx6", m, v, k, targets)
+    want, want_lse, _, eloss, else_, _ = f.entropy(a, w, targets)
+    f.check(lse, want_lse, else_, "lse")
+    f.check(loss, want, eloss, "loss")
+    assert (loss[targets < 0] == 0).all()
+
+
+@pytest.mark.parametrize("fa", ["mx4", "mx6", "mx9"])
+@pytest.mark.parametrize("fw", ["mx4", "mx6", "mx9"])
+@pytest.mark.parametrize("m", [5, 150])
+def test_formats(fa, fw, m):
+    v, k = 700, 336
+    (pa, a), (pw, w), targets, _ = operands(m, v, k, fa, fw, 1)
+    loss, lse = run(pa, pw, fa, fw, m, v, k, targets)
+    want, want_lse, _, eloss, else_, _ = f.entropy(a, w, targets)
+    f.check(lse, want_lse, else_, "lse")
+    f.check(loss, want, eloss, "loss")
+
+
+GRAD_SIZES = [(1, 1, 1), (1, 300, 64), (3, 127, 300), (128, 256, 64), (257, 130, 200), (300, 1000, 1111), (70, 2100, 520)]
+
+
+@pytest.mark.parametrize("m,v,k", GRAD_SIZES)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_gradients(m, v, k, dtype):
+    (pa, a), (pw, w), targets, gen = operands(m, v, k, "mx9", "mx6", 2)
+    targets[1::5] = -1
+    _, lse = run(pa, pw, "mx9", "mx6", m, v, k, targets)
+    dloss = torch.randn(m, device="cuda", generator=gen)
+    da, dw = run_grads(pa, pw, "mx9", "mx6", m, v, k, targets, lse, dloss, dtype)
+    want_a, want_w, ea, ew = f.entropy_grads(a, w, targets, lse.double(), dloss.double(), dtype)
+    f.check(da, want_a, ea, "da")
+    f.check(dw, want_w, ew, "dw")
+    assert (da[targets < 0] == 0).all()
+    ws = f.workspace(bdr.mx_cross_entropy_bwd_workspace_bytes(m, v, k, dtype))
+    one, other = torch.empty_like(da), torch.empty_like(dw)
+    bdr.mx_cross_entropy_bwd(bdr.MX9, pa, bdr.MX6, pw, m, v, k, targets, lse, dloss, one, None, ws)
+    bdr.mx_cross_entropy_bwd(bdr.MX9, pa, bdr.MX6, pw, m, v, k, targets, lse, dloss, None, other, ws)
+    assert torch.equal(one, da) and torch.equal(other, dw)
+
+
+def test_gradients_by_differences():
+    m, v, k = 20, 50, 48
+    (pa, a), (pw, w), targets, gen = operands(m, v, k, "mx9", "mx9", 3)
+    targets[4] = -100
+    _, lse = run(pa, pw, "mx9", "mx9", m, v, k, targets)
+    dloss = torch.rand(m, device="cuda", generator=gen)
+    da, dw = run_grads(pa, pw, "mx9", "mx9", m, v, k, targets, lse, dloss, torch.float32)
+    total = lambda a, w: (f.entropy(a, w, targets)[0] * dloss.double()).sum()  # noqa: E731
+    step = 2.0 ** -12
+    for t, g, at in ((w, dw, ((0, 0), (49, 47), (int(targets[0]), 3))), (a, da, ((0, 0), (4, 9), (19, 47)))):
+        for i, j in at:
+            e = torch.zeros_like(t)
+            e[i, j] = step
+            up, down = (total(a, w + s * e) if t is w else total(a + s * e, w) for s in (1, -1))
+            assert abs(float((up - down) / (2 * step) - g[i, j])) < 1e-4      # (fp32 logits, and a third derivative times step^2 / 6)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_pieces_of_the_vocabulary(dtype):
+    # enough rows that the vocabulary is taken in more than one piece, the last one ragged
+    m, v, k = 4000, 34567, 96
+    (pa, a), (pw, w), targets, gen = operands(m, v, k, "mx6", "mx4", 4)
+    loss, lse = run(pa, pw, "mx6", "mx4", m, v, k, targets)
+    want, want_lse, _, eloss, else_, _ = f.entropy(a, w, targets)
+    f.check(lse, want_lse, else_, "lse")
+    f.check(loss, want, eloss, "loss")
+    dloss = torch.full((m,), 1.0 / m, device="cuda")
+    da, dw = run_grads(pa, pw, "mx6", "mx4", m, v, k, targets, lse, dloss, dtype)
+    want_a, want_w, ea, ew = f.entropy_grads(a, w, targets, lse.double(), dloss.double(), dtype)
+    f.check(da, want_a, ea, "da")
+    f.check(dw, want_w, ew, "dw")
+
+
+def test_rows_that_do_not_count():
+    m, v, k = 130, 300, 64
+    (pa, a), (pw, w), targets, _ = operands(m, v, k, seed=5)
+    targets[:] = -100
+    loss, lse = run(pa, pw, "mx6", "mx6", m, v, k, targets)
+    assert (loss == 0).all() and lse.isfinite().all()
+    nothing = torch.full((m,), float("nan"), device="cuda")
+    da, dw = run_grads(pa, pw, "mx6", "mx6", m, v, k, targets, nothing, nothing, torch.float32)
+    assert (da == 0).all() and (dw == 0).all()
+
+
+def test_a_target_beyond_the_vocabulary_is_reported():
+    m, v, k = 40, 300, 64
+    (pa, a), (pw, w), targets, _ = operands(m, v, k, seed=6)
+    bad = targets.clone()
+    bad[3], bad[17] = v, 2 ** 40
+    bdr.bdr_device_status_reset()
+    loss, lse = run(pa, pw, "mx6", "mx6", m, v, k, targets)
+    assert bdr.bdr_device_status() == 0
+    other, other_lse = run(pa, pw, "mx6", "mx6", m, v, k, bad)
+    assert bdr.bdr_device_status_reset() == -5
+    assert other.isnan().nonzero()[:, 0].tolist() == [3, 17] and torch.equal(lse, other_lse)
+    there = bad < v
+    assert torch.equal(other[there], loss[there])
+    dloss = torch.ones(m, device="cuda")
+    da, dw = run_grads(pa, pw, "mx6", "mx6", m, v, k, bad, lse, dloss, torch.float32)
+    none = torch.where(there, bad, -1)
+    ca, cw = run_grads(pa, pw, "mx6", "mx6", m, v, k, none, lse, dloss, torch.float32)
+    assert torch.equal(da, ca) and torch.equal(dw, cw)
+    assert bdr.bdr_device_status() == 0
+
+
+def test_large_and_equal_logits():
+    # one logit of thousands, and rows whose logits are all equal
+    m, v, k = 6, 300, 32
+    a, w = torch.zeros(m, k, device="cuda"), torch.zeros(v, k, device="cuda")
+    a[0, 0], a[1, 0], a[2, 1] = 100.0, -100.0, 2.0 ** 40
+    w[7, 0], w[9, 1] = 64.0, -1.0
+    (pa, a), (pw, w) = f.packed(bdr.MX9, a), f.packed(bdr.MX9, w)
+    targets = torch.tensor([7, 7, 9, 0, 299, -1], device="cuda")
+    loss, lse = run(pa, pw, "mx9", "mx9", m, v, k, targets)
+    want, want_lse, _, _, _, _ = f.entropy(a, w, targets)
+    f.check(lse, want_lse, 2.0 ** -20 * (1 + want_lse.abs()), "lse")
+    f.check(loss, want, 2.0 ** -20 * (1 + want.abs()), "loss")
+    da, dw = run_grads(pa, pw, "mx9", "mx9", m, v, k, targets, lse, torch.ones(m, device="cuda"), torch.float32)
+    assert da.isfinite().all() and dw.isfinite().all()
+
+
+def test_blocks_without_values_poison_their_own_rows():
+    m, v, k = 150, 400, 64
+    (pa, a), (pw, w), targets, _ = operands(m, v, k, seed=7)
+    clean = run(pa, pw, "mx6", "mx6", m, v, k, targets)
+    pa.exps[3, 1] = 0xFF
+    loss, lse = run(pa, pw, "mx6", "mx6", m, v, k, targets)
+    assert lse.isnan().nonzero()[:, 0].tolist() == [3] and loss.isnan().nonzero()[:, 0].tolist() == [3]
+    rest = torch.arange(m, device="cuda") != 3
+    assert torch.equal(lse[rest], clean[1][rest])
+    pw.exps[399, 0] = 0xFF
+    assert run(pa, pw, "mx6", "mx6", m, v, k, targets)[1].isnan().all()
+
+
+def test_strides_and_surroundings():
+    m, v, k = 133, 270, 90
+    (pa, a), (pw, w), targets, gen = operands(m, v, k, "mx6", "mx4", 8)
+    _, lse = run(pa, pw, "mx6", "mx4", m, v, k, targets)
+    dloss = torch.randn(m, device="cuda", generator=gen)
+    for dtype in (torch.bfloat16, torch.float32):
+        x, y = run_grads(pa, pw, "mx6", "mx4", m, v, k, targets, lse, dloss, dtype)
+        da, dw = torch.full((m + 2, k + 9), 7.0, device="cuda", dtype=dtype), torch.full((v + 2, k + 1), 7.0, device="cuda", dtype=dtype)
+        ws = f.workspace(bdr.mx_cross_entropy_bwd_workspace_bytes(m, v, k, dtype))
+        bdr.mx_cross_entropy_bwd(bdr.MX6, pa, bdr.MX4, pw, m, v, k, targets, lse, dloss, da[1:-1, 4:4 + k], dw[1:-1, 1:], ws)
+        assert torch.equal(da[1:-1, 4:4 + k], x) and torch.equal(dw[1:-1, 1:], y)
+        da[1:-1, 4:4 + k] = 7.0
+        dw[1:-1, 1:] = 7.0
+        assert (da == 7).all() and (dw == 7).all()
+
+
+def test_no_rows():
+    (pa, _), (pw, _), _, _ = operands(4, 40, 32)
+    ws = f.workspace(bdr.mx_cross_entropy_bwd_workspace_bytes(4, 40, 32, torch.float32))
+    none, at = torch.empty(0, device="cuda"), torch.empty(0, dtype=torch.int64, device="cuda")
+    bdr.mx_cross_entropy(bdr.MX6, pa, bdr.MX6, pw, 0, 40, 32, at, none, none.clone(), ws)
+    dw = torch.full((40, 32), 7.0, device="cuda")
+    bdr.mx_cross_entropy_bwd(bdr.MX6, pa, bdr.MX6, pw, 0, 40, 32, at, none, none, torch.empty(0, 32, device="cuda"), dw, ws)
+    assert (dw == 0).all()
+
+
+def test_captured_and_replayed():
+    m, v, k = 260, 700, 200
+    (pa, a), (pw, w), targets, gen = operands(m, v, k, seed=9)
+    dloss = torch.rand(m, device="cuda", generator=gen)
+    size = max(bdr.mx_cross_entropy_workspace_bytes(m, v, k), bdr.mx_cross_entropy_bwd_workspace_bytes(m, v, k))
+    ws = f.workspace(size)
+    new = lambda *s, **kw: torch.empty(s, device="cuda", **kw)  # noqa: E731
+    outs = [(new(m), new(m), new(m, k, dtype=torch.bfloat16), new(v, k, dtype=torch.bfloat16)) for _ in range(2)]
+
+    def step(loss, lse, da, dw):
+        bdr.mx_cross_entropy(bdr.MX6, pa, bdr.MX6, pw, m, v, k, targets, loss, lse, ws)
+        bdr.mx_cross_entropy_bwd(bdr.MX6, pa, bdr.MX6, pw, m, v, k, targets, lse, dloss, da, dw, ws)
+
+    step(*outs[0])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step(*outs[1])
+    for _ in range(3):
+        for t in outs[1]:
+            t.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        for t, want in zip(outs[1], outs[0]):
+            assert torch.equal(t, want)
