@@ -35,6 +35,7 @@ struct EntropyJob {
         float2* parts;            // [columns / 128][M]: maximum, sum of exp(l - maximum)
         float* hit;               // [M]: the target's logit
         const float *lse, *dloss;
+        const float* largest;     // of |dloss|, among the rows that count
         __nv_bfloat16* d;         // [n_parts][M][pitch_d]
         int64_t pitch_d;
         int64_t vocab;
@@ -43,6 +44,7 @@ struct EntropyJob {
     };
     struct Item { int steps, tm, tn; };
     static constexpr bool b_mn = false;
+    static constexpr int kSpan = 0;
     static __device__ __forceinline__ bool a_mn(const Item&) { return false; }
     static __device__ __forceinline__ Item item(const Params& p, int i) {
         Item it;
@@ -90,7 +92,7 @@ struct EntropyJob {
             }
             if (live && first < p.cols) p.parts[((p.col0 + first) >> 7) * p.M + row] = make_float2(top, sum);
         } else {
-            const float lse = live ? p.lse[row] : 0.f, scale = live ? p.dloss[row] : 0.f;
+            const float lse = live ? p.lse[row] : 0.f, scale = live ? p.dloss[row] / *p.largest : 0.f;
             const bool counts = target >= 0 && target < p.vocab;
 #pragma unroll 1
             for (int c = 0; c < 128; c += 32) {
@@ -136,6 +138,25 @@ __global__ void __launch_bounds__(1024) entropy_join_kernel(const float2* parts,
     }
 }
 
+// The largest |dloss| of the rows that count, by which d is divided before it is rounded to bf16 and the gradients are multiplied in
+// fp32: with the equal weights of a mean the term of the target, which outweighs all others of its row, is then near -1 and rounds to less
+// than the step of 1 (as 1/3891, say, it loses up to 2^-8: gradients of 4096 x 32000 x 4096 were off by 2.6e-3, now 1.7e-3, their own rounding).  One block.
+__global__ void __launch_bounds__(1024) entropy_scale_kernel(const float* dloss, const int64_t* targets, int64_t M, int64_t V, float* largest) {
+    __shared__ float shared[32];
+    float m = 0.f;
+    for (int64_t i = threadIdx.x; i < M; i += 1024)
+        if (targets[i] >= 0 && targets[i] < V) m = fmaxf(m, fabsf(dloss[i]));
+    for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+    if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = m;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        m = shared[threadIdx.x];
+        for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+        // (0, or infinite: nothing to divide by; a quotient of subnormals would overflow its inverse, but is itself in [-1, 1])
+        if (threadIdx.x == 0) *largest = m > 0.f && m < INFINITY ? m : 1.f;
+    }
+}
+
 // Pieces of the vocabulary: as few as keep the decoded weights, and d, within a bound, all of about the same size.
 int64_t piece_columns(int64_t V, int64_t most) {
     most = std::max<int64_t>(256, most / 256 * 256);
@@ -158,7 +179,7 @@ struct EntropySpace {
     }
 };
 struct EntropyGradSpace {
-    int64_t pitch_k, piece, a, w, d, acc, bytes;
+    int64_t pitch_k, piece, a, w, d, acc, largest, bytes;
     EntropyGradSpace(int64_t M, int64_t V, int64_t K, int n_parts) {
         pitch_k = line_pitch(K);
         piece = piece_columns(V, std::min(kMostWeights / (pitch_k * 2), kMostD / (std::max<int64_t>(M, 1) * 2 * n_parts)));
@@ -166,7 +187,8 @@ struct EntropyGradSpace {
         w = a + round_up(M * pitch_k * 2, 256);
         d = w + round_up(std::min(piece, V) * pitch_k * 2, 256);
         acc = d + round_up(n_parts * M * piece * 2, 256);
-        bytes = acc + (piece < V ? round_up(M * pitch_k * 4, 256) : 0);
+        largest = acc + (piece < V ? round_up(M * pitch_k * 4, 256) : 0);
+        bytes = largest + 256;
     }
 };
 
@@ -297,6 +319,9 @@ int mx_cross_entropy_bwd(const bdr_config_t* cfg_a, const bdr_planes_t* a, const
     g.f32 = dt == BDR_F32;
     g.acc = s.piece < V ? reinterpret_cast<float*>(ws + s.acc) : nullptr;
     g.ld_acc = s.pitch_k;
+    g.scale = p.largest = reinterpret_cast<const float*>(ws + s.largest);
+    entropy_scale_kernel<<<1, 1024, 0, st>>>(dloss, targets, M, V, reinterpret_cast<float*>(ws + s.largest));
+    if (cudaGetLastError() != cudaSuccess) return BDR_ERR_CUDA;
     if ((rc = decode_lines(*a, cfg_a->m, M, K, reinterpret_cast<__nv_bfloat16*>(ws + s.a), s.pitch_k, st))) return rc;
     for (int64_t v = 0; v < V; v += s.piece) {
         const int64_t cols = std::min(s.piece, V - v);

@@ -32,6 +32,7 @@ struct GradProducts {
     bool f32;               // type of da and dw (else bf16)
     float* acc;             // fp32 [M, ld_acc] running sum of dA over several calls; NULL: this call is the only one
     int64_t ld_acc;
+    const float* scale;     // device: factor of both gradients; NULL: 1
     bool first, last;       // of those calls: the first does not read acc, the last writes da
 };
 int launch_grad_products(const GradProducts& g, cudaStream_t st);

@@ -12,7 +12,12 @@
 //   Item item(p, i)                work item i of p.n_items; Item::steps is its number of K steps of 64
 //   load(p, it, kk, rank, dst, bar)   TMA loads of K step kk: exactly kFuStageBytes bytes
 //   a_mn(it), b_mn                 whether an operand lies with its rows (M or N) contiguous instead of K
-//   epilogue(p, it, rank, ew, lane, tmem)   ew = 0..7; `tmem` addresses this warp's lanes of the accumulator
+//   kSpan                          K steps after which the accumulator is handed to the epilogue: 0 = at the end of the item
+//   epilogue(p, it, r, half, tmem)    (kSpan == 0) row r of 256, columns 128 half .. of the accumulator; `tmem` addresses this warp's lanes
+//   finish(p, it, r, half, v)         (kSpan > 0) the same, with the 128 sums in registers
+// The tensor core cuts its fp32 additions off instead of rounding them, toward zero: over a chain of n instructions of 16 K each the sum
+// loses about n 2^-25 of itself.  That is nothing beside 16-bit results, nor for operands of few bits, whose sums are mostly exact; sums of full-width values for
+// 32-bit results are taken kSpan steps at a time and added with rounded additions in the epilogue's registers, while the next span runs.
 #pragma once
 
 #include "bdr_host.h"
@@ -113,14 +118,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
                     const uint32_t idesc = kPairInstrDesc | (a_mn ? kMnA : 0u) | (Job::b_mn ? kMnB : 0u);
                     const uint64_t a_step = a_mn ? 128 : 2;  // 16 K: two groups of eight K rows, or 32 bytes along a row
                     const uint64_t b_step = Job::b_mn ? 128 : 2;
-                    const int buf = tcount & 1;
-                    if (tcount >= 2) {  // the epilogues of both CTAs have drained this buffer
-                        ok = mbar_wait_cluster(&bars.tmem_empty[buf], ((tcount >> 1) - 1) & 1);
-                        if (!ok) break;
-                        tc_fence_after();
-                    }
-                    const uint32_t acc = tmem_base + (uint32_t)buf * 256u;
-                    for (int kk = 0; kk < item.steps; ++kk, ++it) {
+                    const int span = Job::kSpan ? Job::kSpan : item.steps;
+                    int buf = 0, left = 0;  // K steps that the current buffer still takes
+                    uint32_t acc = 0;
+                    for (int kk = 0; kk < item.steps; ++kk, ++it, --left) {
+                        if (left == 0) {
+                            if (kk > 0) { umma_commit2(&bars.tmem_full[buf]); ++tcount; }
+                            left = span;
+                            buf = tcount & 1;
+                            acc = tmem_base + (uint32_t)buf * 256u;
+                            if (tcount >= 2) {  // the epilogues of both CTAs have drained this buffer
+                                ok = mbar_wait_cluster(&bars.tmem_empty[buf], ((tcount >> 1) - 1) & 1);
+                                if (!ok) break;
+                                tc_fence_after();
+                            }
+                        }
                         const int stage = it % kStages;
                         ok = mbar_wait_cluster(&bars.full[stage], (it / kStages) & 1);
                         if (!ok) break;
@@ -129,7 +141,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
                         const uint64_t da = a_mn ? make_mn_desc(sa) : make_smem_desc(sa);
                         const uint64_t db = Job::b_mn ? make_mn_desc(sb) : make_smem_desc(sb);
 #pragma unroll
-                        for (int k = 0; k < kBK / 16; ++k) umma2_bf16(acc, da + k * a_step, db + k * b_step, idesc, (kk | k) != 0);
+                        for (int k = 0; k < kBK / 16; ++k) umma2_bf16(acc, da + k * a_step, db + k * b_step, idesc, left != span || k != 0);
                         umma_commit2(&bars.empty[stage]);
                     }
                     if (ok) umma_commit2(&bars.tmem_full[buf]);
@@ -156,16 +168,46 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
         int tcount = 0;
         for (int i = cluster_id; i < p.n_items; i += n_clusters, ++tcount) {
             const typename Job::Item item = Job::item(p, i);
-            const int buf = tcount & 1;
-            ok = ok && mbar_wait(&bars.tmem_full[buf], (tcount >> 1) & 1);
-            ok = __all_sync(0xFFFFFFFFu, ok);
-            if (!ok) break;
-            tc_fence_after();
-            // row of the 256: rank * 128 + (warp & 3) * 32 + lane; half of the columns: ew >> 2
-            Job::epilogue(p, item, (int)rank * kRows + (warp & 3) * 32 + lane, ew >> 2, tmem_base + my_lanes + (uint32_t)buf * 256u);
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(&bars.tmem_empty[buf], 0);
+            const int r = (int)rank * kRows + (warp & 3) * 32 + lane, half = ew >> 2;
+            auto next = [&](int buf) {  // waits for the next accumulator
+                ok = ok && mbar_wait(&bars.tmem_full[buf], (tcount >> 1) & 1);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                tc_fence_after();
+                return ok;
+            };
+            auto done = [&](int buf) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(&bars.tmem_empty[buf], 0);
+            };
+            if constexpr (Job::kSpan == 0) {
+                const int buf = tcount & 1;
+                if (!next(buf)) break;
+                Job::epilogue(p, item, r, half, tmem_base + my_lanes + (uint32_t)buf * 256u);
+                done(buf);
+            } else {
+                float v[4][32];
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[q][j] = 0.f;
+                for (int k0 = 0; k0 < item.steps; k0 += Job::kSpan) {
+                    if (k0 > 0) ++tcount;
+                    const int buf = tcount & 1;
+                    if (!next(buf)) break;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        uint32_t u[32];
+                        tmem_ld32(tmem_base + my_lanes + (uint32_t)(buf * 256 + half * 128 + 32 * q), u);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[q][j] += __uint_as_float(u[j]);
+                    }
+                    done(buf);
+                }
+                if (!ok) break;
+                Job::finish(p, item, r, half, v);
+                __syncwarp();
+            }
         }
         if (!ok) bars.failed = 1;
         tc_fence_before();

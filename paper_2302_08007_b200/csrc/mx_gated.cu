@@ -42,6 +42,7 @@ struct GatedJob {
     };
     struct Item { int steps, tm, tn; };
     static constexpr bool b_mn = false;
+    static constexpr int kSpan = 0;
     static __device__ __forceinline__ bool a_mn(const Item&) { return false; }
     static __device__ __forceinline__ Item item(const Params& p, int i) {
         Item it;

@@ -22,6 +22,7 @@ struct Target {
     int64_t ld_acc;
 };
 
+template <bool F32>
 struct GradJob {
     struct Params {
         CUtensorMap d_k;   // D, boxes of 64 (K) x 128 rows: A operand of dA
@@ -31,7 +32,8 @@ struct GradJob {
         int n_items, items_da, items_dw_seg;
         int tiles_m, tiles_n, tiles_k;
         int steps_n, steps_m;  // K steps over one segment's columns of D, over tokens
-        int segs, parts, f32;
+        int segs, parts;
+        const float* scale;
         int cols;              // K
         int* status;
     };
@@ -39,6 +41,7 @@ struct GradJob {
         int steps, tm, tk, seg;  // seg < 0: dA
     };
     static constexpr bool b_mn = true;
+    static constexpr int kSpan = F32 ? 4 : 0;  // 16 instructions in a chain
     static __device__ __forceinline__ bool a_mn(const Item& it) { return it.seg >= 0; }
     static __device__ __forceinline__ Item item(const Params& p, int i) {
         Item it;
@@ -59,45 +62,57 @@ struct GradJob {
         uint8_t* const b = dst + fused::kOperandBytes;
         constexpr int kChunk = fused::kOperandBytes / 2;
         if (it.seg < 0) {
-            const int z = kk / p.steps_n, k = (kk - z * p.steps_n) * kBK;  // z = part * segs + segment
-            const int seg = z % p.segs;
+            const int i = kk / p.steps_n, k = (kk - i * p.steps_n) * kBK;
+            const int z = p.segs * p.parts - 1 - i, seg = z % p.segs;  // z = part * segs + segment; the smallest part first
             tma_load_3d(dst, &p.d_k, k, row, z, bar);
             tma_load_3d(b, &p.w, col, k, seg, bar);
             tma_load_3d(b + kChunk, &p.w, col + 64, k, seg, bar);
         } else {
-            const int part = kk / p.steps_m, k = (kk - part * p.steps_m) * kBK, z = part * p.segs + it.seg;
+            const int i = kk / p.steps_m, k = (kk - i * p.steps_m) * kBK, z = (p.parts - 1 - i) * p.segs + it.seg;
             tma_load_3d(dst, &p.d_mn, row, k, z, bar);
             tma_load_3d(dst + kChunk, &p.d_mn, row + 64, k, z, bar);
             tma_load_3d(b, &p.a, col, k, 0, bar);
             tma_load_3d(b + kChunk, &p.a, col + 64, k, 0, bar);
         }
     }
-    static __device__ __forceinline__ void epilogue(const Params& p, const Item& it, int r, int half, uint32_t tmem) {
+    // 32 sums of a row, from column c of the 256
+    static __device__ __forceinline__ void put(const Params& p, const Item& it, int r, int c, float (&v)[32]) {
         const Target& t = it.seg < 0 ? p.da : p.dw;
-        const int row = it.tm * 256 + r;
+        const int row = it.tm * 256 + r, col = it.tk * 256 + c, n = min(32, p.cols - col);
+        if (row >= t.rows || n <= 0) return;
         const int64_t out_row = row + (it.seg > 0 ? (int64_t)it.seg * t.rows : 0);
+        if (t.read) {
+            float old[32];
+            fused::load_run(t.read + out_row * t.ld_acc, col, old, n, true, true);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] += old[j];
+        }
+        if (t.keep) {
+            fused::store_run(t.keep + out_row * t.ld_acc, col, v, n, true, true);
+        } else {
+            if (p.scale) {
+                const float s = *p.scale;
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[j] *= s;
+            }
+            fused::store_run(static_cast<char*>(t.out) + out_row * t.ld * (F32 ? 4 : 2), col, v, n, F32, t.vec);
+        }
+    }
+    static __device__ __forceinline__ void epilogue(const Params& p, const Item& it, int r, int half, uint32_t tmem) {
 #pragma unroll 1
-        for (int c = 0; c < 128; c += 32) {
+        for (int c = half * 128; c < half * 128 + 128; c += 32) {
             __syncwarp();
             uint32_t u[32];
-            tmem_ld32(tmem + (uint32_t)(half * 128 + c), u);
-            const int col = it.tk * 256 + half * 128 + c, n = min(32, p.cols - col);
-            if (row >= t.rows || n <= 0) continue;
+            tmem_ld32(tmem + (uint32_t)c, u);
             float v[32];
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(u[j]);
-            if (t.read) {
-                float old[32];
-                load_run(t.read + out_row * t.ld_acc, col, old, n, true, true);
-#pragma unroll
-                for (int j = 0; j < 32; ++j) v[j] += old[j];
-            }
-            if (t.keep) fused::store_run(t.keep + out_row * t.ld_acc, col, v, n, true, true);
-            else fused::store_run(static_cast<char*>(t.out) + out_row * t.ld * (p.f32 ? 4 : 2), col, v, n, p.f32, t.vec);
+            put(p, it, r, c, v);
         }
     }
-    static __device__ __forceinline__ void load_run(const float* row, int64_t at, float (&v)[32], int n, bool f32, bool vec) {
-        fused::load_run(row, at, v, n, f32, vec);
+    static __device__ __forceinline__ void finish(const Params& p, const Item& it, int r, int half, float (&v)[4][32]) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) put(p, it, r, half * 128 + 32 * q, v[q]);
     }
 };
 
@@ -165,15 +180,16 @@ int decode_lines(const bdr_planes_t& in, int m, int64_t rows, int64_t K, __nv_bf
     return BDR_ERR_UNSUPPORTED;
 }
 
-int launch_grad_products(const GradProducts& g, cudaStream_t st) {
-    GradJob::Params p = {};
+template <bool F32>
+static int launch_grads(const GradProducts& g, cudaStream_t st) {
+    typename GradJob<F32>::Params p = {};
     const int64_t z = (int64_t)g.segs * g.parts;
     if (!fused::make_map(&p.d_k, g.d, g.N, g.M, z, g.pitch_d, g.M * g.pitch_d, kRows) ||
         !fused::make_map(&p.d_mn, g.d, g.N, g.M, z, g.pitch_d, g.M * g.pitch_d, kBK) ||
         !fused::make_map(&p.w, g.w, g.K, g.N, g.segs, g.pitch_k, g.N * g.pitch_k, kBK) ||
         !fused::make_map(&p.a, g.a, g.K, g.M, 1, g.pitch_k, g.M * g.pitch_k, kBK))
         return BDR_ERR_CUDA;
-    const int width = g.f32 ? 4 : 2;
+    const int width = F32 ? 4 : 2;
     p.da = {g.da, g.ld_da, (int)g.M, fused::rows_aligned(g.da, g.ld_da, width), g.first ? nullptr : g.acc, g.last ? nullptr : g.acc, g.ld_acc};
     p.dw = {g.dw, g.ld_dw, (int)g.N, fused::rows_aligned(g.dw, g.ld_dw, width), nullptr, nullptr, 0};
     p.tiles_m = (int)((g.M + 255) / 256);
@@ -181,7 +197,7 @@ int launch_grad_products(const GradProducts& g, cudaStream_t st) {
     p.tiles_k = (int)((g.K + 255) / 256);
     p.steps_n = (int)((g.N + kBK - 1) / kBK);
     p.steps_m = (int)((g.M + kBK - 1) / kBK);
-    p.segs = g.segs; p.parts = g.parts; p.f32 = g.f32;
+    p.segs = g.segs; p.parts = g.parts; p.scale = g.scale;
     p.cols = (int)g.K;
     p.items_da = g.da ? p.tiles_m * p.tiles_k : 0;
     p.items_dw_seg = p.tiles_n * p.tiles_k;
@@ -189,8 +205,10 @@ int launch_grad_products(const GradProducts& g, cudaStream_t st) {
     p.status = device_status_word();
     if (!p.status) return BDR_ERR_CUDA;
     if (p.n_items == 0) return BDR_OK;
-    return fused::launch<GradJob>(p, st);
+    return fused::launch<GradJob<F32>>(p, st);
 }
+
+int launch_grad_products(const GradProducts& g, cudaStream_t st) { return g.f32 ? launch_grads<true>(g, st) : launch_grads<false>(g, st); }
 
 int check_fused_operands(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bdr_config_t* cfg_w, const bdr_planes_t* w, int64_t K) {
     int rc = check_table2_config(cfg_a);
