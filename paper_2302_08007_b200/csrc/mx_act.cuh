@@ -26,7 +26,8 @@ __device__ __forceinline__ float of(float g) {
 template <int ACT>
 __device__ __forceinline__ void both(float g, float& y, float& slope) {
     if constexpr (ACT == MX_ACT_SILU) {
-        const float p = sigmoid(g), q = sigmoid(-g);
+        const float t = expf(-fabsf(g)), r = __fdividef(1.f, 1.f + t), s = t * r;  // the sigmoid of |g| and what it lacks to one
+        const float p = g < 0.f ? s : r, q = g < 0.f ? r : s;
         y = g * p;
         slope = p + y * q;
     } else if constexpr (ACT == MX_ACT_GELU) {

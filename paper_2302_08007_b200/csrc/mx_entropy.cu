@@ -14,6 +14,7 @@ namespace bdr {
 namespace {
 
 using fused::kRows;
+using fused::Rows;
 
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -28,16 +29,15 @@ template <bool GRAD>
 struct EntropyJob {
     struct Params {
         CUtensorMap a, w;         // bf16 [M][K]; [columns of this piece][K]
-        int n_items, tiles_m, tiles_n, band_rows, steps;
+        int n_items, bn, tiles_m, tiles_n, band_rows, steps;
         int M, cols;
         int64_t col0;             // the piece's first column
         const int64_t* targets;
-        float2* parts;            // [columns / 128][M]: maximum, sum of exp(l - maximum)
+        float2* parts;            // [columns / (bn / 2)][M]: maximum, sum of exp(l - maximum)
         float* hit;               // [M]: the target's logit
         const float *lse, *dloss;
         const float* largest;     // of |dloss|, among the rows that count
-        __nv_bfloat16* d;         // [n_parts][M][pitch_d]
-        int64_t pitch_d;
+        Rows d;                   // [n_parts][M][piece]
         int64_t vocab;
         int n_parts;
         int* status;
@@ -54,21 +54,21 @@ struct EntropyJob {
     }
     static __device__ __forceinline__ void load(const Params& p, const Item& it, int kk, int rank, uint8_t* dst, uint64_t* bar) {
         tma_load_3d(dst, &p.a, kk * kBK, (it.tm * 2 + rank) * kRows, 0, bar);
-        tma_load_3d(dst + fused::kOperandBytes, &p.w, kk * kBK, (it.tn * 2 + rank) * kRows, 0, bar);
+        tma_load_3d(dst + fused::kOperandBytes, &p.w, kk * kBK, it.tn * p.bn + rank * (p.bn >> 1), 0, bar);
     }
-    static __device__ __forceinline__ void epilogue(const Params& p, const Item& it, int r, int half, uint32_t tmem) {
-        const int64_t row = (int64_t)it.tm * 256 + r;
-        const int first = it.tn * 256 + half * 128;  // column in the piece
+    static __device__ __forceinline__ void epilogue(const Params& p, const Item& it, const fused::Epi& e) {
+        const int64_t row0 = (int64_t)it.tm * 256 + e.r0, row = row0 + e.lane;
+        const int width = p.bn >> 1, first = it.tn * p.bn + e.half * width;  // columns in the piece
         const bool live = row < p.M;
         const int64_t target = live ? p.targets[row] : -1;
-        const int64_t at = target - p.col0 - first;  // column of the target among these 128
+        const int64_t at = target - p.col0 - first;  // column of the target among these
         if constexpr (!GRAD) {
             float top = -INFINITY, sum = 0.f;
 #pragma unroll 1
-            for (int c = 0; c < 128; c += 32) {
+            for (int c = 0; c < width; c += 32) {
                 __syncwarp();
                 uint32_t u[32];
-                tmem_ld32(tmem + (uint32_t)(half * 128 + c), u);
+                tmem_ld32(e.tmem + (uint32_t)(e.half * width + c), u);
                 float v[32];
                 const int n = p.cols - first - c;
 #pragma unroll
@@ -90,24 +90,24 @@ struct EntropyJob {
                 top = m;
                 sum = s;
             }
-            if (live && first < p.cols) p.parts[((p.col0 + first) >> 7) * p.M + row] = make_float2(top, sum);
+            if (live && first < p.cols) p.parts[(p.col0 + first) / width * p.M + row] = make_float2(top, sum);
         } else {
             const float lse = live ? p.lse[row] : 0.f, scale = live ? p.dloss[row] / *p.largest : 0.f;
             const bool counts = target >= 0 && target < p.vocab;
+            const int rows = (int)min((int64_t)32, p.M - row0);
 #pragma unroll 1
-            for (int c = 0; c < 128; c += 32) {
+            for (int c = 0; c < width; c += 32) {
                 __syncwarp();
                 uint32_t u[32];
-                tmem_ld32(tmem + (uint32_t)(half * 128 + c), u);
-                const int n = min(32, p.cols - first - c);
-                if (!live || n <= 0) continue;
+                tmem_ld32(e.tmem + (uint32_t)(e.half * width + c), u);
+                if (rows <= 0 || first + c >= p.cols) continue;  // (the same for the whole warp)
                 float v[32];
 #pragma unroll
                 for (int j = 0; j < 32; ++j) {
-                    const float e = exp2_of((__uint_as_float(u[j]) - lse) * kLog2e) - (at - c == j ? 1.f : 0.f);
-                    v[j] = counts ? scale * e : 0.f;
+                    const float x = exp2_of((__uint_as_float(u[j]) - lse) * kLog2e) - (at - c == j ? 1.f : 0.f);
+                    v[j] = counts ? scale * x : 0.f;
                 }
-                fused::store_parts(p.d + row * p.pitch_d + first + c, p.M * p.pitch_d, p.n_parts, v, n);
+                fused::store_parts(e, p.d, p.M, row0, first + c, rows, p.n_parts, v);
             }
         }
     }
@@ -116,6 +116,7 @@ struct EntropyJob {
 // Joins a row's maxima and sums: 32 rows per block, their pieces shared out to 32 warps.
 __global__ void __launch_bounds__(1024) entropy_join_kernel(const float2* parts, int n_parts, int64_t M, const float* hit, const int64_t* targets,
                                                             int64_t V, float* loss, float* lse, int* status) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // launched as a programmatic dependent of the product
     __shared__ float2 shared[32][33];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t row = (int64_t)blockIdx.x * 32 + lane;
@@ -174,12 +175,12 @@ struct EntropySpace {
         a = 0;
         w = a + round_up(M * pitch_k * 2, 256);
         parts = w + round_up(std::min(piece, V) * pitch_k * 2, 256);
-        hit = parts + round_up((V + 127) / 128 * M * 8, 256);
+        hit = parts + round_up((V + 31) / 32 * M * 8, 256);
         bytes = hit + round_up(M * 4, 256);
     }
 };
 struct EntropyGradSpace {
-    int64_t pitch_k, piece, a, w, d, acc, largest, bytes;
+    int64_t pitch_k, piece, a, w, d, acc, largest, sums, bytes;
     EntropyGradSpace(int64_t M, int64_t V, int64_t K, int n_parts) {
         pitch_k = line_pitch(K);
         piece = piece_columns(V, std::min(kMostWeights / (pitch_k * 2), kMostD / (std::max<int64_t>(M, 1) * 2 * n_parts)));
@@ -188,7 +189,8 @@ struct EntropyGradSpace {
         d = w + round_up(std::min(piece, V) * pitch_k * 2, 256);
         acc = d + round_up(n_parts * M * piece * 2, 256);
         largest = acc + (piece < V ? round_up(M * pitch_k * 4, 256) : 0);
-        bytes = largest + 256;
+        sums = largest + 256;
+        bytes = sums + grad_sums_bytes(M, std::min(piece, V), K, 1);
     }
 };
 
@@ -196,13 +198,14 @@ constexpr int64_t kMost = 1ll << 30;
 
 template <class Params>
 int set_piece(Params& p, int64_t M, int64_t K, int64_t col0, int64_t cols, int64_t pitch_k, const uint8_t* a, const uint8_t* w) {
-    if (!fused::make_map(&p.a, a, K, M, 1, pitch_k, M * pitch_k, kRows) || !fused::make_map(&p.w, w, K, cols, 1, pitch_k, cols * pitch_k, kRows))
-        return BDR_ERR_CUDA;
     p.tiles_m = (int)((M + 255) / 256);
-    p.tiles_n = (int)((cols + 255) / 256);
+    p.steps = (int)((K + kBK - 1) / kBK);
+    if (col0 == 0) p.bn = fused::pick_bn(p.tiles_m, cols, 1, p.steps, sm_count() / 2);  // (the last piece keeps it)
+    p.tiles_n = (int)((cols + p.bn - 1) / p.bn);
+    if (!fused::make_map(&p.a, a, K, M, 1, pitch_k, M * pitch_k, kRows) || !fused::make_map(&p.w, w, K, cols, 1, pitch_k, cols * pitch_k, p.bn / 2))
+        return BDR_ERR_CUDA;
     p.n_items = p.tiles_m * p.tiles_n;
     p.band_rows = gemm_band_rows((M + cols) * K * 2);
-    p.steps = (int)((K + kBK - 1) / kBK);
     p.M = (int)M;
     p.cols = (int)cols;
     p.col0 = col0;
@@ -256,15 +259,16 @@ int mx_cross_entropy(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bdr
     p.hit = reinterpret_cast<float*>(ws + s.hit);
     p.status = device_status_word();
     if (!p.status) return BDR_ERR_CUDA;
-    if ((rc = decode_lines(*a, cfg_a->m, M, K, reinterpret_cast<__nv_bfloat16*>(ws + s.a), s.pitch_k, st))) return rc;
+    __nv_bfloat16 *const wa = reinterpret_cast<__nv_bfloat16*>(ws + s.a), *const ww = reinterpret_cast<__nv_bfloat16*>(ws + s.w);
     for (int64_t v = 0; v < V; v += s.piece) {
         const int64_t cols = std::min(s.piece, V - v);
-        if ((rc = decode_lines(lines_from(*w, v), cfg_w->m, cols, K, reinterpret_cast<__nv_bfloat16*>(ws + s.w), s.pitch_k, st))) return rc;
+        if ((rc = decode_pair(*a, cfg_a->m, v == 0 ? M : 0, wa, lines_from(*w, v), cfg_w->m, cols, ww, K, s.pitch_k, st))) return rc;
         if ((rc = set_piece(p, M, K, v, cols, s.pitch_k, ws + s.a, ws + s.w))) return rc;
         if ((rc = fused::launch<EntropyJob<false>>(p, st))) return rc;
     }
-    entropy_join_kernel<<<(unsigned)((M + 31) / 32), 1024, 0, st>>>(p.parts, (int)((V + 127) / 128), M, p.hit, targets, V, loss, lse, p.status);
-    return cudaGetLastError() == cudaSuccess ? BDR_OK : BDR_ERR_CUDA;
+    const int n_parts = (int)((V + p.bn / 2 - 1) / (p.bn / 2));
+    return launch_dependent(entropy_join_kernel, dim3((unsigned)((M + 31) / 32)), dim3(1024), st, (const float2*)p.parts, n_parts, M, (const float*)p.hit, targets,
+                            V, loss, lse, p.status);
 }
 
 int64_t mx_cross_entropy_bwd_workspace_bytes(int64_t M, int64_t V, int64_t K, bdr_dtype_t dt) {
@@ -304,13 +308,12 @@ int mx_cross_entropy_bwd(const bdr_config_t* cfg_a, const bdr_planes_t* a, const
     p.vocab = V;
     p.lse = lse;
     p.dloss = dloss;
-    p.d = reinterpret_cast<__nv_bfloat16*>(ws + s.d);
-    p.pitch_d = s.piece;
+    p.d = fused::make_rows(ws + s.d, s.piece, false);
     p.n_parts = n_parts;
     p.status = device_status_word();
     if (!p.status) return BDR_ERR_CUDA;
     GradProducts g = {};
-    g.d = p.d;
+    g.d = reinterpret_cast<__nv_bfloat16*>(ws + s.d);
     g.a = reinterpret_cast<__nv_bfloat16*>(ws + s.a);
     g.w = reinterpret_cast<__nv_bfloat16*>(ws + s.w);
     g.M = M; g.K = K; g.pitch_d = s.piece; g.pitch_k = s.pitch_k;
@@ -319,13 +322,14 @@ int mx_cross_entropy_bwd(const bdr_config_t* cfg_a, const bdr_planes_t* a, const
     g.f32 = dt == BDR_F32;
     g.acc = s.piece < V ? reinterpret_cast<float*>(ws + s.acc) : nullptr;
     g.ld_acc = s.pitch_k;
+    g.sums = reinterpret_cast<float*>(ws + s.sums);
     g.scale = p.largest = reinterpret_cast<const float*>(ws + s.largest);
     entropy_scale_kernel<<<1, 1024, 0, st>>>(dloss, targets, M, V, reinterpret_cast<float*>(ws + s.largest));
     if (cudaGetLastError() != cudaSuccess) return BDR_ERR_CUDA;
-    if ((rc = decode_lines(*a, cfg_a->m, M, K, reinterpret_cast<__nv_bfloat16*>(ws + s.a), s.pitch_k, st))) return rc;
+    __nv_bfloat16 *const wa = reinterpret_cast<__nv_bfloat16*>(ws + s.a), *const ww = reinterpret_cast<__nv_bfloat16*>(ws + s.w);
     for (int64_t v = 0; v < V; v += s.piece) {
         const int64_t cols = std::min(s.piece, V - v);
-        if ((rc = decode_lines(lines_from(*w, v), cfg_w->m, cols, K, reinterpret_cast<__nv_bfloat16*>(ws + s.w), s.pitch_k, st))) return rc;
+        if ((rc = decode_pair(*a, cfg_a->m, v == 0 ? M : 0, wa, lines_from(*w, v), cfg_w->m, cols, ww, K, s.pitch_k, st))) return rc;
         if ((rc = set_piece(p, M, K, v, cols, s.pitch_k, ws + s.a, ws + s.w))) return rc;
         if ((rc = fused::launch<EntropyJob<true>>(p, st))) return rc;
         g.N = cols;

@@ -17,8 +17,27 @@ constexpr int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * t
 // Pitch (elements) of lines of K decoded elements: whole items of the decode kernel.
 constexpr int64_t line_pitch(int64_t K) { return round_up(K, 32); }
 
-// Packed lines (Table II formats, m magnitude bits) -> bf16 [rows, pitch]; what lies behind K in a row is unspecified.
-int decode_lines(const bdr_planes_t& in, int m, int64_t rows, int64_t K, __nv_bfloat16* out, int64_t pitch, cudaStream_t st);
+// Packed lines of K elements (Table II formats, m magnitude bits) of two operands -> bf16 [rows, pitch]; what lies behind K in a row is
+// unspecified.
+int decode_pair(const bdr_planes_t& a, int m_a, int64_t rows_a, __nv_bfloat16* out_a, const bdr_planes_t& w, int m_w, int64_t rows_w, __nv_bfloat16* out_w,
+                int64_t K, int64_t pitch, cudaStream_t st);
+
+// Launches a kernel without shared memory behind another in the stream so that it is set up while that one drains; the kernel waits for it
+// (griddepcontrol.wait) before it touches memory.
+template <typename... P, typename... A>
+int launch_dependent(void (*kern)(P...), dim3 grid, dim3 block, cudaStream_t st, A... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, P(args)...);
+    return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? BDR_OK : BDR_ERR_CUDA;
+}
 
 // The gradient products.  D is bf16 [parts * segs][M][pitch_d] of which N columns count: D = sum over parts, segment s belongs to
 // the weight lines w + s * N * pitch_k.  dA[M, K] (+)= sum_s D_s W_s, dW[s * N + n, K] = D_s^T A.  W is bf16 [segs * N, pitch_k],
@@ -32,9 +51,11 @@ struct GradProducts {
     bool f32;               // type of da and dw (else bf16)
     float* acc;             // fp32 [M, ld_acc] running sum of dA over several calls; NULL: this call is the only one
     int64_t ld_acc;
+    float* sums;            // grad_sums_bytes(M, N, K, segs) bytes
     const float* scale;     // device: factor of both gradients; NULL: 1
     bool first, last;       // of those calls: the first does not read acc, the last writes da
 };
+int64_t grad_sums_bytes(int64_t M, int64_t N, int64_t K, int segs);
 int launch_grad_products(const GradProducts& g, cudaStream_t st);
 
 // What the operators accept of two packed operands A [M, K] and W [lines, K] (host).

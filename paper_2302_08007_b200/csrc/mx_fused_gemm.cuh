@@ -1,23 +1,24 @@
-// The product kernel behind the fused operators: a persistent, TMA-fed tcgen05 kernel over 256 x 256 accumulators, one cluster of
-// two CTAs per SM pair, whose operands and epilogue come from a Job.  The pipeline is that of the dense phase of mx_gemm_ws:
-//   warp 0   : one lane issues the TMA loads of this CTA's 128 rows of A and its 128 columns of B (64 K elements, 32 KB) into a ring
-//   warp 1   : leader CTA: one lane issues tcgen05.mma.cta_group::2 (M 256, N 256, K 16) into one of two accumulator buffers;
-//              peer CTA: relays "my stage is full" to the leader's barrier
-//   warps 2-9: epilogue of this CTA's 128 x 256 block of the item, overlapping the next item's main loop
+// The product kernel behind the fused operators: a persistent, TMA-fed tcgen05 kernel over 256 x (64, 128 or 256) accumulators, one
+// cluster of two CTAs per SM pair, whose operands and epilogue come from a Job.  The pipeline is that of the dense phase of mx_gemm_ws:
+//   warp 0   : one lane issues the TMA loads of this CTA's 128 rows of A and its half of B's columns (64 K elements) into a ring
+//   warp 1   : leader CTA: one lane issues tcgen05.mma.cta_group::2 (M 256, N the accumulator's columns, K 16) into one of two accumulator
+//              buffers;  peer CTA: relays "my stage is full" to the leader's barrier
+//   warps 2-9: epilogue of this CTA's 128 rows of the item, overlapping the next item's main loop
 // Ragged sizes cost nothing in the main loop: the tensor maps carry the true extents, what lies beyond them arrives as zeros, and the
 // epilogues mask rows and columns.  Every wait is bounded; one that runs out sets the status word and the role leaves its loop.
 //
 // A Job has
-//   Params                         kernel argument (tensor maps and sizes)
+//   Params                         kernel argument: tensor maps, sizes, n_items, bn (the accumulator's columns), status
 //   Item item(p, i)                work item i of p.n_items; Item::steps is its number of K steps of 64
-//   load(p, it, kk, rank, dst, bar)   TMA loads of K step kk: exactly kFuStageBytes bytes
+//   load(p, it, kk, rank, dst, bar)   TMA loads of K step kk: A at dst, B kOperandBytes behind it, 16384 + 64 bn bytes in all
 //   a_mn(it), b_mn                 whether an operand lies with its rows (M or N) contiguous instead of K
 //   kSpan                          K steps after which the accumulator is handed to the epilogue: 0 = at the end of the item
-//   epilogue(p, it, r, half, tmem)    (kSpan == 0) row r of 256, columns 128 half .. of the accumulator; `tmem` addresses this warp's lanes
-//   finish(p, it, r, half, v)         (kSpan > 0) the same, with the 128 sums in registers
+//   epilogue(p, it, e)             (kSpan == 0) reads the accumulator through e.tmem
+//   finish(p, it, e, v)            (kSpan > 0, bn == 256) the same, with the 128 sums of a thread's row and half of the columns in registers
 // The tensor core cuts its fp32 additions off instead of rounding them, toward zero: over a chain of n instructions of 16 K each the sum
-// loses about n 2^-25 of itself.  That is nothing beside 16-bit results, nor for operands of few bits, whose sums are mostly exact; sums of full-width values for
-// 32-bit results are taken kSpan steps at a time and added with rounded additions in the epilogue's registers, while the next span runs.
+// loses about n 2^-25 of itself.  That is nothing beside 16-bit results, nor for operands of few bits, whose sums are mostly exact; sums
+// of full-width values for 32-bit results are taken kSpan steps at a time and added with rounded additions in the epilogue's registers,
+// while the next span runs.
 #pragma once
 
 #include "bdr_host.h"
@@ -33,7 +34,8 @@ constexpr int kOperandBytes = kRows * kBK * 2;      // 16 KB
 constexpr int kStageBytes = 2 * kOperandBytes;
 constexpr int kEpiWarps = 8;
 constexpr int kThreads = (2 + kEpiWarps) * 32;
-constexpr size_t kSmem = (size_t)kStages * kStageBytes + 1024 /*bookkeeping*/ + 1024 /*alignment*/;
+constexpr int kTileBytes = 32 * 64;                 // of an epilogue warp, see store_tile
+constexpr size_t kSmem = (size_t)kStages * kStageBytes + kEpiWarps * kTileBytes + 1024 /*bookkeeping*/ + 1024 /*alignment*/;
 
 struct Bars {
     uint64_t full[kStages], full_local[kStages], empty[kStages], tmem_full[2], tmem_empty[2];
@@ -52,13 +54,23 @@ __device__ __forceinline__ uint64_t make_mn_desc(uint32_t smem_addr) {
     d |= (uint64_t)2 << 61;
     return d;
 }
-constexpr uint32_t kMnA = 1u << 15, kMnB = 1u << 16;  // instruction descriptor: the operand's rows are contiguous
+// Instruction descriptor: D = fp32, A = B = bf16, M = 256, N = bn; bits 15 and 16: A's, B's rows are contiguous.
+constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(256 >> 4) << 24), kMnA = 1u << 15, kMnB = 1u << 16;
+
+// What an epilogue warp works on.
+struct Epi {
+    uint32_t tmem;   // its 32 lanes of the accumulator, column 0
+    int r0;          // their first row of the item's 256
+    int half, lane;  // two warps share the lanes: half of the columns each
+    uint32_t tile;   // shared-memory address of the warp's own 2 KB
+};
 
 template <class Job>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_gemm_kernel(const __grid_constant__ typename Job::Params p) {
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t* stages = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-    Bars& bars = *reinterpret_cast<Bars*>(stages + kStages * kStageBytes);
+    uint8_t* const tiles = stages + kStages * kStageBytes;
+    Bars& bars = *reinterpret_cast<Bars*>(tiles + kEpiWarps * kTileBytes);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();
     const int cluster_id = blockIdx.x >> 1, n_clusters = gridDim.x >> 1;
@@ -83,7 +95,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
     tc_fence_after();
     const uint32_t tmem_base = bars.tmem_base;
 
-    // nothing above touched global memory: launched as a programmatic dependent, it overlaps the tail of the kernel before
+    // nothing above touched global memory: launched as a programmatic dependent, it overlaps the tail of the kernel before; and the kernel
+    // behind may be set up already
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
     if (warp == 0) {
@@ -99,11 +113,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
                         ok = mbar_wait(&bars.empty[stage], ((it / kStages) - 1) & 1);
                         if (!ok) break;
                     }
-                    mbar_expect_tx(&my_full[stage], kStageBytes);
+                    mbar_expect_tx(&my_full[stage], kOperandBytes + 64 * p.bn);
                     Job::load(p, item, kk, (int)rank, stages + stage * kStageBytes, &my_full[stage]);
                 }
             }
-            if (!ok) bars.failed = 1;
+            if (!ok) {
+                bars.failed = 1;
+                // the copies still on their way: one more bounded wait for each
+                for (uint32_t j = it < kStages ? 0 : it - kStages; j < it; ++j) mbar_wait(&my_full[j % kStages], (j / kStages) & 1);
+            }
         }
         __syncwarp();
     } else if (warp == 1) {
@@ -115,7 +133,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
                 for (int i = cluster_id; i < p.n_items && ok; i += n_clusters, ++tcount) {
                     const typename Job::Item item = Job::item(p, i);
                     const bool a_mn = Job::a_mn(item);
-                    const uint32_t idesc = kPairInstrDesc | (a_mn ? kMnA : 0u) | (Job::b_mn ? kMnB : 0u);
+                    const uint32_t idesc = kIdesc | ((uint32_t)(p.bn >> 3) << 17) | (a_mn ? kMnA : 0u) | (Job::b_mn ? kMnB : 0u);
                     const uint64_t a_step = a_mn ? 128 : 2;  // 16 K: two groups of eight K rows, or 32 bytes along a row
                     const uint64_t b_step = Job::b_mn ? 128 : 2;
                     const int span = Job::kSpan ? Job::kSpan : item.steps;
@@ -168,7 +186,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
         int tcount = 0;
         for (int i = cluster_id; i < p.n_items; i += n_clusters, ++tcount) {
             const typename Job::Item item = Job::item(p, i);
-            const int r = (int)rank * kRows + (warp & 3) * 32 + lane, half = ew >> 2;
+            Epi e;
+            e.r0 = (int)rank * kRows + (warp & 3) * 32;
+            e.half = ew >> 2;
+            e.lane = lane;
+            e.tile = smem_u32(tiles + ew * kTileBytes);
             auto next = [&](int buf) {  // waits for the next accumulator
                 ok = ok && mbar_wait(&bars.tmem_full[buf], (tcount >> 1) & 1);
                 ok = __all_sync(0xFFFFFFFFu, ok);
@@ -183,7 +205,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
             if constexpr (Job::kSpan == 0) {
                 const int buf = tcount & 1;
                 if (!next(buf)) break;
-                Job::epilogue(p, item, r, half, tmem_base + my_lanes + (uint32_t)buf * 256u);
+                e.tmem = tmem_base + my_lanes + (uint32_t)buf * 256u;
+                Job::epilogue(p, item, e);
                 done(buf);
             } else {
                 float v[4][32];
@@ -198,15 +221,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         uint32_t u[32];
-                        tmem_ld32(tmem_base + my_lanes + (uint32_t)(buf * 256 + half * 128 + 32 * q), u);
+                        tmem_ld32(tmem_base + my_lanes + (uint32_t)(buf * 256 + e.half * 128 + 32 * q), u);
 #pragma unroll
                         for (int j = 0; j < 32; ++j) v[q][j] += __uint_as_float(u[j]);
                     }
                     done(buf);
                 }
                 if (!ok) break;
-                Job::finish(p, item, r, half, v);
-                __syncwarp();
+                Job::finish(p, item, e, v);
             }
         }
         if (!ok) bars.failed = 1;
@@ -262,79 +284,188 @@ __device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// n (at most 32) values of a row, from column `at` of row pointer `row`, rounded once to the type; vec: 16-byte stores are possible
-__device__ __forceinline__ void store_run(void* row, int64_t at, const float (&v)[32], int n, bool f32, bool vec) {
-    if (f32) {
-        float* to = static_cast<float*>(row) + at;
-        if (vec && n == 32) {
+// A row-major tensor as an epilogue sees it.  align: 16, 4 or 2, the bytes that every row start (and so every multiple of 32 columns) is
+// aligned to.
+struct Rows {
+    void* p;
+    int64_t ld;  // bytes
+    int f32, align;
+    __device__ __forceinline__ char* at(int64_t row, int64_t col) const { return static_cast<char*>(p) + row * ld + col * (f32 ? 4 : 2); }
+};
+inline Rows make_rows(const void* p, int64_t ld, bool f32) {  // ld in elements (host)
+    const int64_t bytes = ld * (f32 ? 4 : 2);
+    const uint64_t both = (uintptr_t)p | (uint64_t)bytes;
+    return {const_cast<void*>(p), bytes, f32, both % 16 == 0 ? 16 : (both % 4 == 0 ? 4 : 2)};
+}
+
+// Tiles of 32 rows x 32 columns between the lanes of a warp (a lane holds a row, as tensor memory gives it) and global memory.  They pass
+// through 64 bytes per row of shared memory, the 16-byte pieces of rows 2i and 2i + 1 exchanged by i so that neither side meets in a bank, and
+// so that a warp's accesses to global memory run along rows, whatever the rows' alignment.
+__device__ __forceinline__ uint32_t tile_at(uint32_t tile, int row, int piece) { return tile + row * 64 + ((piece ^ ((row >> 1) & 3)) << 4); }
+__device__ __forceinline__ void sts128(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t addr) {
+    uint32_t v;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ void sts32(uint32_t addr, uint32_t v) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
+__device__ __forceinline__ uint16_t lds16(uint32_t addr) {
+    uint16_t v;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ void sts16(uint32_t addr, uint16_t v) { asm volatile("st.shared.u16 [%0], %1;" ::"r"(addr), "h"(v) : "memory"); }
+
+// shared -> global: `rows` rows of n elements (16 fp32 or 32 bf16 at most) to `to`, ld bytes apart
+template <bool F32>
+__device__ __forceinline__ void flush_tile(const Epi& e, char* to, int64_t ld, int rows, int n, int align) {
+    __syncwarp();
+    if (align == 16 && n == (F32 ? 16 : 32)) {
 #pragma unroll
-            for (int q = 0; q < 8; ++q) *reinterpret_cast<float4*>(to + 4 * q) = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-                if (j < n) to[j] = v[j];
+        for (int i = 0; i < 4; ++i) {
+            const int row = 8 * i + (e.lane >> 2);
+            const uint4 v = lds128(tile_at(e.tile, row, e.lane & 3));
+            if (row < rows) *reinterpret_cast<uint4*>(to + row * ld + 16 * (e.lane & 3)) = v;
+        }
+    } else if (F32 || align >= 4) {
+        const int w = e.lane & 15, have = F32 ? n - w : n - 2 * w;
+#pragma unroll 4
+        for (int i = 0; i < 16; ++i) {
+            const int row = 2 * i + (e.lane >> 4);
+            const uint32_t v = lds32(tile_at(e.tile, row, w >> 2) + 4 * (w & 3));
+            char* const at = to + row * ld + 4 * w;
+            if (row >= rows || have <= 0) continue;
+            if (F32 || have >= 2) *reinterpret_cast<uint32_t*>(at) = v;
+            else *reinterpret_cast<uint16_t*>(at) = (uint16_t)v;
         }
     } else {
-        __nv_bfloat16* to = static_cast<__nv_bfloat16*>(row) + at;
-        if (vec && n == 32) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                *reinterpret_cast<uint4*>(to + 8 * q) = make_uint4(bf16x2(v[8 * q], v[8 * q + 1]), bf16x2(v[8 * q + 2], v[8 * q + 3]),
-                                                                   bf16x2(v[8 * q + 4], v[8 * q + 5]), bf16x2(v[8 * q + 6], v[8 * q + 7]));
-        } else {
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-                if (j < n) to[j] = __float2bfloat16_rn(v[j]);
+#pragma unroll 4
+        for (int row = 0; row < 32; ++row) {
+            const uint16_t v = lds16(tile_at(e.tile, row, e.lane >> 3) + 2 * (e.lane & 7));
+            if (row < rows && e.lane < n) *reinterpret_cast<uint16_t*>(to + row * ld + 2 * e.lane) = v;
         }
     }
+    __syncwarp();
 }
-__device__ __forceinline__ void load_run(const void* row, int64_t at, float (&v)[32], int n, bool f32, bool vec) {
-    if (f32) {
-        const float* from = static_cast<const float*>(row) + at;
-        if (vec && n == 32) {
+// global -> shared, zeros where there is nothing
+template <bool F32>
+__device__ __forceinline__ void fetch_tile(const Epi& e, const char* from, int64_t ld, int rows, int n, int align) {
+    __syncwarp();
+    if (align == 16 && n == (F32 ? 16 : 32)) {
 #pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                const float4 x = *reinterpret_cast<const float4*>(from + 4 * q);
-                v[4 * q] = x.x; v[4 * q + 1] = x.y; v[4 * q + 2] = x.z; v[4 * q + 3] = x.w;
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = j < n ? from[j] : 0.f;
+        for (int i = 0; i < 4; ++i) {
+            const int row = 8 * i + (e.lane >> 2);
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (row < rows) v = *reinterpret_cast<const uint4*>(from + row * ld + 16 * (e.lane & 3));
+            sts128(tile_at(e.tile, row, e.lane & 3), v.x, v.y, v.z, v.w);
+        }
+    } else if (F32 || align >= 4) {
+        const int w = e.lane & 15, have = F32 ? n - w : n - 2 * w;
+#pragma unroll 8
+        for (int i = 0; i < 16; ++i) {
+            const int row = 2 * i + (e.lane >> 4);
+            const char* const at = from + row * ld + 4 * w;
+            uint32_t v = 0;
+            if (row < rows && have > 0) v = F32 || have >= 2 ? *reinterpret_cast<const uint32_t*>(at) : *reinterpret_cast<const uint16_t*>(at);
+            sts32(tile_at(e.tile, row, w >> 2) + 4 * (w & 3), v);
         }
     } else {
-        const __nv_bfloat16* from = static_cast<const __nv_bfloat16*>(row) + at;
-        if (vec && n == 32) {
+#pragma unroll 8
+        for (int row = 0; row < 32; ++row) {
+            uint16_t v = 0;
+            if (row < rows && e.lane < n) v = *reinterpret_cast<const uint16_t*>(from + row * ld + 2 * e.lane);
+            sts16(tile_at(e.tile, row, e.lane >> 3) + 2 * (e.lane & 7), v);
+        }
+    }
+    __syncwarp();
+}
+
+// The warp's 32 x 32 values v to t at (row, col), rounded once to t's type; rows, n: how many of them are there.  All lanes take part.
+__device__ __forceinline__ void store_tile(const Epi& e, const Rows& t, int64_t row, int64_t col, int rows, int n, const float (&v)[32]) {
+    if (rows <= 0 || n <= 0) return;
+    char* const to = t.at(row, col);
+    if (t.f32) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if (n <= 16 * h) break;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const uint4 x = *reinterpret_cast<const uint4*>(from + 8 * q);
-                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    v[8 * q + 2 * e] = __uint_as_float(w[e] << 16);
-                    v[8 * q + 2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
-                }
+                const int j = 16 * h + 4 * q;
+                sts128(tile_at(e.tile, e.lane, q), __float_as_uint(v[j]), __float_as_uint(v[j + 1]), __float_as_uint(v[j + 2]), __float_as_uint(v[j + 3]));
             }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = j < n ? __bfloat162float(from[j]) : 0.f;
+            flush_tile<true>(e, to + 64 * h, t.ld, rows, min(16, n - 16 * h), t.align);
         }
+    } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            sts128(tile_at(e.tile, e.lane, q), bf16x2(v[8 * q], v[8 * q + 1]), bf16x2(v[8 * q + 2], v[8 * q + 3]), bf16x2(v[8 * q + 4], v[8 * q + 5]),
+                   bf16x2(v[8 * q + 6], v[8 * q + 7]));
+        flush_tile<false>(e, to, t.ld, rows, n, t.align);
     }
 }
-// whether rows of `width`-byte elements at p, ld apart, allow 16-byte accesses at multiples of 32 elements (host)
-inline bool rows_aligned(const void* p, int64_t ld, int width) { return (uintptr_t)p % 16 == 0 && ld * width % 16 == 0; }
+__device__ __forceinline__ void load_tile(const Epi& e, const Rows& t, int64_t row, int64_t col, int rows, int n, float (&v)[32]) {
+    const char* const from = t.at(row, col);
+    if (t.f32) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            fetch_tile<true>(e, from + 64 * h, t.ld, rows, max(0, min(16, n - 16 * h)), t.align);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const uint4 x = lds128(tile_at(e.tile, e.lane, q));
+                const int j = 16 * h + 4 * q;
+                v[j] = __uint_as_float(x.x); v[j + 1] = __uint_as_float(x.y); v[j + 2] = __uint_as_float(x.z); v[j + 3] = __uint_as_float(x.w);
+            }
+        }
+    } else {
+        fetch_tile<false>(e, from, t.ld, rows, n, t.align);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint4 x = lds128(tile_at(e.tile, e.lane, q));
+            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[8 * q + 2 * i] = __uint_as_float(w[i] << 16);
+                v[8 * q + 2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+            }
+        }
+    }
+    __syncwarp();
+}
 
 // The gradient of a product enters the tensor core as bf16.  Gradients of 16 bits take its nearest value: off by 2^-8 of it at most, half a step
 // of the results' own type, in every term of their sums.  Gradients of 32 bits take three parts, each the nearest value of
 // what the ones before leave: 24 bits, all that the 32-bit value has (unless its last part falls below 2^-133).
 constexpr int kPartsF32 = 3;
-__device__ __forceinline__ void store_parts(__nv_bfloat16* to, int64_t part_pitch, int parts, float (&v)[32], int n) {
-    store_run(to, 0, v, n, false, true);
+// d: bf16 parts of part_rows rows each, pitch a multiple of 64 columns (what lies beyond the last column is never read)
+__device__ __forceinline__ void store_parts(const Epi& e, const Rows& d, int64_t part_rows, int64_t row, int64_t col, int rows, int parts, float (&v)[32]) {
+    store_tile(e, d, row, col, rows, 32, v);
 #pragma unroll 1
     for (int i = 1; i < parts; ++i) {
 #pragma unroll
         for (int j = 0; j < 32; ++j) v[j] -= __bfloat162float(__float2bfloat16_rn(v[j]));
-        store_run(to + i * part_pitch, 0, v, n, false, true);
+        store_tile(e, d, i * part_rows + row, col, rows, 32, v);
     }
+}
+
+// Columns of an accumulator for a product of tiles_m x cols (cols_per of the product's columns per accumulator column): the fewest K steps
+// in a row, weighed with what a step takes.  A step moves 16 KB of A and bn / 2 columns of B into an SM at about 64 bytes a clock and
+// multiplies for 2 bn clocks; an item's start and epilogue take about 1500 clocks that nothing hides when it is its cluster's only one.
+inline int pick_bn(int64_t tiles_m, int64_t cols, int cols_div, int64_t steps, int clusters) {
+    int best = 256;
+    double least = 0;
+    for (int bn = 256; bn >= 64; bn /= 2) {
+        const int64_t n = bn / cols_div, items = tiles_m * ((cols + n - 1) / n), rounds = (items + clusters - 1) / clusters;
+        const double t = (double)rounds * (steps * (double)(2 * bn > 256 + bn ? 2 * bn : 256 + bn) + 1500.0 * bn / 256);
+        if (bn == 256 || t < 0.98 * least) { best = bn; least = t; }
+    }
+    return best;
 }
 
 }  // namespace fused

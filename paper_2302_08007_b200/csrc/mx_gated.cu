@@ -18,25 +18,18 @@ namespace bdr {
 namespace {
 
 using fused::kRows;
-
-struct Rows {           // a row-major tensor of the call's type
-    void* p;
-    int64_t ld;
-    int vec;            // 16-byte accesses at multiples of 32 columns
-    __device__ __forceinline__ void* row(int64_t r, int f32) const { return static_cast<char*>(p) + r * ld * (f32 ? 4 : 2); }
-};
+using fused::Rows;
 
 // GRAD: the epilogue writes dG and dU instead of h
 template <bool GRAD>
 struct GatedJob {
     struct Params {
         CUtensorMap a, w;          // bf16 [M][K]; [2][N][K]
-        int n_items, tiles_m, tiles_n, band_rows, steps;
-        int M, N, act, f32;
+        int n_items, bn, tiles_m, tiles_n, band_rows, steps;
+        int M, N, act;
         Rows h;                    // h, or dh
         Rows gate, up;             // where the two products go (NULL: nowhere)
-        __nv_bfloat16* d;          // [parts][2][M][pitch_d]
-        int64_t pitch_d;
+        Rows d;                    // [parts][2][M][pitch]
         int parts;
         int* status;
     };
@@ -52,35 +45,36 @@ struct GatedJob {
     }
     static __device__ __forceinline__ void load(const Params& p, const Item& it, int kk, int rank, uint8_t* dst, uint64_t* bar) {
         tma_load_3d(dst, &p.a, kk * kBK, (it.tm * 2 + rank) * kRows, 0, bar);
-        tma_load_3d(dst + fused::kOperandBytes, &p.w, kk * kBK, it.tn * kRows, rank, bar);
+        tma_load_3d(dst + fused::kOperandBytes, &p.w, kk * kBK, it.tn * (p.bn >> 1), rank, bar);
     }
-    static __device__ __forceinline__ void epilogue(const Params& p, const Item& it, int r, int half, uint32_t tmem) {
-        const int64_t row = (int64_t)it.tm * 256 + r;
+    static __device__ __forceinline__ void epilogue(const Params& p, const Item& it, const fused::Epi& e) {
+        const int64_t row = (int64_t)it.tm * 256 + e.r0;
+        const int rows = (int)min((int64_t)32, p.M - row), cols = p.bn >> 1;  // half of the accumulator is the gate
 #pragma unroll 1
-        for (int c = half * 64; c < half * 64 + 64; c += 32) {
-            __syncwarp();
+        for (int c = e.half * 32; c < cols; c += 64) {
             uint32_t gu[2][32];
-            tmem_ld32_nowait(tmem + (uint32_t)c, gu[0]);
-            tmem_ld32_nowait(tmem + (uint32_t)(128 + c), gu[1]);
+            __syncwarp();
+            tmem_ld32_nowait(e.tmem + (uint32_t)c, gu[0]);
+            tmem_ld32_nowait(e.tmem + (uint32_t)(cols + c), gu[1]);
             tmem_ld_wait();
-            const int col = it.tn * kRows + c, n = min(32, p.N - col);
-            if (row >= p.M || n <= 0) continue;
+            const int col = it.tn * cols + c, n = min(32, p.N - col);
+            if (rows <= 0 || n <= 0) continue;  // (the same for the whole warp)
             float g[32], u[32];
 #pragma unroll
             for (int j = 0; j < 32; ++j) { g[j] = __uint_as_float(gu[0][j]); u[j] = __uint_as_float(gu[1][j]); }
             if constexpr (!GRAD) {
                 if (p.gate.p) {
-                    fused::store_run(p.gate.row(row, p.f32), col, g, n, p.f32, p.gate.vec);
-                    fused::store_run(p.up.row(row, p.f32), col, u, n, p.f32, p.up.vec);
+                    fused::store_tile(e, p.gate, row, col, rows, n, g);
+                    fused::store_tile(e, p.up, row, col, rows, n, u);
                 }
                 act::with(p.act, [&](auto f) {
 #pragma unroll
                     for (int j = 0; j < 32; ++j) g[j] = act::of<decltype(f)::value>(g[j]) * u[j];
                 });
-                fused::store_run(p.h.row(row, p.f32), col, g, n, p.f32, p.h.vec);
+                fused::store_tile(e, p.h, row, col, rows, n, g);
             } else {
                 float dh[32];
-                fused::load_run(p.h.row(row, p.f32), col, dh, n, p.f32, p.h.vec);
+                fused::load_tile(e, p.h, row, col, rows, n, dh);
                 act::with(p.act, [&](auto f) {
 #pragma unroll
                     for (int j = 0; j < 32; ++j) {
@@ -90,83 +84,102 @@ struct GatedJob {
                         u[j] = dh[j] * y;
                     }
                 });
-                __nv_bfloat16* const to = p.d + row * p.pitch_d + col;
-                const int64_t z = (int64_t)p.M * p.pitch_d;
-                fused::store_parts(to, 2 * z, p.parts, g, n);
-                fused::store_parts(to + z, 2 * z, p.parts, u, n);
+                fused::store_parts(e, p.d, 2 * (int64_t)p.M, row, col, rows, p.parts, g);
+                fused::store_parts(e, p.d, 2 * (int64_t)p.M, p.M + row, col, rows, p.parts, u);
             }
         }
     }
 };
 
-// dG and dU from the stored products: eight columns of a row per thread.  Bound by memory (bf16: 6 bytes in, 4 out per output).
+// dG and dU from the stored products.  A thread keeps its eight columns and walks down the rows.  Bound by memory (bf16: 6 bytes in, 4 out
+// per output).
 template <bool F32>
-__global__ void __launch_bounds__(256) gated_grad_kernel(Rows gate, Rows up, Rows dh, int act, int64_t M, int N, __nv_bfloat16* d, int64_t pitch_d) {
-    const int groups = (N + 7) / 8;
-    const int64_t total = M * groups, stride = (int64_t)gridDim.x * 256, z = M * pitch_d;
-    auto get = [&](const Rows& t, int64_t row, int col, int n, float (&v)[8]) {
-        if constexpr (F32) {
-            const float* from = static_cast<const float*>(t.row(row, 1)) + col;
-            if (t.vec && n == 8) {
-                const float4 a = *reinterpret_cast<const float4*>(from), b = *reinterpret_cast<const float4*>(from + 4);
-                v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = j < n ? from[j] : 0.f;
-            }
+__device__ __forceinline__ void read8(const Rows& t, int64_t row, int col, int n, float (&v)[8]) {
+    const char* const from = t.at(row, col);
+    if constexpr (F32) {
+        if (t.align == 16 && n == 8) {
+            const float4 a = *reinterpret_cast<const float4*>(from), b = *reinterpret_cast<const float4*>(from + 16);
+            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
         } else {
-            const __nv_bfloat16* from = static_cast<const __nv_bfloat16*>(t.row(row, 0)) + col;
-            if (t.vec && n == 8) {
-                const uint4 x = *reinterpret_cast<const uint4*>(from);
-                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-                for (int e = 0; e < 4; ++e) { v[2 * e] = __uint_as_float(w[e] << 16); v[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u); }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = j < n ? __bfloat162float(from[j]) : 0.f;
-            }
+            for (int j = 0; j < 8; ++j) v[j] = j < n ? reinterpret_cast<const float*>(from)[j] : 0.f;
         }
-    };
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += stride) {
-        const int64_t row = i / groups;
-        const int col = (int)(i - row * groups) * 8, n = min(8, N - col);
-        float g[8], u[8], e[8];
-        get(gate, row, col, n, g);
-        get(up, row, col, n, u);
-        get(dh, row, col, n, e);
-        act::with(act, [&](auto f) {
+    } else {
+        if (t.align == 16 && n == 8) {
+            const uint4 x = *reinterpret_cast<const uint4*>(from);
+            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { v[2 * e] = __uint_as_float(w[e] << 16); v[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u); }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = j < n ? __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(from)[j]) : 0.f;
+        }
+    }
+}
+template <bool F32, int ACT>
+__global__ void __launch_bounds__(256) gated_grad_kernel(Rows gate, Rows up, Rows dh, int64_t M, int N, Rows d) {
+    const int col = ((int)blockIdx.x * (int)blockDim.x + (int)threadIdx.x) * 8, n = min(8, N - col);
+    if (n <= 0) return;
+    constexpr int kAhead = F32 ? 1 : 2;  // rows in flight
+    for (int64_t row0 = (int64_t)blockIdx.y * kAhead; row0 < M; row0 += (int64_t)gridDim.y * kAhead) {
+        float g[kAhead][8], u[kAhead][8], e[kAhead][8];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int64_t row = min(row0 + i, M - 1);
+            read8<F32>(gate, row, col, n, g[i]);
+            read8<F32>(up, row, col, n, u[i]);
+            read8<F32>(dh, row, col, n, e[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (row0 + i >= M) break;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 float y, slope;
-                act::both<decltype(f)::value>(g[j], y, slope);
-                g[j] = e[j] * u[j] * slope;
-                u[j] = e[j] * y;
+                act::both<ACT>(g[i][j], y, slope);
+                g[i][j] = e[i][j] * u[i][j] * slope;
+                u[i][j] = e[i][j] * y;
             }
-        });
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            float(&v)[8] = s ? u : g;
-            __nv_bfloat16* const to = d + s * z + row * pitch_d + col;  // (the pitch has room for whole groups)
+            for (int s = 0; s < 2; ++s) {
+                float(&v)[8] = s ? u[i] : g[i];
 #pragma unroll
-            for (int part = 0; part < (F32 ? fused::kPartsF32 : 1); ++part) {
-                *reinterpret_cast<uint4*>(to + 2 * part * z) = make_uint4(fused::bf16x2(v[0], v[1]), fused::bf16x2(v[2], v[3]), fused::bf16x2(v[4], v[5]), fused::bf16x2(v[6], v[7]));
+                for (int part = 0; part < (F32 ? fused::kPartsF32 : 1); ++part) {  // (the pitch has room for whole groups)
+                    *reinterpret_cast<uint4*>(d.at((2 * part + s) * M + row0 + i, col)) =
+                        make_uint4(fused::bf16x2(v[0], v[1]), fused::bf16x2(v[2], v[3]), fused::bf16x2(v[4], v[5]), fused::bf16x2(v[6], v[7]));
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] -= __bfloat162float(__float2bfloat16_rn(v[j]));
+                    for (int j = 0; j < 8; ++j) v[j] -= __bfloat162float(__float2bfloat16_rn(v[j]));
+                }
             }
         }
     }
 }
+template <bool F32>
+int launch_gated_grad(const Rows& gate, const Rows& up, const Rows& dh, int act, int64_t M, int64_t N, const Rows& d, cudaStream_t st) {
+    const int64_t groups = (N + 7) / 8;
+    const int threads = groups >= 256 ? 256 : (int)round_up(groups, 32);
+    const int64_t x = (groups + threads - 1) / threads, y = std::min<int64_t>(M, std::max<int64_t>(1, (int64_t)sm_count() * 4096 / (x * threads)));
+    const dim3 grid((unsigned)x, (unsigned)std::min<int64_t>(y, 65535));
+    switch (act) {
+        case MX_ACT_SILU: gated_grad_kernel<F32, MX_ACT_SILU><<<grid, threads, 0, st>>>(gate, up, dh, M, (int)N, d); break;
+        case MX_ACT_GELU: gated_grad_kernel<F32, MX_ACT_GELU><<<grid, threads, 0, st>>>(gate, up, dh, M, (int)N, d); break;
+        case MX_ACT_GELU_TANH: gated_grad_kernel<F32, MX_ACT_GELU_TANH><<<grid, threads, 0, st>>>(gate, up, dh, M, (int)N, d); break;
+        default: gated_grad_kernel<F32, MX_ACT_RELU><<<grid, threads, 0, st>>>(gate, up, dh, M, (int)N, d); break;
+    }
+    return cudaGetLastError() == cudaSuccess ? BDR_OK : BDR_ERR_CUDA;
+}
 
 // Workspace: A, W and, for gradients, D.
 struct GatedSpace {
-    int64_t pitch_k, pitch_d, a, w, d, bytes;  // offsets in bytes
+    int64_t pitch_k, pitch_d, a, w, d, sums, bytes;  // offsets in bytes
     GatedSpace(int64_t M, int64_t N, int64_t K, int parts) {
         pitch_k = line_pitch(K);
         pitch_d = round_up(N, 64);
         a = 0;
         w = a + round_up(M * pitch_k * 2, 256);
         d = w + round_up(2 * N * pitch_k * 2, 256);
-        bytes = d + (parts ? round_up((int64_t)parts * 2 * M * pitch_d * 2, 256) : 0);
+        sums = d + (parts ? round_up((int64_t)parts * 2 * M * pitch_d * 2, 256) : 0);
+        bytes = sums + (parts ? grad_sums_bytes(M, N, K, 2) : 0);
     }
 };
 
@@ -178,18 +191,17 @@ int check_rows(const void* p, int64_t ld, int64_t cols, int width) {
     return (uintptr_t)p % width ? BDR_ERR_MISALIGNED : BDR_OK;
 }
 
-Rows make_rows(const void* p, int64_t ld, int width) { return {const_cast<void*>(p), ld, p ? fused::rows_aligned(p, ld, width) : 0}; }
-
 template <class Params>
 int set_products(Params& p, int64_t M, int64_t N, int64_t K, const GatedSpace& s, uint8_t* ws) {
-    if (!fused::make_map(&p.a, ws + s.a, K, M, 1, s.pitch_k, M * s.pitch_k, kRows) ||
-        !fused::make_map(&p.w, ws + s.w, K, N, 2, s.pitch_k, N * s.pitch_k, kRows))
-        return BDR_ERR_CUDA;
     p.tiles_m = (int)((M + 255) / 256);
-    p.tiles_n = (int)((N + kRows - 1) / kRows);
+    p.steps = (int)((K + kBK - 1) / kBK);
+    p.bn = fused::pick_bn(p.tiles_m, N, 2, p.steps, sm_count() / 2);
+    p.tiles_n = (int)((N + p.bn / 2 - 1) / (p.bn / 2));
+    if (!fused::make_map(&p.a, ws + s.a, K, M, 1, s.pitch_k, M * s.pitch_k, kRows) ||
+        !fused::make_map(&p.w, ws + s.w, K, N, 2, s.pitch_k, N * s.pitch_k, p.bn / 2))
+        return BDR_ERR_CUDA;
     p.n_items = p.tiles_m * p.tiles_n;
     p.band_rows = gemm_band_rows((M + 2 * N) * K * 2);
-    p.steps = (int)((K + kBK - 1) / kBK);
     p.M = (int)M;
     p.N = (int)N;
     p.status = device_status_word();
@@ -227,15 +239,15 @@ int mx_gated_gemm(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bdr_co
     if ((uintptr_t)workspace % 256) return BDR_ERR_MISALIGNED;
     cudaStream_t st = (cudaStream_t)stream;
     uint8_t* const ws = static_cast<uint8_t*>(workspace);
-    if ((rc = decode_lines(*a, cfg_a->m, M, K, reinterpret_cast<__nv_bfloat16*>(ws + s.a), s.pitch_k, st))) return rc;
-    if ((rc = decode_lines(*w, cfg_w->m, 2 * N, K, reinterpret_cast<__nv_bfloat16*>(ws + s.w), s.pitch_k, st))) return rc;
+    if ((rc = decode_pair(*a, cfg_a->m, M, reinterpret_cast<__nv_bfloat16*>(ws + s.a), *w, cfg_w->m, 2 * N, reinterpret_cast<__nv_bfloat16*>(ws + s.w), K,
+                          s.pitch_k, st)))
+        return rc;
     GatedJob<false>::Params p = {};
     if ((rc = set_products(p, M, N, K, s, ws))) return rc;
     p.act = act;
-    p.f32 = dt == BDR_F32;
-    p.h = make_rows(h, ldh, width);
-    p.gate = make_rows(gate_up, ld_gate_up, width);
-    p.up = make_rows(gate_up ? static_cast<char*>(gate_up) + N * width : nullptr, ld_gate_up, width);
+    p.h = fused::make_rows(h, ldh, dt == BDR_F32);
+    p.gate = fused::make_rows(gate_up, ld_gate_up, dt == BDR_F32);
+    p.up = fused::make_rows(gate_up ? static_cast<char*>(gate_up) + N * width : nullptr, ld_gate_up, dt == BDR_F32);
     return fused::launch<GatedJob<false>>(p, st);
 }
 
@@ -277,23 +289,19 @@ int mx_gated_gemm_bwd(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bd
     uint8_t* const ws = static_cast<uint8_t*>(workspace);
     __nv_bfloat16 *const wa = reinterpret_cast<__nv_bfloat16*>(ws + s.a), *const ww = reinterpret_cast<__nv_bfloat16*>(ws + s.w),
                          *const d = reinterpret_cast<__nv_bfloat16*>(ws + s.d);
-    if ((rc = decode_lines(*a, cfg_a->m, M, K, wa, s.pitch_k, st))) return rc;
-    if ((rc = decode_lines(*w, cfg_w->m, 2 * N, K, ww, s.pitch_k, st))) return rc;
-    const Rows dh_rows = make_rows(dh, ld_dh, width);
+    if ((rc = decode_pair(*a, cfg_a->m, M, wa, *w, cfg_w->m, 2 * N, ww, K, s.pitch_k, st))) return rc;
+    const bool f32 = dt == BDR_F32;
+    const Rows dh_rows = fused::make_rows(dh, ld_dh, f32), d_rows = fused::make_rows(d, s.pitch_d, false);
     if (gate_up) {
-        const Rows g = make_rows(gate_up, ld_gate_up, width), u = make_rows(static_cast<const char*>(gate_up) + N * width, ld_gate_up, width);
-        const unsigned grid = (unsigned)std::min<int64_t>((M * ((N + 7) / 8) + 255) / 256, (int64_t)sm_count() * 16);
-        if (dt == BDR_F32) gated_grad_kernel<true><<<grid, 256, 0, st>>>(g, u, dh_rows, act, M, (int)N, d, s.pitch_d);
-        else gated_grad_kernel<false><<<grid, 256, 0, st>>>(g, u, dh_rows, act, M, (int)N, d, s.pitch_d);
-        if (cudaGetLastError() != cudaSuccess) return BDR_ERR_CUDA;
+        const Rows g = fused::make_rows(gate_up, ld_gate_up, f32), u = fused::make_rows(static_cast<const char*>(gate_up) + N * width, ld_gate_up, f32);
+        rc = f32 ? launch_gated_grad<true>(g, u, dh_rows, act, M, N, d_rows, st) : launch_gated_grad<false>(g, u, dh_rows, act, M, N, d_rows, st);
+        if (rc) return rc;
     } else {
         GatedJob<true>::Params p = {};
         if ((rc = set_products(p, M, N, K, s, ws))) return rc;
         p.act = act;
-        p.f32 = dt == BDR_F32;
         p.h = dh_rows;
-        p.d = d;
-        p.pitch_d = s.pitch_d;
+        p.d = d_rows;
         p.parts = parts;
         if ((rc = fused::launch<GatedJob<true>>(p, st))) return rc;
     }
@@ -302,7 +310,8 @@ int mx_gated_gemm_bwd(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bd
     g.M = M; g.N = N; g.K = K; g.pitch_d = s.pitch_d; g.pitch_k = s.pitch_k;
     g.segs = 2; g.parts = parts;
     g.da = da; g.dw = dw; g.ld_da = ld_da; g.ld_dw = ld_dw;
-    g.f32 = dt == BDR_F32;
+    g.f32 = f32;
+    g.sums = reinterpret_cast<float*>(ws + s.sums);
     g.first = g.last = true;
     return launch_grad_products(g, st);
 }

@@ -4,6 +4,9 @@
 // and D^T is D.  Nothing is transposed for it: the tensor core reads an operand with its rows contiguous just as well (descriptors of
 // rows-contiguous chunks, see mx_fused_gemm.cuh), so TMA fetches boxes of 64 columns x 64 K from the matrices as they lie.
 // Both products run in one launch: their tiles share the clusters, and a last round that is half empty is paid for once.
+#include <algorithm>
+
+#include "bdr_async.cuh"
 #include "bdr_x2.cuh"
 #include "mx_fused_gemm.cuh"
 #include "mx_frag.cuh"
@@ -12,14 +15,18 @@ namespace bdr {
 namespace {
 
 using fused::kRows;
+using fused::Rows;
 
+// Where the sums of one of the products go: to the result itself, or, of a part of the K steps, to fp32 sums of the workspace.
 struct Target {
-    void* out;
-    int64_t ld;
-    int rows, vec;   // rows of a segment
-    float* read;     // fp32 sums to add to, or NULL
-    float* keep;     // fp32 sums to store instead of `out`, or NULL
-    int64_t ld_acc;
+    Rows out;        // the result (or the running sum of several calls)
+    Rows sums;       // [splits * rows of all segments][K]; NULL: not split
+    const float* read;  // running sum of earlier calls to add, or NULL
+    int64_t ld_read;
+    int rows;        // of a segment
+    int splits, span;   // K steps of a part
+    int steps;
+    int scaled;      // `out` is the result, which takes the factor
 };
 
 template <bool F32>
@@ -29,7 +36,7 @@ struct GradJob {
         CUtensorMap d_mn;  // D, boxes of 64 (rows of dW) x 64 (K)
         CUtensorMap w, a;  // boxes of 64 columns x 64 K
         Target da, dw;
-        int n_items, items_da, items_dw_seg;
+        int n_items, bn, items_da, items_da_split, items_dw_split, items_dw_seg;
         int tiles_m, tiles_n, tiles_k;
         int steps_n, steps_m;  // K steps over one segment's columns of D, over tokens
         int segs, parts;
@@ -39,6 +46,7 @@ struct GradJob {
     };
     struct Item {
         int steps, tm, tk, seg;  // seg < 0: dA
+        int split, k0;           // first K step
     };
     static constexpr bool b_mn = true;
     static constexpr int kSpan = F32 ? 4 : 0;  // 16 instructions in a chain
@@ -46,19 +54,24 @@ struct GradJob {
     static __device__ __forceinline__ Item item(const Params& p, int i) {
         Item it;
         if (i < p.items_da) {
+            it.split = i / p.items_da_split;
             it.seg = -1;
-            it.steps = p.steps_n * p.segs * p.parts;
-            gemm_tile_coords(i, p.tiles_m, p.tiles_k, 8, it.tm, it.tk);
+            gemm_tile_coords(i - it.split * p.items_da_split, p.tiles_m, p.tiles_k, 8, it.tm, it.tk);
         } else {
             i -= p.items_da;
+            it.split = i / p.items_dw_split;
+            i -= it.split * p.items_dw_split;
             it.seg = i / p.items_dw_seg;
-            it.steps = p.steps_m * p.parts;
             gemm_tile_coords(i - it.seg * p.items_dw_seg, p.tiles_n, p.tiles_k, 8, it.tm, it.tk);
         }
+        const Target& t = it.seg < 0 ? p.da : p.dw;
+        it.k0 = it.split * t.span;
+        it.steps = min(t.span, t.steps - it.k0);
         return it;
     }
     static __device__ __forceinline__ void load(const Params& p, const Item& it, int kk, int rank, uint8_t* dst, uint64_t* bar) {
         const int row = (it.tm * 2 + rank) * kRows, col = (it.tk * 2 + rank) * kRows;
+        kk += it.k0;
         uint8_t* const b = dst + fused::kOperandBytes;
         constexpr int kChunk = fused::kOperandBytes / 2;
         if (it.seg < 0) {
@@ -75,53 +88,94 @@ struct GradJob {
             tma_load_3d(b + kChunk, &p.a, col + 64, k, 0, bar);
         }
     }
-    // 32 sums of a row, from column c of the 256
-    static __device__ __forceinline__ void put(const Params& p, const Item& it, int r, int c, float (&v)[32]) {
+    // a warp's 32 x 32 sums, from column c of the 256
+    static __device__ __forceinline__ void put(const Params& p, const Item& it, const fused::Epi& e, int c, float (&v)[32]) {
         const Target& t = it.seg < 0 ? p.da : p.dw;
-        const int row = it.tm * 256 + r, col = it.tk * 256 + c, n = min(32, p.cols - col);
-        if (row >= t.rows || n <= 0) return;
-        const int64_t out_row = row + (it.seg > 0 ? (int64_t)it.seg * t.rows : 0);
+        const int64_t row = (int64_t)it.tm * 256 + e.r0;
+        const int col = it.tk * 256 + c, rows = (int)min((int64_t)32, t.rows - row), n = min(32, p.cols - col);
+        if (rows <= 0 || n <= 0) return;
+        const int64_t segs = it.seg < 0 ? 1 : p.segs, out_row = row + (it.seg > 0 ? (int64_t)it.seg * t.rows : 0);
+        if (t.sums.p) {
+            fused::store_tile(e, t.sums, it.split * segs * t.rows + out_row, col, rows, n, v);
+            return;
+        }
         if (t.read) {
             float old[32];
-            fused::load_run(t.read + out_row * t.ld_acc, col, old, n, true, true);
+            const Rows from = {const_cast<float*>(t.read), t.ld_read, 1, 16};
+            fused::load_tile(e, from, out_row, col, rows, n, old);
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] += old[j];
         }
-        if (t.keep) {
-            fused::store_run(t.keep + out_row * t.ld_acc, col, v, n, true, true);
-        } else {
-            if (p.scale) {
-                const float s = *p.scale;
+        if (t.scaled && p.scale) {
+            const float s = *p.scale;
 #pragma unroll
-                for (int j = 0; j < 32; ++j) v[j] *= s;
-            }
-            fused::store_run(static_cast<char*>(t.out) + out_row * t.ld * (F32 ? 4 : 2), col, v, n, F32, t.vec);
+            for (int j = 0; j < 32; ++j) v[j] *= s;
         }
+        fused::store_tile(e, t.out, out_row, col, rows, n, v);
     }
-    static __device__ __forceinline__ void epilogue(const Params& p, const Item& it, int r, int half, uint32_t tmem) {
+    static __device__ __forceinline__ void epilogue(const Params& p, const Item& it, const fused::Epi& e) {
 #pragma unroll 1
-        for (int c = half * 128; c < half * 128 + 128; c += 32) {
+        for (int c = e.half * 128; c < e.half * 128 + 128; c += 32) {
             __syncwarp();
             uint32_t u[32];
-            tmem_ld32(tmem + (uint32_t)c, u);
+            tmem_ld32(e.tmem + (uint32_t)c, u);
             float v[32];
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(u[j]);
-            put(p, it, r, c, v);
+            put(p, it, e, c, v);
         }
     }
-    static __device__ __forceinline__ void finish(const Params& p, const Item& it, int r, int half, float (&v)[4][32]) {
+    static __device__ __forceinline__ void finish(const Params& p, const Item& it, const fused::Epi& e, float (&v)[4][32]) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) put(p, it, r, half * 128 + 32 * q, v[q]);
+        for (int q = 0; q < 4; ++q) put(p, it, e, e.half * 128 + 32 * q, v[q]);
     }
 };
 
+// Adds the parts of a split product in order, and what earlier calls left, and writes the result: four columns per thread.  blockIdx.z: dA, dW
+__global__ void __launch_bounds__(128) grad_join_kernel(Target da, Target dw, int64_t rows_da, int64_t rows_dw, int cols, const float* scale) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // launched as a programmatic dependent of the products
+    const Target& t = blockIdx.z ? dw : da;
+    const int64_t rows = blockIdx.z ? rows_dw : rows_da;
+    const int col = ((int)blockIdx.x * 128 + (int)threadIdx.x) * 4, n = min(4, cols - col);
+    if (!t.sums.p || n <= 0) return;
+    for (int64_t row = blockIdx.y; row < rows; row += gridDim.y) {
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);  // (the pitch of the sums has room for whole groups)
+        for (int s = 0; s < t.splits; ++s) {
+            const float4 x = *reinterpret_cast<const float4*>(t.sums.at(s * rows + row, col));
+            v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+        }
+        if (t.read) {
+            const float4 x = *reinterpret_cast<const float4*>(reinterpret_cast<const char*>(t.read) + row * t.ld_read + col * 4);
+            v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+        }
+        if (t.scaled && scale) {
+            const float s = *scale;
+            v.x *= s; v.y *= s; v.z *= s; v.w *= s;
+        }
+        const float w[4] = {v.x, v.y, v.z, v.w};
+        char* const to = t.out.at(row, col);
+        if (t.out.f32) {
+            if (t.out.align == 16 && n == 4) *reinterpret_cast<float4*>(to) = v;
+            else
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (j < n) reinterpret_cast<float*>(to)[j] = w[j];
+        } else {
+            if (t.out.align == 16 && n == 4) *reinterpret_cast<uint2*>(to) = make_uint2(fused::bf16x2(v.x, v.y), fused::bf16x2(v.z, v.w));
+            else
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (j < n) reinterpret_cast<__nv_bfloat16*>(to)[j] = __float2bfloat16_rn(w[j]);
+        }
+    }
+}
+
 // One thread decodes 32 elements of a line (two blocks) straight from the planes and writes 64 bytes.
 template <int W>
-__global__ void __launch_bounds__(256) decode_lines_kernel(bdr_planes_t in, __nv_bfloat16* out, int64_t pitch, int64_t n_items, uint32_t items_per_row, int nb) {
-    const int64_t stride = (int64_t)gridDim.x * 256;
-    for (int64_t g = (int64_t)blockIdx.x * 256 + threadIdx.x; g < n_items; g += stride) {
-        const int64_t row = g / items_per_row;
+__device__ __forceinline__ void decode_items(const bdr_planes_t& in, __nv_bfloat16* out, int64_t pitch, int64_t n_items, uint32_t items_per_row, int nb,
+                                             int64_t first, int64_t stride) {
+    for (int64_t g = first; g < n_items; g += stride) {
+        const int64_t row = (uint64_t)n_items >> 32 ? g / items_per_row : (uint32_t)g / items_per_row;
         const uint32_t it = (uint32_t)(g - row * items_per_row);
         const int64_t at = (int64_t)it * 4 * W;
         const uint8_t* codes = in.elems + row * in.ld_elems + at;
@@ -150,34 +204,69 @@ __global__ void __launch_bounds__(256) decode_lines_kernel(bdr_planes_t in, __nv
 #pragma unroll
             for (int k = 0; k < 16; ++k) yw[k] = o.y[k];
         }
-        uint4* dst = reinterpret_cast<uint4*>(out + row * pitch + (int64_t)it * 32);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) dst[k] = make_uint4(yw[4 * k], yw[4 * k + 1], yw[4 * k + 2], yw[4 * k + 3]);
+        __nv_bfloat16* const to = out + row * pitch + (int64_t)it * 32;
+        async::stg256(to, yw);
+        async::stg256(to + 16, yw + 8);
     }
 }
 
-template <int W>
-int launch_decode(const bdr_planes_t& in, int64_t rows, int64_t K, __nv_bfloat16* out, int64_t pitch, cudaStream_t st) {
-    const int64_t per_row = (K + 31) / 32, n = rows * per_row;
-    if (n == 0) return BDR_OK;
-    const unsigned grid = (unsigned)std::min<int64_t>((n + 255) / 256, (int64_t)sm_count() * 32);
-    decode_lines_kernel<W><<<grid, 256, 0, st>>>(in, out, pitch, n, (uint32_t)per_row, (int)((K + 15) / 16));
-    return cudaGetLastError() == cudaSuccess ? BDR_OK : BDR_ERR_CUDA;
+struct Lines {
+    bdr_planes_t in;
+    __nv_bfloat16* out;
+    int64_t n_items;
+    int m;
+};
+// Both operands in one launch: blocks 0 .. first_blocks - 1 take the first.
+__global__ void __launch_bounds__(256) decode_pair_kernel(Lines first, Lines second, unsigned first_blocks, int64_t pitch, uint32_t items_per_row, int nb) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the product's set-up may begin
+    const bool one = blockIdx.x < first_blocks;
+    const Lines& l = one ? first : second;
+    const int64_t at = (int64_t)(one ? blockIdx.x : blockIdx.x - first_blocks) * 256 + threadIdx.x, stride = (int64_t)(one ? first_blocks : gridDim.x - first_blocks) * 256;
+    switch (l.m) {
+        case 2: decode_items<3>(l.in, l.out, pitch, l.n_items, items_per_row, nb, at, stride); break;
+        case 4: decode_items<5>(l.in, l.out, pitch, l.n_items, items_per_row, nb, at, stride); break;
+        default: decode_items<8>(l.in, l.out, pitch, l.n_items, items_per_row, nb, at, stride); break;
+    }
 }
 
 }  // namespace
 
-int decode_lines(const bdr_planes_t& in, int m, int64_t rows, int64_t K, __nv_bfloat16* out, int64_t pitch, cudaStream_t st) {
-    QParams qp;
-    qp.k1 = 16; qp.k2 = 2; qp.d2 = 1; qp.m = m; qp.rounding = BDR_ROUND_NEAREST_EVEN; qp.beta = 1; qp.qmax = (1u << m) - 1u;
-    const int rc = unpack_rowwise_mx_x2(in, out, rows, K, pitch, qp, st);  // whole runs of 2048 elements: through shared memory
-    if (rc != BDR_ERR_UNSUPPORTED) return rc;
-    switch (m) {
-        case 2: return launch_decode<3>(in, rows, K, out, pitch, st);
-        case 4: return launch_decode<5>(in, rows, K, out, pitch, st);
-        case 7: return launch_decode<8>(in, rows, K, out, pitch, st);
+int decode_pair(const bdr_planes_t& a, int m_a, int64_t rows_a, __nv_bfloat16* out_a, const bdr_planes_t& w, int m_w, int64_t rows_w, __nv_bfloat16* out_w,
+                int64_t K, int64_t pitch, cudaStream_t st) {
+    Lines l[2] = {{a, out_a, rows_a, m_a}, {w, out_w, rows_w, m_w}};
+    const int64_t per_row = (K + 31) / 32;
+    for (Lines& x : l) {
+        if (x.n_items * K >= (1ll << 23)) {
+            QParams qp;
+            qp.k1 = 16; qp.k2 = 2; qp.d2 = 1; qp.m = x.m; qp.rounding = BDR_ROUND_NEAREST_EVEN; qp.beta = 1; qp.qmax = (1u << x.m) - 1u;
+            const int rc = unpack_rowwise_mx_x2(x.in, x.out, x.n_items, K, pitch, qp, st);  // whole runs of 2048 elements: through shared memory
+            if (rc == BDR_OK) x.n_items = 0;
+            else if (rc != BDR_ERR_UNSUPPORTED) return rc;
+        }
+        x.n_items *= per_row;
     }
-    return BDR_ERR_UNSUPPORTED;
+    if (l[0].n_items + l[1].n_items == 0) return BDR_OK;
+    unsigned blocks[2];
+    for (int i = 0; i < 2; ++i) blocks[i] = (unsigned)std::min<int64_t>((l[i].n_items + 255) / 256, (int64_t)sm_count() * 32);
+    decode_pair_kernel<<<blocks[0] + blocks[1], 256, 0, st>>>(l[0], l[1], blocks[0], pitch, (uint32_t)per_row, (int)((K + 15) / 16));
+    return cudaGetLastError() == cudaSuccess ? BDR_OK : BDR_ERR_CUDA;
+}
+
+// How the K steps of the two products are cut.  Few tiles with long sums (dA of few tokens, dW of a narrow layer) would keep few clusters
+// busy: their steps go to several clusters, whose fp32 sums another kernel adds in order.  That costs a launch (about 3 us) and a pass over the
+// sums, so a cut has to shorten the longest item by 16 steps (of 0.27 us) at least.
+constexpr int kPlanClusters = 74;
+static int grad_cut(int64_t tiles, int64_t steps, int64_t share) {
+    const int64_t most = std::min<int64_t>(32, 2 * kPlanClusters / tiles);
+    const int64_t n = std::min(most, (steps + share - 1) / share);
+    if (n < 2) return 1;
+    const int64_t span = (steps + n - 1) / n;
+    return steps - span < 16 ? 1 : (int)((steps + span - 1) / span);
+}
+// Bytes of the fp32 sums that launch_grad_products may need for M tokens and any number of outputs up to N: at most 2 x 74 tiles of each product.
+int64_t grad_sums_bytes(int64_t M, int64_t N, int64_t K, int segs) {
+    const int64_t most = 2 * kPlanClusters * 256 / ((K + 255) / 256) + 1;
+    return round_up((std::min(most, 32 * M) + std::min(most, 32 * segs * N)) * line_pitch(K) * 4, 256);
 }
 
 template <bool F32>
@@ -189,9 +278,7 @@ static int launch_grads(const GradProducts& g, cudaStream_t st) {
         !fused::make_map(&p.w, g.w, g.K, g.N, g.segs, g.pitch_k, g.N * g.pitch_k, kBK) ||
         !fused::make_map(&p.a, g.a, g.K, g.M, 1, g.pitch_k, g.M * g.pitch_k, kBK))
         return BDR_ERR_CUDA;
-    const int width = F32 ? 4 : 2;
-    p.da = {g.da, g.ld_da, (int)g.M, fused::rows_aligned(g.da, g.ld_da, width), g.first ? nullptr : g.acc, g.last ? nullptr : g.acc, g.ld_acc};
-    p.dw = {g.dw, g.ld_dw, (int)g.N, fused::rows_aligned(g.dw, g.ld_dw, width), nullptr, nullptr, 0};
+    p.bn = 256;
     p.tiles_m = (int)((g.M + 255) / 256);
     p.tiles_n = (int)((g.N + 255) / 256);
     p.tiles_k = (int)((g.K + 255) / 256);
@@ -199,13 +286,42 @@ static int launch_grads(const GradProducts& g, cudaStream_t st) {
     p.steps_m = (int)((g.M + kBK - 1) / kBK);
     p.segs = g.segs; p.parts = g.parts; p.scale = g.scale;
     p.cols = (int)g.K;
-    p.items_da = g.da ? p.tiles_m * p.tiles_k : 0;
+    p.items_da_split = g.da ? p.tiles_m * p.tiles_k : 0;
     p.items_dw_seg = p.tiles_n * p.tiles_k;
-    p.n_items = p.items_da + (g.dw ? g.segs * p.items_dw_seg : 0);
+    p.items_dw_split = g.dw ? g.segs * p.items_dw_seg : 0;
+    p.da.rows = (int)g.M;
+    p.dw.rows = (int)g.N;
+    p.da.steps = p.steps_n * g.segs * g.parts;
+    p.dw.steps = p.steps_m * g.parts;
+    const int64_t work = (int64_t)p.items_da_split * p.da.steps + (int64_t)p.items_dw_split * p.dw.steps;
+    const int64_t share = std::max<int64_t>(16, (work + kPlanClusters - 1) / kPlanClusters);
+    float* sums = g.sums;
+    const int64_t pitch = line_pitch(g.K);
+    for (int i = 0; i < 2; ++i) {
+        Target& t = i ? p.dw : p.da;
+        const int tiles = i ? p.items_dw_split : p.items_da_split;
+        const int64_t rows = i ? g.segs * g.N : g.M;
+        t.out = i ? fused::make_rows(g.dw, g.ld_dw, F32) : (g.last ? fused::make_rows(g.da, g.ld_da, F32) : fused::make_rows(g.acc, g.ld_acc, true));
+        t.scaled = i || g.last;
+        t.read = i || g.first ? nullptr : g.acc;
+        t.ld_read = g.ld_acc * 4;
+        t.splits = tiles ? grad_cut(tiles, t.steps, share) : 1;
+        t.span = (t.steps + t.splits - 1) / t.splits;
+        if (t.splits > 1) {
+            t.sums = fused::make_rows(sums, pitch, true);
+            sums += t.splits * rows * pitch;
+        }
+    }
+    p.items_da = p.items_da_split * p.da.splits;
+    p.n_items = p.items_da + p.items_dw_split * p.dw.splits;
     p.status = device_status_word();
     if (!p.status) return BDR_ERR_CUDA;
     if (p.n_items == 0) return BDR_OK;
-    return fused::launch<GradJob<F32>>(p, st);
+    const int rc = fused::launch<GradJob<F32>>(p, st);
+    if (rc || (p.da.splits == 1 && p.dw.splits == 1)) return rc;
+    const int64_t rows_da = g.M, rows_dw = g.segs * g.N;
+    const dim3 grid((unsigned)((g.K + 511) / 512), (unsigned)std::min<int64_t>(2048, std::max(p.da.splits > 1 ? rows_da : 0, p.dw.splits > 1 ? rows_dw : 0)), 2);
+    return launch_dependent(grad_join_kernel, grid, dim3(128), st, p.da, p.dw, rows_da, rows_dw, p.cols, p.scale);
 }
 
 int launch_grad_products(const GradProducts& g, cudaStream_t st) { return g.f32 ? launch_grads<true>(g, st) : launch_grads<false>(g, st); }
