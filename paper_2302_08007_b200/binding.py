@@ -581,45 +581,52 @@ def mx_gated_gemv(cfg_w: Config, w: Planes, N: int, K: int, x: torch.Tensor, h: 
     return h
 
 
-def _rows(t: torch.Tensor, rows: int, cols: int, dtype, what: str) -> int:
-    """Row pitch of a [rows, cols] CUDA tensor of `dtype` whose rows are contiguous."""
-    if t.dtype != dtype or t.shape != (rows, cols) or (t.stride(1) != 1 and cols > 1):
-        raise ValueError("%s: expected %s [%d, %d] with contiguous rows" % (what, dtype, rows, cols))
-    return _pitch(t.stride(0), rows, cols, what)
+def _matrix(t: torch.Tensor, rows: int, cols: int, dtype, what: str, here: int) -> int:
+    """Row pitch of a [rows, cols] tensor of `dtype` on the current GPU `here` whose rows are contiguous."""
+    if t.shape != (rows, cols) or t.dtype != dtype:
+        raise ValueError("%s: expected %s [%d, %d]" % (what, dtype, rows, cols))
+    pitch, step = t.stride()
+    if step != 1 and cols > 1:
+        raise ValueError("%s: expected contiguous rows" % what)
+    if t.get_device() != here:
+        raise ValueError("%s: expected a CUDA tensor of the current device" % what)
+    return pitch if pitch >= cols else _pitch(pitch, rows, cols, what)
 
 
-def _vector(t: torch.Tensor, n: int, dtype, what: str) -> None:
+def _vector(t: torch.Tensor, n: int, dtype, what: str, here: int) -> int:
+    """Address of a contiguous [n] tensor of `dtype` on the current GPU."""
     if t.dtype != dtype or t.shape != (n,) or not t.is_contiguous():
         raise ValueError("%s: contiguous %s [%d]" % (what, dtype, n))
+    if t.get_device() != here:
+        raise ValueError("%s: expected a CUDA tensor of the current device" % what)
+    return t.data_ptr()
 
 
-def _operand(p: Planes, lines: int, what: str):
+def _operand(p: Planes, lines: int, what: str, here: int) -> int:
+    """Address of the C view of planes of at least `lines` lines on the current GPU."""
     if p.lines() < lines:
         raise ValueError("%s: the planes hold fewer than %d lines" % (what, lines))
-    return p._view
+    if not p._on_gpu or p.exps.get_device() != here:
+        raise ValueError("%s: expected CUDA tensors of the current device" % what)
+    return C.addressof(p._view)
 
 
-def _on_current(*tensors) -> None:
-    """All (None: left out) on the GPU that launches go to."""
-    here = torch.cuda.current_device() if torch.cuda.is_available() else None
-    for t in tensors:
-        if t is None:
-            continue
-        if isinstance(t, Planes):
-            t.c()
-            if not t._on_gpu:
-                raise ValueError("expected CUDA tensors")
-            t = t.exps
-        if not t.is_cuda:
-            raise ValueError("expected CUDA tensors")
-        if t.device.index != here:
-            raise ValueError("expected tensors of the current device")
-
-
-def _bytes(t: torch.Tensor) -> int:
+def _scratch(t: torch.Tensor, here: int) -> int:
+    """Bytes of a workspace."""
     if not t.is_contiguous():
         raise ValueError("workspace: expected a contiguous tensor")
-    return t.numel() * t.element_size()
+    if t.get_device() != here:
+        raise ValueError("workspace: expected a CUDA tensor of the current device")
+    return t.nbytes
+
+
+def _here() -> int:
+    """The GPU that launches go to; without one no tensor's device equals it."""
+    if not torch.cuda.is_initialized():
+        if not torch.cuda.is_available():
+            return -2
+        torch.cuda.init()
+    return _raw_device() if _raw_device is not None else torch.cuda.current_device()
 
 
 def mx_gated_gemm_workspace_bytes(M: int, N: int, K: int) -> int:
@@ -630,12 +637,13 @@ def mx_gated_gemm(cfg_a: Config, a: Planes, cfg_w: Config, w: Planes, M: int, N:
                   act: int = ACT_SILU, gate_up: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """h[M,N] (float32 or bfloat16) = act(A Wg^T) * (A Wu^T) for A packed [M, K] and w packed [2 N, K], the N lines of Wg before those
     of Wu.  gate_up: [M, 2 N] of h's type for both products, which mx_gated_gemm_bwd reads."""
-    ca, cw, pa, pw = cfg_a.c(), cfg_w.c(), _operand(a, M, "a"), _operand(w, 2 * N, "w")
-    dt, ldh = _dt(h), _rows(h, M, N, h.dtype, "h")
-    ldg = _rows(gate_up, M, 2 * N, h.dtype, "gate_up") if gate_up is not None else 0
-    _on_current(a, w, h, gate_up, workspace)
-    _check(lib().mx_gated_gemm(C.addressof(ca), C.addressof(pa), C.addressof(cw), C.addressof(pw), M, N, K, act, _ptr(h), dt, ldh,
-                               _ptr(gate_up), ldg, _ptr(workspace), _bytes(workspace), _stream(stream)), "mx_gated_gemm")
+    here, dtype = _here(), h.dtype
+    pa, pw, ldh = _operand(a, M, "a", here), _operand(w, 2 * N, "w", here), _matrix(h, M, N, dtype, "h", here)
+    ldg = _matrix(gate_up, M, 2 * N, dtype, "gate_up", here) if gate_up is not None else 0
+    ca, cw = cfg_a.c(), cfg_w.c()
+    _check(lib().mx_gated_gemm(C.addressof(ca), pa, C.addressof(cw), pw, M, N, K, act, h.data_ptr(), _dt(h), ldh,
+                               gate_up.data_ptr() if ldg else None, ldg, workspace.data_ptr(), _scratch(workspace, here), _stream(stream)),
+           "mx_gated_gemm")
     return h
 
 
@@ -648,15 +656,15 @@ def mx_gated_gemm_bwd(cfg_a: Config, a: Planes, cfg_w: Config, w: Planes, M: int
                       dw: torch.Tensor | None, workspace: torch.Tensor, act: int = ACT_SILU, gate_up: torch.Tensor | None = None, stream=None):
     """Gradients of mx_gated_gemm from dh [M, N]: da [M, K] and dw [2 N, K] of dh's type (None: not wanted).  gate_up: what the forward
     call stored; None: both products are computed again."""
-    ca, cw, pa, pw = cfg_a.c(), cfg_w.c(), _operand(a, M, "a"), _operand(w, 2 * N, "w")
-    dt, ldh = _dt(dh), _rows(dh, M, N, dh.dtype, "dh")
-    ldg = _rows(gate_up, M, 2 * N, dh.dtype, "gate_up") if gate_up is not None else 0
-    lda = _rows(da, M, K, dh.dtype, "da") if da is not None else 0
-    ldw = _rows(dw, 2 * N, K, dh.dtype, "dw") if dw is not None else 0
-    _on_current(a, w, dh, gate_up, da, dw, workspace)
-    _check(lib().mx_gated_gemm_bwd(C.addressof(ca), C.addressof(pa), C.addressof(cw), C.addressof(pw), M, N, K, act, _ptr(dh), dt, ldh,
-                                   _ptr(gate_up), ldg, _ptr(da), lda, _ptr(dw), ldw, _ptr(workspace), _bytes(workspace), _stream(stream)),
-           "mx_gated_gemm_bwd")
+    here, dtype = _here(), dh.dtype
+    pa, pw, ldh = _operand(a, M, "a", here), _operand(w, 2 * N, "w", here), _matrix(dh, M, N, dtype, "dh", here)
+    ldg = _matrix(gate_up, M, 2 * N, dtype, "gate_up", here) if gate_up is not None else 0
+    lda = _matrix(da, M, K, dtype, "da", here) if da is not None else 0
+    ldw = _matrix(dw, 2 * N, K, dtype, "dw", here) if dw is not None else 0
+    ca, cw = cfg_a.c(), cfg_w.c()
+    _check(lib().mx_gated_gemm_bwd(C.addressof(ca), pa, C.addressof(cw), pw, M, N, K, act, dh.data_ptr(), _dt(dh), ldh,
+                                   gate_up.data_ptr() if ldg else None, ldg, da.data_ptr() if lda else None, lda, dw.data_ptr() if ldw else None, ldw,
+                                   workspace.data_ptr(), _scratch(workspace, here), _stream(stream)), "mx_gated_gemm_bwd")
     return da, dw
 
 
@@ -668,13 +676,12 @@ def mx_cross_entropy(cfg_a: Config, a: Planes, cfg_w: Config, w: Planes, M: int,
                      lse: torch.Tensor, workspace: torch.Tensor, stream=None):
     """loss and lse (float32 [M]) of the logits A W^T, which are not stored, for A packed [M, K] and w packed [V, K]; targets: int64
     [M], negative = the row does not count (loss 0)."""
-    ca, cw, pa, pw = cfg_a.c(), cfg_w.c(), _operand(a, M, "a"), _operand(w, V, "w")
-    _vector(targets, M, torch.int64, "targets")
-    _vector(loss, M, torch.float32, "loss")
-    _vector(lse, M, torch.float32, "lse")
-    _on_current(a, w, targets, loss, lse, workspace)
-    _check(lib().mx_cross_entropy(C.addressof(ca), C.addressof(pa), C.addressof(cw), C.addressof(pw), M, V, K, _ptr(targets), _ptr(loss),
-                                  _ptr(lse), _ptr(workspace), _bytes(workspace), _stream(stream)), "mx_cross_entropy")
+    here = _here()
+    pa, pw = _operand(a, M, "a", here), _operand(w, V, "w", here)
+    t, x, y = _vector(targets, M, torch.int64, "targets", here), _vector(loss, M, torch.float32, "loss", here), _vector(lse, M, torch.float32, "lse", here)
+    ca, cw = cfg_a.c(), cfg_w.c()
+    _check(lib().mx_cross_entropy(C.addressof(ca), pa, C.addressof(cw), pw, M, V, K, t, x, y, workspace.data_ptr(), _scratch(workspace, here),
+                                  _stream(stream)), "mx_cross_entropy")
     return loss, lse
 
 
@@ -687,19 +694,16 @@ def mx_cross_entropy_bwd(cfg_a: Config, a: Planes, cfg_w: Config, w: Planes, M: 
                          dloss: torch.Tensor, da: torch.Tensor | None, dw: torch.Tensor | None, workspace: torch.Tensor, stream=None):
     """Gradients of mx_cross_entropy from dloss (float32 [M]) and the forward call's lse: da [M, K] and dw [V, K], both float32 or both
     bfloat16 (None: not wanted)."""
-    ca, cw, pa, pw = cfg_a.c(), cfg_w.c(), _operand(a, M, "a"), _operand(w, V, "w")
-    _vector(targets, M, torch.int64, "targets")
-    _vector(lse, M, torch.float32, "lse")
-    _vector(dloss, M, torch.float32, "dloss")
-    dtype = (da if da is not None else dw).dtype if da is not None or dw is not None else torch.float32
-    lda = _rows(da, M, K, dtype, "da") if da is not None else 0
-    ldw = _rows(dw, V, K, dtype, "dw") if dw is not None else 0
-    dt = F32 if dtype == torch.float32 else BF16
-    if dtype not in (torch.float32, torch.bfloat16):
-        raise TypeError("tensor dtype must be float32 or bfloat16")
-    _on_current(a, w, targets, lse, dloss, da, dw, workspace)
-    _check(lib().mx_cross_entropy_bwd(C.addressof(ca), C.addressof(pa), C.addressof(cw), C.addressof(pw), M, V, K, _ptr(targets), _ptr(lse),
-                                      _ptr(dloss), _ptr(da), lda, _ptr(dw), ldw, dt, _ptr(workspace), _bytes(workspace), _stream(stream)),
+    here = _here()
+    pa, pw = _operand(a, M, "a", here), _operand(w, V, "w", here)
+    t, x, y = _vector(targets, M, torch.int64, "targets", here), _vector(lse, M, torch.float32, "lse", here), _vector(dloss, M, torch.float32, "dloss", here)
+    first = da if da is not None else dw
+    dt, dtype = (_dt(first), first.dtype) if first is not None else (F32, None)
+    lda = _matrix(da, M, K, dtype, "da", here) if da is not None else 0
+    ldw = _matrix(dw, V, K, dtype, "dw", here) if dw is not None else 0
+    ca, cw = cfg_a.c(), cfg_w.c()
+    _check(lib().mx_cross_entropy_bwd(C.addressof(ca), pa, C.addressof(cw), pw, M, V, K, t, x, y, da.data_ptr() if lda else None, lda,
+                                      dw.data_ptr() if ldw else None, ldw, dt, workspace.data_ptr(), _scratch(workspace, here), _stream(stream)),
            "mx_cross_entropy_bwd")
     return da, dw
 

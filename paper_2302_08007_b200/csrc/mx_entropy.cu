@@ -1,7 +1,7 @@
 // Softmax cross entropy over a vocabulary, from packed hidden states A [M, K] and packed vocabulary weights W [V, K]: with l = A W^T,
 //     lse_i = log sum_j exp(l_ij),   loss_i = lse_i - l_i,t_i      (rows whose target is negative do not count: loss 0, no gradient)
 //     d_ij = dloss_i (exp(l_ij - lse_i) - [j = t_i]),   dA = d W,   dW = d^T A
-// The logits are never stored.  Forward: the epilogue of the product reduces a row's 128 columns to their maximum and their sum of
+// The logits of a batch are never stored.  Forward: the epilogue of the product reduces a row's 128 columns to their maximum and their sum of
 // exponentials (fp32), which a second kernel joins; the thread that meets a row's target column writes that logit.  Backward: pieces of
 // the vocabulary, each computed again, turned into d (bf16, or three bf16 parts) by the epilogue, and multiplied with W and A by the two
 // products of mx_grad_gemm.cu; dA is summed over the pieces in fp32, in order.
@@ -113,6 +113,41 @@ struct EntropyJob {
     }
 };
 
+// Few rows: their logits come from the few-token kernel, [M][pitch] fp32.  A block reduces kChunk columns of a row as the epilogue above does.
+constexpr int kChunk = 2048;
+__global__ void __launch_bounds__(256) entropy_rows_kernel(const float* logits, int64_t pitch, int64_t M, int64_t V, const int64_t* targets, float2* parts, float* hit) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int64_t row = blockIdx.y, col0 = (int64_t)blockIdx.x * kChunk;
+    const float* const l = logits + row * pitch;
+    float v[kChunk / 256];
+    float m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kChunk / 256; ++i) {
+        const int64_t col = col0 + 256 * i + threadIdx.x;
+        v[i] = col < V ? l[col] : -INFINITY;
+        m = fmaxf(m, v[i]);
+    }
+    __shared__ float shared[2][8];
+    for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+    if ((threadIdx.x & 31) == 0) shared[0][threadIdx.x >> 5] = m;
+    __syncthreads();
+    for (int i = 0; i < 8; ++i) m = fmaxf(m, shared[0][i]);
+    const float ref = m == -INFINITY ? 0.f : m;
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < kChunk / 256; ++i) s += exp2_of((v[i] - ref) * kLog2e);
+    for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
+    if ((threadIdx.x & 31) == 0) shared[1][threadIdx.x >> 5] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        s = 0.f;
+        for (int i = 0; i < 8; ++i) s += shared[1][i];
+        parts[(int64_t)blockIdx.x * M + row] = make_float2(m, s);
+        const int64_t t = targets[row];
+        if (t >= col0 && t < col0 + kChunk && t < V) hit[row] = l[t];
+    }
+}
+
 // Joins a row's maxima and sums: 32 rows per block, their pieces shared out to 32 warps.
 __global__ void __launch_bounds__(1024) entropy_join_kernel(const float2* parts, int n_parts, int64_t M, const float* hit, const int64_t* targets,
                                                             int64_t V, float* loss, float* lse, int* status) {
@@ -150,6 +185,10 @@ __global__ void __launch_bounds__(1024) entropy_scale_kernel(const float* dloss,
     for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
     if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = m;
     __syncthreads();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    // It runs beside the decoding in front of it, on which it does not depend, and does not finish before it: whoever waits for this kernel has
+    // the decoded operands too.
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     if (threadIdx.x < 32) {
         m = shared[threadIdx.x];
         for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
@@ -173,8 +212,8 @@ struct EntropySpace {
         pitch_k = line_pitch(K);
         piece = piece_columns(V, kMostWeights / (pitch_k * 2));
         a = 0;
-        w = a + round_up(M * pitch_k * 2, 256);
-        parts = w + round_up(std::min(piece, V) * pitch_k * 2, 256);
+        w = a + round_up(M * pitch_k * 2, 256);  // few rows: their logits instead
+        parts = w + (M <= kFewRows ? round_up(M * round_up(V, 64) * 4, 256) : round_up(std::min(piece, V) * pitch_k * 2, 256));
         hit = parts + round_up((V + 31) / 32 * M * 8, 256);
         bytes = hit + round_up(M * 4, 256);
     }
@@ -252,6 +291,19 @@ int mx_cross_entropy(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bdr
     if ((uintptr_t)workspace % 256) return BDR_ERR_MISALIGNED;
     cudaStream_t st = (cudaStream_t)stream;
     uint8_t* const ws = static_cast<uint8_t*>(workspace);
+    if (M <= kFewRows) {
+        __nv_bfloat16* const x = reinterpret_cast<__nv_bfloat16*>(ws + s.a);
+        float *const logits = reinterpret_cast<float*>(ws + s.w), *const hit = reinterpret_cast<float*>(ws + s.hit);
+        float2* const parts = reinterpret_cast<float2*>(ws + s.parts);
+        int* const status = device_status_word();
+        if (!status) return BDR_ERR_CUDA;
+        const int64_t pitch = round_up(V, 64), chunks = (V + kChunk - 1) / kChunk;
+        if ((rc = decode_pair(*a, cfg_a->m, M, x, *w, cfg_w->m, 0, nullptr, K, s.pitch_k, st))) return rc;
+        if ((rc = mx_gemv(cfg_w, w, V, K, x, BDR_BF16, s.pitch_k, M, logits, BDR_F32, pitch, stream))) return rc;
+        entropy_rows_kernel<<<dim3((unsigned)chunks, (unsigned)M), 256, 0, st>>>(logits, pitch, M, V, targets, parts, hit);
+        if (cudaGetLastError() != cudaSuccess) return BDR_ERR_CUDA;
+        return launch_dependent(entropy_join_kernel, dim3(1), dim3(1024), st, (const float2*)parts, (int)chunks, M, (const float*)hit, targets, V, loss, lse, status);
+    }
     EntropyJob<false>::Params p = {};
     p.targets = targets;
     p.vocab = V;
@@ -324,12 +376,12 @@ int mx_cross_entropy_bwd(const bdr_config_t* cfg_a, const bdr_planes_t* a, const
     g.ld_acc = s.pitch_k;
     g.sums = reinterpret_cast<float*>(ws + s.sums);
     g.scale = p.largest = reinterpret_cast<const float*>(ws + s.largest);
-    entropy_scale_kernel<<<1, 1024, 0, st>>>(dloss, targets, M, V, reinterpret_cast<float*>(ws + s.largest));
-    if (cudaGetLastError() != cudaSuccess) return BDR_ERR_CUDA;
     __nv_bfloat16 *const wa = reinterpret_cast<__nv_bfloat16*>(ws + s.a), *const ww = reinterpret_cast<__nv_bfloat16*>(ws + s.w);
     for (int64_t v = 0; v < V; v += s.piece) {
         const int64_t cols = std::min(s.piece, V - v);
         if ((rc = decode_pair(*a, cfg_a->m, v == 0 ? M : 0, wa, lines_from(*w, v), cfg_w->m, cols, ww, K, s.pitch_k, st))) return rc;
+        if (v == 0 && (rc = launch_dependent(entropy_scale_kernel, dim3(1), dim3(1024), st, dloss, targets, M, V, reinterpret_cast<float*>(ws + s.largest))))
+            return rc;
         if ((rc = set_piece(p, M, K, v, cols, s.pitch_k, ws + s.a, ws + s.w))) return rc;
         if ((rc = fused::launch<EntropyJob<true>>(p, st))) return rc;
         g.N = cols;

@@ -58,6 +58,14 @@ struct GradProducts {
 int64_t grad_sums_bytes(int64_t M, int64_t N, int64_t K, int segs);
 int launch_grad_products(const GradProducts& g, cudaStream_t st);
 
+// The gated layer of a few rows of bf16 x (mx_gated_gemv), with both products stored where `products` is not NULL.
+int gated_rows(const bdr_config_t* cfg_w, const bdr_planes_t* w, int64_t N, int64_t K, const __nv_bfloat16* x, int64_t ldx, int64_t T, int act, void* h,
+               bdr_dtype_t dt, int64_t ldh, void* products, int64_t ld_products, cudaStream_t st);
+
+// Rows up to which a product is left to the few-token kernel, which reads the packed weights, instead of decoding them for the tensor-core
+// kernel, which would multiply 256 rows all the same.
+constexpr int64_t kFewRows = 32;
+
 // What the operators accept of two packed operands A [M, K] and W [lines, K] (host).
 int check_fused_operands(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bdr_config_t* cfg_w, const bdr_planes_t* w, int64_t K);
 

@@ -29,7 +29,7 @@ namespace bdr {
 namespace fused {
 
 constexpr int kRows = 128;                          // rows of A, and columns of B, per CTA
-constexpr int kStages = 6;
+constexpr int kStages = 6, kMostStages = 9;          // of 256 columns; narrower ones leave room for more, and a ring's turn takes the same time
 constexpr int kOperandBytes = kRows * kBK * 2;      // 16 KB
 constexpr int kStageBytes = 2 * kOperandBytes;
 constexpr int kEpiWarps = 8;
@@ -38,7 +38,7 @@ constexpr int kTileBytes = 32 * 64;                 // of an epilogue warp, see 
 constexpr size_t kSmem = (size_t)kStages * kStageBytes + kEpiWarps * kTileBytes + 1024 /*bookkeeping*/ + 1024 /*alignment*/;
 
 struct Bars {
-    uint64_t full[kStages], full_local[kStages], empty[kStages], tmem_full[2], tmem_empty[2];
+    uint64_t full[kMostStages], full_local[kMostStages], empty[kMostStages], tmem_full[2], tmem_empty[2];
     uint32_t tmem_base;
     int failed;
 };
@@ -74,9 +74,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();
     const int cluster_id = blockIdx.x >> 1, n_clusters = gridDim.x >> 1;
+    const int stage_bytes = kOperandBytes + 64 * p.bn, n_stages = min(kMostStages, kStages * kStageBytes / stage_bytes);
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kStages; ++s) {
+        for (int s = 0; s < kMostStages; ++s) {
             mbar_init(&bars.full[s], 2);        // leader: its own TMA bytes (arrive.expect_tx) + the peer's relay
             mbar_init(&bars.full_local[s], 1);  // peer: its own TMA bytes
             mbar_init(&bars.empty[s], 1);       // multicast commit of the MMAs that read the stage
@@ -104,30 +105,31 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
         if (lane == 0) {
             uint64_t* const my_full = rank == 0 ? bars.full : bars.full_local;
             bool ok = true;
-            uint32_t it = 0;
+            int stage = 0, turn = 0;  // of the ring
             for (int i = cluster_id; i < p.n_items && ok; i += n_clusters) {
                 const typename Job::Item item = Job::item(p, i);
-                for (int kk = 0; kk < item.steps; ++kk, ++it) {
-                    const int stage = it % kStages;
-                    if (it >= kStages) {
-                        ok = mbar_wait(&bars.empty[stage], ((it / kStages) - 1) & 1);
+                for (int kk = 0; kk < item.steps; ++kk) {
+                    if (turn > 0) {
+                        ok = mbar_wait(&bars.empty[stage], (turn - 1) & 1);
                         if (!ok) break;
                     }
-                    mbar_expect_tx(&my_full[stage], kOperandBytes + 64 * p.bn);
-                    Job::load(p, item, kk, (int)rank, stages + stage * kStageBytes, &my_full[stage]);
+                    mbar_expect_tx(&my_full[stage], stage_bytes);
+                    Job::load(p, item, kk, (int)rank, stages + stage * stage_bytes, &my_full[stage]);
+                    if (++stage == n_stages) { stage = 0; ++turn; }
                 }
             }
             if (!ok) {
                 bars.failed = 1;
                 // the copies still on their way: one more bounded wait for each
-                for (uint32_t j = it < kStages ? 0 : it - kStages; j < it; ++j) mbar_wait(&my_full[j % kStages], (j / kStages) & 1);
+                for (int s = 0; s < n_stages; ++s)
+                    if (s < stage || turn > 0) mbar_wait(&my_full[s], (s < stage ? turn : turn - 1) & 1);
             }
         }
         __syncwarp();
     } else if (warp == 1) {
         if (lane == 0) {
             bool ok = true;
-            uint32_t it = 0;
+            int stage = 0, turn = 0;
             if (rank == 0) {
                 int tcount = 0;
                 for (int i = cluster_id; i < p.n_items && ok; i += n_clusters, ++tcount) {
@@ -139,7 +141,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
                     const int span = Job::kSpan ? Job::kSpan : item.steps;
                     int buf = 0, left = 0;  // K steps that the current buffer still takes
                     uint32_t acc = 0;
-                    for (int kk = 0; kk < item.steps; ++kk, ++it, --left) {
+                    for (int kk = 0; kk < item.steps; ++kk, --left) {
                         if (left == 0) {
                             if (kk > 0) { umma_commit2(&bars.tmem_full[buf]); ++tcount; }
                             left = span;
@@ -151,27 +153,27 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
                                 tc_fence_after();
                             }
                         }
-                        const int stage = it % kStages;
-                        ok = mbar_wait_cluster(&bars.full[stage], (it / kStages) & 1);
+                        ok = mbar_wait_cluster(&bars.full[stage], turn & 1);
                         if (!ok) break;
                         tc_fence_after();
-                        const uint32_t sa = smem_u32(stages + stage * kStageBytes), sb = sa + kOperandBytes;
+                        const uint32_t sa = smem_u32(stages + stage * stage_bytes), sb = sa + kOperandBytes;
                         const uint64_t da = a_mn ? make_mn_desc(sa) : make_smem_desc(sa);
                         const uint64_t db = Job::b_mn ? make_mn_desc(sb) : make_smem_desc(sb);
 #pragma unroll
                         for (int k = 0; k < kBK / 16; ++k) umma2_bf16(acc, da + k * a_step, db + k * b_step, idesc, left != span || k != 0);
                         umma_commit2(&bars.empty[stage]);
+                        if (++stage == n_stages) { stage = 0; ++turn; }
                     }
                     if (ok) umma_commit2(&bars.tmem_full[buf]);
                 }
             } else {
                 for (int i = cluster_id; i < p.n_items && ok; i += n_clusters) {
                     const typename Job::Item item = Job::item(p, i);
-                    for (int kk = 0; kk < item.steps; ++kk, ++it) {
-                        const int stage = it % kStages;
-                        ok = mbar_wait(&bars.full_local[stage], (it / kStages) & 1);
+                    for (int kk = 0; kk < item.steps; ++kk) {
+                        ok = mbar_wait(&bars.full_local[stage], turn & 1);
                         if (!ok) break;
                         mbar_arrive_cluster(&bars.full[stage], 0);
+                        if (++stage == n_stages) { stage = 0; ++turn; }
                     }
                 }
             }
@@ -219,11 +221,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
                     const int buf = tcount & 1;
                     if (!next(buf)) break;
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        uint32_t u[32];
-                        tmem_ld32(tmem_base + my_lanes + (uint32_t)(buf * 256 + e.half * 128 + 32 * q), u);
+                    for (int q = 0; q < 8; ++q) {  // sixteen columns at a time: more would not fit beside the sums
+                        uint32_t u[16];
+                        tmem_ld16(tmem_base + my_lanes + (uint32_t)(buf * 256 + e.half * 128 + 16 * q), u);
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[q][j] += __uint_as_float(u[j]);
+                        for (int j = 0; j < 16; ++j) v[q >> 1][16 * (q & 1) + j] += __uint_as_float(u[j]);
                     }
                     done(buf);
                 }
@@ -454,7 +456,7 @@ __device__ __forceinline__ void store_parts(const Epi& e, const Rows& d, int64_t
     }
 }
 
-// Columns of an accumulator for a product of tiles_m x cols (cols_per of the product's columns per accumulator column): the fewest K steps
+// Columns of an accumulator for a product of tiles_m x cols (cols_div accumulator columns for each of the product's): the fewest K steps
 // in a row, weighed with what a step takes.  A step moves 16 KB of A and bn / 2 columns of B into an SM at about 64 bytes a clock and
 // multiplies for 2 bn clocks; an item's start and epilogue take about 1500 clocks that nothing hides when it is its cluster's only one.
 inline int pick_bn(int64_t tiles_m, int64_t cols, int cols_div, int64_t steps, int clusters) {

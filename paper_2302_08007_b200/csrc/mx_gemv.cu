@@ -33,6 +33,7 @@
 #include "bdr_host.h"
 #include "mx_act.cuh"
 #include "mx_frag.cuh"
+#include "mx_fused.h"
 
 namespace bdr {
 
@@ -75,6 +76,8 @@ struct GemvArgs {
     int rounds;          // of the groups over all tiles, rounded down; the first `rest` CTAs have one more
     unsigned rest;
     int act;             // GATED: the activation
+    void* products;      // GATED: NULL, or where both products go, [tokens][2 n] of y's type
+    int64_t ld_products;
     int phase_steps;     // steps whose activations are in shared memory at once: all, or a multiple of kw in each of two buffers
 };
 
@@ -456,7 +459,20 @@ __global__ void __launch_bounds__((GemvShape<W, NT, WARPS>::kThreads), 1) mx_gem
                 return v * 2.f;  // the operand was decoded halved
             };
             float v = total(r);
-            if constexpr (GATED) act::with(a.act, [&](auto f) { v = act::of<decltype(f)::value>(v) * total(r + 8); });
+            if constexpr (GATED) {
+                const float u = total(r + 8);
+                if (a.products) {
+                    const int64_t to = (int64_t)(t0 + t) * a.ld_products + kOut * tile + r;
+                    if (a.y32) {
+                        static_cast<float*>(a.products)[to] = v;
+                        static_cast<float*>(a.products)[to + a.n] = u;
+                    } else {
+                        static_cast<__nv_bfloat16*>(a.products)[to] = __float2bfloat16_rn(v);
+                        static_cast<__nv_bfloat16*>(a.products)[to + a.n] = __float2bfloat16_rn(u);
+                    }
+                }
+                act::with(a.act, [&](auto f) { v = act::of<decltype(f)::value>(v) * u; });
+            }
             const int64_t at = (int64_t)(t0 + t) * a.ldy + kOut * tile + r;
             if (a.y32) static_cast<float*>(a.y)[at] = v;
             else static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(v);
@@ -524,7 +540,7 @@ using namespace bdr;
 // mx_gemv, and the gated layer, whose W has 2 N lines
 template <bool GATED>
 static int run_gemv(const bdr_config_t* cfg_w, const bdr_planes_t* w, int64_t N, int64_t K, const void* x, bdr_dtype_t x_dt,
-                    int64_t ldx, int64_t T, int act, void* y, bdr_dtype_t y_dt, int64_t ldy, void* stream) {
+                    int64_t ldx, int64_t T, int act, void* y, bdr_dtype_t y_dt, int64_t ldy, void* products, int64_t ld_products, void* stream) {
     int rc = check_table2_config(cfg_w);
     if (rc) return rc;
     if (GATED && !act::known(act)) return BDR_ERR_UNSUPPORTED;
@@ -542,7 +558,7 @@ static int run_gemv(const bdr_config_t* cfg_w, const bdr_planes_t* w, int64_t N,
         a.w = *w;
     }
     a.x = x; a.y = y; a.ldx = ldx; a.ldy = ldy; a.n = N; a.k = K; a.tokens = (int)T;
-    a.act = act;
+    a.act = act; a.products = products; a.ld_products = ld_products;
     a.x32 = x_dt == BDR_F32; a.y32 = y_dt == BDR_F32;
     const int64_t xb = a.x32 ? 4 : 2;
     const uintptr_t at = (uintptr_t)x | (T == 1 ? 0 : (uintptr_t)(ldx * xb));
@@ -558,10 +574,17 @@ static int run_gemv(const bdr_config_t* cfg_w, const bdr_planes_t* w, int64_t N,
 
 extern "C" int mx_gemv(const bdr_config_t* cfg_w, const bdr_planes_t* w, int64_t N, int64_t K, const void* x, bdr_dtype_t x_dt,
                        int64_t ldx, int64_t T, void* y, bdr_dtype_t y_dt, int64_t ldy, void* stream) {
-    return run_gemv<false>(cfg_w, w, N, K, x, x_dt, ldx, T, 0, y, y_dt, ldy, stream);
+    return run_gemv<false>(cfg_w, w, N, K, x, x_dt, ldx, T, 0, y, y_dt, ldy, nullptr, 0, stream);
 }
 
 extern "C" int mx_gated_gemv(const bdr_config_t* cfg_w, const bdr_planes_t* w, int64_t N, int64_t K, const void* x, bdr_dtype_t x_dt,
                              int64_t ldx, int64_t T, int32_t act, void* h, bdr_dtype_t h_dt, int64_t ldh, void* stream) {
-    return run_gemv<true>(cfg_w, w, N, K, x, x_dt, ldx, T, act, h, h_dt, ldh, stream);
+    return run_gemv<true>(cfg_w, w, N, K, x, x_dt, ldx, T, act, h, h_dt, ldh, nullptr, 0, stream);
 }
+
+namespace bdr {
+int gated_rows(const bdr_config_t* cfg_w, const bdr_planes_t* w, int64_t N, int64_t K, const __nv_bfloat16* x, int64_t ldx, int64_t T, int act, void* h,
+               bdr_dtype_t dt, int64_t ldh, void* products, int64_t ld_products, cudaStream_t st) {
+    return run_gemv<true>(cfg_w, w, N, K, x, BDR_BF16, ldx, T, act, h, dt, ldh, products, ld_products, st);
+}
+}  // namespace bdr
