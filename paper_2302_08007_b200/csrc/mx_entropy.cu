@@ -8,6 +8,7 @@
 #include <algorithm>
 
 #include "mx_frag.cuh"
+#include "mx_fused_f8.cuh"
 #include "mx_fused_gemm.cuh"
 
 namespace bdr {
@@ -40,6 +41,8 @@ struct EntropyJob {
         Rows d;                   // [n_parts][M][piece]
         int64_t vocab;
         int n_parts;
+        fused::F8 f8;             // 8-bit operands, where they are used
+        const int* gate;
         int* status;
     };
     struct Item { int steps, tm, tn; };
@@ -56,60 +59,98 @@ struct EntropyJob {
         tma_load_3d(dst, &p.a, kk * kBK, (it.tm * 2 + rank) * kRows, 0, bar);
         tma_load_3d(dst + fused::kOperandBytes, &p.w, kk * kBK, it.tn * p.bn + rank * (p.bn >> 1), 0, bar);
     }
-    static __device__ __forceinline__ void epilogue(const Params& p, const Item& it, const fused::Epi& e) {
-        const int64_t row0 = (int64_t)it.tm * 256 + e.r0, row = row0 + e.lane;
-        const int width = p.bn >> 1, first = it.tn * p.bn + e.half * width;  // columns in the piece
-        const bool live = row < p.M;
-        const int64_t target = live ? p.targets[row] : -1;
-        const int64_t at = target - p.col0 - first;  // column of the target among these
-        if constexpr (!GRAD) {
-            float top = -INFINITY, sum = 0.f;
-#pragma unroll 1
-            for (int c = 0; c < width; c += 32) {
-                __syncwarp();
-                uint32_t u[32];
-                tmem_ld32(e.tmem + (uint32_t)(e.half * width + c), u);
-                float v[32];
-                const int n = p.cols - first - c;
-#pragma unroll
-                for (int j = 0; j < 32; ++j) v[j] = j < n ? __uint_as_float(u[j]) : -INFINITY;
-                if (at >= c && at < c + 32 && at < c + n) {
-                    float x = 0.f;
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) x = at - c == j ? v[j] : x;
-                    p.hit[row] = x;
-                }
-                float m = v[0];
-#pragma unroll
-                for (int j = 1; j < 32; ++j) m = fmaxf(m, v[j]);
-                m = fmaxf(m, top);
-                const float ref = m == -INFINITY ? 0.f : m;  // nothing yet: every term is zero (a NaN among the terms stays one)
-                float s = sum * exp2_of((top - ref) * kLog2e);
-#pragma unroll
-                for (int j = 0; j < 32; ++j) s += exp2_of((v[j] - ref) * kLog2e);
-                top = m;
-                sum = s;
-            }
-            if (live && first < p.cols) p.parts[(p.col0 + first) / width * p.M + row] = make_float2(top, sum);
+    static __device__ __forceinline__ void load8(const Params& p, const Item& it, int kk, int rank, uint8_t* dst, uint64_t* bar) {
+        tma_load_3d(dst, &p.f8.a, kk * fused::kK8, (it.tm * 2 + rank) * kRows, 0, bar);
+        tma_load_3d(dst + kRows * fused::kK8, &p.f8.w, kk * fused::kK8, (it.tn * 2 + rank) * kRows, 0, bar);
+        uint8_t* const sf = dst + fused::kTiles8;
+        bulk_load_g2s(sf, p.f8.sf_a + ((int64_t)kk * p.f8.row_tiles_a + it.tm * 2 + rank) * 512, 512, bar);
+        bulk_load_g2s(sf + 512, p.f8.sf_w + ((int64_t)kk * p.f8.row_tiles_w + it.tn * 2) * 512, 1024, bar);
+    }
+    static __device__ __forceinline__ int column(int half, int q) { return half * 128 + 32 * q; }
+
+    // What a thread knows of its row, and of the columns of its half.
+    struct Row {
+        int64_t row0, row, at;   // of the warp, of the lane; the target's column among these
+        int width, first, rows;  // columns, the first in the piece; rows of the warp that are there
+        bool live, counts;
+        float lse, scale;        // GRAD
+        float top, sum;          // else: so far
+    };
+    static __device__ __forceinline__ Row begin(const Params& p, const Item& it, const fused::Epi& e) {
+        Row r;
+        r.row0 = (int64_t)it.tm * 256 + e.r0;
+        r.row = r.row0 + e.lane;
+        r.width = p.bn >> 1;
+        r.first = it.tn * p.bn + e.half * r.width;
+        r.rows = (int)min((int64_t)32, p.M - r.row0);
+        r.live = r.row < p.M;
+        const int64_t target = r.live ? p.targets[r.row] : -1;
+        r.at = target - p.col0 - r.first;
+        r.counts = target >= 0 && target < p.vocab;
+        if constexpr (GRAD) {
+            r.lse = r.live ? p.lse[r.row] : 0.f;
+            r.scale = r.live ? p.dloss[r.row] / *p.largest : 0.f;
         } else {
-            const float lse = live ? p.lse[row] : 0.f, scale = live ? p.dloss[row] / *p.largest : 0.f;
-            const bool counts = target >= 0 && target < p.vocab;
-            const int rows = (int)min((int64_t)32, p.M - row0);
-#pragma unroll 1
-            for (int c = 0; c < width; c += 32) {
-                __syncwarp();
-                uint32_t u[32];
-                tmem_ld32(e.tmem + (uint32_t)(e.half * width + c), u);
-                if (rows <= 0 || first + c >= p.cols) continue;  // (the same for the whole warp)
-                float v[32];
-#pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    const float x = exp2_of((__uint_as_float(u[j]) - lse) * kLog2e) - (at - c == j ? 1.f : 0.f);
-                    v[j] = counts ? scale * x : 0.f;
-                }
-                fused::store_parts(e, p.d, p.M, row0, first + c, rows, p.n_parts, v);
-            }
+            r.top = -INFINITY;
+            r.sum = 0.f;
         }
+        return r;
+    }
+    // 32 logits of every row, from column c of the half
+    static __device__ __forceinline__ void take(const Params& p, const fused::Epi& e, Row& r, int c, float (&v)[32]) {
+        const int n = p.cols - r.first - c;
+        if constexpr (!GRAD) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = j < n ? v[j] : -INFINITY;
+            if (r.at >= c && r.at < c + 32 && r.at < c + n) {
+                float x = 0.f;
+#pragma unroll
+                for (int j = 0; j < 32; ++j) x = r.at - c == j ? v[j] : x;
+                p.hit[r.row] = x;
+            }
+            float m = v[0];
+#pragma unroll
+            for (int j = 1; j < 32; ++j) m = fmaxf(m, v[j]);
+            m = fmaxf(m, r.top);
+            const float ref = m == -INFINITY ? 0.f : m;  // nothing yet: every term is zero (a NaN among the terms stays one)
+            float s = r.sum * exp2_of((r.top - ref) * kLog2e);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) s += exp2_of((v[j] - ref) * kLog2e);
+            r.top = m;
+            r.sum = s;
+        } else {
+            if (r.rows <= 0 || n <= 0) return;  // (the same for the whole warp)
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+                const float x = exp2_of((v[j] - r.lse) * kLog2e) - (r.at - c == j ? 1.f : 0.f);
+                v[j] = r.counts ? r.scale * x : 0.f;
+            }
+            fused::store_parts(e, p.d, p.M, r.row0, r.first + c, r.rows, p.n_parts, v);
+        }
+    }
+    static __device__ __forceinline__ void end(const Params& p, const Row& r) {
+        if constexpr (!GRAD)
+            if (r.live && r.first < p.cols) p.parts[(p.col0 + r.first) / r.width * p.M + r.row] = make_float2(r.top, r.sum);
+    }
+    static __device__ __forceinline__ void epilogue(const Params& p, const Item& it, const fused::Epi& e) {
+        Row r = begin(p, it, e);
+#pragma unroll 1
+        for (int c = 0; c < r.width; c += 32) {
+            __syncwarp();
+            uint32_t u[32];
+            tmem_ld32(e.tmem + (uint32_t)(e.half * r.width + c), u);
+            float v[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(u[j]);
+            take(p, e, r, c, v);
+        }
+        end(p, r);
+    }
+    static __device__ __forceinline__ void finish(const Params& p, const Item& it, const fused::Epi& e, float (&v)[4][32]) {
+        Row r = begin(p, it, e);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) take(p, e, r, 32 * q, v[q]);
+        end(p, r);
     }
 };
 
@@ -207,19 +248,21 @@ constexpr int64_t kMostWeights = 512ll << 20;   // bytes of decoded weights at a
 constexpr int64_t kMostD = 256ll << 20;         // bytes of d at a time
 
 struct EntropySpace {
-    int64_t pitch_k, piece, a, w, parts, hit, bytes;
+    int64_t pitch_k, piece, a, w, parts, hit, flag, bytes;
     EntropySpace(int64_t M, int64_t V, int64_t K) {
         pitch_k = line_pitch(K);
         piece = piece_columns(V, kMostWeights / (pitch_k * 2));
         a = 0;
         w = a + round_up(M * pitch_k * 2, 256);  // few rows: their logits instead
         parts = w + (M <= kFewRows ? round_up(M * round_up(V, 64) * 4, 256) : round_up(std::min(piece, V) * pitch_k * 2, 256));
+        parts = std::max(parts, fused::f8_bytes(M, std::min(piece, V), K));
         hit = parts + round_up((V + 31) / 32 * M * 8, 256);
-        bytes = hit + round_up(M * 4, 256);
+        flag = hit + round_up(M * 4, 256);
+        bytes = flag + 256;
     }
 };
 struct EntropyGradSpace {
-    int64_t pitch_k, piece, a, w, d, acc, largest, sums, bytes;
+    int64_t pitch_k, piece, a, w, d, acc, largest, sums, f8, flag, bytes;
     EntropyGradSpace(int64_t M, int64_t V, int64_t K, int n_parts) {
         pitch_k = line_pitch(K);
         piece = piece_columns(V, std::min(kMostWeights / (pitch_k * 2), kMostD / (std::max<int64_t>(M, 1) * 2 * n_parts)));
@@ -229,17 +272,19 @@ struct EntropyGradSpace {
         acc = d + round_up(n_parts * M * piece * 2, 256);
         largest = acc + (piece < V ? round_up(M * pitch_k * 4, 256) : 0);
         sums = largest + 256;
-        bytes = sums + grad_sums_bytes(M, std::min(piece, V), K, 1);
+        f8 = sums + grad_sums_bytes(M, std::min(piece, V), K, 1);
+        flag = f8 + (fused::takes_f8(4, 4, M, V, V, K) ? fused::f8_bytes(M, std::min(piece, V), K) : 0);
+        bytes = flag + 256;
     }
 };
 
 constexpr int64_t kMost = 1ll << 30;
 
 template <class Params>
-int set_piece(Params& p, int64_t M, int64_t K, int64_t col0, int64_t cols, int64_t pitch_k, const uint8_t* a, const uint8_t* w) {
+int set_piece(Params& p, int64_t M, int64_t K, int64_t col0, int64_t cols, int64_t pitch_k, const uint8_t* a, const uint8_t* w, bool f8) {
     p.tiles_m = (int)((M + 255) / 256);
     p.steps = (int)((K + kBK - 1) / kBK);
-    if (col0 == 0) p.bn = fused::pick_bn(p.tiles_m, cols, 1, p.steps, sm_count() / 2);  // (the last piece keeps it)
+    if (col0 == 0) p.bn = f8 ? 256 : fused::pick_bn(p.tiles_m, cols, 1, p.steps, sm_count() / 2);  // (the last piece keeps it)
     p.tiles_n = (int)((cols + p.bn - 1) / p.bn);
     if (!fused::make_map(&p.a, a, K, M, 1, pitch_k, M * pitch_k, kRows) || !fused::make_map(&p.w, w, K, cols, 1, pitch_k, cols * pitch_k, p.bn / 2))
         return BDR_ERR_CUDA;
@@ -312,10 +357,17 @@ int mx_cross_entropy(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bdr
     p.status = device_status_word();
     if (!p.status) return BDR_ERR_CUDA;
     __nv_bfloat16 *const wa = reinterpret_cast<__nv_bfloat16*>(ws + s.a), *const ww = reinterpret_cast<__nv_bfloat16*>(ws + s.w);
+    const bool f8 = fused::takes_f8(cfg_a->m, cfg_w->m, M, V, V, K);
     for (int64_t v = 0; v < V; v += s.piece) {
         const int64_t cols = std::min(s.piece, V - v);
-        if ((rc = decode_pair(*a, cfg_a->m, v == 0 ? M : 0, wa, lines_from(*w, v), cfg_w->m, cols, ww, K, s.pitch_k, st))) return rc;
-        if ((rc = set_piece(p, M, K, v, cols, s.pitch_k, ws + s.a, ws + s.w))) return rc;
+        const bdr_planes_t lines = lines_from(*w, v);
+        if ((rc = set_piece(p, M, K, v, cols, s.pitch_k, ws + s.a, ws + s.w, f8))) return rc;
+        if (f8) {  // the bytes lie where the bf16 operands would: those are written only once the 8-bit kernel has found nothing to do
+            if ((rc = fused::encode_f8(*a, cfg_a->m, M, lines, cfg_w->m, cols, 1, K, ws, reinterpret_cast<int*>(ws + s.flag), &p.f8, &p.gate, st))) return rc;
+            if ((rc = fused::launch_f8<EntropyJob<false>>(p, st))) return rc;
+        }
+        // (with an 8-bit path in front, A's bf16 values are overwritten by the next piece's bytes)
+        if ((rc = decode_pair(*a, cfg_a->m, v == 0 || f8 ? M : 0, wa, lines, cfg_w->m, cols, ww, K, s.pitch_k, st, p.gate))) return rc;
         if ((rc = fused::launch<EntropyJob<false>>(p, st))) return rc;
     }
     const int n_parts = (int)((V + p.bn / 2 - 1) / (p.bn / 2));
@@ -377,12 +429,18 @@ int mx_cross_entropy_bwd(const bdr_config_t* cfg_a, const bdr_planes_t* a, const
     g.sums = reinterpret_cast<float*>(ws + s.sums);
     g.scale = p.largest = reinterpret_cast<const float*>(ws + s.largest);
     __nv_bfloat16 *const wa = reinterpret_cast<__nv_bfloat16*>(ws + s.a), *const ww = reinterpret_cast<__nv_bfloat16*>(ws + s.w);
+    const bool f8 = fused::takes_f8(cfg_a->m, cfg_w->m, M, V, V, K);
     for (int64_t v = 0; v < V; v += s.piece) {
         const int64_t cols = std::min(s.piece, V - v);
-        if ((rc = decode_pair(*a, cfg_a->m, v == 0 ? M : 0, wa, lines_from(*w, v), cfg_w->m, cols, ww, K, s.pitch_k, st))) return rc;
+        const bdr_planes_t lines = lines_from(*w, v);
+        if ((rc = decode_pair(*a, cfg_a->m, v == 0 ? M : 0, wa, lines, cfg_w->m, cols, ww, K, s.pitch_k, st))) return rc;
         if (v == 0 && (rc = launch_dependent(entropy_scale_kernel, dim3(1), dim3(1024), st, dloss, targets, M, V, reinterpret_cast<float*>(ws + s.largest))))
             return rc;
-        if ((rc = set_piece(p, M, K, v, cols, s.pitch_k, ws + s.a, ws + s.w))) return rc;
+        if ((rc = set_piece(p, M, K, v, cols, s.pitch_k, ws + s.a, ws + s.w, f8))) return rc;
+        if (f8) {
+            if ((rc = fused::encode_f8(*a, cfg_a->m, M, lines, cfg_w->m, cols, 1, K, ws + s.f8, reinterpret_cast<int*>(ws + s.flag), &p.f8, &p.gate, st))) return rc;
+            if ((rc = fused::launch_f8<EntropyJob<true>>(p, st))) return rc;
+        }
         if ((rc = fused::launch<EntropyJob<true>>(p, st))) return rc;
         g.N = cols;
         g.dw = dw ? static_cast<char*>(dw) + v * ld_dw * width : nullptr;

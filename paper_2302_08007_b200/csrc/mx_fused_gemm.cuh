@@ -8,7 +8,8 @@
 // epilogues mask rows and columns.  Every wait is bounded; one that runs out sets the status word and the role leaves its loop.
 //
 // A Job has
-//   Params                         kernel argument: tensor maps, sizes, n_items, bn (the accumulator's columns), status
+//   Params                         kernel argument: tensor maps, sizes, n_items, bn (the accumulator's columns), status; gate: NULL, or device
+//                                  flag without which the kernel does nothing
 //   Item item(p, i)                work item i of p.n_items; Item::steps is its number of K steps of 64
 //   load(p, it, kk, rank, dst, bar)   TMA loads of K step kk: A at dst, B kOperandBytes behind it, 16384 + 64 bn bytes in all
 //   a_mn(it), b_mn                 whether an operand lies with its rows (M or N) contiguous instead of K
@@ -100,8 +101,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
     // behind may be set up already
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    const bool open = !p.gate || *p.gate != 0;  // the same for every thread of the grid
 
-    if (warp == 0) {
+    if (!open) {
+        // the 8-bit kernel has done it
+    } else if (warp == 0) {
         if (lane == 0) {
             uint64_t* const my_full = rank == 0 ? bars.full : bars.full_local;
             bool ok = true;
@@ -257,6 +261,23 @@ inline bool make_map(CUtensorMap* out, const void* base, int64_t cols, int64_t r
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+template <class Params>
+int launch_clusters(void (*kern)(Params), const Params& p, int threads, size_t smem, cudaStream_t st) {
+    const int n_clusters = p.n_items < sm_count() / 2 ? p.n_items : sm_count() / 2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(2 * n_clusters));
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, p);
+    return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? BDR_OK : BDR_ERR_CUDA;
+}
+
 template <class Job>
 int launch(const typename Job::Params& p, cudaStream_t st) {
     static PerDevice once;
@@ -264,19 +285,7 @@ int launch(const typename Job::Params& p, cudaStream_t st) {
             return cudaFuncSetAttribute(fused_gemm_kernel<Job>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem) == cudaSuccess ? 1 : 0;
         }) < 1)
         return BDR_ERR_CUDA;
-    const int n_clusters = p.n_items < sm_count() / 2 ? p.n_items : sm_count() / 2;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(2 * n_clusters));
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = kSmem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, fused_gemm_kernel<Job>, p);
-    return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? BDR_OK : BDR_ERR_CUDA;
+    return launch_clusters(fused_gemm_kernel<Job>, p, kThreads, kSmem, st);
 }
 
 // ---- epilogue pieces ----------------------------------------------------------------------------------------

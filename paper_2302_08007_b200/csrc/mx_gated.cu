@@ -12,6 +12,7 @@
 
 #include "mx_act.cuh"
 #include "mx_frag.cuh"
+#include "mx_fused_f8.cuh"
 #include "mx_fused_gemm.cuh"
 
 namespace bdr {
@@ -28,9 +29,11 @@ struct GatedJob {
         int n_items, bn, tiles_m, tiles_n, band_rows, steps;
         int M, N, act;
         Rows h;                    // h, or dh
-        Rows gate, up;             // where the two products go (NULL: nowhere)
+        Rows gate_out, up_out;     // where the two products go (NULL: nowhere)
         Rows d;                    // [parts][2][M][pitch]
         int parts;
+        fused::F8 f8;              // 8-bit operands, where they are used
+        const int* gate;
         int* status;
     };
     struct Item { int steps, tm, tn; };
@@ -47,6 +50,54 @@ struct GatedJob {
         tma_load_3d(dst, &p.a, kk * kBK, (it.tm * 2 + rank) * kRows, 0, bar);
         tma_load_3d(dst + fused::kOperandBytes, &p.w, kk * kBK, it.tn * (p.bn >> 1), rank, bar);
     }
+    static __device__ __forceinline__ void load8(const Params& p, const Item& it, int kk, int rank, uint8_t* dst, uint64_t* bar) {
+        tma_load_3d(dst, &p.f8.a, kk * fused::kK8, (it.tm * 2 + rank) * kRows, 0, bar);
+        tma_load_3d(dst + kRows * fused::kK8, &p.f8.w, kk * fused::kK8, it.tn * kRows, rank, bar);
+        uint8_t* const sf = dst + fused::kTiles8;
+        const uint8_t* const w = p.f8.sf_w + ((int64_t)kk * p.f8.row_tiles_w + it.tn) * 512;
+        bulk_load_g2s(sf, p.f8.sf_a + ((int64_t)kk * p.f8.row_tiles_a + it.tm * 2 + rank) * 512, 512, bar);
+        bulk_load_g2s(sf + 512, w, 512, bar);                                            // of the gate
+        bulk_load_g2s(sf + 1024, w + (int64_t)(p.f8.row_tiles_w >> 1) * 512, 512, bar);  // of the other projection
+    }
+    static __device__ __forceinline__ int column(int half, int q) { return (q & 2) * 64 + half * 64 + (q & 1) * 32; }
+    static __device__ __forceinline__ void finish(const Params& p, const Item& it, const fused::Epi& e, float (&v)[4][32]) {
+        const int64_t row = (int64_t)it.tm * 256 + e.r0;
+        const int rows = (int)min((int64_t)32, p.M - row);
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int col = it.tn * kRows + column(e.half, q);
+            one_tile(p, e, row, col, rows, min(32, p.N - col), v[q], v[q + 2]);
+        }
+    }
+    // a warp's 32 x 32 outputs, whose products are g and u
+    static __device__ __forceinline__ void one_tile(const Params& p, const fused::Epi& e, int64_t row, int col, int rows, int n, float (&g)[32], float (&u)[32]) {
+        if (rows <= 0 || n <= 0) return;  // (the same for the whole warp)
+        if constexpr (!GRAD) {
+            if (p.gate_out.p) {
+                fused::store_tile(e, p.gate_out, row, col, rows, n, g);
+                fused::store_tile(e, p.up_out, row, col, rows, n, u);
+            }
+            act::with(p.act, [&](auto f) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) g[j] = act::of<decltype(f)::value>(g[j]) * u[j];
+            });
+            fused::store_tile(e, p.h, row, col, rows, n, g);
+        } else {
+            float dh[32];
+            fused::load_tile(e, p.h, row, col, rows, n, dh);
+            act::with(p.act, [&](auto f) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    float y, slope;
+                    act::both<decltype(f)::value>(g[j], y, slope);
+                    g[j] = dh[j] * u[j] * slope;
+                    u[j] = dh[j] * y;
+                }
+            });
+            fused::store_parts(e, p.d, 2 * (int64_t)p.M, row, col, rows, p.parts, g);
+            fused::store_parts(e, p.d, 2 * (int64_t)p.M, p.M + row, col, rows, p.parts, u);
+        }
+    }
     static __device__ __forceinline__ void epilogue(const Params& p, const Item& it, const fused::Epi& e) {
         const int64_t row = (int64_t)it.tm * 256 + e.r0;
         const int rows = (int)min((int64_t)32, p.M - row), cols = p.bn >> 1;  // half of the accumulator is the gate
@@ -58,35 +109,10 @@ struct GatedJob {
             tmem_ld32_nowait(e.tmem + (uint32_t)(cols + c), gu[1]);
             tmem_ld_wait();
             const int col = it.tn * cols + c, n = min(32, p.N - col);
-            if (rows <= 0 || n <= 0) continue;  // (the same for the whole warp)
             float g[32], u[32];
 #pragma unroll
             for (int j = 0; j < 32; ++j) { g[j] = __uint_as_float(gu[0][j]); u[j] = __uint_as_float(gu[1][j]); }
-            if constexpr (!GRAD) {
-                if (p.gate.p) {
-                    fused::store_tile(e, p.gate, row, col, rows, n, g);
-                    fused::store_tile(e, p.up, row, col, rows, n, u);
-                }
-                act::with(p.act, [&](auto f) {
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) g[j] = act::of<decltype(f)::value>(g[j]) * u[j];
-                });
-                fused::store_tile(e, p.h, row, col, rows, n, g);
-            } else {
-                float dh[32];
-                fused::load_tile(e, p.h, row, col, rows, n, dh);
-                act::with(p.act, [&](auto f) {
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        float y, slope;
-                        act::both<decltype(f)::value>(g[j], y, slope);
-                        g[j] = dh[j] * u[j] * slope;
-                        u[j] = dh[j] * y;
-                    }
-                });
-                fused::store_parts(e, p.d, 2 * (int64_t)p.M, row, col, rows, p.parts, g);
-                fused::store_parts(e, p.d, 2 * (int64_t)p.M, p.M + row, col, rows, p.parts, u);
-            }
+            one_tile(p, e, row, col, rows, n, g, u);
         }
     }
 };
@@ -171,7 +197,7 @@ int launch_gated_grad(const Rows& gate, const Rows& up, const Rows& dh, int act,
 
 // Workspace: A, W and, for gradients, D.
 struct GatedSpace {
-    int64_t pitch_k, pitch_d, a, w, d, sums, bytes;  // offsets in bytes
+    int64_t pitch_k, pitch_d, a, w, d, sums, f8, flag, bytes;  // offsets in bytes
     GatedSpace(int64_t M, int64_t N, int64_t K, int parts) {
         pitch_k = line_pitch(K);
         pitch_d = round_up(N, 64);
@@ -179,7 +205,10 @@ struct GatedSpace {
         w = a + round_up(M * pitch_k * 2, 256);
         d = w + round_up(2 * N * pitch_k * 2, 256);
         sums = d + (parts ? round_up((int64_t)parts * 2 * M * pitch_d * 2, 256) : 0);
-        bytes = sums + (parts ? grad_sums_bytes(M, N, K, 2) : 0);
+        f8 = sums + (parts ? grad_sums_bytes(M, N, K, 2) : 0);
+        // (whether it will be used depends on the formats too; a forward pass keeps the bytes where the bf16 operands would lie)
+        flag = parts ? f8 + (fused::takes_f8(4, 4, M, 2 * N, N, K) ? fused::f8_bytes(M, 2 * N, K) : 0) : std::max(f8, fused::f8_bytes(M, 2 * N, K));
+        bytes = flag + 256;
     }
 };
 
@@ -192,10 +221,10 @@ int check_rows(const void* p, int64_t ld, int64_t cols, int width) {
 }
 
 template <class Params>
-int set_products(Params& p, int64_t M, int64_t N, int64_t K, const GatedSpace& s, uint8_t* ws) {
+int set_products(Params& p, int64_t M, int64_t N, int64_t K, const GatedSpace& s, uint8_t* ws, bool f8) {
     p.tiles_m = (int)((M + 255) / 256);
     p.steps = (int)((K + kBK - 1) / kBK);
-    p.bn = fused::pick_bn(p.tiles_m, N, 2, p.steps, sm_count() / 2);
+    p.bn = f8 ? 256 : fused::pick_bn(p.tiles_m, N, 2, p.steps, sm_count() / 2);
     p.tiles_n = (int)((N + p.bn / 2 - 1) / (p.bn / 2));
     if (!fused::make_map(&p.a, ws + s.a, K, M, 1, s.pitch_k, M * s.pitch_k, kRows) ||
         !fused::make_map(&p.w, ws + s.w, K, N, 2, s.pitch_k, N * s.pitch_k, p.bn / 2))
@@ -244,15 +273,20 @@ int mx_gated_gemm(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bdr_co
         if ((rc = decode_pair(*a, cfg_a->m, M, x, *w, cfg_w->m, 0, nullptr, K, s.pitch_k, st))) return rc;
         return gated_rows(cfg_w, w, N, K, x, s.pitch_k, M, act, h, dt, ldh, gate_up, ld_gate_up, st);
     }
-    if ((rc = decode_pair(*a, cfg_a->m, M, reinterpret_cast<__nv_bfloat16*>(ws + s.a), *w, cfg_w->m, 2 * N, reinterpret_cast<__nv_bfloat16*>(ws + s.w), K,
-                          s.pitch_k, st)))
-        return rc;
     GatedJob<false>::Params p = {};
-    if ((rc = set_products(p, M, N, K, s, ws))) return rc;
+    const bool f8 = fused::takes_f8(cfg_a->m, cfg_w->m, M, 2 * N, N, K);
     p.act = act;
     p.h = fused::make_rows(h, ldh, dt == BDR_F32);
-    p.gate = fused::make_rows(gate_up, ld_gate_up, dt == BDR_F32);
-    p.up = fused::make_rows(gate_up ? static_cast<char*>(gate_up) + N * width : nullptr, ld_gate_up, dt == BDR_F32);
+    p.gate_out = fused::make_rows(gate_up, ld_gate_up, dt == BDR_F32);
+    p.up_out = fused::make_rows(gate_up ? static_cast<char*>(gate_up) + N * width : nullptr, ld_gate_up, dt == BDR_F32);
+    if ((rc = set_products(p, M, N, K, s, ws, f8))) return rc;
+    if (f8) {  // the bytes lie where the bf16 operands would: those are written only once the 8-bit kernel has found nothing to do
+        if ((rc = fused::encode_f8(*a, cfg_a->m, M, *w, cfg_w->m, 2 * N, 2, K, ws, reinterpret_cast<int*>(ws + s.flag), &p.f8, &p.gate, st))) return rc;
+        if ((rc = fused::launch_f8<GatedJob<false>>(p, st))) return rc;
+    }
+    if ((rc = decode_pair(*a, cfg_a->m, M, reinterpret_cast<__nv_bfloat16*>(ws + s.a), *w, cfg_w->m, 2 * N, reinterpret_cast<__nv_bfloat16*>(ws + s.w), K,
+                          s.pitch_k, st, p.gate)))
+        return rc;
     return fused::launch<GatedJob<false>>(p, st);
 }
 
@@ -303,11 +337,16 @@ int mx_gated_gemm_bwd(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bd
         if (rc) return rc;
     } else {
         GatedJob<true>::Params p = {};
-        if ((rc = set_products(p, M, N, K, s, ws))) return rc;
+        const bool f8 = fused::takes_f8(cfg_a->m, cfg_w->m, M, 2 * N, N, K);
+        if ((rc = set_products(p, M, N, K, s, ws, f8))) return rc;
         p.act = act;
         p.h = dh_rows;
         p.d = d_rows;
         p.parts = parts;
+        if (f8) {
+            if ((rc = fused::encode_f8(*a, cfg_a->m, M, *w, cfg_w->m, 2 * N, 2, K, ws + s.f8, reinterpret_cast<int*>(ws + s.flag), &p.f8, &p.gate, st))) return rc;
+            if ((rc = fused::launch_f8<GatedJob<true>>(p, st))) return rc;
+        }
         if ((rc = fused::launch<GatedJob<true>>(p, st))) return rc;
     }
     GradProducts g = {};

@@ -42,6 +42,7 @@ struct GradJob {
         int segs, parts;
         const float* scale;
         int cols;              // K
+        const int* gate;
         int* status;
     };
     struct Item {
@@ -217,8 +218,10 @@ struct Lines {
     int m;
 };
 // Both operands in one launch: blocks 0 .. first_blocks - 1 take the first.
-__global__ void __launch_bounds__(256) decode_pair_kernel(Lines first, Lines second, unsigned first_blocks, int64_t pitch, uint32_t items_per_row, int nb) {
+__global__ void __launch_bounds__(256) decode_pair_kernel(Lines first, Lines second, unsigned first_blocks, int64_t pitch, uint32_t items_per_row, int nb,
+                                                           const int* gate) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the product's set-up may begin
+    if (gate && *gate == 0) return;
     const bool one = blockIdx.x < first_blocks;
     const Lines& l = one ? first : second;
     const int64_t at = (int64_t)(one ? blockIdx.x : blockIdx.x - first_blocks) * 256 + threadIdx.x, stride = (int64_t)(one ? first_blocks : gridDim.x - first_blocks) * 256;
@@ -232,11 +235,11 @@ __global__ void __launch_bounds__(256) decode_pair_kernel(Lines first, Lines sec
 }  // namespace
 
 int decode_pair(const bdr_planes_t& a, int m_a, int64_t rows_a, __nv_bfloat16* out_a, const bdr_planes_t& w, int m_w, int64_t rows_w, __nv_bfloat16* out_w,
-                int64_t K, int64_t pitch, cudaStream_t st) {
+                int64_t K, int64_t pitch, cudaStream_t st, const int* gate) {
     Lines l[2] = {{a, out_a, rows_a, m_a}, {w, out_w, rows_w, m_w}};
     const int64_t per_row = (K + 31) / 32;
     for (Lines& x : l) {
-        if (x.n_items * K >= (1ll << 23)) {
+        if (!gate && x.n_items * K >= (1ll << 23)) {
             QParams qp;
             qp.k1 = 16; qp.k2 = 2; qp.d2 = 1; qp.m = x.m; qp.rounding = BDR_ROUND_NEAREST_EVEN; qp.beta = 1; qp.qmax = (1u << x.m) - 1u;
             const int rc = unpack_rowwise_mx_x2(x.in, x.out, x.n_items, K, pitch, qp, st);  // whole runs of 2048 elements: through shared memory
@@ -247,8 +250,8 @@ int decode_pair(const bdr_planes_t& a, int m_a, int64_t rows_a, __nv_bfloat16* o
     }
     if (l[0].n_items + l[1].n_items == 0) return BDR_OK;
     unsigned blocks[2];
-    for (int i = 0; i < 2; ++i) blocks[i] = (unsigned)std::min<int64_t>((l[i].n_items + 255) / 256, (int64_t)sm_count() * 32);
-    decode_pair_kernel<<<blocks[0] + blocks[1], 256, 0, st>>>(l[0], l[1], blocks[0], pitch, (uint32_t)per_row, (int)((K + 15) / 16));
+    for (int i = 0; i < 2; ++i) blocks[i] = (unsigned)std::min<int64_t>((l[i].n_items + 255) / 256, (int64_t)sm_count() * (gate ? 4 : 32));  // behind a gate it rarely has anything to do
+    decode_pair_kernel<<<blocks[0] + blocks[1], 256, 0, st>>>(l[0], l[1], blocks[0], pitch, (uint32_t)per_row, (int)((K + 15) / 16), gate);
     return cudaGetLastError() == cudaSuccess ? BDR_OK : BDR_ERR_CUDA;
 }
 
