@@ -1,4 +1,4 @@
-"""The attention half of a decoder block, one new token per sequence, on MX storage: the weights (Section V, inferencing) and the
+"""The two halves of a decoder block, one new token per sequence, on MX storage: the weights (Section V, inferencing) and the
 key-value cache are kept in the MX format; the activations stay in bf16 or fp32, which is this library's choice (the section
 quantizes them too).  Like ``linear``, this module only sequences calls of the C ABI; all arithmetic is in the kernels.
 
@@ -6,6 +6,9 @@ quantizes them too).  Like ``linear``, this module only sequences calls of the C
     k, q rotated by position; k, v       mx_kv_append: quantized and written to the sequences' next slots
     a    = attention of q over the cache mx_attn_decode
     out  = a Wout^T                      mx_gemv
+
+    f    = act(h Wg^T) * (h Wu^T)        mx_gated_gemv
+    out  = f Wdown^T                     mx_gemv
 """
 from __future__ import annotations
 
@@ -90,4 +93,36 @@ def step(block: AttentionBlock, h: torch.Tensor, page_table: torch.Tensor, lengt
         held = lengths.add_(1) if advance else lengths + 1
         bdr.mx_attn_decode(c, block.q, page_table, held, block.attended, block.workspace, window=window)
         bdr.mx_gemv(block.cfg_w, block.w_out, d_model, n_q * c.head_dim, block.attended.view(n_seqs, -1), out)
+    return out
+
+
+@dataclass
+class FeedForwardBlock:
+    """Weights and buffer of the gated feed-forward half for a fixed number of sequences."""
+    cfg_w: bdr.Config
+    w_gate_up: bdr.Planes    # packed along K: [2 d_ff, d_model], the gate's rows first
+    w_down: bdr.Planes       # packed along K: [d_model, d_ff]
+    act: int
+    hidden: torch.Tensor     # [n_seqs, d_ff]
+
+
+def alloc_feed_forward(cfg_w: bdr.Config, w_gate_up: torch.Tensor, w_down: torch.Tensor, n_seqs: int, act: int = bdr.ACT_SILU,
+                       dtype=torch.bfloat16) -> FeedForwardBlock:
+    d_model, d_ff = w_down.shape
+    if w_gate_up.shape != (2 * d_ff, d_model):
+        raise ValueError("w_gate_up is [2 d_ff, d_model], w_down [d_model, d_ff]")
+    return FeedForwardBlock(cfg_w, pack_weight(cfg_w, w_gate_up), pack_weight(cfg_w, w_down), act,
+                            torch.empty((n_seqs, d_ff), dtype=dtype, device=w_down.device))
+
+
+def feed_forward(block: FeedForwardBlock, h: torch.Tensor, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """The block's output [n_seqs, d_model] for h [n_seqs, d_model].  Everything runs on `stream` (the current one when None): h has to
+    be ready there, and an output that the call allocates belongs to it."""
+    n_seqs, d_model = h.shape
+    d_ff = block.hidden.shape[1]
+    with torch.cuda.stream(stream) if stream is not None else torch.cuda.stream(torch.cuda.current_stream()):
+        if out is None:
+            out = torch.empty_like(h)
+        bdr.mx_gated_gemv(block.cfg_w, block.w_gate_up, d_ff, d_model, h, block.hidden[:n_seqs], act=block.act)
+        bdr.mx_gemv(block.cfg_w, block.w_down, d_model, d_ff, block.hidden[:n_seqs], out)
     return out

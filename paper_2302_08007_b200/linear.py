@@ -46,6 +46,17 @@ def alloc(cfg: bdr.Config, tokens: int, d_in: int, d_out: int, device="cuda", tw
                          torch.empty((d_out, d_in), dtype=torch.float32, device=device), ws)
 
 
+def product(cfg: bdr.Config, a: bdr.Planes, b: bdr.Planes, M: int, N: int, K: int, c: torch.Tensor, workspace: torch.Tensor | None = None, stream=None):
+    """C = A B^T by the fastest kernel that the format and the workspace (None: none) allow."""
+    if workspace is not None and cfg.m <= 4:
+        bdr.mx_gemm_f8(cfg, a, cfg, b, M, N, K, c, workspace[:bdr.mx_gemm_f8_workspace_bytes(M, N, K)], stream=stream)
+    elif workspace is not None:
+        bdr.mx_gemm_ws(cfg, a, cfg, b, M, N, K, c, workspace, stream=stream)
+    else:
+        bdr.mx_gemm(cfg, a, cfg, b, M, N, K, c, stream=stream)
+    return c
+
+
 def step(cfg: bdr.Config, x: torch.Tensor, w: torch.Tensor, dy: torch.Tensor, buf: LinearBuffers, stream=None):
     """Six quantizations (three dual-direction calls, with fused QSNR sums) and three MX GEMMs.  Returns (Y, dX, dW)."""
     tokens, d_in = x.shape
@@ -57,12 +68,7 @@ def step(cfg: bdr.Config, x: torch.Tensor, w: torch.Tensor, dy: torch.Tensor, bu
     p = buf.planes
 
     def gemm(a, b, M, N, K, c):
-        if buf.workspace is not None and cfg.m <= 4:
-            bdr.mx_gemm_f8(cfg, a, cfg, b, M, N, K, c, buf.workspace[:bdr.mx_gemm_f8_workspace_bytes(M, N, K)], stream=stream)
-        elif buf.workspace is not None:
-            bdr.mx_gemm_ws(cfg, a, cfg, b, M, N, K, c, buf.workspace, stream=stream)
-        else:
-            bdr.mx_gemm(cfg, a, cfg, b, M, N, K, c, stream=stream)
+        product(cfg, a, b, M, N, K, c, buf.workspace, stream)
 
     gemm(p[("x", 1)], p[("w", 1)], tokens, d_out, d_in, buf.y)      # Y  = X W^T
     gemm(p[("dy", 1)], p[("w", 0)], tokens, d_in, d_out, buf.dx)    # dX = dY W
