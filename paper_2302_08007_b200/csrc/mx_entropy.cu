@@ -30,7 +30,9 @@ template <bool GRAD>
 struct EntropyJob {
     struct Params {
         CUtensorMap a, w;         // bf16 [M][K]; [columns of this piece][K]
-        int n_items, bn, tiles_m, tiles_n, band_rows, steps;
+        int n_items, bn, tiles_m, tiles_n, band_rows, steps, splits, span;
+        float* partials;
+        int* counters;
         int M, cols;
         int64_t col0;             // the piece's first column
         const int64_t* targets;
@@ -45,17 +47,26 @@ struct EntropyJob {
         const int* gate;
         int* status;
     };
-    struct Item { int steps, tm, tn; };
+    struct Item { int steps, tm, tn, tile, split; };
     static constexpr bool b_mn = false;
     static constexpr int kSpan = 0;
+    static constexpr bool kCut = true;
+    static __device__ __forceinline__ int rows(const Params& p) { return p.M; }
+    static __device__ __forceinline__ int chunks(int bn, int) { return bn / 64; }
+    static __device__ __forceinline__ int chunk(int bn, int half, int i) { return half * (bn / 2) + 32 * i; }
+    static __device__ __forceinline__ void prefetch(const Params& p) { prefetch_map(&p.a); prefetch_map(&p.w); }
     static __device__ __forceinline__ bool a_mn(const Item&) { return false; }
     static __device__ __forceinline__ Item item(const Params& p, int i) {
         Item it;
-        it.steps = p.steps;
-        gemm_tile_coords(i, p.tiles_m, p.tiles_n, p.band_rows, it.tm, it.tn);
+        const int tiles = p.tiles_m * p.tiles_n;
+        it.split = i / tiles;
+        it.tile = i - it.split * tiles;
+        it.steps = min(p.span, p.steps - it.split * p.span);
+        gemm_tile_coords(it.tile, p.tiles_m, p.tiles_n, p.band_rows, it.tm, it.tn);
         return it;
     }
     static __device__ __forceinline__ void load(const Params& p, const Item& it, int kk, int rank, uint8_t* dst, uint64_t* bar) {
+        kk += it.split * p.span;
         tma_load_3d(dst, &p.a, kk * kBK, (it.tm * 2 + rank) * kRows, 0, bar);
         tma_load_3d(dst + fused::kOperandBytes, &p.w, kk * kBK, it.tn * p.bn + rank * (p.bn >> 1), 0, bar);
     }
@@ -248,7 +259,7 @@ constexpr int64_t kMostWeights = 512ll << 20;   // bytes of decoded weights at a
 constexpr int64_t kMostD = 256ll << 20;         // bytes of d at a time
 
 struct EntropySpace {
-    int64_t pitch_k, piece, a, w, parts, hit, flag, bytes;
+    int64_t pitch_k, piece, a, w, parts, hit, flag, partials, counters, n_counters, bytes;
     EntropySpace(int64_t M, int64_t V, int64_t K) {
         pitch_k = line_pitch(K);
         piece = piece_columns(V, kMostWeights / (pitch_k * 2));
@@ -258,11 +269,16 @@ struct EntropySpace {
         parts = std::max(parts, fused::f8_bytes(M, std::min(piece, V), K));
         hit = parts + round_up((V + 31) / 32 * M * 8, 256);
         flag = hit + round_up(M * 4, 256);
-        bytes = flag + 256;
+        const int64_t tiles_m = (M + 255) / 256;
+        const fused::Share share = fused::share_product(tiles_m, std::min(piece, V), 1, (K + kBK - 1) / kBK);
+        partials = flag + 256;
+        counters = partials + round_up(share.partial_bytes(tiles_m), 256);
+        n_counters = share.counters(tiles_m);
+        bytes = counters + round_up(n_counters * 4, 256);
     }
 };
 struct EntropyGradSpace {
-    int64_t pitch_k, piece, a, w, d, acc, largest, sums, f8, flag, bytes;
+    int64_t pitch_k, piece, a, w, d, acc, largest, sums, f8, flag, partials, counters, n_counters, bytes;
     EntropyGradSpace(int64_t M, int64_t V, int64_t K, int n_parts) {
         pitch_k = line_pitch(K);
         piece = piece_columns(V, std::min(kMostWeights / (pitch_k * 2), kMostD / (std::max<int64_t>(M, 1) * 2 * n_parts)));
@@ -274,7 +290,12 @@ struct EntropyGradSpace {
         sums = largest + 256;
         f8 = sums + grad_sums_bytes(M, std::min(piece, V), K, 1);
         flag = f8 + (fused::takes_f8(4, 4, M, V, V, K) ? fused::f8_bytes(M, std::min(piece, V), K) : 0);
-        bytes = flag + 256;
+        const int64_t tiles_m = (M + 255) / 256;
+        const fused::Share share = fused::share_product(tiles_m, std::min(piece, V), 1, (K + kBK - 1) / kBK);
+        partials = flag + 256;
+        counters = partials + round_up(share.partial_bytes(tiles_m), 256);
+        n_counters = share.counters(tiles_m);
+        bytes = counters + round_up(n_counters * 4, 256);
     }
 };
 
@@ -284,11 +305,16 @@ template <class Params>
 int set_piece(Params& p, int64_t M, int64_t K, int64_t col0, int64_t cols, int64_t pitch_k, const uint8_t* a, const uint8_t* w, bool f8) {
     p.tiles_m = (int)((M + 255) / 256);
     p.steps = (int)((K + kBK - 1) / kBK);
-    if (col0 == 0) p.bn = f8 ? 256 : fused::pick_bn(p.tiles_m, cols, 1, p.steps, sm_count() / 2);  // (the last piece keeps it)
+    if (col0 == 0) {  // (the last piece, which may be shorter, keeps the accumulator and the cut)
+        const fused::Share share = fused::share_product(p.tiles_m, cols, 1, p.steps, f8);
+        p.bn = share.bn;
+        p.splits = share.splits;
+        p.span = share.span;
+    }
     p.tiles_n = (int)((cols + p.bn - 1) / p.bn);
     if (!fused::make_map(&p.a, a, K, M, 1, pitch_k, M * pitch_k, kRows) || !fused::make_map(&p.w, w, K, cols, 1, pitch_k, cols * pitch_k, p.bn / 2))
         return BDR_ERR_CUDA;
-    p.n_items = p.tiles_m * p.tiles_n;
+    p.n_items = p.tiles_m * p.tiles_n * p.splits;
     p.band_rows = gemm_band_rows((M + cols) * K * 2);
     p.M = (int)M;
     p.cols = (int)cols;
@@ -353,6 +379,8 @@ int mx_cross_entropy(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bdr
     p.targets = targets;
     p.vocab = V;
     p.parts = reinterpret_cast<float2*>(ws + s.parts);
+    p.partials = reinterpret_cast<float*>(ws + s.partials);
+    p.counters = reinterpret_cast<int*>(ws + s.counters);
     p.hit = reinterpret_cast<float*>(ws + s.hit);
     p.status = device_status_word();
     if (!p.status) return BDR_ERR_CUDA;
@@ -367,7 +395,8 @@ int mx_cross_entropy(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bdr
             if ((rc = fused::launch_f8<EntropyJob<false>>(p, st))) return rc;
         }
         // (with an 8-bit path in front, A's bf16 values are overwritten by the next piece's bytes)
-        if ((rc = decode_pair(*a, cfg_a->m, v == 0 || f8 ? M : 0, wa, lines, cfg_w->m, cols, ww, K, s.pitch_k, st, p.gate))) return rc;
+        if ((rc = decode_pair(*a, cfg_a->m, v == 0 || f8 ? M : 0, wa, lines, cfg_w->m, cols, ww, K, s.pitch_k, st, p.gate, p.counters, s.n_counters)))
+            return rc;
         if ((rc = fused::launch<EntropyJob<false>>(p, st))) return rc;
     }
     const int n_parts = (int)((V + p.bn / 2 - 1) / (p.bn / 2));
@@ -413,6 +442,8 @@ int mx_cross_entropy_bwd(const bdr_config_t* cfg_a, const bdr_planes_t* a, const
     p.lse = lse;
     p.dloss = dloss;
     p.d = fused::make_rows(ws + s.d, s.piece, false);
+    p.partials = reinterpret_cast<float*>(ws + s.partials);
+    p.counters = reinterpret_cast<int*>(ws + s.counters);
     p.n_parts = n_parts;
     p.status = device_status_word();
     if (!p.status) return BDR_ERR_CUDA;
@@ -433,7 +464,7 @@ int mx_cross_entropy_bwd(const bdr_config_t* cfg_a, const bdr_planes_t* a, const
     for (int64_t v = 0; v < V; v += s.piece) {
         const int64_t cols = std::min(s.piece, V - v);
         const bdr_planes_t lines = lines_from(*w, v);
-        if ((rc = decode_pair(*a, cfg_a->m, v == 0 ? M : 0, wa, lines, cfg_w->m, cols, ww, K, s.pitch_k, st))) return rc;
+        if ((rc = decode_pair(*a, cfg_a->m, v == 0 ? M : 0, wa, lines, cfg_w->m, cols, ww, K, s.pitch_k, st, nullptr, p.counters, s.n_counters))) return rc;
         if (v == 0 && (rc = launch_dependent(entropy_scale_kernel, dim3(1), dim3(1024), st, dloss, targets, M, V, reinterpret_cast<float*>(ws + s.largest))))
             return rc;
         if ((rc = set_piece(p, M, K, v, cols, s.pitch_k, ws + s.a, ws + s.w, f8))) return rc;

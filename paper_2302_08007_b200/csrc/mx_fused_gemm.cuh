@@ -15,12 +15,19 @@
 //   a_mn(it), b_mn                 whether an operand lies with its rows (M or N) contiguous instead of K
 //   kSpan                          K steps after which the accumulator is handed to the epilogue: 0 = at the end of the item
 //   epilogue(p, it, e)             (kSpan == 0) reads the accumulator through e.tmem
-//   finish(p, it, e, v)            (kSpan > 0, bn == 256) the same, with the 128 sums of a thread's row and half of the columns in registers
+//   finish(p, it, e, v)            (kSpan > 0) the same, with the sums of a thread's row and half of the columns in registers
+//   prefetch(p)                    the tensor maps that load() uses
+//   kCut                           whether a tile's K steps may be cut into p.splits items (Item::tile, Item::split): the parts' sums go to
+//                                  p.partials, and the warp that comes last (p.counters) adds them in order, puts the total back into its tensor
+//                                  memory and runs the epilogue; it needs rows(p), chunks(bn, half) and chunk(bn, half, i), the 32-column pieces of
+//                                  the accumulator that the epilogue of a half reads
 // The tensor core cuts its fp32 additions off instead of rounding them, toward zero: over a chain of n instructions of 16 K each the sum
 // loses about n 2^-25 of itself.  That is nothing beside 16-bit results, nor for operands of few bits, whose sums are mostly exact; sums
 // of full-width values for 32-bit results are taken kSpan steps at a time and added with rounded additions in the epilogue's registers,
 // while the next span runs.
 #pragma once
+
+#include <algorithm>
 
 #include "bdr_host.h"
 #include "mx_fused.h"
@@ -66,13 +73,60 @@ struct Epi {
     uint32_t tile;   // shared-memory address of the warp's own 2 KB
 };
 
+// A cut tile: stores this part's sums of the warp's rows and columns; true for the warp that finds all parts there, with the total in its
+// tensor memory.  Nobody waits.  Slots are 256 x bn floats in pieces of 32 rows x 32 columns, four columns of 32 rows together.
+template <class Job>
+__device__ __forceinline__ bool last_part(const typename Job::Params& p, const typename Job::Item& it, const Epi& e) {
+    const int64_t slot = 256 * p.bn;
+    float* const base = p.partials + (int64_t)it.tile * p.splits * slot + e.r0 * p.bn + 4 * e.lane;
+    const int n = Job::chunks(p.bn, e.half);
+    for (int i = 0; i < n; ++i) {
+        const int col = Job::chunk(p.bn, e.half, i);
+        __syncwarp();
+        uint32_t u[32];
+        tmem_ld32(e.tmem + (uint32_t)col, u);
+        float* const to = base + it.split * slot + col * 32;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) __stcg(reinterpret_cast<uint4*>(to + 128 * j), make_uint4(u[4 * j], u[4 * j + 1], u[4 * j + 2], u[4 * j + 3]));
+    }
+    __threadfence();
+    __syncwarp();
+    int before = 0;
+    if (e.lane == 0) before = atomicAdd(&p.counters[it.tile * 16 + (e.r0 >> 5) * 2 + e.half], 1);
+    before = __shfl_sync(0xFFFFFFFFu, before, 0);
+    if (before != p.splits - 1) return false;
+    __threadfence();
+    for (int i = 0; i < n; ++i) {
+        const int col = Job::chunk(p.bn, e.half, i);
+        float v[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] = 0.f;
+#pragma unroll 2
+        for (int s = 0; s < p.splits; ++s) {
+            const float* const from = base + s * slot + col * 32;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float4 x = __ldcg(reinterpret_cast<const float4*>(from + 128 * j));
+                v[4 * j] += x.x; v[4 * j + 1] += x.y; v[4 * j + 2] += x.z; v[4 * j + 3] += x.w;
+            }
+        }
+        uint32_t u[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) u[j] = __float_as_uint(v[j]);
+        __syncwarp();
+        tmem_st32(e.tmem + (uint32_t)col, u);
+    }
+    return true;
+}
+
 template <class Job>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_gemm_kernel(const __grid_constant__ typename Job::Params p) {
+    static_assert(Job::kSpan == 0 || !Job::kCut, "spans are added in registers, not in tensor memory");
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t* stages = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     uint8_t* const tiles = stages + kStages * kStageBytes;
     Bars& bars = *reinterpret_cast<Bars*>(tiles + kEpiWarps * kTileBytes);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();
     const int cluster_id = blockIdx.x >> 1, n_clusters = gridDim.x >> 1;
     const int stage_bytes = kOperandBytes + 64 * p.bn, n_stages = min(kMostStages, kStages * kStageBytes / stage_bytes);
@@ -90,6 +144,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
         bars.failed = 0;
         fence_barrier_init();
     }
+    if (threadIdx.x == 32 * kEpiWarps) Job::prefetch(p);
     if (warp == 1) tmem_alloc2_cols(&bars.tmem_base, 512);
     tc_fence_before();
     __syncthreads();
@@ -106,83 +161,92 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
     if (!open) {
         // the 8-bit kernel has done it
     } else if (warp == 0) {
-        if (lane == 0) {
-            uint64_t* const my_full = rank == 0 ? bars.full : bars.full_local;
-            bool ok = true;
-            int stage = 0, turn = 0;  // of the ring
-            for (int i = cluster_id; i < p.n_items && ok; i += n_clusters) {
-                const typename Job::Item item = Job::item(p, i);
-                for (int kk = 0; kk < item.steps; ++kk) {
-                    if (turn > 0) {
-                        ok = mbar_wait(&bars.empty[stage], (turn - 1) & 1);
-                        if (!ok) break;
-                    }
+        // The roles' warps run their loops together, and one elected thread issues: what the instructions take from uniform registers (descriptors,
+        // addresses) then stays there.  With one lane in a branch of its own a K step took at least 560 clocks, whatever the columns.
+        uint64_t* const my_full = rank == 0 ? bars.full : bars.full_local;
+        bool ok = true;
+        int stage = 0, turn = 0;  // of the ring
+        for (int i = cluster_id; i < p.n_items && ok; i += n_clusters) {
+            const typename Job::Item item = Job::item(p, i);
+            for (int kk = 0; kk < item.steps; ++kk) {
+                if (turn > 0) {
+                    ok = mbar_wait(&bars.empty[stage], (turn - 1) & 1);
+                    if (!ok) break;
+                }
+                if (elect_one()) {
                     mbar_expect_tx(&my_full[stage], stage_bytes);
                     Job::load(p, item, kk, (int)rank, stages + stage * stage_bytes, &my_full[stage]);
-                    if (++stage == n_stages) { stage = 0; ++turn; }
                 }
+                __syncwarp();
+                if (++stage == n_stages) { stage = 0; ++turn; }
             }
-            if (!ok) {
-                bars.failed = 1;
-                // the copies still on their way: one more bounded wait for each
-                for (int s = 0; s < n_stages; ++s)
-                    if (s < stage || turn > 0) mbar_wait(&my_full[s], (s < stage ? turn : turn - 1) & 1);
-            }
+        }
+        if (!ok) {
+            bars.failed = 1;
+            // the copies still on their way: one more bounded wait for each
+            for (int s = 0; s < n_stages; ++s)
+                if (s < stage || turn > 0) mbar_wait(&my_full[s], (s < stage ? turn : turn - 1) & 1);
         }
         __syncwarp();
     } else if (warp == 1) {
-        if (lane == 0) {
-            bool ok = true;
-            int stage = 0, turn = 0;
-            if (rank == 0) {
-                int tcount = 0;
-                for (int i = cluster_id; i < p.n_items && ok; i += n_clusters, ++tcount) {
-                    const typename Job::Item item = Job::item(p, i);
-                    const bool a_mn = Job::a_mn(item);
-                    const uint32_t idesc = kIdesc | ((uint32_t)(p.bn >> 3) << 17) | (a_mn ? kMnA : 0u) | (Job::b_mn ? kMnB : 0u);
-                    const uint64_t a_step = a_mn ? 128 : 2;  // 16 K: two groups of eight K rows, or 32 bytes along a row
-                    const uint64_t b_step = Job::b_mn ? 128 : 2;
-                    const int span = Job::kSpan ? Job::kSpan : item.steps;
-                    int buf = 0, left = 0;  // K steps that the current buffer still takes
-                    uint32_t acc = 0;
-                    for (int kk = 0; kk < item.steps; ++kk, --left) {
-                        if (left == 0) {
-                            if (kk > 0) { umma_commit2(&bars.tmem_full[buf]); ++tcount; }
-                            left = span;
-                            buf = tcount & 1;
-                            acc = tmem_base + (uint32_t)buf * 256u;
-                            if (tcount >= 2) {  // the epilogues of both CTAs have drained this buffer
-                                ok = mbar_wait_cluster(&bars.tmem_empty[buf], ((tcount >> 1) - 1) & 1);
-                                if (!ok) break;
-                                tc_fence_after();
-                            }
+        bool ok = true;
+        int stage = 0, turn = 0;
+        if (rank == 0) {
+            int tcount = 0;
+            for (int i = cluster_id; i < p.n_items && ok; i += n_clusters, ++tcount) {
+                const typename Job::Item item = Job::item(p, i);
+                const bool a_mn = Job::a_mn(item);
+                const uint32_t idesc = kIdesc | ((uint32_t)(p.bn >> 3) << 17) | (a_mn ? kMnA : 0u) | (Job::b_mn ? kMnB : 0u);
+                const uint64_t a_step = a_mn ? 128 : 2;  // 16 K: two groups of eight K rows, or 32 bytes along a row
+                const uint64_t b_step = Job::b_mn ? 128 : 2;
+                const int span = Job::kSpan ? Job::kSpan : item.steps;
+                int buf = 0, left = 0;  // K steps that the current buffer still takes
+                uint32_t acc = 0;
+                for (int kk = 0; kk < item.steps; ++kk, --left) {
+                    if (left == 0) {
+                        if (kk > 0) {
+                            if (elect_one()) umma_commit2(&bars.tmem_full[buf]);
+                            ++tcount;
                         }
-                        ok = mbar_wait_cluster(&bars.full[stage], turn & 1);
-                        if (!ok) break;
-                        tc_fence_after();
-                        const uint32_t sa = smem_u32(stages + stage * stage_bytes), sb = sa + kOperandBytes;
-                        const uint64_t da = a_mn ? make_mn_desc(sa) : make_smem_desc(sa);
-                        const uint64_t db = Job::b_mn ? make_mn_desc(sb) : make_smem_desc(sb);
+                        left = span;
+                        buf = tcount & 1;
+                        acc = tmem_base + (uint32_t)buf * 256u;
+                        if (tcount >= 2) {  // the epilogues of both CTAs have drained this buffer
+                            ok = mbar_wait_cluster(&bars.tmem_empty[buf], ((tcount >> 1) - 1) & 1);
+                            if (!ok) break;
+                            tc_fence_after();
+                        }
+                    }
+                    ok = mbar_wait_cluster(&bars.full[stage], turn & 1);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t sa = smem_u32(stages + stage * stage_bytes), sb = sa + kOperandBytes;
+                    const uint64_t da = a_mn ? make_mn_desc(sa) : make_smem_desc(sa);
+                    const uint64_t db = Job::b_mn ? make_mn_desc(sb) : make_smem_desc(sb);
+                    if (elect_one()) {
 #pragma unroll
                         for (int k = 0; k < kBK / 16; ++k) umma2_bf16(acc, da + k * a_step, db + k * b_step, idesc, left != span || k != 0);
                         umma_commit2(&bars.empty[stage]);
-                        if (++stage == n_stages) { stage = 0; ++turn; }
                     }
-                    if (ok) umma_commit2(&bars.tmem_full[buf]);
+                    __syncwarp();
+                    if (++stage == n_stages) { stage = 0; ++turn; }
                 }
-            } else {
-                for (int i = cluster_id; i < p.n_items && ok; i += n_clusters) {
-                    const typename Job::Item item = Job::item(p, i);
-                    for (int kk = 0; kk < item.steps; ++kk) {
-                        ok = mbar_wait(&bars.full_local[stage], turn & 1);
-                        if (!ok) break;
-                        mbar_arrive_cluster(&bars.full[stage], 0);
-                        if (++stage == n_stages) { stage = 0; ++turn; }
-                    }
+                if (ok && elect_one()) umma_commit2(&bars.tmem_full[buf]);
+                __syncwarp();
+            }
+        } else {
+            for (int i = cluster_id; i < p.n_items && ok; i += n_clusters) {
+                const typename Job::Item item = Job::item(p, i);
+                for (int kk = 0; kk < item.steps; ++kk) {
+                    ok = mbar_wait(&bars.full_local[stage], turn & 1);
+                    if (!ok) break;
+                    if (elect_one()) mbar_arrive_cluster(&bars.full[stage], 0);
+                    __syncwarp();
+                    if (++stage == n_stages) { stage = 0; ++turn; }
                 }
             }
-            if (!ok) bars.failed = 1;
         }
+        if (!ok) bars.failed = 1;
         __syncwarp();
         tc_fence_before();
     } else {
@@ -212,7 +276,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
                 const int buf = tcount & 1;
                 if (!next(buf)) break;
                 e.tmem = tmem_base + my_lanes + (uint32_t)buf * 256u;
-                Job::epilogue(p, item, e);
+                bool mine = true;
+                if constexpr (Job::kCut) {
+                    mine = item.tm * 256 + e.r0 < Job::rows(p);
+                    if (mine && p.splits > 1) mine = last_part<Job>(p, item, e);
+                }
+                if (mine) Job::epilogue(p, item, e);
                 done(buf);
             } else {
                 float v[4][32];
@@ -226,8 +295,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
                     if (!next(buf)) break;
 #pragma unroll
                     for (int q = 0; q < 8; ++q) {  // sixteen columns at a time: more would not fit beside the sums
+                        if (32 * q >= p.bn) break;
                         uint32_t u[16];
-                        tmem_ld16(tmem_base + my_lanes + (uint32_t)(buf * 256 + e.half * 128 + 16 * q), u);
+                        tmem_ld16(tmem_base + my_lanes + (uint32_t)(buf * 256 + e.half * (p.bn >> 1) + 16 * q), u);
 #pragma unroll
                         for (int j = 0; j < 16; ++j) v[q >> 1][16 * (q & 1) + j] += __uint_as_float(u[j]);
                     }
@@ -465,16 +535,33 @@ __device__ __forceinline__ void store_parts(const Epi& e, const Rows& d, int64_t
     }
 }
 
-// Columns of an accumulator for a product of tiles_m x cols (cols_div accumulator columns for each of the product's): the fewest K steps
-// in a row, weighed with what a step takes.  A step moves 16 KB of A and bn / 2 columns of B into an SM at about 64 bytes a clock and
-// multiplies for 2 bn clocks; an item's start and epilogue take about 1500 clocks that nothing hides when it is its cluster's only one.
-inline int pick_bn(int64_t tiles_m, int64_t cols, int cols_div, int64_t steps, int clusters) {
-    int best = 256;
+// How a product of tiles_m x cols is shared out: the accumulator's columns (cols_div of them for each of the product's) and the items that a
+// tile's K steps are cut into.  A step takes about 480 + 0.55 bn clocks (measured from 64 to 256 columns: below 256 it is the barriers and the
+// instructions' issue that count), an item's start and epilogue 1500 at 256 columns; narrow tiles pay where wide ones would leave clusters
+// idle.  A cut pays where few tiles have long sums: it costs the way through memory and back, and the last warp's reading of all parts.
+constexpr int kClusters = 74;  // (the workspaces' sizes follow from it, without a GPU)
+struct Share {
+    int bn, tiles_n, splits, span;
+    int64_t items(int64_t tiles_m) const { return tiles_m * tiles_n * splits; }
+    int64_t partial_bytes(int64_t tiles_m) const { return splits > 1 ? items(tiles_m) * 256 * bn * 4 : 0; }
+    int64_t counters(int64_t tiles_m) const { return splits > 1 ? tiles_m * tiles_n * 16 : 0; }
+};
+inline Share share_product(int64_t tiles_m, int64_t cols, int cols_div, int64_t steps, bool whole = false) {
+    Share best = {};
     double least = 0;
-    for (int bn = 256; bn >= 64; bn /= 2) {
-        const int64_t n = bn / cols_div, items = tiles_m * ((cols + n - 1) / n), rounds = (items + clusters - 1) / clusters;
-        const double t = (double)rounds * (steps * (double)(2 * bn > 256 + bn ? 2 * bn : 256 + bn) + 1500.0 * bn / 256);
-        if (bn == 256 || t < 0.98 * least) { best = bn; least = t; }
+    for (int bn = 256; bn >= (whole ? 256 : 64); bn /= 2) {
+        const int64_t n = bn / cols_div, tiles_n = (cols + n - 1) / n, tiles = tiles_m * tiles_n;
+        const int64_t most = whole || tiles > kClusters / 2 ? 1 : std::min<int64_t>(16, kClusters / tiles);
+        for (int64_t want = 1; want <= most; ++want) {
+            const int64_t span = (steps + want - 1) / want, splits = (steps + span - 1) / span;
+            if (splits != want) continue;
+            const double rounds = (double)((tiles * splits + kClusters - 1) / kClusters);
+            const double t = rounds * (span * (480 + 0.55 * bn) + 1500.0 * bn / 256) + (splits > 1 ? 9000 + splits * 400.0 * bn / 64 : 0);
+            if (!best.bn || t < 0.97 * least) {
+                best = {bn, (int)tiles_n, (int)splits, (int)span};
+                least = t;
+            }
+        }
     }
     return best;
 }

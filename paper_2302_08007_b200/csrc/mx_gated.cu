@@ -26,7 +26,9 @@ template <bool GRAD>
 struct GatedJob {
     struct Params {
         CUtensorMap a, w;          // bf16 [M][K]; [2][N][K]
-        int n_items, bn, tiles_m, tiles_n, band_rows, steps;
+        int n_items, bn, tiles_m, tiles_n, band_rows, steps, splits, span;
+        float* partials;
+        int* counters;
         int M, N, act;
         Rows h;                    // h, or dh
         Rows gate_out, up_out;     // where the two products go (NULL: nowhere)
@@ -36,17 +38,30 @@ struct GatedJob {
         const int* gate;
         int* status;
     };
-    struct Item { int steps, tm, tn; };
+    struct Item { int steps, tm, tn, tile, split; };
     static constexpr bool b_mn = false;
     static constexpr int kSpan = 0;
+    static constexpr bool kCut = true;
+    static __device__ __forceinline__ int rows(const Params& p) { return p.M; }
+    // half of the accumulator is the gate, whose pieces of 32 columns the two halves of the warps take in turn
+    static __device__ __forceinline__ int chunks(int bn, int half) { return 2 * ((bn / 64 + 1 - half) / 2); }
+    static __device__ __forceinline__ int chunk(int bn, int half, int i) {
+        const int gates = (bn / 64 + 1 - half) / 2;
+        return i < gates ? 32 * (half + 2 * i) : bn / 2 + 32 * (half + 2 * (i - gates));
+    }
+    static __device__ __forceinline__ void prefetch(const Params& p) { prefetch_map(&p.a); prefetch_map(&p.w); }
     static __device__ __forceinline__ bool a_mn(const Item&) { return false; }
     static __device__ __forceinline__ Item item(const Params& p, int i) {
         Item it;
-        it.steps = p.steps;
-        gemm_tile_coords(i, p.tiles_m, p.tiles_n, p.band_rows, it.tm, it.tn);
+        const int tiles = p.tiles_m * p.tiles_n;
+        it.split = i / tiles;
+        it.tile = i - it.split * tiles;
+        it.steps = min(p.span, p.steps - it.split * p.span);
+        gemm_tile_coords(it.tile, p.tiles_m, p.tiles_n, p.band_rows, it.tm, it.tn);
         return it;
     }
     static __device__ __forceinline__ void load(const Params& p, const Item& it, int kk, int rank, uint8_t* dst, uint64_t* bar) {
+        kk += it.split * p.span;
         tma_load_3d(dst, &p.a, kk * kBK, (it.tm * 2 + rank) * kRows, 0, bar);
         tma_load_3d(dst + fused::kOperandBytes, &p.w, kk * kBK, it.tn * (p.bn >> 1), rank, bar);
     }
@@ -197,7 +212,7 @@ int launch_gated_grad(const Rows& gate, const Rows& up, const Rows& dh, int act,
 
 // Workspace: A, W and, for gradients, D.
 struct GatedSpace {
-    int64_t pitch_k, pitch_d, a, w, d, sums, f8, flag, bytes;  // offsets in bytes
+    int64_t pitch_k, pitch_d, a, w, d, sums, f8, flag, partials, counters, n_counters, bytes;  // offsets in bytes
     GatedSpace(int64_t M, int64_t N, int64_t K, int parts) {
         pitch_k = line_pitch(K);
         pitch_d = round_up(N, 64);
@@ -208,7 +223,12 @@ struct GatedSpace {
         f8 = sums + (parts ? grad_sums_bytes(M, N, K, 2) : 0);
         // (whether it will be used depends on the formats too; a forward pass keeps the bytes where the bf16 operands would lie)
         flag = parts ? f8 + (fused::takes_f8(4, 4, M, 2 * N, N, K) ? fused::f8_bytes(M, 2 * N, K) : 0) : std::max(f8, fused::f8_bytes(M, 2 * N, K));
-        bytes = flag + 256;
+        const int64_t tiles_m = (M + 255) / 256;
+        const fused::Share share = fused::share_product(tiles_m, N, 2, (K + kBK - 1) / kBK);
+        partials = flag + 256;
+        counters = partials + round_up(share.partial_bytes(tiles_m), 256);
+        n_counters = share.counters(tiles_m);
+        bytes = counters + round_up(n_counters * 4, 256);
     }
 };
 
@@ -224,12 +244,17 @@ template <class Params>
 int set_products(Params& p, int64_t M, int64_t N, int64_t K, const GatedSpace& s, uint8_t* ws, bool f8) {
     p.tiles_m = (int)((M + 255) / 256);
     p.steps = (int)((K + kBK - 1) / kBK);
-    p.bn = f8 ? 256 : fused::pick_bn(p.tiles_m, N, 2, p.steps, sm_count() / 2);
-    p.tiles_n = (int)((N + p.bn / 2 - 1) / (p.bn / 2));
+    const fused::Share share = fused::share_product(p.tiles_m, N, 2, p.steps, f8);
+    p.bn = share.bn;
+    p.tiles_n = share.tiles_n;
+    p.splits = share.splits;
+    p.span = share.span;
+    p.partials = reinterpret_cast<float*>(ws + s.partials);
+    p.counters = reinterpret_cast<int*>(ws + s.counters);
     if (!fused::make_map(&p.a, ws + s.a, K, M, 1, s.pitch_k, M * s.pitch_k, kRows) ||
         !fused::make_map(&p.w, ws + s.w, K, N, 2, s.pitch_k, N * s.pitch_k, p.bn / 2))
         return BDR_ERR_CUDA;
-    p.n_items = p.tiles_m * p.tiles_n;
+    p.n_items = p.tiles_m * p.tiles_n * p.splits;
     p.band_rows = gemm_band_rows((M + 2 * N) * K * 2);
     p.M = (int)M;
     p.N = (int)N;
@@ -285,7 +310,7 @@ int mx_gated_gemm(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bdr_co
         if ((rc = fused::launch_f8<GatedJob<false>>(p, st))) return rc;
     }
     if ((rc = decode_pair(*a, cfg_a->m, M, reinterpret_cast<__nv_bfloat16*>(ws + s.a), *w, cfg_w->m, 2 * N, reinterpret_cast<__nv_bfloat16*>(ws + s.w), K,
-                          s.pitch_k, st, p.gate)))
+                          s.pitch_k, st, p.gate, p.counters, s.n_counters)))
         return rc;
     return fused::launch<GatedJob<false>>(p, st);
 }
@@ -328,7 +353,8 @@ int mx_gated_gemm_bwd(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bd
     uint8_t* const ws = static_cast<uint8_t*>(workspace);
     __nv_bfloat16 *const wa = reinterpret_cast<__nv_bfloat16*>(ws + s.a), *const ww = reinterpret_cast<__nv_bfloat16*>(ws + s.w),
                          *const d = reinterpret_cast<__nv_bfloat16*>(ws + s.d);
-    if ((rc = decode_pair(*a, cfg_a->m, M, wa, *w, cfg_w->m, 2 * N, ww, K, s.pitch_k, st))) return rc;
+    if ((rc = decode_pair(*a, cfg_a->m, M, wa, *w, cfg_w->m, 2 * N, ww, K, s.pitch_k, st, nullptr, reinterpret_cast<int*>(ws + s.counters), s.n_counters)))
+        return rc;
     const bool f32 = dt == BDR_F32;
     const Rows dh_rows = fused::make_rows(dh, ld_dh, f32), d_rows = fused::make_rows(d, s.pitch_d, false);
     if (gate_up) {

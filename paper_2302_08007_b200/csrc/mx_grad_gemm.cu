@@ -50,6 +50,8 @@ struct GradJob {
         int split, k0;           // first K step
     };
     static constexpr bool b_mn = true;
+    static constexpr bool kCut = false;
+    static __device__ __forceinline__ void prefetch(const Params& p) { prefetch_map(&p.d_k); prefetch_map(&p.d_mn); prefetch_map(&p.w); prefetch_map(&p.a); }
     static constexpr int kSpan = F32 ? 4 : 0;  // 16 instructions in a chain
     static __device__ __forceinline__ bool a_mn(const Item& it) { return it.seg >= 0; }
     static __device__ __forceinline__ Item item(const Params& p, int i) {
@@ -71,7 +73,8 @@ struct GradJob {
         return it;
     }
     static __device__ __forceinline__ void load(const Params& p, const Item& it, int kk, int rank, uint8_t* dst, uint64_t* bar) {
-        const int row = (it.tm * 2 + rank) * kRows, col = (it.tk * 2 + rank) * kRows;
+        const int row = (it.tm * 2 + rank) * kRows, col = it.tk * p.bn + rank * (p.bn >> 1);
+        const bool wide = p.bn == 256;  // else half of the columns: one box of 64 of them
         kk += it.k0;
         uint8_t* const b = dst + fused::kOperandBytes;
         constexpr int kChunk = fused::kOperandBytes / 2;
@@ -80,20 +83,20 @@ struct GradJob {
             const int z = p.segs * p.parts - 1 - i, seg = z % p.segs;  // z = part * segs + segment; the smallest part first
             tma_load_3d(dst, &p.d_k, k, row, z, bar);
             tma_load_3d(b, &p.w, col, k, seg, bar);
-            tma_load_3d(b + kChunk, &p.w, col + 64, k, seg, bar);
+            if (wide) tma_load_3d(b + kChunk, &p.w, col + 64, k, seg, bar);
         } else {
             const int i = kk / p.steps_m, k = (kk - i * p.steps_m) * kBK, z = (p.parts - 1 - i) * p.segs + it.seg;
             tma_load_3d(dst, &p.d_mn, row, k, z, bar);
             tma_load_3d(dst + kChunk, &p.d_mn, row + 64, k, z, bar);
             tma_load_3d(b, &p.a, col, k, 0, bar);
-            tma_load_3d(b + kChunk, &p.a, col + 64, k, 0, bar);
+            if (wide) tma_load_3d(b + kChunk, &p.a, col + 64, k, 0, bar);
         }
     }
-    // a warp's 32 x 32 sums, from column c of the 256
+    // a warp's 32 x 32 sums, from column c of the accumulator
     static __device__ __forceinline__ void put(const Params& p, const Item& it, const fused::Epi& e, int c, float (&v)[32]) {
         const Target& t = it.seg < 0 ? p.da : p.dw;
         const int64_t row = (int64_t)it.tm * 256 + e.r0;
-        const int col = it.tk * 256 + c, rows = (int)min((int64_t)32, t.rows - row), n = min(32, p.cols - col);
+        const int col = it.tk * p.bn + c, rows = (int)min((int64_t)32, t.rows - row), n = min(32, p.cols - col);
         if (rows <= 0 || n <= 0) return;
         const int64_t segs = it.seg < 0 ? 1 : p.segs, out_row = row + (it.seg > 0 ? (int64_t)it.seg * t.rows : 0);
         if (t.sums.p) {
@@ -116,7 +119,7 @@ struct GradJob {
     }
     static __device__ __forceinline__ void epilogue(const Params& p, const Item& it, const fused::Epi& e) {
 #pragma unroll 1
-        for (int c = e.half * 128; c < e.half * 128 + 128; c += 32) {
+        for (int c = e.half * (p.bn >> 1); c < (e.half + 1) * (p.bn >> 1); c += 32) {
             __syncwarp();
             uint32_t u[32];
             tmem_ld32(e.tmem + (uint32_t)c, u);
@@ -128,7 +131,8 @@ struct GradJob {
     }
     static __device__ __forceinline__ void finish(const Params& p, const Item& it, const fused::Epi& e, float (&v)[4][32]) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) put(p, it, e, e.half * 128 + 32 * q, v[q]);
+        for (int q = 0; q < 4; ++q)
+            if (64 * q < p.bn) put(p, it, e, e.half * (p.bn >> 1) + 32 * q, v[q]);
     }
 };
 
@@ -219,9 +223,11 @@ struct Lines {
 };
 // Both operands in one launch: blocks 0 .. first_blocks - 1 take the first.
 __global__ void __launch_bounds__(256) decode_pair_kernel(Lines first, Lines second, unsigned first_blocks, int64_t pitch, uint32_t items_per_row, int nb,
-                                                           const int* gate) {
+                                                           const int* gate, int* zero, int n_zero) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the product's set-up may begin
     if (gate && *gate == 0) return;
+    if (blockIdx.x == 0)
+        for (int i = threadIdx.x; i < n_zero; i += 256) zero[i] = 0;
     const bool one = blockIdx.x < first_blocks;
     const Lines& l = one ? first : second;
     const int64_t at = (int64_t)(one ? blockIdx.x : blockIdx.x - first_blocks) * 256 + threadIdx.x, stride = (int64_t)(one ? first_blocks : gridDim.x - first_blocks) * 256;
@@ -235,7 +241,7 @@ __global__ void __launch_bounds__(256) decode_pair_kernel(Lines first, Lines sec
 }  // namespace
 
 int decode_pair(const bdr_planes_t& a, int m_a, int64_t rows_a, __nv_bfloat16* out_a, const bdr_planes_t& w, int m_w, int64_t rows_w, __nv_bfloat16* out_w,
-                int64_t K, int64_t pitch, cudaStream_t st, const int* gate) {
+                int64_t K, int64_t pitch, cudaStream_t st, const int* gate, int* zero, int64_t n_zero) {
     Lines l[2] = {{a, out_a, rows_a, m_a}, {w, out_w, rows_w, m_w}};
     const int64_t per_row = (K + 31) / 32;
     for (Lines& x : l) {
@@ -248,10 +254,10 @@ int decode_pair(const bdr_planes_t& a, int m_a, int64_t rows_a, __nv_bfloat16* o
         }
         x.n_items *= per_row;
     }
-    if (l[0].n_items + l[1].n_items == 0) return BDR_OK;
+    if (l[0].n_items + l[1].n_items == 0) return n_zero == 0 || cudaMemsetAsync(zero, 0, n_zero * 4, st) == cudaSuccess ? BDR_OK : BDR_ERR_CUDA;
     unsigned blocks[2];
     for (int i = 0; i < 2; ++i) blocks[i] = (unsigned)std::min<int64_t>((l[i].n_items + 255) / 256, (int64_t)sm_count() * (gate ? 4 : 32));  // behind a gate it rarely has anything to do
-    decode_pair_kernel<<<blocks[0] + blocks[1], 256, 0, st>>>(l[0], l[1], blocks[0], pitch, (uint32_t)per_row, (int)((K + 15) / 16), gate);
+    decode_pair_kernel<<<blocks[0] + blocks[1], 256, 0, st>>>(l[0], l[1], blocks[0], pitch, (uint32_t)per_row, (int)((K + 15) / 16), gate, zero, (int)n_zero);
     return cudaGetLastError() == cudaSuccess ? BDR_OK : BDR_ERR_CUDA;
 }
 
@@ -268,7 +274,7 @@ static int grad_cut(int64_t tiles, int64_t steps, int64_t share) {
 }
 // Bytes of the fp32 sums that launch_grad_products may need for M tokens and any number of outputs up to N: at most 2 x 74 tiles of each product.
 int64_t grad_sums_bytes(int64_t M, int64_t N, int64_t K, int segs) {
-    const int64_t most = 2 * kPlanClusters * 256 / ((K + 255) / 256) + 1;
+    const int64_t most = 2 * kPlanClusters * 256 / ((K + 255) / 256) + 1;  // (tiles of 128 columns are more, and have as many rows)
     return round_up((std::min(most, 32 * M) + std::min(most, 32 * segs * N)) * line_pitch(K) * 4, 256);
 }
 
@@ -281,10 +287,11 @@ static int launch_grads(const GradProducts& g, cudaStream_t st) {
         !fused::make_map(&p.w, g.w, g.K, g.N, g.segs, g.pitch_k, g.N * g.pitch_k, kBK) ||
         !fused::make_map(&p.a, g.a, g.K, g.M, 1, g.pitch_k, g.M * g.pitch_k, kBK))
         return BDR_ERR_CUDA;
-    p.bn = 256;
     p.tiles_m = (int)((g.M + 255) / 256);
     p.tiles_n = (int)((g.N + 255) / 256);
-    p.tiles_k = (int)((g.K + 255) / 256);
+    // A step of 128 columns takes almost as long as one of 256: the narrow accumulator is for tiles that all find a cluster at once.
+    p.bn = ((g.da ? p.tiles_m : 0) + (g.dw ? g.segs * p.tiles_n : 0)) * ((g.K + 127) / 128) <= kPlanClusters ? 128 : 256;
+    p.tiles_k = (int)((g.K + p.bn - 1) / p.bn);
     p.steps_n = (int)((g.N + kBK - 1) / kBK);
     p.steps_m = (int)((g.M + kBK - 1) / kBK);
     p.segs = g.segs; p.parts = g.parts; p.scale = g.scale;

@@ -58,6 +58,23 @@ def test_formats(fa, fw, m):
     f.check(loss, want, eloss, "loss")
 
 
+@pytest.mark.parametrize("m,v,k", [(256, 500, 3584), (40, 100, 4001), (33, 60, 8192), (300, 300, 2000), (520, 700, 1500)])
+def test_few_tiles_with_long_sums(m, v, k):
+    # the sums of a tile are shared out to several clusters
+    (pa, a), (pw, w), targets, gen = operands(m, v, k, "mx9", "mx6", 10, 1.0)
+    runs = [run(pa, pw, "mx9", "mx6", m, v, k, targets) for _ in range(3)]
+    want, want_lse, _, eloss, else_, _ = f.entropy(a, w, targets)
+    f.check(runs[0][1], want_lse, else_, "lse")
+    f.check(runs[0][0], want, eloss, "loss")
+    dloss = torch.rand(m, device="cuda", generator=gen)
+    out = [run_grads(pa, pw, "mx9", "mx6", m, v, k, targets, runs[0][1], dloss, torch.float32) for _ in range(3)]
+    want_a, want_w, ea, ew = f.entropy_grads(a, w, targets, runs[0][1].double(), dloss.double(), torch.float32)
+    f.check(out[0][0], want_a, ea, "da")
+    f.check(out[0][1], want_w, ew, "dw")
+    for i in (1, 2):
+        assert all(torch.equal(x, y) for x, y in zip(runs[i], runs[0])) and all(torch.equal(x, y) for x, y in zip(out[i], out[0]))
+
+
 GRAD_SIZES = [(1, 1, 1), (1, 300, 64), (3, 127, 300), (128, 256, 64), (257, 130, 200), (300, 1000, 1111), (70, 2100, 520)]
 
 

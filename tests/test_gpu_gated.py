@@ -51,6 +51,31 @@ def test_formats(fa, fw):
     assert torch.equal(h, again)
 
 
+@pytest.mark.parametrize("m,n,k", [(256, 256, 3584), (40, 100, 4001), (33, 20, 8192), (300, 64, 2000), (520, 300, 1500), (1, 31, 640)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_few_tiles_with_long_sums(m, n, k, dtype):
+    # the sums of a tile are shared out to several clusters
+    (pa, a), (pw, w), gen = operands(m, n, k, "mx9", "mx6", 8)
+    runs = [run_forward(pa, pw, "mx9", "mx6", m, n, k, dtype, "silu") for _ in range(3)]
+    want, products, eh, e = f.gated(a, w, n, "silu")
+    f.check(runs[0][1], products, e + f.HALF_STEP[dtype] * (products.abs() + e), "gate_up")
+    f.check(runs[0][0], want, eh + f.HALF_STEP[dtype] * (want.abs() + eh) + 2.0 ** -126, "h")
+    for h, gu in runs[1:]:
+        assert torch.equal(h, runs[0][0]) and torch.equal(gu, runs[0][1])
+    dh = (torch.randn(m, n, device="cuda", generator=gen) * 1e-2).to(dtype)
+    ws = f.workspace(bdr.mx_gated_gemm_bwd_workspace_bytes(m, n, k, dtype))
+    out = []
+    for _ in range(3):
+        da, dw = torch.empty(m, k, device="cuda", dtype=dtype), torch.empty(2 * n, k, device="cuda", dtype=dtype)
+        bdr.mx_gated_gemm_bwd(bdr.MX9, pa, bdr.MX6, pw, m, n, k, dh, da, dw, ws)
+        out.append((da, dw))
+    want_a, want_w, ea, ew = f.gated_grads(a, w, n, "silu", dh.double(), products, e, dtype)
+    f.check(out[0][0], want_a, ea, "da")
+    f.check(out[0][1], want_w, ew, "dw")
+    for da, dw in out[1:]:
+        assert torch.equal(da, out[0][0]) and torch.equal(dw, out[0][1])
+
+
 GRAD_SIZES = [(1, 1, 1), (1, 130, 70), (3, 5, 300), (128, 64, 256), (257, 129, 200), (300, 250, 1111), (700, 300, 264)]
 
 
