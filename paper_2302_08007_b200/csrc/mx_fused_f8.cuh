@@ -37,7 +37,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads8, 1) fused_
     uint8_t* stages = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     uint8_t* const tiles = stages + kStages8 * kStage8Bytes;
     Bars8& bars = *reinterpret_cast<Bars8*>(tiles + kEpiWarps * kTileBytes);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();
     const int cluster_id = blockIdx.x >> 1, n_clusters = gridDim.x >> 1, steps = p.f8.steps;
 
@@ -67,73 +67,77 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads8, 1) fused_
     if (!open) {
         // nothing to do but to give the tensor memory back
     } else if (warp == 0) {
-        if (lane == 0) {
-            uint64_t* const my_full = rank == 0 ? bars.full : bars.full_local;
-            bool ok = true;
-            int stage = 0, turn = 0;
-            for (int i = cluster_id; i < p.n_items && ok; i += n_clusters) {
-                const typename Job::Item item = Job::item(p, i);
-                for (int kk = 0; kk < steps; ++kk) {
-                    if (turn > 0) {
-                        ok = mbar_wait(&bars.empty[stage], (turn - 1) & 1);
-                        if (!ok) break;
-                    }
+        uint64_t* const my_full = rank == 0 ? bars.full : bars.full_local;
+        bool ok = true;
+        int stage = 0, turn = 0;
+        for (int i = cluster_id; i < p.n_items && ok; i += n_clusters) {
+            const typename Job::Item item = Job::item(p, i);
+            for (int kk = 0; kk < steps; ++kk) {
+                if (turn > 0) {
+                    ok = mbar_wait(&bars.empty[stage], (turn - 1) & 1);
+                    if (!ok) break;
+                }
+                if (elect_one()) {
                     mbar_expect_tx(&my_full[stage], kTx8Bytes);
                     Job::load8(p, item, kk, (int)rank, stages + stage * kStage8Bytes, &my_full[stage]);
-                    if (++stage == kStages8) { stage = 0; ++turn; }
                 }
+                __syncwarp();
+                if (++stage == kStages8) { stage = 0; ++turn; }
             }
-            if (!ok) {
-                bars.failed = 1;
-                // the copies still on their way: one more bounded wait for each
-                for (int s = 0; s < kStages8; ++s)
-                    if (s < stage || turn > 0) mbar_wait(&my_full[s], (s < stage ? turn : turn - 1) & 1);
-            }
+        }
+        if (!ok) {
+            bars.failed = 1;
+            // the copies still on their way: one more bounded wait for each
+            for (int s = 0; s < kStages8; ++s)
+                if (s < stage || turn > 0) mbar_wait(&my_full[s], (s < stage ? turn : turn - 1) & 1);
         }
         __syncwarp();
     } else if (warp == 1) {
-        if (lane == 0) {
-            bool ok = true;
-            int stage = 0, turn = 0;
-            if (rank == 0) {
-                int tcount = 0;
-                for (int i = cluster_id; i < p.n_items && ok; i += n_clusters, ++tcount) {
-                    if (tcount >= 1) {  // the epilogues of both CTAs hold the item before in registers
-                        ok = mbar_wait_cluster(&bars.tmem_empty, (tcount - 1) & 1);
-                        if (!ok) break;
-                        tc_fence_after();
-                    }
-                    for (int kk = 0; kk < steps; ++kk) {
-                        ok = mbar_wait_cluster(&bars.sf_ready[stage], turn & 1);  // data landed, scales copied
-                        if (!ok) break;
-                        tc_fence_after();
-                        const uint32_t sa = smem_u32(stages + stage * kStage8Bytes);
-                        const uint32_t tsfa = tmem_base + kScaleCol0 + (uint32_t)stage * kScaleCols, tsfb = tsfa + 4;
-                        const uint64_t da = make_smem_desc(sa), db = make_smem_desc(sa + kRows * kK8);
+        bool ok = true;
+        int stage = 0, turn = 0;
+        if (rank == 0) {
+            int tcount = 0;
+            for (int i = cluster_id; i < p.n_items && ok; i += n_clusters, ++tcount) {
+                if (tcount >= 1) {  // the epilogues of both CTAs hold the item before in registers
+                    ok = mbar_wait_cluster(&bars.tmem_empty, (tcount - 1) & 1);
+                    if (!ok) break;
+                    tc_fence_after();
+                }
+                for (int kk = 0; kk < steps; ++kk) {
+                    ok = mbar_wait_cluster(&bars.sf_ready[stage], turn & 1);  // data landed, scales copied
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t sa = smem_u32(stages + stage * kStage8Bytes);
+                    const uint32_t tsfa = tmem_base + kScaleCol0 + (uint32_t)stage * kScaleCols, tsfb = tsfa + 4;
+                    const uint64_t da = make_smem_desc(sa), db = make_smem_desc(sa + kRows * kK8);
+                    if (elect_one()) {
 #pragma unroll
                         for (int k = 0; k < kK8 / 32; ++k)  // 32 bytes of K per MMA; scale byte k of the columns
                             umma2_mxf8(tmem_base, da + (uint64_t)(2 * k), db + (uint64_t)(2 * k), kF8InstrDesc | ((uint32_t)k << 29) | ((uint32_t)k << 4),
                                        (kk | k) != 0, tsfa, tsfb);
                         umma_commit2(&bars.empty[stage]);
-                        if (++stage == kStages8) { stage = 0; ++turn; }
                     }
-                    if (ok) umma_commit2(&bars.tmem_full);
+                    __syncwarp();
+                    if (++stage == kStages8) { stage = 0; ++turn; }
                 }
-            } else {
-                for (int i = cluster_id; i < p.n_items && ok; i += n_clusters)
-                    for (int kk = 0; kk < steps; ++kk) {
-                        ok = mbar_wait(&bars.full_local[stage], turn & 1);
-                        if (!ok) break;
-                        mbar_arrive_cluster(&bars.full[stage], 0);
-                        if (++stage == kStages8) { stage = 0; ++turn; }
-                    }
+                if (ok && elect_one()) umma_commit2(&bars.tmem_full);
+                __syncwarp();
             }
-            if (!ok) bars.failed = 1;
+        } else {
+            for (int i = cluster_id; i < p.n_items && ok; i += n_clusters)
+                for (int kk = 0; kk < steps; ++kk) {
+                    ok = mbar_wait(&bars.full_local[stage], turn & 1);
+                    if (!ok) break;
+                    if (elect_one()) mbar_arrive_cluster(&bars.full[stage], 0);
+                    __syncwarp();
+                    if (++stage == kStages8) { stage = 0; ++turn; }
+                }
         }
+        if (!ok) bars.failed = 1;
         __syncwarp();
         tc_fence_before();
     } else if (warp == kCopyWarp8) {
-        if (lane == 0 && rank == 0) {
+        if (rank == 0) {
             bool ok = true;
             int stage = 0, turn = 0;
             for (int i = cluster_id; i < p.n_items && ok; i += n_clusters)
@@ -144,10 +148,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads8, 1) fused_
                     tc_fence_after();
                     const uint32_t sf = smem_u32(stages + stage * kStage8Bytes) + kTiles8;
                     const uint32_t tsfa = tmem_base + kScaleCol0 + (uint32_t)stage * kScaleCols;
-                    sf_copy2(tsfa, make_sf_desc(sf));
-                    sf_copy2(tsfa + 4, make_sf_desc(sf + 512));
-                    sf_copy2(tsfa + 8, make_sf_desc(sf + 1024));
-                    umma_commit2_leader(&bars.sf_ready[stage]);
+                    if (elect_one()) {
+                        sf_copy2(tsfa, make_sf_desc(sf));
+                        sf_copy2(tsfa + 4, make_sf_desc(sf + 512));
+                        sf_copy2(tsfa + 8, make_sf_desc(sf + 1024));
+                        umma_commit2_leader(&bars.sf_ready[stage]);
+                    }
+                    __syncwarp();
                     if (++stage == kStages8) { stage = 0; ++turn; }
                 }
             if (!ok) bars.failed = 1;
