@@ -536,9 +536,11 @@ __device__ __forceinline__ void store_parts(const Epi& e, const Rows& d, int64_t
 }
 
 // How a product of tiles_m x cols is shared out: the accumulator's columns (cols_div of them for each of the product's) and the items that a
-// tile's K steps are cut into.  A step takes about 480 + 0.55 bn clocks (measured from 64 to 256 columns: below 256 it is the barriers and the
-// instructions' issue that count), an item's start and epilogue 1500 at 256 columns; narrow tiles pay where wide ones would leave clusters
-// idle.  A cut pays where few tiles have long sums: it costs the way through memory and back, and the last warp's reading of all parts.
+// tile's K steps are cut into.  Measured, a step takes about 640, 360 and 310 clocks at 256, 128 and 64 columns (the last two are bound by
+// barriers and issue rather than by the tensor core), an item's start and epilogue 1500 at 256: narrower tiles pay where they save a round or
+// fill idle clusters (300 x 2000 x 1024: 11.5, 9.1 and 11.5 us; 1003 x 2747 x 1500: 22.8, 21.1, 28.9).  A cut pays where few tiles have long sums: it costs
+// the way through memory and back, and the last warp's reading of all parts (64 columns, 300 x 300 x 8192 26.1 us, in three 17.2; 256 x 256 x 3584
+// 13.7, 11.8; 256 x 256 x 1280 8.0, 10.1).
 constexpr int kClusters = 74;  // (the workspaces' sizes follow from it, without a GPU)
 struct Share {
     int bn, tiles_n, splits, span;
@@ -556,7 +558,7 @@ inline Share share_product(int64_t tiles_m, int64_t cols, int cols_div, int64_t 
             const int64_t span = (steps + want - 1) / want, splits = (steps + span - 1) / span;
             if (splits != want) continue;
             const double rounds = (double)((tiles * splits + kClusters - 1) / kClusters);
-            const double t = rounds * (span * (480 + 0.55 * bn) + 1500.0 * bn / 256) + (splits > 1 ? 9000 + splits * 400.0 * bn / 64 : 0);
+            const double t = rounds * (span * (bn == 256 ? 640.0 : (bn == 128 ? 360.0 : 310.0)) + 1500.0 * bn / 256) + (splits < 2 ? 0.0 : (bn == 256 ? 7000.0 + 2200.0 * splits : 3500.0 + 1600.0 * splits));
             if (!best.bn || t < 0.97 * least) {
                 best = {bn, (int)tiles_n, (int)splits, (int)span};
                 least = t;
