@@ -129,6 +129,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();
     const int cluster_id = blockIdx.x >> 1, n_clusters = gridDim.x >> 1;
+    // Items are dealt out in rounds, all but the first in reverse: long items come first, and whoever got one of those comes last in a round
+    // that is not full.
+    auto next_item = [&](int i) { return i < n_clusters ? 2 * n_clusters - 1 - cluster_id : i + n_clusters; };
     const int stage_bytes = kOperandBytes + 64 * p.bn, n_stages = min(kMostStages, kStages * kStageBytes / stage_bytes);
 
     if (threadIdx.x == 0) {
@@ -166,7 +169,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
         uint64_t* const my_full = rank == 0 ? bars.full : bars.full_local;
         bool ok = true;
         int stage = 0, turn = 0;  // of the ring
-        for (int i = cluster_id; i < p.n_items && ok; i += n_clusters) {
+        for (int i = cluster_id; i < p.n_items && ok; i = next_item(i)) {
             const typename Job::Item item = Job::item(p, i);
             for (int kk = 0; kk < item.steps; ++kk) {
                 if (turn > 0) {
@@ -193,7 +196,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
         int stage = 0, turn = 0;
         if (rank == 0) {
             int tcount = 0;
-            for (int i = cluster_id; i < p.n_items && ok; i += n_clusters, ++tcount) {
+            for (int i = cluster_id; i < p.n_items && ok; i = next_item(i), ++tcount) {
                 const typename Job::Item item = Job::item(p, i);
                 const bool a_mn = Job::a_mn(item);
                 const uint32_t idesc = kIdesc | ((uint32_t)(p.bn >> 3) << 17) | (a_mn ? kMnA : 0u) | (Job::b_mn ? kMnB : 0u);
@@ -235,7 +238,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
                 __syncwarp();
             }
         } else {
-            for (int i = cluster_id; i < p.n_items && ok; i += n_clusters) {
+            for (int i = cluster_id; i < p.n_items && ok; i = next_item(i)) {
                 const typename Job::Item item = Job::item(p, i);
                 for (int kk = 0; kk < item.steps; ++kk) {
                     ok = mbar_wait(&bars.full_local[stage], turn & 1);
@@ -254,7 +257,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
         const uint32_t my_lanes = (uint32_t)((warp & 3) * 32) << 16;  // the tensor-memory lanes this warp may read
         bool ok = true;
         int tcount = 0;
-        for (int i = cluster_id; i < p.n_items; i += n_clusters, ++tcount) {
+        for (int i = cluster_id; i < p.n_items; i = next_item(i), ++tcount) {
             const typename Job::Item item = Job::item(p, i);
             Epi e;
             e.r0 = (int)rank * kRows + (warp & 3) * 32;

@@ -52,7 +52,7 @@ struct GradJob {
     static constexpr bool b_mn = true;
     static constexpr bool kCut = false;
     static __device__ __forceinline__ void prefetch(const Params& p) { prefetch_map(&p.d_k); prefetch_map(&p.d_mn); prefetch_map(&p.w); prefetch_map(&p.a); }
-    static constexpr int kSpan = F32 ? 4 : 0;  // 16 instructions in a chain
+    static constexpr int kSpan = F32 ? 4 : 0;  // 16 instructions in a chain (32: 4 % faster; 2.6e-7 of a result lost, 5e-7 with 32)
     static __device__ __forceinline__ bool a_mn(const Item& it) { return it.seg >= 0; }
     static __device__ __forceinline__ Item item(const Params& p, int i) {
         Item it;
@@ -198,7 +198,8 @@ __device__ __forceinline__ void decode_items(const bdr_planes_t& in, __nv_bfloat
         // (pitches are multiples of 16 bytes: the second of the two scale bytes is in the line's pitch even where there is no such block)
         const uint32_t Fw = __ldg(reinterpret_cast<const uint16_t*>(in.exps + row * in.ld_exps) + it);
         const uint32_t mw = __ldg(reinterpret_cast<const uint16_t*>(in.micro + row * in.ld_micro) + it);
-        const uint32_t F0 = Fw & 0xFFu, F1 = Fw >> 8;
+        // (a block that is not there takes the other's exponent: whatever its padding holds must not send the warp the slow way)
+        const uint32_t F0 = Fw & 0xFFu, F1 = 2 * (int)it + 1 < nb ? Fw >> 8 : F0;
         if ((F0 - x2::kMinF <= (uint32_t)(x2::kMaxDecodeF - x2::kMinF)) && (F1 - x2::kMinF <= (uint32_t)(x2::kMaxDecodeF - x2::kMinF))) {
             x2::decode_two_blocks_row<W>(s, F0, F1, mw, yw);
         } else {
@@ -263,14 +264,14 @@ int decode_pair(const bdr_planes_t& a, int m_a, int64_t rows_a, __nv_bfloat16* o
 
 // How the K steps of the two products are cut.  Few tiles with long sums (dA of few tokens, dW of a narrow layer) would keep few clusters
 // busy: their steps go to several clusters, whose fp32 sums another kernel adds in order.  That costs a launch (about 3 us) and a pass over the
-// sums, so a cut has to shorten the longest item by 16 steps (of 0.27 us) at least.
+// sums, so a cut has to shorten the longest item by 24 steps (of 0.16 to 0.3 us) at least.
 constexpr int kPlanClusters = 74;
 static int grad_cut(int64_t tiles, int64_t steps, int64_t share) {
     const int64_t most = std::min<int64_t>(32, 2 * kPlanClusters / tiles);
     const int64_t n = std::min(most, (steps + share - 1) / share);
     if (n < 2) return 1;
     const int64_t span = (steps + n - 1) / n;
-    return steps - span < 16 ? 1 : (int)((steps + span - 1) / span);
+    return steps - span < 24 ? 1 : (int)((steps + span - 1) / span);
 }
 // Bytes of the fp32 sums that launch_grad_products may need for M tokens and any number of outputs up to N: at most 2 x 74 tiles of each product.
 int64_t grad_sums_bytes(int64_t M, int64_t N, int64_t K, int segs) {
