@@ -257,6 +257,12 @@ int64_t piece_columns(int64_t V, int64_t most) {
 }
 constexpr int64_t kMostWeights = 512ll << 20;   // bytes of decoded weights at a time
 constexpr int64_t kMostD = 256ll << 20;         // bytes of d at a time
+// Columns of a piece that are decoded, and multiplied, at a time: a large piece goes in four parts, each decoded beside the product of the one before
+// (4096 x 32000 x 4096 MX9: 692 us in one part, 682 in four; 837 and 818 in a long run).  A part has more tiles than there are clusters, twice over.
+int64_t part_columns(int64_t M, int64_t cols, int64_t K) {
+    const int64_t part = round_up((cols + 3) / 4, 256);
+    return cols * K >= 1ll << 25 && ((M + 255) / 256) * (part / 256) >= 4 * fused::kClusters / 2 ? part : cols;
+}
 
 struct EntropySpace {
     int64_t pitch_k, piece, a, w, parts, hit, flag, partials, counters, n_counters, bytes;
@@ -265,7 +271,7 @@ struct EntropySpace {
         piece = piece_columns(V, kMostWeights / (pitch_k * 2));
         a = 0;
         w = a + round_up(M * pitch_k * 2, 256);  // few rows: their logits instead
-        parts = w + (M <= kFewRows ? round_up(M * round_up(V, 64) * 4, 256) : round_up(std::min(piece, V) * pitch_k * 2, 256));
+        parts = w + (few_rows(M, V, K) ? round_up(M * round_up(V, 64) * 4, 256) : round_up(std::min(piece, V) * pitch_k * 2, 256));
         parts = std::max(parts, fused::f8_bytes(M, std::min(piece, V), K));
         hit = parts + round_up((V + 31) / 32 * M * 8, 256);
         flag = hit + round_up(M * 4, 256);
@@ -362,7 +368,7 @@ int mx_cross_entropy(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bdr
     if ((uintptr_t)workspace % 256) return BDR_ERR_MISALIGNED;
     cudaStream_t st = (cudaStream_t)stream;
     uint8_t* const ws = static_cast<uint8_t*>(workspace);
-    if (M <= kFewRows) {
+    if (few_rows(M, V, K)) {
         __nv_bfloat16* const x = reinterpret_cast<__nv_bfloat16*>(ws + s.a);
         float *const logits = reinterpret_cast<float*>(ws + s.w), *const hit = reinterpret_cast<float*>(ws + s.hit);
         float2* const parts = reinterpret_cast<float2*>(ws + s.parts);
@@ -373,7 +379,7 @@ int mx_cross_entropy(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bdr
         if ((rc = mx_gemv(cfg_w, w, V, K, x, BDR_BF16, s.pitch_k, M, logits, BDR_F32, pitch, stream))) return rc;
         entropy_rows_kernel<<<dim3((unsigned)chunks, (unsigned)M), 256, 0, st>>>(logits, pitch, M, V, targets, parts, hit);
         if (cudaGetLastError() != cudaSuccess) return BDR_ERR_CUDA;
-        return launch_dependent(entropy_join_kernel, dim3(1), dim3(1024), st, (const float2*)parts, (int)chunks, M, (const float*)hit, targets, V, loss, lse, status);
+        return launch_dependent(entropy_join_kernel, dim3((unsigned)((M + 31) / 32)), dim3(1024), st, (const float2*)parts, (int)chunks, M, (const float*)hit, targets, V, loss, lse, status);
     }
     EntropyJob<false>::Params p = {};
     p.targets = targets;
@@ -394,10 +400,16 @@ int mx_cross_entropy(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bdr
             if ((rc = fused::encode_f8(*a, cfg_a->m, M, lines, cfg_w->m, cols, 1, K, ws, reinterpret_cast<int*>(ws + s.flag), &p.f8, &p.gate, st))) return rc;
             if ((rc = fused::launch_f8<EntropyJob<false>>(p, st))) return rc;
         }
-        // (with an 8-bit path in front, A's bf16 values are overwritten by the next piece's bytes)
-        if ((rc = decode_pair(*a, cfg_a->m, v == 0 || f8 ? M : 0, wa, lines, cfg_w->m, cols, ww, K, s.pitch_k, st, p.gate, p.counters, s.n_counters)))
-            return rc;
-        if ((rc = fused::launch<EntropyJob<false>>(p, st))) return rc;
+        const int64_t part = f8 ? cols : part_columns(M, cols, K);
+        for (int64_t c = 0; c < cols; c += part) {
+            const int64_t n = std::min(part, cols - c);
+            // (with an 8-bit path in front, A's bf16 values are overwritten by the next piece's bytes)
+            if ((rc = decode_pair(*a, cfg_a->m, c == 0 && (v == 0 || f8) ? M : 0, wa, lines_from(*w, v + c), cfg_w->m, n, ww + c * s.pitch_k, K, s.pitch_k, st, p.gate,
+                                  p.counters, s.n_counters, c > 0)))
+                return rc;
+            if (part < cols && (rc = set_piece(p, M, K, v + c, n, s.pitch_k, ws + s.a, ws + s.w + c * s.pitch_k * 2, f8))) return rc;
+            if ((rc = fused::launch<EntropyJob<false>>(p, st))) return rc;
+        }
     }
     const int n_parts = (int)((V + p.bn / 2 - 1) / (p.bn / 2));
     return launch_dependent(entropy_join_kernel, dim3((unsigned)((M + 31) / 32)), dim3(1024), st, (const float2*)p.parts, n_parts, M, (const float*)p.hit, targets,
@@ -464,7 +476,8 @@ int mx_cross_entropy_bwd(const bdr_config_t* cfg_a, const bdr_planes_t* a, const
     for (int64_t v = 0; v < V; v += s.piece) {
         const int64_t cols = std::min(s.piece, V - v);
         const bdr_planes_t lines = lines_from(*w, v);
-        if ((rc = decode_pair(*a, cfg_a->m, v == 0 ? M : 0, wa, lines, cfg_w->m, cols, ww, K, s.pitch_k, st, nullptr, p.counters, s.n_counters))) return rc;
+        const int64_t part = f8 ? cols : part_columns(M, cols, K);
+        if ((rc = decode_pair(*a, cfg_a->m, v == 0 ? M : 0, wa, lines, cfg_w->m, part, ww, K, s.pitch_k, st, nullptr, p.counters, s.n_counters))) return rc;
         if (v == 0 && (rc = launch_dependent(entropy_scale_kernel, dim3(1), dim3(1024), st, dloss, targets, M, V, reinterpret_cast<float*>(ws + s.largest))))
             return rc;
         if ((rc = set_piece(p, M, K, v, cols, s.pitch_k, ws + s.a, ws + s.w, f8))) return rc;
@@ -472,7 +485,15 @@ int mx_cross_entropy_bwd(const bdr_config_t* cfg_a, const bdr_planes_t* a, const
             if ((rc = fused::encode_f8(*a, cfg_a->m, M, lines, cfg_w->m, cols, 1, K, ws + s.f8, reinterpret_cast<int*>(ws + s.flag), &p.f8, &p.gate, st))) return rc;
             if ((rc = fused::launch_f8<EntropyJob<true>>(p, st))) return rc;
         }
-        if ((rc = fused::launch<EntropyJob<true>>(p, st))) return rc;
+        for (int64_t c = 0; c < cols; c += part) {
+            const int64_t n = std::min(part, cols - c);
+            if (c > 0 && (rc = decode_pair(*a, cfg_a->m, 0, wa, lines_from(*w, v + c), cfg_w->m, n, ww + c * s.pitch_k, K, s.pitch_k, st, nullptr, p.counters,
+                                           s.n_counters, true)))
+                return rc;
+            if (part < cols && (rc = set_piece(p, M, K, v + c, n, s.pitch_k, ws + s.a, ws + s.w + c * s.pitch_k * 2, f8))) return rc;
+            p.d = fused::make_rows(ws + s.d + c * 2, s.piece, false);
+            if ((rc = fused::launch<EntropyJob<true>>(p, st))) return rc;
+        }
         g.N = cols;
         g.dw = dw ? static_cast<char*>(dw) + v * ld_dw * width : nullptr;
         g.first = v == 0;

@@ -19,8 +19,10 @@ constexpr int64_t line_pitch(int64_t K) { return round_up(K, 32); }
 
 // Packed lines of K elements (Table II formats, m magnitude bits) of two operands -> bf16 [rows, pitch]; what lies behind K in a row is
 // unspecified.  gate: NULL, or device flag without which nothing is decoded.  n_zero words at `zero` are cleared on the side.
+// beside: the kernel in front in the stream is a product that does not read the output: it is decoded on what that product leaves free of the
+// SMs, and is complete when both are.
 int decode_pair(const bdr_planes_t& a, int m_a, int64_t rows_a, __nv_bfloat16* out_a, const bdr_planes_t& w, int m_w, int64_t rows_w, __nv_bfloat16* out_w,
-                int64_t K, int64_t pitch, cudaStream_t st, const int* gate = nullptr, int* zero = nullptr, int64_t n_zero = 0);
+                int64_t K, int64_t pitch, cudaStream_t st, const int* gate = nullptr, int* zero = nullptr, int64_t n_zero = 0, bool beside = false);
 
 // Launches a kernel without shared memory behind another in the stream so that it is set up while that one drains; the kernel waits for it
 // (griddepcontrol.wait) before it touches memory.
@@ -62,9 +64,12 @@ int launch_grad_products(const GradProducts& g, cudaStream_t st);
 int gated_rows(const bdr_config_t* cfg_w, const bdr_planes_t* w, int64_t N, int64_t K, const __nv_bfloat16* x, int64_t ldx, int64_t T, int act, void* h,
                bdr_dtype_t dt, int64_t ldh, void* products, int64_t ld_products, cudaStream_t st);
 
-// Rows up to which a product is left to the few-token kernel, which reads the packed weights, instead of decoding them for the tensor-core
-// kernel, which would multiply 256 rows all the same.
-constexpr int64_t kFewRows = 32;
+// Few rows are left to the few-token kernel, which reads the packed weights, instead of decoding them for the tensor-core kernel, which would
+// multiply 256 rows all the same.  Measured (gated layer, MX9, few-token and tensor-core kernel): 8000 lines of 1024, 24 rows 17.4 and 21.4 us, 32 rows 19.5 and
+// 21.4, 48 rows 21.5 and 21.4; 2000 lines of 8192, 24 rows 33.8 and 35.8, 32 rows 37.9 and 33.9; 32000 lines of 4096, 16 rows 54 and 140, 48 rows 114 and
+// 140; 1000 lines of 256 alike up to 16 rows, where the cross entropy, which needs two launches more for the few-token kernel's logits, takes 19.5 and 15.4.
+constexpr int64_t kMostFewRows = 48;
+inline bool few_rows(int64_t M, int64_t lines, int64_t K) { return lines * K >= 1ll << 21 && M <= (lines * K >= 1ll << 25 ? kMostFewRows : 24); }
 
 // What the operators accept of two packed operands A [M, K] and W [lines, K] (host).
 int check_fused_operands(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bdr_config_t* cfg_w, const bdr_planes_t* w, int64_t K);

@@ -293,7 +293,7 @@ int mx_gated_gemm(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bdr_co
     if ((uintptr_t)workspace % 256) return BDR_ERR_MISALIGNED;
     cudaStream_t st = (cudaStream_t)stream;
     uint8_t* const ws = static_cast<uint8_t*>(workspace);
-    if (M <= kFewRows) {
+    if (few_rows(M, 2 * N, K)) {
         __nv_bfloat16* const x = reinterpret_cast<__nv_bfloat16*>(ws + s.a);
         if ((rc = decode_pair(*a, cfg_a->m, M, x, *w, cfg_w->m, 0, nullptr, K, s.pitch_k, st))) return rc;
         return gated_rows(cfg_w, w, N, K, x, s.pitch_k, M, act, h, dt, ldh, gate_up, ld_gate_up, st);

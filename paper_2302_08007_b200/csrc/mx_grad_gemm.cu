@@ -224,7 +224,7 @@ struct Lines {
 };
 // Both operands in one launch: blocks 0 .. first_blocks - 1 take the first.
 __global__ void __launch_bounds__(256) decode_pair_kernel(Lines first, Lines second, unsigned first_blocks, int64_t pitch, uint32_t items_per_row, int nb,
-                                                           const int* gate, int* zero, int n_zero) {
+                                                           const int* gate, int* zero, int n_zero, int beside) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the product's set-up may begin
     if (gate && *gate == 0) return;
     if (blockIdx.x == 0)
@@ -237,16 +237,17 @@ __global__ void __launch_bounds__(256) decode_pair_kernel(Lines first, Lines sec
         case 4: decode_items<5>(l.in, l.out, pitch, l.n_items, items_per_row, nb, at, stride); break;
         default: decode_items<8>(l.in, l.out, pitch, l.n_items, items_per_row, nb, at, stride); break;
     }
+    if (beside) asm volatile("griddepcontrol.wait;" ::: "memory");  // not before the product in front: whoever waits for this kernel has both
 }
 
 }  // namespace
 
 int decode_pair(const bdr_planes_t& a, int m_a, int64_t rows_a, __nv_bfloat16* out_a, const bdr_planes_t& w, int m_w, int64_t rows_w, __nv_bfloat16* out_w,
-                int64_t K, int64_t pitch, cudaStream_t st, const int* gate, int* zero, int64_t n_zero) {
+                int64_t K, int64_t pitch, cudaStream_t st, const int* gate, int* zero, int64_t n_zero, bool beside) {
     Lines l[2] = {{a, out_a, rows_a, m_a}, {w, out_w, rows_w, m_w}};
     const int64_t per_row = (K + 31) / 32;
     for (Lines& x : l) {
-        if (!gate && x.n_items * K >= (1ll << 23)) {
+        if (!gate && !beside && x.n_items * K >= (1ll << 23)) {
             QParams qp;
             qp.k1 = 16; qp.k2 = 2; qp.d2 = 1; qp.m = x.m; qp.rounding = BDR_ROUND_NEAREST_EVEN; qp.beta = 1; qp.qmax = (1u << x.m) - 1u;
             const int rc = unpack_rowwise_mx_x2(x.in, x.out, x.n_items, K, pitch, qp, st);  // whole runs of 2048 elements: through shared memory
@@ -256,9 +257,14 @@ int decode_pair(const bdr_planes_t& a, int m_a, int64_t rows_a, __nv_bfloat16* o
         x.n_items *= per_row;
     }
     if (l[0].n_items + l[1].n_items == 0) return n_zero == 0 || cudaMemsetAsync(zero, 0, n_zero * 4, st) == cudaSuccess ? BDR_OK : BDR_ERR_CUDA;
+    // Behind a gate there rarely is anything to do.  Beside a product one block fits on an SM, and stays until it ends: all of the work is theirs.
+    const int64_t most = (int64_t)sm_count() * (beside ? 1 : (gate ? 4 : 32));
     unsigned blocks[2];
-    for (int i = 0; i < 2; ++i) blocks[i] = (unsigned)std::min<int64_t>((l[i].n_items + 255) / 256, (int64_t)sm_count() * (gate ? 4 : 32));  // behind a gate it rarely has anything to do
-    decode_pair_kernel<<<blocks[0] + blocks[1], 256, 0, st>>>(l[0], l[1], blocks[0], pitch, (uint32_t)per_row, (int)((K + 15) / 16), gate, zero, (int)n_zero);
+    for (int i = 0; i < 2; ++i) blocks[i] = (unsigned)std::min<int64_t>((l[i].n_items + 255) / 256, i == 1 && beside ? most - blocks[0] : most);
+    const dim3 grid(blocks[0] + blocks[1]);
+    if (beside)
+        return launch_dependent(decode_pair_kernel, grid, dim3(256), st, l[0], l[1], blocks[0], pitch, (uint32_t)per_row, (int)((K + 15) / 16), gate, zero, (int)n_zero, 1);
+    decode_pair_kernel<<<grid, 256, 0, st>>>(l[0], l[1], blocks[0], pitch, (uint32_t)per_row, (int)((K + 15) / 16), gate, zero, (int)n_zero, 0);
     return cudaGetLastError() == cudaSuccess ? BDR_OK : BDR_ERR_CUDA;
 }
 

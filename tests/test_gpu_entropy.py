@@ -130,6 +130,50 @@ def test_pieces_of_the_vocabulary(dtype):
     f.check(dw, want_w, ew, "dw")
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_parts_of_a_piece(dtype):
+    # large enough that the next columns are decoded while the ones before are multiplied; the last part is ragged
+    m, v, k = 2100, 18100, 2000
+    (pa, a), (pw, w), targets, gen = operands(m, v, k, "mx9", "mx9", 11, 1.0)
+    targets[:4] = torch.tensor([0, v - 1, 4700, 9300], device="cuda")
+    dloss = torch.full((m,), 1.0 / m, device="cuda")
+    runs = []
+    for _ in range(2):
+        loss, lse = run(pa, pw, "mx9", "mx9", m, v, k, targets)
+        runs.append((loss, lse, *run_grads(pa, pw, "mx9", "mx9", m, v, k, targets, lse, dloss, dtype)))
+    assert all(torch.equal(x, y) for x, y in zip(*runs))
+    loss, lse, da, dw = runs[0]
+    want, want_lse, _, eloss, else_, _ = f.entropy(a, w, targets)
+    f.check(lse, want_lse, else_, "lse")
+    f.check(loss, want, eloss, "loss")
+    want_a, want_w, ea, ew = f.entropy_grads(a, w, targets, lse.double(), dloss.double(), dtype)
+    f.check(da, want_a, ea, "da")
+    f.check(dw, want_w, ew, "dw")
+
+
+@pytest.mark.parametrize("m,v,k", [(1, 8200, 260), (7, 70001, 33), (24, 4099, 530), (25, 4099, 530), (1, 32800, 1030), (48, 32801, 1029), (49, 32801, 1029)])
+@pytest.mark.parametrize("fw", ["mx4", "mx9"])
+def test_few_rows(m, v, k, fw):
+    # both sides of the limits up to which the few-token kernel computes the logits
+    (pa, a), (pw, w), targets, gen = operands(m, v, k, "mx9", fw, 12)
+    targets[0] = v - 1
+    if m > 1:
+        targets[1], targets[-1] = -100, 2048
+    bdr.bdr_device_status_reset()
+    loss, lse = run(pa, pw, "mx9", fw, m, v, k, targets)
+    want, want_lse, _, eloss, else_, _ = f.entropy(a, w, targets)
+    f.check(lse, want_lse, else_, "lse")
+    f.check(loss, want, eloss, "loss")
+    if m > 3:
+        targets[2] = v
+        other, other_lse = run(pa, pw, "mx9", fw, m, v, k, targets)
+        assert other.isnan().nonzero()[:, 0].tolist() == [2] and torch.equal(lse, other_lse)
+        assert bdr.bdr_device_status_reset() == -5
+        pa.exps[3, 0] = 0xFF
+        assert run(pa, pw, "mx9", fw, m, v, k, targets)[1].isnan().nonzero()[:, 0].tolist() == [3]
+        bdr.bdr_device_status_reset()
+
+
 def test_rows_that_do_not_count():
     m, v, k = 130, 300, 64
     (pa, a), (pw, w), targets, _ = operands(m, v, k, seed=5)

@@ -64,3 +64,14 @@ def test_entropy(fa, fw, spread):
     f.check(da, want_a, ea, "da")
     f.check(dw, want_w, ew, "dw")
     assert bdr.bdr_device_status() == 0
+
+
+def test_a_block_without_values_poisons_its_own_row():
+    m, n, k = 2304, 1920, 4096
+    gen = torch.Generator(device="cuda").manual_seed(13)
+    pa, a = planes("mx6", m, k, gen, 1.0, False)
+    pw, w = planes("mx6", 2 * n, k, gen, k ** -0.5, False)
+    pa.exps[1000, 3] = 0xFF
+    h = torch.zeros((m, n), device="cuda")
+    bdr.mx_gated_gemm(bdr.MX6, pa, bdr.MX6, pw, m, n, k, h, f.workspace(bdr.mx_gated_gemm_workspace_bytes(m, n, k)))
+    assert h[1000].isnan().all() and int(h.isnan().sum()) == n

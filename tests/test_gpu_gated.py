@@ -76,6 +76,19 @@ def test_few_tiles_with_long_sums(m, n, k, dtype):
         assert torch.equal(da, out[0][0]) and torch.equal(dw, out[0][1])
 
 
+@pytest.mark.parametrize("m,n,k", [(1, 4100, 260), (7, 35001, 33), (24, 2050, 530), (25, 2050, 530), (48, 16401, 1029), (49, 16401, 1029)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_few_rows(m, n, k, dtype):
+    # both sides of the limits up to which the few-token kernel takes the packed rows
+    (pa, a), (pw, w), _ = operands(m, n, k, "mx9", "mx4", 9)
+    for act in f.ACTS if m == 24 else ("silu",):
+        h, gu = run_forward(pa, pw, "mx9", "mx4", m, n, k, dtype, act)
+        want, products, eh, e = f.gated(a, w, n, act)
+        f.check(gu, products, e + f.HALF_STEP[dtype] * (products.abs() + e), "gate_up")
+        f.check(h, want, eh + f.HALF_STEP[dtype] * (want.abs() + eh) + 2.0 ** -126, "h " + act)
+        assert torch.equal(run_forward(pa, pw, "mx9", "mx4", m, n, k, dtype, act, keep=False)[0], h)
+
+
 GRAD_SIZES = [(1, 1, 1), (1, 130, 70), (3, 5, 300), (128, 64, 256), (257, 129, 200), (300, 250, 1111), (700, 300, 264)]
 
 
