@@ -30,7 +30,7 @@ template <bool GRAD>
 struct EntropyJob {
     struct Params {
         CUtensorMap a, w;         // bf16 [M][K]; [columns of this piece][K]
-        int n_items, bn, tiles_m, tiles_n, band_rows, steps, splits, span;
+        int n_items, n_long, extra, bn, tiles_m, tiles_n, band_rows, steps, splits, span;
         float* partials;
         int* counters;
         int M, cols;
@@ -320,7 +320,8 @@ int set_piece(Params& p, int64_t M, int64_t K, int64_t col0, int64_t cols, int64
     p.tiles_n = (int)((cols + p.bn - 1) / p.bn);
     if (!fused::make_map(&p.a, a, K, M, 1, pitch_k, M * pitch_k, kRows) || !fused::make_map(&p.w, w, K, cols, 1, pitch_k, cols * pitch_k, p.bn / 2))
         return BDR_ERR_CUDA;
-    p.n_items = p.tiles_m * p.tiles_n * p.splits;
+    p.n_items = p.n_long = p.tiles_m * p.tiles_n * p.splits;
+    p.extra = 0;
     p.band_rows = gemm_band_rows((M + cols) * K * 2);
     p.M = (int)M;
     p.cols = (int)cols;

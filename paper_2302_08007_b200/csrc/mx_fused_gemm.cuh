@@ -10,7 +10,7 @@
 // A Job has
 //   Params                         kernel argument: tensor maps, sizes, n_items, bn (the accumulator's columns), status; gate: NULL, or device
 //                                  flag without which the kernel does nothing
-//   Item item(p, i)                work item i of p.n_items; Item::steps is its number of K steps of 64
+//   Item item(p, i)                work item i of p.n_items; Item::steps is its number of K steps of 64 (p.n_long, p.extra: see Deal)
 //   load(p, it, kk, rank, dst, bar)   TMA loads of K step kk: A at dst, B kOperandBytes behind it, 16384 + 64 bn bytes in all
 //   a_mn(it), b_mn                 whether an operand lies with its rows (M or N) contiguous instead of K
 //   kSpan                          K steps after which the accumulator is handed to the epilogue: 0 = at the end of the item
@@ -64,6 +64,24 @@ __device__ __forceinline__ uint64_t make_mn_desc(uint32_t smem_addr) {
 }
 // Instruction descriptor: D = fp32, A = B = bf16, M = 256, N = bn; bits 15 and 16: A's, B's rows are contiguous.
 constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(256 >> 4) << 24), kMnA = 1u << 15, kMnB = 1u << 16;
+
+// Which items a cluster takes.  The first n_long items are as long as `extra` of the others, rounded down.  They are dealt out in rounds; the clusters that
+// a last round of them does not reach take `extra` of the others each, and the rest is dealt out in rounds again, from the other end.
+struct Deal {
+    int n_items, n_long, extra, cluster, clusters;
+    __device__ __forceinline__ int reached() const { return n_long % clusters; }
+    __device__ __forceinline__ int extras() const { return reached() ? (clusters - reached()) * extra : 0; }
+    __device__ __forceinline__ int rest() const { return n_long + extras() + clusters - 1 - cluster; }
+    __device__ __forceinline__ int others() const {
+        return extras() && cluster >= reached() && n_long + (cluster - reached()) * extra < n_items ? n_long + (cluster - reached()) * extra : rest();
+    }
+    __device__ __forceinline__ int first() const { return cluster < n_long ? cluster : others(); }
+    __device__ __forceinline__ int next(int i) const {
+        if (i < n_long) return i + clusters < n_long ? i + clusters : others();
+        if (i >= n_long + extras()) return i + clusters;
+        return (i + 1 - n_long) % extra && i + 1 < n_items ? i + 1 : rest();
+    }
+};
 
 // What an epilogue warp works on.
 struct Epi {
@@ -129,9 +147,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();
     const int cluster_id = blockIdx.x >> 1, n_clusters = gridDim.x >> 1;
-    // Items are dealt out in rounds, all but the first in reverse: long items come first, and whoever got one of those comes last in a round
-    // that is not full.
-    auto next_item = [&](int i) { return i < n_clusters ? 2 * n_clusters - 1 - cluster_id : i + n_clusters; };
+    const Deal deal = {p.n_items, p.n_long, p.extra, cluster_id, n_clusters};
     const int stage_bytes = kOperandBytes + 64 * p.bn, n_stages = min(kMostStages, kStages * kStageBytes / stage_bytes);
 
     if (threadIdx.x == 0) {
@@ -169,7 +185,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
         uint64_t* const my_full = rank == 0 ? bars.full : bars.full_local;
         bool ok = true;
         int stage = 0, turn = 0;  // of the ring
-        for (int i = cluster_id; i < p.n_items && ok; i = next_item(i)) {
+        for (int i = deal.first(); i < p.n_items && ok; i = deal.next(i)) {
             const typename Job::Item item = Job::item(p, i);
             for (int kk = 0; kk < item.steps; ++kk) {
                 if (turn > 0) {
@@ -196,7 +212,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
         int stage = 0, turn = 0;
         if (rank == 0) {
             int tcount = 0;
-            for (int i = cluster_id; i < p.n_items && ok; i = next_item(i), ++tcount) {
+            for (int i = deal.first(); i < p.n_items && ok; i = deal.next(i), ++tcount) {
                 const typename Job::Item item = Job::item(p, i);
                 const bool a_mn = Job::a_mn(item);
                 const uint32_t idesc = kIdesc | ((uint32_t)(p.bn >> 3) << 17) | (a_mn ? kMnA : 0u) | (Job::b_mn ? kMnB : 0u);
@@ -238,7 +254,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
                 __syncwarp();
             }
         } else {
-            for (int i = cluster_id; i < p.n_items && ok; i = next_item(i)) {
+            for (int i = deal.first(); i < p.n_items && ok; i = deal.next(i)) {
                 const typename Job::Item item = Job::item(p, i);
                 for (int kk = 0; kk < item.steps; ++kk) {
                     ok = mbar_wait(&bars.full_local[stage], turn & 1);
@@ -257,7 +273,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
         const uint32_t my_lanes = (uint32_t)((warp & 3) * 32) << 16;  // the tensor-memory lanes this warp may read
         bool ok = true;
         int tcount = 0;
-        for (int i = cluster_id; i < p.n_items; i = next_item(i), ++tcount) {
+        for (int i = deal.first(); i < p.n_items; i = deal.next(i), ++tcount) {
             const typename Job::Item item = Job::item(p, i);
             Epi e;
             e.r0 = (int)rank * kRows + (warp & 3) * 32;

@@ -26,7 +26,7 @@ template <bool GRAD>
 struct GatedJob {
     struct Params {
         CUtensorMap a, w;          // bf16 [M][K]; [2][N][K]
-        int n_items, bn, tiles_m, tiles_n, band_rows, steps, splits, span;
+        int n_items, n_long, extra, bn, tiles_m, tiles_n, band_rows, steps, splits, span;
         float* partials;
         int* counters;
         int M, N, act;
@@ -254,7 +254,8 @@ int set_products(Params& p, int64_t M, int64_t N, int64_t K, const GatedSpace& s
     if (!fused::make_map(&p.a, ws + s.a, K, M, 1, s.pitch_k, M * s.pitch_k, kRows) ||
         !fused::make_map(&p.w, ws + s.w, K, N, 2, s.pitch_k, N * s.pitch_k, p.bn / 2))
         return BDR_ERR_CUDA;
-    p.n_items = p.tiles_m * p.tiles_n * p.splits;
+    p.n_items = p.n_long = p.tiles_m * p.tiles_n * p.splits;
+    p.extra = 0;
     p.band_rows = gemm_band_rows((M + 2 * N) * K * 2);
     p.M = (int)M;
     p.N = (int)N;

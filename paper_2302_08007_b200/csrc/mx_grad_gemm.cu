@@ -36,7 +36,7 @@ struct GradJob {
         CUtensorMap d_mn;  // D, boxes of 64 (rows of dW) x 64 (K)
         CUtensorMap w, a;  // boxes of 64 columns x 64 K
         Target da, dw;
-        int n_items, bn, items_da, items_da_split, items_dw_split, items_dw_seg;
+        int n_items, n_long, extra, bn, dw_first, items_da_split, items_dw_split, items_dw_seg;
         int tiles_m, tiles_n, tiles_k;
         int steps_n, steps_m;  // K steps over one segment's columns of D, over tokens
         int segs, parts;
@@ -56,12 +56,13 @@ struct GradJob {
     static __device__ __forceinline__ bool a_mn(const Item& it) { return it.seg >= 0; }
     static __device__ __forceinline__ Item item(const Params& p, int i) {
         Item it;
-        if (i < p.items_da) {
+        const bool first = i < p.n_long;  // the longer items come first
+        if (!first) i -= p.n_long;
+        if (first != (bool)p.dw_first) {
             it.split = i / p.items_da_split;
             it.seg = -1;
             gemm_tile_coords(i - it.split * p.items_da_split, p.tiles_m, p.tiles_k, 8, it.tm, it.tk);
         } else {
-            i -= p.items_da;
             it.split = i / p.items_dw_split;
             i -= it.split * p.items_dw_split;
             it.seg = i / p.items_dw_seg;
@@ -329,8 +330,12 @@ static int launch_grads(const GradProducts& g, cudaStream_t st) {
             sums += t.splits * rows * pitch;
         }
     }
-    p.items_da = p.items_da_split * p.da.splits;
-    p.n_items = p.items_da + p.items_dw_split * p.dw.splits;
+    const int n_da = p.items_da_split * p.da.splits, n_dw = p.items_dw_split * p.dw.splits;
+    p.n_items = n_da + n_dw;
+    p.dw_first = p.dw.span > p.da.span;
+    p.n_long = p.dw_first ? n_dw : n_da;
+    constexpr int kEpilogue = 16;  // of an item, in K steps: what a short one takes longest for
+    p.extra = (std::max(p.da.span, p.dw.span) + kEpilogue) / (std::min(p.da.span, p.dw.span) + kEpilogue);
     p.status = device_status_word();
     if (!p.status) return BDR_ERR_CUDA;
     if (p.n_items == 0) return BDR_OK;
