@@ -269,21 +269,60 @@ int decode_pair(const bdr_planes_t& a, int m_a, int64_t rows_a, __nv_bfloat16* o
     return cudaGetLastError() == cudaSuccess ? BDR_OK : BDR_ERR_CUDA;
 }
 
-// How the K steps of the two products are cut.  Few tiles with long sums (dA of few tokens, dW of a narrow layer) would keep few clusters
-// busy: their steps go to several clusters, whose fp32 sums another kernel adds in order.  That costs a launch (about 3 us) and a pass over the
-// sums, so a cut has to shorten the longest item by 24 steps (of 0.16 to 0.3 us) at least.
-constexpr int kPlanClusters = 74;
-static int grad_cut(int64_t tiles, int64_t steps, int64_t share) {
-    const int64_t most = std::min<int64_t>(32, 2 * kPlanClusters / tiles);
-    const int64_t n = std::min(most, (steps + share - 1) / share);
-    if (n < 2) return 1;
-    const int64_t span = (steps + n - 1) / n;
-    return steps - span < 24 ? 1 : (int)((steps + span - 1) / span);
+// How the tiles of the two products are shared out: the accumulator's columns, and into how many parts the K steps of each product's tiles are cut.
+// Few tiles with long sums (dA of few tokens, dW of a narrow layer) would keep few clusters busy: their steps go to several clusters, whose fp32
+// sums another kernel adds in order.  The shares are those that let the last cluster finish first, with what was measured (in 10 ns): a step
+// 34 with 256 columns and 20 with 128; an item's epilogue 270, 32-bit results 540, with 256 columns and half of that with 128; the joining kernel 350.
+// (Always as for both products: a gradient does not depend on whether the other is wanted.)
+constexpr int kPlanClusters = 74, kMostCuts = 32;
+struct GradPlan {
+    int bn = 256, tiles_k = 0, da = 0, dw = 0;       // tiles of each product
+    int cut_da = 1, cut_dw = 1, span_da = 0, span_dw = 0;
+    bool dw_first = false;
+    int n_da() const { return da * cut_da; }
+    int n_dw() const { return dw * cut_dw; }
+    int extra = 0;                                   // see fused::Deal
+};
+static int64_t makespan(int n1, int64_t t1, int n2, int64_t t2, int64_t extra) {  // of n1 long items and n2 others, dealt out as Deal does
+    const int C = std::min(kPlanClusters, n1 + n2), q = n1 / C, r = n1 % C;
+    const int given = r ? (int)std::min<int64_t>(n2, (C - r) * extra) : 0, rest = n2 - given, full = rest / C, part = rest % C;
+    const int64_t reached = r ? (q + 1) * t1 + (full + (part > C - r)) * t2 : 0;
+    return std::max(reached, q * t1 + ((given > 0 ? std::min<int64_t>(extra, given) : 0) + full + (part > 0)) * t2);
+}
+static GradPlan plan_grads(int64_t M, int64_t N, int64_t K, int segs, int parts, bool f32) {
+    GradPlan best;
+    int64_t least = -1;
+    const int64_t tiles_m = (M + 255) / 256, tiles_n = segs * ((N + 255) / 256);
+    const int64_t steps_da = (N + kBK - 1) / kBK * segs * parts, steps_dw = (M + kBK - 1) / kBK * parts;
+    static const int kCuts[] = {1, 2, 3, 4, 6, 10, 16, kMostCuts};  // (of sums of 24 steps at least)
+    for (int bn = 256; bn >= 128; bn /= 2) {
+        const int64_t tiles_k = (K + bn - 1) / bn, da = tiles_m * tiles_k, dw = tiles_n * tiles_k;
+        const int64_t step = bn == 256 ? 34 : 20, epilogue = (f32 ? 540 : 270) * bn / 256;
+        for (int i : kCuts) {
+            if (i > 1 && (da * i > kPlanClusters || steps_da < 24)) break;
+            const int64_t span_da = (steps_da + i - 1) / i, n_da = da * ((steps_da + span_da - 1) / span_da);
+            for (int j : kCuts) {
+                if (j > 1 && (dw * j > kPlanClusters || steps_dw < 24)) break;
+                const int64_t span_dw = (steps_dw + j - 1) / j, n_dw = dw * ((steps_dw + span_dw - 1) / span_dw);
+                const int64_t t_da = span_da * step + epilogue, t_dw = span_dw * step + epilogue;
+                const bool dw_first = t_dw > t_da;
+                const int64_t extra = std::max(t_da, t_dw) / std::min(t_da, t_dw);
+                const int64_t t = (dw_first ? makespan(n_dw, t_dw, n_da, t_da, extra) : makespan(n_da, t_da, n_dw, t_dw, extra)) + (i > 1 || j > 1 ? 350 : 0);
+                if (least >= 0 && t * 100 >= least * 98) continue;
+                least = t;
+                best.bn = bn; best.tiles_k = (int)tiles_k; best.da = (int)da; best.dw = (int)dw;
+                best.cut_da = (int)(n_da / da); best.cut_dw = (int)(n_dw / dw);
+                best.span_da = (int)span_da; best.span_dw = (int)span_dw;
+                best.dw_first = dw_first; best.extra = (int)extra;
+            }
+        }
+    }
+    return best;
 }
 // Bytes of the fp32 sums that launch_grad_products may need for M tokens and any number of outputs up to N: at most 2 x 74 tiles of each product.
 int64_t grad_sums_bytes(int64_t M, int64_t N, int64_t K, int segs) {
     const int64_t most = 2 * kPlanClusters * 256 / ((K + 255) / 256) + 1;  // (tiles of 128 columns are more, and have as many rows)
-    return round_up((std::min(most, 32 * M) + std::min(most, 32 * segs * N)) * line_pitch(K) * 4, 256);
+    return round_up((std::min(most, kMostCuts * M) + std::min(most, kMostCuts * segs * N)) * line_pitch(K) * 4, 256);
 }
 
 template <bool F32>
@@ -295,47 +334,44 @@ static int launch_grads(const GradProducts& g, cudaStream_t st) {
         !fused::make_map(&p.w, g.w, g.K, g.N, g.segs, g.pitch_k, g.N * g.pitch_k, kBK) ||
         !fused::make_map(&p.a, g.a, g.K, g.M, 1, g.pitch_k, g.M * g.pitch_k, kBK))
         return BDR_ERR_CUDA;
+    GradPlan plan = plan_grads(g.M, g.N, g.K, g.segs, g.parts, F32);
+    if (!g.da) { plan.da = 0; plan.cut_da = 1; }
+    if (!g.dw) { plan.dw = 0; plan.cut_dw = 1; }
     p.tiles_m = (int)((g.M + 255) / 256);
     p.tiles_n = (int)((g.N + 255) / 256);
-    // A step of 128 columns takes almost as long as one of 256: the narrow accumulator is for tiles that all find a cluster at once.
-    p.bn = ((g.da ? p.tiles_m : 0) + (g.dw ? g.segs * p.tiles_n : 0)) * ((g.K + 127) / 128) <= kPlanClusters ? 128 : 256;
-    p.tiles_k = (int)((g.K + p.bn - 1) / p.bn);
+    p.tiles_k = plan.tiles_k;
+    p.bn = plan.bn;
     p.steps_n = (int)((g.N + kBK - 1) / kBK);
     p.steps_m = (int)((g.M + kBK - 1) / kBK);
     p.segs = g.segs; p.parts = g.parts; p.scale = g.scale;
     p.cols = (int)g.K;
-    p.items_da_split = g.da ? p.tiles_m * p.tiles_k : 0;
+    p.items_da_split = plan.da;
     p.items_dw_seg = p.tiles_n * p.tiles_k;
-    p.items_dw_split = g.dw ? g.segs * p.items_dw_seg : 0;
+    p.items_dw_split = plan.dw;
     p.da.rows = (int)g.M;
     p.dw.rows = (int)g.N;
     p.da.steps = p.steps_n * g.segs * g.parts;
     p.dw.steps = p.steps_m * g.parts;
-    const int64_t work = (int64_t)p.items_da_split * p.da.steps + (int64_t)p.items_dw_split * p.dw.steps;
-    const int64_t share = std::max<int64_t>(16, (work + kPlanClusters - 1) / kPlanClusters);
     float* sums = g.sums;
     const int64_t pitch = line_pitch(g.K);
     for (int i = 0; i < 2; ++i) {
         Target& t = i ? p.dw : p.da;
-        const int tiles = i ? p.items_dw_split : p.items_da_split;
         const int64_t rows = i ? g.segs * g.N : g.M;
         t.out = i ? fused::make_rows(g.dw, g.ld_dw, F32) : (g.last ? fused::make_rows(g.da, g.ld_da, F32) : fused::make_rows(g.acc, g.ld_acc, true));
         t.scaled = i || g.last;
         t.read = i || g.first ? nullptr : g.acc;
         t.ld_read = g.ld_acc * 4;
-        t.splits = tiles ? grad_cut(tiles, t.steps, share) : 1;
-        t.span = (t.steps + t.splits - 1) / t.splits;
+        t.splits = i ? plan.cut_dw : plan.cut_da;
+        t.span = i ? plan.span_dw : plan.span_da;
         if (t.splits > 1) {
             t.sums = fused::make_rows(sums, pitch, true);
             sums += t.splits * rows * pitch;
         }
     }
-    const int n_da = p.items_da_split * p.da.splits, n_dw = p.items_dw_split * p.dw.splits;
-    p.n_items = n_da + n_dw;
-    p.dw_first = p.dw.span > p.da.span;
-    p.n_long = p.dw_first ? n_dw : n_da;
-    constexpr int kEpilogue = 16;  // of an item, in K steps: what a short one takes longest for
-    p.extra = (std::max(p.da.span, p.dw.span) + kEpilogue) / (std::min(p.da.span, p.dw.span) + kEpilogue);
+    p.n_items = plan.n_da() + plan.n_dw();
+    p.dw_first = plan.dw_first;
+    p.n_long = plan.dw_first ? plan.n_dw() : plan.n_da();
+    p.extra = plan.extra;
     p.status = device_status_word();
     if (!p.status) return BDR_ERR_CUDA;
     if (p.n_items == 0) return BDR_OK;
