@@ -403,7 +403,8 @@ int mx_attn_decode(const mx_kv_cache_t* cache /*host*/, const void* q, int64_t l
  * Products of packed operands with what follows them fused to them.  Operands are axis-1 planes in the Table II formats (k1 = 16,
  * k2 = 2, d2 = 1, m in {2, 4, 7}; either tie rule; the two formats of a call may differ), any sizes with K >= 1; pitches and plane
  * addresses are multiples of 16 bytes.  Products are those of the decoded values (in bf16, so blocks whose unit is below 2^-133 lose
- * low bits, as in mx_gemm_ws) with fp32 accumulation; blocks with the exponent byte 0xFF decode to NaN.  Results do not change from run to run.
+ * low bits, as in mx_gemm_ws; a few rows take mx_gemv's kernel, with its limits) with fp32 accumulation; blocks with the exponent byte 0xFF
+ * decode to NaN.  Results do not change from run to run.  The tensors of a call do not overlap.
  * A workspace is device scratch, 256-byte aligned, contents overwritten, of the size that the call's _workspace_bytes gives (0 for
  * sizes that the call refuses).  Bounded waits that run out leave BDR_ERR_TIMEOUT in the sticky word of bdr_device_status. */
 

@@ -103,7 +103,8 @@ class Planes:
         sizes = (e.numel, m.numel, x.numel)
         lines = min(t.shape[0] for t in (e, m, x) if t.numel()) if e.numel() else 0
         on_gpu = e.is_cuda and x.is_cuda and (m.is_cuda or not m.numel())
-        self.__dict__.update(_on_gpu=on_gpu, _view=view, _known=tuple(f() for f in probe), _probe=probe, _sizes=sizes, _counts=tuple(f() for f in sizes), _lines=lines)
+        devices = {t.get_device() for t in (e, m, x) if t.numel()}
+        self.__dict__.update(_on_gpu=on_gpu, _device=devices.pop() if on_gpu and len(devices) == 1 else -1, _address=C.addressof(view), _view=view, _known=tuple(f() for f in probe), _probe=probe, _sizes=sizes, _counts=tuple(f() for f in sizes), _lines=lines)
 
     def lines(self) -> int:
         """Lines that every plane holds."""
@@ -603,12 +604,18 @@ def _vector(t: torch.Tensor, n: int, dtype, what: str, here: int) -> int:
 
 
 def _operand(p: Planes, lines: int, what: str, here: int) -> int:
-    """Address of the C view of planes of at least `lines` lines on the current GPU."""
-    if p.lines() < lines:
+    """Address of the C view of planes of at least `lines` lines on the current GPU (Planes.lines and Planes.c in one)."""
+    q = p._probe
+    if q is None or (q[0](), q[1](), q[2](), q[3](), q[4](), q[5]()) != p._known:
+        p._describe()
+    n = p._sizes
+    if (n[0](), n[1](), n[2]()) != p._counts:
+        p._describe()
+    if p._lines < lines:
         raise ValueError("%s: the planes hold fewer than %d lines" % (what, lines))
-    if not p._on_gpu or p.exps.get_device() != here:
+    if p._device != here and lines:
         raise ValueError("%s: expected CUDA tensors of the current device" % what)
-    return C.addressof(p._view)
+    return p._address
 
 
 def _scratch(t: torch.Tensor, here: int) -> int:

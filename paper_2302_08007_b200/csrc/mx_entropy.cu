@@ -25,6 +25,12 @@ __device__ __forceinline__ float exp2_of(float x) {
     return y;
 }
 
+// Two parts of a row, each a maximum and the sum of the exponentials of what is above it.
+__device__ __forceinline__ float2 join(float2 a, float2 b) {
+    const float m = fmaxf(a.x, b.x), ref = m == -INFINITY ? 0.f : m;
+    return make_float2(m, a.y * exp2_of((a.x - ref) * kLog2e) + b.y * exp2_of((b.x - ref) * kLog2e));
+}
+
 // GRAD: the epilogue writes d instead of a row's maxima and sums
 template <bool GRAD>
 struct EntropyJob {
@@ -207,10 +213,6 @@ __global__ void __launch_bounds__(1024) entropy_join_kernel(const float2* parts,
     __shared__ float2 shared[32][33];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t row = (int64_t)blockIdx.x * 32 + lane;
-    auto join = [](float2 a, float2 b) {
-        const float m = fmaxf(a.x, b.x), ref = m == -INFINITY ? 0.f : m;
-        return make_float2(m, a.y * exp2_of((a.x - ref) * kLog2e) + b.y * exp2_of((b.x - ref) * kLog2e));
-    };
     float2 mine = make_float2(-INFINITY, 0.f);
     if (row < M)
         for (int i = warp; i < n_parts; i += 32) mine = join(mine, parts[(int64_t)i * M + row]);
@@ -223,29 +225,6 @@ __global__ void __launch_bounds__(1024) entropy_join_kernel(const float2* parts,
         const int64_t t = targets[row];
         if (t >= V) atomicCAS(status, 0, (int)BDR_ERR_SIZE);
         loss[row] = t < 0 ? 0.f : (t < V ? l - hit[row] : __int_as_float(0x7FC00000));
-    }
-}
-
-// The largest |dloss| of the rows that count, by which d is divided before it is rounded to bf16 and the gradients are multiplied in
-// fp32: with the equal weights of a mean the term of the target, which outweighs all others of its row, is then near -1 and rounds to less
-// than the step of 1 (as 1/3891, say, it loses up to 2^-8: gradients of 4096 x 32000 x 4096 were off by 2.6e-3, now 1.7e-3, their own rounding).  One block.
-__global__ void __launch_bounds__(1024) entropy_scale_kernel(const float* dloss, const int64_t* targets, int64_t M, int64_t V, float* largest) {
-    __shared__ float shared[32];
-    float m = 0.f;
-    for (int64_t i = threadIdx.x; i < M; i += 1024)
-        if (targets[i] >= 0 && targets[i] < V) m = fmaxf(m, fabsf(dloss[i]));
-    for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
-    if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = m;
-    __syncthreads();
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    // It runs beside the decoding in front of it, on which it does not depend, and does not finish before it: whoever waits for this kernel has
-    // the decoded operands too.
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (threadIdx.x < 32) {
-        m = shared[threadIdx.x];
-        for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
-        // (0, or infinite: nothing to divide by; a quotient of subnormals would overflow its inverse, but is itself in [-1, 1])
-        if (threadIdx.x == 0) *largest = m > 0.f && m < INFINITY ? m : 1.f;
     }
 }
 
@@ -472,14 +451,17 @@ int mx_cross_entropy_bwd(const bdr_config_t* cfg_a, const bdr_planes_t* a, const
     g.ld_acc = s.pitch_k;
     g.sums = reinterpret_cast<float*>(ws + s.sums);
     g.scale = p.largest = reinterpret_cast<const float*>(ws + s.largest);
+    // With the equal weights of a mean the term of the target, which outweighs all others of its row, is then near -1 and rounds to less than the step of 1
+    // (as 1/3891, say, it loses up to 2^-8: gradients of 4096 x 32000 x 4096 were off by 2.6e-3, now 1.9e-3, of which 1.6e-3 are their own rounding).
+    const Largest largest = {dloss, targets, M, V, reinterpret_cast<float*>(ws + s.largest)};
     __nv_bfloat16 *const wa = reinterpret_cast<__nv_bfloat16*>(ws + s.a), *const ww = reinterpret_cast<__nv_bfloat16*>(ws + s.w);
     const bool f8 = fused::takes_f8(cfg_a->m, cfg_w->m, M, V, V, K);
     for (int64_t v = 0; v < V; v += s.piece) {
         const int64_t cols = std::min(s.piece, V - v);
         const bdr_planes_t lines = lines_from(*w, v);
         const int64_t part = f8 ? cols : part_columns(M, cols, K);
-        if ((rc = decode_pair(*a, cfg_a->m, v == 0 ? M : 0, wa, lines, cfg_w->m, part, ww, K, s.pitch_k, st, nullptr, p.counters, s.n_counters))) return rc;
-        if (v == 0 && (rc = launch_dependent(entropy_scale_kernel, dim3(1), dim3(1024), st, dloss, targets, M, V, reinterpret_cast<float*>(ws + s.largest))))
+        if ((rc = decode_pair(*a, cfg_a->m, v == 0 ? M : 0, wa, lines, cfg_w->m, part, ww, K, s.pitch_k, st, nullptr, p.counters, s.n_counters, false,
+                              v == 0 ? &largest : nullptr)))
             return rc;
         if ((rc = set_piece(p, M, K, v, cols, s.pitch_k, ws + s.a, ws + s.w, f8))) return rc;
         if (f8) {

@@ -17,12 +17,20 @@ constexpr int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * t
 // Pitch (elements) of lines of K decoded elements: whole items of the decode kernel.
 constexpr int64_t line_pitch(int64_t K) { return round_up(K, 32); }
 
+// The largest |dloss| of the rows that count (0 <= target < V), by which a gradient is divided before it is rounded to bf16 and the results are
+// multiplied in fp32; 1 where there is none, or an infinity.
+struct Largest {
+    const float* dloss;
+    const int64_t* targets;
+    int64_t M, V;
+    float* out;
+};
 // Packed lines of K elements (Table II formats, m magnitude bits) of two operands -> bf16 [rows, pitch]; what lies behind K in a row is
 // unspecified.  gate: NULL, or device flag without which nothing is decoded.  n_zero words at `zero` are cleared on the side.
 // beside: the kernel in front in the stream is a product that does not read the output: it is decoded on what that product leaves free of the
-// SMs, and is complete when both are.
+// SMs, and is complete when both are.  largest: NULL, or what a block of its own computes on the side.
 int decode_pair(const bdr_planes_t& a, int m_a, int64_t rows_a, __nv_bfloat16* out_a, const bdr_planes_t& w, int m_w, int64_t rows_w, __nv_bfloat16* out_w,
-                int64_t K, int64_t pitch, cudaStream_t st, const int* gate = nullptr, int* zero = nullptr, int64_t n_zero = 0, bool beside = false);
+                int64_t K, int64_t pitch, cudaStream_t st, const int* gate = nullptr, int* zero = nullptr, int64_t n_zero = 0, bool beside = false, const Largest* largest = nullptr);
 
 // Launches a kernel without shared memory behind another in the stream so that it is set up while that one drains; the kernel waits for it
 // (griddepcontrol.wait) before it touches memory.

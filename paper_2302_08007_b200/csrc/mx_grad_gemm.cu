@@ -223,16 +223,36 @@ struct Lines {
     int64_t n_items;
     int m;
 };
+__device__ __forceinline__ void largest_of(const Largest& l) {  // a block of 256
+    __shared__ float shared[8];
+    float m = 0.f;
+    for (int64_t i = threadIdx.x; i < l.M; i += 256) {
+        const int64_t t = l.targets[i];
+        if (t >= 0 && t < l.V) m = fmaxf(m, fabsf(l.dloss[i]));
+    }
+    for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+    if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = m;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < 8; ++i) m = fmaxf(m, shared[i]);
+        *l.out = m > 0.f && m < INFINITY ? m : 1.f;
+    }
+}
 // Both operands in one launch: blocks 0 .. first_blocks - 1 take the first.
 __global__ void __launch_bounds__(256) decode_pair_kernel(Lines first, Lines second, unsigned first_blocks, int64_t pitch, uint32_t items_per_row, int nb,
-                                                           const int* gate, int* zero, int n_zero, int beside) {
+                                                           const int* gate, int* zero, int n_zero, int beside, Largest largest) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the product's set-up may begin
     if (gate && *gate == 0) return;
     if (blockIdx.x == 0)
         for (int i = threadIdx.x; i < n_zero; i += 256) zero[i] = 0;
+    const unsigned blocks = gridDim.x - (largest.out ? 1u : 0u);
+    if (blockIdx.x == blocks) {
+        largest_of(largest);
+        return;
+    }
     const bool one = blockIdx.x < first_blocks;
     const Lines& l = one ? first : second;
-    const int64_t at = (int64_t)(one ? blockIdx.x : blockIdx.x - first_blocks) * 256 + threadIdx.x, stride = (int64_t)(one ? first_blocks : gridDim.x - first_blocks) * 256;
+    const int64_t at = (int64_t)(one ? blockIdx.x : blockIdx.x - first_blocks) * 256 + threadIdx.x, stride = (int64_t)(one ? first_blocks : blocks - first_blocks) * 256;
     switch (l.m) {
         case 2: decode_items<3>(l.in, l.out, pitch, l.n_items, items_per_row, nb, at, stride); break;
         case 4: decode_items<5>(l.in, l.out, pitch, l.n_items, items_per_row, nb, at, stride); break;
@@ -244,7 +264,8 @@ __global__ void __launch_bounds__(256) decode_pair_kernel(Lines first, Lines sec
 }  // namespace
 
 int decode_pair(const bdr_planes_t& a, int m_a, int64_t rows_a, __nv_bfloat16* out_a, const bdr_planes_t& w, int m_w, int64_t rows_w, __nv_bfloat16* out_w,
-                int64_t K, int64_t pitch, cudaStream_t st, const int* gate, int* zero, int64_t n_zero, bool beside) {
+                int64_t K, int64_t pitch, cudaStream_t st, const int* gate, int* zero, int64_t n_zero, bool beside,
+                const Largest* largest) {
     Lines l[2] = {{a, out_a, rows_a, m_a}, {w, out_w, rows_w, m_w}};
     const int64_t per_row = (K + 31) / 32;
     for (Lines& x : l) {
@@ -257,15 +278,17 @@ int decode_pair(const bdr_planes_t& a, int m_a, int64_t rows_a, __nv_bfloat16* o
         }
         x.n_items *= per_row;
     }
-    if (l[0].n_items + l[1].n_items == 0) return n_zero == 0 || cudaMemsetAsync(zero, 0, n_zero * 4, st) == cudaSuccess ? BDR_OK : BDR_ERR_CUDA;
+    if (l[0].n_items + l[1].n_items == 0 && !largest) return n_zero == 0 || cudaMemsetAsync(zero, 0, n_zero * 4, st) == cudaSuccess ? BDR_OK : BDR_ERR_CUDA;
     // Behind a gate there rarely is anything to do.  Beside a product one block fits on an SM, and stays until it ends: all of the work is theirs.
     const int64_t most = (int64_t)sm_count() * (beside ? 1 : (gate ? 4 : 32));
     unsigned blocks[2];
     for (int i = 0; i < 2; ++i) blocks[i] = (unsigned)std::min<int64_t>((l[i].n_items + 255) / 256, i == 1 && beside ? most - blocks[0] : most);
-    const dim3 grid(blocks[0] + blocks[1]);
+    const dim3 grid(blocks[0] + blocks[1] + (largest ? 1 : 0));
+    const Largest none = {};
     if (beside)
-        return launch_dependent(decode_pair_kernel, grid, dim3(256), st, l[0], l[1], blocks[0], pitch, (uint32_t)per_row, (int)((K + 15) / 16), gate, zero, (int)n_zero, 1);
-    decode_pair_kernel<<<grid, 256, 0, st>>>(l[0], l[1], blocks[0], pitch, (uint32_t)per_row, (int)((K + 15) / 16), gate, zero, (int)n_zero, 0);
+        return launch_dependent(decode_pair_kernel, grid, dim3(256), st, l[0], l[1], blocks[0], pitch, (uint32_t)per_row, (int)((K + 15) / 16), gate, zero, (int)n_zero, 1, none);
+    decode_pair_kernel<<<grid, 256, 0, st>>>(l[0], l[1], blocks[0], pitch, (uint32_t)per_row, (int)((K + 15) / 16), gate, zero, (int)n_zero, 0,
+                                           largest ? *largest : none);
     return cudaGetLastError() == cudaSuccess ? BDR_OK : BDR_ERR_CUDA;
 }
 

@@ -130,6 +130,38 @@ def test_pieces_of_the_vocabulary(dtype):
     f.check(dw, want_w, ew, "dw")
 
 
+@pytest.mark.parametrize("m,v,k", [(33, 1024, 100), (700, 1025, 64), (300, 2048, 300), (2000, 4096, 200), (5000, 4097, 130), (64, 33, 4000), (9500, 4000, 9000)])
+def test_parts_of_a_row(m, v, k):
+    # few and many parts to join; in the last case they come from several launches
+    (pa, a), (pw, w), targets, _ = operands(m, v, k, "mx6", "mx9", 14, 1.0)
+    targets[-1], targets[1] = v - 1, -100
+    runs = [run(pa, pw, "mx6", "mx9", m, v, k, targets) for _ in range(3)]
+    want, want_lse, _, eloss, else_, _ = f.entropy(a, w, targets)
+    f.check(runs[0][1], want_lse, else_, "lse")
+    f.check(runs[0][0], want, eloss, "loss")
+    assert all(torch.equal(x, y) for r in runs[1:] for x, y in zip(r, runs[0]))
+
+
+@pytest.mark.parametrize("m,fmt", [(60, "mx9"), (256, "mx4")])
+def test_pieces_of_a_large_vocabulary(m, fmt):
+    # decoded weights of more than half a GB: two pieces, in the second case on the 8-bit path
+    v, k = 140032, 2048
+    gen = torch.Generator(device="cuda").manual_seed(13)
+    (pa, a), (pw, w) = (f.packed(f.CFG[fmt], torch.randn(r, k, device="cuda", generator=gen) * s) for r, s in ((m, 1.0), (v, k ** -0.5)))
+    targets = torch.randint(0, v, (m,), device="cuda", generator=gen)
+    targets[:5] = torch.tensor([v - 1, 70143, 70144, 0, -1], device="cuda")
+    loss, lse = run(pa, pw, fmt, fmt, m, v, k, targets)
+    want, want_lse, _, eloss, else_, _ = f.entropy(a, w, targets)
+    f.check(lse, want_lse, else_, "lse")
+    f.check(loss, want, eloss, "loss")
+    dloss = torch.rand(m, device="cuda", generator=gen)
+    da, dw = run_grads(pa, pw, fmt, fmt, m, v, k, targets, lse, dloss, torch.bfloat16)
+    want_a, want_w, ea, ew = f.entropy_grads(a, w, targets, lse.double(), dloss.double(), torch.bfloat16)
+    f.check(da, want_a, ea, "da")
+    f.check(dw, want_w, ew, "dw")
+    assert bdr.bdr_device_status() == 0
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_parts_of_a_piece(dtype):
     # large enough that the next columns are decoded while the ones before are multiplied; the last part is ragged
