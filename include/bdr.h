@@ -401,7 +401,7 @@ int mx_attn_decode(const mx_kv_cache_t* cache /*host*/, const void* q, int64_t l
 
 /* ---- Feed-forward layer and vocabulary head of a language model ------------------------------------------------
  * Products of packed operands with what follows them fused to them.  Operands are axis-1 planes in the Table II formats (k1 = 16,
- * k2 = 2, d2 = 1, m in {2, 4, 7}; either tie rule; the two formats of a call may differ), any sizes with K >= 1; pitches and plane
+ * k2 = 2, d2 = 1, m in {2, 4, 7}; either tie rule; the two formats of a call may differ), any sizes up to 2^28 with K >= 1; pitches and plane
  * addresses are multiples of 16 bytes.  Products are those of the decoded values (in bf16, so blocks whose unit is below 2^-133 lose
  * low bits, as in mx_gemm_ws; a few rows take mx_gemv's kernel, with its limits) with fp32 accumulation; blocks with the exponent byte 0xFF
  * decode to NaN.  Results do not change from run to run.  The tensors of a call do not overlap.

@@ -284,7 +284,7 @@ struct EntropyGradSpace {
     }
 };
 
-constexpr int64_t kMost = 1ll << 30;
+constexpr int64_t kMost = 1ll << 28;  // of every size: no product of two sizes and a few bytes leaves 64 bits
 
 template <class Params>
 int set_piece(Params& p, int64_t M, int64_t K, int64_t col0, int64_t cols, int64_t pitch_k, const uint8_t* a, const uint8_t* w, bool f8) {

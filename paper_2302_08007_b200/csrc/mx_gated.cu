@@ -232,7 +232,7 @@ struct GatedSpace {
     }
 };
 
-constexpr int64_t kMostRows = 1ll << 30;
+constexpr int64_t kMost = 1ll << 28;  // of every size: no product of two sizes and a few bytes leaves 64 bits
 
 int check_rows(const void* p, int64_t ld, int64_t cols, int width) {
     if (!p) return BDR_ERR_NULL;
@@ -271,7 +271,7 @@ using namespace bdr;
 extern "C" {
 
 int64_t mx_gated_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K) {
-    if (M < 0 || N < 0 || K < 0 || M > kMostRows || N > kMostRows || K > kMostRows) return 0;
+    if (M < 0 || N < 0 || K < 0 || M > kMost || N > kMost || K > kMost) return 0;
     return GatedSpace(M, N, K, 0).bytes;
 }
 
@@ -280,7 +280,7 @@ int mx_gated_gemm(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bdr_co
                   int64_t workspace_bytes, void* stream) {
     if (dt != BDR_F32 && dt != BDR_BF16) return BDR_ERR_UNSUPPORTED;
     if (!act::known(act)) return BDR_ERR_UNSUPPORTED;
-    if (M < 0 || N < 0 || K < 0 || M > kMostRows || N > kMostRows / 2 || K > kMostRows) return BDR_ERR_SIZE;
+    if (M < 0 || N < 0 || K < 0 || M > kMost || N > kMost || K > kMost) return BDR_ERR_SIZE;
     if (K == 0 || ((M + 255) / 256) * ((N + kRows - 1) / kRows) >= (1ll << 30)) return BDR_ERR_UNSUPPORTED;
     int rc = check_table2_config(cfg_a);
     if (!rc) rc = check_table2_config(cfg_w);
@@ -317,7 +317,7 @@ int mx_gated_gemm(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bdr_co
 }
 
 int64_t mx_gated_gemm_bwd_workspace_bytes(int64_t M, int64_t N, int64_t K, bdr_dtype_t dt) {
-    if (M < 0 || N < 0 || K < 0 || M > kMostRows || N > kMostRows || K > kMostRows) return 0;
+    if (M < 0 || N < 0 || K < 0 || M > kMost || N > kMost || K > kMost) return 0;
     return GatedSpace(M, N, K, dt == BDR_F32 ? fused::kPartsF32 : 1).bytes;
 }
 
@@ -326,7 +326,7 @@ int mx_gated_gemm_bwd(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bd
                       int64_t ld_da, void* dw, int64_t ld_dw, void* workspace, int64_t workspace_bytes, void* stream) {
     if (dt != BDR_F32 && dt != BDR_BF16) return BDR_ERR_UNSUPPORTED;
     if (!act::known(act)) return BDR_ERR_UNSUPPORTED;
-    if (M < 0 || N < 0 || K < 0 || M > kMostRows || N > kMostRows / 2 || K > kMostRows) return BDR_ERR_SIZE;
+    if (M < 0 || N < 0 || K < 0 || M > kMost || N > kMost || K > kMost) return BDR_ERR_SIZE;
     const int64_t tiles_k = (K + 255) / 256;
     if (K == 0 || ((M + 255) / 256) * std::max(tiles_k, (N + kRows - 1) / kRows) >= (1ll << 29) || ((N + 255) / 256) * tiles_k >= (1ll << 29) ||
         (N + kBK - 1) / kBK * 4 >= (1ll << 30))

@@ -67,6 +67,11 @@ def test_sizes_of_the_workspaces_are_demanded():
         assert L.mx_gated_gemm_workspace_bytes(*bad) == 0 and L.mx_gated_gemm_bwd_workspace_bytes(*bad, 1) == 0
         assert L.mx_cross_entropy_workspace_bytes(*bad) == 0 and L.mx_cross_entropy_bwd_workspace_bytes(*bad, 1) == 0
     assert L.mx_cross_entropy_workspace_bytes(M, 0, K) == 0
+    most = 1 << 28                                               # the largest sizes: nothing overflows
+    for size in (L.mx_gated_gemm_workspace_bytes(most, most, most), L.mx_gated_gemm_bwd_workspace_bytes(most, most, most, 0),
+                 L.mx_cross_entropy_workspace_bytes(most, most, most), L.mx_cross_entropy_bwd_workspace_bytes(most, most, most, 0)):
+        assert size > most * most * 2
+    assert L.mx_gated_gemm_workspace_bytes(most + 1, 1, 1) == 0 and L.mx_cross_entropy_workspace_bytes(1, most + 1, 1) == 0
 
 
 def test_tensors_are_checked():
