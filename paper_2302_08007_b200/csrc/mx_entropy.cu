@@ -43,6 +43,7 @@ struct EntropyJob {
         int64_t col0;             // the piece's first column
         const int64_t* targets;
         float2* parts;            // [columns / (bn / 2)][M]: maximum, sum of exp(l - maximum)
+        int part0;                // the piece's first
         float* hit;               // [M]: the target's logit
         const float *lse, *dloss;
         const float* largest;     // of |dloss|, among the rows that count
@@ -147,7 +148,7 @@ struct EntropyJob {
     }
     static __device__ __forceinline__ void end(const Params& p, const Row& r) {
         if constexpr (!GRAD)
-            if (r.live && r.first < p.cols) p.parts[(p.col0 + r.first) / r.width * p.M + r.row] = make_float2(r.top, r.sum);
+            if (r.live && r.first < p.cols) p.parts[(int64_t)(p.part0 + r.first / r.width) * p.M + r.row] = make_float2(r.top, r.sum);
     }
     static __device__ __forceinline__ void epilogue(const Params& p, const Item& it, const fused::Epi& e) {
         Row r = begin(p, it, e);
@@ -389,9 +390,10 @@ int mx_cross_entropy(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bdr
                 return rc;
             if (part < cols && (rc = set_piece(p, M, K, v + c, n, s.pitch_k, ws + s.a, ws + s.w + c * s.pitch_k * 2, f8))) return rc;
             if ((rc = fused::launch<EntropyJob<false>>(p, st))) return rc;
+            p.part0 += (int)((n + p.bn / 2 - 1) / (p.bn / 2));
         }
     }
-    const int n_parts = (int)((V + p.bn / 2 - 1) / (p.bn / 2));
+    const int n_parts = p.part0;
     return launch_dependent(entropy_join_kernel, dim3((unsigned)((M + 31) / 32)), dim3(1024), st, (const float2*)p.parts, n_parts, M, (const float*)p.hit, targets,
                             V, loss, lse, p.status);
 }

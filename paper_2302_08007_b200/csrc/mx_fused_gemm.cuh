@@ -1,4 +1,4 @@
-// The product kernel behind the fused operators: a persistent, TMA-fed tcgen05 kernel over 256 x (64, 128 or 256) accumulators, one
+// The product kernel behind the fused operators: a persistent, TMA-fed tcgen05 kernel over 256 x (64, 128, 192 or 256) accumulators, one
 // cluster of two CTAs per SM pair, whose operands and epilogue come from a Job.  The pipeline is that of the dense phase of mx_gemm_ws:
 //   warp 0   : one lane issues the TMA loads of this CTA's 128 rows of A and its half of B's columns (64 K elements) into a ring
 //   warp 1   : leader CTA: one lane issues tcgen05.mma.cta_group::2 (M 256, N the accumulator's columns, K 16) into one of two accumulator
@@ -555,11 +555,12 @@ __device__ __forceinline__ void store_parts(const Epi& e, const Rows& d, int64_t
 }
 
 // How a product of tiles_m x cols is shared out: the accumulator's columns (cols_div of them for each of the product's) and the items that a
-// tile's K steps are cut into.  Measured, a step takes about 640, 360 and 310 clocks at 256, 128 and 64 columns (the last two are bound by
-// barriers and issue rather than by the tensor core), an item's start and epilogue 1500 at 256: narrower tiles pay where they save a round or
-// fill idle clusters (300 x 2000 x 1024: 11.5, 9.1 and 11.5 us; 1003 x 2747 x 1500: 22.8, 21.1, 28.9).  A cut pays where few tiles have long sums: it costs
-// the way through memory and back, and the last warp's reading of all parts (64 columns, 300 x 300 x 8192 26.1 us, in three 17.2; 256 x 256 x 3584
-// 13.7, 11.8; 256 x 256 x 1280 8.0, 10.1).
+// tile's K steps are cut into.  Measured, a step takes about 650, 527, 370 and 340 clocks at 256, 192, 128 and 64 columns when all clusters are at it (the SMs'
+// intake of 50 bytes a clock; 300 with 64 or 128 columns and few clusters: barriers and issue), an item's start and epilogue 1500 at 256: narrower tiles pay
+// where they save a round or fill idle clusters (256, 192, 128, 64 columns: 256 x 7000 x 1024 13.1, 12.0, 13.2, 16.4 us; 1003 x 2747 x 1500 24.2, 21.2, 22.2,
+// 30.7; 600 x 1500 x 3000 22.7, 19.0, 16.1, 23.7; 2048 x 2304 x 1024 18.7, 19.2, 20.6, 32.3).  A cut pays where few tiles have long sums: it costs the way through
+// memory and back, and the last warp's reading of all parts (64 columns, 300 x 300 x 8192 26.1 us, in three 17.2; 256 x 256 x 3584 13.7, 11.8; 256 x 256 x 1280
+// 8.0, 10.1).
 constexpr int kClusters = 74;  // (the workspaces' sizes follow from it, without a GPU)
 struct Share {
     int bn, tiles_n, splits, span;
@@ -570,14 +571,14 @@ struct Share {
 inline Share share_product(int64_t tiles_m, int64_t cols, int cols_div, int64_t steps, bool whole = false) {
     Share best = {};
     double least = 0;
-    for (int bn = 256; bn >= (whole ? 256 : 64); bn /= 2) {
+    for (int bn = 256; bn >= (whole ? 256 : 64); bn -= 64) {
         const int64_t n = bn / cols_div, tiles_n = (cols + n - 1) / n, tiles = tiles_m * tiles_n;
         const int64_t most = whole || tiles > kClusters / 2 ? 1 : std::min<int64_t>(16, kClusters / tiles);
         for (int64_t want = 1; want <= most; ++want) {
             const int64_t span = (steps + want - 1) / want, splits = (steps + span - 1) / span;
             if (splits != want) continue;
             const double rounds = (double)((tiles * splits + kClusters - 1) / kClusters);
-            const double t = rounds * (span * (bn == 256 ? 640.0 : (bn == 128 ? 360.0 : 310.0)) + 1500.0 * bn / 256) + (splits < 2 ? 0.0 : (bn == 256 ? 7000.0 + 2200.0 * splits : 3500.0 + 1600.0 * splits));
+            const double t = rounds * (span * (bn == 256 ? 650.0 : (bn == 192 ? 527.0 : (bn == 128 ? 370.0 : 340.0))) + 1500.0 * bn / 256) + (splits < 2 ? 0.0 : (bn == 256 ? 7000.0 + 2200.0 * splits : 3500.0 + 1600.0 * splits));
             if (!best.bn || t < 0.97 * least) {
                 best = {bn, (int)tiles_n, (int)splits, (int)span};
                 least = t;
