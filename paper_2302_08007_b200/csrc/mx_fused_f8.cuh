@@ -3,7 +3,8 @@
 // Products and scales are exact, so results differ from the bf16 kernel's in summation order only.  The pipeline is that of mx_gemm_f8.cuh:
 // stages of 128 K with their scale atoms, a warp of the leader CTA that copies the atoms to tensor memory, one accumulator of 256 columns (the
 // scales take the rest), which the epilogue warps pull into registers at once so that the next item can begin.  It does nothing when *gate is not
-// zero: some element was not representable, and the bf16 kernel, launched behind it with the same gate, computes the product instead.
+// zero: some element was not representable, and the bf16 kernel, launched behind it with the same gate, computes the product instead (with nothing to do that takes
+// 4 us, and 2.6 us the decoding in front of it).
 //
 // Additionally to mx_fused_gemm.cuh a Job has
 //   load8(p, it, kk, rank, dst, bar)   loads of K step kk of 128: A, B, and 512 bytes of scales of A and twice 512 of B behind them

@@ -22,6 +22,10 @@
 // memory's rate for one token; MX6 and MX4 are bound by decoding (the integer/logic pipe, and latency: no pipe is more than two thirds
 // busy); sixteen tokens by decoding on half the warps, which is what the registers of two column groups allow.  Small products are
 // a launch and one trip to memory.
+//
+// The gated layer is the same kernel: of the sixteen rows of a tile eight are lines of the gate and eight the same lines of the other projection, which the matrix
+// instruction gives to the same lanes; the activation and the product are taken where a tile's sums are joined.  One token of 2 x 8192 lines of 4096 MX4 18.5 us = 1.8 TB/s (issue
+// 60 %, integer pipe 52 %, matrix pipe 11 %), 16 of 2 x 16384 MX9 43 us = 3.5 TB/s.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
