@@ -575,8 +575,9 @@ def mx_gated_gemv(cfg_w: Config, w: Planes, N: int, K: int, x: torch.Tensor, h: 
     lines, c, p = w.lines(), cfg_w.c(), w._view
     if k != K or h2.shape != (T, N) or (sx != 1 and K > 1) or (sh != 1 and N > 1) or lines < 2 * N:
         raise ValueError("x is [T, K], h is [T, N], rows contiguous, and the planes hold 2 N lines")
-    if not (x.is_cuda and h.is_cuda and w._on_gpu):
-        raise ValueError("expected CUDA tensors")
+    here = _here()
+    if x.get_device() != here or h.get_device() != here or (w._device != here and lines):
+        raise ValueError("expected CUDA tensors of the current device")
     _check(lib().mx_gated_gemv(C.addressof(c), C.addressof(p), N, K, x2.data_ptr(), _dt(x2), _pitch(ldx, T, K, "x"), T, act, h2.data_ptr(),
                                _dt(h2), _pitch(ldh, T, N, "h"), _stream(stream)), "mx_gated_gemv")
     return h

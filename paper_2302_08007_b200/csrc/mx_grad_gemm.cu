@@ -228,10 +228,20 @@ struct Lines {
 };
 __device__ __forceinline__ void largest_of(const Largest& l) {  // a block of 256
     __shared__ float shared[8];
+    constexpr int kAtOnce = 16;  // rows in flight per thread
     float m = 0.f;
-    for (int64_t i = threadIdx.x; i < l.M; i += 256) {
-        const int64_t t = l.targets[i];
-        if (t >= 0 && t < l.V) m = fmaxf(m, fabsf(l.dloss[i]));
+    for (int64_t i0 = threadIdx.x; i0 < l.M; i0 += 256 * kAtOnce) {
+        int64_t t[kAtOnce];
+        float d[kAtOnce];
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+            const int64_t i = i0 + 256 * j;
+            t[j] = i < l.M ? l.targets[i] : -1;
+            d[j] = i < l.M ? l.dloss[i] : 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j)
+            if (t[j] >= 0 && t[j] < l.V) m = fmaxf(m, fabsf(d[j]));
     }
     for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
     if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = m;
