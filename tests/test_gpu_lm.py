@@ -82,3 +82,65 @@ def test_a_token_through_a_whole_block(dtype):
     other = decode.feed_forward(feed, a, stream=side)
     side.synchronize()
     assert torch.equal(other, out) and (lengths == 2).all()
+
+
+def test_the_head_keeps_the_weights_it_packed():
+    tokens, vocab, d_model = 100, 333, 200
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    rand = lambda *s: torch.randn(s, device="cuda", generator=gen)  # noqa: E731
+    x, z, w = rand(tokens, d_model), rand(tokens, d_model), rand(vocab, d_model) * d_model ** -0.5
+    targets = torch.randint(0, vocab, (tokens,), device="cuda", generator=gen)
+    kept, fresh = head.alloc(bdr.MX9, tokens, vocab, d_model), head.alloc(bdr.MX9, tokens, vocab, d_model)
+    head.losses(x, w, targets, kept)
+    assert torch.equal(head.losses(z, None, targets, kept), head.losses(z, w, targets, fresh))
+
+
+# rows around those that one pass of the search for the largest weight holds in flight (256 threads, 16 rows each); the largest is the last
+@pytest.mark.parametrize("tokens", [4095, 4096, 4097, 4353, 8192, 8193])
+def test_the_largest_weight_of_many_rows(tokens):
+    vocab, d_model = 70, 48
+    gen = torch.Generator(device="cuda").manual_seed(tokens)
+    rand = lambda *s: torch.randn(s, device="cuda", generator=gen)  # noqa: E731
+    targets = torch.randint(0, vocab, (tokens,), device="cuda", generator=gen)
+    dloss = torch.rand(tokens, device="cuda", generator=gen) * 2.0 ** -12
+    dloss[-1] = 3.0
+    buf = head.alloc(bdr.MX6, tokens, vocab, d_model)
+    head.losses(rand(tokens, d_model), rand(vocab, d_model) * d_model ** -0.5, targets, buf)
+    da, dw = head.gradients(targets, dloss, buf)
+    xq, wq = values(bdr.MX6, buf.hidden, tokens, d_model), values(bdr.MX6, buf.weight, vocab, d_model)
+    want_da, want_dw, ea, ew = f.entropy_grads(xq, wq, targets, buf.lse.double(), dloss.double(), torch.bfloat16)
+    f.check(da, want_da, ea, "da")
+    f.check(dw, want_dw, ew, "dw")
+
+
+def test_a_captured_training_step_is_the_eager_one():
+    tokens, d_model, d_ff, vocab = 256, 256, 512, 777
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    rand = lambda *s: torch.randn(s, device="cuda", generator=gen)  # noqa: E731
+    x, w1, w2, wv = rand(tokens, d_model).bfloat16(), (rand(2 * d_ff, d_model) / 16).bfloat16(), (rand(d_model, d_ff) / 22).bfloat16(), rand(vocab, d_model) / 16
+    targets = torch.randint(0, vocab, (tokens,), device="cuda", generator=gen)
+    dloss = torch.full((tokens,), 1 / tokens, device="cuda")
+    layer, top = ffn.alloc(bdr.MX6, tokens, d_model, d_ff), head.alloc(bdr.MX6, tokens, vocab, d_model)
+
+    def step():
+        head.losses(ffn.forward(x, w1, w2, layer), wv, targets, top)
+        dy, dwv = head.gradients(targets, dloss, top)
+        return (top.loss, dwv, *ffn.backward(dy, layer))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for _ in range(2):
+        x.copy_(rand(tokens, d_model))
+        targets.copy_(torch.randint(-1, vocab, (tokens,), device="cuda", generator=gen))
+        graph.replay()
+        got = [t.clone() for t in held]
+        for t in held:
+            t.zero_()
+        assert all(torch.equal(a, b) for a, b in zip(got, step()))
+    assert bdr.bdr_device_status() == 0 and bdr.mx_gemm_status() == 0
