@@ -308,7 +308,9 @@ int decode_pair(const bdr_planes_t& a, int m_a, int64_t rows_a, __nv_bfloat16* o
 // How the tiles of the two products are shared out: the accumulator's columns, and into how many parts the K steps of each product's tiles are cut.
 // Few tiles with long sums (dA of few tokens, dW of a narrow layer) would keep few clusters busy: their steps go to several clusters, whose fp32
 // sums another kernel adds in order.  The shares are those that let the last cluster finish first, with what was measured (in 10 ns): a step
-// 34 with 256 columns and 20 with 128; an item's epilogue 270, 32-bit results 540, with 256 columns and half of that with 128; the joining kernel 350.
+// 40 with 256 columns and 33 with 128, the loads (rows that are not there cost none: 34 and 20 up to 128 tokens); an item's epilogue 270, 32-bit results 540, with
+// 256 columns, and half of that with 128, 400 for 32-bit results of many tokens; the joining kernel 350.  (With 34 and 20 for any tokens too many products took
+// 128 columns: 5888 x 5120 x 512 fp32 245 us, now 193; 1839 x 1605 x 311 fp32 58, 45.  With 40 and 33 for few, 3 x 14809 x 259 30.6 -> 34.4 us.)
 // (Always as for both products: a gradient does not depend on whether the other is wanted.)
 constexpr int kPlanClusters = 74, kMostCuts = 32;
 struct GradPlan {
@@ -333,7 +335,8 @@ static GradPlan plan_grads(int64_t M, int64_t N, int64_t K, int segs, int parts,
     static const int kCuts[] = {1, 2, 3, 4, 6, 10, 16, kMostCuts};  // (of sums of 24 steps at least)
     for (int bn = 256; bn >= 128; bn /= 2) {
         const int64_t tiles_k = (K + bn - 1) / bn, da = tiles_m * tiles_k, dw = tiles_n * tiles_k;
-        const int64_t step = bn == 256 ? 34 : 20, epilogue = (f32 ? 540 : 270) * bn / 256;
+        const bool few = M <= 128;
+        const int64_t step = bn == 256 ? (few ? 34 : 40) : (few ? 20 : 33), epilogue = f32 && !few && bn == 128 ? 400 : (f32 ? 540 : 270) * bn / 256;
         for (int i : kCuts) {
             if (i > 1 && (da * i > kPlanClusters || steps_da < 24)) break;
             const int64_t span_da = (steps_da + i - 1) / i, n_da = da * ((steps_da + span_da - 1) / span_da);
