@@ -175,11 +175,19 @@ struct EntropyJob {
     }
 };
 
-// Few rows: their logits come from the few-token kernel, [M][pitch] fp32.  A block reduces kChunk columns of a row as the epilogue above does (32000 columns of one
-// row: 3 us, a launch and one trip to the L2).
+__device__ __forceinline__ void write_loss(float2 all, float hit, int64_t target, int64_t V, float* loss, float* lse, int* status) {
+    const float l = all.x + logf(all.y);
+    *lse = l;
+    if (target >= V) atomicCAS(status, 0, (int)BDR_ERR_SIZE);
+    *loss = target < 0 ? 0.f : (target < V ? l - hit : __int_as_float(0x7FC00000));
+}
+
+// Few rows: their logits come from the few-token kernel, [M][pitch] fp32.  A block reduces kChunk columns of a row as the epilogue above does, and the one
+// that comes last joins the row's parts, in order (32000 columns of one row: 4 us, a launch and two trips to the L2).
 constexpr int kChunk = 2048;
-__global__ void __launch_bounds__(256) entropy_rows_kernel(const float* logits, int64_t pitch, int64_t M, int64_t V, const int64_t* targets, float2* parts, float* hit) {
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+__global__ void __launch_bounds__(256) entropy_rows_kernel(const float* logits, int64_t pitch, int64_t V, const int64_t* targets, float2* parts, int* counters,
+                                                           float* loss, float* lse, int* status) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // launched as a programmatic dependent of the product
     const int64_t row = blockIdx.y, col0 = (int64_t)blockIdx.x * kChunk;
     const float* const l = logits + row * pitch;
     float v[kChunk / 256];
@@ -202,12 +210,30 @@ __global__ void __launch_bounds__(256) entropy_rows_kernel(const float* logits, 
     for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
     if ((threadIdx.x & 31) == 0) shared[1][threadIdx.x >> 5] = s;
     __syncthreads();
+    __shared__ int last;
+    float2* const of_row = parts + row * gridDim.x;
     if (threadIdx.x == 0) {
         s = 0.f;
         for (int i = 0; i < 8; ++i) s += shared[1][i];
-        parts[(int64_t)blockIdx.x * M + row] = make_float2(m, s);
+        of_row[blockIdx.x] = make_float2(m, s);
+        __threadfence();
+        last = atomicAdd(&counters[row], 1) == (int)gridDim.x - 1;
+    }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    float2 all = make_float2(-INFINITY, 0.f);
+    for (int i = threadIdx.x; i < (int)gridDim.x; i += 256) all = join(all, __ldcg(&of_row[i]));
+    for (int d = 16; d; d >>= 1) all = join(all, make_float2(__shfl_down_sync(0xFFFFFFFFu, all.x, d), __shfl_down_sync(0xFFFFFFFFu, all.y, d)));
+    if ((threadIdx.x & 31) == 0) {
+        shared[0][threadIdx.x >> 5] = all.x;  // (what the block held there before has been read)
+        shared[1][threadIdx.x >> 5] = all.y;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < 8; ++i) all = join(all, make_float2(shared[0][i], shared[1][i]));
         const int64_t t = targets[row];
-        if (t >= col0 && t < col0 + kChunk && t < V) hit[row] = l[t];
+        write_loss(all, t < V && t >= 0 ? l[t] : 0.f, t, V, loss + row, lse + row, status);
     }
 }
 
@@ -225,11 +251,8 @@ __global__ void __launch_bounds__(1024) entropy_join_kernel(const float2* parts,
     __syncthreads();
     if (warp == 0 && row < M) {
         for (int i = 1; i < 32; ++i) mine = join(mine, shared[i][lane]);
-        const float l = mine.x + logf(mine.y);
-        lse[row] = l;
         const int64_t t = targets[row];
-        if (t >= V) atomicCAS(status, 0, (int)BDR_ERR_SIZE);
-        loss[row] = t < 0 ? 0.f : (t < V ? l - hit[row] : __int_as_float(0x7FC00000));
+        write_loss(mine, t >= 0 && t < V ? hit[row] : 0.f, t, V, loss + row, lse + row, status);
     }
 }
 
@@ -263,7 +286,7 @@ struct EntropySpace {
         const fused::Share share = fused::share_product(tiles_m, std::min(piece, V), 1, (K + kBK - 1) / kBK);
         partials = flag + 256;
         counters = partials + round_up(share.partial_bytes(tiles_m), 256);
-        n_counters = share.counters(tiles_m);
+        n_counters = few_rows(M, V, K) ? M : share.counters(tiles_m);
         bytes = counters + round_up(n_counters * 4, 256);
     }
 };
@@ -355,16 +378,16 @@ int mx_cross_entropy(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bdr
     uint8_t* const ws = static_cast<uint8_t*>(workspace);
     if (few_rows(M, V, K)) {
         __nv_bfloat16* const x = reinterpret_cast<__nv_bfloat16*>(ws + s.a);
-        float *const logits = reinterpret_cast<float*>(ws + s.w), *const hit = reinterpret_cast<float*>(ws + s.hit);
+        float* const logits = reinterpret_cast<float*>(ws + s.w);
+        int* const counters = reinterpret_cast<int*>(ws + s.counters);
         float2* const parts = reinterpret_cast<float2*>(ws + s.parts);
         int* const status = device_status_word();
         if (!status) return BDR_ERR_CUDA;
         const int64_t pitch = round_up(V, 64), chunks = (V + kChunk - 1) / kChunk;
-        if ((rc = decode_pair(*a, cfg_a->m, M, x, *w, cfg_w->m, 0, nullptr, K, s.pitch_k, st))) return rc;
+        if ((rc = decode_pair(*a, cfg_a->m, M, x, *w, cfg_w->m, 0, nullptr, K, s.pitch_k, st, nullptr, counters, s.n_counters))) return rc;
         if ((rc = mx_gemv(cfg_w, w, V, K, x, BDR_BF16, s.pitch_k, M, logits, BDR_F32, pitch, stream))) return rc;
-        entropy_rows_kernel<<<dim3((unsigned)chunks, (unsigned)M), 256, 0, st>>>(logits, pitch, M, V, targets, parts, hit);
-        if (cudaGetLastError() != cudaSuccess) return BDR_ERR_CUDA;
-        return launch_dependent(entropy_join_kernel, dim3((unsigned)((M + 31) / 32)), dim3(1024), st, (const float2*)parts, (int)chunks, M, (const float*)hit, targets, V, loss, lse, status);
+        return launch_dependent(entropy_rows_kernel, dim3((unsigned)chunks, (unsigned)M), dim3(256), st, (const float*)logits, pitch, V, targets, parts, counters, loss, lse,
+                                status);
     }
     EntropyJob<false>::Params p = {};
     p.targets = targets;

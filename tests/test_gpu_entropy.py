@@ -319,3 +319,29 @@ def test_captured_and_replayed():
         torch.cuda.synchronize()
         for t, want in zip(outs[1], outs[0]):
             assert torch.equal(t, want)
+
+
+# few rows of a long vocabulary: blocks of 2048 columns, the last of which may hold one; more of them than the last block has threads, in one case
+@pytest.mark.parametrize("m,v,k", [(1, 32768, 64), (24, 32769, 64), (7, 34815, 64), (48, 40961, 840), (3, 530000, 64)])
+def test_few_rows_of_many_blocks(m, v, k):
+    (pa, a), (pw, w), targets, _ = operands(m, v, k, "mx9", "mx6", v)
+    targets[0] = v - 1
+    if m > 2:
+        targets[1], targets[2] = 2047, 2048
+    loss, lse = run(pa, pw, "mx9", "mx6", m, v, k, targets)
+    want, want_lse, _, eloss, else_, _ = f.entropy(a, w, targets)
+    f.check(lse, want_lse, else_, "lse")
+    f.check(loss, want, eloss, "loss")
+    # whichever block comes last, the sums are the same; a target behind the vocabulary is reported, a negative one does not count
+    workspace = f.workspace(bdr.mx_cross_entropy_workspace_bytes(m, v, k))
+    again, again_lse = torch.empty_like(loss), torch.empty_like(lse)
+    for _ in range(5):
+        bdr.mx_cross_entropy(f.CFG["mx9"], pa, f.CFG["mx6"], pw, m, v, k, targets, again, again_lse, workspace)
+        assert torch.equal(again, loss) and torch.equal(again_lse, lse)
+    targets[0] = v
+    targets[m - 1] = -1 if m > 1 else v
+    bdr.mx_cross_entropy(f.CFG["mx9"], pa, f.CFG["mx6"], pw, m, v, k, targets, again, again_lse, workspace)
+    assert torch.equal(again_lse, lse) and again[0].isnan() and (m == 1 or again[-1] == 0)
+    assert torch.equal(again[1:m - 1], loss[1:m - 1])
+    assert bdr.bdr_device_status() != 0
+    bdr.bdr_device_status_reset()
