@@ -96,7 +96,8 @@ int bdr_device_status_reset(void);
  * int of device memory that the caller zeroed: NOT the library's own sticky word, which stays clean) and
  * ends normally, so the context stays usable.  It shows that a wait that gives up is reported and does not
  * hang the GPU.  bdr_selftest_host checks, without any CUDA call, the per-device bookkeeping that decides when
- * a kernel's launch attributes are set (once per device, not once per process); BDR_OK when it holds. */
+ * a kernel's launch attributes are set (once per device, not once per process), and that the pieces into which the
+ * cross entropy cuts a vocabulary stay inside it, over sizes from one to the largest; BDR_OK when both hold. */
 int bdr_selftest_bounded_wait(int* status_dev, void* stream);
 int bdr_selftest_host(void);
 

@@ -842,7 +842,7 @@ def bdr_selftest_bounded_wait(status_word) -> None:
 
 
 def bdr_selftest_host() -> int:
-    """Host-only check of the per-device launch bookkeeping (0 = ok); makes no CUDA call."""
+    """Host-only check of the per-device launch bookkeeping and of the cross entropy's pieces (0 = ok); makes no CUDA call."""
     return int(lib().bdr_selftest_host())
 
 

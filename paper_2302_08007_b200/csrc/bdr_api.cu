@@ -6,6 +6,7 @@
 #include "bdr_async.cuh"
 #include "bdr_device.cuh"
 #include "bdr_host.h"
+#include "mx_fused.h"
 
 namespace bdr {
 
@@ -201,7 +202,7 @@ int bdr_selftest_bounded_wait(int* status_dev, void* stream) {
 
 int bdr_selftest_host(void) {
     // PerDevice: the set-up runs once per device, a failed set-up is not remembered, bad indices are refused
-    static PerDevice once;
+    PerDevice once{};
     int runs[kMaxDevices] = {};
     auto setup_for = [&](int dev) { return [&runs, dev]() -> int { ++runs[dev]; return 10 + dev; }; };
     const int order[] = {0, 1, 0, 63, 1, 0, 63};
@@ -213,7 +214,7 @@ int bdr_selftest_host(void) {
     if (once.get(2, [&]() -> int { ++failures; return 7; }) != 7) return BDR_ERR_CUDA;  // ... so the next call sets up again
     if (once.get(2, [&]() -> int { ++failures; return 9; }) != 7 || failures != 2) return BDR_ERR_CUDA;
     if (once.get(-1, setup_for(0)) != -1 || once.get(kMaxDevices, setup_for(0)) != -1 || runs[0] != 1) return BDR_ERR_CUDA;
-    return BDR_OK;
+    return entropy_pieces_hold() ? BDR_OK : BDR_ERR_SIZE;
 }
 
 int bdr_packed_sizes(const bdr_config_t* cfg, int64_t rows, int64_t cols, int axis, int64_t ld_out[3],

@@ -267,8 +267,8 @@ constexpr int64_t kMostD = 256ll << 20;         // bytes of d at a time
 // Columns of a piece that are decoded, and multiplied, at a time: a large piece goes in four parts, each decoded beside the product of the one before
 // (4096 x 32000 x 4096 MX9: 692 us in one part, 682 in four; 837 and 818 in a long run).  A part has more tiles than there are clusters, twice over.
 int64_t part_columns(int64_t M, int64_t cols, int64_t K) {
-    const int64_t part = round_up((cols + 3) / 4, 256);
-    return cols * K >= 1ll << 25 && ((M + 255) / 256) * (part / 256) >= 4 * fused::kClusters / 2 ? part : cols;
+    const int64_t part = round_up((cols + 3) / 4, 256);  // (more than there are, of fewer than 256 columns)
+    return part < cols && cols * K >= 1ll << 25 && ((M + 255) / 256) * (part / 256) >= 4 * fused::kClusters / 2 ? part : cols;
 }
 
 struct EntropySpace {
@@ -353,6 +353,26 @@ int check_entropy(const bdr_config_t* cfg_a, const bdr_config_t* cfg_w, int64_t 
 }
 
 }  // namespace
+
+// Pieces, and the parts that are decoded at a time, over sizes from one to the largest: none is longer than what it is taken from, and all but the last
+// start on a tile.
+bool entropy_pieces_hold() {
+    const int64_t Ms[] = {1, 255, 4096, 37632, 37633, 131072, kMost};
+    const int64_t Vs[] = {1, 2, 127, 255, 256, 257, 300, 1023, 1025, 32000, 140032, 530001, kMost};
+    const int64_t Ks[] = {1, 64, 1003, 4096, 131071, 131616, 1 << 22, kMost};
+    for (int64_t M : Ms)
+        for (int64_t V : Vs)
+            for (int64_t K : Ks)
+                for (int64_t piece : {EntropySpace(M, V, K).piece, EntropyGradSpace(M, V, K, 1).piece, EntropyGradSpace(M, V, K, fused::kPartsF32).piece}) {
+                    if (piece < 1 || (piece < V && piece % 256)) return false;
+                    for (int64_t cols : {std::min(piece, V), V - (V - 1) / piece * piece}) {  // the first, the last
+                        const int64_t part = part_columns(M, cols, K);
+                        if (part < 1 || part > cols || (part < cols && part % 256)) return false;
+                    }
+                }
+    return true;
+}
+
 }  // namespace bdr
 
 using namespace bdr;

@@ -79,6 +79,9 @@ int gated_rows(const bdr_config_t* cfg_w, const bdr_planes_t* w, int64_t N, int6
 constexpr int64_t kMostFewRows = 48;
 inline bool few_rows(int64_t M, int64_t lines, int64_t K) { return lines * K >= 1ll << 21 && M <= (lines * K >= 1ll << 25 ? kMostFewRows : 24); }
 
+// Host checks of the shares that the operators' launches follow, over sizes from one to the largest (bdr_selftest_host).
+bool entropy_pieces_hold();
+
 // What the operators accept of two packed operands A [M, K] and W [lines, K] (host).
 int check_fused_operands(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bdr_config_t* cfg_w, const bdr_planes_t* w, int64_t K);
 
