@@ -570,6 +570,7 @@ struct Share {
 };
 inline Share share_product(int64_t tiles_m, int64_t cols, int cols_div, int64_t steps, bool whole = false) {
     Share best = {};
+    if (tiles_m == 0 || cols == 0 || steps == 0) return {256, 0, 1, 0};  // no items
     double least = 0;
     for (int bn = 256; bn >= (whole ? 256 : 64); bn -= 64) {
         const int64_t n = bn / cols_div, tiles_n = (cols + n - 1) / n, tiles = tiles_m * tiles_n;

@@ -274,7 +274,7 @@ using namespace bdr;
 extern "C" {
 
 int64_t mx_gated_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K) {
-    if (M < 0 || N < 0 || K < 0 || M > kMost || N > kMost || K > kMost) return 0;
+    if (M < 0 || N < 0 || K < 1 || M > kMost || N > kMost || K > kMost) return 0;
     return GatedSpace(M, N, K, 0).bytes;
 }
 
@@ -320,7 +320,7 @@ int mx_gated_gemm(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bdr_co
 }
 
 int64_t mx_gated_gemm_bwd_workspace_bytes(int64_t M, int64_t N, int64_t K, bdr_dtype_t dt) {
-    if (M < 0 || N < 0 || K < 0 || M > kMost || N > kMost || K > kMost) return 0;
+    if (M < 0 || N < 0 || K < 1 || M > kMost || N > kMost || K > kMost) return 0;
     return GatedSpace(M, N, K, dt == BDR_F32 ? fused::kPartsF32 : 1).bytes;
 }
 

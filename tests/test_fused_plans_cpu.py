@@ -1,7 +1,29 @@
 """How the fused operators' calls are shared out, over sizes from one to the largest: host arithmetic, no GPU is used."""
+import itertools
+
 from paper_2302_08007_b200 import binding as bdr
+from paper_2302_08007_b200 import head
 
 
 def test_no_part_of_a_vocabulary_is_longer_than_what_it_is_taken_from():
     # 37633 rows, 255 columns and a reduction of 131616: one part of 256 columns was decoded
     assert bdr.bdr_selftest_host() == 0
+
+
+def test_sizes_of_workspaces_of_nothing():
+    # what the calls accept has a workspace; what they refuse has none
+    L = bdr.lib()
+    gated = (lambda *s: L.mx_gated_gemm_workspace_bytes(*s), lambda *s: L.mx_gated_gemm_bwd_workspace_bytes(*s, 0), lambda *s: L.mx_gated_gemm_bwd_workspace_bytes(*s, 1))
+    entropy = (lambda *s: L.mx_cross_entropy_workspace_bytes(*s), lambda *s: L.mx_cross_entropy_bwd_workspace_bytes(*s, 0),
+               lambda *s: L.mx_cross_entropy_bwd_workspace_bytes(*s, 1))
+    for m, n, k in itertools.product((0, 1, 256, 1000), (0, 1, 256, 1000), (0, 1, 64, 4096)):
+        for query in gated:
+            assert (query(m, n, k) > 0) == (k > 0)
+        for query in entropy:
+            assert (query(m, n, k) > 0) == (n > 0 and k > 0)
+
+
+def test_buffers_of_no_tokens():
+    for cfg in (bdr.MX6, bdr.MX9):
+        buf = head.alloc(cfg, 0, 300, 64, device="cpu")
+        assert buf.workspace.numel() > 0 and buf.d_weight.shape == (300, 64)
