@@ -449,7 +449,8 @@ int mx_cross_entropy(const bdr_config_t* cfg_a /*host*/, const bdr_planes_t* a /
 
 /* Its gradients with regard to the decoded values of A and W, from the lse of the forward call and dloss (fp32 [M]):
  *     d_ij = dloss[i] (exp(l_ij - lse[i]) - [j = targets[i]]),   dA[M,K] = d W,   dW[V,K] = d^T A
- * Rows whose target is negative, or >= V, have none (whatever dloss, lse and their logits are).  The logits are computed again, piece by piece
+ * Rows whose target is negative, or >= V, have none: their rows of dA are zeros and they add nothing to dW, whatever dloss, lse, their logits
+ * and their lines of A hold (blocks without values included).  The logits are computed again, piece by piece
  * of the vocabulary.  dA and dW are of type `dt`, either may be NULL; d enters the products as bf16 for dt = BF16 and as the sum of three
  * bf16 parts (24 bits) for F32. */
 int64_t mx_cross_entropy_bwd_workspace_bytes(int64_t M, int64_t V, int64_t K, bdr_dtype_t dt);

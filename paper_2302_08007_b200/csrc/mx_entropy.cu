@@ -107,7 +107,7 @@ struct EntropyJob {
         r.live = r.row < p.M;
         const int64_t target = r.live ? p.targets[r.row] : -1;
         r.at = target - p.col0 - r.first;
-        r.counts = target >= 0 && target < p.vocab;
+        r.counts = row_counts(target, p.vocab);
         if constexpr (GRAD) {
             r.lse = r.live ? p.lse[r.row] : 0.f;
             r.scale = r.live ? p.dloss[r.row] / *p.largest : 0.f;
@@ -495,6 +495,7 @@ int mx_cross_entropy_bwd(const bdr_config_t* cfg_a, const bdr_planes_t* a, const
     g.M = M; g.K = K; g.pitch_d = s.piece; g.pitch_k = s.pitch_k;
     g.segs = 1; g.parts = n_parts;
     g.da = da; g.ld_da = ld_da; g.ld_dw = ld_dw;
+    g.targets = targets; g.vocab = V;
     g.f32 = dt == BDR_F32;
     g.acc = s.piece < V ? reinterpret_cast<float*>(ws + s.acc) : nullptr;
     g.ld_acc = s.pitch_k;

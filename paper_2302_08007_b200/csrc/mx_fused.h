@@ -17,7 +17,9 @@ constexpr int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * t
 // Pitch (elements) of lines of K decoded elements: whole items of the decode kernel.
 constexpr int64_t line_pitch(int64_t K) { return round_up(K, 32); }
 
-// The largest |dloss| of the rows that count (0 <= target < V), by which a gradient is divided before it is rounded to bf16 and the results are
+// Whether a row counts: its target is a column of the vocabulary.
+__host__ __device__ constexpr bool row_counts(int64_t target, int64_t V) { return target >= 0 && target < V; }
+// The largest |dloss| of the rows that count, by which a gradient is divided before it is rounded to bf16 and the results are
 // multiplied in fp32; 1 where there is none, or an infinity.
 struct Largest {
     const float* dloss;
@@ -28,7 +30,8 @@ struct Largest {
 // Packed lines of K elements (Table II formats, m magnitude bits) of two operands -> bf16 [rows, pitch]; what lies behind K in a row is
 // unspecified.  gate: NULL, or device flag without which nothing is decoded.  n_zero words at `zero` are cleared on the side.
 // beside: the kernel in front in the stream is a product that does not read the output: it is decoded on what that product leaves free of the
-// SMs, and is complete when both are.  largest: NULL, or what a block of its own computes on the side.
+// SMs, and is complete when both are.  largest: NULL, or what a block of its own computes on the side; blocks of a without values (exponent
+// byte 0xFF) in rows that do not count are then zeros instead of NaN, which would stay NaN in a product with the row's zero gradient.
 int decode_pair(const bdr_planes_t& a, int m_a, int64_t rows_a, __nv_bfloat16* out_a, const bdr_planes_t& w, int m_w, int64_t rows_w, __nv_bfloat16* out_w,
                 int64_t K, int64_t pitch, cudaStream_t st, const int* gate = nullptr, int* zero = nullptr, int64_t n_zero = 0, bool beside = false, const Largest* largest = nullptr);
 
@@ -63,6 +66,8 @@ struct GradProducts {
     int64_t ld_acc;
     float* sums;            // grad_sums_bytes(M, N, K, segs) bytes
     const float* scale;     // device: factor of both gradients; NULL: 1
+    const int64_t* targets; // device, NULL or [M]: rows of dA that do not count are zeros, whatever W holds
+    int64_t vocab;
     bool first, last;       // of those calls: the first does not read acc, the last writes da
 };
 int64_t grad_sums_bytes(int64_t M, int64_t N, int64_t K, int segs);

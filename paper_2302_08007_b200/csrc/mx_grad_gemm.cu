@@ -30,6 +30,9 @@ struct Target {
     int splits, span;   // K steps of a part
     int steps;
     int scaled;      // `out` is the result, which takes the factor
+    const int64_t* targets;  // NULL, or the rows of the result that do not count are zeros
+    int64_t vocab;
+    __device__ __forceinline__ bool nothing(int64_t row) const { return targets && !row_counts(targets[row], vocab); }
 };
 
 template <bool F32>
@@ -119,6 +122,10 @@ struct GradJob {
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] *= s;
         }
+        if (e.lane < rows && t.nothing(out_row + e.lane)) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = 0.f;
+        }
         fused::store_tile(e, t.out, out_row, col, rows, n, v);
     }
     static __device__ __forceinline__ void epilogue(const Params& p, const Item& it, const fused::Epi& e) {
@@ -161,6 +168,7 @@ __global__ void __launch_bounds__(128) grad_join_kernel(Target da, Target dw, in
             const float s = *scale;
             v.x *= s; v.y *= s; v.z *= s; v.w *= s;
         }
+        if (t.nothing(row)) v = make_float4(0.f, 0.f, 0.f, 0.f);
         const float w[4] = {v.x, v.y, v.z, v.w};
         char* const to = t.out.at(row, col);
         if (t.out.f32) {
@@ -180,9 +188,10 @@ __global__ void __launch_bounds__(128) grad_join_kernel(Target da, Target dw, in
 }
 
 // One thread decodes 32 elements of a line (two blocks) straight from the planes and writes 64 bytes.  Bound by memory: 15547 lines of 3417 MX6 27 us = 5.4 TB/s.
+// targets: NULL, or blocks out of the ordinary (all those without values among them) of rows that do not count are zeros.
 template <int W>
 __device__ __forceinline__ void decode_items(const bdr_planes_t& in, __nv_bfloat16* out, int64_t pitch, int64_t n_items, uint32_t items_per_row, int nb,
-                                             int64_t first, int64_t stride) {
+                                             int64_t first, int64_t stride, const int64_t* targets, int64_t vocab) {
     for (int64_t g = first; g < n_items; g += stride) {
         const int64_t row = (uint64_t)n_items >> 32 ? g / items_per_row : (uint32_t)g / items_per_row;
         const uint32_t it = (uint32_t)(g - row * items_per_row);
@@ -206,6 +215,9 @@ __device__ __forceinline__ void decode_items(const bdr_planes_t& in, __nv_bfloat
         const uint32_t F0 = Fw & 0xFFu, F1 = 2 * (int)it + 1 < nb ? Fw >> 8 : F0;
         if ((F0 - x2::kMinF <= (uint32_t)(x2::kMaxDecodeF - x2::kMinF)) && (F1 - x2::kMinF <= (uint32_t)(x2::kMaxDecodeF - x2::kMinF))) {
             x2::decode_two_blocks_row<W>(s, F0, F1, mw, yw);
+        } else if (targets && !row_counts(targets[row], vocab)) {
+#pragma unroll
+            for (int k = 0; k < 16; ++k) yw[k] = 0u;
         } else {
             x2::TwoBlocks<W> in2;
 #pragma unroll
@@ -241,7 +253,7 @@ __device__ __forceinline__ void largest_of(const Largest& l) {  // a block of 25
         }
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j)
-            if (t[j] >= 0 && t[j] < l.V) m = fmaxf(m, fabsf(d[j]));
+            if (row_counts(t[j], l.V)) m = fmaxf(m, fabsf(d[j]));
     }
     for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
     if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = m;
@@ -266,10 +278,11 @@ __global__ void __launch_bounds__(256) decode_pair_kernel(Lines first, Lines sec
     const bool one = blockIdx.x < first_blocks;
     const Lines& l = one ? first : second;
     const int64_t at = (int64_t)(one ? blockIdx.x : blockIdx.x - first_blocks) * 256 + threadIdx.x, stride = (int64_t)(one ? first_blocks : blocks - first_blocks) * 256;
+    const int64_t* const targets = one && largest.out ? largest.targets : nullptr;
     switch (l.m) {
-        case 2: decode_items<3>(l.in, l.out, pitch, l.n_items, items_per_row, nb, at, stride); break;
-        case 4: decode_items<5>(l.in, l.out, pitch, l.n_items, items_per_row, nb, at, stride); break;
-        default: decode_items<8>(l.in, l.out, pitch, l.n_items, items_per_row, nb, at, stride); break;
+        case 2: decode_items<3>(l.in, l.out, pitch, l.n_items, items_per_row, nb, at, stride, targets, largest.V); break;
+        case 4: decode_items<5>(l.in, l.out, pitch, l.n_items, items_per_row, nb, at, stride, targets, largest.V); break;
+        default: decode_items<8>(l.in, l.out, pitch, l.n_items, items_per_row, nb, at, stride, targets, largest.V); break;
     }
     if (beside) asm volatile("griddepcontrol.wait;" ::: "memory");  // not before the product in front: whoever waits for this kernel has both
 }
@@ -282,7 +295,8 @@ int decode_pair(const bdr_planes_t& a, int m_a, int64_t rows_a, __nv_bfloat16* o
     Lines l[2] = {{a, out_a, rows_a, m_a}, {w, out_w, rows_w, m_w}};
     const int64_t per_row = (K + 31) / 32;
     for (Lines& x : l) {
-        if (!gate && !beside && x.n_items * K >= (1ll << 23)) {
+        const bool rows_count = &x == l && largest;  // (the other kernel knows no rows)
+        if (!gate && !beside && !rows_count && x.n_items * K >= (1ll << 23)) {
             QParams qp;
             qp.k1 = 16; qp.k2 = 2; qp.d2 = 1; qp.m = x.m; qp.rounding = BDR_ROUND_NEAREST_EVEN; qp.beta = 1; qp.qmax = (1u << x.m) - 1u;
             const int rc = unpack_rowwise_mx_x2(x.in, x.out, x.n_items, K, pitch, qp, st);  // whole runs of 2048 elements: through shared memory
@@ -398,6 +412,8 @@ static int launch_grads(const GradProducts& g, cudaStream_t st) {
         const int64_t rows = i ? g.segs * g.N : g.M;
         t.out = i ? fused::make_rows(g.dw, g.ld_dw, F32) : (g.last ? fused::make_rows(g.da, g.ld_da, F32) : fused::make_rows(g.acc, g.ld_acc, true));
         t.scaled = i || g.last;
+        t.targets = !i && g.last ? g.targets : nullptr;
+        t.vocab = g.vocab;
         t.read = i || g.first ? nullptr : g.acc;
         t.ld_read = g.ld_acc * 4;
         t.splits = i ? plan.cut_dw : plan.cut_da;

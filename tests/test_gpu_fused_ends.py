@@ -31,3 +31,42 @@ def test_no_tokens_with_workspaces_of_their_own(dtype):
     buf.d_weight.fill_(7.0)
     d_hidden, d_weight = head.gradients(targets, torch.empty(0, device="cuda"), buf)
     assert loss.shape == (0,) and d_hidden.shape == (0, k) and (d_weight == 0).all()
+
+
+# rows decoded by either kernel, one and several pieces of the vocabulary, sums of few tiles cut or not, and the 8-bit path (which falls back)
+@pytest.mark.parametrize("m,v,k,fmt", [(40, 300, 64, "mx6"), (33, 60, 8192, "mx9"), (300, 1000, 1111, "mx4"), (4100, 500, 2048, "mx9"), (4000, 34567, 96, "mx6"),
+                                       (1024, 16640, 2176, "mx6")])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_rows_that_do_not_count_hold_no_values(m, v, k, fmt, dtype):
+    gen = torch.Generator(device="cuda").manual_seed(21)
+    (pa, a), (pw, w) = (f.packed(f.CFG[fmt], torch.randn(r, k, device="cuda", generator=gen) * s) for r, s in ((m, 1.0), (v, k ** -0.5)))
+    targets = torch.randint(0, v, (m,), device="cuda", generator=gen)
+    out = torch.zeros(m, dtype=torch.bool, device="cuda")
+    out[torch.tensor([0, 7, m // 2, m - 1], device="cuda")] = True
+    targets[out] = torch.tensor([-100, v, -1, 2 ** 40], device="cuda")
+    pa.exps[out] = 0xFF
+    loss, lse = torch.empty(m, device="cuda"), torch.empty(m, device="cuda")
+    bdr.mx_cross_entropy(f.CFG[fmt], pa, f.CFG[fmt], pw, m, v, k, targets, loss, lse, f.workspace(bdr.mx_cross_entropy_workspace_bytes(m, v, k)))
+    assert torch.equal(lse.isnan(), out) and (loss[targets < 0] == 0).all()
+    assert bdr.bdr_device_status_reset() == -5
+    dloss = torch.rand(m, device="cuda", generator=gen)
+    dloss[out] = float("nan")
+
+    def grads():
+        da, dw = torch.full((m, k), float("nan"), device="cuda", dtype=dtype), torch.full((v, k), float("nan"), device="cuda", dtype=dtype)
+        ws = f.workspace(bdr.mx_cross_entropy_bwd_workspace_bytes(m, v, k, dtype))
+        bdr.mx_cross_entropy_bwd(f.CFG[fmt], pa, f.CFG[fmt], pw, m, v, k, targets, lse, dloss, da, dw, ws)
+        return da, dw
+
+    da, dw = grads()
+    a[out] = 0.0
+    clean = torch.where(out, 0.0, lse.double())
+    want_a, want_w, ea, ew = f.entropy_grads(a, w, targets, clean, torch.where(out, 0.0, dloss.double()), dtype)
+    f.check(da, want_a, ea, "da")
+    f.check(dw, want_w, ew, "dw")
+    assert (da[out] == 0).all()
+    # a line of the weights without values leaves its own in every row that counts, in no other
+    pw.exps[v - 1, 0] = 0xFF
+    da, _ = grads()
+    assert (da[out] == 0).all() and da[~out][:, :16].isnan().all()
+    assert bdr.bdr_device_status() == 0
