@@ -402,12 +402,14 @@ int mx_attn_decode(const mx_kv_cache_t* cache /*host*/, const void* q, int64_t l
 
 /* ---- Feed-forward layer and vocabulary head of a language model ------------------------------------------------
  * Products of packed operands with what follows them fused to them.  Operands are axis-1 planes in the Table II formats (k1 = 16,
- * k2 = 2, d2 = 1, m in {2, 4, 7}; either tie rule; the two formats of a call may differ), any sizes up to 2^28 with K >= 1; pitches and plane
+ * k2 = 2, d2 = 1, m in {2, 4, 7}; either tie rule; the two formats of a call may differ), any sizes up to 2^28 with K >= 1; of matrices of M, N (or V)
+ * and K rows and columns with 2^29 tiles of 256 x 128 or more, ragged ones counted whole, a call can be refused (BDR_ERR_UNSUPPORTED).  Pitches and plane
  * addresses are multiples of 16 bytes.  Products are those of the decoded values (in bf16, so blocks whose unit is below 2^-133 lose
  * low bits, as in mx_gemm_ws; a few rows take mx_gemv's kernel, with its limits) with fp32 accumulation; blocks with the exponent byte 0xFF
  * decode to NaN.  Results do not change from run to run.  The tensors of a call do not overlap.
  * A workspace is device scratch, 256-byte aligned, contents overwritten, of the size that the call's _workspace_bytes gives: a positive
- * number where M or N is 0 too, which the calls accept, and 0 for negative sizes, sizes above 2^28, and K or V of 0.  Bounded waits that run out leave BDR_ERR_TIMEOUT in the sticky word of bdr_device_status. */
+ * number where M or N is 0 too, which the calls accept, and 0 for negative sizes, sizes above 2^28, and K or V of 0.
+ * Bounded waits that run out leave BDR_ERR_TIMEOUT in the sticky word of bdr_device_status. */
 
 /* Activations.  SILU x / (1 + exp(-x)); GELU x Phi(x); GELU_TANH x (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))) / 2; RELU max(x, 0),
  * with derivative 0 at 0. */

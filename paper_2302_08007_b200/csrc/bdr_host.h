@@ -132,6 +132,7 @@ struct ZeroTiles {   // `count` tiles of 256 x 256 floats of c (row pitch ldc), 
     int64_t ldc;
     int tiles_n, tile0, count, tiles_m, band_rows;
 };
+constexpr int64_t kMostReencodeK = 65535ll * 1024;  // segments of 1024 are the grid's second dimension
 int reencode_rowwise_e4m3(const bdr_planes_t& a, int m_a, const bdr_planes_t& b, int m_b, int64_t M, int64_t N, int64_t K,
                           uint8_t* out_a, uint8_t* out_b, uint8_t* sf_a, uint8_t* sf_b, int* inexact, const ZeroTiles& z,
                           cudaStream_t st);

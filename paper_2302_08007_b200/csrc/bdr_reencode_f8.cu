@@ -257,7 +257,7 @@ int reencode_rowwise_e4m3(const bdr_planes_t& a, int m_a, const bdr_planes_t& b,
                           uint8_t* out_a, uint8_t* out_b, uint8_t* sf_a, uint8_t* sf_b, int* inexact, const ZeroTiles& z,
                           cudaStream_t st) {
     if (M % 128 || N % 128 || K % 128 || K <= 0) return BDR_ERR_UNSUPPORTED;
-    if ((M + N) / kF8StripRows + z.count > 0x7FFFFFFF || (K + 1023) / 1024 > 65535) return BDR_ERR_UNSUPPORTED;
+    if ((M + N) / kF8StripRows + z.count > 0x7FFFFFFF || K > kMostReencodeK) return BDR_ERR_UNSUPPORTED;
     if (m_a == 2 && m_b == 2) return launch_reencode<3, 3>(a, b, M, N, K, out_a, out_b, sf_a, sf_b, inexact, z, st);
     if (m_a == 2 && m_b == 4) return launch_reencode<3, 5>(a, b, M, N, K, out_a, out_b, sf_a, sf_b, inexact, z, st);
     if (m_a == 4 && m_b == 2) return launch_reencode<5, 3>(a, b, M, N, K, out_a, out_b, sf_a, sf_b, inexact, z, st);

@@ -226,9 +226,10 @@ int launch_f8(const typename Job::Params& p, cudaStream_t st) {
 }
 
 // Whether a product A [M, K] x W [lines, K] (lines in groups of `group` rows that start on a tile) takes the 8-bit path: formats that E4M3 holds, whole
-// tiles, and enough work that half the product's time outweighs four more launches (the re-encoding, and the bf16 kernels that look at the flag).
+// tiles, enough work that half the product's time outweighs four more launches (the re-encoding, and the bf16 kernels that look at the flag), and no
+// longer a reduction than the re-encoding takes.
 inline bool takes_f8(int m_a, int m_w, int64_t M, int64_t lines, int64_t group, int64_t K) {
-    return m_a <= 4 && m_w <= 4 && M % 256 == 0 && group % 128 == 0 && K % 128 == 0 && lines % 256 == 0 && M * lines >= (1ll << 35) / K;
+    return m_a <= 4 && m_w <= 4 && M % 256 == 0 && group % 128 == 0 && K % 128 == 0 && K <= kMostReencodeK && lines % 256 == 0 && M * lines >= (1ll << 35) / K;
 }
 // Bytes of the re-encoded operands and their scales.
 inline int64_t f8_bytes(int64_t M, int64_t lines, int64_t K) { return round_up((M + lines) * K + (M + lines) * K / 32, 256); }

@@ -27,3 +27,11 @@ def test_buffers_of_no_tokens():
     for cfg in (bdr.MX6, bdr.MX9):
         buf = head.alloc(cfg, 0, 300, 64, device="cpu")
         assert buf.workspace.numel() > 0 and buf.d_weight.shape == (300, 64)
+
+
+def test_a_reduction_longer_than_the_reencoding_takes_has_no_space_for_it():
+    # MX4 / MX6 operands of more than 65535 x 1024 elements a line stay on the bf16 path: the 8-bit one would refuse them half way through the call
+    L, most = bdr.lib(), 65535 * 1024
+    for query, args in ((L.mx_gated_gemm_bwd_workspace_bytes, (256, 128)), (L.mx_cross_entropy_bwd_workspace_bytes, (256, 256))):
+        assert query(*args, most + 1024, 1) < query(*args, most, 1)
+        assert query(*args, most, 1) > query(*args, most - 1, 1) + 256 * most
