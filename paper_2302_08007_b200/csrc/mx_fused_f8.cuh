@@ -75,7 +75,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads8, 1) fused_
             const typename Job::Item item = Job::item(p, i);
             for (int kk = 0; kk < steps; ++kk) {
                 if (turn > 0) {
-                    ok = mbar_wait(&bars.empty[stage], (turn - 1) & 1);
+                    ok = mbar_wait_warp(&bars.empty[stage], (turn - 1) & 1);
                     if (!ok) break;
                 }
                 if (elect_one()) {
@@ -100,12 +100,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads8, 1) fused_
             int tcount = 0;
             for (int i = cluster_id; i < p.n_items && ok; i += n_clusters, ++tcount) {
                 if (tcount >= 1) {  // the epilogues of both CTAs hold the item before in registers
-                    ok = mbar_wait_cluster(&bars.tmem_empty, (tcount - 1) & 1);
+                    ok = mbar_wait_warp(&bars.tmem_empty, (tcount - 1) & 1);
                     if (!ok) break;
                     tc_fence_after();
                 }
                 for (int kk = 0; kk < steps; ++kk) {
-                    ok = mbar_wait_cluster(&bars.sf_ready[stage], turn & 1);  // data landed, scales copied
+                    ok = mbar_wait_warp(&bars.sf_ready[stage], turn & 1);  // data landed, scales copied
                     if (!ok) break;
                     tc_fence_after();
                     const uint32_t sa = smem_u32(stages + stage * kStage8Bytes);
@@ -127,7 +127,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads8, 1) fused_
         } else {
             for (int i = cluster_id; i < p.n_items && ok; i += n_clusters)
                 for (int kk = 0; kk < steps; ++kk) {
-                    ok = mbar_wait(&bars.full_local[stage], turn & 1);
+                    ok = mbar_wait_warp(&bars.full_local[stage], turn & 1);
                     if (!ok) break;
                     if (elect_one()) mbar_arrive_cluster(&bars.full[stage], 0);
                     __syncwarp();
@@ -144,7 +144,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads8, 1) fused_
             for (int i = cluster_id; i < p.n_items && ok; i += n_clusters)
                 for (int kk = 0; kk < steps; ++kk) {
                     // (the stage's previous MMAs are done: the producer refilled it only after their commit)
-                    ok = mbar_wait_cluster(&bars.full[stage], turn & 1);
+                    ok = mbar_wait_warp(&bars.full[stage], turn & 1);
                     if (!ok) break;
                     tc_fence_after();
                     const uint32_t sf = smem_u32(stages + stage * kStage8Bytes) + kTiles8;
@@ -173,8 +173,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads8, 1) fused_
         int tcount = 0;
         for (int i = cluster_id; i < p.n_items; i += n_clusters, ++tcount) {
             const typename Job::Item item = Job::item(p, i);
-            ok = ok && mbar_wait(&bars.tmem_full, tcount & 1);
-            ok = __all_sync(0xFFFFFFFFu, ok);
+            ok = ok && mbar_wait_warp(&bars.tmem_full, tcount & 1);
             if (!ok) break;
             tc_fence_after();
             uint32_t u[4][32];

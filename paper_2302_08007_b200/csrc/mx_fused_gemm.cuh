@@ -189,7 +189,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
             const typename Job::Item item = Job::item(p, i);
             for (int kk = 0; kk < item.steps; ++kk) {
                 if (turn > 0) {
-                    ok = mbar_wait(&bars.empty[stage], (turn - 1) & 1);
+                    ok = mbar_wait_warp(&bars.empty[stage], (turn - 1) & 1);
                     if (!ok) break;
                 }
                 if (elect_one()) {
@@ -231,12 +231,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
                         buf = tcount & 1;
                         acc = tmem_base + (uint32_t)buf * 256u;
                         if (tcount >= 2) {  // the epilogues of both CTAs have drained this buffer
-                            ok = mbar_wait_cluster(&bars.tmem_empty[buf], ((tcount >> 1) - 1) & 1);
+                            ok = mbar_wait_warp(&bars.tmem_empty[buf], ((tcount >> 1) - 1) & 1);
                             if (!ok) break;
                             tc_fence_after();
                         }
                     }
-                    ok = mbar_wait_cluster(&bars.full[stage], turn & 1);
+                    ok = mbar_wait_warp(&bars.full[stage], turn & 1);
                     if (!ok) break;
                     tc_fence_after();
                     const uint32_t sa = smem_u32(stages + stage * stage_bytes), sb = sa + kOperandBytes;
@@ -257,7 +257,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
             for (int i = deal.first(); i < p.n_items && ok; i = deal.next(i)) {
                 const typename Job::Item item = Job::item(p, i);
                 for (int kk = 0; kk < item.steps; ++kk) {
-                    ok = mbar_wait(&bars.full_local[stage], turn & 1);
+                    ok = mbar_wait_warp(&bars.full_local[stage], turn & 1);
                     if (!ok) break;
                     if (elect_one()) mbar_arrive_cluster(&bars.full[stage], 0);
                     __syncwarp();
@@ -281,8 +281,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
             e.lane = lane;
             e.tile = smem_u32(tiles + ew * kTileBytes);
             auto next = [&](int buf) {  // waits for the next accumulator
-                ok = ok && mbar_wait(&bars.tmem_full[buf], (tcount >> 1) & 1);
-                ok = __all_sync(0xFFFFFFFFu, ok);
+                ok = ok && mbar_wait_warp(&bars.tmem_full[buf], (tcount >> 1) & 1);
                 tc_fence_after();
                 return ok;
             };

@@ -1,5 +1,7 @@
 """How the fused operators' calls are shared out, over sizes from one to the largest: host arithmetic, no GPU is used."""
 import itertools
+import os
+import re
 
 from paper_2302_08007_b200 import binding as bdr
 from paper_2302_08007_b200 import head
@@ -35,3 +37,14 @@ def test_a_reduction_longer_than_the_reencoding_takes_has_no_space_for_it():
     for query, args in ((L.mx_gated_gemm_bwd_workspace_bytes, (256, 128)), (L.mx_cross_entropy_bwd_workspace_bytes, (256, 256))):
         assert query(*args, most + 1024, 1) < query(*args, most, 1)
         assert query(*args, most, 1) > query(*args, most - 1, 1) + 256 * most
+
+
+def test_the_lanes_of_a_role_get_one_answer_from_a_wait():
+    # The warps of the fused kernels issue with elect.sync: a lane that left its loop alone, because its own polls of a bounded wait ran out, would keep
+    # the others waiting for good.  Making a wait run out in the middle of a phase is no test for a GPU, so the source is looked at: only the waits behind
+    # a failure, whose answers nobody reads, are each lane's own.
+    for name in ("mx_fused_gemm.cuh", "mx_fused_f8.cuh"):
+        with open(os.path.join(os.path.dirname(bdr.__file__), "csrc", name)) as f:
+            waits = [line.strip() for line in f if re.search(r"\bmbar_wait\w*\(", line)]
+        assert len(waits) >= 6
+        assert all("mbar_wait_warp(" in w or w.startswith("if (s < stage || turn > 0) mbar_wait(") for w in waits), waits
