@@ -175,11 +175,13 @@ struct EntropyJob {
     }
 };
 
+// The loss is not the difference of lse, whose rounding would be all that is left of a small one beside large logits, but the log of the sum beside that
+// of two logits, which is exact where they are near.
 __device__ __forceinline__ void write_loss(float2 all, float hit, int64_t target, int64_t V, float* loss, float* lse, int* status) {
-    const float l = all.x + logf(all.y);
-    *lse = l;
+    const float above = logf(all.y);
+    *lse = all.x + above;
     if (target >= V) atomicCAS(status, 0, (int)BDR_ERR_SIZE);
-    *loss = target < 0 ? 0.f : (target < V ? l - hit : __int_as_float(0x7FC00000));
+    *loss = target < 0 ? 0.f : (target < V ? (all.x - hit) + above : __int_as_float(0x7FC00000));
 }
 
 // Few rows: their logits come from the few-token kernel, [M][pitch] fp32.  A block reduces kChunk columns of a row as the epilogue above does, and the one

@@ -70,3 +70,24 @@ def test_rows_that_do_not_count_hold_no_values(m, v, k, fmt, dtype):
     da, _ = grads()
     assert (da[out] == 0).all() and da[~out][:, :16].isnan().all()
     assert bdr.bdr_device_status() == 0
+
+
+# the two kernels that join a row's parts; many rows, few of a short vocabulary, few of a long one
+@pytest.mark.parametrize("m,v,below", [(200, 300, 13), (3, 300, 13), (200, 36069, 18), (3, 36069, 18)])
+def test_small_losses_beside_large_logits(m, v, below):
+    # logits 1024 (the target's) and 1024 - below, exact in every step; the log of their sum lies half way between two fp32 numbers, 6e-5 from each
+    k = 64
+    a, w = torch.zeros(m, k, device="cuda"), torch.zeros(v, k, device="cuda")
+    a[:, 0], a[:, 16] = 1024.0, -1.0
+    w[:, 0], w[:, 16] = 1.0, float(below)
+    w[v // 2, 16] = 0.0
+    (pa, a), (pw, w) = f.packed(bdr.MX9, a), f.packed(bdr.MX9, w)
+    logits = a @ w.T
+    assert (logits == 1024).sum() == m and (logits == 1024 - below).sum() == m * (v - 1)
+    targets = torch.full((m,), v // 2, device="cuda", dtype=torch.int64)
+    loss, lse = torch.empty(m, device="cuda"), torch.empty(m, device="cuda")
+    bdr.mx_cross_entropy(bdr.MX9, pa, bdr.MX9, pw, m, v, k, targets, loss, lse, f.workspace(bdr.mx_cross_entropy_workspace_bytes(m, v, k)))
+    want = torch.log1p((v - 1) * torch.exp(torch.tensor(-float(below), dtype=torch.float64, device="cuda"))).expand(m)
+    # a sum just above 1: what its additions round off, as in fused_helpers.entropy, exponentials within 2^-21 of themselves, and the logarithm
+    f.check(loss, want, (160 + v / 128) * 2.0 ** -24 + 2.0 ** -20 * want, "loss")
+    f.check(lse, 1024 + want, 2.0 ** -23 * (1024 + want), "lse")
