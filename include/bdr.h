@@ -405,8 +405,9 @@ int mx_attn_decode(const mx_kv_cache_t* cache /*host*/, const void* q, int64_t l
  * k2 = 2, d2 = 1, m in {2, 4, 7}; either tie rule; the two formats of a call may differ), any sizes up to 2^28 with K >= 1; of matrices of M, N (or V)
  * and K rows and columns with 2^29 tiles of 256 x 128 or more, ragged ones counted whole, a call can be refused (BDR_ERR_UNSUPPORTED).  Pitches and plane
  * addresses are multiples of 16 bytes.  Products are those of the decoded values (in bf16, so blocks whose unit is below 2^-133 lose
- * low bits, as in mx_gemm_ws; a few rows take mx_gemv's kernel, with its limits) with fp32 accumulation; blocks with the exponent byte 0xFF
- * decode to NaN.  Results do not change from run to run.  The tensors of a call do not overlap.
+ * low bits, as in mx_gemm_ws; a few rows take mx_gemv's kernel, with its limits) with fp32 accumulation, whose additions the tensor
+ * core cuts off instead of rounding them (32-bit results of sums of one sign are off by about as much as plain fp32 sums: 3e-7 to 5e-6 for 4096 to 16384
+ * terms); blocks with the exponent byte 0xFF decode to NaN.  Results do not change from run to run.  The tensors of a call do not overlap.
  * A workspace is device scratch, 256-byte aligned, contents overwritten, of the size that the call's _workspace_bytes gives: a positive
  * number where M or N is 0 too, which the calls accept, and 0 for negative sizes, sizes above 2^28, and K or V of 0.
  * Bounded waits that run out leave BDR_ERR_TIMEOUT in the sticky word of bdr_device_status. */

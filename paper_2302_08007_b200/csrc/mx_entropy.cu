@@ -60,7 +60,7 @@ struct EntropyJob {
     struct Item { int steps, tm, tn, tile, split; };
     static constexpr bool b_mn = false;
     static constexpr int kSpan = 0;
-    static constexpr bool kCut = true;
+    static constexpr bool kCut = true, kBack = false;
     static __device__ __forceinline__ int rows(const Params& p) { return p.M; }
     static __device__ __forceinline__ int chunks(int bn, int) { return bn / 64; }
     static __device__ __forceinline__ int chunk(int bn, int half, int i) { return half * (bn / 2) + 32 * i; }
@@ -174,6 +174,17 @@ struct EntropyJob {
         end(p, r);
     }
 };
+
+// where one chain of additions would lose bits of the logits; of the gradients' too, which lse goes with
+template <bool GRAD>
+struct EntropyJobInSpans : EntropyJob<GRAD> {
+    static constexpr int kSpan = fused::kBackSpan;
+    static constexpr bool kBack = true;
+};
+template <bool GRAD>
+int launch_piece(const typename EntropyJob<GRAD>::Params& p, int m_a, int m_w, cudaStream_t st) {
+    return fused::one_chain(m_a, m_w, p.span) ? fused::launch<EntropyJob<GRAD>>(p, st) : fused::launch<EntropyJobInSpans<GRAD>>(p, st);
+}
 
 // The loss is not the difference of lse, whose rounding would be all that is left of a small one beside large logits, but the log of the sum beside that
 // of two logits, which is exact where they are near.
@@ -422,6 +433,7 @@ int mx_cross_entropy(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bdr
     if (!p.status) return BDR_ERR_CUDA;
     __nv_bfloat16 *const wa = reinterpret_cast<__nv_bfloat16*>(ws + s.a), *const ww = reinterpret_cast<__nv_bfloat16*>(ws + s.w);
     const bool f8 = fused::takes_f8(cfg_a->m, cfg_w->m, M, V, V, K);
+    const bool beside = fused::one_chain(cfg_a->m, cfg_w->m, (K + kBK - 1) / kBK);  // (else the product leaves no registers for the decoding)
     for (int64_t v = 0; v < V; v += s.piece) {
         const int64_t cols = std::min(s.piece, V - v);
         const bdr_planes_t lines = lines_from(*w, v);
@@ -430,7 +442,7 @@ int mx_cross_entropy(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bdr
             if ((rc = fused::encode_f8(*a, cfg_a->m, M, lines, cfg_w->m, cols, 1, K, ws, reinterpret_cast<int*>(ws + s.flag), &p.f8, &p.gate, st))) return rc;
             if ((rc = fused::launch_f8<EntropyJob<false>>(p, st))) return rc;
         }
-        const int64_t part = f8 ? cols : part_columns(M, cols, K);
+        const int64_t part = f8 || !beside ? cols : part_columns(M, cols, K);
         for (int64_t c = 0; c < cols; c += part) {
             const int64_t n = std::min(part, cols - c);
             // (with an 8-bit path in front, A's bf16 values are overwritten by the next piece's bytes)
@@ -438,7 +450,7 @@ int mx_cross_entropy(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bdr
                                   p.counters, s.n_counters, c > 0)))
                 return rc;
             if (part < cols && (rc = set_piece(p, M, K, v + c, n, s.pitch_k, ws + s.a, ws + s.w + c * s.pitch_k * 2, f8))) return rc;
-            if ((rc = fused::launch<EntropyJob<false>>(p, st))) return rc;
+            if ((rc = launch_piece<false>(p, cfg_a->m, cfg_w->m, st))) return rc;
             p.part0 += (int)((n + p.bn / 2 - 1) / (p.bn / 2));
         }
     }
@@ -508,10 +520,11 @@ int mx_cross_entropy_bwd(const bdr_config_t* cfg_a, const bdr_planes_t* a, const
     const Largest largest = {dloss, targets, M, V, reinterpret_cast<float*>(ws + s.largest)};
     __nv_bfloat16 *const wa = reinterpret_cast<__nv_bfloat16*>(ws + s.a), *const ww = reinterpret_cast<__nv_bfloat16*>(ws + s.w);
     const bool f8 = fused::takes_f8(cfg_a->m, cfg_w->m, M, V, V, K);
+    const bool beside = fused::one_chain(cfg_a->m, cfg_w->m, (K + kBK - 1) / kBK);  // (else the product leaves no registers for the decoding)
     for (int64_t v = 0; v < V; v += s.piece) {
         const int64_t cols = std::min(s.piece, V - v);
         const bdr_planes_t lines = lines_from(*w, v);
-        const int64_t part = f8 ? cols : part_columns(M, cols, K);
+        const int64_t part = f8 || !beside ? cols : part_columns(M, cols, K);
         if ((rc = decode_pair(*a, cfg_a->m, v == 0 ? M : 0, wa, lines, cfg_w->m, part, ww, K, s.pitch_k, st, nullptr, p.counters, s.n_counters, false,
                               v == 0 ? &largest : nullptr)))
             return rc;
@@ -527,7 +540,7 @@ int mx_cross_entropy_bwd(const bdr_config_t* cfg_a, const bdr_planes_t* a, const
                 return rc;
             if (part < cols && (rc = set_piece(p, M, K, v + c, n, s.pitch_k, ws + s.a, ws + s.w + c * s.pitch_k * 2, f8))) return rc;
             p.d = fused::make_rows(ws + s.d + c * 2, s.piece, false);
-            if ((rc = fused::launch<EntropyJob<true>>(p, st))) return rc;
+            if ((rc = launch_piece<true>(p, cfg_a->m, cfg_w->m, st))) return rc;
         }
         g.N = cols;
         g.dw = dw ? static_cast<char*>(dw) + v * ld_dw * width : nullptr;

@@ -14,17 +14,19 @@
 //   load(p, it, kk, rank, dst, bar)   TMA loads of K step kk: A at dst, B kOperandBytes behind it, 16384 + 64 bn bytes in all
 //   a_mn(it), b_mn                 whether an operand lies with its rows (M or N) contiguous instead of K
 //   kSpan                          K steps after which the accumulator is handed to the epilogue: 0 = at the end of the item
-//   epilogue(p, it, e)             (kSpan == 0) reads the accumulator through e.tmem
-//   finish(p, it, e, v)            (kSpan > 0) the same, with the sums of a thread's row and half of the columns in registers
+//   kBack                          (kSpan > 0) the total of the spans goes back to tensor memory; else it stays in registers
+//   epilogue(p, it, e)             (kSpan == 0 or kBack) reads the accumulator through e.tmem
+//   finish(p, it, e, v)            (kSpan > 0, not kBack) the same, with the sums of a thread's row and half of the columns in registers
 //   prefetch(p)                    the tensor maps that load() uses
 //   kCut                           whether a tile's K steps may be cut into p.splits items (Item::tile, Item::split): the parts' sums go to
 //                                  p.partials, and the warp that comes last (p.counters) adds them in order, puts the total back into its tensor
-//                                  memory and runs the epilogue; it needs rows(p), chunks(bn, half) and chunk(bn, half, i), the 32-column pieces of
-//                                  the accumulator that the epilogue of a half reads
+//                                  memory and runs the epilogue
+//   rows(p), chunks(bn, half), chunk(bn, half, i)   (kCut or kBack) the rows that are there, and the 32-column pieces of the accumulator that the
+//                                  epilogue of a half reads, four at most
 // The tensor core cuts its fp32 additions off instead of rounding them, toward zero: over a chain of n instructions of 16 K each the sum
-// loses about n 2^-25 of itself.  That is nothing beside 16-bit results, nor for operands of few bits, whose sums are mostly exact; sums
-// of full-width values for 32-bit results are taken kSpan steps at a time and added with rounded additions in the epilogue's registers,
-// while the next span runs.
+// loses up to n 2^-25 of itself.  That is nothing beside 16-bit results.  Sums of full-width values for 32-bit results are taken kSpan steps at a
+// time and added with rounded additions in the epilogue's registers, while the next span runs.  Products of packed values are sums of 4 to 14
+// bits times powers of two, exact as long as 24 bits hold the sum: one_chain says up to where.
 #pragma once
 
 #include <algorithm>
@@ -139,7 +141,7 @@ __device__ __forceinline__ bool last_part(const typename Job::Params& p, const t
 
 template <class Job>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_gemm_kernel(const __grid_constant__ typename Job::Params p) {
-    static_assert(Job::kSpan == 0 || !Job::kCut, "spans are added in registers, not in tensor memory");
+    static_assert(Job::kSpan == 0 || Job::kBack || !Job::kCut, "the parts of a cut tile are read from tensor memory");
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t* stages = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     uint8_t* const tiles = stages + kStages * kStageBytes;
@@ -290,9 +292,50 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) fused_g
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(&bars.tmem_empty[buf], 0);
             };
-            if constexpr (Job::kSpan == 0) {
+            if constexpr (Job::kSpan == 0 || Job::kBack) {
+                if constexpr (Job::kSpan > 0) {
+                    const int n = Job::chunks(p.bn, e.half);
+                    float v[4][32];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[q][j] = 0.f;
+                    auto take = [&](uint32_t from) {
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) {  // sixteen columns at a time, as below
+                            if (q >= 2 * n) break;
+                            uint32_t u[16];
+                            tmem_ld16(from + (uint32_t)(Job::chunk(p.bn, e.half, q >> 1) + 16 * (q & 1)), u);
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) v[q >> 1][16 * (q & 1) + j] += __uint_as_float(u[j]);
+                        }
+                    };
+                    for (int k0 = Job::kSpan; k0 < item.steps; k0 += Job::kSpan) {
+                        const int buf = tcount & 1;
+                        if (!next(buf)) break;
+                        take(tmem_base + my_lanes + (uint32_t)buf * 256u);
+                        done(buf);
+                        ++tcount;
+                    }
+                    if (!ok) break;
+                    if (!next(tcount & 1)) break;
+                    if (item.steps > Job::kSpan) {  // the last span's sums give way to the total
+                        const uint32_t last = tmem_base + my_lanes + (uint32_t)(tcount & 1) * 256u;
+                        take(last);
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            if (q >= n) break;
+                            uint32_t u[32];
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) u[j] = __float_as_uint(v[q][j]);
+                            __syncwarp();
+                            tmem_st32(last + (uint32_t)Job::chunk(p.bn, e.half, q), u);
+                        }
+                    }
+                } else {
+                    if (!next(tcount & 1)) break;
+                }
                 const int buf = tcount & 1;
-                if (!next(buf)) break;
                 e.tmem = tmem_base + my_lanes + (uint32_t)buf * 256u;
                 bool mine = true;
                 if constexpr (Job::kCut) {
@@ -552,6 +595,15 @@ __device__ __forceinline__ void store_parts(const Epi& e, const Rows& d, int64_t
         store_tile(e, d, i * part_rows + row, col, rows, 32, v);
     }
 }
+
+// Whether the products of formats with m_a and m_w magnitude bits may be summed in one chain of that many K steps: as long as 24 bits hold the sum of
+// products of one size, or the chain is short; else they are taken kBackSpan steps at a time.  Largest relative error of 32-bit results whose terms have
+// one sign, in one chain, in spans, and of plain fp32 sums: MX9 x MX9 of 4096 K 3.1e-6, 4.6e-7, 3.1e-6, of 8192 8.8e-6, 3.7e-7, 5.9e-6, of 16384 2.8e-5,
+// 3.7e-7, 1e-5; with a hundredth of the channels, the first, 64 times as large as the others 7.2e-6, 3e-6, 5.5e-6; 2.2e-5, 2.9e-6, 8.8e-6; 7e-5, 4.5e-6,
+// 1.3e-5.  MX9 x MX6 of 8192 K in one chain 2.2e-7 (plain 2.8e-7), with the large channels 1.6e-6 (1.4e-6); MX6 x MX6 is exact there.  Spans cost 1 %
+// (4096 x 32000 x 4096 693 -> 699 us, 4096 x 4096 x 4096 gated 189 -> 190), 16 steps 3 %.
+constexpr int kBackSpan = 32;
+inline bool one_chain(int m_a, int m_w, int64_t steps) { return steps <= kBackSpan || steps * kBK << (m_a + m_w) <= 1ll << 24; }
 
 // How a product of tiles_m x cols is shared out: the accumulator's columns (cols_div of them for each of the product's) and the items that a
 // tile's K steps are cut into.  Measured, a step takes about 650, 527, 370 and 340 clocks at 256, 192, 128 and 64 columns when all clusters are at it (the SMs'

@@ -44,7 +44,7 @@ struct GatedJob {
     struct Item { int steps, tm, tn, tile, split; };
     static constexpr bool b_mn = false;
     static constexpr int kSpan = 0;
-    static constexpr bool kCut = true;
+    static constexpr bool kCut = true, kBack = false;
     static __device__ __forceinline__ int rows(const Params& p) { return p.M; }
     // half of the accumulator is the gate, whose pieces of 32 columns the two halves of the warps take in turn
     static __device__ __forceinline__ int chunks(int bn, int half) { return 2 * ((bn / 64 + 1 - half) / 2); }
@@ -133,6 +133,13 @@ struct GatedJob {
             one_tile(p, e, row, col, rows, n, g, u);
         }
     }
+};
+
+// for 32-bit results, where one chain of additions would lose bits of them
+template <bool GRAD>
+struct GatedJobInSpans : GatedJob<GRAD> {
+    static constexpr int kSpan = fused::kBackSpan;
+    static constexpr bool kBack = true;
 };
 
 // dG and dU from the stored products.  A thread keeps its eight columns and walks down the rows, two at a time.  Bound by memory (bf16: 6 bytes in, 4 out
@@ -316,6 +323,7 @@ int mx_gated_gemm(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bdr_co
     if ((rc = decode_pair(*a, cfg_a->m, M, reinterpret_cast<__nv_bfloat16*>(ws + s.a), *w, cfg_w->m, 2 * N, reinterpret_cast<__nv_bfloat16*>(ws + s.w), K,
                           s.pitch_k, st, p.gate, p.counters, s.n_counters)))
         return rc;
+    if (dt == BDR_F32 && !fused::one_chain(cfg_a->m, cfg_w->m, p.span)) return fused::launch<GatedJobInSpans<false>>(p, st);
     return fused::launch<GatedJob<false>>(p, st);
 }
 
@@ -377,7 +385,8 @@ int mx_gated_gemm_bwd(const bdr_config_t* cfg_a, const bdr_planes_t* a, const bd
             if ((rc = fused::encode_f8(*a, cfg_a->m, M, *w, cfg_w->m, 2 * N, 2, K, ws + s.f8, reinterpret_cast<int*>(ws + s.flag), &p.f8, &p.gate, st))) return rc;
             if ((rc = fused::launch_f8<GatedJob<true>>(p, st))) return rc;
         }
-        if ((rc = fused::launch<GatedJob<true>>(p, st))) return rc;
+        rc = f32 && !fused::one_chain(cfg_a->m, cfg_w->m, p.span) ? fused::launch<GatedJobInSpans<true>>(p, st) : fused::launch<GatedJob<true>>(p, st);
+        if (rc) return rc;
     }
     GradProducts g = {};
     g.d = d; g.a = wa; g.w = ww;

@@ -56,7 +56,7 @@ struct GradJob {
         int split, k0;           // first K step
     };
     static constexpr bool b_mn = true;
-    static constexpr bool kCut = false;
+    static constexpr bool kCut = false, kBack = false;
     static __device__ __forceinline__ void prefetch(const Params& p) { prefetch_map(&p.d_k); prefetch_map(&p.d_mn); prefetch_map(&p.w); prefetch_map(&p.a); }
     static constexpr int kSpan = F32 ? 4 : 0;  // 16 instructions in a chain (32: 4 % faster; 2.6e-7 of a result lost, 5e-7 with 32)
     static __device__ __forceinline__ bool a_mn(const Item& it) { return it.seg >= 0; }
