@@ -7,7 +7,7 @@
 // products of mx_grad_gemm.cu; dA is summed over the pieces in fp32, in order.
 //
 // The epilogue's exponentials (one per logit and SM at a time: 16 a clock) take a tenth of the product's time at K = 4096 and run beside it.  Measured: 4096 x 32000 x
-// 4096 forward, MX9 4 x 160 us = 1680 TFLOP/s and 30 us of decoding that nothing hides, MX6 on the 8-bit path 337 us = 3190 TFLOP/s; the same with d written 369 us.
+// 4096 forward, MX9/MX6 4 x 160 us = 1680 TFLOP/s and 30 us of decoding that nothing hides, MX6 on the 8-bit path 337 us = 3190 TFLOP/s; the same with d written 369 us.
 #include <algorithm>
 
 #include "mx_frag.cuh"
@@ -277,11 +277,13 @@ int64_t piece_columns(int64_t V, int64_t most) {
 }
 constexpr int64_t kMostWeights = 512ll << 20;   // bytes of decoded weights at a time
 constexpr int64_t kMostD = 256ll << 20;         // bytes of d at a time
-// Columns of a piece that are decoded, and multiplied, at a time: a large piece goes in four parts, each decoded beside the product of the one before
-// (4096 x 32000 x 4096 MX9: 692 us in one part, 682 in four; 837 and 818 in a long run).  A part has more tiles than there are clusters, twice over.
+// Columns of a piece that are decoded, and multiplied, at a time: a large piece of long lines goes in four parts, each decoded beside the product of the one
+// before (in one part and in four, in us, and in a long run: 4096 x 32000 x 4096 MX9/MX6 715 and 696, 753 both; of 2048 K MX9 386 and 389, 397 and 407;
+// 2048 x 50000 x 1000 MX9/MX4 187 and 200, 161 and 168).  A part has more tiles than there are clusters, twice over.
+constexpr int64_t kLeastBesideK = 4096;
 int64_t part_columns(int64_t M, int64_t cols, int64_t K) {
     const int64_t part = round_up((cols + 3) / 4, 256);  // (more than there are, of fewer than 256 columns)
-    return part < cols && cols * K >= 1ll << 25 && ((M + 255) / 256) * (part / 256) >= 4 * fused::kClusters / 2 ? part : cols;
+    return part < cols && K >= kLeastBesideK && cols * K >= 1ll << 25 && ((M + 255) / 256) * (part / 256) >= 4 * fused::kClusters / 2 ? part : cols;
 }
 
 struct EntropySpace {

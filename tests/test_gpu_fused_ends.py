@@ -91,3 +91,30 @@ def test_small_losses_beside_large_logits(m, v, below):
     # a sum just above 1: what its additions round off, as in fused_helpers.entropy, exponentials within 2^-21 of themselves, and the logarithm
     f.check(loss, want, (160 + v / 128) * 2.0 ** -24 + 2.0 ** -20 * want, "loss")
     f.check(lse, 1024 + want, 2.0 ** -23 * (1024 + want), "lse")
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_columns_decoded_beside_a_product(dtype):
+    # a vocabulary of long lines that is decoded in four parts; the last part is ragged
+    m, v, k = 2100, 18100, 4100
+    gen = torch.Generator(device="cuda").manual_seed(22)
+    (pa, a), (pw, w) = f.packed(bdr.MX9, torch.randn(m, k, device="cuda", generator=gen)), f.packed(bdr.MX6, torch.randn(v, k, device="cuda", generator=gen) * k ** -0.5)
+    targets = torch.randint(0, v, (m,), device="cuda", generator=gen)
+    targets[:5] = torch.tensor([0, v - 1, 4608, 9215, -100], device="cuda")
+    dloss = torch.full((m,), 1.0 / m, device="cuda")
+    runs = []
+    for _ in range(2):
+        loss, lse = torch.empty(m, device="cuda"), torch.empty(m, device="cuda")
+        bdr.mx_cross_entropy(bdr.MX9, pa, bdr.MX6, pw, m, v, k, targets, loss, lse, f.workspace(bdr.mx_cross_entropy_workspace_bytes(m, v, k)))
+        da, dw = torch.empty(m, k, device="cuda", dtype=dtype), torch.empty(v, k, device="cuda", dtype=dtype)
+        ws = f.workspace(bdr.mx_cross_entropy_bwd_workspace_bytes(m, v, k, dtype))
+        bdr.mx_cross_entropy_bwd(bdr.MX9, pa, bdr.MX6, pw, m, v, k, targets, lse, dloss, da, dw, ws)
+        runs.append((loss, lse, da, dw))
+    assert all(torch.equal(x, y) for x, y in zip(*runs))
+    loss, lse, da, dw = runs[0]
+    want, want_lse, _, eloss, else_, _ = f.entropy(a, w, targets)
+    f.check(lse, want_lse, else_, "lse")
+    f.check(loss, want, eloss, "loss")
+    want_a, want_w, ea, ew = f.entropy_grads(a, w, targets, lse.double(), dloss.double(), dtype)
+    f.check(da, want_a, ea, "da")
+    f.check(dw, want_w, ew, "dw")
